@@ -25,6 +25,12 @@
  *     next call that synchronises (ace_last_skip_mask, ace_layer_sync).
  *   - One forward may be in flight per layer at a time; calls on different
  *     layers are independent.
+ *
+ * The second half of the header is the rest of a speculative decode step around
+ * the MoE layers: a paged key/value cache that is quantised as it is written
+ * (ace_kv_*), attention for trees of drafted tokens over it (ace_tree_*) and the
+ * verification of the drafted tokens (ace_verify_tree). The paper has no
+ * counterpart for these; their formulas stand at each call.
  */
 #ifndef ACE_H
 #define ACE_H
@@ -369,6 +375,167 @@ ace_status ace_offline_tables_device(int d, int N, int m, const void* gamma, con
 
 /* Fills *desc with the layer's descriptor (after defaults were applied). */
 ace_status ace_layer_get_desc(const ace_layer* layer, ace_layer_desc* desc);
+
+/* ===================================================================== *
+ * Speculative decode step                                               *
+ * ===================================================================== *
+ *
+ * A request b has a committed prefix of lens[b] tokens in the cache and, in a
+ * step, a tree of n_b nodes (n_b = node_offsets[b + 1] - node_offsets[b]): node
+ * 0 is the last committed token, whose K and V the step computes, the others
+ * are drafted tokens, each after its parent. Rows of all requests' nodes are
+ * packed: node i of request b is row node_offsets[b] + i of q, out, logits and
+ * so on. One drafted chain, a plain decode step (n_b = 1) and a chunk of a
+ * prompt are trees too.
+ *
+ *   ace_kv_write        the nodes' K and V go to positions lens[b] + i
+ *   ace_tree_attention  every node attends to the prefix and its ancestors
+ *   (MoE layers: ace_moe_forward on the packed rows)
+ *   ace_verify_tree     which nodes are accepted, and the next token
+ *   ace_kv_keep         the accepted nodes' rows move to positions lens[b] + 0, 1, ..
+ *
+ * Cache memory belongs to the caller. With H = n_kv_heads, P = page_size, D = head_dim:
+ *   pool   [layers, n_pages, H, P, D]   K and V each; position p of request b is row
+ *          p % P of page page_table[b, p / P]; slot = page * P + row
+ *   scale  [layers, n_pages, H, P] uint8, format ACE_KV_FP8 only
+ * ACE_KV_PLAIN keeps rows in dtype. ACE_KV_FP8 keeps e4m3 codes: with e the
+ * smallest integer >= -126 such that the row's largest finite |x| <= 448 * 2^e,
+ * scale = e + 127 and code = x * 2^-e rounded to nearest even (NaN and
+ * infinities to e4m3's NaN); a code stands for code * 2^e. A power of two
+ * loses nothing against 448 / max |x|: a float's rounding is relative, and
+ * scaling is exact in both directions.
+ */
+typedef enum ace_kv_format { ACE_KV_PLAIN = 0, ACE_KV_FP8 = 1 } ace_kv_format;
+
+typedef struct ace_kv_desc {
+    int layers;          /* >= 1 */
+    int n_pages;         /* >= 1, pages per layer */
+    int page_size;       /* tokens per page: 16, 32, 64, 128 or 256 */
+    int n_kv_heads;      /* >= 1 */
+    int head_dim;        /* multiple of 8, <= 256 */
+    int dtype;           /* ace_dtype of k, v, q and out */
+    int format;          /* ace_kv_format */
+} ace_kv_desc;
+
+typedef struct ace_kv ace_kv;   /* opaque */
+
+/*
+ * ace_kv_create - a handle over caller-owned cache memory on the current device.
+ *   k_pool, v_pool    device, 16-byte aligned; they must outlive the handle
+ *   k_scale, v_scale  device; ACE_KV_FP8 only (ignored otherwise)
+ * The pools' contents are not touched: rows that no call wrote may hold
+ * anything, NaN included. Allocates the attention's workspace (tens of MB);
+ * the calls below allocate nothing, are asynchronous on `stream` and can be
+ * captured in a CUDA graph. One call may be in flight per handle at a time.
+ * Indices in device memory (slots, pages, lengths, offsets, paths) are checked
+ * by the kernels: what points outside is left out, and the next ace_kv_sync
+ * returns ACE_ERR_INVALID_ARG.
+ * Errors: INVALID_ARG (NULL, sizes, alignment), UNSUPPORTED (page_size, head_dim,
+ * more than 2^31 - 1 rows layers * n_pages * H * P), OOM, CUDA.
+ */
+ace_status ace_kv_create(const ace_kv_desc* desc, void* k_pool, void* v_pool, void* k_scale, void* v_scale,
+                         void* stream, ace_kv** out_kv);
+/* Frees the handle and its workspace (not the pools). NULL is a no-op. Synchronises the device. */
+void ace_kv_destroy(ace_kv* kv);
+/* Waits for the handle's last stream and reports errors that its kernels found. */
+ace_status ace_kv_sync(ace_kv* kv);
+
+/*
+ * ace_kv_write - quantise (or copy) T tokens' rows into one layer of the cache.
+ *   k, v    device, dtype: head h of token t starts at k + t * k_token_stride +
+ *           h * k_head_stride elements and is contiguous (any stride >= 0)
+ *   slots   [T] int64 device: slot of each token, negative to leave it out; a slot
+ *           that two tokens name holds either one's row
+ * Errors: INVALID_ARG (NULL, layer, T < 0, negative stride).
+ */
+ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_stride, long long k_head_stride,
+                        const void* v, long long v_token_stride, long long v_head_stride, const int64_t* slots, int T,
+                        void* stream);
+
+/*
+ * ace_kv_read - the rows at `slots` [T] as dtype values (code * 2^e rounded to dtype).
+ *   layer         0 .. layers - 1, or -1 for all of them
+ *   k_out, v_out  [T, H, D] (layer -1: [layers, T, H, D]), contiguous, 16-byte aligned;
+ *                 a negative slot gives zeros
+ */
+ace_status ace_kv_read(ace_kv* kv, int layer, const int64_t* slots, int T, void* k_out, void* v_out, void* stream);
+
+/*
+ * ace_kv_keep - after verification, in all layers: the rows of nodes path[b, 0 .. n_keep[b])
+ * move, codes and scales as they are, to positions lens[b] + 0, 1, .. of their request.
+ *   page_table [B, max_pages] int32, lens [B] int32, path [B, max_nodes] int32
+ *   (strictly increasing within a request, as a path from the root is), n_keep [B] int32
+ *   new_lens   [B] int32 out: lens[b] + n_keep[b]; not lens itself; may be NULL
+ * A request whose path is not increasing or leaves its pages is left out and keeps its length
+ * (error, see ace_kv_create). Errors: INVALID_ARG; UNSUPPORTED for layers * H > 65535.
+ */
+ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, const int32_t* lens, const int32_t* path,
+                       int max_nodes, const int32_t* n_keep, int B, int32_t* new_lens, void* stream);
+
+/*
+ * ace_tree_mask - ancestor masks and depths of trees given by their parents.
+ *   parents      [T] int32 device: a node's parent as its index in the request, below its own;
+ *                anything else (-1 for node 0) counts as no parent
+ *   node_offsets [B + 1] int32 device, non-decreasing, last one T
+ *   mask         [T, W] uint64 out, W = ceil(max_nodes / 64): bit m of a node's words says
+ *                that it sees node m (itself and its ancestors)
+ *   depth        [T] int32 out: number of ancestors (so position lens[b] + depth); may be NULL
+ * Errors: INVALID_ARG (NULL, B < 0, max_nodes outside 1..256). Requests with more than
+ * max_nodes nodes are left out.
+ */
+ace_status ace_tree_mask(const int32_t* parents, const int32_t* node_offsets, int B, int max_nodes, uint64_t* mask,
+                         int32_t* depth, void* stream);
+
+/*
+ * ace_tree_attention - with G = n_heads / H, for row t (node i of request b) and head q,
+ *   s_p = scale * q[t, q] . k_p, kv head q / G, over the positions p < lens[b] and
+ *         p = lens[b] + m for every m < n_b whose bit is set in mask[t]
+ *   out[t, q] = sum_p softmax(s)_p v_p,   lse[t, q] = log sum_p exp(s_p)
+ * A position that a row does not see never matters, whatever it holds. A row that
+ * sees nothing gives zeros and lse = -inf.
+ *   q     device, dtype: head q of row t at q + t * q_token_stride + q * q_head_stride
+ *   mask  [T, ceil(max_nodes / 64)] uint64; NULL: node i sees nodes 0 .. i (a chain)
+ *   out   [T, n_heads, D] dtype, contiguous, 16-byte aligned; lse [T, n_heads] float32 or NULL
+ *   T     rows of q and out, node_offsets[B]; max_nodes bounds every n_b
+ * Scores, softmax and sums are fp32. bf16 caches round the softmax weights to bf16 for the
+ * tensor cores, fp8 caches to fp16. The work is split over the long axis by the lengths, in an
+ * order that depends on them alone: the same call gives the same bits.
+ * Errors: INVALID_ARG (NULL, layer, n_heads no multiple of H, max_nodes outside 1..256, scale not
+ * finite, misaligned out).
+ */
+ace_status ace_tree_attention(ace_kv* kv, int layer, const void* q, long long q_token_stride, long long q_head_stride,
+                              int n_heads, const int32_t* page_table, int max_pages, const int32_t* lens,
+                              const int32_t* node_offsets, const uint64_t* mask, int B, int T, int max_nodes,
+                              float scale, void* out, float* lse, void* stream);
+
+/*
+ * ace_verify_tree - lossless verification of the drafted tokens (speculative sampling
+ * without replacement). At a node, beginning with node 0, r = softmax(logits / temperature)
+ * and q = the node's row of draft_probs. Its children, in index order, each with token x
+ * and number u: accepted when r(x) > 0 and u * q(x) <= r(x), and the walk goes on there;
+ * else r becomes max(r - q, 0), renormalised (r stays where that is zero everywhere), and q loses
+ * x, renormalised. Where no child is accepted the next token is argmax_v r(v) / noise(v)
+ * over r(v) > 0, lowest index on ties: a sample of r when the noise is exponential.
+ * With draft_probs NULL, q is 1 at the child's token (trees that were not sampled).
+ * Temperature 0 accepts the child that is the argmax (lowest index on ties).
+ *   logits       [T, vocab] ACE_BF16 or ACE_F32 device, rows logits_stride elements apart
+ *   tokens, parents [T] int32 (tokens of nodes 0 are not read; parents as ace_tree_mask takes them)
+ *   draft_probs  [T, vocab] float32, rows draft_stride apart, or NULL; rows of nodes with children are read
+ *   temperature  [B] float32 >= 0, or NULL for 1
+ *   uniforms     [T] float32 in [0, 1): u of each drafted node
+ *   noise        [B, vocab] float32 > 0, rows noise_stride apart
+ *   path         [B, max_nodes] int32 out: node 0 and the accepted nodes, then -1
+ *   n_keep       [B] int32 out: length of the path (0 for a request without nodes)
+ *   next_token   [B] int32 out; -1 for a request without nodes, and where a visited row has a
+ *                NaN, a +inf or no finite logit (the walk ends there). -inf is a filtered token.
+ * A drafted token outside the vocabulary is never accepted.
+ * Errors: INVALID_ARG (NULL, dtype, vocab < 1, strides < vocab, max_nodes outside 1..256), CUDA.
+ */
+ace_status ace_verify_tree(const void* logits, int dtype, long long logits_stride, int vocab, const int32_t* tokens,
+                           const int32_t* parents, const int32_t* node_offsets, int B, int T, int max_nodes,
+                           const float* draft_probs, long long draft_stride, const float* temperature,
+                           const float* uniforms, const float* noise, long long noise_stride, int32_t* path,
+                           int32_t* n_keep, int32_t* next_token, void* stream);
 
 const char* ace_status_string(ace_status status);
 const char* ace_last_error_message(void);

@@ -20,6 +20,7 @@ LIBPATH = os.path.join(_LIBDIR, LIBNAME)
 
 ACE_BF16, ACE_F32 = 0, 1
 ACE_SKIP_THRESHOLD, ACE_SKIP_RATIO = 0, 1
+ACE_KV_PLAIN, ACE_KV_FP8 = 0, 1
 # Skip rules (ace_fusion): index = enum value. "max" is ACE.
 FUSIONS = ("max", "min", "mean", "gsp", "rcr", "score")
 ACE_FUSION_MAX, ACE_FUSION_MIN, ACE_FUSION_MEAN, ACE_FUSION_GSP, ACE_FUSION_RCR, ACE_FUSION_SCORE = range(6)
@@ -44,9 +45,17 @@ class ace_skip_ctl(ctypes.Structure):
     _fields_ = [("mode", ctypes.c_int), ("value", ctypes.c_float), ("fusion", ctypes.c_int)]
 
 
+class ace_kv_desc(ctypes.Structure):
+    _fields_ = [("layers", ctypes.c_int), ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("format", ctypes.c_int)]
+
+
 _lib = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
+_LL = ctypes.c_longlong
+_F = ctypes.c_float
 _S = ctypes.c_int  # ace_status
 
 
@@ -85,6 +94,15 @@ def lib() -> ctypes.CDLL:
             "ace_stack_forward_host": (_S, [_P, _P, _P, _I, ace_skip_ctl, _P]),
             "ace_offline_tables_device": (_S, [_I, _I, _I, _P, _P, _P, _P, _P, ctypes.c_double, _I, ctypes.c_size_t,
                                                _P, _P, _P]),
+            "ace_kv_create": (_S, [ctypes.POINTER(ace_kv_desc), _P, _P, _P, _P, _P, ctypes.POINTER(_P)]),
+            "ace_kv_destroy": (None, [_P]),
+            "ace_kv_sync": (_S, [_P]),
+            "ace_kv_write": (_S, [_P, _I, _P, _LL, _LL, _P, _LL, _LL, _P, _I, _P]),
+            "ace_kv_read": (_S, [_P, _I, _P, _I, _P, _P, _P]),
+            "ace_kv_keep": (_S, [_P, _P, _I, _P, _P, _I, _P, _I, _P, _P]),
+            "ace_tree_mask": (_S, [_P, _P, _I, _I, _P, _P, _P]),
+            "ace_tree_attention": (_S, [_P, _I, _P, _LL, _LL, _I, _P, _I, _P, _P, _P, _I, _I, _I, _F, _P, _P, _P]),
+            "ace_verify_tree": (_S, [_P, _I, _LL, _I, _P, _P, _P, _I, _I, _I, _P, _LL, _P, _P, _P, _LL, _P, _P, _P, _P]),
             "ace_status_string": (ctypes.c_char_p, [_S]),
             "ace_last_error_message": (ctypes.c_char_p, []),
         }
@@ -276,6 +294,205 @@ def ace_layer_get_desc(layer: int) -> ace_layer_desc:
     d = ace_layer_desc()
     _check(lib().ace_layer_get_desc(layer, ctypes.byref(d)))
     return d
+
+
+# --------------------------------------------------------------------------
+# Speculative decode step: the cache, attention for trees of drafted tokens, verification
+# --------------------------------------------------------------------------
+
+def ace_kv_create(desc: ace_kv_desc, k_pool, v_pool, k_scale=None, v_scale=None, stream=None) -> int:
+    out = _P()
+    _check(lib().ace_kv_create(ctypes.byref(desc), _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale),
+                               _stream(stream), ctypes.byref(out)))
+    return out.value
+
+
+def ace_kv_destroy(kv: int) -> None:
+    if kv:
+        lib().ace_kv_destroy(kv)
+
+
+def ace_kv_sync(kv: int) -> None:
+    _check(lib().ace_kv_sync(kv))
+
+
+def ace_kv_write(kv: int, layer: int, k, k_token_stride: int, k_head_stride: int, v, v_token_stride: int,
+                 v_head_stride: int, slots, T: int, stream=None) -> None:
+    _check(lib().ace_kv_write(kv, layer, _ptr(k), k_token_stride, k_head_stride, _ptr(v), v_token_stride, v_head_stride,
+                              _ptr(slots), T, _stream(stream)))
+
+
+def ace_kv_read(kv: int, layer: int, slots, T: int, k_out, v_out, stream=None) -> None:
+    _check(lib().ace_kv_read(kv, layer, _ptr(slots), T, _ptr(k_out), _ptr(v_out), _stream(stream)))
+
+
+def ace_kv_keep(kv: int, page_table, max_pages: int, lens, path, max_nodes: int, n_keep, B: int, new_lens=None,
+                stream=None) -> None:
+    _check(lib().ace_kv_keep(kv, _ptr(page_table), max_pages, _ptr(lens), _ptr(path), max_nodes, _ptr(n_keep), B,
+                             _ptr(new_lens), _stream(stream)))
+
+
+def ace_tree_mask(parents, node_offsets, B: int, max_nodes: int, mask, depth=None, stream=None) -> None:
+    """Ancestor masks [T, ceil(max_nodes / 64)] (64-bit words) and depths of trees given by parents."""
+    _check(lib().ace_tree_mask(_ptr(parents), _ptr(node_offsets), B, max_nodes, _ptr(mask), _ptr(depth), _stream(stream)))
+
+
+def ace_tree_attention(kv: int, layer: int, q, q_token_stride: int, q_head_stride: int, n_heads: int, page_table,
+                       max_pages: int, lens, node_offsets, mask, B: int, T: int, max_nodes: int, scale: float, out,
+                       lse=None, stream=None) -> None:
+    _check(lib().ace_tree_attention(kv, layer, _ptr(q), q_token_stride, q_head_stride, n_heads, _ptr(page_table), max_pages,
+                                    _ptr(lens), _ptr(node_offsets), _ptr(mask), B, T, max_nodes, scale, _ptr(out),
+                                    _ptr(lse), _stream(stream)))
+
+
+def _want(name: str, t, dtype: str, shape=None, contiguous: bool = True):
+    """Checks a torch tensor argument: its type, shape (None: any size) and layout."""
+    if str(t.dtype) != "torch." + dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and (t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape))):
+        raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a GPU")
+
+
+def ace_verify_tree(logits, tokens, parents, node_offsets, max_nodes: int, uniforms, noise, path, n_keep, next_token,
+                    draft_probs=None, temperature=None, stream=None) -> None:
+    """Verification of drafted tokens (torch tensors; layouts in include/ace.h): fills path [B, max_nodes],
+    n_keep [B] and next_token [B] (int32). logits and draft_probs [T, vocab] and noise [B, vocab] may have padded rows."""
+    T, V = logits.shape
+    B = node_offsets.shape[0] - 1
+    dt = {"torch.bfloat16": ACE_BF16, "torch.float32": ACE_F32}.get(str(logits.dtype))
+    if dt is None:
+        raise ValueError(f"logits must be bfloat16 or float32, not {logits.dtype}")
+    _want("logits", logits, str(logits.dtype)[6:], (T, V), False)
+    _want("noise", noise, "float32", (B, V), False)
+    _want("uniforms", uniforms, "float32", (T,))
+    if draft_probs is not None:
+        _want("draft_probs", draft_probs, "float32", (T, V), False)
+    if temperature is not None:
+        _want("temperature", temperature, "float32", (B,))
+    for name, t, shape in (("tokens", tokens, (T,)), ("parents", parents, (T,)), ("node_offsets", node_offsets, (B + 1,)),
+                           ("path", path, (B, max_nodes)), ("n_keep", n_keep, (B,)), ("next_token", next_token, (B,))):
+        _want(name, t, "int32", shape)
+    for name, t in (("logits", logits), ("noise", noise), ("draft_probs", draft_probs)):
+        if t is not None and t.shape[0] and t.stride(1) != 1 and V > 1:
+            raise ValueError(f"the rows of {name} must be contiguous")
+    _check(lib().ace_verify_tree(logits.data_ptr(), dt, max(V, logits.stride(0)), V, tokens.data_ptr(), parents.data_ptr(),
+                                 node_offsets.data_ptr(), B, T, max_nodes, _ptr(draft_probs),
+                                 max(V, draft_probs.stride(0)) if draft_probs is not None else V, _ptr(temperature),
+                                 uniforms.data_ptr(), noise.data_ptr(), max(V, noise.stride(0)), path.data_ptr(),
+                                 n_keep.data_ptr(), next_token.data_ptr(), _stream(stream)))
+
+
+class AceKvCache:
+    """A paged key/value cache of a model's layers and its ace_kv handle. The pools are torch tensors:
+    those given, or new ones (zeros). fmt "plain" keeps rows in dtype, "fp8" e4m3 codes and a scale
+    byte per (token, head). Slots are page * page_size + row."""
+
+    def __init__(self, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, layers: int = 1, dtype: str = "bf16",
+                 fmt: str = "fp8", k_pool=None, v_pool=None, k_scale=None, v_scale=None, device: int = 0):
+        import torch
+
+        if dtype not in ("bf16", "f32") or fmt not in ("plain", "fp8"):
+            raise ValueError("dtype must be 'bf16' or 'f32' and fmt 'plain' or 'fp8'")
+        self.handle = None
+        self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.layers, self.n_pages, self.page_size = int(layers), int(n_pages), int(page_size)
+        self.n_kv_heads, self.head_dim = int(n_kv_heads), int(head_dim)
+        rows = (self.layers, self.n_pages, self.n_kv_heads, self.page_size)
+        dev = torch.device("cuda", device)
+        pool_dt = torch.float8_e4m3fn if fmt == "fp8" else self.torch_dtype
+
+        def own(t, shape, dt, name):
+            if t is None:
+                return torch.zeros(shape, dtype=dt, device=dev)
+            _want(name, t, str(dt)[6:], shape)
+            return t
+
+        self.k_pool = own(k_pool, rows + (self.head_dim,), pool_dt, "k_pool")
+        self.v_pool = own(v_pool, rows + (self.head_dim,), pool_dt, "v_pool")
+        self.k_scale = self.v_scale = None
+        if fmt == "fp8":
+            self.k_scale = own(k_scale, rows, torch.uint8, "k_scale")
+            self.v_scale = own(v_scale, rows, torch.uint8, "v_scale")
+        self.desc = ace_kv_desc(self.layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
+                                ACE_BF16 if dtype == "bf16" else ACE_F32, ACE_KV_FP8 if fmt == "fp8" else ACE_KV_PLAIN)
+        with torch.cuda.device(self.k_pool.device):
+            torch.cuda.synchronize()
+            self.handle = ace_kv_create(self.desc, self.k_pool, self.v_pool, self.k_scale, self.v_scale)
+
+    def _rows(self, name, t, heads):
+        """(token stride, head stride) of rows [T, heads, head_dim] of any strides but the last."""
+        _want(name, t, str(self.torch_dtype)[6:], (None, heads, self.head_dim), False)
+        if t.numel() and t.stride(2) != 1:
+            raise ValueError(f"the last axis of {name} must be contiguous")
+        return t.stride(0), t.stride(1)
+
+    def write(self, layer: int, k, v, slots, stream=None) -> None:
+        """k, v [T, n_kv_heads, head_dim] (any strides but the last) to `slots` [T] int64 of a layer."""
+        T = k.shape[0]
+        ks, vs = self._rows("k", k, self.n_kv_heads), self._rows("v", v, self.n_kv_heads)
+        if v.shape[0] != T:
+            raise ValueError("k and v must have the same tokens")
+        _want("slots", slots, "int64", (T,))
+        ace_kv_write(self.handle, layer, k, *ks, v, *vs, slots, T, stream)
+
+    def read(self, layer, slots, k_out, v_out, stream=None) -> None:
+        """The rows at `slots` [T] to k_out, v_out [T, n_kv_heads, head_dim]; layer None: of all layers,
+        [layers, T, n_kv_heads, head_dim]."""
+        T = slots.shape[0]
+        shape = (T, self.n_kv_heads, self.head_dim)
+        if layer is None:
+            layer, shape = -1, (self.layers,) + shape
+        _want("slots", slots, "int64", (T,))
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            _want(name, t, str(self.torch_dtype)[6:], shape)
+        ace_kv_read(self.handle, layer, slots, T, k_out, v_out, stream)
+
+    def keep(self, page_table, lens, path, n_keep, new_lens=None, stream=None) -> None:
+        """The rows of nodes path[b, :n_keep[b]] move to positions lens[b] + 0, 1, .. in every layer."""
+        B, max_pages = page_table.shape
+        max_nodes = path.shape[1]
+        _want("page_table", page_table, "int32")
+        _want("path", path, "int32", (B, max_nodes))
+        for name, t in (("lens", lens), ("n_keep", n_keep)) + ((("new_lens", new_lens),) if new_lens is not None else ()):
+            _want(name, t, "int32", (B,))
+        ace_kv_keep(self.handle, page_table, max_pages, lens, path, max_nodes, n_keep, B, new_lens, stream)
+
+    def attend(self, layer: int, q, page_table, lens, node_offsets, out, mask=None, max_nodes: int = 1, scale=None,
+               lse=None, stream=None) -> None:
+        """q [T, n_heads, head_dim] (any strides but the last) attends to the cached prefixes and, by
+        `mask` (int64 words, None: a chain), to the trees' nodes; out like q, contiguous; scale None: 1 / sqrt(head_dim)."""
+        T, heads = q.shape[0], q.shape[1]
+        qs = self._rows("q", q, heads)
+        B, max_pages = page_table.shape
+        _want("page_table", page_table, "int32")
+        _want("lens", lens, "int32", (B,))
+        _want("node_offsets", node_offsets, "int32", (B + 1,))
+        _want("out", out, str(self.torch_dtype)[6:], tuple(q.shape))
+        if mask is not None:
+            _want("mask", mask, "int64", (T, (max_nodes + 63) // 64))
+        if lse is not None:
+            _want("lse", lse, "float32", (T, heads))
+        ace_tree_attention(self.handle, layer, q, *qs, heads, page_table, max_pages, lens, node_offsets, mask, B, T,
+                           max_nodes, self.head_dim ** -0.5 if scale is None else scale, out, lse, stream)
+
+    def sync(self) -> None:
+        """Waits for the last call and raises AceError for what its kernels found."""
+        ace_kv_sync(self.handle)
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            ace_kv_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # --------------------------------------------------------------------------

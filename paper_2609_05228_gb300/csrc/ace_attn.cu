@@ -1,0 +1,237 @@
+// ace_attn.cu — attention for trees of drafted tokens on the CUDA cores: any dtype, format and head size
+// (the tensor-core kernel takes bf16 with head sizes 64 and 128). With G query heads per kv head, a unit
+// is 16 rows (node, head of the group) of one request and kv head; a CTA walks its share of 64-key tiles:
+//   s_j = scale q.k_j,  m = max s,  p_j = 2^(s_j - m) (base 2),  l = sum p_j,  o = sum p_j v_j
+// with m, l and o rescaled when m grows (one pass over the cache). fp32 throughout.
+#include "ace_kv_device.cuh"
+
+namespace ace {
+namespace {
+
+constexpr int kRows = 16, kKeys = 64, kThreads = 256;
+
+__host__ __device__ constexpr int pitch(int D) { return D + 4; }   // floats a row: 16-byte chunks of 8 rows in distinct banks
+int core_smem(int D) { return (2 * kKeys * pitch(D) + kRows * pitch(D) + kRows * kKeys) * 4; }
+
+// 8 elements of a cached row as floats.
+template <typename T, bool FP8>
+__device__ __forceinline__ void cached8(const void* pool, long long row, int D, int d, float (&f)[8]) {
+    if constexpr (FP8) {
+        e4m3x8_to_float(__ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + row * D + d)), f);
+    } else if constexpr (sizeof(T) == 2) {
+        Vec16<T>::to_float(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(pool) + row * D + d)), f);
+    } else {
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const T*>(pool) + row * D + d);
+        Vec16<T>::to_float(__ldg(p), f);
+        Vec16<T>::to_float(__ldg(p + 1), f + 4);
+    }
+}
+
+template <typename T, bool FP8>
+__global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ AttnArgs a) {
+    using W = Work<kRows, kKeys>;
+    extern __shared__ __align__(16) float sm[];
+    const int D = a.head_dim, P = pitch(D);
+    float* sk = sm;
+    float* sv = sk + kKeys * P;
+    float* sq = sv + kKeys * P;
+    float* sp = sq + kRows * P;
+    __shared__ Segment seg;
+    __shared__ int go, joins;
+    const int tid = threadIdx.x, row = tid >> 4, sub = tid & 15;
+    Cursor cur{};
+    bool more = false;
+    if (tid < 32) more = cursor_init<kRows, kKeys>(a, blockIdx.x, gridDim.x, cur);
+    while (true) {
+        if (tid < 32) {
+            Segment s;
+            const bool ok = more && cursor_next<kRows, kKeys>(a, blockIdx.x, cur, s);
+            if (tid == 0) {
+                go = ok;
+                if (ok) seg = s;
+            }
+        }
+        __syncthreads();
+        if (!go) break;
+        const Segment s = seg;
+        const bool live = row < s.rows;
+        const int node = live ? (s.row0 + row) / a.group : 0;          // of the request
+        const int hq = s.head * a.group + (s.row0 + row) % a.group;
+        // the unit's q rows, scaled to base 2
+        for (int i = tid; i < kRows * D; i += kThreads) {
+            const int r = i / D, d = i % D;
+            float v = 0.f;
+            if (r < s.rows) {
+                const int t = s.node0 + (s.row0 + r) / a.group, h = s.head * a.group + (s.row0 + r) % a.group;
+                v = to_f32(static_cast<const T*>(a.q)[t * a.q_token_stride + h * a.q_head_stride + d]) * a.scale_log2;
+            }
+            sq[r * P + d] = v;
+        }
+        float m = -INFINITY, l = 0.f;
+        float4 o[kMaxHeadDim / 64];
+#pragma unroll
+        for (int i = 0; i < kMaxHeadDim / 64; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int total = s.len + s.n;
+        for (int tile = s.tile0; tile < s.tile1; ++tile) {
+            const int pos0 = tile * kKeys;
+            // K and V rows of the tile; rows past the end are zeros
+            const int chunks = D / 8;
+            for (int i = tid; i < kKeys * chunks; i += kThreads) {
+                const int j = i / chunks, d = i % chunks * 8, pos = pos0 + j;
+                float fk[8] = {}, fv[8] = {};
+                if (pos < total) {
+                    const int page = page_of(a, s.b, pos);
+                    if (page >= 0) {
+                        const long long r = ((long long)page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
+                        cached8<T, FP8>(a.k_pool, r, D, d, fk);
+                        cached8<T, FP8>(a.v_pool, r, D, d, fv);
+                        if constexpr (FP8) {
+                            const float mk = pow2_of_byte(a.k_scale[r]), mv = pow2_of_byte(a.v_scale[r]);
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) fk[x] *= mk, fv[x] *= mv;
+                        }
+                    }
+                }
+                store8f(sk + j * P + d, fk);
+                store8f(sv + j * P + d, fv);
+            }
+            __syncthreads();
+            // thread (row, sub): scores of keys sub, sub + 16, ..
+            float sc[kKeys / 16] = {};
+            for (int d = 0; d < D; d += 4) {
+                const float4 q = *reinterpret_cast<const float4*>(sq + row * P + d);
+#pragma unroll
+                for (int i = 0; i < kKeys / 16; ++i) {
+                    const float4 k = *reinterpret_cast<const float4*>(sk + (sub + 16 * i) * P + d);
+                    sc[i] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, sc[i]))));
+                }
+            }
+            const bool drafted = pos0 + kKeys > s.len;      // holds rows that not every node sees
+            if (drafted) {
+#pragma unroll
+                for (int i = 0; i < kKeys / 16; ++i) {
+                    const int pos = pos0 + sub + 16 * i, mth = pos - s.len;
+                    if (mth >= 0 && !(sees_word(a, s.node0, s.n, node, mth >> 6) >> (mth & 63) & 1)) sc[i] = -INFINITY;
+                }
+            }
+            float top = sc[0];
+#pragma unroll
+            for (int i = 1; i < kKeys / 16; ++i) top = fmaxf(top, sc[i]);
+#pragma unroll
+            for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.f : m_new;
+            const float back = exp2f(m - ref);
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kKeys / 16; ++i) {
+                const float p = exp2f(sc[i] - ref);
+                sum += p;
+                sp[row * kKeys + sub + 16 * i] = p;
+            }
+#pragma unroll
+            for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+            l = fmaf(l, back, sum);
+            m = m_new;
+#pragma unroll
+            for (int i = 0; i < kMaxHeadDim / 64; ++i) {
+                o[i].x *= back;
+                o[i].y *= back;
+                o[i].z *= back;
+                o[i].w *= back;
+            }
+            __syncwarp();
+            // thread (row, sub): dimensions 4 sub + 64 i; a weight of zero leaves out whatever a masked row holds
+            for (int j = 0; j < kKeys; ++j) {
+                const float p = sp[row * kKeys + j];
+                if (drafted && p == 0.f) continue;
+#pragma unroll
+                for (int i = 0; i < kMaxHeadDim / 64; ++i) {
+                    const int d = 4 * sub + 64 * i;
+                    if (d < D) {
+                        const float4 v = *reinterpret_cast<const float4*>(sv + j * P + d);
+                        o[i].x = fmaf(p, v.x, o[i].x);
+                        o[i].y = fmaf(p, v.y, o[i].y);
+                        o[i].z = fmaf(p, v.z, o[i].z);
+                        o[i].w = fmaf(p, v.w, o[i].w);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        if (s.part < 0) {
+            if (live) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const long long at = (long long)(s.node0 + node) * a.n_heads + hq;
+#pragma unroll
+                for (int i = 0; i < kMaxHeadDim / 64; ++i) {
+                    const int d = 4 * sub + 64 * i;
+                    if (d < D) {
+                        T* out = static_cast<T*>(a.out) + at * D + d;
+                        out[0] = from_f32<T>(o[i].x * inv);
+                        out[1] = from_f32<T>(o[i].y * inv);
+                        out[2] = from_f32<T>(o[i].z * inv);
+                        out[3] = from_f32<T>(o[i].w * inv);
+                    }
+                }
+                if (sub == 0 && a.lse) a.lse[at] = (m + log2f(l)) * 0.69314718055994530942f;
+            }
+            __syncthreads();
+            continue;
+        }
+        if (live) {
+            const long long slot = (long long)s.part * kRows + row;
+#pragma unroll
+            for (int i = 0; i < kMaxHeadDim / 64; ++i) {
+                const int d = 4 * sub + 64 * i;
+                if (d < D) *reinterpret_cast<float4*>(a.ws.part_o + slot * D + d) = o[i];
+            }
+            if (sub == 0) a.ws.part_ml[slot] = make_float2(m, l);
+        }
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) joins = last_of_unit(a, s);
+        __syncthreads();
+        if (joins) {
+            __threadfence();
+            join_unit<T, kRows>(a, s, tid, kThreads);
+        }
+    }
+}
+
+template <typename T, bool FP8>
+cudaError_t core_attr(int D) {
+    return raise_smem_limit(k_attn_core<T, FP8>, core_smem(D));
+}
+
+}  // namespace
+
+cudaError_t attn_init(ace_kv* kv) {
+    const ace_kv_desc& D = kv->desc;
+    const bool fp8 = D.format == ACE_KV_FP8, bf = D.dtype == ACE_BF16;
+    cudaError_t e = bf ? (fp8 ? core_attr<__nv_bfloat16, true>(D.head_dim) : core_attr<__nv_bfloat16, false>(D.head_dim))
+                       : (fp8 ? core_attr<float, true>(D.head_dim) : core_attr<float, false>(D.head_dim));
+    if (e != cudaSuccess) return e;
+    const int fit = 220 * 1024 / (core_smem(D.head_dim) + 2048);
+    kv->core_ctas_per_sm = fit < 1 ? 1 : fit > 4 ? 4 : fit;
+    const size_t ctas = (size_t)kv->num_sms * kv->core_ctas_per_sm;
+    const size_t rows = 2 * ctas * kRows;
+    if ((e = cudaMalloc(&kv->ws.part_o, rows * D.head_dim * sizeof(float))) != cudaSuccess) return e;
+    if ((e = cudaMalloc(&kv->ws.part_ml, rows * sizeof(float2))) != cudaSuccess) return e;
+    if ((e = cudaMalloc(&kv->ws.ticket, ctas * sizeof(int))) != cudaSuccess) return e;
+    return cudaMemsetAsync(kv->ws.ticket, 0, ctas * sizeof(int), kv->last_stream);
+}
+
+cudaError_t launch_tree_attention(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
+    const bool fp8 = kv->desc.format == ACE_KV_FP8;
+    const int grid = kv->num_sms * kv->core_ctas_per_sm, smem = core_smem(a.head_dim);
+    if (kv->desc.dtype == ACE_BF16) {
+        if (fp8) k_attn_core<__nv_bfloat16, true><<<grid, kThreads, smem, s>>>(a);
+        else k_attn_core<__nv_bfloat16, false><<<grid, kThreads, smem, s>>>(a);
+    } else {
+        if (fp8) k_attn_core<float, true><<<grid, kThreads, smem, s>>>(a);
+        else k_attn_core<float, false><<<grid, kThreads, smem, s>>>(a);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace ace
