@@ -208,20 +208,29 @@ cudaError_t core_attr(int D) {
 cudaError_t attn_init(ace_kv* kv) {
     const ace_kv_desc& D = kv->desc;
     const bool fp8 = D.format == ACE_KV_FP8, bf = D.dtype == ACE_BF16;
-    cudaError_t e = bf ? (fp8 ? core_attr<__nv_bfloat16, true>(D.head_dim) : core_attr<__nv_bfloat16, false>(D.head_dim))
-                       : (fp8 ? core_attr<float, true>(D.head_dim) : core_attr<float, false>(D.head_dim));
+    kv->tc = attn_tc_supported(kv);
+    size_t ctas = kv->num_sms, rows = kTcMaxRows;
+    cudaError_t e;
+    if (kv->tc) {
+        e = attn_tc_init(kv);
+    } else {
+        e = bf ? (fp8 ? core_attr<__nv_bfloat16, true>(D.head_dim) : core_attr<__nv_bfloat16, false>(D.head_dim))
+               : (fp8 ? core_attr<float, true>(D.head_dim) : core_attr<float, false>(D.head_dim));
+        const int fit = 220 * 1024 / (core_smem(D.head_dim) + 2048);
+        kv->core_ctas_per_sm = fit < 1 ? 1 : fit > 4 ? 4 : fit;
+        ctas *= kv->core_ctas_per_sm;
+        rows = kRows;
+    }
     if (e != cudaSuccess) return e;
-    const int fit = 220 * 1024 / (core_smem(D.head_dim) + 2048);
-    kv->core_ctas_per_sm = fit < 1 ? 1 : fit > 4 ? 4 : fit;
-    const size_t ctas = (size_t)kv->num_sms * kv->core_ctas_per_sm;
-    const size_t rows = 2 * ctas * kRows;
-    if ((e = cudaMalloc(&kv->ws.part_o, rows * D.head_dim * sizeof(float))) != cudaSuccess) return e;
-    if ((e = cudaMalloc(&kv->ws.part_ml, rows * sizeof(float2))) != cudaSuccess) return e;
+    if ((e = cudaMalloc(&kv->ws.part_o, 2 * ctas * rows * D.head_dim * sizeof(float))) != cudaSuccess) return e;
+    if ((e = cudaMalloc(&kv->ws.part_ml, 2 * ctas * rows * sizeof(float2))) != cudaSuccess) return e;
     if ((e = cudaMalloc(&kv->ws.ticket, ctas * sizeof(int))) != cudaSuccess) return e;
+    kv->tickets = (int)ctas;
     return cudaMemsetAsync(kv->ws.ticket, 0, ctas * sizeof(int), kv->last_stream);
 }
 
 cudaError_t launch_tree_attention(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
+    if (kv->tc) return launch_tree_attention_tc(kv, a, s);
     const bool fp8 = kv->desc.format == ACE_KV_FP8;
     const int grid = kv->num_sms * kv->core_ctas_per_sm, smem = core_smem(a.head_dim);
     if (kv->desc.dtype == ACE_BF16) {

@@ -1,0 +1,907 @@
+// ace_attn_tc.cu — attention for trees of drafted tokens on the tensor cores (bf16 activations, head sizes 64 and
+// 128, plain and fp8 caches): flash attention with the keys of a request split over CTAs by the work line of
+// ace_kv_device.cuh.
+//
+// A unit is one request, kv head and block of query rows r = node * G + g (G query heads share a kv head, so
+// they share its cached rows too). A CTA walks key tiles of 128 positions:
+//   S = Q K^T              tcgen05.mma, 128 x 128 fp32 in TMEM
+//   P = 2^(S - m), l += P  softmax warps, a thread per row; P goes back to TMEM as bf16 / fp16
+//   O += P V               tcgen05.mma, A = P from TMEM, B = V as stored (its rows are K indices)
+// Two accumulators and two S buffers: with RT = 2 they belong to two blocks of 128 rows that share each
+// loaded tile; with RT = 1 to even and odd tiles of one block, joined at the end, so that the softmax
+// of one tile runs beside the products of the next either way.
+// fp8 caches: K's codes are the B operand as stored (kind::f8f6f4), against q split into two e4m3 terms, which
+// hold 8 significant bits, all of a bf16 q (elements 2^-10 and more below the row's largest lose their last bits, a
+// 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory (exact), with
+// their scales on P: P V accumulates in units of 2^eref, a power of two above the scales seen so far.
+#include "ace_kv_device.cuh"
+#include "ace_tc.cuh"
+
+namespace ace {
+namespace {
+
+constexpr int kTcKeys = 128, kTcThreads = 512, kSegRing = 4, kAuxRing = 3;
+constexpr int kLazy = 8;                // the reference maximum moves once a row's maximum is 2^8 above it
+constexpr int kPUp = 6;                 // fp16 weights carry a factor 2^6: up to 2^(kLazy + kPUp), 2^-14 is normal
+constexpr int kConvThreads = 128;
+// Every wait is on an mbarrier and bounded. A wait names a phase by its parity, so each waiter takes part in every phase
+// of its barriers, or what it waits for in between implies the phases that it leaves out.
+
+struct TcAttnArgs {
+    AttnArgs a;
+    CUtensorMap k, v;
+    int box_rows;                       // positions of a page in one box
+};
+
+template <bool FP8, int D, int RT>
+struct Cfg {
+    static constexpr int ROWS = 128 * RT;
+    static constexpr int Q = 256 * D;                   // bytes of a row block: bf16, or two e4m3 terms
+    static constexpr int TILE = 128 * D * (FP8 ? 1 : 2);
+    static constexpr int CONV = FP8 ? 128 * D * 2 : 0;  // V as fp16
+    static constexpr int NC = FP8 ? 2 : 0;
+    static constexpr int NK = D == 64 ? (FP8 ? 6 : 4) : FP8 && RT == 1 ? 4 : 3;
+    static constexpr int NV = D == 64 ? (FP8 ? 6 : 4) : FP8 && RT == 1 ? 3 : 2;
+    static constexpr int OFF_K = RT * Q;
+    static constexpr int OFF_V = OFF_K + NK * TILE;
+    static constexpr int OFF_C = OFF_V + NV * TILE;
+    static constexpr int OFF_MISC = OFF_C + NC * CONV;
+};
+
+struct TcSegment {
+    Segment s;
+    int go, pad;
+    unsigned long long bad[kMaxNodes / 64];     // nodes whose V row holds what is not finite
+};
+
+template <bool FP8, int RT>
+struct Misc {
+    uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], v_ready[6], c_empty[2];
+    uint64_t s_full[2], p_ready[2], o_done[2], q_full, q_free, soft, drain;
+    uint64_t seg_full[kSegRing], seg_empty[kSegRing], aux_full[kAuxRing], aux_empty[kAuxRing];
+    uint32_t tmem;
+    int abort_flag, joins, pad;
+    TcSegment seg[kSegRing];
+    float2 ml[RT == 1 ? 256 : 1];               // RT = 1: both halves' running maximum and sum
+    int eref1[RT == 1 ? 2 : 1];
+    float q_scale[2][FP8 ? 128 * RT : 1];       // by turns of segments: softmax may be one behind
+    float4 kf[FP8 ? kAuxRing : 1][FP8 ? 32 : 1], vf[FP8 ? kAuxRing : 1][FP8 ? 32 : 1];   // 128 factors a tile
+    int eref[kAuxRing];
+};
+
+template <bool FP8, int D, int RT>
+constexpr int tc_smem() { return 1024 + Cfg<FP8, D, RT>::OFF_MISC + (int)sizeof(Misc<FP8, RT>); }
+
+static_assert(tc_smem<false, 128, 2>() <= 232448 && tc_smem<false, 128, 1>() <= 232448, "shared memory");
+static_assert(tc_smem<true, 128, 2>() <= 232448 && tc_smem<true, 128, 1>() <= 232448, "shared memory");
+static_assert(tc_smem<false, 64, 2>() <= 232448 && tc_smem<true, 64, 2>() <= 232448, "shared memory");
+
+// Shared-memory descriptor, K-major rows of 64 bytes in the 64-byte swizzle (8-row atoms of 512 bytes).
+__device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(512 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)4 << 61;
+}
+
+// V as stored: rows are K indices, 64-element blocks of 128-byte rows in the 128-byte swizzle, 16 KB apart.
+__device__ __forceinline__ uint64_t smem_desc_v(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)(16384 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+           (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+// Instruction descriptor: fp32 accumulator; type codes of A and B (kind::f16: 0 fp16, 1 bf16; kind::f8f6f4: 0 e4m3).
+__host__ __device__ constexpr uint32_t idesc_of(int type, int M, int N, bool b_mn) {
+    return (1u << 4) | ((uint32_t)type << 7) | ((uint32_t)type << 10) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc),
+        "r"(acc));
+}
+
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc),
+        "r"(acc));
+}
+
+#define ACE_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define ACE_V8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : ACE_R8(r, 0), ACE_R8(r, 8), ACE_R8(r, 16), ACE_R8(r, 24)
+        : "r"(taddr));
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::ACE_V8(r, 0),
+        ACE_V8(r, 8), ACE_V8(r, 16), ACE_V8(r, 24), "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::ACE_V8(r, 0),
+        ACE_V8(r, 8), "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Which of the 32 keys from position `pos` on row `node` sees: the prefix, and the nodes of its mask.
+__device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, int node, int pos) {
+    const int m0 = pos - s.len;         // first node
+    if (m0 <= -32) return 0xffffffffu;
+    const int from = m0 < 0 ? 0 : m0;
+    const int w = from >> 6, sh = from & 63;
+    unsigned long long bits = sees_word(a, s.node0, s.n, node, w) >> sh;
+    if (sh > 32) bits |= sees_word(a, s.node0, s.n, node, w + 1) << (64 - sh);
+    uint32_t r = (uint32_t)bits;
+    if (m0 < 0) r = r << -m0 | ((1u << -m0) - 1u);
+    return r;
+}
+
+struct Ring {
+    int i = 0;
+    uint32_t phase = 0;
+    template <int N>
+    __device__ __forceinline__ void next() {
+        if (++i == N) i = 0, phase ^= 1u;
+    }
+};
+
+template <bool FP8, int D, int RT>
+__global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant__ TcAttnArgs p) {
+    using C = Cfg<FP8, D, RT>;
+    constexpr int ROWS = C::ROWS, NK = C::NK, NV = C::NV, NC = C::NC;
+    constexpr int kHalves = D / 64;                     // 64-element blocks of a bf16 / fp16 row
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    using M = Misc<FP8, RT>;
+    M& m = *reinterpret_cast<M*>(smem + C::OFF_MISC);
+    const AttnArgs& a = p.a;
+    volatile int* abort_flag = &m.abort_flag;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < NK; ++i) mbar_init(&m.k_full[i], 1), mbar_init(&m.k_empty[i], 1);
+        for (int i = 0; i < NV; ++i) mbar_init(&m.v_full[i], 1), mbar_init(&m.v_empty[i], FP8 ? 4 : 1);
+        for (int i = 0; i < (FP8 ? NC : NV); ++i) mbar_init(&m.v_ready[i], 4);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&m.c_empty[i], 1);
+            mbar_init(&m.s_full[i], 1);
+            mbar_init(&m.p_ready[i], 4);
+            mbar_init(&m.o_done[i], 1);
+        }
+        mbar_init(&m.q_full, 4);
+        mbar_init(&m.soft, 8);
+        mbar_init(&m.q_free, 1);
+        mbar_init(&m.drain, 1);
+        for (int i = 0; i < kSegRing; ++i) {
+            mbar_init(&m.seg_full[i], 1);
+            mbar_init(&m.seg_empty[i], FP8 ? 15 : 14);  // producer, MMA, (scales,) 8 softmax and 4 converting warps
+        }
+        for (int i = 0; i < kAuxRing; ++i) {
+            mbar_init(&m.aux_full[i], 1);
+            mbar_init(&m.aux_empty[i], 4 * RT);
+        }
+        m.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&m.tmem)), "r"(512u));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = m.tmem;                       // S0, S1, O0, O1
+    constexpr uint32_t kO = 256;
+    Ring seg;
+
+    // Every role but the scheduler walks the CTA's segments; false: no more (or aborted).
+    auto next_segment = [&](Segment& s) -> bool {
+        if (!mbar_wait_warp(&m.seg_full[seg.i], seg.phase, a.err, abort_flag)) {
+            *abort_flag = 1;
+            return false;
+        }
+        if (!m.seg[seg.i].go) return false;
+        s = m.seg[seg.i].s;
+        return true;
+    };
+    auto segment_done = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&m.seg_empty[seg.i]);
+        seg.next<kSegRing>();
+    };
+
+    if (warp == 3) {
+        // ------------------------------------------------ scheduler
+        Cursor cur{};
+        bool more = cursor_init<ROWS, kTcKeys>(a, blockIdx.x, gridDim.x, cur);
+        while (true) {
+            if (!mbar_wait_warp(&m.seg_empty[seg.i], seg.phase ^ 1u, a.err, abort_flag)) {
+                *abort_flag = 1;
+                break;
+            }
+            Segment s{};
+            more = more && cursor_next<ROWS, kTcKeys>(a, blockIdx.x, cur, s);
+            if (lane == 0) {
+                m.seg[seg.i].s = s;
+                m.seg[seg.i].go = more;
+                for (int w = 0; w < kMaxNodes / 64; ++w) m.seg[seg.i].bad[w] = 0;
+                mbar_arrive(&m.seg_full[seg.i]);
+            }
+            seg.next<kSegRing>();
+            if (!more) break;
+        }
+    } else if (warp == 0) {
+        // ------------------------------------------------ TMA: lane x loads box x of a tile
+        Ring rk, rv;
+        long long nk = 0, nv = 0;
+        bool ok = true;
+        Segment s;
+        const int boxes = kTcKeys / p.box_rows;
+        while (ok && next_segment(s)) {
+            const int total = s.len + s.n;
+            for (int t = s.tile0; t < s.tile1; ++t) {
+                const int pos = t * kTcKeys + lane * p.box_rows;
+                int page = -1;
+                if (lane < boxes && pos < total) page = page_of(a, s.b, pos);
+                const int row = a.row0 + (page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
+                const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= 0)) * (uint32_t)(p.box_rows * (C::TILE / 128));
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    Ring& r = kv ? rv : rk;
+                    uint64_t* full = kv ? m.v_full : m.k_full;
+                    uint64_t* empty = kv ? m.v_empty : m.k_empty;
+                    if (!mbar_wait_warp(&empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    if (lane == 0) mbar_expect_tx(&full[r.i], bytes);
+                    __syncwarp();
+                    if (page >= 0) {
+                        unsigned char* dst = smem + (kv ? C::OFF_V : C::OFF_K) + r.i * C::TILE;
+                        const CUtensorMap* map = kv ? &p.v : &p.k;
+                        if constexpr (FP8) {
+                            tma_load_2d(dst + lane * p.box_rows * D, map, &full[r.i], 0, row);
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h)
+                                tma_load_2d(dst + h * 16384 + lane * p.box_rows * 128, map, &full[r.i], h * 64, row);
+                        }
+                    }
+                    if (kv) ++nv, rv.next<NV>(); else ++nk, rk.next<NK>();
+                }
+                if (!ok) break;
+            }
+            segment_done();
+        }
+        if (!ok) *abort_flag = 1;
+        if (*abort_flag) {
+            // let the copies already issued land before the CTA exits
+            for (long long f = nk - 1; f >= 0 && f >= nk - NK; --f)
+                if (!mbar_wait(&m.k_full[f % NK], (uint32_t)((f / NK) & 1), a.err)) break;
+            for (long long f = nv - 1; f >= 0 && f >= nv - NV; --f)
+                if (!mbar_wait(&m.v_full[f % NV], (uint32_t)((f / NV) & 1), a.err)) break;
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issuer
+        Ring rk, rv, rc;
+        uint32_t q_phase = 0, p_phase[2] = {0, 0};
+        bool ok = true;
+        Segment s;
+        while (ok && next_segment(s)) {
+            const int items = (s.tile1 - s.tile0) * RT;
+            if (!mbar_wait_warp(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
+            q_phase ^= 1u;
+            for (int i = 0; i <= items; ++i) {
+                if (i < items) {
+                    // S[i & 1] = Q K^T; the PV that read P from this buffer was issued before
+                    const int rt = RT == 2 ? i & 1 : 0;
+                    if (rt == 0 && !mbar_wait_warp(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t q_addr = smem_u32(smem + rt * C::Q), k_addr = smem_u32(smem + C::OFF_K + rk.i * C::TILE);
+                        const uint32_t d = tmem + (uint32_t)((i & 1) * 128);
+                        if constexpr (FP8) {
+                            constexpr uint32_t idesc = idesc_of(0, 128, 128, false);
+#pragma unroll
+                            for (int term = 0; term < 2; ++term) {
+                                const uint64_t ad = D == 128 ? smem_desc_sw128(q_addr + term * C::Q / 2) : smem_desc_sw64(q_addr + term * C::Q / 2);
+                                const uint64_t bd = D == 128 ? smem_desc_sw128(k_addr) : smem_desc_sw64(k_addr);
+#pragma unroll
+                                for (int kk = 0; kk < D / 32; ++kk) mma_f8(d, ad + 2 * kk, bd + 2 * kk, idesc, term || kk);
+                            }
+                        } else {
+                            constexpr uint32_t idesc = idesc_of(1, 128, 128, false);
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h) {
+                                const uint64_t ad = smem_desc_sw128(q_addr + h * 16384), bd = smem_desc_sw128(k_addr + h * 16384);
+#pragma unroll
+                                for (int kk = 0; kk < 4; ++kk) mma_bf16(d, ad + 2 * kk, bd + 2 * kk, idesc, h || kk);
+                            }
+                        }
+                        mma_commit(&m.s_full[i & 1]);
+                        if (rt == RT - 1) mma_commit(&m.k_empty[rk.i]);
+                        if (i == items - 1) mma_commit(&m.q_free);
+                    }
+                    __syncwarp();
+                    if (rt == RT - 1) rk.next<NK>();
+                }
+                if (i > 0) {
+                    // O[j & 1] += P V
+                    const int j = i - 1, rt = RT == 2 ? j & 1 : 0;
+                    Ring& r = FP8 ? rc : rv;
+                    if (!mbar_wait_warp(&m.p_ready[j & 1], p_phase[j & 1], a.err, abort_flag)) { ok = false; break; }
+                    p_phase[j & 1] ^= 1u;
+                    if (rt == 0 && !mbar_wait_warp(&m.v_ready[r.i], r.phase, a.err, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        constexpr uint32_t idesc = idesc_of(FP8 ? 0 : 1, 128, D, true);
+                        const uint32_t v_addr = smem_u32(smem + (FP8 ? C::OFF_C + r.i * C::CONV : C::OFF_V + r.i * C::TILE));
+                        const uint64_t bd = smem_desc_v(v_addr);
+                        const uint32_t d = tmem + kO + (uint32_t)((j & 1) * D), pa = tmem + (uint32_t)((j & 1) * 128);
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk) mma_ts(d, pa + 8 * kk, bd + 128 * kk, idesc, j >= 2 || kk > 0);
+                        mma_commit(&m.o_done[j & 1]);
+                        if (rt == RT - 1) mma_commit(FP8 ? &m.c_empty[r.i] : &m.v_empty[r.i]);
+                    }
+                    __syncwarp();
+                    if (rt == RT - 1) {
+                        if (FP8) rc.next<NC ? NC : 1>(); else rv.next<NV>();
+                    }
+                }
+            }
+            if (ok) segment_done();
+        }
+        if (!ok) *abort_flag = 1;
+        if (*abort_flag) {
+            // products in flight read shared memory and TMEM
+            if (elect_one()) mma_commit(&m.drain);
+            __syncwarp();
+            mbar_wait(&m.drain, 0, a.err);
+        }
+    } else if (warp == 2) {
+        // ------------------------------------------------ scales of fp8 rows: 4 positions a lane
+        if constexpr (FP8) {
+            Ring r;
+            bool ok = true;
+            Segment s;
+            while (ok && next_segment(s)) {
+                const int total = s.len + s.n;
+                int eref = -1000;
+                for (int t = s.tile0; t < s.tile1; ++t) {
+                    const int pos = t * kTcKeys + lane * 4;
+                    uint32_t kb = 0, vb = 0;
+                    if (pos < total) {
+                        const int page = page_of(a, s.b, pos);
+                        if (page >= 0) {
+                            const long long at = ((long long)page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
+                            kb = __ldg(reinterpret_cast<const uint32_t*>(a.k_scale + at));
+                            vb = __ldg(reinterpret_cast<const uint32_t*>(a.v_scale + at));
+                        }
+                    }
+                    if (pos + 4 > total) {
+                        const int left = total - pos;       // positions of the four that exist
+                        const uint32_t have = left <= 0 ? 0u : 0xffffffffu >> (8 * (4 - left));
+                        kb &= have;
+                        vb &= have;
+                    }
+                    int top = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = max(top, (int)(vb >> (8 * i) & 0xff));
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    // two octaves of room, so that small differences between tiles do not move it
+                    if (top - 127 > eref) eref = top - 127 + 2;
+                    float kf[4], vf[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int vbyte = (int)(vb >> (8 * i) & 0xff);
+                        kf[i] = pow2_of_byte((int)(kb >> (8 * i) & 0xff));
+                        const int e = vbyte - eref + kPUp;      // 2^(e_j - eref + kPUp), biased exponent
+                        vf[i] = vbyte == 0 || e <= 0 ? 0.f : pow2_of_byte(e);
+                    }
+                    if (!mbar_wait_warp(&m.aux_empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    m.kf[r.i][lane] = make_float4(kf[0], kf[1], kf[2], kf[3]);
+                    m.vf[r.i][lane] = make_float4(vf[0], vf[1], vf[2], vf[3]);
+                    if (lane == 0) m.eref[r.i] = eref;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&m.aux_full[r.i]);
+                    r.next<kAuxRing>();
+                }
+                if (ok) segment_done();
+            }
+            if (!ok) *abort_flag = 1;
+        }
+    } else if (warp >= 12) {
+        // ------------------------------------------------ q rows, and V tiles made ready
+        const int tid = threadIdx.x - 384;
+        Ring rv, rc;
+        uint32_t q_phase = 1;           // the first segment's q buffer is free
+        bool ok = true;
+        Segment s;
+        while (ok && next_segment(s)) {
+            if (!mbar_wait_warp(&m.q_free, q_phase, a.err, abort_flag)) { ok = false; break; }
+            q_phase ^= 1u;
+            const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
+            constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
+            // (rows of the block past the unit's keep what they hold: rows of S, P and O do not mix)
+            for (int r0 = 0; r0 < s.rows; r0 += 128 / kChunks) {
+                const int r = r0 + tid / kChunks, c = tid % kChunks;
+                float f[8] = {};
+                if (r < s.rows) {
+                    const int row = s.row0 + r;
+                    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (s.node0 + row / a.group) * a.q_token_stride +
+                                               (s.head * a.group + row % a.group) * a.q_head_stride + c * 8;
+                    if ((uintptr_t)src % 16 == 0) {
+                        Vec16<__nv_bfloat16>::to_float(__ldg(reinterpret_cast<const uint4*>(src)), f);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = to_f32(src[i]);
+                    }
+                }
+                unsigned char* tile = smem + (r >> 7) * C::Q;
+                const int rr = r & 127;
+                if constexpr (FP8) {
+                    float amax = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] = finite_or_nan(f[i] * q_mul), amax = fmaxf(amax, fabsf(f[i]));
+#pragma unroll
+                    for (int o = kChunks / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                    const int byte = e4m3_scale_byte(amax);
+                    const float mul = pow2_of_minus_byte(byte);
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = f[2 * i] * mul, y = f[2 * i + 1] * mul;
+                        hi[i] = e4m3x2(x, y);
+                        const uint32_t h = f16x2_of_e4m3x2(hi[i]);
+                        const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                        lo[i] = e4m3x2(x - back.x, y - back.y);
+                    }
+                    // 8 bytes of a 16-byte chunk
+                    const int ch = c >> 1;
+                    const uint32_t off = D == 128 ? (uint32_t)rr * 128u + (uint32_t)((ch ^ (rr & 7)) << 4)
+                                                  : (uint32_t)rr * 64u + (uint32_t)((ch ^ ((rr >> 1) & 3)) << 4);
+                    *reinterpret_cast<uint2*>(tile + off + (c & 1) * 8) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                    *reinterpret_cast<uint2*>(tile + C::Q / 2 + off + (c & 1) * 8) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                    if (c == 0) m.q_scale[seg.i & 1][r] = pow2_of_byte(byte);
+                } else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
+                        w[i] = *reinterpret_cast<const uint32_t*>(&v);
+                    }
+                    *reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
+                        make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.q_full);
+            unsigned long long* bad = m.seg[seg.i].bad;
+            const int total = s.len + s.n;
+            for (int t = s.tile0; t < s.tile1; ++t) {
+                const int pos0 = t * kTcKeys;
+                const bool drafted = pos0 + kTcKeys > s.len;    // rows that not every node sees, or past the end
+                if (!mbar_wait_warp(&m.v_full[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                unsigned char* v = smem + C::OFF_V + rv.i * C::TILE;
+                if constexpr (FP8) {
+                    if (!mbar_wait_warp(&m.c_empty[rc.i], rc.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    unsigned char* out = smem + C::OFF_C + rc.i * C::CONV;
+                    constexpr int kUnits = D / 16;      // 16 codes become two 16-byte chunks
+#pragma unroll
+                    for (int u = tid; u < 128 * kUnits; u += kConvThreads) {
+                        const int row = u / kUnits, c = u % kUnits;
+                        uint4 w = *reinterpret_cast<const uint4*>(v + row * D + c * 16);
+                        if (drafted) {
+                            if (pos0 + row >= total) {
+                                w = make_uint4(0, 0, 0, 0);
+                            } else if (pos0 + row >= s.len) {
+                                // e4m3's NaN: all bits of the code but the sign
+                                uint32_t* x = reinterpret_cast<uint32_t*>(&w);
+                                bool found = false;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint32_t nan = ((x[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                                    if (nan) {
+                                        found = true;
+                                        x[i] &= ~((nan >> 7) * 0xffu);
+                                    }
+                                }
+                                if (found) atomicOr(&bad[(pos0 + row - s.len) >> 6], 1ull << ((pos0 + row - s.len) & 63));
+                            }
+                        }
+                        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+                        uint32_t h[8];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) h[2 * i] = f16x2_of_e4m3x2(x[i] & 0xffffu), h[2 * i + 1] = f16x2_of_e4m3x2(x[i] >> 16);
+                        unsigned char* dst = out + (c >> 2) * 16384 + row * 128;
+                        const int c0 = (c & 3) * 2;
+                        // the upper half's threads write their chunks in the other order: distinct banks
+                        const bool swap = c & 4;
+                        const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+                        *reinterpret_cast<uint4*>(dst + (((c0 + (swap ? 1 : 0)) ^ (row & 7)) << 4)) = swap ? hi : lo;
+                        *reinterpret_cast<uint4*>(dst + (((c0 + (swap ? 0 : 1)) ^ (row & 7)) << 4)) = swap ? lo : hi;
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(&m.v_ready[rc.i]);
+                        mbar_arrive(&m.v_empty[rv.i]);
+                    }
+                    rc.next<NC ? NC : 1>();
+                } else {
+                    if (drafted) {
+                        for (int u = tid; u < 128 * kChunks; u += kConvThreads) {
+                            const int row = u / kChunks, c = u % kChunks;
+                            if (pos0 + row < s.len) continue;
+                            uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+                            if (pos0 + row >= total) {
+                                *at = make_uint4(0, 0, 0, 0);
+                                continue;
+                            }
+                            uint4 w = *at;
+                            uint32_t* x = reinterpret_cast<uint32_t*>(&w);
+                            bool found = false;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if ((x[i] & 0x7f80u) == 0x7f80u) found = true, x[i] &= 0xffff0000u;
+                                if ((x[i] & 0x7f800000u) == 0x7f800000u) found = true, x[i] &= 0xffffu;
+                            }
+                            if (found) {
+                                *at = w;
+                                atomicOr(&bad[(pos0 + row - s.len) >> 6], 1ull << ((pos0 + row - s.len) & 63));
+                            }
+                        }
+                        fence_async_smem();
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&m.v_ready[rv.i]);
+                }
+                rv.next<NV>();
+            }
+            if (ok) segment_done();
+        }
+        if (!ok) *abort_flag = 1;
+    } else {
+        // ------------------------------------------------ softmax: group g of 4 warps, a thread per row
+        const int g = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const int tid = threadIdx.x - 128;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        const uint32_t s_t = tmem + lanes + (uint32_t)(g * 128), o_t = tmem + lanes + kO + (uint32_t)(g * D);
+        uint32_t s_phase = 0, o_phase = 0, soft_phase = 0;
+        // the eight warps meet
+        auto soft_sync = [&]() -> bool {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.soft);
+            soft_phase ^= 1u;
+            return mbar_wait_warp(&m.soft, soft_phase ^ 1u, a.err, abort_flag);
+        };
+        Ring ra;
+        bool ok = true;
+        Segment s;
+        while (ok && next_segment(s)) {
+            const int row = RT == 2 ? g * 128 + r : r;          // of the unit
+            const bool live = row < s.rows;
+            const bool warp_live = (RT == 2 ? g * 128 : 0) + quad * 32 < s.rows;
+            const int node = live ? (s.row0 + row) / a.group : 0;
+            const int hq = s.head * a.group + (live ? (s.row0 + row) % a.group : 0);
+            const int tiles = s.tile1 - s.tile0;
+            const float f_row0 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+            float f_row = f_row0;
+            float ref = -INFINITY, l = 0.f;
+            int eref = 0;
+            int mine = 0;               // tiles of this group so far
+            for (int t = 0; t < tiles; ++t) {
+                const bool turn = RT == 2 || (t & 1) == g;
+                if (!turn) {
+                    if (FP8) ra.next<kAuxRing>();
+                    continue;
+                }
+                const int pos0 = (s.tile0 + t) * kTcKeys;
+                const bool drafted = pos0 + kTcKeys > s.len;
+                if (FP8 && !mbar_wait_warp(&m.aux_full[ra.i], ra.phase, a.err, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp(&m.s_full[g], s_phase, a.err, abort_flag)) { ok = false; break; }
+                s_phase ^= 1u;
+                tc_fence_after();
+                float o_mul = 1.f;
+                if (warp_live) {
+                    if (FP8) {
+                        f_row = fmaxf(f_row0 * m.q_scale[seg.i & 1][row], 0x1p-126f);     // 0 times a masked -inf is no score
+                        const int e = m.eref[ra.i];
+                        if (mine && e > eref) o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
+                        eref = e;
+                    }
+                    // the row's maximum
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t x[32];
+                        tmem_ld32(s_t + 32 * c, x);
+                        tmem_ld_wait();
+                        const uint32_t see = drafted ? sees32(a, s, node, pos0 + 32 * c) : 0xffffffffu;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 kf = FP8 ? m.kf[ra.i][c * 8 + i / 4] : make_float4(1.f, 1.f, 1.f, 1.f);
+                            const float k4[4] = {kf.x, kf.y, kf.z, kf.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                float v = __uint_as_float(x[i + j]);
+                                if (FP8) v *= k4[j];
+                                if (drafted && !(see >> (i + j) & 1)) v = -INFINITY;
+                                top = fmaxf(top, v);
+                            }
+                        }
+                    }
+                    top = top == -INFINITY ? top : top * f_row;
+                    if (top > ref + (float)kLazy || ref == -INFINITY) {
+                        const float f = ref == -INFINITY ? 0.f : exp2_approx(ref - top);
+                        ref = top;
+                        l *= f;
+                        if (mine) o_mul *= f;
+                    }
+                    const float shift = ref == -INFINITY ? 0.f : -ref;
+                    // the weights, in place of the scores that are read already
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t x[32], w[16];
+                        tmem_ld32(s_t + 32 * c, x);
+                        tmem_ld_wait();
+                        const uint32_t see = drafted ? sees32(a, s, node, pos0 + 32 * c) : 0xffffffffu;
+                        float sum[4] = {};
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 kf = FP8 ? m.kf[ra.i][c * 8 + i / 4] : make_float4(1.f, 1.f, 1.f, 1.f);
+                            const float4 vf = FP8 ? m.vf[ra.i][c * 8 + i / 4] : make_float4(1.f, 1.f, 1.f, 1.f);
+                            const float k4[4] = {kf.x, kf.y, kf.z, kf.w}, v4[4] = {vf.x, vf.y, vf.z, vf.w};
+                            float e[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                float v = __uint_as_float(x[i + j]);
+                                if (FP8) v *= k4[j];
+                                if (drafted && !(see >> (i + j) & 1)) v = -INFINITY;
+                                e[j] = exp2_approx(fmaf(v, f_row, shift));
+                                sum[j] += e[j];
+                                if (FP8) e[j] *= v4[j];
+                            }
+                            if constexpr (FP8) {
+                                const __half2 p0 = __floats2half2_rn(e[0], e[1]), p1 = __floats2half2_rn(e[2], e[3]);
+                                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+                            } else {
+                                const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
+                                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+                            }
+                        }
+                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                        tmem_st16(s_t + 16 * c, w);
+                    }
+                    tmem_st_wait();
+                }
+                if (FP8) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&m.aux_empty[ra.i]);
+                    ra.next<kAuxRing>();
+                }
+                // the group's previous product has left O
+                if (mine) {
+                    if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+                    o_phase ^= 1u;
+                    if (__any_sync(0xffffffffu, o_mul != 1.f)) {
+                        tc_fence_after();
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t x[32];
+                            tmem_ld32(o_t + 32 * c, x);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * o_mul);
+                            tmem_st32(o_t + 32 * c, x);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&m.p_ready[g]);
+                ++mine;
+            }
+            if (!ok) break;
+            if (mine) {
+                if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+                o_phase ^= 1u;
+            }
+            tc_fence_after();
+            // ---------------- the unit's result, or this CTA's part of it
+            float up0 = 1.f, up1 = 0.f;         // factors of O0 and O1 (RT = 1), of this group's O (RT = 2: up0)
+            float m_all = ref, l_all = l;
+            int c0 = 0, c1 = D;                 // dimensions of this thread
+            uint32_t ta = o_t, tb = o_t;
+            const float unit = FP8 ? exp2f((float)(eref - kPUp)) : 1.f;
+            if constexpr (RT == 1) {
+                m.ml[g * 128 + r] = make_float2(ref, l);
+                if (r == 0) m.eref1[g] = eref;
+                if (!soft_sync()) { ok = false; break; }
+                const float2 x = m.ml[r], y = m.ml[128 + r];
+                m_all = fmaxf(x.x, y.x);
+                const float z = m_all == -INFINITY ? 0.f : m_all;
+                up0 = exp2f(x.x - z);
+                up1 = exp2f(y.x - z);
+                l_all = x.y * up0 + y.y * up1;
+                if (FP8) {
+                    up0 *= exp2f((float)(m.eref1[0] - kPUp));
+                    up1 *= exp2f((float)(m.eref1[1] - kPUp));
+                }
+                if (tiles < 2) up1 = 0.f;
+                ta = tmem + lanes + kO;
+                tb = ta + D;
+                c0 = g * (D / 2);
+                c1 = c0 + D / 2;
+            } else {
+                up0 = unit;
+            }
+            const bool whole = s.part < 0;
+            if (whole) {
+                const float inv = l_all == 0.f ? 0.f : 1.f / l_all;
+                up0 *= inv;
+                up1 *= inv;
+            }
+            const long long at = (long long)(s.node0 + node) * a.n_heads + hq;
+            if (warp_live) {
+                const TcSegment& ts = m.seg[seg.i];
+                for (int c = c0; c < c1; c += 32) {
+                    uint32_t x[32];
+                    float o[32];
+                    tmem_ld32(ta + c, x);
+                    tmem_ld_wait();
+                    // a row that has seen nothing has l = 0 and takes nothing from O either
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = up0 == 0.f ? 0.f : __uint_as_float(x[i]) * up0;
+                    if (RT == 1 && tiles > 1) {
+                        tmem_ld32(tb + c, x);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] += up1 == 0.f ? 0.f : __uint_as_float(x[i]) * up1;
+                    }
+                    // V values that are not finite were left out of the products: the rows that see them get them here
+                    for (int w = 0; w < kMaxNodes / 64; ++w) {
+                        unsigned long long b = ts.bad[w];
+                        if (b && live) b &= sees_word(a, s.node0, s.n, node, w);
+                        while (b && live) {
+                            const int nd = w * 64 + __ffsll((long long)b) - 1;
+                            b &= b - 1;
+                            const int page = page_of(a, s.b, s.len + nd);
+                            if (page < 0) continue;
+                            const long long vr = ((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + nd) & (a.page_size - 1));
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                if constexpr (FP8) {
+                                    const uint8_t code = static_cast<const uint8_t*>(a.v_pool)[vr * D + c + i];
+                                    if ((code & 0x7f) == 0x7f) o[i] = __uint_as_float(0x7fffffffu);
+                                } else {
+                                    const float v = to_f32(static_cast<const __nv_bfloat16*>(a.v_pool)[vr * D + c + i]);
+                                    if (!(fabsf(v) < INFINITY)) o[i] += v;
+                                }
+                            }
+                        }
+                    }
+                    if (!live) continue;
+                    if (whole) {
+                        uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + at * D + c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const __nv_bfloat162 v = __floats2bfloat162_rn(o[8 * i + 2 * j], o[8 * i + 2 * j + 1]);
+                                w[j] = *reinterpret_cast<const uint32_t*>(&v);
+                            }
+                            dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    } else {
+                        float4* dst = reinterpret_cast<float4*>(a.ws.part_o + ((long long)s.part * ROWS + row) * D + c);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    }
+                }
+                if (live && c0 == 0) {
+                    if (!whole) a.ws.part_ml[(long long)s.part * ROWS + row] = make_float2(m_all, l_all);
+                    else if (a.lse) a.lse[at] = (m_all + log2f(l_all)) * 0.69314718055994530942f;
+                }
+            }
+            tc_fence_before();
+            if (RT == 1 || !whole) {
+                if (!whole) __threadfence();
+                if (!soft_sync()) { ok = false; break; }        // O and ml may be overwritten, partial results are written
+                if (!whole) {
+                    if (tid == 0) m.joins = last_of_unit(a, s);
+                    if (!soft_sync()) { ok = false; break; }
+                    if (m.joins) {
+                        __threadfence();
+                        join_unit<__nv_bfloat16, ROWS>(a, s, tid, 256);
+                    }
+                }
+            }
+            segment_done();
+        }
+        if (!ok) *abort_flag = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+}
+
+template <bool FP8, int D, int RT>
+cudaError_t tc_attr() {
+    return raise_smem_limit(k_attn_tc<FP8, D, RT>, tc_smem<FP8, D, RT>());
+}
+
+template <bool FP8, int D>
+cudaError_t tc_attrs() {
+    const cudaError_t e = tc_attr<FP8, D, 1>();
+    return e == cudaSuccess ? tc_attr<FP8, D, 2>() : e;
+}
+
+template <bool FP8, int D>
+cudaError_t tc_launch(const TcAttnArgs& p, int ctas, cudaStream_t s) {
+    // one block of 128 rows a unit where that holds a request's largest tree, else two that share the loaded tiles
+    if ((long long)p.a.max_nodes * p.a.group <= 128)
+        k_attn_tc<FP8, D, 1><<<ctas, kTcThreads, tc_smem<FP8, D, 1>(), s>>>(p);
+    else
+        k_attn_tc<FP8, D, 2><<<ctas, kTcThreads, tc_smem<FP8, D, 2>(), s>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+bool attn_tc_supported(const ace_kv* kv) {
+    return kv->desc.dtype == ACE_BF16 && (kv->desc.head_dim == 64 || kv->desc.head_dim == 128);
+}
+
+cudaError_t attn_tc_init(ace_kv* kv) {
+    const ace_kv_desc& D = kv->desc;
+    const bool fp8 = D.format == ACE_KV_FP8;
+    const uint64_t rows = (uint64_t)D.layers * D.n_pages * D.n_kv_heads * D.page_size;
+    const uint32_t box = D.page_size < kTcKeys ? D.page_size : kTcKeys;
+    cudaError_t e;
+    if (fp8) {
+        const int swizzle = D.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+        if ((e = make_byte_map(&kv->maps.k, kv->k_pool, rows, D.head_dim, box, swizzle)) != cudaSuccess) return e;
+        if ((e = make_byte_map(&kv->maps.v, kv->v_pool, rows, D.head_dim, box, CU_TENSOR_MAP_SWIZZLE_NONE)) != cudaSuccess) return e;
+        return D.head_dim == 128 ? tc_attrs<true, 128>() : tc_attrs<true, 64>();
+    }
+    if ((e = make_tensor_map(&kv->maps.k, kv->k_pool, rows, D.head_dim, box, true)) != cudaSuccess) return e;
+    if ((e = make_tensor_map(&kv->maps.v, kv->v_pool, rows, D.head_dim, box, true)) != cudaSuccess) return e;
+    return D.head_dim == 128 ? tc_attrs<false, 128>() : tc_attrs<false, 64>();
+}
+
+cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
+    TcAttnArgs p;
+    p.a = a;
+    p.k = kv->maps.k;
+    p.v = kv->maps.v;
+    p.box_rows = a.page_size < kTcKeys ? a.page_size : kTcKeys;
+    if (kv->desc.format == ACE_KV_FP8)
+        return a.head_dim == 128 ? tc_launch<true, 128>(p, kv->num_sms, s) : tc_launch<true, 64>(p, kv->num_sms, s);
+    return a.head_dim == 128 ? tc_launch<false, 128>(p, kv->num_sms, s) : tc_launch<false, 64>(p, kv->num_sms, s);
+}
+
+}  // namespace ace

@@ -38,6 +38,7 @@ struct ace_kv {
     long long slots = 0;                // n_pages * page_size, per layer
     int* err = nullptr;
     ace::AttnWorkspace ws;
+    int tickets = 0;
     int core_ctas_per_sm = 1;           // CUDA-core attention
     bool tc = false;                    // tensor-core attention in use
     ace::KvMaps maps;
@@ -69,5 +70,12 @@ struct AttnArgs {
 
 cudaError_t attn_init(ace_kv* kv);      // kernel attributes, workspace, tensor maps
 cudaError_t launch_tree_attention(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
+// tensor-core kernel (ace_attn_tc.cu): bf16, head sizes 64 and 128
+constexpr int kTcMaxRows = 256;         // rows of a unit
+bool attn_tc_supported(const ace_kv* kv);
+cudaError_t attn_tc_init(ace_kv* kv);
+cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
+// 2-D map of bytes [rows, cols], boxes of box_rows whole rows (ace_expert_tc.cu)
+cudaError_t make_byte_map(CUtensorMap* m, const void* base, uint64_t rows, uint32_t cols, uint32_t box_rows, int swizzle);
 
 }  // namespace ace
