@@ -24,6 +24,8 @@ constexpr int kTcKeys = 128, kTcThreads = 512, kSegRing = 4, kAuxRing = 3;
 constexpr int kLazy = 8;                // the reference maximum moves once a row's maximum is 2^8 above it
 constexpr int kPUp = 6;                 // fp16 weights carry a factor 2^6: up to 2^(kLazy + kPUp), 2^-14 is normal
 constexpr int kConvThreads = 128;
+constexpr int kSoftRegs = 184, kOtherRegs = 72;
+static_assert(256 * (kSoftRegs + kOtherRegs) <= kTcThreads * 128, "the split must fit the launch's registers");
 // Every wait is on an mbarrier and bounded. A wait names a phase by its parity, so each waiter takes part in every phase
 // of its barriers, or what it waits for in between implies the phases that it leaves out.
 
@@ -143,6 +145,107 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
+// Two fp32 values in one operation each.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// A row's 128 scores from TMEM, with fp8 rows' scales; returns their maximum. The scores stay in registers.
+template <bool FP8>
+__device__ __forceinline__ float load_scores(uint32_t s_t, float (&x)[128], const float4* kf) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint32_t* r = reinterpret_cast<uint32_t*>(x) + 32 * c;
+        tmem_ld32(s_t + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(r));
+    }
+    tmem_ld_wait();
+    if (FP8) {
+#pragma unroll
+        for (int i = 0; i < 128; i += 4) {
+            const float4 k = kf[i / 4];
+            unpair(mul2(pair(x[i], x[i + 1]), pair(k.x, k.y)), x[i], x[i + 1]);
+            unpair(mul2(pair(x[i + 2], x[i + 3]), pair(k.z, k.w)), x[i + 2], x[i + 3]);
+        }
+    }
+    float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int i = 4; i < 128; i += 8) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], i + 4 + j < 128 ? fmaxf(x[i + j], x[i + 4 + j]) : x[i + j]);
+    }
+    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+
+// The same where not every position counts.
+template <bool FP8>
+__device__ __forceinline__ float mask_scores(float (&x)[128], const uint32_t (&see)[4]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 128; ++i) {
+        x[i] = see[i >> 5] >> (i & 31) & 1 ? x[i] : -INFINITY;
+        top = fmaxf(top, x[i]);
+    }
+    return top;
+}
+
+// P = 2^(x f + shift) to TMEM (with the scales of fp8 rows of V), over the scores that are read already; returns the sum of P.
+template <bool FP8>
+__device__ __forceinline__ float store_weights(uint32_t s_t, const float (&x)[128], float f, float shift, const float4* vf) {
+    const uint64_t f2 = pair(f, f), shift2 = pair(shift, shift);
+    uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            float e[4];
+            unpair(fma2(pair(x[32 * c + i], x[32 * c + i + 1]), f2, shift2), e[0], e[1]);
+            unpair(fma2(pair(x[32 * c + i + 2], x[32 * c + i + 3]), f2, shift2), e[2], e[3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]);
+            const uint64_t e01 = pair(e[0], e[1]), e23 = pair(e[2], e[3]);
+            sum[0] = add2(sum[0], e01);
+            sum[1] = add2(sum[1], e23);
+            if constexpr (FP8) {
+                const float4 v = vf[c * 8 + i / 4];
+                unpair(mul2(e01, pair(v.x, v.y)), e[0], e[1]);
+                unpair(mul2(e23, pair(v.z, v.w)), e[2], e[3]);
+                const __half2 p0 = __floats2half2_rn(e[0], e[1]), p1 = __floats2half2_rn(e[2], e[3]);
+                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+            } else {
+                const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
+                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+            }
+        }
+        tmem_st16(s_t + 16 * c, w);
+    }
+    tmem_st_wait();
+    float a, b, c, d;
+    unpair(sum[0], a, b);
+    unpair(sum[1], c, d);
+    return (a + b) + (c + d);
+}
+
 // Which of the 32 keys from position `pos` on row `node` sees: the prefix, and the nodes of its mask.
 __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, int node, int pos) {
     const int m0 = pos - s.len;         // first node
@@ -229,6 +332,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         seg.next<kSegRing>();
     };
 
+    // the softmax warps, which keep a row's scores in registers, take registers of the others' (one instruction a warpgroup)
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == 3) {
         // ------------------------------------------------ scheduler
         Cursor cur{};
@@ -258,10 +364,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         const int boxes = kTcKeys / p.box_rows;
         while (ok && next_segment(s)) {
             const int total = s.len + s.n;
+            // a tile's pages are looked up while the tile before it is loaded
+            auto look_up = [&](int t) {
+                const int at = t * kTcKeys + lane * p.box_rows;
+                return t < s.tile1 && lane < boxes && at < total ? page_of(a, s.b, at) : -1;
+            };
+            int next_page = look_up(s.tile0);
             for (int t = s.tile0; t < s.tile1; ++t) {
                 const int pos = t * kTcKeys + lane * p.box_rows;
-                int page = -1;
-                if (lane < boxes && pos < total) page = page_of(a, s.b, pos);
+                const int page = next_page;
+                next_page = look_up(t + 1);
                 const int row = a.row0 + (page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
                 const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= 0)) * (uint32_t)(p.box_rows * (C::TILE / 128));
 #pragma unroll
@@ -383,17 +495,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             while (ok && next_segment(s)) {
                 const int total = s.len + s.n;
                 int eref = -1000;
+                // pages two tiles and scales one tile ahead
+                auto look_up = [&](int t) {
+                    const int at = t * kTcKeys + lane * 4;
+                    return t < s.tile1 && at < total ? page_of(a, s.b, at) : -1;
+                };
+                auto load = [&](int page, int t, uint32_t& kb, uint32_t& vb) {
+                    kb = vb = 0;
+                    if (page >= 0) {
+                        const long long at = ((long long)page * a.kv_heads + s.head) * a.page_size + ((t * kTcKeys + lane * 4) & (a.page_size - 1));
+                        kb = __ldg(reinterpret_cast<const uint32_t*>(a.k_scale + at));
+                        vb = __ldg(reinterpret_cast<const uint32_t*>(a.v_scale + at));
+                    }
+                };
+                uint32_t kb_next, vb_next;
+                load(look_up(s.tile0), s.tile0, kb_next, vb_next);
+                int next_page = look_up(s.tile0 + 1);
                 for (int t = s.tile0; t < s.tile1; ++t) {
                     const int pos = t * kTcKeys + lane * 4;
-                    uint32_t kb = 0, vb = 0;
-                    if (pos < total) {
-                        const int page = page_of(a, s.b, pos);
-                        if (page >= 0) {
-                            const long long at = ((long long)page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-                            kb = __ldg(reinterpret_cast<const uint32_t*>(a.k_scale + at));
-                            vb = __ldg(reinterpret_cast<const uint32_t*>(a.v_scale + at));
-                        }
-                    }
+                    uint32_t kb = kb_next, vb = vb_next;
+                    load(next_page, t + 1, kb_next, vb_next);
+                    next_page = look_up(t + 2);
                     if (pos + 4 > total) {
                         const int left = total - pos;       // positions of the four that exist
                         const uint32_t have = left <= 0 ? 0u : 0xffffffffu >> (8 * (4 - left));
@@ -427,8 +549,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             }
             if (!ok) *abort_flag = 1;
         }
+    }
     } else if (warp >= 12) {
         // ------------------------------------------------ q rows, and V tiles made ready
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         const int tid = threadIdx.x - 384;
         Ring rv, rc;
         uint32_t q_phase = 1;           // the first segment's q buffer is free
@@ -505,7 +629,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     if (!mbar_wait_warp(&m.c_empty[rc.i], rc.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
                     unsigned char* out = smem + C::OFF_C + rc.i * C::CONV;
                     constexpr int kUnits = D / 16;      // 16 codes become two 16-byte chunks
-#pragma unroll
+#pragma unroll 2
                     for (int u = tid; u < 128 * kUnits; u += kConvThreads) {
                         const int row = u / kUnits, c = u % kUnits;
                         uint4 w = *reinterpret_cast<const uint4*>(v + row * D + c * 16);
@@ -581,6 +705,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         if (!ok) *abort_flag = 1;
     } else {
         // ------------------------------------------------ softmax: group g of 4 warps, a thread per row
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         const int g = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const int tid = threadIdx.x - 128;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
@@ -628,26 +753,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         if (mine && e > eref) o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
                         eref = e;
                     }
-                    // the row's maximum
-                    float top = -INFINITY;
+                    float x[128];
+                    float top = load_scores<FP8>(s_t, x, m.kf[FP8 ? ra.i : 0]);
+                    if (drafted) {
+                        uint32_t see[4];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32];
-                        tmem_ld32(s_t + 32 * c, x);
-                        tmem_ld_wait();
-                        const uint32_t see = drafted ? sees32(a, s, node, pos0 + 32 * c) : 0xffffffffu;
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            const float4 kf = FP8 ? m.kf[ra.i][c * 8 + i / 4] : make_float4(1.f, 1.f, 1.f, 1.f);
-                            const float k4[4] = {kf.x, kf.y, kf.z, kf.w};
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                float v = __uint_as_float(x[i + j]);
-                                if (FP8) v *= k4[j];
-                                if (drafted && !(see >> (i + j) & 1)) v = -INFINITY;
-                                top = fmaxf(top, v);
-                            }
-                        }
+                        for (int c = 0; c < 4; ++c) see[c] = sees32(a, s, node, pos0 + 32 * c);
+                        top = mask_scores<FP8>(x, see);
                     }
                     top = top == -INFINITY ? top : top * f_row;
                     if (top > ref + (float)kLazy || ref == -INFINITY) {
@@ -657,43 +769,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         if (mine) o_mul *= f;
                     }
                     const float shift = ref == -INFINITY ? 0.f : -ref;
-                    // the weights, in place of the scores that are read already
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32], w[16];
-                        tmem_ld32(s_t + 32 * c, x);
-                        tmem_ld_wait();
-                        const uint32_t see = drafted ? sees32(a, s, node, pos0 + 32 * c) : 0xffffffffu;
-                        float sum[4] = {};
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            const float4 kf = FP8 ? m.kf[ra.i][c * 8 + i / 4] : make_float4(1.f, 1.f, 1.f, 1.f);
-                            const float4 vf = FP8 ? m.vf[ra.i][c * 8 + i / 4] : make_float4(1.f, 1.f, 1.f, 1.f);
-                            const float k4[4] = {kf.x, kf.y, kf.z, kf.w}, v4[4] = {vf.x, vf.y, vf.z, vf.w};
-                            float e[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                float v = __uint_as_float(x[i + j]);
-                                if (FP8) v *= k4[j];
-                                if (drafted && !(see >> (i + j) & 1)) v = -INFINITY;
-                                e[j] = exp2_approx(fmaf(v, f_row, shift));
-                                sum[j] += e[j];
-                                if (FP8) e[j] *= v4[j];
-                            }
-                            if constexpr (FP8) {
-                                const __half2 p0 = __floats2half2_rn(e[0], e[1]), p1 = __floats2half2_rn(e[2], e[3]);
-                                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
-                                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
-                            } else {
-                                const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
-                                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
-                                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
-                            }
-                        }
-                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                        tmem_st16(s_t + 16 * c, w);
-                    }
-                    tmem_st_wait();
+                    l += store_weights<FP8>(s_t, x, f_row, shift, m.vf[FP8 ? ra.i : 0]);
                 }
                 if (FP8) {
                     __syncwarp();
@@ -851,6 +927,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
 
 template <bool FP8, int D, int RT>
 cudaError_t tc_attr() {
+    // a split above what the block is launched with would wait for ever
+    cudaFuncAttributes f;
+    const cudaError_t e = cudaFuncGetAttributes(&f, k_attn_tc<FP8, D, RT>);
+    if (e != cudaSuccess) return e;
+    if (f.numRegs * kTcThreads < 256 * (kSoftRegs + kOtherRegs)) return cudaErrorLaunchOutOfResources;
     return raise_smem_limit(k_attn_tc<FP8, D, RT>, tc_smem<FP8, D, RT>());
 }
 
