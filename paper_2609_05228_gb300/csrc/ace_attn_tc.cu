@@ -78,17 +78,13 @@ static_assert(tc_smem<false, 128, 2>() <= 232448 && tc_smem<false, 128, 1>() <= 
 static_assert(tc_smem<true, 128, 2>() <= 232448 && tc_smem<true, 128, 1>() <= 232448, "shared memory");
 static_assert(tc_smem<false, 64, 2>() <= 232448 && tc_smem<true, 64, 2>() <= 232448, "shared memory");
 
-// Shared-memory descriptor, K-major rows of 64 bytes in the 64-byte swizzle (8-row atoms of 512 bytes).
-__device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t addr) {
-    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(512 >> 4) << 32 | (uint64_t)1 << 46 |
-           (uint64_t)4 << 61;
-}
-
-// V as stored: rows are K indices, 64-element blocks of 128-byte rows in the 128-byte swizzle, 16 KB apart.
-__device__ __forceinline__ uint64_t smem_desc_v(uint32_t addr) {
-    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)(16384 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
-           (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// Shared-memory descriptors by halves: the low word holds the address, to which a K step adds, and the leading byte
+// offset; the high one the stride byte offset, the version and the swizzle (2: 128 bytes, 4: 64 bytes).
+constexpr uint32_t desc_hi(uint32_t sbo, uint32_t swizzle) { return (sbo >> 4) | 1u << 14 | swizzle << 29; }
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return addr >> 4 | (lbo >> 4) << 16; }
+constexpr uint32_t kRows128 = desc_hi(1024, 2);     // K-major rows of 128 bytes, or V as stored (8 K indices to the next group)
+constexpr uint32_t kRows64 = desc_hi(512, 4);       // K-major rows of 64 bytes
+constexpr uint32_t kVBlock = 16384;                 // V: to the next 64 dimensions
 
 // Instruction descriptor: fp32 accumulator; type codes of A and B (kind::f16: 0 fp16, 1 bf16; kind::f8f6f4: 0 e4m3).
 __host__ __device__ constexpr uint32_t idesc_of(int type, int M, int N, bool b_mn) {
@@ -96,18 +92,26 @@ __host__ __device__ constexpr uint32_t idesc_of(int type, int M, int N, bool b_m
            ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc),
-        "r"(acc));
+template <bool F8>
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool acc) {
+    if constexpr (F8)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc),
+            "r"((uint32_t)acc));
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc),
+            "r"((uint32_t)acc));
 }
 
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+// A from TMEM.
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool acc) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc),
-        "r"(acc));
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc),
+        "r"((uint32_t)acc));
 }
 
 #define ACE_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
@@ -411,81 +415,81 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         }
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issuer
-        Ring rk, rv, rc;
-        uint32_t q_phase = 0, p_phase[2] = {0, 0};
-        bool ok = true;
-        Segment s;
-        while (ok && next_segment(s)) {
-            const int items = (s.tile1 - s.tile0) * RT;
-            if (!mbar_wait_warp(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
-            q_phase ^= 1u;
-            for (int i = 0; i <= items; ++i) {
-                if (i < items) {
-                    // S[i & 1] = Q K^T; the PV that read P from this buffer was issued before
+        if (elect_one()) {
+            Ring rk, rv;                        // rv: V's ring, as stored (plain) or as fp16 (fp8)
+            constexpr int NP = FP8 ? NC : NV, kVTile = FP8 ? C::CONV : C::TILE;
+            uint64_t* v_free = FP8 ? m.c_empty : m.v_empty;
+            uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit g of the two S buffers
+            const uint32_t q0 = desc_lo(smem_u32(smem), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
+            const uint32_t v0 = desc_lo(smem_u32(smem + (FP8 ? C::OFF_C : C::OFF_V)), kVBlock);
+            bool ok = true;
+            while (true) {
+                if (!mbar_wait_or_abort(&m.seg_full[seg.i], seg.phase, a.err, abort_flag)) { ok = false; break; }
+                if (!m.seg[seg.i].go) break;
+                const int items = (m.seg[seg.i].s.tile1 - m.seg[seg.i].s.tile0) * RT;
+                mbar_arrive(&m.seg_empty[seg.i]);
+                seg.next<kSegRing>();
+                if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
+                q_phase ^= 1u;
+                for (int i = 0; i <= items; ++i) {
                     const int rt = RT == 2 ? i & 1 : 0;
-                    if (rt == 0 && !mbar_wait_warp(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t q_addr = smem_u32(smem + rt * C::Q), k_addr = smem_u32(smem + C::OFF_K + rk.i * C::TILE);
+                    if (i < items) {
+                        // S[i & 1] = Q K^T; the product that read P from this buffer was issued before
+                        if (rt == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
+                        tc_fence_after();
                         const uint32_t d = tmem + (uint32_t)((i & 1) * 128);
+                        const uint32_t ql = q0 + (uint32_t)(rt * (C::Q >> 4)), kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4));
                         if constexpr (FP8) {
-                            constexpr uint32_t idesc = idesc_of(0, 128, 128, false);
 #pragma unroll
-                            for (int term = 0; term < 2; ++term) {
-                                const uint64_t ad = D == 128 ? smem_desc_sw128(q_addr + term * C::Q / 2) : smem_desc_sw64(q_addr + term * C::Q / 2);
-                                const uint64_t bd = D == 128 ? smem_desc_sw128(k_addr) : smem_desc_sw64(k_addr);
-#pragma unroll
-                                for (int kk = 0; kk < D / 32; ++kk) mma_f8(d, ad + 2 * kk, bd + 2 * kk, idesc, term || kk);
+                            for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
+                                const uint32_t st = kk % (D / 32) * 2;
+                                mma_ss<true>(d, ql + (kk < D / 32 ? 0 : C::Q >> 5) + st, kl + st, D == 128 ? kRows128 : kRows64,
+                                             idesc_of(0, 128, 128, false), kk > 0);
                             }
                         } else {
-                            constexpr uint32_t idesc = idesc_of(1, 128, 128, false);
 #pragma unroll
-                            for (int h = 0; h < kHalves; ++h) {
-                                const uint64_t ad = smem_desc_sw128(q_addr + h * 16384), bd = smem_desc_sw128(k_addr + h * 16384);
-#pragma unroll
-                                for (int kk = 0; kk < 4; ++kk) mma_bf16(d, ad + 2 * kk, bd + 2 * kk, idesc, h || kk);
+                            for (int kk = 0; kk < D / 16; ++kk) {
+                                const uint32_t st = (kk >> 2) * (16384 >> 4) + (kk & 3) * 2;
+                                mma_ss<false>(d, ql + st, kl + st, kRows128, idesc_of(1, 128, 128, false), kk > 0);
                             }
                         }
                         mma_commit(&m.s_full[i & 1]);
-                        if (rt == RT - 1) mma_commit(&m.k_empty[rk.i]);
+                        if (rt == RT - 1) {
+                            mma_commit(&m.k_empty[rk.i]);
+                            rk.next<NK>();
+                        }
                         if (i == items - 1) mma_commit(&m.q_free);
                     }
-                    __syncwarp();
-                    if (rt == RT - 1) rk.next<NK>();
-                }
-                if (i > 0) {
-                    // O[j & 1] += P V
-                    const int j = i - 1, rt = RT == 2 ? j & 1 : 0;
-                    Ring& r = FP8 ? rc : rv;
-                    if (!mbar_wait_warp(&m.p_ready[j & 1], p_phase[j & 1], a.err, abort_flag)) { ok = false; break; }
-                    p_phase[j & 1] ^= 1u;
-                    if (rt == 0 && !mbar_wait_warp(&m.v_ready[r.i], r.phase, a.err, abort_flag)) { ok = false; break; }
-                    tc_fence_after();
-                    if (elect_one()) {
-                        constexpr uint32_t idesc = idesc_of(FP8 ? 0 : 1, 128, D, true);
-                        const uint32_t v_addr = smem_u32(smem + (FP8 ? C::OFF_C + r.i * C::CONV : C::OFF_V + r.i * C::TILE));
-                        const uint64_t bd = smem_desc_v(v_addr);
-                        const uint32_t d = tmem + kO + (uint32_t)((j & 1) * D), pa = tmem + (uint32_t)((j & 1) * 128);
+                    if (i > 0) {
+                        // O[j & 1] += P V, j = i - 1
+                        const int j = i - 1, g = j & 1;
+                        const bool last = RT == 1 || g == 1;
+                        if (!mbar_wait_or_abort(&m.p_ready[g], p_phase >> g & 1u, a.err, abort_flag)) { ok = false; break; }
+                        p_phase ^= 1u << g;
+                        if ((RT == 1 || g == 0) && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t vl = v0 + (uint32_t)(rv.i * (kVTile >> 4));
+                        const uint32_t d = tmem + kO + (uint32_t)(g * D), pa = tmem + (uint32_t)(g * 128);
 #pragma unroll
-                        for (int kk = 0; kk < 8; ++kk) mma_ts(d, pa + 8 * kk, bd + 128 * kk, idesc, j >= 2 || kk > 0);
-                        mma_commit(&m.o_done[j & 1]);
-                        if (rt == RT - 1) mma_commit(FP8 ? &m.c_empty[r.i] : &m.v_empty[r.i]);
-                    }
-                    __syncwarp();
-                    if (rt == RT - 1) {
-                        if (FP8) rc.next<NC ? NC : 1>(); else rv.next<NV>();
+                        for (int kk = 0; kk < 8; ++kk)
+                            mma_ts(d, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j >= 2 || kk > 0);
+                        mma_commit(&m.o_done[g]);
+                        if (last) {
+                            mma_commit(&v_free[rv.i]);
+                            rv.next<NP>();
+                        }
                     }
                 }
+                if (!ok) break;
             }
-            if (ok) segment_done();
+            if (!ok) *abort_flag = 1;
+            if (*abort_flag) {
+                // products in flight read shared memory and TMEM
+                mma_commit(&m.drain);
+                mbar_wait(&m.drain, 0, a.err);
+            }
         }
-        if (!ok) *abort_flag = 1;
-        if (*abort_flag) {
-            // products in flight read shared memory and TMEM
-            if (elect_one()) mma_commit(&m.drain);
-            __syncwarp();
-            mbar_wait(&m.drain, 0, a.err);
-        }
+        __syncwarp();
     } else if (warp == 2) {
         // ------------------------------------------------ scales of fp8 rows: 4 positions a lane
         if constexpr (FP8) {
