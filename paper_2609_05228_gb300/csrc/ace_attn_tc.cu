@@ -263,6 +263,16 @@ __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, 
     return r;
 }
 
+// 8 elements of a unit's q row (bf16), from dimension d on.
+__device__ __forceinline__ uint4 load_q(const AttnArgs& a, const Segment& s, int row, int d) {
+    const int nd = row / a.group;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (s.node0 + nd) * a.q_token_stride +
+                               (s.head * a.group + row - nd * a.group) * a.q_head_stride + d;
+    if ((uintptr_t)src % 16 == 0) return __ldg(reinterpret_cast<const uint4*>(src));
+    const uint16_t* u = reinterpret_cast<const uint16_t*>(src);
+    return make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
+}
+
 struct Ring {
     int i = 0;
     uint32_t phase = 0;
@@ -568,55 +578,55 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
             // (rows of the block past the unit's keep what they hold: rows of S, P and O do not mix)
-            for (int r0 = 0; r0 < s.rows; r0 += 128 / kChunks) {
-                const int r = r0 + tid / kChunks, c = tid % kChunks;
-                float f[8] = {};
-                if (r < s.rows) {
-                    const int row = s.row0 + r;
-                    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (s.node0 + row / a.group) * a.q_token_stride +
-                                               (s.head * a.group + row % a.group) * a.q_head_stride + c * 8;
-                    if ((uintptr_t)src % 16 == 0) {
-                        Vec16<__nv_bfloat16>::to_float(__ldg(reinterpret_cast<const uint4*>(src)), f);
-                    } else {
+            constexpr int kStep = 128 / kChunks, kBatch = 4;        // rows a pass; passes whose loads are under way together
+            for (int b0 = 0; b0 < s.rows; b0 += kStep * kBatch) {
+                uint4 qv[kBatch];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = to_f32(src[i]);
-                    }
+                for (int j = 0; j < kBatch; ++j) {
+                    const int r = b0 + j * kStep + tid / kChunks;
+                    qv[j] = r < s.rows ? load_q(a, s, s.row0 + r, tid % kChunks * 8) : make_uint4(0, 0, 0, 0);
                 }
-                unsigned char* tile = smem + (r >> 7) * C::Q;
-                const int rr = r & 127;
-                if constexpr (FP8) {
-                    float amax = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = finite_or_nan(f[i] * q_mul), amax = fmaxf(amax, fabsf(f[i]));
+                for (int j = 0; j < kBatch; ++j) {
+                    const int r = b0 + j * kStep + tid / kChunks, c = tid % kChunks;
+                    float f[8];
+                    Vec16<__nv_bfloat16>::to_float(qv[j], f);
+                    unsigned char* tile = smem + (r >> 7) * C::Q;
+                    const int rr = r & 127;
+                    if constexpr (FP8) {
+                        float amax = 0.f;
 #pragma unroll
-                    for (int o = kChunks / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                    const int byte = e4m3_scale_byte(amax);
-                    const float mul = pow2_of_minus_byte(byte);
-                    uint32_t hi[4], lo[4];
+                        for (int i = 0; i < 8; ++i) f[i] = finite_or_nan(f[i] * q_mul), amax = fmaxf(amax, fabsf(f[i]));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float x = f[2 * i] * mul, y = f[2 * i + 1] * mul;
-                        hi[i] = e4m3x2(x, y);
-                        const uint32_t h = f16x2_of_e4m3x2(hi[i]);
-                        const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                        lo[i] = e4m3x2(x - back.x, y - back.y);
+                        for (int o = kChunks / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                        const int byte = e4m3_scale_byte(amax);
+                        const float mul = pow2_of_minus_byte(byte);
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = f[2 * i] * mul, y = f[2 * i + 1] * mul;
+                            hi[i] = e4m3x2(x, y);
+                            const uint32_t h = f16x2_of_e4m3x2(hi[i]);
+                            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                            lo[i] = e4m3x2(x - back.x, y - back.y);
+                        }
+                        // 8 bytes of a 16-byte chunk
+                        const int ch = c >> 1;
+                        const uint32_t off = D == 128 ? (uint32_t)rr * 128u + (uint32_t)((ch ^ (rr & 7)) << 4)
+                                                      : (uint32_t)rr * 64u + (uint32_t)((ch ^ ((rr >> 1) & 3)) << 4);
+                        *reinterpret_cast<uint2*>(tile + off + (c & 1) * 8) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                        *reinterpret_cast<uint2*>(tile + C::Q / 2 + off + (c & 1) * 8) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                        if (c == 0) m.q_scale[seg.i & 1][r] = pow2_of_byte(byte);
+                    } else {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
+                            w[i] = *reinterpret_cast<const uint32_t*>(&v);
+                        }
+                        *reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
+                            make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                    // 8 bytes of a 16-byte chunk
-                    const int ch = c >> 1;
-                    const uint32_t off = D == 128 ? (uint32_t)rr * 128u + (uint32_t)((ch ^ (rr & 7)) << 4)
-                                                  : (uint32_t)rr * 64u + (uint32_t)((ch ^ ((rr >> 1) & 3)) << 4);
-                    *reinterpret_cast<uint2*>(tile + off + (c & 1) * 8) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                    *reinterpret_cast<uint2*>(tile + C::Q / 2 + off + (c & 1) * 8) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-                    if (c == 0) m.q_scale[seg.i & 1][r] = pow2_of_byte(byte);
-                } else {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
-                        w[i] = *reinterpret_cast<const uint32_t*>(&v);
-                    }
-                    *reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
-                        make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
             fence_async_smem();
