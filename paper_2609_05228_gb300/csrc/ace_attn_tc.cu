@@ -20,9 +20,11 @@
 namespace ace {
 namespace {
 
-constexpr int kTcKeys = 128, kTcThreads = 512, kSegRing = 4, kAuxRing = 3;
-constexpr int kLazy = 8;                // the reference maximum moves once a row's maximum is 2^8 above it
-constexpr int kPUp = 6;                 // fp16 weights carry a factor 2^6: up to 2^(kLazy + kPUp), 2^-14 is normal
+constexpr int kTcKeys = 128, kTcThreads = 512, kSegRing = 4, kAuxRing = 4;
+// A row's reference is its maximum less kPUp when it is set, and moves once the maximum is kLazy above that
+// (base 2): weights are at most 2^(kLazy + kPUp), which fp16 holds, and normal in fp16 down to 2^-(14 + kPUp) of the largest.
+constexpr int kLazy = 8, kPUp = 6;
+constexpr int kVUp = 6;                 // fp16 rows of V are code * 2^(e - eref + kVUp): at most 448 * 2^6, eref >= e
 constexpr int kConvThreads = 128;
 constexpr int kSoftRegs = 184, kOtherRegs = 72;
 static_assert(256 * (kSoftRegs + kOtherRegs) <= kTcThreads * 128, "the split must fit the launch's registers");
@@ -42,12 +44,13 @@ struct Cfg {
     static constexpr int TILE = 128 * D * (FP8 ? 1 : 2);
     static constexpr int CONV = FP8 ? 128 * D * 2 : 0;  // V as fp16
     static constexpr int NC = FP8 ? 2 : 0;
-    static constexpr int NK = D == 64 ? (FP8 ? 6 : 4) : FP8 && RT == 1 ? 4 : 3;
+    static constexpr int NK = D == 64 ? (FP8 ? 6 : 4) : 3;
     static constexpr int NV = D == 64 ? (FP8 ? 6 : 4) : FP8 && RT == 1 ? 3 : 2;
     static constexpr int OFF_K = RT * Q;
     static constexpr int OFF_V = OFF_K + NK * TILE;
     static constexpr int OFF_C = OFF_V + NV * TILE;
-    static constexpr int OFF_MISC = OFF_C + NC * CONV;
+    static constexpr int OFF_MERGE = OFF_C + NC * CONV;     // RT = 1: 16 dimensions of each group's 128 rows of O
+    static constexpr int OFF_MISC = OFF_MERGE + (RT == 1 ? 2 * 128 * 16 * 4 : 0);
 };
 
 struct TcSegment {
@@ -59,7 +62,7 @@ struct TcSegment {
 template <bool FP8, int RT>
 struct Misc {
     uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], v_ready[6], c_empty[2];
-    uint64_t s_full[2], p_ready[2], o_done[2], q_full, q_free, soft, drain;
+    uint64_t s_full[2], p_ready[2], o_done[2], q_full, q_free, soft, group[2], drain;
     uint64_t seg_full[kSegRing], seg_empty[kSegRing], aux_full[kAuxRing], aux_empty[kAuxRing];
     uint32_t tmem;
     int abort_flag, joins, pad;
@@ -67,7 +70,8 @@ struct Misc {
     float2 ml[RT == 1 ? 256 : 1];               // RT = 1: both halves' running maximum and sum
     int eref1[RT == 1 ? 2 : 1];
     float q_scale[2][FP8 ? 128 * RT : 1];       // by turns of segments: softmax may be one behind
-    float4 kf[FP8 ? kAuxRing : 1][FP8 ? 32 : 1], vf[FP8 ? kAuxRing : 1][FP8 ? 32 : 1];   // 128 factors a tile
+    float4 kf[FP8 ? kAuxRing : 1][FP8 ? 32 : 1];            // 128 factors a tile
+    __half vf[FP8 ? kAuxRing : 1][FP8 ? 128 : 1];
     int eref[kAuxRing];
 };
 
@@ -172,84 +176,6 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     return r;
 }
 
-// A row's 128 scores from TMEM, with fp8 rows' scales; returns their maximum. The scores stay in registers.
-template <bool FP8>
-__device__ __forceinline__ float load_scores(uint32_t s_t, float (&x)[128], const float4* kf) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        uint32_t* r = reinterpret_cast<uint32_t*>(x) + 32 * c;
-        tmem_ld32(s_t + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(r));
-    }
-    tmem_ld_wait();
-    if (FP8) {
-#pragma unroll
-        for (int i = 0; i < 128; i += 4) {
-            const float4 k = kf[i / 4];
-            unpair(mul2(pair(x[i], x[i + 1]), pair(k.x, k.y)), x[i], x[i + 1]);
-            unpair(mul2(pair(x[i + 2], x[i + 3]), pair(k.z, k.w)), x[i + 2], x[i + 3]);
-        }
-    }
-    float top[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-    for (int i = 4; i < 128; i += 8) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], i + 4 + j < 128 ? fmaxf(x[i + j], x[i + 4 + j]) : x[i + j]);
-    }
-    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-}
-
-// The same where not every position counts.
-template <bool FP8>
-__device__ __forceinline__ float mask_scores(float (&x)[128], const uint32_t (&see)[4]) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 128; ++i) {
-        x[i] = see[i >> 5] >> (i & 31) & 1 ? x[i] : -INFINITY;
-        top = fmaxf(top, x[i]);
-    }
-    return top;
-}
-
-// P = 2^(x f + shift) to TMEM (with the scales of fp8 rows of V), over the scores that are read already; returns the sum of P.
-template <bool FP8>
-__device__ __forceinline__ float store_weights(uint32_t s_t, const float (&x)[128], float f, float shift, const float4* vf) {
-    const uint64_t f2 = pair(f, f), shift2 = pair(shift, shift);
-    uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        uint32_t w[16];
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            float e[4];
-            unpair(fma2(pair(x[32 * c + i], x[32 * c + i + 1]), f2, shift2), e[0], e[1]);
-            unpair(fma2(pair(x[32 * c + i + 2], x[32 * c + i + 3]), f2, shift2), e[2], e[3]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]);
-            const uint64_t e01 = pair(e[0], e[1]), e23 = pair(e[2], e[3]);
-            sum[0] = add2(sum[0], e01);
-            sum[1] = add2(sum[1], e23);
-            if constexpr (FP8) {
-                const float4 v = vf[c * 8 + i / 4];
-                unpair(mul2(e01, pair(v.x, v.y)), e[0], e[1]);
-                unpair(mul2(e23, pair(v.z, v.w)), e[2], e[3]);
-                const __half2 p0 = __floats2half2_rn(e[0], e[1]), p1 = __floats2half2_rn(e[2], e[3]);
-                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
-                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
-            } else {
-                const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
-                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
-                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
-            }
-        }
-        tmem_st16(s_t + 16 * c, w);
-    }
-    tmem_st_wait();
-    float a, b, c, d;
-    unpair(sum[0], a, b);
-    unpair(sum[1], c, d);
-    return (a + b) + (c + d);
-}
-
 // Which of the 32 keys from position `pos` on row `node` sees: the prefix, and the nodes of its mask.
 __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, int node, int pos) {
     const int m0 = pos - s.len;         // first node
@@ -263,6 +189,153 @@ __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, 
     return r;
 }
 
+// N of a row's scores from TMEM, with fp8 rows' scales; returns their maximum. The scores stay in registers.
+template <bool FP8, int N>
+__device__ __forceinline__ float load_scores(uint32_t s_t, float (&x)[N], const float4* kf) {
+#pragma unroll
+    for (int c = 0; c < N / 32; ++c) {
+        uint32_t* r = reinterpret_cast<uint32_t*>(x) + 32 * c;
+        tmem_ld32(s_t + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(r));
+    }
+    float4 k[8];
+    if (FP8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] = kf[i];
+    }
+    tmem_ld_wait();
+    if (FP8) {
+#pragma unroll
+        for (int c = 0; c < N / 32; ++c) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float* y = x + 32 * c + 4 * i;
+                unpair(mul2(pair(y[0], y[1]), pair(k[i].x, k[i].y)), y[0], y[1]);
+                unpair(mul2(pair(y[2], y[3]), pair(k[i].z, k[i].w)), y[2], y[3]);
+                if (c + 1 < N / 32) k[i] = kf[8 * (c + 1) + i];
+            }
+        }
+    }
+    float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int i = 4; i < N; i += 8) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], i + 4 + j < N ? fmaxf(x[i + j], x[i + 4 + j]) : x[i + j]);
+    }
+    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+
+// The same where not every position counts.
+template <int N>
+__device__ __forceinline__ float mask_scores(float (&x)[N], const uint32_t (&see)[N / 32]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = see[i >> 5] >> (i & 31) & 1 ? x[i] : -INFINITY;
+        top = fmaxf(top, x[i]);
+    }
+    return top;
+}
+
+// P = 2^(x f + shift) to TMEM; returns the sum of P.
+template <bool FP8, int N>
+__device__ __forceinline__ float store_weights(uint32_t p_t, const float (&x)[N], float f, float shift) {
+    const uint64_t f2 = pair(f, f), shift2 = pair(shift, shift);
+    uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+    for (int c = 0; c < N / 32; ++c) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            float e[4];
+            unpair(fma2(pair(x[32 * c + i], x[32 * c + i + 1]), f2, shift2), e[0], e[1]);
+            unpair(fma2(pair(x[32 * c + i + 2], x[32 * c + i + 3]), f2, shift2), e[2], e[3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]);
+            sum[0] = add2(sum[0], pair(e[0], e[1]));
+            sum[1] = add2(sum[1], pair(e[2], e[3]));
+            if constexpr (FP8) {
+                const __half2 p0 = __floats2half2_rn(e[0], e[1]), p1 = __floats2half2_rn(e[2], e[3]);
+                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+            } else {
+                const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
+                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+            }
+        }
+        tmem_st16(p_t + 16 * c, w);
+    }
+    float a, b, c, d;
+    unpair(sum[0], a, b);
+    unpair(sum[1], c, d);
+    return (a + b) + (c + d);
+}
+
+// A thread's row of the running softmax.
+struct RowState {
+    float ref, l, o_mul;                // reference, sum, what O has to be multiplied with
+};
+
+// One tile of a row: N scores from column `col` on become weights; the row's other columns of P are zero.
+template <bool FP8, int N>
+__device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s, uint32_t s_t, int col, const float4* kf, bool drafted,
+                                             int node, int pos0, float f_row, bool first, RowState& st) {
+    float x[N];
+    float top = load_scores<FP8, N>(s_t + col, x, kf + col / 4);
+    if (drafted) {
+        uint32_t see[N / 32];
+#pragma unroll
+        for (int c = 0; c < N / 32; ++c) see[c] = sees32(a, s, node, pos0 + col + 32 * c);
+        top = mask_scores<N>(x, see);
+    }
+    top = top == -INFINITY ? top : top * f_row;
+    constexpr float kUp = FP8 ? (float)kPUp : 0.f;
+    if (top > st.ref + (float)kLazy + kUp || st.ref == -INFINITY) {
+        const float ref = top - kUp;
+        const float f = st.ref == -INFINITY ? 0.f : exp2_approx(st.ref - ref);
+        st.ref = ref;
+        st.l *= f;
+        if (!first) st.o_mul *= f;
+    }
+    const float shift = st.ref == -INFINITY ? 0.f : -st.ref;
+    st.l += store_weights<FP8, N>(s_t + col / 2, x, f_row, shift);
+    if constexpr (N < 128) {
+        const uint32_t zero[16] = {};
+#pragma unroll
+        for (int c = 0; c < 64; c += 16)
+            if (c < col / 2 || c >= col / 2 + N / 2) tmem_st16(s_t + c, zero);
+    }
+    tmem_st_wait();
+}
+
+// Values of V that are not finite were left out of the products: what they add to dimensions d .. d + 3 of a row that sees them.
+template <bool FP8>
+__device__ __noinline__ float4 add_not_finite(const AttnArgs& a, const Segment& s, const unsigned long long* bad, int node, int d, float4 sum) {
+    float o[4] = {sum.x, sum.y, sum.z, sum.w};
+    for (int w = 0; w < kMaxNodes / 64; ++w) {
+        unsigned long long b = bad[w];
+        if (b) b &= sees_word(a, s.node0, s.n, node, w);
+        while (b) {
+            const int pos = s.len + w * 64 + __ffsll((long long)b) - 1;
+            b &= b - 1;
+            const int page = page_of(a, s.b, pos);
+            if (page < 0) continue;
+            const long long row = ((long long)page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (FP8) {
+                    const uint8_t code = static_cast<const uint8_t*>(a.v_pool)[row * a.head_dim + d + i];
+                    if ((code & 0x7f) == 0x7f) o[i] = __uint_as_float(0x7fffffffu);
+                } else {
+                    const float v = to_f32(static_cast<const __nv_bfloat16*>(a.v_pool)[row * a.head_dim + d + i]);
+                    if (!(fabsf(v) < INFINITY)) o[i] += v;
+                }
+            }
+        }
+    }
+    return make_float4(o[0], o[1], o[2], o[3]);
+}
+
 // 8 elements of a unit's q row (bf16), from dimension d on.
 __device__ __forceinline__ uint4 load_q(const AttnArgs& a, const Segment& s, int row, int d) {
     const int nd = row / a.group;
@@ -272,6 +345,10 @@ __device__ __forceinline__ uint4 load_q(const AttnArgs& a, const Segment& s, int
     const uint16_t* u = reinterpret_cast<const uint16_t*>(src);
     return make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
 }
+
+// With few rows (RT = 1) the block holds them 2 or 4 times, 64 or 32 lanes apart, and each copy's warps take that
+// share of a tile's columns: the tile's softmax takes as much less time, and the copies' O are added at the end.
+__device__ __forceinline__ int copies_of(int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
 
 struct Ring {
     int i = 0;
@@ -306,6 +383,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         }
         mbar_init(&m.q_full, 4);
         mbar_init(&m.soft, 8);
+        mbar_init(&m.group[0], 4), mbar_init(&m.group[1], 4);
         mbar_init(&m.q_free, 1);
         mbar_init(&m.drain, 1);
         for (int i = 0; i < kSegRing; ++i) {
@@ -314,7 +392,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         }
         for (int i = 0; i < kAuxRing; ++i) {
             mbar_init(&m.aux_full[i], 1);
-            mbar_init(&m.aux_empty[i], 4 * RT);
+            mbar_init(&m.aux_empty[i], 4 * RT + 4);
         }
         m.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -543,17 +621,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
                     // two octaves of room, so that small differences between tiles do not move it
                     if (top - 127 > eref) eref = top - 127 + 2;
-                    float kf[4], vf[4];
+                    float kf[4];
+                    alignas(8) __half vf[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int vbyte = (int)(vb >> (8 * i) & 0xff);
                         kf[i] = pow2_of_byte((int)(kb >> (8 * i) & 0xff));
-                        const int e = vbyte - eref + kPUp;      // 2^(e_j - eref + kPUp), biased exponent
-                        vf[i] = vbyte == 0 || e <= 0 ? 0.f : pow2_of_byte(e);
+                        const int e = vbyte - eref + kVUp;      // 2^(e_j - eref + kVUp), biased exponent
+                        vf[i] = __float2half_rn(vbyte == 0 || e <= 0 ? 0.f : pow2_of_byte(e));
                     }
                     if (!mbar_wait_warp(&m.aux_empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
                     m.kf[r.i][lane] = make_float4(kf[0], kf[1], kf[2], kf[3]);
-                    m.vf[r.i][lane] = make_float4(vf[0], vf[1], vf[2], vf[3]);
+                    *reinterpret_cast<uint2*>(&m.vf[r.i][lane * 4]) = *reinterpret_cast<const uint2*>(vf);
                     if (lane == 0) m.eref[r.i] = eref;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&m.aux_full[r.i]);
@@ -568,7 +647,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         // ------------------------------------------------ q rows, and V tiles made ready
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         const int tid = threadIdx.x - 384;
-        Ring rv, rc;
+        Ring rv, rc, ra;
         uint32_t q_phase = 1;           // the first segment's q buffer is free
         bool ok = true;
         Segment s;
@@ -577,8 +656,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             q_phase ^= 1u;
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
-            // (rows of the block past the unit's keep what they hold: rows of S, P and O do not mix)
             constexpr int kStep = 128 / kChunks, kBatch = 4;        // rows a pass; passes whose loads are under way together
+            const int copies = RT == 1 ? copies_of(s.rows) : 1, apart = 128 / copies;
+            // (rows of the block past the unit's keep what they hold: rows of S, P and O do not mix)
             for (int b0 = 0; b0 < s.rows; b0 += kStep * kBatch) {
                 uint4 qv[kBatch];
 #pragma unroll
@@ -592,7 +672,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     float f[8];
                     Vec16<__nv_bfloat16>::to_float(qv[j], f);
                     unsigned char* tile = smem + (r >> 7) * C::Q;
-                    const int rr = r & 127;
                     if constexpr (FP8) {
                         float amax = 0.f;
 #pragma unroll
@@ -610,22 +689,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                             const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
                             lo[i] = e4m3x2(x - back.x, y - back.y);
                         }
+                        if (r >= s.rows) continue;
                         // 8 bytes of a 16-byte chunk
                         const int ch = c >> 1;
-                        const uint32_t off = D == 128 ? (uint32_t)rr * 128u + (uint32_t)((ch ^ (rr & 7)) << 4)
-                                                      : (uint32_t)rr * 64u + (uint32_t)((ch ^ ((rr >> 1) & 3)) << 4);
-                        *reinterpret_cast<uint2*>(tile + off + (c & 1) * 8) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                        *reinterpret_cast<uint2*>(tile + C::Q / 2 + off + (c & 1) * 8) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                        for (int rr = r & 127, k = 0; k < copies; ++k, rr += apart) {
+                            const uint32_t off = D == 128 ? (uint32_t)rr * 128u + (uint32_t)((ch ^ (rr & 7)) << 4)
+                                                          : (uint32_t)rr * 64u + (uint32_t)((ch ^ ((rr >> 1) & 3)) << 4);
+                            *reinterpret_cast<uint2*>(tile + off + (c & 1) * 8) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                            *reinterpret_cast<uint2*>(tile + C::Q / 2 + off + (c & 1) * 8) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                        }
                         if (c == 0) m.q_scale[seg.i & 1][r] = pow2_of_byte(byte);
                     } else {
+                        if (r >= s.rows) continue;
                         uint32_t w[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
                             w[i] = *reinterpret_cast<const uint32_t*>(&v);
                         }
-                        *reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
-                            make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int rr = r & 127, k = 0; k < copies; ++k, rr += apart)
+                            *reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
+                                make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
             }
@@ -641,6 +725,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 unsigned char* v = smem + C::OFF_V + rv.i * C::TILE;
                 if constexpr (FP8) {
                     if (!mbar_wait_warp(&m.c_empty[rc.i], rc.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait_warp(&m.aux_full[ra.i], ra.phase, a.err, abort_flag)) { ok = false; break; }
                     unsigned char* out = smem + C::OFF_C + rc.i * C::CONV;
                     constexpr int kUnits = D / 16;      // 16 codes become two 16-byte chunks
 #pragma unroll 2
@@ -669,6 +754,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         uint32_t h[8];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) h[2 * i] = f16x2_of_e4m3x2(x[i] & 0xffffu), h[2 * i + 1] = f16x2_of_e4m3x2(x[i] >> 16);
+                        const __half2 f2 = __half2half2(m.vf[ra.i][row]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h[i]), f2);
+                            h[i] = *reinterpret_cast<const uint32_t*>(&y);
+                        }
                         unsigned char* dst = out + (c >> 2) * 16384 + row * 128;
                         const int c0 = (c & 3) * 2;
                         // the upper half's threads write their chunks in the other order: distinct banks
@@ -682,7 +773,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     if (lane == 0) {
                         mbar_arrive(&m.v_ready[rc.i]);
                         mbar_arrive(&m.v_empty[rv.i]);
+                        mbar_arrive(&m.aux_empty[ra.i]);
                     }
+                    ra.next<kAuxRing>();
                     rc.next<NC ? NC : 1>();
                 } else {
                     if (drafted) {
@@ -733,18 +826,28 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             return mbar_wait_warp(&m.soft, soft_phase ^ 1u, a.err, abort_flag);
         };
         Ring ra;
+        uint32_t group_phase = 0;
+        // this group's four warps meet
+        auto group_sync = [&]() -> bool {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.group[g]);
+            group_phase ^= 1u;
+            return mbar_wait_warp(&m.group[g], group_phase ^ 1u, a.err, abort_flag);
+        };
         bool ok = true;
         Segment s;
         while (ok && next_segment(s)) {
-            const int row = RT == 2 ? g * 128 + r : r;          // of the unit
+            const int copies = RT == 1 ? copies_of(s.rows) : 1, apart = 128 / copies;
+            const int row = RT == 2 ? g * 128 + r : r & (apart - 1);        // of the unit
+            const int col = RT == 2 ? 0 : r / apart * apart;                // first column of this copy
             const bool live = row < s.rows;
-            const bool warp_live = (RT == 2 ? g * 128 : 0) + quad * 32 < s.rows;
+            const bool warp_live = row - lane < s.rows;
             const int node = live ? (s.row0 + row) / a.group : 0;
             const int hq = s.head * a.group + (live ? (s.row0 + row) % a.group : 0);
             const int tiles = s.tile1 - s.tile0;
             const float f_row0 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
             float f_row = f_row0;
-            float ref = -INFINITY, l = 0.f;
+            RowState st{-INFINITY, 0.f, 1.f};
             int eref = 0;
             int mine = 0;               // tiles of this group so far
             for (int t = 0; t < tiles; ++t) {
@@ -759,31 +862,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 if (!mbar_wait_warp(&m.s_full[g], s_phase, a.err, abort_flag)) { ok = false; break; }
                 s_phase ^= 1u;
                 tc_fence_after();
-                float o_mul = 1.f;
+                st.o_mul = 1.f;
                 if (warp_live) {
+                    const float4* kf = m.kf[FP8 ? ra.i : 0];
                     if (FP8) {
                         f_row = fmaxf(f_row0 * m.q_scale[seg.i & 1][row], 0x1p-126f);     // 0 times a masked -inf is no score
                         const int e = m.eref[ra.i];
-                        if (mine && e > eref) o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
+                        if (mine && e > eref) st.o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
                         eref = e;
                     }
-                    float x[128];
-                    float top = load_scores<FP8>(s_t, x, m.kf[FP8 ? ra.i : 0]);
-                    if (drafted) {
-                        uint32_t see[4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) see[c] = sees32(a, s, node, pos0 + 32 * c);
-                        top = mask_scores<FP8>(x, see);
-                    }
-                    top = top == -INFINITY ? top : top * f_row;
-                    if (top > ref + (float)kLazy || ref == -INFINITY) {
-                        const float f = ref == -INFINITY ? 0.f : exp2_approx(ref - top);
-                        ref = top;
-                        l *= f;
-                        if (mine) o_mul *= f;
-                    }
-                    const float shift = ref == -INFINITY ? 0.f : -ref;
-                    l += store_weights<FP8>(s_t, x, f_row, shift, m.vf[FP8 ? ra.i : 0]);
+                    if (copies == 1) softmax_tile<FP8, 128>(a, s, s_t, 0, kf, drafted, node, pos0, f_row, !mine, st);
+                    else if (RT == 1 && copies == 2) softmax_tile<FP8, 64>(a, s, s_t, col, kf, drafted, node, pos0, f_row, !mine, st);
+                    else if (RT == 1) softmax_tile<FP8, 32>(a, s, s_t, col, kf, drafted, node, pos0, f_row, !mine, st);
                 }
                 if (FP8) {
                     __syncwarp();
@@ -794,7 +884,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 if (mine) {
                     if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
                     o_phase ^= 1u;
-                    if (__any_sync(0xffffffffu, o_mul != 1.f)) {
+                    if (__any_sync(0xffffffffu, st.o_mul != 1.f)) {
                         tc_fence_after();
 #pragma unroll
                         for (int c = 0; c < D / 32; ++c) {
@@ -802,7 +892,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                             tmem_ld32(o_t + 32 * c, x);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * o_mul);
+                            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * st.o_mul);
                             tmem_st32(o_t + 32 * c, x);
                         }
                         tmem_st_wait();
@@ -820,101 +910,111 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             }
             tc_fence_after();
             // ---------------- the unit's result, or this CTA's part of it
-            float up0 = 1.f, up1 = 0.f;         // factors of O0 and O1 (RT = 1), of this group's O (RT = 2: up0)
-            float m_all = ref, l_all = l;
-            int c0 = 0, c1 = D;                 // dimensions of this thread
-            uint32_t ta = o_t, tb = o_t;
-            const float unit = FP8 ? exp2f((float)(eref - kPUp)) : 1.f;
+            const bool whole = s.part < 0;
+            const long long at = (long long)(s.node0 + node) * a.n_heads + hq;
+            float up0, up1 = 0.f;               // factors of O0 and O1 (RT = 1), of this group's O (RT = 2: up0)
+            float m_all = st.ref, l_all = st.l;
             if constexpr (RT == 1) {
-                m.ml[g * 128 + r] = make_float2(ref, l);
+                m.ml[g * 128 + r] = make_float2(st.ref, st.l);
                 if (r == 0) m.eref1[g] = eref;
                 if (!soft_sync()) { ok = false; break; }
-                const float2 x = m.ml[r], y = m.ml[128 + r];
-                m_all = fmaxf(x.x, y.x);
+                // over both accumulators and all copies of the row
+                m_all = -INFINITY;
+                for (int k = row; k < 256; k += apart) m_all = fmaxf(m_all, m.ml[k].x);
                 const float z = m_all == -INFINITY ? 0.f : m_all;
-                up0 = exp2f(x.x - z);
-                up1 = exp2f(y.x - z);
-                l_all = x.y * up0 + y.y * up1;
+                l_all = 0.f;
+                for (int k = row; k < 256; k += apart) l_all += m.ml[k].y * exp2f(m.ml[k].x - z);
+                up0 = exp2f(m.ml[r].x - z);
+                up1 = tiles > 1 ? exp2f(m.ml[128 + r].x - z) : 0.f;
                 if (FP8) {
-                    up0 *= exp2f((float)(m.eref1[0] - kPUp));
-                    up1 *= exp2f((float)(m.eref1[1] - kPUp));
+                    up0 *= exp2f((float)(m.eref1[0] - kVUp));
+                    up1 *= exp2f((float)(m.eref1[1] - kVUp));
                 }
-                if (tiles < 2) up1 = 0.f;
-                ta = tmem + lanes + kO;
-                tb = ta + D;
-                c0 = g * (D / 2);
-                c1 = c0 + D / 2;
             } else {
-                up0 = unit;
+                up0 = st.ref == -INFINITY ? 0.f : FP8 ? exp2f((float)(eref - kVUp)) : 1.f;
             }
-            const bool whole = s.part < 0;
+            // (read behind the meeting above: a group without tiles has waited for nothing else)
+            const unsigned long long* bad = m.seg[seg.i].bad;
+            const bool any_bad = bad[0] | bad[1] | bad[2] | bad[3];
             if (whole) {
                 const float inv = l_all == 0.f ? 0.f : 1.f / l_all;
                 up0 *= inv;
                 up1 *= inv;
             }
-            const long long at = (long long)(s.node0 + node) * a.n_heads + hq;
-            if (warp_live) {
-                const TcSegment& ts = m.seg[seg.i];
-                for (int c = c0; c < c1; c += 32) {
-                    uint32_t x[32];
-                    float o[32];
-                    tmem_ld32(ta + c, x);
-                    tmem_ld_wait();
-                    // a row that has seen nothing has l = 0 and takes nothing from O either
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = up0 == 0.f ? 0.f : __uint_as_float(x[i]) * up0;
-                    if (RT == 1 && tiles > 1) {
-                        tmem_ld32(tb + c, x);
+            // group g takes half of the dimensions of both accumulators (RT = 1), or its own accumulator
+            const int c0 = RT == 1 ? g * (D / 2) : 0, c1 = RT == 1 ? c0 + D / 2 : D;
+            const uint32_t ta = tmem + lanes + kO + (uint32_t)(RT == 1 ? 0 : g * D), tb = ta + D;
+            auto emit4 = [&](int urow, long long to, int d, float4 o) {      // 4 dimensions of a finished row
+                if (any_bad) o = add_not_finite<FP8>(a, s, bad, (s.row0 + urow) / a.group, d, o);
+                if (whole) {
+                    const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x, o.y), hi = __floats2bfloat162_rn(o.z, o.w);
+                    uint2 w;
+                    w.x = *reinterpret_cast<const uint32_t*>(&lo);
+                    w.y = *reinterpret_cast<const uint32_t*>(&hi);
+                    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to * D + d) = w;
+                } else {
+                    *reinterpret_cast<float4*>(a.ws.part_o + ((long long)s.part * ROWS + urow) * D + d) = o;
+                }
+            };
+            if (RT == 1 && copies > 1) {
+                float* buf = reinterpret_cast<float*>(smem + C::OFF_MERGE) + g * 128 * 16;
+                for (int c = c0; c < c1; c += 16) {
+                    if (warp_live) {
+                        uint32_t x[16], y[16];
+                        tmem_ld16(ta + c, x);
+                        if (tiles > 1) tmem_ld16(tb + c, y);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] += up1 == 0.f ? 0.f : __uint_as_float(x[i]) * up1;
-                    }
-                    // V values that are not finite were left out of the products: the rows that see them get them here
-                    for (int w = 0; w < kMaxNodes / 64; ++w) {
-                        unsigned long long b = ts.bad[w];
-                        if (b && live) b &= sees_word(a, s.node0, s.n, node, w);
-                        while (b && live) {
-                            const int nd = w * 64 + __ffsll((long long)b) - 1;
-                            b &= b - 1;
-                            const int page = page_of(a, s.b, s.len + nd);
-                            if (page < 0) continue;
-                            const long long vr = ((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + nd) & (a.page_size - 1));
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                if constexpr (FP8) {
-                                    const uint8_t code = static_cast<const uint8_t*>(a.v_pool)[vr * D + c + i];
-                                    if ((code & 0x7f) == 0x7f) o[i] = __uint_as_float(0x7fffffffu);
-                                } else {
-                                    const float v = to_f32(static_cast<const __nv_bfloat16*>(a.v_pool)[vr * D + c + i]);
-                                    if (!(fabsf(v) < INFINITY)) o[i] += v;
-                                }
-                            }
-                        }
-                    }
-                    if (!live) continue;
-                    if (whole) {
-                        uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + at * D + c);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t w[4];
+                        for (int i = 0; i < 16; i += 4) {
+                            float o[4];
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                const __nv_bfloat162 v = __floats2bfloat162_rn(o[8 * i + 2 * j], o[8 * i + 2 * j + 1]);
-                                w[j] = *reinterpret_cast<const uint32_t*>(&v);
+                                o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[i + j]) * up0;
+                                if (tiles > 1 && up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
                             }
-                            dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                            // chunks of 16 bytes turned by the row, so that 8 rows' chunks lie in distinct banks
+                            *reinterpret_cast<float4*>(buf + r * 16 + ((i / 4 + (r >> 1)) & 3) * 4) = make_float4(o[0], o[1], o[2], o[3]);
                         }
-                    } else {
-                        float4* dst = reinterpret_cast<float4*>(a.ws.part_o + ((long long)s.part * ROWS + row) * D + c);
+                    }
+                    if (!group_sync()) { ok = false; break; }
+                    for (int i = r; i < s.rows * 4; i += 128) {
+                        const int urow = i >> 2, q4 = i & 3;
+                        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int k = urow; k < 128; k += apart) {
+                            const float4 v = *reinterpret_cast<const float4*>(buf + k * 16 + ((q4 + (k >> 1)) & 3) * 4);
+                            o.x += v.x;
+                            o.y += v.y;
+                            o.z += v.z;
+                            o.w += v.w;
+                        }
+                        const int ur = s.row0 + urow;
+                        emit4(urow, (long long)(s.node0 + ur / a.group) * a.n_heads + s.head * a.group + ur % a.group, c + q4 * 4, o);
+                    }
+                    if (!group_sync()) { ok = false; break; }
+                }
+                if (!ok) break;
+            } else if (warp_live) {
+                for (int c = c0; c < c1; c += 16) {
+                    uint32_t x[16], y[16];
+                    tmem_ld16(ta + c, x);
+                    if (RT == 1 && tiles > 1) tmem_ld16(tb + c, y);
+                    tmem_ld_wait();
+                    if (!live) continue;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    for (int i = 0; i < 16; i += 4) {
+                        float o[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[i + j]) * up0;
+                            if (RT == 1 && tiles > 1 && up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
+                        }
+                        emit4(row, at, c + i, make_float4(o[0], o[1], o[2], o[3]));
                     }
                 }
-                if (live && c0 == 0) {
-                    if (!whole) a.ws.part_ml[(long long)s.part * ROWS + row] = make_float2(m_all, l_all);
-                    else if (a.lse) a.lse[at] = (m_all + log2f(l_all)) * 0.69314718055994530942f;
-                }
+            }
+            if (live && c0 == 0 && r < apart) {
+                if (!whole) a.ws.part_ml[(long long)s.part * ROWS + row] = make_float2(m_all, l_all);
+                else if (a.lse) a.lse[at] = (m_all + log2f(l_all)) * 0.69314718055994530942f;
             }
             tc_fence_before();
             if (RT == 1 || !whole) {
