@@ -25,6 +25,7 @@ constexpr int kTcKeys = 128, kTcThreads = 512, kSegRing = 4, kAuxRing = 4;
 // (base 2): weights are at most 2^(kLazy + kPUp), which fp16 holds, and normal in fp16 down to 2^-(14 + kPUp) of the largest.
 constexpr int kLazy = 8, kPUp = 6;
 constexpr int kVUp = 6;                 // fp16 rows of V are code * 2^(e - eref + kVUp): at most 448 * 2^6, eref >= e
+constexpr int kVShift = 8;              // codes' bits moved to fp16's places stand for 2^-8 of their values
 constexpr int kConvThreads = 128;
 constexpr int kSoftRegs = 184, kOtherRegs = 72;
 static_assert(256 * (kSoftRegs + kOtherRegs) <= kTcThreads * 128, "the split must fit the launch's registers");
@@ -280,14 +281,14 @@ struct RowState {
 template <bool FP8, int N>
 __device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s, uint32_t s_t, int col, const float4* kf, bool drafted,
                                              int node, int pos0, float f_row, bool first, RowState& st) {
-    float x[N];
-    float top = load_scores<FP8, N>(s_t + col, x, kf + col / 4);
+    uint32_t see[N / 32];
     if (drafted) {
-        uint32_t see[N / 32];
 #pragma unroll
         for (int c = 0; c < N / 32; ++c) see[c] = sees32(a, s, node, pos0 + col + 32 * c);
-        top = mask_scores<N>(x, see);
     }
+    float x[N];
+    float top = load_scores<FP8, N>(s_t + col, x, kf + col / 4);
+    if (drafted) top = mask_scores<N>(x, see);
     top = top == -INFINITY ? top : top * f_row;
     constexpr float kUp = FP8 ? (float)kPUp : 0.f;
     if (top > st.ref + (float)kLazy + kUp || st.ref == -INFINITY) {
@@ -308,32 +309,31 @@ __device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s
     tmem_st_wait();
 }
 
-// Values of V that are not finite were left out of the products: what they add to dimensions d .. d + 3 of a row that sees them.
-template <bool FP8>
-__device__ __noinline__ float4 add_not_finite(const AttnArgs& a, const Segment& s, const unsigned long long* bad, int node, int d, float4 sum) {
-    float o[4] = {sum.x, sum.y, sum.z, sum.w};
-    for (int w = 0; w < kMaxNodes / 64; ++w) {
-        unsigned long long b = bad[w];
-        if (b) b &= sees_word(a, s.node0, s.n, node, w);
-        while (b) {
-            const int pos = s.len + w * 64 + __ffsll((long long)b) - 1;
-            b &= b - 1;
-            const int page = page_of(a, s.b, pos);
-            if (page < 0) continue;
-            const long long row = ((long long)page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (FP8) {
-                    const uint8_t code = static_cast<const uint8_t*>(a.v_pool)[row * a.head_dim + d + i];
-                    if ((code & 0x7f) == 0x7f) o[i] = __uint_as_float(0x7fffffffu);
-                } else {
-                    const float v = to_f32(static_cast<const __nv_bfloat16*>(a.v_pool)[row * a.head_dim + d + i]);
-                    if (!(fabsf(v) < INFINITY)) o[i] += v;
-                }
+// Values of V that are not finite were left out of the products: row `urow` of the unit, written already, gets those of
+// the nodes that it sees in dimensions d .. d + 3.
+template <bool FP8, int ROWS>
+__device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment& s, const unsigned long long* bad, int urow, int d) {
+    const int nd = (s.row0 + urow) / a.group, hq = s.head * a.group + (s.row0 + urow) % a.group;
+#pragma unroll 1
+    for (int m = 0; m < s.n; ++m) {
+        if (!(bad[m >> 6] & sees_word(a, s.node0, s.n, nd, m >> 6) & 1ull << (m & 63))) continue;
+        const int page = page_of(a, s.b, s.len + m);
+        if (page < 0) continue;
+        const long long row = ((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + m) & (a.page_size - 1));
+#pragma unroll 1
+        for (int i = d; i < d + 4; ++i) {
+            float v;
+            if constexpr (FP8) v = (static_cast<const uint8_t*>(a.v_pool)[row * a.head_dim + i] & 0x7f) == 0x7f ? __uint_as_float(0x7fffffffu) : 0.f;
+            else v = to_f32(static_cast<const __nv_bfloat16*>(a.v_pool)[row * a.head_dim + i]);
+            if (fabsf(v) < INFINITY) continue;
+            if (s.part < 0) {
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + ((long long)(s.node0 + nd) * a.n_heads + hq) * a.head_dim + i;
+                *out = from_f32<__nv_bfloat16>(to_f32(*out) + v);
+            } else {
+                a.ws.part_o[((long long)s.part * ROWS + urow) * a.head_dim + i] += v;
             }
         }
     }
-    return make_float4(o[0], o[1], o[2], o[3]);
 }
 
 // 8 elements of a unit's q row (bf16), from dimension d on.
@@ -344,6 +344,62 @@ __device__ __forceinline__ uint4 load_q(const AttnArgs& a, const Segment& s, int
     if ((uintptr_t)src % 16 == 0) return __ldg(reinterpret_cast<const uint4*>(src));
     const uint16_t* u = reinterpret_cast<const uint16_t*>(src);
     return make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
+}
+
+// Place of codes 16 c .. 16 c + 15 of a row in a tile of V as TMA leaves it (rows of 128 or 64 bytes, swizzled).
+template <int D>
+__device__ __forceinline__ int raw_v_offset(int row, int c) {
+    return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+}
+
+// Two codes of `x`, which `pick` takes to the upper bytes of two halves, as fp16 times `f` times 2^-kVShift.
+__device__ __forceinline__ uint32_t f16x2_bits(uint32_t x, uint32_t pick, __half2 f) {
+    const uint32_t b = __byte_perm(x, 0, pick), y = (b & 0x80008000u) | (b >> 1 & 0x3f803f80u);
+    const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&y), f);
+    return *reinterpret_cast<const uint32_t*>(&z);
+}
+
+// A tile of V codes with drafted rows: zeros past the end and in place of NaN (all bits of a code but the sign), whose
+// nodes are noted. Each thread cleans the 16 codes that it reads afterwards (row0 and c0 of the first).
+template <int D>
+__device__ __forceinline__ void clean_codes(unsigned char* v, int row0, int c0, const Segment& s, int pos0, unsigned long long* bad) {
+    const int total = s.len + s.n;
+#pragma unroll 1
+    for (int i = 0; i < D / 16; ++i) {
+        const int row = row0 + (i & 3) * 32, pos = pos0 + row;
+        if (pos < s.len) continue;
+        uint4* at = reinterpret_cast<uint4*>(v + raw_v_offset<D>(row, c0 + (i >> 2) * 4));
+        if (pos >= total) {
+            *at = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        const uint4 w = *at;
+        uint32_t x[4] = {w.x, w.y, w.z, w.w}, any = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t nan = ((x[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            any |= nan;
+            x[j] &= ~((nan >> 7) * 0xffu);
+        }
+        if (any) {
+            *at = make_uint4(x[0], x[1], x[2], x[3]);
+            atomicOr(&bad[(pos - s.len) >> 6], 1ull << ((pos - s.len) & 63));
+        }
+    }
+}
+
+// NaN where this thread's codes are NaN.
+template <int D>
+__device__ __forceinline__ void put_nan(const unsigned char* v, unsigned char* out, int row0, int c0) {
+#pragma unroll 1
+    for (int i = 0; i < D / 16; ++i) {
+        const int row = row0 + (i & 3) * 32, c = c0 + (i >> 2) * 4;
+        const unsigned char* codes = v + raw_v_offset<D>(row, c);
+#pragma unroll 1
+        for (int j = 0; j < 16; ++j)
+            if ((codes[j] & 0x7f) == 0x7f)
+                *reinterpret_cast<uint16_t*>(out + (c >> 2) * 16384 + row * 128 + ((((c & 3) * 2 + (j >> 3)) ^ (row & 7)) << 4) + (j & 7) * 2) = 0x7fff;
+    }
 }
 
 // With few rows (RT = 1) the block holds them 2 or 4 times, 64 or 32 lanes apart, and each copy's warps take that
@@ -409,14 +465,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     Ring seg;
 
     // Every role but the scheduler walks the CTA's segments; false: no more (or aborted).
-    auto next_segment = [&](Segment& s) -> bool {
+    // The segment stays in shared memory until segment_done().
+    auto next_segment = [&]() -> bool {
         if (!mbar_wait_warp(&m.seg_full[seg.i], seg.phase, a.err, abort_flag)) {
             *abort_flag = 1;
             return false;
         }
-        if (!m.seg[seg.i].go) return false;
-        s = m.seg[seg.i].s;
-        return true;
+        return m.seg[seg.i].go != 0;
     };
     auto segment_done = [&]() {
         __syncwarp();
@@ -452,9 +507,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         Ring rk, rv;
         long long nk = 0, nv = 0;
         bool ok = true;
-        Segment s;
         const int boxes = kTcKeys / p.box_rows;
-        while (ok && next_segment(s)) {
+        while (ok && next_segment()) {
+            const Segment& s = m.seg[seg.i].s;
             const int total = s.len + s.n;
             // a tile's pages are looked up while the tile before it is loaded
             auto look_up = [&](int t) {
@@ -583,8 +638,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         if constexpr (FP8) {
             Ring r;
             bool ok = true;
-            Segment s;
-            while (ok && next_segment(s)) {
+            while (ok && next_segment()) {
+                const Segment& s = m.seg[seg.i].s;
                 const int total = s.len + s.n;
                 int eref = -1000;
                 // pages two tiles and scales one tile ahead
@@ -627,7 +682,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     for (int i = 0; i < 4; ++i) {
                         const int vbyte = (int)(vb >> (8 * i) & 0xff);
                         kf[i] = pow2_of_byte((int)(kb >> (8 * i) & 0xff));
-                        const int e = vbyte - eref + kVUp;      // 2^(e_j - eref + kVUp), biased exponent
+                        const int e = vbyte - eref + kVUp + kVShift;    // biased exponent
                         vf[i] = __float2half_rn(vbyte == 0 || e <= 0 ? 0.f : pow2_of_byte(e));
                     }
                     if (!mbar_wait_warp(&m.aux_empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
@@ -650,10 +705,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         Ring rv, rc, ra;
         uint32_t q_phase = 1;           // the first segment's q buffer is free
         bool ok = true;
-        Segment s;
-        while (ok && next_segment(s)) {
-            if (!mbar_wait_warp(&m.q_free, q_phase, a.err, abort_flag)) { ok = false; break; }
-            q_phase ^= 1u;
+        while (ok && next_segment()) {
+            const Segment& s = m.seg[seg.i].s;
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
             constexpr int kStep = 128 / kChunks, kBatch = 4;        // rows a pass; passes whose loads are under way together
@@ -665,6 +718,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 for (int j = 0; j < kBatch; ++j) {
                     const int r = b0 + j * kStep + tid / kChunks;
                     qv[j] = r < s.rows ? load_q(a, s, s.row0 + r, tid % kChunks * 8) : make_uint4(0, 0, 0, 0);
+                }
+                // the rows are under way while the last products with the segment before read its q
+                if (b0 == 0) {
+                    if (!mbar_wait_warp(&m.q_free, q_phase, a.err, abort_flag)) { ok = false; break; }
+                    q_phase ^= 1u;
                 }
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
@@ -713,6 +771,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     }
                 }
             }
+            if (!ok) break;
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&m.q_full);
@@ -727,47 +786,31 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     if (!mbar_wait_warp(&m.c_empty[rc.i], rc.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
                     if (!mbar_wait_warp(&m.aux_full[ra.i], ra.phase, a.err, abort_flag)) { ok = false; break; }
                     unsigned char* out = smem + C::OFF_C + rc.i * C::CONV;
-                    constexpr int kUnits = D / 16;      // 16 codes become two 16-byte chunks
-#pragma unroll 2
-                    for (int u = tid; u < 128 * kUnits; u += kConvThreads) {
-                        const int row = u / kUnits, c = u % kUnits;
-                        uint4 w = *reinterpret_cast<const uint4*>(v + row * D + c * 16);
-                        if (drafted) {
-                            if (pos0 + row >= total) {
-                                w = make_uint4(0, 0, 0, 0);
-                            } else if (pos0 + row >= s.len) {
-                                // e4m3's NaN: all bits of the code but the sign
-                                uint32_t* x = reinterpret_cast<uint32_t*>(&w);
-                                bool found = false;
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const uint32_t nan = ((x[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-                                    if (nan) {
-                                        found = true;
-                                        x[i] &= ~((nan >> 7) * 0xffu);
-                                    }
-                                }
-                                if (found) atomicOr(&bad[(pos0 + row - s.len) >> 6], 1ull << ((pos0 + row - s.len) & 63));
-                            }
-                        }
+                    if (drafted) clean_codes<D>(v, (tid >> 5) * 8 + (lane & 7), lane >> 3, s, pos0, bad);
+                    // 16 codes become two 16-byte chunks; a warp takes 8 rows of 4 chunks a turn, which lie in distinct
+                    // banks on both sides. Integer operations put the codes' bits in fp16's places (cvt alone took 2800
+                    // cycles a tile); NaN codes, which that does not keep, are rare and put right afterwards.
+                    const int row0 = (tid >> 5) * 8 + (lane & 7);
+                    uint32_t nan = 0;
+#pragma unroll 1
+                    for (int i = 0; i < D / 16; ++i) {
+                        const int row = row0 + (i & 3) * 32, c = (lane >> 3) + (i >> 2) * 4;
+                        const uint4 w = *reinterpret_cast<const uint4*>(v + raw_v_offset<D>(row, c));
+                        const __half2 f = __half2half2(m.vf[ra.i][row]);
                         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
                         uint32_t h[8];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) h[2 * i] = f16x2_of_e4m3x2(x[i] & 0xffffu), h[2 * i + 1] = f16x2_of_e4m3x2(x[i] >> 16);
-                        const __half2 f2 = __half2half2(m.vf[ra.i][row]);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h[i]), f2);
-                            h[i] = *reinterpret_cast<const uint32_t*>(&y);
+                        for (int j = 0; j < 4; ++j) {
+                            nan |= (x[j] & 0x7f7f7f7fu) + 0x01010101u;
+                            h[2 * j] = f16x2_bits(x[j], 0x1404, f);
+                            h[2 * j + 1] = f16x2_bits(x[j], 0x3424, f);
                         }
                         unsigned char* dst = out + (c >> 2) * 16384 + row * 128;
-                        const int c0 = (c & 3) * 2;
-                        // the upper half's threads write their chunks in the other order: distinct banks
-                        const bool swap = c & 4;
-                        const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-                        *reinterpret_cast<uint4*>(dst + (((c0 + (swap ? 1 : 0)) ^ (row & 7)) << 4)) = swap ? hi : lo;
-                        *reinterpret_cast<uint4*>(dst + (((c0 + (swap ? 0 : 1)) ^ (row & 7)) << 4)) = swap ? lo : hi;
+                        const int at = ((c & 3) * 2 ^ (row & 7)) << 4;
+                        *reinterpret_cast<uint4*>(dst + at) = make_uint4(h[0], h[1], h[2], h[3]);
+                        *reinterpret_cast<uint4*>(dst + (at ^ 16)) = make_uint4(h[4], h[5], h[6], h[7]);
                     }
+                    if (nan & 0x80808080u) put_nan<D>(v, out, row0, lane >> 3);
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
@@ -835,8 +878,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             return mbar_wait_warp(&m.group[g], group_phase ^ 1u, a.err, abort_flag);
         };
         bool ok = true;
-        Segment s;
-        while (ok && next_segment(s)) {
+        while (ok && next_segment()) {
+            const Segment& s = m.seg[seg.i].s;
             const int copies = RT == 1 ? copies_of(s.rows) : 1, apart = 128 / copies;
             const int row = RT == 2 ? g * 128 + r : r & (apart - 1);        // of the unit
             const int col = RT == 2 ? 0 : r / apart * apart;                // first column of this copy
@@ -945,7 +988,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             const int c0 = RT == 1 ? g * (D / 2) : 0, c1 = RT == 1 ? c0 + D / 2 : D;
             const uint32_t ta = tmem + lanes + kO + (uint32_t)(RT == 1 ? 0 : g * D), tb = ta + D;
             auto emit4 = [&](int urow, long long to, int d, float4 o) {      // 4 dimensions of a finished row
-                if (any_bad) o = add_not_finite<FP8>(a, s, bad, (s.row0 + urow) / a.group, d, o);
                 if (whole) {
                     const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x, o.y), hi = __floats2bfloat162_rn(o.z, o.w);
                     uint2 w;
@@ -957,40 +999,49 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 }
             };
             if (RT == 1 && copies > 1) {
+                // as many dimensions at a time as the buffer holds of the unit's rows and copies: 16 to D / 2
                 float* buf = reinterpret_cast<float*>(smem + C::OFF_MERGE) + g * 128 * 16;
-                for (int c = c0; c < c1; c += 16) {
+                const int held = s.rows * copies, fit = 128 * 16 / held & ~15, wide = fit < D / 2 ? fit : D / 2;
+                const int mine_at = (r / apart * s.rows + row) * wide;
+                for (int c = c0; c < c1; c += wide) {
+                    const int w = min(wide, c1 - c);
                     if (warp_live) {
-                        uint32_t x[16], y[16];
-                        tmem_ld16(ta + c, x);
-                        if (tiles > 1) tmem_ld16(tb + c, y);
-                        tmem_ld_wait();
+                        for (int d = 0; d < w; d += 16) {
+                            uint32_t x[16], y[16];
+                            tmem_ld16(ta + c + d, x);
+                            if (tiles > 1) tmem_ld16(tb + c + d, y);
+                            tmem_ld_wait();
+                            if (!live) continue;
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            float o[4];
+                            for (int i = 0; i < 16; i += 4) {
+                                float o[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[i + j]) * up0;
-                                if (tiles > 1 && up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
+                                for (int j = 0; j < 4; ++j) {
+                                    o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[i + j]) * up0;
+                                    if (tiles > 1 && up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
+                                }
+                                // 16-byte chunks turned by the row: rows' equal chunks lie in distinct banks
+                                *reinterpret_cast<float4*>(buf + mine_at + ((d + i) / 4 + row) % (wide / 4) * 4) = make_float4(o[0], o[1], o[2], o[3]);
                             }
-                            // chunks of 16 bytes turned by the row, so that 8 rows' chunks lie in distinct banks
-                            *reinterpret_cast<float4*>(buf + r * 16 + ((i / 4 + (r >> 1)) & 3) * 4) = make_float4(o[0], o[1], o[2], o[3]);
                         }
                     }
                     if (!group_sync()) { ok = false; break; }
-                    for (int i = r; i < s.rows * 4; i += 128) {
-                        const int urow = i >> 2, q4 = i & 3;
+                    for (int i = r; i < s.rows * (w / 4); i += 128) {
+                        const int urow = i / (w / 4), q4 = i - urow * (w / 4);
                         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                        for (int k = urow; k < 128; k += apart) {
-                            const float4 v = *reinterpret_cast<const float4*>(buf + k * 16 + ((q4 + (k >> 1)) & 3) * 4);
+                        for (int k = 0; k < copies; ++k) {
+                            const float4 v = *reinterpret_cast<const float4*>(buf + (k * s.rows + urow) * wide + (q4 + urow) % (wide / 4) * 4);
                             o.x += v.x;
                             o.y += v.y;
                             o.z += v.z;
                             o.w += v.w;
                         }
-                        const int ur = s.row0 + urow;
-                        emit4(urow, (long long)(s.node0 + ur / a.group) * a.n_heads + s.head * a.group + ur % a.group, c + q4 * 4, o);
+                        const int ur = s.row0 + urow, nd = ur / a.group;
+                        emit4(urow, (long long)(s.node0 + nd) * a.n_heads + s.head * a.group + ur - nd * a.group, c + q4 * 4, o);
                     }
-                    if (!group_sync()) { ok = false; break; }
+                    if (any_bad)
+                        for (int i = r; i < s.rows * (w / 4); i += 128) add_not_finite<FP8, ROWS>(a, s, bad, i / (w / 4), c + i % (w / 4) * 4);
+                    if (c + wide < c1 && !group_sync()) { ok = false; break; }
                 }
                 if (!ok) break;
             } else if (warp_live) {
@@ -1011,6 +1062,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         emit4(row, at, c + i, make_float4(o[0], o[1], o[2], o[3]));
                     }
                 }
+                if (any_bad && live)
+                    for (int d = c0; d < c1; d += 4) add_not_finite<FP8, ROWS>(a, s, bad, row, d);
             }
             if (live && c0 == 0 && r < apart) {
                 if (!whole) a.ws.part_ml[(long long)s.part * ROWS + row] = make_float2(m_all, l_all);
@@ -1080,7 +1133,7 @@ cudaError_t attn_tc_init(ace_kv* kv) {
     if (fp8) {
         const int swizzle = D.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
         if ((e = make_byte_map(&kv->maps.k, kv->k_pool, rows, D.head_dim, box, swizzle)) != cudaSuccess) return e;
-        if ((e = make_byte_map(&kv->maps.v, kv->v_pool, rows, D.head_dim, box, CU_TENSOR_MAP_SWIZZLE_NONE)) != cudaSuccess) return e;
+        if ((e = make_byte_map(&kv->maps.v, kv->v_pool, rows, D.head_dim, box, swizzle)) != cudaSuccess) return e;
         return D.head_dim == 128 ? tc_attrs<true, 128>() : tc_attrs<true, 64>();
     }
     if ((e = make_tensor_map(&kv->maps.k, kv->k_pool, rows, D.head_dim, box, true)) != cudaSuccess) return e;

@@ -201,29 +201,52 @@ __device__ __forceinline__ unsigned long long sees_word(const AttnArgs& a, int n
     return left >= 64 ? m : m & ((1ull << left) - 1ull);
 }
 
-// Joins a unit's partial results: row r of the unit from the slots of CTAs first .. last, in that order. `lane_d`
-// threads side by side hold 4 dimensions each (D / 4 of them, a power of two or not). Every thread of a
-// CTA calls it; all partial results must be visible.
+// Joins a unit's partial results: row r of the unit from the slots of CTAs first .. last, in that order, 4
+// dimensions a thread and turn. Every thread of a CTA calls it; all partial results must be visible. kJoin loads are
+// under way together: a unit of a long context is spread over many CTAs, and each load takes most of a microsecond.
+constexpr int kJoin = 4;
+
 template <typename T, int ROWS>
 __device__ void join_unit(const AttnArgs& a, const Segment& s, int tid, int threads) {
     const int D = a.head_dim, quads = D / 4;
     for (int idx = tid; idx < s.rows * quads; idx += threads) {
         const int r = idx / quads, d = idx % quads * 4;
-        float M = -INFINITY;
-        for (int c = s.first; c <= s.last; ++c) M = fmaxf(M, __ldcg(&a.ws.part_ml[(long long)part_slot(c, s.first) * ROWS + r].x));
-        const float ref = M == -INFINITY ? 0.f : M;
-        float L = 0.f;
+        // partial results with the reference that they turn up with: they are rescaled as it grows
+        float M = -INFINITY, L = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c = s.first; c <= s.last; ++c) {
-            const long long slot = (long long)part_slot(c, s.first) * ROWS + r;
-            const float2 ml = __ldcg(&a.ws.part_ml[slot]);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + slot * D + d));
-            const float f = exp2f(ml.x - ref);
-            L = fmaf(ml.y, f, L);
-            o.x = fmaf(v.x, f, o.x);
-            o.y = fmaf(v.y, f, o.y);
-            o.z = fmaf(v.z, f, o.z);
-            o.w = fmaf(v.w, f, o.w);
+        for (int c0 = s.first; c0 <= s.last; c0 += kJoin) {
+            float2 ml[kJoin];
+            float4 v[kJoin];
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) {
+                const int c = c0 + j;
+                ml[j] = make_float2(-INFINITY, 0.f);
+                v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (c <= s.last) {
+                    const long long slot = (long long)part_slot(c, s.first) * ROWS + r;
+                    ml[j] = __ldcg(&a.ws.part_ml[slot]);
+                    v[j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + slot * D + d));
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) top = fmaxf(top, ml[j].x);
+            const float ref = top == -INFINITY ? 0.f : top, back = exp2f(M - ref);
+            M = top;
+            L *= back;
+            o.x *= back;
+            o.y *= back;
+            o.z *= back;
+            o.w *= back;
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) {
+                const float f = exp2f(ml[j].x - ref);
+                L = fmaf(ml[j].y, f, L);
+                o.x = fmaf(v[j].x, f, o.x);
+                o.y = fmaf(v[j].y, f, o.y);
+                o.z = fmaf(v[j].z, f, o.z);
+                o.w = fmaf(v[j].w, f, o.w);
+            }
         }
         const float inv = L == 0.f ? 0.f : 1.f / L;
         const int row = s.row0 + r, node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
