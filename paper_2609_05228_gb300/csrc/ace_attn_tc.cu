@@ -38,7 +38,7 @@ struct TcAttnArgs {
     int box_rows;                       // positions of a page in one box
 };
 
-template <bool FP8, int D, int RT>
+template <bool FP8, int D, int RT, int CP>
 struct Cfg {
     static constexpr int ROWS = 128 * RT;
     static constexpr int Q = 256 * D;                   // bytes of a row block: bf16, or two e4m3 terms
@@ -50,8 +50,8 @@ struct Cfg {
     static constexpr int OFF_K = RT * Q;
     static constexpr int OFF_V = OFF_K + NK * TILE;
     static constexpr int OFF_C = OFF_V + NV * TILE;
-    static constexpr int OFF_MERGE = OFF_C + NC * CONV;     // RT = 1: 16 dimensions of each group's 128 rows of O
-    static constexpr int OFF_MISC = OFF_MERGE + (RT == 1 ? 2 * 128 * 16 * 4 : 0);
+    static constexpr int OFF_MERGE = OFF_C + NC * CONV;     // CP > 1: 16 dimensions of each group's 128 rows of O
+    static constexpr int OFF_MISC = OFF_MERGE + (CP > 1 ? 2 * 128 * 16 * 4 : 0);
 };
 
 struct TcSegment {
@@ -76,12 +76,12 @@ struct Misc {
     int eref[kAuxRing];
 };
 
-template <bool FP8, int D, int RT>
-constexpr int tc_smem() { return 1024 + Cfg<FP8, D, RT>::OFF_MISC + (int)sizeof(Misc<FP8, RT>); }
+template <bool FP8, int D, int RT, int CP>
+constexpr int tc_smem() { return 1024 + Cfg<FP8, D, RT, CP>::OFF_MISC + (int)sizeof(Misc<FP8, RT>); }
 
-static_assert(tc_smem<false, 128, 2>() <= 232448 && tc_smem<false, 128, 1>() <= 232448, "shared memory");
-static_assert(tc_smem<true, 128, 2>() <= 232448 && tc_smem<true, 128, 1>() <= 232448, "shared memory");
-static_assert(tc_smem<false, 64, 2>() <= 232448 && tc_smem<true, 64, 2>() <= 232448, "shared memory");
+static_assert(tc_smem<false, 128, 2, 1>() <= 232448 && tc_smem<false, 128, 1, 2>() <= 232448, "shared memory");
+static_assert(tc_smem<true, 128, 2, 1>() <= 232448 && tc_smem<true, 128, 1, 2>() <= 232448, "shared memory");
+static_assert(tc_smem<false, 64, 2, 1>() <= 232448 && tc_smem<true, 64, 1, 2>() <= 232448, "shared memory");
 
 // Shared-memory descriptors by halves: the low word holds the address, to which a K step adds, and the leading byte
 // offset; the high one the stride byte offset, the version and the swizzle (2: 128 bytes, 4: 64 bytes).
@@ -198,22 +198,22 @@ __device__ __forceinline__ float load_scores(uint32_t s_t, float (&x)[N], const 
         uint32_t* r = reinterpret_cast<uint32_t*>(x) + 32 * c;
         tmem_ld32(s_t + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(r));
     }
-    float4 k[8];
+    // fp8: a few factors ahead of their products
+    constexpr int kAhead = 4;
+    float4 k[kAhead];
     if (FP8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) k[i] = kf[i];
+        for (int i = 0; i < kAhead; ++i) k[i] = kf[i];
     }
     tmem_ld_wait();
     if (FP8) {
 #pragma unroll
-        for (int c = 0; c < N / 32; ++c) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float* y = x + 32 * c + 4 * i;
-                unpair(mul2(pair(y[0], y[1]), pair(k[i].x, k[i].y)), y[0], y[1]);
-                unpair(mul2(pair(y[2], y[3]), pair(k[i].z, k[i].w)), y[2], y[3]);
-                if (c + 1 < N / 32) k[i] = kf[8 * (c + 1) + i];
-            }
+        for (int i = 0; i < N / 4; ++i) {
+            const float4 f = k[i % kAhead];
+            if (i + kAhead < N / 4) k[i % kAhead] = kf[i + kAhead];
+            float* y = x + 4 * i;
+            unpair(mul2(pair(y[0], y[1]), pair(f.x, f.y)), y[0], y[1]);
+            unpair(mul2(pair(y[2], y[3]), pair(f.z, f.w)), y[2], y[3]);
         }
     }
     float top[4] = {x[0], x[1], x[2], x[3]};
@@ -402,10 +402,6 @@ __device__ __forceinline__ void put_nan(const unsigned char* v, unsigned char* o
     }
 }
 
-// With few rows (RT = 1) the block holds them 2 or 4 times, 64 or 32 lanes apart, and each copy's warps take that
-// share of a tile's columns: the tile's softmax takes as much less time, and the copies' O are added at the end.
-__device__ __forceinline__ int copies_of(int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
-
 struct Ring {
     int i = 0;
     uint32_t phase = 0;
@@ -415,9 +411,11 @@ struct Ring {
     }
 };
 
-template <bool FP8, int D, int RT>
+// CP: with few rows (RT = 1) the block holds them CP = 2 or 4 times, 64 or 32 lanes apart, and each copy's warps take that
+// share of a tile's columns: the tile's softmax takes as much less time, and the copies' O are added at the end.
+template <bool FP8, int D, int RT, int CP>
 __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant__ TcAttnArgs p) {
-    using C = Cfg<FP8, D, RT>;
+    using C = Cfg<FP8, D, RT, CP>;
     constexpr int ROWS = C::ROWS, NK = C::NK, NV = C::NV, NC = C::NC;
     constexpr int kHalves = D / 64;                     // 64-element blocks of a bf16 / fp16 row
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -710,7 +708,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
             constexpr int kStep = 128 / kChunks, kBatch = 4;        // rows a pass; passes whose loads are under way together
-            const int copies = RT == 1 ? copies_of(s.rows) : 1, apart = 128 / copies;
+            constexpr int apart = 128 / CP;
             // (rows of the block past the unit's keep what they hold: rows of S, P and O do not mix)
             for (int b0 = 0; b0 < s.rows; b0 += kStep * kBatch) {
                 uint4 qv[kBatch];
@@ -750,7 +748,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         if (r >= s.rows) continue;
                         // 8 bytes of a 16-byte chunk
                         const int ch = c >> 1;
-                        for (int rr = r & 127, k = 0; k < copies; ++k, rr += apart) {
+                        for (int rr = r & 127, k = 0; k < CP; ++k, rr += apart) {
                             const uint32_t off = D == 128 ? (uint32_t)rr * 128u + (uint32_t)((ch ^ (rr & 7)) << 4)
                                                           : (uint32_t)rr * 64u + (uint32_t)((ch ^ ((rr >> 1) & 3)) << 4);
                             *reinterpret_cast<uint2*>(tile + off + (c & 1) * 8) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
@@ -765,7 +763,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                             const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
                             w[i] = *reinterpret_cast<const uint32_t*>(&v);
                         }
-                        for (int rr = r & 127, k = 0; k < copies; ++k, rr += apart)
+                        for (int rr = r & 127, k = 0; k < CP; ++k, rr += apart)
                             *reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
                                 make_uint4(w[0], w[1], w[2], w[3]);
                     }
@@ -791,24 +789,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     // banks on both sides. Integer operations put the codes' bits in fp16's places (cvt alone took 2800
                     // cycles a tile); NaN codes, which that does not keep, are rare and put right afterwards.
                     const int row0 = (tid >> 5) * 8 + (lane & 7);
+                    const unsigned char* src0 = v + raw_v_offset<D>(row0, lane >> 3);
+                    unsigned char* dst0 = out + row0 * 128 + (((lane >> 3) * 2 ^ (lane & 7)) << 4);
+                    unsigned char* dst1 = out + row0 * 128 + (((lane >> 3) * 2 ^ (lane & 7) ^ 1) << 4);
+                    const __half* vf = m.vf[ra.i] + row0;
+                    // all loads first: the compiler keeps them behind stores that it cannot tell apart from them
+                    uint4 w[D / 16];
+                    __half f[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        f[i] = vf[32 * i];
+                        // rows 32 apart share their swizzle; D = 128: the row's other 64 codes lie at chunk ^ 4
+                        w[i] = *reinterpret_cast<const uint4*>(src0 + i * 32 * D);
+                        if (D == 128) w[D / 16 - 4 + i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>((uintptr_t)src0 ^ 64) + i * 32 * D);
+                    }
                     uint32_t nan = 0;
-#pragma unroll 1
+#pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
-                        const int row = row0 + (i & 3) * 32, c = (lane >> 3) + (i >> 2) * 4;
-                        const uint4 w = *reinterpret_cast<const uint4*>(v + raw_v_offset<D>(row, c));
-                        const __half2 f = __half2half2(m.vf[ra.i][row]);
-                        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+                        const __half2 f2 = __half2half2(f[i & 3]);
+                        const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
                         uint32_t h[8];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             nan |= (x[j] & 0x7f7f7f7fu) + 0x01010101u;
-                            h[2 * j] = f16x2_bits(x[j], 0x1404, f);
-                            h[2 * j + 1] = f16x2_bits(x[j], 0x3424, f);
+                            h[2 * j] = f16x2_bits(x[j], 0x1404, f2);
+                            h[2 * j + 1] = f16x2_bits(x[j], 0x3424, f2);
                         }
-                        unsigned char* dst = out + (c >> 2) * 16384 + row * 128;
-                        const int at = ((c & 3) * 2 ^ (row & 7)) << 4;
-                        *reinterpret_cast<uint4*>(dst + at) = make_uint4(h[0], h[1], h[2], h[3]);
-                        *reinterpret_cast<uint4*>(dst + (at ^ 16)) = make_uint4(h[4], h[5], h[6], h[7]);
+                        *reinterpret_cast<uint4*>(dst0 + (i >> 2) * 16384 + (i & 3) * 4096) = make_uint4(h[0], h[1], h[2], h[3]);
+                        *reinterpret_cast<uint4*>(dst1 + (i >> 2) * 16384 + (i & 3) * 4096) = make_uint4(h[4], h[5], h[6], h[7]);
                     }
                     if (nan & 0x80808080u) put_nan<D>(v, out, row0, lane >> 3);
                     fence_async_smem();
@@ -880,7 +888,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         bool ok = true;
         while (ok && next_segment()) {
             const Segment& s = m.seg[seg.i].s;
-            const int copies = RT == 1 ? copies_of(s.rows) : 1, apart = 128 / copies;
+            constexpr int apart = 128 / CP;
             const int row = RT == 2 ? g * 128 + r : r & (apart - 1);        // of the unit
             const int col = RT == 2 ? 0 : r / apart * apart;                // first column of this copy
             const bool live = row < s.rows;
@@ -914,9 +922,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         if (mine && e > eref) st.o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
                         eref = e;
                     }
-                    if (copies == 1) softmax_tile<FP8, 128>(a, s, s_t, 0, kf, drafted, node, pos0, f_row, !mine, st);
-                    else if (RT == 1 && copies == 2) softmax_tile<FP8, 64>(a, s, s_t, col, kf, drafted, node, pos0, f_row, !mine, st);
-                    else if (RT == 1) softmax_tile<FP8, 32>(a, s, s_t, col, kf, drafted, node, pos0, f_row, !mine, st);
+                    softmax_tile<FP8, apart>(a, s, s_t, col, kf, drafted, node, pos0, f_row, !mine, st);
                 }
                 if (FP8) {
                     __syncwarp();
@@ -998,10 +1004,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     *reinterpret_cast<float4*>(a.ws.part_o + ((long long)s.part * ROWS + urow) * D + d) = o;
                 }
             };
-            if (RT == 1 && copies > 1) {
+            if constexpr (CP > 1) {
                 // as many dimensions at a time as the buffer holds of the unit's rows and copies: 16 to D / 2
                 float* buf = reinterpret_cast<float*>(smem + C::OFF_MERGE) + g * 128 * 16;
-                const int held = s.rows * copies, fit = 128 * 16 / held & ~15, wide = fit < D / 2 ? fit : D / 2;
+                const int held = s.rows * CP, fit = 128 * 16 / held & ~15, wide = fit < D / 2 ? fit : D / 2;
                 const int mine_at = (r / apart * s.rows + row) * wide;
                 for (int c = c0; c < c1; c += wide) {
                     const int w = min(wide, c1 - c);
@@ -1029,7 +1035,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     for (int i = r; i < s.rows * (w / 4); i += 128) {
                         const int urow = i / (w / 4), q4 = i - urow * (w / 4);
                         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                        for (int k = 0; k < copies; ++k) {
+                        for (int k = 0; k < CP; ++k) {
                             const float4 v = *reinterpret_cast<const float4*>(buf + (k * s.rows + urow) * wide + (q4 + urow) % (wide / 4) * 4);
                             o.x += v.x;
                             o.y += v.y;
@@ -1092,30 +1098,39 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
-template <bool FP8, int D, int RT>
+template <bool FP8, int D, int RT, int CP>
 cudaError_t tc_attr() {
     // a split above what the block is launched with would wait for ever
     cudaFuncAttributes f;
-    const cudaError_t e = cudaFuncGetAttributes(&f, k_attn_tc<FP8, D, RT>);
+    const cudaError_t e = cudaFuncGetAttributes(&f, k_attn_tc<FP8, D, RT, CP>);
     if (e != cudaSuccess) return e;
     if (f.numRegs * kTcThreads < 256 * (kSoftRegs + kOtherRegs)) return cudaErrorLaunchOutOfResources;
-    return raise_smem_limit(k_attn_tc<FP8, D, RT>, tc_smem<FP8, D, RT>());
+    return raise_smem_limit(k_attn_tc<FP8, D, RT, CP>, tc_smem<FP8, D, RT, CP>());
 }
 
 template <bool FP8, int D>
 cudaError_t tc_attrs() {
-    const cudaError_t e = tc_attr<FP8, D, 1>();
-    return e == cudaSuccess ? tc_attr<FP8, D, 2>() : e;
+    cudaError_t e = tc_attr<FP8, D, 1, 4>();
+    if (e == cudaSuccess) e = tc_attr<FP8, D, 1, 2>();
+    if (e == cudaSuccess) e = tc_attr<FP8, D, 1, 1>();
+    return e == cudaSuccess ? tc_attr<FP8, D, 2, 1>() : e;
+}
+
+template <bool FP8, int D, int RT, int CP>
+cudaError_t tc_go(const TcAttnArgs& p, int ctas, cudaStream_t s) {
+    k_attn_tc<FP8, D, RT, CP><<<ctas, kTcThreads, tc_smem<FP8, D, RT, CP>(), s>>>(p);
+    return cudaGetLastError();
 }
 
 template <bool FP8, int D>
 cudaError_t tc_launch(const TcAttnArgs& p, int ctas, cudaStream_t s) {
-    // one block of 128 rows a unit where that holds a request's largest tree, else two that share the loaded tiles
-    if ((long long)p.a.max_nodes * p.a.group <= 128)
-        k_attn_tc<FP8, D, 1><<<ctas, kTcThreads, tc_smem<FP8, D, 1>(), s>>>(p);
-    else
-        k_attn_tc<FP8, D, 2><<<ctas, kTcThreads, tc_smem<FP8, D, 2>(), s>>>(p);
-    return cudaGetLastError();
+    // by the rows of the largest tree: one block of 128 rows a unit where that holds them (as often as it can), else two
+    // that share the loaded tiles
+    const long long rows = (long long)p.a.max_nodes * p.a.group;
+    if (rows <= 32) return tc_go<FP8, D, 1, 4>(p, ctas, s);
+    if (rows <= 64) return tc_go<FP8, D, 1, 2>(p, ctas, s);
+    if (rows <= 128) return tc_go<FP8, D, 1, 1>(p, ctas, s);
+    return tc_go<FP8, D, 2, 1>(p, ctas, s);
 }
 
 }  // namespace
