@@ -190,82 +190,67 @@ __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, 
     return r;
 }
 
-// N of a row's scores from TMEM, with fp8 rows' scales; returns their maximum. The scores stay in registers.
-template <bool FP8, int N>
-__device__ __forceinline__ float load_scores(uint32_t s_t, float (&x)[N], const float4* kf) {
-#pragma unroll
-    for (int c = 0; c < N / 32; ++c) {
-        uint32_t* r = reinterpret_cast<uint32_t*>(x) + 32 * c;
-        tmem_ld32(s_t + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(r));
-    }
-    // fp8: a few factors ahead of their products
-    constexpr int kAhead = 4;
-    float4 k[kAhead];
-    if (FP8) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) k[i] = kf[i];
-    }
+// The tile's loops are rolled (32 scores a turn) on purpose: unrolled over a tile's 128 scores they and the fp16
+// conversion overflow the instruction cache, and warps that run different roles then stall on fetches (a fp8 tile of
+// 128 rows 9600 cycles unrolled; no_instruction stalls 2.7 an issue against 0.5).
+
+// 32 of a row's scores from TMEM, with fp8 rows' scales, and -inf where the row does not see the position.
+template <bool FP8>
+__device__ __forceinline__ void load_scores(uint32_t s_t, float (&x)[32], const float4* kf, bool masked, uint32_t see) {
+    tmem_ld32(s_t, *reinterpret_cast<uint32_t(*)[32]>(&x));
     tmem_ld_wait();
     if (FP8) {
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const float4 f = k[i % kAhead];
-            if (i + kAhead < N / 4) k[i % kAhead] = kf[i + kAhead];
-            float* y = x + 4 * i;
-            unpair(mul2(pair(y[0], y[1]), pair(f.x, f.y)), y[0], y[1]);
-            unpair(mul2(pair(y[2], y[3]), pair(f.z, f.w)), y[2], y[3]);
+        for (int i = 0; i < 32; i += 4) {
+            const float4 f = kf[i / 4];
+            unpair(mul2(pair(x[i], x[i + 1]), pair(f.x, f.y)), x[i], x[i + 1]);
+            unpair(mul2(pair(x[i + 2], x[i + 3]), pair(f.z, f.w)), x[i + 2], x[i + 3]);
         }
     }
+    if (masked) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = see >> i & 1 ? x[i] : -INFINITY;
+    }
+}
+
+__device__ __forceinline__ float max32(const float (&x)[32]) {
     float top[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-    for (int i = 4; i < N; i += 8) {
+    for (int i = 4; i < 28; i += 8) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], i + 4 + j < N ? fmaxf(x[i + j], x[i + 4 + j]) : x[i + j]);
+        for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], fmaxf(x[i + j], x[i + 4 + j]));
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], x[28 + j]);
     return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
 
-// The same where not every position counts.
-template <int N>
-__device__ __forceinline__ float mask_scores(float (&x)[N], const uint32_t (&see)[N / 32]) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        x[i] = see[i >> 5] >> (i & 31) & 1 ? x[i] : -INFINITY;
-        top = fmaxf(top, x[i]);
-    }
-    return top;
-}
-
-// P = 2^(x f + shift) to TMEM; returns the sum of P.
-template <bool FP8, int N>
-__device__ __forceinline__ float store_weights(uint32_t p_t, const float (&x)[N], float f, float shift) {
+// 32 weights 2^(x f + shift) to TMEM; returns their sum.
+template <bool FP8>
+__device__ __forceinline__ float store_weights(uint32_t p_t, const float (&x)[32], float f, float shift) {
     const uint64_t f2 = pair(f, f), shift2 = pair(shift, shift);
     uint64_t sum[2] = {0ull, 0ull};
+    uint32_t w[16];
 #pragma unroll
-    for (int c = 0; c < N / 32; ++c) {
-        uint32_t w[16];
+    for (int i = 0; i < 32; i += 4) {
+        float e[4];
+        unpair(fma2(pair(x[i], x[i + 1]), f2, shift2), e[0], e[1]);
+        unpair(fma2(pair(x[i + 2], x[i + 3]), f2, shift2), e[2], e[3]);
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            float e[4];
-            unpair(fma2(pair(x[32 * c + i], x[32 * c + i + 1]), f2, shift2), e[0], e[1]);
-            unpair(fma2(pair(x[32 * c + i + 2], x[32 * c + i + 3]), f2, shift2), e[2], e[3]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]);
-            sum[0] = add2(sum[0], pair(e[0], e[1]));
-            sum[1] = add2(sum[1], pair(e[2], e[3]));
-            if constexpr (FP8) {
-                const __half2 p0 = __floats2half2_rn(e[0], e[1]), p1 = __floats2half2_rn(e[2], e[3]);
-                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
-                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
-            } else {
-                const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
-                w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
-                w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
-            }
+        for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]);
+        sum[0] = add2(sum[0], pair(e[0], e[1]));
+        sum[1] = add2(sum[1], pair(e[2], e[3]));
+        if constexpr (FP8) {
+            const __half2 p0 = __floats2half2_rn(e[0], e[1]), p1 = __floats2half2_rn(e[2], e[3]);
+            w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+            w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+        } else {
+            const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
+            w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+            w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
         }
-        tmem_st16(p_t + 16 * c, w);
     }
+    tmem_st16(p_t, w);
     float a, b, c, d;
     unpair(sum[0], a, b);
     unpair(sum[1], c, d);
@@ -277,18 +262,18 @@ struct RowState {
     float ref, l, o_mul;                // reference, sum, what O has to be multiplied with
 };
 
-// One tile of a row: N scores from column `col` on become weights; the row's other columns of P are zero.
+// One tile of a row: N scores from column `col` on become weights, over the scores that are read already; the row's other
+// columns of P are zero.
 template <bool FP8, int N>
 __device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s, uint32_t s_t, int col, const float4* kf, bool drafted,
                                              int node, int pos0, float f_row, bool first, RowState& st) {
-    uint32_t see[N / 32];
-    if (drafted) {
-#pragma unroll
-        for (int c = 0; c < N / 32; ++c) see[c] = sees32(a, s, node, pos0 + col + 32 * c);
+    float x[32];
+    float top = -INFINITY;
+#pragma unroll 1
+    for (int c = col; c < col + N; c += 32) {
+        load_scores<FP8>(s_t + c, x, kf + c / 4, drafted, drafted ? sees32(a, s, node, pos0 + c) : 0u);
+        top = fmaxf(top, max32(x));
     }
-    float x[N];
-    float top = load_scores<FP8, N>(s_t + col, x, kf + col / 4);
-    if (drafted) top = mask_scores<N>(x, see);
     top = top == -INFINITY ? top : top * f_row;
     constexpr float kUp = FP8 ? (float)kPUp : 0.f;
     if (top > st.ref + (float)kLazy + kUp || st.ref == -INFINITY) {
@@ -299,7 +284,15 @@ __device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s
         if (!first) st.o_mul *= f;
     }
     const float shift = st.ref == -INFINITY ? 0.f : -st.ref;
-    st.l += store_weights<FP8, N>(s_t + col / 2, x, f_row, shift);
+    if constexpr (N == 32) {
+        st.l += store_weights<FP8>(s_t + col / 2, x, f_row, shift);
+    } else {
+#pragma unroll 1
+        for (int c = col; c < col + N; c += 32) {
+            load_scores<FP8>(s_t + c, x, kf + c / 4, drafted, drafted ? sees32(a, s, node, pos0 + c) : 0u);
+            st.l += store_weights<FP8>(s_t + c / 2, x, f_row, shift);
+        }
+    }
     if constexpr (N < 128) {
         const uint32_t zero[16] = {};
 #pragma unroll
@@ -793,30 +786,29 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     unsigned char* dst0 = out + row0 * 128 + (((lane >> 3) * 2 ^ (lane & 7)) << 4);
                     unsigned char* dst1 = out + row0 * 128 + (((lane >> 3) * 2 ^ (lane & 7) ^ 1) << 4);
                     const __half* vf = m.vf[ra.i] + row0;
-                    // all loads first: the compiler keeps them behind stores that it cannot tell apart from them
-                    uint4 w[D / 16];
-                    __half f[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        f[i] = vf[32 * i];
-                        // rows 32 apart share their swizzle; D = 128: the row's other 64 codes lie at chunk ^ 4
-                        w[i] = *reinterpret_cast<const uint4*>(src0 + i * 32 * D);
-                        if (D == 128) w[D / 16 - 4 + i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>((uintptr_t)src0 ^ 64) + i * 32 * D);
-                    }
                     uint32_t nan = 0;
+#pragma unroll 1
+                    for (int i = 0; i < 4; ++i) {
+                        // a turn's loads before its stores; rows 32 apart share their swizzle, and the other 64 codes of a
+                        // row (D = 128) lie at chunk ^ 4
+                        const __half2 f2 = __half2half2(vf[32 * i]);
+                        uint4 w[D / 64];
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const __half2 f2 = __half2half2(f[i & 3]);
-                        const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-                        uint32_t h[8];
+                        for (int k = 0; k < D / 64; ++k)
+                            w[k] = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>((uintptr_t)src0 ^ (64 * k)) + i * 32 * D);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            nan |= (x[j] & 0x7f7f7f7fu) + 0x01010101u;
-                            h[2 * j] = f16x2_bits(x[j], 0x1404, f2);
-                            h[2 * j + 1] = f16x2_bits(x[j], 0x3424, f2);
+                        for (int k = 0; k < D / 64; ++k) {
+                            const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                            uint32_t h[8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                nan |= (x[j] & 0x7f7f7f7fu) + 0x01010101u;
+                                h[2 * j] = f16x2_bits(x[j], 0x1404, f2);
+                                h[2 * j + 1] = f16x2_bits(x[j], 0x3424, f2);
+                            }
+                            *reinterpret_cast<uint4*>(dst0 + k * 16384 + i * 4096) = make_uint4(h[0], h[1], h[2], h[3]);
+                            *reinterpret_cast<uint4*>(dst1 + k * 16384 + i * 4096) = make_uint4(h[4], h[5], h[6], h[7]);
                         }
-                        *reinterpret_cast<uint4*>(dst0 + (i >> 2) * 16384 + (i & 3) * 4096) = make_uint4(h[0], h[1], h[2], h[3]);
-                        *reinterpret_cast<uint4*>(dst1 + (i >> 2) * 16384 + (i & 3) * 4096) = make_uint4(h[4], h[5], h[6], h[7]);
                     }
                     if (nan & 0x80808080u) put_nan<D>(v, out, row0, lane >> 3);
                     fence_async_smem();
