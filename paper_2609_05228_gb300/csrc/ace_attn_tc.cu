@@ -25,7 +25,6 @@ constexpr int kTcKeys = 128, kTcThreads = 512, kSegRing = 4, kAuxRing = 4;
 // (base 2): weights are at most 2^(kLazy + kPUp), which fp16 holds, and normal in fp16 down to 2^-(14 + kPUp) of the largest.
 constexpr int kLazy = 8, kPUp = 6;
 constexpr int kVUp = 6;                 // fp16 rows of V are code * 2^(e - eref + kVUp): at most 448 * 2^6, eref >= e
-constexpr int kVShift = 8;              // codes' bits moved to fp16's places stand for 2^-8 of their values
 constexpr int kConvThreads = 128;
 constexpr int kSoftRegs = 184, kOtherRegs = 72;
 static_assert(256 * (kSoftRegs + kOtherRegs) <= kTcThreads * 128, "the split must fit the launch's registers");
@@ -345,9 +344,9 @@ __device__ __forceinline__ int raw_v_offset(int row, int c) {
     return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
 }
 
-// Two codes of `x`, which `pick` takes to the upper bytes of two halves, as fp16 times `f` times 2^-kVShift.
-__device__ __forceinline__ uint32_t f16x2_bits(uint32_t x, uint32_t pick, __half2 f) {
-    const uint32_t b = __byte_perm(x, 0, pick), y = (b & 0x80008000u) | (b >> 1 & 0x3f803f80u);
+// Two codes as fp16 times `f`.
+__device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
+    const uint32_t y = f16x2_of_e4m3x2(codes);
     const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&y), f);
     return *reinterpret_cast<const uint32_t*>(&z);
 }
@@ -378,20 +377,6 @@ __device__ __forceinline__ void clean_codes(unsigned char* v, int row0, int c0, 
             *at = make_uint4(x[0], x[1], x[2], x[3]);
             atomicOr(&bad[(pos - s.len) >> 6], 1ull << ((pos - s.len) & 63));
         }
-    }
-}
-
-// NaN where this thread's codes are NaN.
-template <int D>
-__device__ __forceinline__ void put_nan(const unsigned char* v, unsigned char* out, int row0, int c0) {
-#pragma unroll 1
-    for (int i = 0; i < D / 16; ++i) {
-        const int row = row0 + (i & 3) * 32, c = c0 + (i >> 2) * 4;
-        const unsigned char* codes = v + raw_v_offset<D>(row, c);
-#pragma unroll 1
-        for (int j = 0; j < 16; ++j)
-            if ((codes[j] & 0x7f) == 0x7f)
-                *reinterpret_cast<uint16_t*>(out + (c >> 2) * 16384 + row * 128 + ((((c & 3) * 2 + (j >> 3)) ^ (row & 7)) << 4) + (j & 7) * 2) = 0x7fff;
     }
 }
 
@@ -673,7 +658,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     for (int i = 0; i < 4; ++i) {
                         const int vbyte = (int)(vb >> (8 * i) & 0xff);
                         kf[i] = pow2_of_byte((int)(kb >> (8 * i) & 0xff));
-                        const int e = vbyte - eref + kVUp + kVShift;    // biased exponent
+                        const int e = vbyte - eref + kVUp;      // biased exponent
                         vf[i] = __float2half_rn(vbyte == 0 || e <= 0 ? 0.f : pow2_of_byte(e));
                     }
                     if (!mbar_wait_warp(&m.aux_empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
@@ -779,14 +764,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     unsigned char* out = smem + C::OFF_C + rc.i * C::CONV;
                     if (drafted) clean_codes<D>(v, (tid >> 5) * 8 + (lane & 7), lane >> 3, s, pos0, bad);
                     // 16 codes become two 16-byte chunks; a warp takes 8 rows of 4 chunks a turn, which lie in distinct
-                    // banks on both sides. Integer operations put the codes' bits in fp16's places (cvt alone took 2800
-                    // cycles a tile); NaN codes, which that does not keep, are rare and put right afterwards.
+                    // banks on both sides (alone, a tile takes 664 cycles this way, and 1013 where integer operations move
+                    // the codes' bits to fp16's places)
                     const int row0 = (tid >> 5) * 8 + (lane & 7);
                     const unsigned char* src0 = v + raw_v_offset<D>(row0, lane >> 3);
                     unsigned char* dst0 = out + row0 * 128 + (((lane >> 3) * 2 ^ (lane & 7)) << 4);
                     unsigned char* dst1 = out + row0 * 128 + (((lane >> 3) * 2 ^ (lane & 7) ^ 1) << 4);
                     const __half* vf = m.vf[ra.i] + row0;
-                    uint32_t nan = 0;
 #pragma unroll 1
                     for (int i = 0; i < 4; ++i) {
                         // a turn's loads before its stores; rows 32 apart share their swizzle, and the other 64 codes of a
@@ -802,15 +786,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                             uint32_t h[8];
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                nan |= (x[j] & 0x7f7f7f7fu) + 0x01010101u;
-                                h[2 * j] = f16x2_bits(x[j], 0x1404, f2);
-                                h[2 * j + 1] = f16x2_bits(x[j], 0x3424, f2);
+                                h[2 * j] = f16x2_scaled(x[j], f2);
+                                h[2 * j + 1] = f16x2_scaled(x[j] >> 16, f2);
                             }
                             *reinterpret_cast<uint4*>(dst0 + k * 16384 + i * 4096) = make_uint4(h[0], h[1], h[2], h[3]);
                             *reinterpret_cast<uint4*>(dst1 + k * 16384 + i * 4096) = make_uint4(h[4], h[5], h[6], h[7]);
                         }
                     }
-                    if (nan & 0x80808080u) put_nan<D>(v, out, row0, lane >> 3);
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
