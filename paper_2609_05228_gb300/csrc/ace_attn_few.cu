@@ -1,0 +1,638 @@
+// ace_attn_few.cu — attention for trees of drafted tokens on the tensor cores where a unit has few query rows
+// (nodes times query heads a kv head at most 16 or 32: decode steps and small trees, bound by the cache's bytes).
+// The products are turned round, so that the 128 rows of a tcgen05.mma are positions of the cache and not mostly
+// empty query rows:
+//   S^T = K Q^T        128 positions x NR rows
+//   P^T = 2^(S^T - ref)  a thread holds one position's scores of all rows; its cached row's scale is one factor
+//   O^T += V^T P^T     D x NR, V as stored (M-major), P^T through shared memory
+// With 128-row blocks of q a tile of 8 live rows costs 16 times the products and exponentials that it needs, and V's codes
+// have to become fp16: 4096 ragged fp8 rows of 64 users took 115 us that way.
+// fp8 caches: both products take the cached codes as they are (kind::f8f6f4). q is split into two e4m3 terms as in
+// ace_attn_tc.cu; a weight (at most 2^kLazy) times its V row's factor (at most 2^kVUp), rounded to fp16, into four e5m2
+// terms: the upper byte of an fp16 is one, and so on with what is left; each takes at least three of the eleven bits.
+// The rows' references lie in shared memory and move only where a score passes them by 2^kLazy (a flag of
+// each warp, met once a tile). Two groups of four warps take even and odd tiles into accumulators of their own.
+#include "ace_attn_tc.cuh"
+
+namespace ace {
+namespace {
+
+constexpr float kNone = -1e30f;         // reference of a row that has seen nothing: any score passes it
+
+template <bool FP8, int D, int NR>
+struct FewCfg {
+    static constexpr int ROW = D * (FP8 ? 1 : 2);               // bytes of a cached row
+    static constexpr int TILE = 128 * ROW;
+    static constexpr int Q = NR * D * 2;                        // bf16, or two e4m3 terms
+    static constexpr int TERMS = FP8 ? 4 : 1;
+    static constexpr int BLOCKS = NR * (FP8 ? 1 : 2) / 16;      // 16-byte pieces of a position's row of P^T
+    static constexpr int TERM = BLOCKS * 128 * 16;
+    static constexpr int P = TERMS * TERM;                      // one group's P^T
+    static constexpr int NK = D == 64 ? 6 : FP8 ? 5 : 3, NV = NK;
+    static constexpr int OFF_K = 0;
+    static constexpr int OFF_V = OFF_K + NK * TILE;
+    static constexpr int OFF_Q = OFF_V + NV * TILE;             // 1024-byte multiples up to here
+    static constexpr int OFF_P = OFF_Q + Q;
+    static constexpr int OFF_MISC = OFF_P + 2 * P;
+    static constexpr uint32_t S = 0, O = 2 * NR, COLS = 4 * NR; // TMEM: S^T of both groups, then O^T
+};
+
+template <bool FP8, int NR>
+struct FewShared : TcShared {
+    float4 kf[FP8 ? kAuxRing : 1][32], vf[FP8 ? kAuxRing : 1][32];
+    float f_row[2][NR];                 // q's scale times the softmax's, by turns of segments
+    int node[2][NR];                    // row's node of the request
+    float ref[2][2][NR];                // [group][turn]
+    int flag[2][2][4];                  // [group][turn][warp]
+    float top[2][4][NR];                // [group][warp]: maxima of a tile's scores
+    float sum[2][4][NR];                // end: sums of weights
+    float ref_end[2][NR];
+    float2 fac[8][NR];                  // [warp]: factors of both accumulators
+    int eref_end[2];
+};
+
+template <bool FP8, int D, int NR>
+constexpr int few_smem() { return 1024 + FewCfg<FP8, D, NR>::OFF_MISC + (int)sizeof(FewShared<FP8, NR>); }
+
+static_assert(few_smem<false, 128, 32>() <= 232448 && few_smem<true, 128, 32>() <= 232448, "shared memory");
+
+// D = A B with A and B in shared memory, operands' descriptors apart.
+template <bool F8>
+__device__ __forceinline__ void mma_few(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, bool acc) {
+    if constexpr (F8)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %5, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi),
+            "r"(idesc), "r"((uint32_t)acc));
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi),
+            "r"(idesc), "r"((uint32_t)acc));
+}
+
+// Instruction descriptor, fp32 accumulator: types and M-/N-majorness of A and B.
+constexpr uint32_t few_idesc(int type_a, int type_b, int M, int N, bool a_mn, bool b_mn) {
+    return (1u << 4) | ((uint32_t)type_a << 7) | ((uint32_t)type_b << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// N columns of TMEM (8, 16 or 32), not waited for.
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&x)[N]) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
+    if constexpr (N == 32) {
+        tmem_ld32(taddr, *reinterpret_cast<uint32_t(*)[32]>(r));
+    } else if constexpr (N == 16) {
+        tmem_ld16(taddr, *reinterpret_cast<uint32_t(*)[16]>(r));
+    } else {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : ACE_R8(r, 0) : "r"(taddr));
+    }
+}
+
+// Maximum over a warp (NaN counts as -inf): floats in the order of integers.
+__device__ __forceinline__ float warp_max(float x) {
+    int i = __float_as_int(x == x ? x : -INFINITY);
+    i ^= (i >> 31) & 0x7fffffff;
+    i = __reduce_max_sync(0xffffffffu, i);
+    return __int_as_float(i ^ ((i >> 31) & 0x7fffffff));
+}
+
+// Sums of v[r] over a warp by halving: lane returns the sum of row lane >> 1 (NR = 16, every pair of lanes) or lane (NR = 32).
+template <int NR>
+__device__ __forceinline__ float row_sums(float (&v)[NR], int lane) {
+    int o = 16;
+#pragma unroll
+    for (int n = NR / 2; n >= 1; n >>= 1, o >>= 1) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float send = lane & o ? v[i] : v[i + n], keep = lane & o ? v[i + n] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        }
+    }
+    if (NR == 16) v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
+    return v[0];
+}
+
+template <bool FP8, int D, int NR>
+__global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constant__ TcAttnArgs p) {
+    using C = FewCfg<FP8, D, NR>;
+    constexpr int NK = C::NK, NV = C::NV;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    using M = FewShared<FP8, NR>;
+    M& m = *reinterpret_cast<M*>(smem + C::OFF_MISC);
+    const AttnArgs& a = p.a;
+    volatile int* abort_flag = &m.abort_flag;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < NK; ++i) mbar_init(&m.k_full[i], 1), mbar_init(&m.k_empty[i], 1);
+        for (int i = 0; i < NV; ++i) mbar_init(&m.v_full[i], 1), mbar_init(&m.v_empty[i], 1), mbar_init(&m.v_ready[i], 4);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&m.s_full[i], 1);
+            mbar_init(&m.p_ready[i], 4);
+            mbar_init(&m.o_done[i], 1);
+            mbar_init(&m.group[i], 4);
+        }
+        mbar_init(&m.q_full, 4);
+        mbar_init(&m.q_free, 1);
+        mbar_init(&m.soft, 8);
+        mbar_init(&m.drain, 1);
+        for (int i = 0; i < kSegRing; ++i) {
+            mbar_init(&m.seg_full[i], 1);
+            mbar_init(&m.seg_empty[i], FP8 ? 15 : 14);  // load, MMA, (scales,) 8 softmax and 4 other warps
+        }
+        for (int i = 0; i < kAuxRing; ++i) {
+            mbar_init(&m.aux_full[i], 1);
+            mbar_init(&m.aux_empty[i], 4);
+        }
+        m.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&m.tmem)), "r"(C::COLS));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = m.tmem;
+    Walk walk{m, a, {}};
+
+    if (warp == 3) {
+        role_schedule<NR>(m, a);
+    } else if (warp == 0) {
+        role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V);
+    } else if (warp == 2) {
+        if constexpr (FP8) role_scales(m, a, m.kf, m.vf);
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issuer
+        if (elect_one()) {
+            Ring rk, rv;
+            uint32_t q_phase = 0, p_phase = 0;
+            const uint32_t q0 = desc_lo(smem_u32(smem + C::OFF_Q), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
+            const uint32_t v0 = desc_lo(smem_u32(smem + C::OFF_V), kVBlock), p0 = desc_lo(smem_u32(smem + C::OFF_P), 128);
+            constexpr uint32_t kHi = C::ROW == 64 ? kRows64 : kRows128;
+            constexpr uint32_t kPHi = desc_hi(128 * 16, 0);     // P^T: 16-byte pieces of 8 positions together, pieces 2 KB apart
+            bool ok = true;
+            while (true) {
+                if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
+                if (!m.seg[walk.seg.i].go) break;
+                const int tiles = m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0;
+                mbar_arrive(&m.seg_empty[walk.seg.i]);
+                walk.seg.next<kSegRing>();
+                if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
+                q_phase ^= 1u;
+                for (int i = 0; i <= tiles; ++i) {
+                    if (i < tiles) {
+                        // S^T of group i & 1: its scores of two tiles ago are read, or the product below had not been issued
+                        if (!mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t d = tmem + C::S + (uint32_t)((i & 1) * NR), kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4));
+                        if constexpr (FP8) {
+#pragma unroll
+                            for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
+                                const uint32_t st = kk % (D / 32) * 2;
+                                mma_few<true>(d, kl + st, kHi, q0 + (kk < D / 32 ? 0 : C::Q >> 5) + st, kHi, few_idesc(0, 0, 128, NR, false, false), kk > 0);
+                            }
+                        } else {
+#pragma unroll
+                            for (int kk = 0; kk < D / 16; ++kk)
+                                mma_few<false>(d, kl + (kk >> 2) * (16384 >> 4) + (kk & 3) * 2, kHi, q0 + (kk >> 2) * (NR * 128 >> 4) + (kk & 3) * 2,
+                                               kHi, few_idesc(1, 1, 128, NR, false, false), kk > 0);
+                        }
+                        mma_commit(&m.s_full[i & 1]);
+                        mma_commit(&m.k_empty[rk.i]);
+                        rk.next<NK>();
+                        if (i == tiles - 1) mma_commit(&m.q_free);
+                    }
+                    if (i > 0) {
+                        const int j = i - 1, g = j & 1;
+                        if (!mbar_wait_or_abort(&m.p_ready[g], p_phase >> g & 1u, a.err, abort_flag)) { ok = false; break; }
+                        p_phase ^= 1u << g;
+                        if (!mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t d = tmem + C::O + (uint32_t)(g * NR), vl = v0 + (uint32_t)(rv.i * (C::TILE >> 4));
+                        const uint32_t pl = p0 + (uint32_t)(g * (C::P >> 4));
+                        if constexpr (FP8) {
+#pragma unroll
+                            for (int kk = 0; kk < 16; ++kk) {           // 32 positions a step; four terms
+                                const uint32_t at = kk & 3;
+                                mma_few<true>(d, vl + at * (32 * C::ROW >> 4), kHi, pl + (kk >> 2) * (C::TERM >> 4) + at * 32, kPHi,
+                                              few_idesc(0, 1, D, NR, true, true), j >= 2 || kk > 0);
+                            }
+                        } else {
+#pragma unroll
+                            for (int kk = 0; kk < 8; ++kk)              // 16 positions a step
+                                mma_few<false>(d, vl + kk * 128, kRows128, pl + kk * 16, kPHi, few_idesc(1, 1, D, NR, true, true), j >= 2 || kk > 0);
+                        }
+                        mma_commit(&m.o_done[g]);
+                        mma_commit(&m.v_empty[rv.i]);
+                        rv.next<NV>();
+                    }
+                }
+                if (!ok) break;
+            }
+            if (!ok) *abort_flag = 1;
+            if (*abort_flag) {
+                // products in flight read shared memory and write TMEM
+                mma_commit(&m.drain);
+                mbar_wait(&m.drain, 0, a.err);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 12) {
+        // ------------------------------------------------ q rows; V tiles with drafted rows
+        const int tid = threadIdx.x - 384;
+        Ring rv;
+        uint32_t q_phase = 1;           // the first segment's q buffer is free
+        bool ok = true;
+        while (ok && walk.next()) {
+            const Segment& s = walk.segment();
+            const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
+            const float f_row0 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+            constexpr int kChunks = D / 8, kStep = 128 / kChunks, kTurns = NR / kStep;
+            uint4 qv[kTurns];
+#pragma unroll
+            for (int j = 0; j < kTurns; ++j) {
+                const int r = j * kStep + tid / kChunks;
+                qv[j] = r < s.rows ? load_q(a, s, s.row0 + r, tid % kChunks * 8) : make_uint4(0, 0, 0, 0);
+            }
+            // the rows are under way while the last products with the segment before read its q
+            if (!mbar_wait_warp(&m.q_free, q_phase, a.err, abort_flag)) { ok = false; break; }
+            q_phase ^= 1u;
+            unsigned char* tile = smem + C::OFF_Q;
+#pragma unroll 1
+            for (int j = 0; j < kTurns; ++j) {
+                const int r = j * kStep + tid / kChunks, c = tid % kChunks;
+                uint4 w0 = qv[0];
+#pragma unroll
+                for (int i = 1; i < kTurns; ++i)
+                    if (i == j) w0 = qv[i];
+                float f[8];
+                Vec16<__nv_bfloat16>::to_float(w0, f);
+                if constexpr (FP8) {
+                    float amax = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] = finite_or_nan(f[i] * q_mul), amax = fmaxf(amax, fabsf(f[i]));
+#pragma unroll
+                    for (int o = kChunks / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                    const int byte = e4m3_scale_byte(amax);
+                    const float mul = pow2_of_minus_byte(byte);
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = f[2 * i] * mul, y = f[2 * i + 1] * mul;
+                        hi[i] = e4m3x2(x, y);
+                        const uint32_t h = f16x2_of_e4m3x2(hi[i]);
+                        const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                        lo[i] = e4m3x2(x - back.x, y - back.y);
+                    }
+                    const int off = raw_v_offset<D>(r, c >> 1) + (c & 1) * 8;
+                    *reinterpret_cast<uint2*>(tile + off) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                    *reinterpret_cast<uint2*>(tile + C::Q / 2 + off) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                    if (c == 0) m.f_row[walk.seg.i & 1][r] = fmaxf(f_row0 * pow2_of_byte(byte), 0x1p-126f);   // 0 times a masked -inf is no score
+                } else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
+                        w[i] = *reinterpret_cast<const uint32_t*>(&v);
+                    }
+                    *reinterpret_cast<uint4*>(tile + (c >> 3) * (NR * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (c == 0) m.f_row[walk.seg.i & 1][r] = f_row0;
+                }
+                if (c == 0) m.node[walk.seg.i & 1][r] = r < s.rows ? (s.row0 + r) / a.group : 0;
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.q_full);
+            unsigned long long* bad = m.seg[walk.seg.i].bad;
+            for (int t = s.tile0; t < s.tile1; ++t) {
+                const int pos0 = t * kTcKeys;
+                if (!mbar_wait_warp(&m.v_full[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                if (pos0 + kTcKeys > s.len) {   // rows that not every node sees, or past the end
+                    unsigned char* v = smem + C::OFF_V + rv.i * C::TILE;
+                    if constexpr (FP8) clean_codes<D>(v, (tid >> 5) * 8 + (lane & 7), lane >> 3, s, pos0, bad);
+                    else clean_bf16<D>(v, tid, s, pos0, bad);
+                    fence_async_smem();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&m.v_ready[rv.i]);
+                rv.next<NV>();
+            }
+            if (ok) walk.done();
+        }
+        if (!ok) *abort_flag = 1;
+    } else {
+        // ------------------------------------------------ softmax: group g of 4 warps, a thread per position of a tile
+        const int g = (warp - 4) >> 2, quad = warp & 3, key = quad * 32 + lane, tid = threadIdx.x - 128;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        const uint32_t s_t = tmem + lanes + C::S + (uint32_t)(g * NR), o_t = tmem + lanes + C::O + (uint32_t)(g * NR);
+        unsigned char* p_out = smem + C::OFF_P + g * C::P + key * 16;
+        uint32_t s_phase = 0, o_phase = 0, soft_phase = 0, group_phase = 0;
+        auto soft_sync = [&]() -> bool {        // the eight warps meet
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.soft);
+            soft_phase ^= 1u;
+            return mbar_wait_warp(&m.soft, soft_phase ^ 1u, a.err, abort_flag);
+        };
+        auto group_sync = [&]() -> bool {       // this group's four warps meet
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.group[g]);
+            group_phase ^= 1u;
+            return mbar_wait_warp(&m.group[g], group_phase ^ 1u, a.err, abort_flag);
+        };
+        Ring ra;
+        bool ok = true;
+        while (ok && walk.next()) {
+            const Segment& s = walk.segment();
+            const int tiles = s.tile1 - s.tile0, total = s.len + s.n;
+            const float* f_row = m.f_row[walk.seg.i & 1];
+            float l[NR];
+#pragma unroll
+            for (int r = 0; r < NR; ++r) l[r] = 0.f;
+            int eref = 0, turn = 0;     // turn: which half of ref and flag holds
+            int mine = 0;
+            for (int t = 0; t < tiles; ++t) {
+                if ((t & 1) != g) {
+                    if (FP8) ra.next<kAuxRing>();
+                    continue;
+                }
+                const int pos = (s.tile0 + t) * kTcKeys + key;
+                float kf = 1.f, vf = 1.f;
+                int e_new = eref;
+                if (FP8) {
+                    if (!mbar_wait_warp(&m.aux_full[ra.i], ra.phase, a.err, abort_flag)) { ok = false; break; }
+                    kf = reinterpret_cast<const float*>(m.kf[ra.i])[key];
+                    vf = reinterpret_cast<const float*>(m.vf[ra.i])[key];
+                    e_new = m.eref[ra.i];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&m.aux_empty[ra.i]);
+                    ra.next<kAuxRing>();
+                }
+                if (!mbar_wait_warp(&m.s_full[g], s_phase, a.err, abort_flag)) { ok = false; break; }
+                s_phase ^= 1u;
+                tc_fence_after();
+                float x[NR];
+                tmem_ld<NR>(s_t, x);
+                tmem_ld_wait();
+                // scores in units of the softmax (base 2)
+#pragma unroll
+                for (int r = 0; r < NR; r += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(f_row + r);
+                    unpair(mul2(pair(x[r], x[r + 1]), mul2(pair(f.x, f.y), pair(kf, kf))), x[r], x[r + 1]);
+                    unpair(mul2(pair(x[r + 2], x[r + 3]), mul2(pair(f.z, f.w), pair(kf, kf))), x[r + 2], x[r + 3]);
+                }
+                if (pos >= s.len) {
+                    const int nd = pos - s.len;
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) {
+                        const bool sees = pos < total && (sees_word(a, s.node0, s.n, m.node[walk.seg.i & 1][r], nd >> 6) >> (nd & 63) & 1);
+                        if (!sees) x[r] = -INFINITY;
+                    }
+                }
+                bool waited = !mine;
+                const float* ref = m.ref[g][turn];
+                bool move = !mine || e_new != eref;
+                if (mine) {
+                    float over = -INFINITY;
+#pragma unroll
+                    for (int r = 0; r < NR; r += 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(ref + r);
+                        over = fmaxf(over, fmaxf(fmaxf(x[r] - f.x, x[r + 1] - f.y), fmaxf(x[r + 2] - f.z, x[r + 3] - f.w)));
+                    }
+                    const bool mine_over = __any_sync(0xffffffffu, over > (float)kLazy);
+                    if (lane == 0) m.flag[g][mine & 1][quad] = mine_over;
+                    if (!group_sync()) { ok = false; break; }
+                    const int4 fl = *reinterpret_cast<const int4*>(m.flag[g][mine & 1]);
+                    move = move || (fl.x | fl.y | fl.z | fl.w);
+                }
+                if (move) {
+                    // new references: the tile's maxima over the group's positions
+#pragma unroll 1
+                    for (int r0 = 0; r0 < NR; r0 += 4) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float v = x[i];
+#pragma unroll
+                            for (int r = 4; r < NR; r += 4)
+                                if (r == r0) v = x[r + i];
+                            v = warp_max(v);
+                            if (lane == 0) m.top[g][quad][r0 + i] = v;
+                        }
+                    }
+                    if (!group_sync()) { ok = false; break; }
+                    if (mine) {
+                        // the group's previous product has left O
+                        if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+                        o_phase ^= 1u;
+                        waited = true;
+                        tc_fence_after();
+                    }
+                    float o[NR];
+                    if (mine) {
+                        tmem_ld<NR>(o_t, o);
+                        tmem_ld_wait();
+                    }
+                    const float units = FP8 && mine ? (e_new - eref > 126 ? 0.f : pow2_of_byte(127 - (e_new - eref))) : 1.f;
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) {
+                        const float top = fmaxf(fmaxf(m.top[g][0][r], m.top[g][1][r]), fmaxf(m.top[g][2][r], m.top[g][3][r]));
+                        const float old = mine ? ref[r] : kNone;
+                        const float now = top > old + (float)kLazy ? top : old;
+                        const float f = exp2_approx(old - now);
+                        if (mine) {
+                            l[r] *= f;
+                            o[r] *= f * units;
+                        }
+                        if (key == r) m.ref[g][turn ^ 1][r] = now;
+                    }
+                    if (mine) {
+                        if constexpr (NR == 32) tmem_st32(o_t, *reinterpret_cast<const uint32_t(*)[32]>(&o));
+                        else tmem_st16(o_t, *reinterpret_cast<const uint32_t(*)[16]>(&o));
+                        tmem_st_wait();
+                    }
+                    turn ^= 1;
+                    eref = e_new;
+                    if (!group_sync()) { ok = false; break; }
+                    ref = m.ref[g][turn];
+                }
+                if (!waited) {
+                    if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+                    o_phase ^= 1u;
+                }
+                // weights: 16 rows' e5m2 terms, or 8 rows' bf16, are one 16-byte piece
+#pragma unroll
+                for (int b = 0; b < NR / 16; ++b) {
+                    uint32_t h[8];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const int r = 16 * b + i;
+                        const float4 f = *reinterpret_cast<const float4*>(ref + r);
+                        float e[4] = {x[r] - f.x, x[r + 1] - f.y, x[r + 2] - f.z, x[r + 3] - f.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]), l[r + j] += e[j];
+                        if constexpr (FP8) {
+                            const __half2 p0 = __floats2half2_rn(e[0] * vf, e[1] * vf), p1 = __floats2half2_rn(e[2] * vf, e[3] * vf);
+                            h[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                            h[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+                        } else {
+                            const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
+                            h[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                            h[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+                        }
+                    }
+                    if constexpr (FP8) {
+#pragma unroll
+                        for (int term = 0; term < 4; ++term) {
+                            uint4 w;
+                            w.x = __byte_perm(h[0], h[1], 0x7531);
+                            w.y = __byte_perm(h[2], h[3], 0x7531);
+                            w.z = __byte_perm(h[4], h[5], 0x7531);
+                            w.w = __byte_perm(h[6], h[7], 0x7531);
+                            *reinterpret_cast<uint4*>(p_out + term * C::TERM + b * 2048) = w;
+                            if (term < 3) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    const uint32_t top = h[i] & 0xff00ff00u;
+                                    const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&top));
+                                    h[i] = *reinterpret_cast<const uint32_t*>(&rest);
+                                }
+                            }
+                        }
+                    } else {
+                        *reinterpret_cast<uint4*>(p_out + (2 * b) * 2048) = make_uint4(h[0], h[1], h[2], h[3]);
+                        *reinterpret_cast<uint4*>(p_out + (2 * b + 1) * 2048) = make_uint4(h[4], h[5], h[6], h[7]);
+                    }
+                }
+                fence_async_smem();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&m.p_ready[g]);
+                ++mine;
+            }
+            if (!ok) break;
+            if (mine) {
+                if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+                o_phase ^= 1u;
+            }
+            tc_fence_after();
+            // ---------------- the unit's result, or this CTA's part of it: group g finishes half of the rows
+            {
+                const float sum = row_sums<NR>(l, lane);
+                if (NR == 32) m.sum[g][quad][lane] = sum;
+                else if (!(lane & 1)) m.sum[g][quad][lane >> 1] = sum;
+                if (key < NR) m.ref_end[g][key] = mine ? m.ref[g][turn][key] : kNone;
+                if (key == 0) m.eref_end[g] = eref;
+            }
+            if (!soft_sync()) { ok = false; break; }
+            const bool whole = s.part < 0;
+            const unsigned long long* bad = m.seg[walk.seg.i].bad;
+            const bool any_bad = bad[0] | bad[1] | bad[2] | bad[3];
+            constexpr int HALF = NR / 2;
+            const int r0 = g * HALF;
+            if (lane < HALF) {
+                const int r = r0 + lane;
+                const float x = m.ref_end[0][r], y = m.ref_end[1][r], top = fmaxf(x, y);
+                float u0 = exp2_approx(x - top), u1 = exp2_approx(y - top);
+                const float sum = ((m.sum[0][0][r] + m.sum[0][1][r]) + (m.sum[0][2][r] + m.sum[0][3][r])) * u0 +
+                                  ((m.sum[1][0][r] + m.sum[1][1][r]) + (m.sum[1][2][r] + m.sum[1][3][r])) * u1;
+                if (FP8) {
+                    u0 *= exp2f((float)(m.eref_end[0] - kVUp));
+                    u1 *= exp2f((float)(m.eref_end[1] - kVUp));
+                }
+                if (whole) {
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    u0 *= inv;
+                    u1 *= inv;
+                }
+                m.fac[warp - 4][lane] = make_float2(u0, u1);
+                if (quad == 0 && r < s.rows) {
+                    const float ref = top == kNone ? -INFINITY : top;
+                    const int ur = s.row0 + r, nd = ur / a.group;
+                    if (!whole) a.ws.part_ml[(long long)s.part * NR + r] = make_float2(ref, sum);
+                    else if (a.lse) a.lse[(long long)(s.node0 + nd) * a.n_heads + s.head * a.group + ur - nd * a.group] = (ref + log2f(sum)) * 0.69314718055994530942f;
+                }
+            }
+            __syncwarp();
+            {
+                // D = 64: an accumulator of 64 rows lies in the first 16 lanes of each warp's 32
+                const int d = D == 128 ? key : quad * 16 + lane;
+                const bool in = D == 128 || lane < 16;
+                float o0[HALF], o1[HALF];
+                tmem_ld<HALF>(tmem + lanes + C::O + (uint32_t)r0, o0);
+                if (tiles > 1) tmem_ld<HALF>(tmem + lanes + C::O + (uint32_t)(NR + r0), o1);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < HALF; ++i) {
+                    const int r = r0 + i;
+                    if (r >= s.rows) break;
+                    const float2 f = m.fac[warp - 4][i];
+                    float o = f.x == 0.f ? 0.f : o0[i] * f.x;
+                    if (tiles > 1 && f.y != 0.f) o += o1[i] * f.y;
+                    if (in) {
+                        const int hq = s.head * a.group + (s.row0 + r) - m.node[walk.seg.i & 1][r] * a.group;
+                        if (whole) static_cast<__nv_bfloat16*>(a.out)[((long long)(s.node0 + m.node[walk.seg.i & 1][r]) * a.n_heads + hq) * D + d] = from_f32<__nv_bfloat16>(o);
+                        else a.ws.part_o[((long long)s.part * NR + r) * D + d] = o;
+                    }
+                }
+                if (any_bad && in)
+                    for (int r = r0; r < min(r0 + HALF, s.rows); ++r) add_not_finite<FP8, NR>(a, s, bad, r, d, 1);
+            }
+            tc_fence_before();
+            if (!whole) __threadfence();
+            if (!soft_sync()) { ok = false; break; }        // O may be overwritten, partial results are written
+            if (!whole) {
+                if (tid == 0) m.joins = last_of_unit(a, s);
+                if (!soft_sync()) { ok = false; break; }
+                if (m.joins) {
+                    __threadfence();
+                    join_unit<__nv_bfloat16, NR>(a, s, tid, 256);
+                }
+            }
+            walk.done();
+        }
+        if (!ok) *abort_flag = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::COLS));
+}
+
+template <bool FP8, int D>
+cudaError_t few_attrs() {
+    const cudaError_t e = raise_smem_limit(k_attn_few<FP8, D, 16>, few_smem<FP8, D, 16>());
+    return e == cudaSuccess ? raise_smem_limit(k_attn_few<FP8, D, 32>, few_smem<FP8, D, 32>()) : e;
+}
+
+template <bool FP8, int D>
+cudaError_t few_go(const TcAttnArgs& p, int ctas, cudaStream_t s) {
+    if ((long long)p.a.max_nodes * p.a.group <= 16)
+        k_attn_few<FP8, D, 16><<<ctas, kTcThreads, few_smem<FP8, D, 16>(), s>>>(p);
+    else
+        k_attn_few<FP8, D, 32><<<ctas, kTcThreads, few_smem<FP8, D, 32>(), s>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t attn_few_init(const ace_kv* kv) {
+    const bool fp8 = kv->desc.format == ACE_KV_FP8;
+    if (kv->desc.head_dim == 128) return fp8 ? few_attrs<true, 128>() : few_attrs<false, 128>();
+    return fp8 ? few_attrs<true, 64>() : few_attrs<false, 64>();
+}
+
+cudaError_t launch_attn_few(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
+    TcAttnArgs p;
+    p.a = a;
+    p.k = kv->maps.k;
+    p.v = kv->maps.v;
+    p.box_rows = a.page_size < kTcKeys ? a.page_size : kTcKeys;
+    if (kv->desc.format == ACE_KV_FP8)
+        return a.head_dim == 128 ? few_go<true, 128>(p, kv->num_sms, s) : few_go<true, 64>(p, kv->num_sms, s);
+    return a.head_dim == 128 ? few_go<false, 128>(p, kv->num_sms, s) : few_go<false, 64>(p, kv->num_sms, s);
+}
+
+}  // namespace ace

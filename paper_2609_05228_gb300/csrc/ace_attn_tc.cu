@@ -14,28 +14,10 @@
 // hold 8 significant bits, all of a bf16 q (elements 2^-10 and more below the row's largest lose their last bits, a
 // 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory (exact), with
 // their scales on P: P V accumulates in units of 2^eref, a power of two above the scales seen so far.
-#include "ace_kv_device.cuh"
-#include "ace_tc.cuh"
+#include "ace_attn_tc.cuh"
 
 namespace ace {
 namespace {
-
-constexpr int kTcKeys = 128, kTcThreads = 512, kSegRing = 4, kAuxRing = 4;
-// A row's reference is its maximum less kPUp when it is set, and moves once the maximum is kLazy above that
-// (base 2): weights are at most 2^(kLazy + kPUp), which fp16 holds, and normal in fp16 down to 2^-(14 + kPUp) of the largest.
-constexpr int kLazy = 8, kPUp = 6;
-constexpr int kVUp = 6;                 // fp16 rows of V are code * 2^(e - eref + kVUp): at most 448 * 2^6, eref >= e
-constexpr int kConvThreads = 128;
-constexpr int kSoftRegs = 184, kOtherRegs = 72;
-static_assert(256 * (kSoftRegs + kOtherRegs) <= kTcThreads * 128, "the split must fit the launch's registers");
-// Every wait is on an mbarrier and bounded. A wait names a phase by its parity, so each waiter takes part in every phase
-// of its barriers, or what it waits for in between implies the phases that it leaves out.
-
-struct TcAttnArgs {
-    AttnArgs a;
-    CUtensorMap k, v;
-    int box_rows;                       // positions of a page in one box
-};
 
 template <bool FP8, int D, int RT, int CP>
 struct Cfg {
@@ -53,26 +35,14 @@ struct Cfg {
     static constexpr int OFF_MISC = OFF_MERGE + (CP > 1 ? 2 * 128 * 16 * 4 : 0);
 };
 
-struct TcSegment {
-    Segment s;
-    int go, pad;
-    unsigned long long bad[kMaxNodes / 64];     // nodes whose V row holds what is not finite
-};
-
 template <bool FP8, int RT>
-struct Misc {
-    uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], v_ready[6], c_empty[2];
-    uint64_t s_full[2], p_ready[2], o_done[2], q_full, q_free, soft, group[2], drain;
-    uint64_t seg_full[kSegRing], seg_empty[kSegRing], aux_full[kAuxRing], aux_empty[kAuxRing];
-    uint32_t tmem;
-    int abort_flag, joins, pad;
-    TcSegment seg[kSegRing];
+struct Misc : TcShared {
+    uint64_t c_empty[2];
     float2 ml[RT == 1 ? 256 : 1];               // RT = 1: both halves' running maximum and sum
     int eref1[RT == 1 ? 2 : 1];
     float q_scale[2][FP8 ? 128 * RT : 1];       // by turns of segments: softmax may be one behind
-    float4 kf[FP8 ? kAuxRing : 1][FP8 ? 32 : 1];            // 128 factors a tile
-    __half vf[FP8 ? kAuxRing : 1][FP8 ? 128 : 1];
-    int eref[kAuxRing];
+    float4 kf[FP8 ? kAuxRing : 1][32];          // 128 factors a tile
+    uint2 vf[FP8 ? kAuxRing : 1][32];           // the same as fp16
 };
 
 template <bool FP8, int D, int RT, int CP>
@@ -82,113 +52,6 @@ static_assert(tc_smem<false, 128, 2, 1>() <= 232448 && tc_smem<false, 128, 1, 2>
 static_assert(tc_smem<true, 128, 2, 1>() <= 232448 && tc_smem<true, 128, 1, 2>() <= 232448, "shared memory");
 static_assert(tc_smem<false, 64, 2, 1>() <= 232448 && tc_smem<true, 64, 1, 2>() <= 232448, "shared memory");
 
-// Shared-memory descriptors by halves: the low word holds the address, to which a K step adds, and the leading byte
-// offset; the high one the stride byte offset, the version and the swizzle (2: 128 bytes, 4: 64 bytes).
-constexpr uint32_t desc_hi(uint32_t sbo, uint32_t swizzle) { return (sbo >> 4) | 1u << 14 | swizzle << 29; }
-__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return addr >> 4 | (lbo >> 4) << 16; }
-constexpr uint32_t kRows128 = desc_hi(1024, 2);     // K-major rows of 128 bytes, or V as stored (8 K indices to the next group)
-constexpr uint32_t kRows64 = desc_hi(512, 4);       // K-major rows of 64 bytes
-constexpr uint32_t kVBlock = 16384;                 // V: to the next 64 dimensions
-
-// Instruction descriptor: fp32 accumulator; type codes of A and B (kind::f16: 0 fp16, 1 bf16; kind::f8f6f4: 0 e4m3).
-__host__ __device__ constexpr uint32_t idesc_of(int type, int M, int N, bool b_mn) {
-    return (1u << 4) | ((uint32_t)type << 7) | ((uint32_t)type << 10) | ((b_mn ? 1u : 0u) << 16) |
-           ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-
-template <bool F8>
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool acc) {
-    if constexpr (F8)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
-            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc),
-            "r"((uint32_t)acc));
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
-            "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc),
-            "r"((uint32_t)acc));
-}
-
-// A from TMEM.
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool acc) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc),
-        "r"((uint32_t)acc));
-}
-
-#define ACE_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
-#define ACE_V8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
-
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : ACE_R8(r, 0), ACE_R8(r, 8), ACE_R8(r, 16), ACE_R8(r, 24)
-        : "r"(taddr));
-}
-
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::ACE_V8(r, 0),
-        ACE_V8(r, 8), ACE_V8(r, 16), ACE_V8(r, 24), "r"(taddr)
-        : "memory");
-}
-
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::ACE_V8(r, 0),
-        ACE_V8(r, 8), "r"(taddr)
-        : "memory");
-}
-
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// Two fp32 values in one operation each.
-__device__ __forceinline__ uint64_t pair(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
-// Which of the 32 keys from position `pos` on row `node` sees: the prefix, and the nodes of its mask.
-__device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, int node, int pos) {
-    const int m0 = pos - s.len;         // first node
-    if (m0 <= -32) return 0xffffffffu;
-    const int from = m0 < 0 ? 0 : m0;
-    const int w = from >> 6, sh = from & 63;
-    unsigned long long bits = sees_word(a, s.node0, s.n, node, w) >> sh;
-    if (sh > 32) bits |= sees_word(a, s.node0, s.n, node, w + 1) << (64 - sh);
-    uint32_t r = (uint32_t)bits;
-    if (m0 < 0) r = r << -m0 | ((1u << -m0) - 1u);
-    return r;
-}
-
 // The tile's loops are rolled (32 scores a turn) on purpose: unrolled over a tile's 128 scores they and the fp16
 // conversion overflow the instruction cache, and warps that run different roles then stall on fetches (a fp8 tile of
 // 128 rows 9600 cycles unrolled; no_instruction stalls 2.7 an issue against 0.5).
@@ -197,11 +60,16 @@ __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, 
 template <bool FP8>
 __device__ __forceinline__ void load_scores(uint32_t s_t, float (&x)[32], const float4* kf, bool masked, uint32_t see) {
     tmem_ld32(s_t, *reinterpret_cast<uint32_t(*)[32]>(&x));
+    float4 k[8];
+    if (FP8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] = kf[i];
+    }
     tmem_ld_wait();
     if (FP8) {
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-            const float4 f = kf[i / 4];
+            const float4 f = k[i / 4];
             unpair(mul2(pair(x[i], x[i + 1]), pair(f.x, f.y)), x[i], x[i + 1]);
             unpair(mul2(pair(x[i + 2], x[i + 3]), pair(f.z, f.w)), x[i + 2], x[i + 3]);
         }
@@ -301,49 +169,6 @@ __device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s
     tmem_st_wait();
 }
 
-// Values of V that are not finite were left out of the products: row `urow` of the unit, written already, gets those of
-// the nodes that it sees in dimensions d .. d + 3.
-template <bool FP8, int ROWS>
-__device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment& s, const unsigned long long* bad, int urow, int d) {
-    const int nd = (s.row0 + urow) / a.group, hq = s.head * a.group + (s.row0 + urow) % a.group;
-#pragma unroll 1
-    for (int m = 0; m < s.n; ++m) {
-        if (!(bad[m >> 6] & sees_word(a, s.node0, s.n, nd, m >> 6) & 1ull << (m & 63))) continue;
-        const int page = page_of(a, s.b, s.len + m);
-        if (page < 0) continue;
-        const long long row = ((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + m) & (a.page_size - 1));
-#pragma unroll 1
-        for (int i = d; i < d + 4; ++i) {
-            float v;
-            if constexpr (FP8) v = (static_cast<const uint8_t*>(a.v_pool)[row * a.head_dim + i] & 0x7f) == 0x7f ? __uint_as_float(0x7fffffffu) : 0.f;
-            else v = to_f32(static_cast<const __nv_bfloat16*>(a.v_pool)[row * a.head_dim + i]);
-            if (fabsf(v) < INFINITY) continue;
-            if (s.part < 0) {
-                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + ((long long)(s.node0 + nd) * a.n_heads + hq) * a.head_dim + i;
-                *out = from_f32<__nv_bfloat16>(to_f32(*out) + v);
-            } else {
-                a.ws.part_o[((long long)s.part * ROWS + urow) * a.head_dim + i] += v;
-            }
-        }
-    }
-}
-
-// 8 elements of a unit's q row (bf16), from dimension d on.
-__device__ __forceinline__ uint4 load_q(const AttnArgs& a, const Segment& s, int row, int d) {
-    const int nd = row / a.group;
-    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (s.node0 + nd) * a.q_token_stride +
-                               (s.head * a.group + row - nd * a.group) * a.q_head_stride + d;
-    if ((uintptr_t)src % 16 == 0) return __ldg(reinterpret_cast<const uint4*>(src));
-    const uint16_t* u = reinterpret_cast<const uint16_t*>(src);
-    return make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
-}
-
-// Place of codes 16 c .. 16 c + 15 of a row in a tile of V as TMA leaves it (rows of 128 or 64 bytes, swizzled).
-template <int D>
-__device__ __forceinline__ int raw_v_offset(int row, int c) {
-    return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
-}
-
 // Two codes as fp16 times `f`.
 __device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
     const uint32_t y = f16x2_of_e4m3x2(codes);
@@ -351,51 +176,12 @@ __device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
     return *reinterpret_cast<const uint32_t*>(&z);
 }
 
-// A tile of V codes with drafted rows: zeros past the end and in place of NaN (all bits of a code but the sign), whose
-// nodes are noted. Each thread cleans the 16 codes that it reads afterwards (row0 and c0 of the first).
-template <int D>
-__device__ __forceinline__ void clean_codes(unsigned char* v, int row0, int c0, const Segment& s, int pos0, unsigned long long* bad) {
-    const int total = s.len + s.n;
-#pragma unroll 1
-    for (int i = 0; i < D / 16; ++i) {
-        const int row = row0 + (i & 3) * 32, pos = pos0 + row;
-        if (pos < s.len) continue;
-        uint4* at = reinterpret_cast<uint4*>(v + raw_v_offset<D>(row, c0 + (i >> 2) * 4));
-        if (pos >= total) {
-            *at = make_uint4(0, 0, 0, 0);
-            continue;
-        }
-        const uint4 w = *at;
-        uint32_t x[4] = {w.x, w.y, w.z, w.w}, any = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t nan = ((x[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-            any |= nan;
-            x[j] &= ~((nan >> 7) * 0xffu);
-        }
-        if (any) {
-            *at = make_uint4(x[0], x[1], x[2], x[3]);
-            atomicOr(&bad[(pos - s.len) >> 6], 1ull << ((pos - s.len) & 63));
-        }
-    }
-}
-
-struct Ring {
-    int i = 0;
-    uint32_t phase = 0;
-    template <int N>
-    __device__ __forceinline__ void next() {
-        if (++i == N) i = 0, phase ^= 1u;
-    }
-};
-
 // CP: with few rows (RT = 1) the block holds them CP = 2 or 4 times, 64 or 32 lanes apart, and each copy's warps take that
 // share of a tile's columns: the tile's softmax takes as much less time, and the copies' O are added at the end.
 template <bool FP8, int D, int RT, int CP>
 __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant__ TcAttnArgs p) {
     using C = Cfg<FP8, D, RT, CP>;
     constexpr int ROWS = C::ROWS, NK = C::NK, NV = C::NV, NC = C::NC;
-    constexpr int kHalves = D / 64;                     // 64-element blocks of a bf16 / fp16 row
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     using M = Misc<FP8, RT>;
@@ -438,100 +224,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     tc_fence_after();
     const uint32_t tmem = m.tmem;                       // S0, S1, O0, O1
     constexpr uint32_t kO = 256;
-    Ring seg;
+    Walk walk{m, a, {}};
 
-    // Every role but the scheduler walks the CTA's segments; false: no more (or aborted).
-    // The segment stays in shared memory until segment_done().
-    auto next_segment = [&]() -> bool {
-        if (!mbar_wait_warp(&m.seg_full[seg.i], seg.phase, a.err, abort_flag)) {
-            *abort_flag = 1;
-            return false;
-        }
-        return m.seg[seg.i].go != 0;
-    };
-    auto segment_done = [&]() {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&m.seg_empty[seg.i]);
-        seg.next<kSegRing>();
-    };
-
-    // the softmax warps, which keep a row's scores in registers, take registers of the others' (one instruction a warpgroup)
-    if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == 3) {
-        // ------------------------------------------------ scheduler
-        Cursor cur{};
-        bool more = cursor_init<ROWS, kTcKeys>(a, blockIdx.x, gridDim.x, cur);
-        while (true) {
-            if (!mbar_wait_warp(&m.seg_empty[seg.i], seg.phase ^ 1u, a.err, abort_flag)) {
-                *abort_flag = 1;
-                break;
-            }
-            Segment s{};
-            more = more && cursor_next<ROWS, kTcKeys>(a, blockIdx.x, cur, s);
-            if (lane == 0) {
-                m.seg[seg.i].s = s;
-                m.seg[seg.i].go = more;
-                for (int w = 0; w < kMaxNodes / 64; ++w) m.seg[seg.i].bad[w] = 0;
-                mbar_arrive(&m.seg_full[seg.i]);
-            }
-            seg.next<kSegRing>();
-            if (!more) break;
-        }
+        role_schedule<ROWS>(m, a);
     } else if (warp == 0) {
-        // ------------------------------------------------ TMA: lane x loads box x of a tile
-        Ring rk, rv;
-        long long nk = 0, nv = 0;
-        bool ok = true;
-        const int boxes = kTcKeys / p.box_rows;
-        while (ok && next_segment()) {
-            const Segment& s = m.seg[seg.i].s;
-            const int total = s.len + s.n;
-            // a tile's pages are looked up while the tile before it is loaded
-            auto look_up = [&](int t) {
-                const int at = t * kTcKeys + lane * p.box_rows;
-                return t < s.tile1 && lane < boxes && at < total ? page_of(a, s.b, at) : -1;
-            };
-            int next_page = look_up(s.tile0);
-            for (int t = s.tile0; t < s.tile1; ++t) {
-                const int pos = t * kTcKeys + lane * p.box_rows;
-                const int page = next_page;
-                next_page = look_up(t + 1);
-                const int row = a.row0 + (page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-                const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= 0)) * (uint32_t)(p.box_rows * (C::TILE / 128));
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    Ring& r = kv ? rv : rk;
-                    uint64_t* full = kv ? m.v_full : m.k_full;
-                    uint64_t* empty = kv ? m.v_empty : m.k_empty;
-                    if (!mbar_wait_warp(&empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
-                    if (lane == 0) mbar_expect_tx(&full[r.i], bytes);
-                    __syncwarp();
-                    if (page >= 0) {
-                        unsigned char* dst = smem + (kv ? C::OFF_V : C::OFF_K) + r.i * C::TILE;
-                        const CUtensorMap* map = kv ? &p.v : &p.k;
-                        if constexpr (FP8) {
-                            tma_load_2d(dst + lane * p.box_rows * D, map, &full[r.i], 0, row);
-                        } else {
-#pragma unroll
-                            for (int h = 0; h < kHalves; ++h)
-                                tma_load_2d(dst + h * 16384 + lane * p.box_rows * 128, map, &full[r.i], h * 64, row);
-                        }
-                    }
-                    if (kv) ++nv, rv.next<NV>(); else ++nk, rk.next<NK>();
-                }
-                if (!ok) break;
-            }
-            segment_done();
-        }
-        if (!ok) *abort_flag = 1;
-        if (*abort_flag) {
-            // let the copies already issued land before the CTA exits
-            for (long long f = nk - 1; f >= 0 && f >= nk - NK; --f)
-                if (!mbar_wait(&m.k_full[f % NK], (uint32_t)((f / NK) & 1), a.err)) break;
-            for (long long f = nv - 1; f >= 0 && f >= nv - NV; --f)
-                if (!mbar_wait(&m.v_full[f % NV], (uint32_t)((f / NV) & 1), a.err)) break;
-        }
+        role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V);
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issuer
         if (elect_one()) {
@@ -543,11 +241,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             const uint32_t v0 = desc_lo(smem_u32(smem + (FP8 ? C::OFF_C : C::OFF_V)), kVBlock);
             bool ok = true;
             while (true) {
-                if (!mbar_wait_or_abort(&m.seg_full[seg.i], seg.phase, a.err, abort_flag)) { ok = false; break; }
-                if (!m.seg[seg.i].go) break;
-                const int items = (m.seg[seg.i].s.tile1 - m.seg[seg.i].s.tile0) * RT;
-                mbar_arrive(&m.seg_empty[seg.i]);
-                seg.next<kSegRing>();
+                if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
+                if (!m.seg[walk.seg.i].go) break;
+                const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * RT;
+                mbar_arrive(&m.seg_empty[walk.seg.i]);
+                walk.seg.next<kSegRing>();
                 if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
                 q_phase ^= 1u;
                 for (int i = 0; i <= items; ++i) {
@@ -610,79 +308,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         }
         __syncwarp();
     } else if (warp == 2) {
-        // ------------------------------------------------ scales of fp8 rows: 4 positions a lane
-        if constexpr (FP8) {
-            Ring r;
-            bool ok = true;
-            while (ok && next_segment()) {
-                const Segment& s = m.seg[seg.i].s;
-                const int total = s.len + s.n;
-                int eref = -1000;
-                // pages two tiles and scales one tile ahead
-                auto look_up = [&](int t) {
-                    const int at = t * kTcKeys + lane * 4;
-                    return t < s.tile1 && at < total ? page_of(a, s.b, at) : -1;
-                };
-                auto load = [&](int page, int t, uint32_t& kb, uint32_t& vb) {
-                    kb = vb = 0;
-                    if (page >= 0) {
-                        const long long at = ((long long)page * a.kv_heads + s.head) * a.page_size + ((t * kTcKeys + lane * 4) & (a.page_size - 1));
-                        kb = __ldg(reinterpret_cast<const uint32_t*>(a.k_scale + at));
-                        vb = __ldg(reinterpret_cast<const uint32_t*>(a.v_scale + at));
-                    }
-                };
-                uint32_t kb_next, vb_next;
-                load(look_up(s.tile0), s.tile0, kb_next, vb_next);
-                int next_page = look_up(s.tile0 + 1);
-                for (int t = s.tile0; t < s.tile1; ++t) {
-                    const int pos = t * kTcKeys + lane * 4;
-                    uint32_t kb = kb_next, vb = vb_next;
-                    load(next_page, t + 1, kb_next, vb_next);
-                    next_page = look_up(t + 2);
-                    if (pos + 4 > total) {
-                        const int left = total - pos;       // positions of the four that exist
-                        const uint32_t have = left <= 0 ? 0u : 0xffffffffu >> (8 * (4 - left));
-                        kb &= have;
-                        vb &= have;
-                    }
-                    int top = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) top = max(top, (int)(vb >> (8 * i) & 0xff));
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    // two octaves of room, so that small differences between tiles do not move it
-                    if (top - 127 > eref) eref = top - 127 + 2;
-                    float kf[4];
-                    alignas(8) __half vf[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int vbyte = (int)(vb >> (8 * i) & 0xff);
-                        kf[i] = pow2_of_byte((int)(kb >> (8 * i) & 0xff));
-                        const int e = vbyte - eref + kVUp;      // biased exponent
-                        vf[i] = __float2half_rn(vbyte == 0 || e <= 0 ? 0.f : pow2_of_byte(e));
-                    }
-                    if (!mbar_wait_warp(&m.aux_empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
-                    m.kf[r.i][lane] = make_float4(kf[0], kf[1], kf[2], kf[3]);
-                    *reinterpret_cast<uint2*>(&m.vf[r.i][lane * 4]) = *reinterpret_cast<const uint2*>(vf);
-                    if (lane == 0) m.eref[r.i] = eref;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&m.aux_full[r.i]);
-                    r.next<kAuxRing>();
-                }
-                if (ok) segment_done();
-            }
-            if (!ok) *abort_flag = 1;
-        }
-    }
+        if constexpr (FP8) role_scales(m, a, m.kf, m.vf);
     } else if (warp >= 12) {
         // ------------------------------------------------ q rows, and V tiles made ready
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         const int tid = threadIdx.x - 384;
         Ring rv, rc, ra;
         uint32_t q_phase = 1;           // the first segment's q buffer is free
         bool ok = true;
-        while (ok && next_segment()) {
-            const Segment& s = m.seg[seg.i].s;
+        while (ok && walk.next()) {
+            const Segment& s = walk.segment();
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
             constexpr int kStep = 128 / kChunks, kBatch = 4;        // rows a pass; passes whose loads are under way together
@@ -732,7 +366,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                             *reinterpret_cast<uint2*>(tile + off + (c & 1) * 8) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
                             *reinterpret_cast<uint2*>(tile + C::Q / 2 + off + (c & 1) * 8) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
                         }
-                        if (c == 0) m.q_scale[seg.i & 1][r] = pow2_of_byte(byte);
+                        if (c == 0) m.q_scale[walk.seg.i & 1][r] = pow2_of_byte(byte);
                     } else {
                         if (r >= s.rows) continue;
                         uint32_t w[4];
@@ -751,8 +385,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&m.q_full);
-            unsigned long long* bad = m.seg[seg.i].bad;
-            const int total = s.len + s.n;
+            unsigned long long* bad = m.seg[walk.seg.i].bad;
             for (int t = s.tile0; t < s.tile1; ++t) {
                 const int pos0 = t * kTcKeys;
                 const bool drafted = pos0 + kTcKeys > s.len;    // rows that not every node sees, or past the end
@@ -770,7 +403,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     const unsigned char* src0 = v + raw_v_offset<D>(row0, lane >> 3);
                     unsigned char* dst0 = out + row0 * 128 + (((lane >> 3) * 2 ^ (lane & 7)) << 4);
                     unsigned char* dst1 = out + row0 * 128 + (((lane >> 3) * 2 ^ (lane & 7) ^ 1) << 4);
-                    const __half* vf = m.vf[ra.i] + row0;
+                    const __half* vf = reinterpret_cast<const __half*>(m.vf[ra.i]) + row0;
 #pragma unroll 1
                     for (int i = 0; i < 4; ++i) {
                         // a turn's loads before its stores; rows 32 apart share their swizzle, and the other 64 codes of a
@@ -804,27 +437,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     rc.next<NC ? NC : 1>();
                 } else {
                     if (drafted) {
-                        for (int u = tid; u < 128 * kChunks; u += kConvThreads) {
-                            const int row = u / kChunks, c = u % kChunks;
-                            if (pos0 + row < s.len) continue;
-                            uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
-                            if (pos0 + row >= total) {
-                                *at = make_uint4(0, 0, 0, 0);
-                                continue;
-                            }
-                            uint4 w = *at;
-                            uint32_t* x = reinterpret_cast<uint32_t*>(&w);
-                            bool found = false;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if ((x[i] & 0x7f80u) == 0x7f80u) found = true, x[i] &= 0xffff0000u;
-                                if ((x[i] & 0x7f800000u) == 0x7f800000u) found = true, x[i] &= 0xffffu;
-                            }
-                            if (found) {
-                                *at = w;
-                                atomicOr(&bad[(pos0 + row - s.len) >> 6], 1ull << ((pos0 + row - s.len) & 63));
-                            }
-                        }
+                        clean_bf16<D>(v, tid, s, pos0, bad);
                         fence_async_smem();
                     }
                     __syncwarp();
@@ -832,12 +445,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 }
                 rv.next<NV>();
             }
-            if (ok) segment_done();
+            if (ok) walk.done();
         }
         if (!ok) *abort_flag = 1;
     } else {
         // ------------------------------------------------ softmax: group g of 4 warps, a thread per row
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         const int g = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const int tid = threadIdx.x - 128;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
@@ -860,8 +472,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             return mbar_wait_warp(&m.group[g], group_phase ^ 1u, a.err, abort_flag);
         };
         bool ok = true;
-        while (ok && next_segment()) {
-            const Segment& s = m.seg[seg.i].s;
+        while (ok && walk.next()) {
+            const Segment& s = walk.segment();
             constexpr int apart = 128 / CP;
             const int row = RT == 2 ? g * 128 + r : r & (apart - 1);        // of the unit
             const int col = RT == 2 ? 0 : r / apart * apart;                // first column of this copy
@@ -891,7 +503,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 if (warp_live) {
                     const float4* kf = m.kf[FP8 ? ra.i : 0];
                     if (FP8) {
-                        f_row = fmaxf(f_row0 * m.q_scale[seg.i & 1][row], 0x1p-126f);     // 0 times a masked -inf is no score
+                        if (!mine) f_row = fmaxf(f_row0 * m.q_scale[walk.seg.i & 1][row], 0x1p-126f);    // 0 times a masked -inf is no score
                         const int e = m.eref[ra.i];
                         if (mine && e > eref) st.o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
                         eref = e;
@@ -957,7 +569,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 up0 = st.ref == -INFINITY ? 0.f : FP8 ? exp2f((float)(eref - kVUp)) : 1.f;
             }
             // (read behind the meeting above: a group without tiles has waited for nothing else)
-            const unsigned long long* bad = m.seg[seg.i].bad;
+            const unsigned long long* bad = m.seg[walk.seg.i].bad;
             const bool any_bad = bad[0] | bad[1] | bad[2] | bad[3];
             if (whole) {
                 const float inv = l_all == 0.f ? 0.f : 1.f / l_all;
@@ -1020,7 +632,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         emit4(urow, (long long)(s.node0 + nd) * a.n_heads + s.head * a.group + ur - nd * a.group, c + q4 * 4, o);
                     }
                     if (any_bad)
-                        for (int i = r; i < s.rows * (w / 4); i += 128) add_not_finite<FP8, ROWS>(a, s, bad, i / (w / 4), c + i % (w / 4) * 4);
+                        for (int i = r; i < s.rows * (w / 4); i += 128) add_not_finite<FP8, ROWS>(a, s, bad, i / (w / 4), c + i % (w / 4) * 4, 4);
                     if (c + wide < c1 && !group_sync()) { ok = false; break; }
                 }
                 if (!ok) break;
@@ -1043,7 +655,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     }
                 }
                 if (any_bad && live)
-                    for (int d = c0; d < c1; d += 4) add_not_finite<FP8, ROWS>(a, s, bad, row, d);
+                    for (int d = c0; d < c1; d += 4) add_not_finite<FP8, ROWS>(a, s, bad, row, d, 4);
             }
             if (live && c0 == 0 && r < apart) {
                 if (!whole) a.ws.part_ml[(long long)s.part * ROWS + row] = make_float2(m_all, l_all);
@@ -1062,7 +674,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     }
                 }
             }
-            segment_done();
+            walk.done();
         }
         if (!ok) *abort_flag = 1;
     }
@@ -1074,18 +686,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
 
 template <bool FP8, int D, int RT, int CP>
 cudaError_t tc_attr() {
-    // a split above what the block is launched with would wait for ever
-    cudaFuncAttributes f;
-    const cudaError_t e = cudaFuncGetAttributes(&f, k_attn_tc<FP8, D, RT, CP>);
-    if (e != cudaSuccess) return e;
-    if (f.numRegs * kTcThreads < 256 * (kSoftRegs + kOtherRegs)) return cudaErrorLaunchOutOfResources;
     return raise_smem_limit(k_attn_tc<FP8, D, RT, CP>, tc_smem<FP8, D, RT, CP>());
 }
 
 template <bool FP8, int D>
 cudaError_t tc_attrs() {
-    cudaError_t e = tc_attr<FP8, D, 1, 4>();
-    if (e == cudaSuccess) e = tc_attr<FP8, D, 1, 2>();
+    cudaError_t e = tc_attr<FP8, D, 1, 2>();
     if (e == cudaSuccess) e = tc_attr<FP8, D, 1, 1>();
     return e == cudaSuccess ? tc_attr<FP8, D, 2, 1>() : e;
 }
@@ -1101,7 +707,6 @@ cudaError_t tc_launch(const TcAttnArgs& p, int ctas, cudaStream_t s) {
     // by the rows of the largest tree: one block of 128 rows a unit where that holds them (as often as it can), else two
     // that share the loaded tiles
     const long long rows = (long long)p.a.max_nodes * p.a.group;
-    if (rows <= 32) return tc_go<FP8, D, 1, 4>(p, ctas, s);
     if (rows <= 64) return tc_go<FP8, D, 1, 2>(p, ctas, s);
     if (rows <= 128) return tc_go<FP8, D, 1, 1>(p, ctas, s);
     return tc_go<FP8, D, 2, 1>(p, ctas, s);
@@ -1118,7 +723,8 @@ cudaError_t attn_tc_init(ace_kv* kv) {
     const bool fp8 = D.format == ACE_KV_FP8;
     const uint64_t rows = (uint64_t)D.layers * D.n_pages * D.n_kv_heads * D.page_size;
     const uint32_t box = D.page_size < kTcKeys ? D.page_size : kTcKeys;
-    cudaError_t e;
+    cudaError_t e = attn_few_init(kv);
+    if (e != cudaSuccess) return e;
     if (fp8) {
         const int swizzle = D.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
         if ((e = make_byte_map(&kv->maps.k, kv->k_pool, rows, D.head_dim, box, swizzle)) != cudaSuccess) return e;
@@ -1131,6 +737,7 @@ cudaError_t attn_tc_init(ace_kv* kv) {
 }
 
 cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
+    if ((long long)a.max_nodes * a.group <= kFewRows) return launch_attn_few(kv, a, s);
     TcAttnArgs p;
     p.a = a;
     p.k = kv->maps.k;

@@ -1,0 +1,444 @@
+// ace_attn_tc.cuh — what the tensor-core attention kernels share: the roles that schedule, load and stage scales,
+// and the wrappers of their instructions.
+#pragma once
+
+#include "ace_kv_device.cuh"
+#include "ace_tc.cuh"
+
+namespace ace {
+namespace {
+
+constexpr int kTcKeys = 128, kTcThreads = 512, kSegRing = 4, kAuxRing = 4;
+// A row's reference is its maximum less kPUp when it is set, and moves once the maximum is kLazy above that
+// (base 2): weights are at most 2^(kLazy + kPUp), which fp16 holds, and normal in fp16 down to 2^-(14 + kPUp) of the largest.
+constexpr int kLazy = 8, kPUp = 6;
+constexpr int kVUp = 6;                 // fp16 rows of V are code * 2^(e - eref + kVUp): at most 448 * 2^6, eref >= e
+constexpr int kConvThreads = 128;
+// Every wait is on an mbarrier and bounded. A wait names a phase by its parity, so each waiter takes part in every phase
+// of its barriers, or what it waits for in between implies the phases that it leaves out.
+
+struct TcAttnArgs {
+    AttnArgs a;
+    CUtensorMap k, v;
+    int box_rows;                       // positions of a page in one box
+};
+
+struct Ring {
+    int i = 0;
+    uint32_t phase = 0;
+    template <int N>
+    __device__ __forceinline__ void next() {
+        if (++i == N) i = 0, phase ^= 1u;
+    }
+};
+
+struct TcSegment {
+    Segment s;
+    int go, pad;
+    unsigned long long bad[kMaxNodes / 64];     // nodes whose V row holds what is not finite
+};
+
+// Barriers and hand-overs of a CTA.
+struct TcShared {
+    uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], v_ready[6];
+    uint64_t s_full[2], p_ready[2], o_done[2], q_full, q_free, soft, group[2], drain;
+    uint64_t seg_full[kSegRing], seg_empty[kSegRing], aux_full[kAuxRing], aux_empty[kAuxRing];
+    uint32_t tmem;
+    int abort_flag, joins, pad;
+    TcSegment seg[kSegRing];
+    int eref[kAuxRing];
+};
+
+// Shared-memory descriptors by halves: the low word holds the address, to which a K step adds, and the leading byte
+// offset; the high one the stride byte offset, the version and the swizzle (2: 128 bytes, 4: 64 bytes).
+constexpr uint32_t desc_hi(uint32_t sbo, uint32_t swizzle) { return (sbo >> 4) | 1u << 14 | swizzle << 29; }
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return addr >> 4 | (lbo >> 4) << 16; }
+constexpr uint32_t kRows128 = desc_hi(1024, 2);     // K-major rows of 128 bytes, or V as stored (8 K indices to the next group)
+constexpr uint32_t kRows64 = desc_hi(512, 4);       // K-major rows of 64 bytes
+constexpr uint32_t kVBlock = 16384;                 // V: to the next 64 dimensions
+
+// Instruction descriptor: fp32 accumulator; type codes of A and B (kind::f16: 0 fp16, 1 bf16; kind::f8f6f4: 0 e4m3).
+__host__ __device__ constexpr uint32_t idesc_of(int type, int M, int N, bool b_mn) {
+    return (1u << 4) | ((uint32_t)type << 7) | ((uint32_t)type << 10) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+template <bool F8>
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool acc) {
+    if constexpr (F8)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc),
+            "r"((uint32_t)acc));
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc),
+            "r"((uint32_t)acc));
+}
+
+// A from TMEM.
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc),
+        "r"((uint32_t)acc));
+}
+
+#define ACE_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define ACE_V8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : ACE_R8(r, 0), ACE_R8(r, 8), ACE_R8(r, 16), ACE_R8(r, 24)
+        : "r"(taddr));
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::ACE_V8(r, 0),
+        ACE_V8(r, 8), ACE_V8(r, 16), ACE_V8(r, 24), "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::ACE_V8(r, 0),
+        ACE_V8(r, 8), "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Two fp32 values in one operation each.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// Which of the 32 keys from position `pos` on row `node` sees: the prefix, and the nodes of its mask.
+__device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, int node, int pos) {
+    const int m0 = pos - s.len;         // first node
+    if (m0 <= -32) return 0xffffffffu;
+    const int from = m0 < 0 ? 0 : m0;
+    const int w = from >> 6, sh = from & 63;
+    unsigned long long bits = sees_word(a, s.node0, s.n, node, w) >> sh;
+    if (sh > 32) bits |= sees_word(a, s.node0, s.n, node, w + 1) << (64 - sh);
+    uint32_t r = (uint32_t)bits;
+    if (m0 < 0) r = r << -m0 | ((1u << -m0) - 1u);
+    return r;
+}
+
+// Values of V that are not finite were left out of the products: row `urow` of the unit, written already, gets those of
+// the nodes that it sees in dimensions d .. d + count - 1.
+template <bool FP8, int ROWS>
+__device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment& s, const unsigned long long* bad, int urow, int d,
+                                               int count) {
+    const int nd = (s.row0 + urow) / a.group, hq = s.head * a.group + (s.row0 + urow) % a.group;
+#pragma unroll 1
+    for (int m = 0; m < s.n; ++m) {
+        if (!(bad[m >> 6] & sees_word(a, s.node0, s.n, nd, m >> 6) & 1ull << (m & 63))) continue;
+        const int page = page_of(a, s.b, s.len + m);
+        if (page < 0) continue;
+        const long long row = ((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + m) & (a.page_size - 1));
+#pragma unroll 1
+        for (int i = d; i < d + count; ++i) {
+            float v;
+            if constexpr (FP8) v = (static_cast<const uint8_t*>(a.v_pool)[row * a.head_dim + i] & 0x7f) == 0x7f ? __uint_as_float(0x7fffffffu) : 0.f;
+            else v = to_f32(static_cast<const __nv_bfloat16*>(a.v_pool)[row * a.head_dim + i]);
+            if (fabsf(v) < INFINITY) continue;
+            if (s.part < 0) {
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + ((long long)(s.node0 + nd) * a.n_heads + hq) * a.head_dim + i;
+                *out = from_f32<__nv_bfloat16>(to_f32(*out) + v);
+            } else {
+                a.ws.part_o[((long long)s.part * ROWS + urow) * a.head_dim + i] += v;
+            }
+        }
+    }
+}
+
+// 8 elements of a unit's q row (bf16), from dimension d on.
+__device__ __forceinline__ uint4 load_q(const AttnArgs& a, const Segment& s, int row, int d) {
+    const int nd = row / a.group;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (s.node0 + nd) * a.q_token_stride +
+                               (s.head * a.group + row - nd * a.group) * a.q_head_stride + d;
+    if ((uintptr_t)src % 16 == 0) return __ldg(reinterpret_cast<const uint4*>(src));
+    const uint16_t* u = reinterpret_cast<const uint16_t*>(src);
+    return make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
+}
+
+// Place of codes 16 c .. 16 c + 15 of a row in a tile of V as TMA leaves it (rows of 128 or 64 bytes, swizzled).
+template <int D>
+__device__ __forceinline__ int raw_v_offset(int row, int c) {
+    return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+}
+
+// A tile of V codes with drafted rows: zeros past the end and in place of NaN (all bits of a code but the sign), whose
+// nodes are noted. Each thread cleans the 16 codes that it reads afterwards (row0 and c0 of the first).
+template <int D>
+__device__ __forceinline__ void clean_codes(unsigned char* v, int row0, int c0, const Segment& s, int pos0, unsigned long long* bad) {
+    const int total = s.len + s.n;
+#pragma unroll 1
+    for (int i = 0; i < D / 16; ++i) {
+        const int row = row0 + (i & 3) * 32, pos = pos0 + row;
+        if (pos < s.len) continue;
+        uint4* at = reinterpret_cast<uint4*>(v + raw_v_offset<D>(row, c0 + (i >> 2) * 4));
+        if (pos >= total) {
+            *at = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        const uint4 w = *at;
+        uint32_t x[4] = {w.x, w.y, w.z, w.w}, any = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t nan = ((x[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            any |= nan;
+            x[j] &= ~((nan >> 7) * 0xffu);
+        }
+        if (any) {
+            *at = make_uint4(x[0], x[1], x[2], x[3]);
+            atomicOr(&bad[(pos - s.len) >> 6], 1ull << ((pos - s.len) & 63));
+        }
+    }
+}
+
+// The same for bf16 rows (infinities and NaN).
+template <int D>
+__device__ __forceinline__ void clean_bf16(unsigned char* v, int tid, const Segment& s, int pos0, unsigned long long* bad) {
+    constexpr int kChunks = D / 8;
+    const int total = s.len + s.n;
+#pragma unroll 1
+    for (int u = tid; u < 128 * kChunks; u += kConvThreads) {
+        const int row = u / kChunks, c = u % kChunks, pos = pos0 + row;
+        if (pos < s.len) continue;
+        uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+        if (pos >= total) {
+            *at = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        const uint4 w = *at;
+        uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if ((x[i] & 0x7f80u) == 0x7f80u) found = true, x[i] &= 0xffff0000u;
+            if ((x[i] & 0x7f800000u) == 0x7f800000u) found = true, x[i] &= 0xffffu;
+        }
+        if (found) {
+            *at = make_uint4(x[0], x[1], x[2], x[3]);
+            atomicOr(&bad[(pos - s.len) >> 6], 1ull << ((pos - s.len) & 63));
+        }
+    }
+}
+
+// ---------------------------------------------------------------- roles
+
+// A role's walk over the CTA's segments. A segment stays in shared memory until done().
+struct Walk {
+    TcShared& m;
+    const AttnArgs& a;
+    Ring seg;
+    // False: no more, or given up.
+    __device__ __forceinline__ bool next() {
+        if (!mbar_wait_warp(&m.seg_full[seg.i], seg.phase, a.err, &m.abort_flag)) {
+            *static_cast<volatile int*>(&m.abort_flag) = 1;
+            return false;
+        }
+        return m.seg[seg.i].go != 0;
+    }
+    __device__ __forceinline__ const Segment& segment() const { return m.seg[seg.i].s; }
+    __device__ __forceinline__ void done() {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&m.seg_empty[seg.i]);
+        seg.next<kSegRing>();
+    }
+};
+
+// One warp: the CTA's segments, a few ahead of the roles that work on them.
+template <int ROWS>
+__device__ __forceinline__ void role_schedule(TcShared& m, const AttnArgs& a) {
+    volatile int* abort_flag = &m.abort_flag;
+    Ring seg;
+    Cursor cur{};
+    bool more = cursor_init<ROWS, kTcKeys>(a, blockIdx.x, gridDim.x, cur);
+    while (true) {
+        if (!mbar_wait_warp(&m.seg_empty[seg.i], seg.phase ^ 1u, a.err, abort_flag)) {
+            *abort_flag = 1;
+            break;
+        }
+        Segment s{};
+        more = more && cursor_next<ROWS, kTcKeys>(a, blockIdx.x, cur, s);
+        if ((threadIdx.x & 31) == 0) {
+            m.seg[seg.i].s = s;
+            m.seg[seg.i].go = more;
+            for (int w = 0; w < kMaxNodes / 64; ++w) m.seg[seg.i].bad[w] = 0;
+            mbar_arrive(&m.seg_full[seg.i]);
+        }
+        seg.next<kSegRing>();
+        if (!more) break;
+    }
+}
+
+// One warp: TMA loads of K and V tiles; lane x loads box x of a tile.
+template <bool FP8, int D, int NK, int NV>
+__device__ __forceinline__ void role_load(TcShared& m, const TcAttnArgs& p, unsigned char* k_smem, unsigned char* v_smem) {
+    constexpr int kTile = 128 * D * (FP8 ? 1 : 2);
+    const AttnArgs& a = p.a;
+    volatile int* abort_flag = &m.abort_flag;
+    const int lane = threadIdx.x & 31;
+    Ring rk, rv;
+    long long nk = 0, nv = 0;
+    bool ok = true;
+    const int boxes = kTcKeys / p.box_rows;
+    Walk walk{m, a, {}};
+    while (ok && walk.next()) {
+        const Segment& s = walk.segment();
+        const int total = s.len + s.n;
+        // a tile's pages are looked up while the tile before it is loaded
+        auto look_up = [&](int t) {
+            const int at = t * kTcKeys + lane * p.box_rows;
+            return t < s.tile1 && lane < boxes && at < total ? page_of(a, s.b, at) : -1;
+        };
+        int next_page = look_up(s.tile0);
+        for (int t = s.tile0; t < s.tile1; ++t) {
+            const int pos = t * kTcKeys + lane * p.box_rows;
+            const int page = next_page;
+            next_page = look_up(t + 1);
+            const int row = a.row0 + (page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
+            const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= 0)) * (uint32_t)(p.box_rows * (kTile / 128));
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                Ring& r = kv ? rv : rk;
+                uint64_t* full = kv ? m.v_full : m.k_full;
+                uint64_t* empty = kv ? m.v_empty : m.k_empty;
+                if (!mbar_wait_warp(&empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                if (lane == 0) mbar_expect_tx(&full[r.i], bytes);
+                __syncwarp();
+                if (page >= 0) {
+                    unsigned char* dst = (kv ? v_smem : k_smem) + r.i * kTile;
+                    const CUtensorMap* map = kv ? &p.v : &p.k;
+                    if constexpr (FP8) {
+                        tma_load_2d(dst + lane * p.box_rows * D, map, &full[r.i], 0, row);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < D / 64; ++h)
+                            tma_load_2d(dst + h * 16384 + lane * p.box_rows * 128, map, &full[r.i], h * 64, row);
+                    }
+                }
+                if (kv) ++nv, rv.next<NV>(); else ++nk, rk.next<NK>();
+            }
+            if (!ok) break;
+        }
+        walk.done();
+    }
+    if (!ok) *abort_flag = 1;
+    if (*abort_flag) {
+        // let the copies already issued land before the CTA exits
+        for (long long f = nk - 1; f >= 0 && f >= nk - NK; --f)
+            if (!mbar_wait(&m.k_full[f % NK], (uint32_t)((f / NK) & 1), a.err)) break;
+        for (long long f = nv - 1; f >= 0 && f >= nv - NV; --f)
+            if (!mbar_wait(&m.v_full[f % NV], (uint32_t)((f / NV) & 1), a.err)) break;
+    }
+}
+
+// One warp, fp8 caches: a tile's scales, 4 positions a lane. K's as factors 2^e; V's as 2^(e - eref + kVUp) with the tile's eref.
+template <typename V4>
+__device__ __forceinline__ void role_scales(TcShared& m, const AttnArgs& a, float4 (*kf_out)[32], V4 (*vf_out)[32]) {
+    volatile int* abort_flag = &m.abort_flag;
+    const int lane = threadIdx.x & 31;
+    Ring r;
+    bool ok = true;
+    Walk walk{m, a, {}};
+    while (ok && walk.next()) {
+        const Segment& s = walk.segment();
+        const int total = s.len + s.n;
+        int eref = -1000;
+        // pages two tiles and scales one tile ahead
+        auto look_up = [&](int t) {
+            const int at = t * kTcKeys + lane * 4;
+            return t < s.tile1 && at < total ? page_of(a, s.b, at) : -1;
+        };
+        auto load = [&](int page, int t, uint32_t& kb, uint32_t& vb) {
+            kb = vb = 0;
+            if (page >= 0) {
+                const long long at = ((long long)page * a.kv_heads + s.head) * a.page_size + ((t * kTcKeys + lane * 4) & (a.page_size - 1));
+                kb = __ldg(reinterpret_cast<const uint32_t*>(a.k_scale + at));
+                vb = __ldg(reinterpret_cast<const uint32_t*>(a.v_scale + at));
+            }
+        };
+        uint32_t kb_next, vb_next;
+        load(look_up(s.tile0), s.tile0, kb_next, vb_next);
+        int next_page = look_up(s.tile0 + 1);
+        for (int t = s.tile0; t < s.tile1; ++t) {
+            const int pos = t * kTcKeys + lane * 4;
+            uint32_t kb = kb_next, vb = vb_next;
+            load(next_page, t + 1, kb_next, vb_next);
+            next_page = look_up(t + 2);
+            if (pos + 4 > total) {
+                const int left = total - pos;       // positions of the four that exist
+                const uint32_t have = left <= 0 ? 0u : 0xffffffffu >> (8 * (4 - left));
+                kb &= have;
+                vb &= have;
+            }
+            int top = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = max(top, (int)(vb >> (8 * i) & 0xff));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            // two octaves of room, so that small differences between tiles do not move it
+            if (top - 127 > eref) eref = top - 127 + 2;
+            float kf[4], vf[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int vbyte = (int)(vb >> (8 * i) & 0xff);
+                kf[i] = pow2_of_byte((int)(kb >> (8 * i) & 0xff));
+                const int e = vbyte - eref + kVUp;      // biased exponent
+                vf[i] = vbyte == 0 || e <= 0 ? 0.f : pow2_of_byte(e);
+            }
+            if (!mbar_wait_warp(&m.aux_empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+            kf_out[r.i][lane] = make_float4(kf[0], kf[1], kf[2], kf[3]);
+            if constexpr (sizeof(V4) == 16) {
+                vf_out[r.i][lane] = make_float4(vf[0], vf[1], vf[2], vf[3]);
+            } else {
+                const __half2 lo = __floats2half2_rn(vf[0], vf[1]), hi = __floats2half2_rn(vf[2], vf[3]);
+                vf_out[r.i][lane] = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+            }
+            if (lane == 0) m.eref[r.i] = eref;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.aux_full[r.i]);
+            r.next<kAuxRing>();
+        }
+        if (ok) walk.done();
+    }
+    if (!ok) *abort_flag = 1;
+}
+
+}  // namespace
+}  // namespace ace

@@ -75,6 +75,10 @@ constexpr int kTcMaxRows = 256;         // rows of a unit
 bool attn_tc_supported(const ace_kv* kv);
 cudaError_t attn_tc_init(ace_kv* kv);
 cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
+// the same for few rows a unit (ace_attn_few.cu)
+constexpr int kFewRows = 32;
+cudaError_t attn_few_init(const ace_kv* kv);
+cudaError_t launch_attn_few(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
 // 2-D map of bytes [rows, cols], boxes of box_rows whole rows (ace_expert_tc.cu)
 cudaError_t make_byte_map(CUtensorMap* m, const void* base, uint64_t rows, uint32_t cols, uint32_t box_rows, int swizzle);
 
