@@ -10,8 +10,9 @@
 // fp8 caches: both products take the cached codes as they are (kind::f8f6f4). q is split into two e4m3 terms as in
 // ace_attn_tc.cu; a weight (at most 2^kLazy) times its V row's factor (at most 2^kVUp), rounded to fp16, into four e5m2
 // terms: the upper byte of an fp16 is one, and so on with what is left; each takes at least three of the eleven bits.
-// The rows' references lie in shared memory and move only where a score passes them by 2^kLazy (a flag of
-// each warp, met once a tile). Two groups of four warps take even and odd tiles into accumulators of their own.
+// The rows' references lie in shared memory and move only where a score passes them by 2^kLazy (one barrier with an
+// "or" a tile). Two groups of four warps take even and odd tiles into accumulators of their own; a group's next
+// scores are computed as soon as it has read the last ones.
 #include "ace_attn_tc.cuh"
 
 namespace ace {
@@ -39,11 +40,11 @@ struct FewCfg {
 
 template <bool FP8, int NR>
 struct FewShared : TcShared {
+    uint64_t s_free[2];
     float4 kf[FP8 ? kAuxRing : 1][32], vf[FP8 ? kAuxRing : 1][32];
     float f_row[2][NR];                 // q's scale times the softmax's, by turns of segments
     int node[2][NR];                    // row's node of the request
     float ref[2][2][NR];                // [group][turn]
-    int flag[2][2][4];                  // [group][turn][warp]
     float top[2][4][NR];                // [group][warp]: maxima of a tile's scores
     float sum[2][4][NR];                // end: sums of weights
     float ref_end[2][NR];
@@ -114,6 +115,18 @@ __device__ __forceinline__ float row_sums(float (&v)[NR], int lane) {
     return v[0];
 }
 
+// Named barriers of the softmax warps; meet_or: whether `x` holds in any thread.
+__device__ __forceinline__ void meet(int id, int threads) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ bool meet_or(int id, int threads, bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %3, 0;\n\tbarrier.cta.red.or.pred p, %1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(id), "r"(threads), "r"((uint32_t)x)
+        : "memory");
+    return r != 0;
+}
+
 template <bool FP8, int D, int NR>
 __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constant__ TcAttnArgs p) {
     using C = FewCfg<FP8, D, NR>;
@@ -130,13 +143,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
         for (int i = 0; i < NV; ++i) mbar_init(&m.v_full[i], 1), mbar_init(&m.v_empty[i], 1), mbar_init(&m.v_ready[i], 4);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&m.s_full[i], 1);
+            mbar_init(&m.s_free[i], 4);
             mbar_init(&m.p_ready[i], 4);
             mbar_init(&m.o_done[i], 1);
-            mbar_init(&m.group[i], 4);
         }
         mbar_init(&m.q_full, 4);
         mbar_init(&m.q_free, 1);
-        mbar_init(&m.soft, 8);
         mbar_init(&m.drain, 1);
         for (int i = 0; i < kSegRing; ++i) {
             mbar_init(&m.seg_full[i], 1);
@@ -169,7 +181,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
         // ------------------------------------------------ MMA issuer
         if (elect_one()) {
             Ring rk, rv;
-            uint32_t q_phase = 0, p_phase = 0;
+            uint32_t q_phase = 0, p_phase = 0, f_phase = 3;     // bit g: a group's barriers; its S^T is free at first
             const uint32_t q0 = desc_lo(smem_u32(smem + C::OFF_Q), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
             const uint32_t v0 = desc_lo(smem_u32(smem + C::OFF_V), kVBlock), p0 = desc_lo(smem_u32(smem + C::OFF_P), 128);
             constexpr uint32_t kHi = C::ROW == 64 ? kRows64 : kRows128;
@@ -183,9 +195,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 walk.seg.next<kSegRing>();
                 if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
                 q_phase ^= 1u;
-                for (int i = 0; i <= tiles; ++i) {
+                for (int i = 0; i < tiles + 2; ++i) {
                     if (i < tiles) {
-                        // S^T of group i & 1: its scores of two tiles ago are read, or the product below had not been issued
+                        // S^T of group i & 1, once the group has read its scores of two tiles ago
+                        if (!mbar_wait_or_abort(&m.s_free[i & 1], f_phase >> (i & 1) & 1u, a.err, abort_flag)) { ok = false; break; }
+                        f_phase ^= 1u << (i & 1);
                         if (!mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
                         const uint32_t d = tmem + C::S + (uint32_t)((i & 1) * NR), kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4));
@@ -206,8 +220,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         rk.next<NK>();
                         if (i == tiles - 1) mma_commit(&m.q_free);
                     }
-                    if (i > 0) {
-                        const int j = i - 1, g = j & 1;
+                    if (i > 1) {
+                        const int j = i - 2, g = j & 1;
                         if (!mbar_wait_or_abort(&m.p_ready[g], p_phase >> g & 1u, a.err, abort_flag)) { ok = false; break; }
                         p_phase ^= 1u << g;
                         if (!mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
@@ -330,22 +344,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t s_t = tmem + lanes + C::S + (uint32_t)(g * NR), o_t = tmem + lanes + C::O + (uint32_t)(g * NR);
         unsigned char* p_out = smem + C::OFF_P + g * C::P + key * 16;
-        uint32_t s_phase = 0, o_phase = 0, soft_phase = 0, group_phase = 0;
-        auto soft_sync = [&]() -> bool {        // the eight warps meet
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&m.soft);
-            soft_phase ^= 1u;
-            return mbar_wait_warp(&m.soft, soft_phase ^ 1u, a.err, abort_flag);
-        };
-        auto group_sync = [&]() -> bool {       // this group's four warps meet
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&m.group[g]);
-            group_phase ^= 1u;
-            return mbar_wait_warp(&m.group[g], group_phase ^ 1u, a.err, abort_flag);
+        uint32_t s_phase = 0, o_phase = 0;
+        // These warps also meet at hardware barriers, which wait without a limit: so a warp whose bounded wait has run out
+        // goes on without waiting (its error is noted, its results are not valid), and all leave together.
+        bool dead = false;
+        auto wait = [&](uint64_t* bar, uint32_t phase) {
+            if (!dead && !mbar_wait_warp(bar, phase, a.err, abort_flag)) dead = true, *abort_flag = 1;
         };
         Ring ra;
-        bool ok = true;
-        while (ok && walk.next()) {
+        while (true) {
+            const bool none = !walk.next();
+            if (meet_or(3, 256, none || dead)) break;
             const Segment& s = walk.segment();
             const int tiles = s.tile1 - s.tile0, total = s.len + s.n;
             const float* f_row = m.f_row[walk.seg.i & 1];
@@ -363,7 +372,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 float kf = 1.f, vf = 1.f;
                 int e_new = eref;
                 if (FP8) {
-                    if (!mbar_wait_warp(&m.aux_full[ra.i], ra.phase, a.err, abort_flag)) { ok = false; break; }
+                    wait(&m.aux_full[ra.i], ra.phase);
                     kf = reinterpret_cast<const float*>(m.kf[ra.i])[key];
                     vf = reinterpret_cast<const float*>(m.vf[ra.i])[key];
                     e_new = m.eref[ra.i];
@@ -371,12 +380,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     if (lane == 0) mbar_arrive(&m.aux_empty[ra.i]);
                     ra.next<kAuxRing>();
                 }
-                if (!mbar_wait_warp(&m.s_full[g], s_phase, a.err, abort_flag)) { ok = false; break; }
+                wait(&m.s_full[g], s_phase);
                 s_phase ^= 1u;
                 tc_fence_after();
                 float x[NR];
                 tmem_ld<NR>(s_t, x);
                 tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&m.s_free[g]);
                 // scores in units of the softmax (base 2)
 #pragma unroll
                 for (int r = 0; r < NR; r += 4) {
@@ -402,11 +414,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         const float4 f = *reinterpret_cast<const float4*>(ref + r);
                         over = fmaxf(over, fmaxf(fmaxf(x[r] - f.x, x[r + 1] - f.y), fmaxf(x[r + 2] - f.z, x[r + 3] - f.w)));
                     }
-                    const bool mine_over = __any_sync(0xffffffffu, over > (float)kLazy);
-                    if (lane == 0) m.flag[g][mine & 1][quad] = mine_over;
-                    if (!group_sync()) { ok = false; break; }
-                    const int4 fl = *reinterpret_cast<const int4*>(m.flag[g][mine & 1]);
-                    move = move || (fl.x | fl.y | fl.z | fl.w);
+                    move = meet_or(1 + g, 128, move || over > (float)kLazy);
                 }
                 if (move) {
                     // new references: the tile's maxima over the group's positions
@@ -422,10 +430,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                             if (lane == 0) m.top[g][quad][r0 + i] = v;
                         }
                     }
-                    if (!group_sync()) { ok = false; break; }
+                    meet(1 + g, 128);
                     if (mine) {
                         // the group's previous product has left O
-                        if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+                        wait(&m.o_done[g], o_phase);
                         o_phase ^= 1u;
                         waited = true;
                         tc_fence_after();
@@ -455,11 +463,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     }
                     turn ^= 1;
                     eref = e_new;
-                    if (!group_sync()) { ok = false; break; }
+                    meet(1 + g, 128);
                     ref = m.ref[g][turn];
                 }
                 if (!waited) {
-                    if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+                    wait(&m.o_done[g], o_phase);    // the product has read the P^T before
                     o_phase ^= 1u;
                 }
                 // weights: 16 rows' e5m2 terms, or 8 rows' bf16, are one 16-byte piece
@@ -512,9 +520,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 if (lane == 0) mbar_arrive(&m.p_ready[g]);
                 ++mine;
             }
-            if (!ok) break;
             if (mine) {
-                if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+                wait(&m.o_done[g], o_phase);
                 o_phase ^= 1u;
             }
             tc_fence_after();
@@ -526,7 +533,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 if (key < NR) m.ref_end[g][key] = mine ? m.ref[g][turn][key] : kNone;
                 if (key == 0) m.eref_end[g] = eref;
             }
-            if (!soft_sync()) { ok = false; break; }
+            meet(3, 256);
             const bool whole = s.part < 0;
             const unsigned long long* bad = m.seg[walk.seg.i].bad;
             const bool any_bad = bad[0] | bad[1] | bad[2] | bad[3];
@@ -582,10 +589,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             }
             tc_fence_before();
             if (!whole) __threadfence();
-            if (!soft_sync()) { ok = false; break; }        // O may be overwritten, partial results are written
+            meet(3, 256);               // O may be overwritten, partial results are written
             if (!whole) {
                 if (tid == 0) m.joins = last_of_unit(a, s);
-                if (!soft_sync()) { ok = false; break; }
+                meet(3, 256);
                 if (m.joins) {
                     __threadfence();
                     join_unit<__nv_bfloat16, NR>(a, s, tid, 256);
@@ -593,7 +600,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             }
             walk.done();
         }
-        if (!ok) *abort_flag = 1;
     }
     tc_fence_before();
     __syncthreads();
