@@ -35,7 +35,11 @@ struct FewCfg {
     static constexpr int OFF_Q = OFF_V + NV * TILE;             // 1024-byte multiples up to here
     static constexpr int OFF_P = OFF_Q + Q;
     static constexpr int OFF_MISC = OFF_P + 2 * P;
-    static constexpr uint32_t S = 0, O = 2 * NR, COLS = 4 * NR; // TMEM: S^T of both groups, then O^T
+    // fp8: q's terms and the weights' terms lie side by side along N, so that a product reads K and V once; their results
+    // are added when they are read
+    static constexpr int SN = FP8 ? 2 * NR : NR, ON = TERMS * NR;
+    static constexpr uint32_t S = 0, O = 2 * SN, COLS = FP8 ? 16 * NR : 4 * NR;     // TMEM: S^T of both groups, then O^T
+    static_assert(2 * (SN + ON) <= (int)COLS && (COLS & (COLS - 1)) == 0, "a power of two");
 };
 
 template <bool FP8, int NR>
@@ -88,6 +92,21 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&x)[N]) {
         tmem_ld16(taddr, *reinterpret_cast<uint32_t(*)[16]>(r));
     } else {
         asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : ACE_R8(r, 0) : "r"(taddr));
+    }
+}
+
+// N columns of an accumulator whose TERMS parts lie STEP columns apart.
+template <int TERMS, int STEP, int N>
+__device__ __forceinline__ void sum_terms(uint32_t taddr, float (&x)[N]) {
+    tmem_ld<N>(taddr, x);
+    tmem_ld_wait();
+#pragma unroll 1
+    for (int t = 1; t < TERMS; ++t) {
+        float y[N];
+        tmem_ld<N>(taddr + t * STEP, y);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] += y[i];
     }
 }
 
@@ -202,13 +221,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         f_phase ^= 1u << (i & 1);
                         if (!mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t d = tmem + C::S + (uint32_t)((i & 1) * NR), kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4));
+                        const uint32_t d = tmem + C::S + (uint32_t)((i & 1) * C::SN), kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4));
                         if constexpr (FP8) {
 #pragma unroll
-                            for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
-                                const uint32_t st = kk % (D / 32) * 2;
-                                mma_few<true>(d, kl + st, kHi, q0 + (kk < D / 32 ? 0 : C::Q >> 5) + st, kHi, few_idesc(0, 0, 128, NR, false, false), kk > 0);
-                            }
+                            for (int kk = 0; kk < D / 32; ++kk)
+                                mma_few<true>(d, kl + 2 * kk, kHi, q0 + 2 * kk, kHi, few_idesc(0, 0, 128, C::SN, false, false), kk > 0);
                         } else {
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk)
@@ -226,15 +243,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         p_phase ^= 1u << g;
                         if (!mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t d = tmem + C::O + (uint32_t)(g * NR), vl = v0 + (uint32_t)(rv.i * (C::TILE >> 4));
+                        const uint32_t d = tmem + C::O + (uint32_t)(g * C::ON), vl = v0 + (uint32_t)(rv.i * (C::TILE >> 4));
                         const uint32_t pl = p0 + (uint32_t)(g * (C::P >> 4));
                         if constexpr (FP8) {
 #pragma unroll
-                            for (int kk = 0; kk < 16; ++kk) {           // 32 positions a step; four terms
-                                const uint32_t at = kk & 3;
-                                mma_few<true>(d, vl + at * (32 * C::ROW >> 4), kHi, pl + (kk >> 2) * (C::TERM >> 4) + at * 32, kPHi,
-                                              few_idesc(0, 1, D, NR, true, true), j >= 2 || kk > 0);
-                            }
+                            for (int kk = 0; kk < 4; ++kk)              // 32 positions a step
+                                mma_few<true>(d, vl + kk * (32 * C::ROW >> 4), kHi, pl + kk * 32, kPHi, few_idesc(0, 1, D, C::ON, true, true), j >= 2 || kk > 0);
                         } else {
 #pragma unroll
                             for (int kk = 0; kk < 8; ++kk)              // 16 positions a step
@@ -342,7 +356,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
         // ------------------------------------------------ softmax: group g of 4 warps, a thread per position of a tile
         const int g = (warp - 4) >> 2, quad = warp & 3, key = quad * 32 + lane, tid = threadIdx.x - 128;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const uint32_t s_t = tmem + lanes + C::S + (uint32_t)(g * NR), o_t = tmem + lanes + C::O + (uint32_t)(g * NR);
+        const uint32_t s_t = tmem + lanes + C::S + (uint32_t)(g * C::SN), o_t = tmem + lanes + C::O + (uint32_t)(g * C::ON);
         unsigned char* p_out = smem + C::OFF_P + g * C::P + key * 16;
         uint32_t s_phase = 0, o_phase = 0;
         // These warps also meet at hardware barriers, which wait without a limit: so a warp whose bounded wait has run out
@@ -385,7 +399,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 tc_fence_after();
                 float x[NR];
                 tmem_ld<NR>(s_t, x);
+                float lower[FP8 ? NR : 1];
+                if constexpr (FP8) tmem_ld<NR>(s_t + NR, lower);
                 tmem_ld_wait();
+                if constexpr (FP8) {
+#pragma unroll
+                    for (int r = 0; r < NR; r += 2) unpair(add2(pair(x[r], x[r + 1]), pair(lower[r], lower[r + 1])), x[r], x[r + 1]);
+                }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&m.s_free[g]);
@@ -438,27 +458,31 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         waited = true;
                         tc_fence_after();
                     }
-                    float o[NR];
-                    if (mine) {
-                        tmem_ld<NR>(o_t, o);
-                        tmem_ld_wait();
-                    }
                     const float units = FP8 && mine ? (e_new - eref > 126 ? 0.f : pow2_of_byte(127 - (e_new - eref))) : 1.f;
+                    float f[NR];
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
                         const float top = fmaxf(fmaxf(m.top[g][0][r], m.top[g][1][r]), fmaxf(m.top[g][2][r], m.top[g][3][r]));
                         const float old = mine ? ref[r] : kNone;
                         const float now = top > old + (float)kLazy ? top : old;
-                        const float f = exp2_approx(old - now);
-                        if (mine) {
-                            l[r] *= f;
-                            o[r] *= f * units;
-                        }
+                        f[r] = exp2_approx(old - now);
+                        l[r] *= f[r];
+                        f[r] *= units;
                         if (key == r) m.ref[g][turn ^ 1][r] = now;
                     }
                     if (mine) {
-                        if constexpr (NR == 32) tmem_st32(o_t, *reinterpret_cast<const uint32_t(*)[32]>(&o));
-                        else tmem_st16(o_t, *reinterpret_cast<const uint32_t(*)[16]>(&o));
+#pragma unroll 1
+                        for (int c = 0; c < C::ON; c += NR) {
+#pragma unroll
+                            for (int r = 0; r < NR; r += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(o_t + c + r, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f[r + i]);
+                                tmem_st16(o_t + c + r, o);
+                            }
+                        }
                         tmem_st_wait();
                     }
                     turn ^= 1;
@@ -568,9 +592,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 const int d = D == 128 ? key : quad * 16 + lane;
                 const bool in = D == 128 || lane < 16;
                 float o0[HALF], o1[HALF];
-                tmem_ld<HALF>(tmem + lanes + C::O + (uint32_t)r0, o0);
-                if (tiles > 1) tmem_ld<HALF>(tmem + lanes + C::O + (uint32_t)(NR + r0), o1);
-                tmem_ld_wait();
+                sum_terms<C::TERMS, NR, HALF>(tmem + lanes + C::O + (uint32_t)r0, o0);
+                if (tiles > 1) sum_terms<C::TERMS, NR, HALF>(tmem + lanes + C::O + (uint32_t)(C::ON + r0), o1);
 #pragma unroll
                 for (int i = 0; i < HALF; ++i) {
                     const int r = r0 + i;

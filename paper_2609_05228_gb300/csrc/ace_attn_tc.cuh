@@ -380,27 +380,41 @@ __device__ __forceinline__ void role_scales(TcShared& m, const AttnArgs& a, floa
         const Segment& s = walk.segment();
         const int total = s.len + s.n;
         int eref = -1000;
-        // pages two tiles and scales one tile ahead
-        auto look_up = [&](int t) {
-            const int at = t * kTcKeys + lane * 4;
-            return t < s.tile1 && at < total ? page_of(a, s.b, at) : -1;
-        };
-        auto load = [&](int page, int t, uint32_t& kb, uint32_t& vb) {
-            kb = vb = 0;
-            if (page >= 0) {
-                const long long at = ((long long)page * a.kv_heads + s.head) * a.page_size + ((t * kTcKeys + lane * 4) & (a.page_size - 1));
-                kb = __ldg(reinterpret_cast<const uint32_t*>(a.k_scale + at));
-                vb = __ldg(reinterpret_cast<const uint32_t*>(a.v_scale + at));
+        // in batches of 4 tiles, pages two and scales one batch ahead: a load takes longer than a tile
+        auto look_up = [&](int t, int (&page)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = (t + i) * kTcKeys + lane * 4;
+                page[i] = t + i < s.tile1 && at < total ? page_of(a, s.b, at) : -1;
             }
         };
-        uint32_t kb_next, vb_next;
-        load(look_up(s.tile0), s.tile0, kb_next, vb_next);
-        int next_page = look_up(s.tile0 + 1);
+        auto load = [&](const int (&page)[4], int t, uint32_t (&kb)[4], uint32_t (&vb)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                kb[i] = vb[i] = 0;
+                if (page[i] >= 0) {
+                    const long long at = ((long long)page[i] * a.kv_heads + s.head) * a.page_size + (((t + i) * kTcKeys + lane * 4) & (a.page_size - 1));
+                    kb[i] = __ldg(reinterpret_cast<const uint32_t*>(a.k_scale + at));
+                    vb[i] = __ldg(reinterpret_cast<const uint32_t*>(a.v_scale + at));
+                }
+            }
+        };
+        int page[4];
+        uint32_t kb_next[4], vb_next[4], kb4[4], vb4[4];
+        look_up(s.tile0, page);
+        load(page, s.tile0, kb_next, vb_next);
+        look_up(s.tile0 + 4, page);
         for (int t = s.tile0; t < s.tile1; ++t) {
-            const int pos = t * kTcKeys + lane * 4;
-            uint32_t kb = kb_next, vb = vb_next;
-            load(next_page, t + 1, kb_next, vb_next);
-            next_page = look_up(t + 2);
+            const int j = (t - s.tile0) & 3, pos = t * kTcKeys + lane * 4;
+            if (j == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) kb4[i] = kb_next[i], vb4[i] = vb_next[i];
+                load(page, t + 4, kb_next, vb_next);
+                look_up(t + 8, page);
+            }
+            uint32_t kb = kb4[0], vb = vb4[0];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) kb4[i] = kb4[i + 1], vb4[i] = vb4[i + 1];
             if (pos + 4 > total) {
                 const int left = total - pos;       // positions of the four that exist
                 const uint32_t have = left <= 0 ? 0u : 0xffffffffu >> (8 * (4 - left));
