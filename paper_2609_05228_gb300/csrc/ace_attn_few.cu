@@ -26,9 +26,8 @@ struct FewCfg {
     static constexpr int TILE = 128 * ROW;
     static constexpr int Q = NR * D * 2;                        // bf16, or two e4m3 terms
     static constexpr int TERMS = FP8 ? 4 : 1;
-    static constexpr int BLOCKS = NR * (FP8 ? 1 : 2) / 16;      // 16-byte pieces of a position's row of P^T
-    static constexpr int TERM = BLOCKS * 128 * 16;
-    static constexpr int P = TERMS * TERM;                      // one group's P^T
+    static constexpr int PIECES = TERMS * NR * (FP8 ? 1 : 2) / 16;      // 16-byte pieces of a position's row of P^T
+    static constexpr int P = PIECES * 128 * 16;                 // one group's P^T
     static constexpr int NK = D == 64 ? 6 : FP8 ? 5 : 3, NV = NK;
     static constexpr int OFF_K = 0;
     static constexpr int OFF_V = OFF_K + NK * TILE;
@@ -82,7 +81,7 @@ constexpr uint32_t few_idesc(int type_a, int type_b, int M, int N, bool a_mn, bo
            ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-// N columns of TMEM (8, 16 or 32), not waited for.
+// N columns of TMEM (4, 8, 16 or 32), not waited for.
 template <int N>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&x)[N]) {
     uint32_t* r = reinterpret_cast<uint32_t*>(x);
@@ -90,8 +89,10 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&x)[N]) {
         tmem_ld32(taddr, *reinterpret_cast<uint32_t(*)[32]>(r));
     } else if constexpr (N == 16) {
         tmem_ld16(taddr, *reinterpret_cast<uint32_t(*)[16]>(r));
-    } else {
+    } else if constexpr (N == 8) {
         asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : ACE_R8(r, 0) : "r"(taddr));
+    } else {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
     }
 }
 
@@ -118,7 +119,7 @@ __device__ __forceinline__ float warp_max(float x) {
     return __int_as_float(i ^ ((i >> 31) & 0x7fffffff));
 }
 
-// Sums of v[r] over a warp by halving: lane returns the sum of row lane >> 1 (NR = 16, every pair of lanes) or lane (NR = 32).
+// Sums of v[r] over a warp by halving: each run of 32 / NR lanes returns the sum of its row.
 template <int NR>
 __device__ __forceinline__ float row_sums(float (&v)[NR], int lane) {
     int o = 16;
@@ -130,7 +131,8 @@ __device__ __forceinline__ float row_sums(float (&v)[NR], int lane) {
             v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
         }
     }
-    if (NR == 16) v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
+#pragma unroll
+    for (; o >= 1; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
     return v[0];
 }
 
@@ -279,7 +281,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             const Segment& s = walk.segment();
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             const float f_row0 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
-            constexpr int kChunks = D / 8, kStep = 128 / kChunks, kTurns = NR / kStep;
+            constexpr int kChunks = D / 8, kStep = 128 / kChunks, kTurns = NR > kStep ? NR / kStep : 1;
             uint4 qv[kTurns];
 #pragma unroll
             for (int j = 0; j < kTurns; ++j) {
@@ -305,6 +307,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     for (int i = 0; i < 8; ++i) f[i] = finite_or_nan(f[i] * q_mul), amax = fmaxf(amax, fabsf(f[i]));
 #pragma unroll
                     for (int o = kChunks / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                    if (kStep > NR && r >= NR) continue;
                     const int byte = e4m3_scale_byte(amax);
                     const float mul = pow2_of_minus_byte(byte);
                     uint32_t hi[4], lo[4];
@@ -472,14 +475,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     }
                     if (mine) {
 #pragma unroll 1
-                        for (int c = 0; c < C::ON; c += NR) {
+                        for (int c = 0; c < C::ON; c += NR < 16 ? 16 : NR) {
 #pragma unroll
                             for (int r = 0; r < NR; r += 16) {
                                 uint32_t o[16];
                                 tmem_ld16(o_t + c + r, o);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f[r + i]);
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f[(r + i) % NR]);
                                 tmem_st16(o_t + c + r, o);
                             }
                         }
@@ -494,13 +497,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     wait(&m.o_done[g], o_phase);    // the product has read the P^T before
                     o_phase ^= 1u;
                 }
-                // weights: 16 rows' e5m2 terms, or 8 rows' bf16, are one 16-byte piece
+                // weights, 16 (or 8) rows at a time; a 16-byte piece holds 16 e5m2 or 8 bf16 values along N = term * NR + row
+                constexpr int RB = NR < 16 ? NR : 16;
 #pragma unroll
-                for (int b = 0; b < NR / 16; ++b) {
-                    uint32_t h[8];
+                for (int b = 0; b < NR / RB; ++b) {
+                    uint32_t h[RB / 2];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const int r = 16 * b + i;
+                    for (int i = 0; i < RB; i += 4) {
+                        const int r = RB * b + i;
                         const float4 f = *reinterpret_cast<const float4*>(ref + r);
                         float e[4] = {x[r] - f.x, x[r + 1] - f.y, x[r + 2] - f.z, x[r + 3] - f.w};
 #pragma unroll
@@ -516,26 +520,32 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         }
                     }
                     if constexpr (FP8) {
+                        uint32_t w[4][RB / 4];
 #pragma unroll
                         for (int term = 0; term < 4; ++term) {
-                            uint4 w;
-                            w.x = __byte_perm(h[0], h[1], 0x7531);
-                            w.y = __byte_perm(h[2], h[3], 0x7531);
-                            w.z = __byte_perm(h[4], h[5], 0x7531);
-                            w.w = __byte_perm(h[6], h[7], 0x7531);
-                            *reinterpret_cast<uint4*>(p_out + term * C::TERM + b * 2048) = w;
+#pragma unroll
+                            for (int i = 0; i < RB / 4; ++i) w[term][i] = __byte_perm(h[2 * i], h[2 * i + 1], 0x7531);
                             if (term < 3) {
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) {
+                                for (int i = 0; i < RB / 2; ++i) {
                                     const uint32_t top = h[i] & 0xff00ff00u;
                                     const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&top));
                                     h[i] = *reinterpret_cast<const uint32_t*>(&rest);
                                 }
                             }
                         }
+                        if constexpr (NR == 8) {
+                            *reinterpret_cast<uint4*>(p_out) = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
+                            *reinterpret_cast<uint4*>(p_out + 2048) = make_uint4(w[2][0], w[2][1], w[3][0], w[3][1]);
+                        } else {
+#pragma unroll
+                            for (int term = 0; term < 4; ++term)
+                                *reinterpret_cast<uint4*>(p_out + (term * (NR / 16) + b) * 2048) =
+                                    make_uint4(w[term][0], w[term][1], w[term][RB / 4 - 2], w[term][RB / 4 - 1]);
+                        }
                     } else {
                         *reinterpret_cast<uint4*>(p_out + (2 * b) * 2048) = make_uint4(h[0], h[1], h[2], h[3]);
-                        *reinterpret_cast<uint4*>(p_out + (2 * b + 1) * 2048) = make_uint4(h[4], h[5], h[6], h[7]);
+                        *reinterpret_cast<uint4*>(p_out + (2 * b + 1) * 2048) = make_uint4(h[RB / 2 - 4], h[RB / 2 - 3], h[RB / 2 - 2], h[RB / 2 - 1]);
                     }
                 }
                 fence_async_smem();
@@ -552,8 +562,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             // ---------------- the unit's result, or this CTA's part of it: group g finishes half of the rows
             {
                 const float sum = row_sums<NR>(l, lane);
-                if (NR == 32) m.sum[g][quad][lane] = sum;
-                else if (!(lane & 1)) m.sum[g][quad][lane >> 1] = sum;
+                if (lane % (32 / NR) == 0) m.sum[g][quad][lane / (32 / NR)] = sum;
                 if (key < NR) m.ref_end[g][key] = mine ? m.ref[g][turn][key] : kNone;
                 if (key == 0) m.eref_end[g] = eref;
             }
@@ -632,13 +641,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
 
 template <bool FP8, int D>
 cudaError_t few_attrs() {
-    const cudaError_t e = raise_smem_limit(k_attn_few<FP8, D, 16>, few_smem<FP8, D, 16>());
+    cudaError_t e = cudaSuccess;
+    if constexpr (FP8) e = raise_smem_limit(k_attn_few<FP8, D, 8>, few_smem<FP8, D, 8>());
+    if (e == cudaSuccess) e = raise_smem_limit(k_attn_few<FP8, D, 16>, few_smem<FP8, D, 16>());
     return e == cudaSuccess ? raise_smem_limit(k_attn_few<FP8, D, 32>, few_smem<FP8, D, 32>()) : e;
 }
 
 template <bool FP8, int D>
 cudaError_t few_go(const TcAttnArgs& p, int ctas, cudaStream_t s) {
-    if ((long long)p.a.max_nodes * p.a.group <= 16)
+    // NR by the rows of the largest tree; 8 are too few for plain caches (M = 128 wants N a multiple of 16, which two terms of
+    // an fp8 q make of them), whose larger tiles leave the softmax time enough
+    const long long rows = (long long)p.a.max_nodes * p.a.group;
+    if constexpr (FP8) {
+        if (rows <= 8) {
+            k_attn_few<FP8, D, 8><<<ctas, kTcThreads, few_smem<FP8, D, 8>(), s>>>(p);
+            return cudaGetLastError();
+        }
+    }
+    if (rows <= 16)
         k_attn_few<FP8, D, 16><<<ctas, kTcThreads, few_smem<FP8, D, 16>(), s>>>(p);
     else
         k_attn_few<FP8, D, 32><<<ctas, kTcThreads, few_smem<FP8, D, 32>(), s>>>(p);
