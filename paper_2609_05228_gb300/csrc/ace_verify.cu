@@ -18,7 +18,8 @@ namespace {
 
 using namespace ace;
 
-constexpr int kVerThreads = 512, kVerWarps = kVerThreads / 32, kMaxCluster = 8, kVerUnroll = 8;
+constexpr int kVerThreads = 512, kVerWarps = kVerThreads / 32, kMaxCluster = 8;
+constexpr int kPassUnroll = 2, kPass = 4 * kVerThreads * kPassUnroll;      // elements of a turn of a pass
 
 struct VerifyArgs {
     const void* logits;
@@ -137,13 +138,109 @@ __device__ __forceinline__ float residual(const Shared& sh, const Row& w, int k,
     return r;
 }
 
-template <typename T, bool DRAFT>
-__global__ void __launch_bounds__(kVerThreads) k_verify(const __grid_constant__ VerifyArgs p) {
+// A turn of a pass over elements lo <= i < hi of up to three rows: calls f(i, z, q, noise) for each of the thread's. With VEC a
+// thread's elements come four at a time in one load a row (all rows 16-byte aligned), else one by one. All
+// loads of a turn are under way together.
+template <typename T, bool VEC, bool Q, bool NOISE, typename F>
+__device__ __forceinline__ void pass(const T* z, const float* q, const float* noise, int lo, int hi, F f) {
+    for (int base = lo; base < hi; base += kPass) {
+        float zf[kPassUnroll][4], qf[kPassUnroll][4], nf[kPassUnroll][4];
+#pragma unroll
+        for (int u = 0; u < kPassUnroll; ++u) {
+            const int i = base + 4 * (threadIdx.x + kVerThreads * u);
+            if (VEC && i + 4 <= hi) {
+                if constexpr (sizeof(T) == 2) {
+                    const uint2 w = __ldg(reinterpret_cast<const uint2*>(z + i));
+                    zf[u][0] = __uint_as_float(w.x << 16), zf[u][1] = __uint_as_float(w.x & 0xffff0000u);
+                    zf[u][2] = __uint_as_float(w.y << 16), zf[u][3] = __uint_as_float(w.y & 0xffff0000u);
+                } else {
+                    *reinterpret_cast<float4*>(zf[u]) = __ldg(reinterpret_cast<const float4*>(z + i));
+                }
+                if (Q) *reinterpret_cast<float4*>(qf[u]) = __ldg(reinterpret_cast<const float4*>(q + i));
+                if (NOISE) *reinterpret_cast<float4*>(nf[u]) = __ldg(reinterpret_cast<const float4*>(noise + i));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int e = VEC ? i + j : base + (int)threadIdx.x + kVerThreads * (4 * u + j);
+                    const bool in = e < hi;
+                    zf[u][j] = in ? to_f32(z[e]) : -INFINITY;
+                    qf[u][j] = Q && in ? __ldg(q + e) : 0.f;
+                    nf[u][j] = NOISE && in ? __ldg(noise + e) : 1.f;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kPassUnroll; ++u) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int e = VEC ? base + 4 * ((int)threadIdx.x + kVerThreads * u) + j : base + (int)threadIdx.x + kVerThreads * (4 * u + j);
+                if (e < hi) f(e, zf[u][j], Q ? qf[u][j] : 0.f, NOISE ? nf[u][j] : 1.f);
+            }
+        }
+    }
+}
+
+// Softmax statistics of z[lo .. hi): 16-byte loads between the unaligned ends, 4 a thread under way together.
+template <typename T>
+__device__ Sums row_stats(const T* z, int lo, int hi, int none, float inv_t) {
+    constexpr int N = Vec16<T>::N, U = 4;
+    Sums v{-INFINITY, 0.f, none, 0};
+    auto one = [&](int i) {
+        const float f = to_f32(z[i]);
+        if (!(f < INFINITY)) v.bad = 1;
+        if (f > v.m) {
+            v.s = v.s * __expf((v.m - f) * inv_t) + 1.f;
+            v.m = f;
+            v.at = i;
+        } else if (f > -INFINITY) {
+            v.s += __expf((f - v.m) * inv_t);
+        }
+    };
+    const int skip = (int)((16 - (uintptr_t)(z + lo) % 16) % 16 / sizeof(T));
+    const int a0 = min(hi, lo + skip), groups = (hi - a0) / N, a1 = a0 + groups * N;
+    // the few elements before and after the aligned ones, in increasing order within a thread
+    if (lo + (int)threadIdx.x < a0) one(lo + threadIdx.x);
+    for (int g0 = threadIdx.x; g0 < groups; g0 += kVerThreads * U) {
+        float f[U][N];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int g = g0 + u * kVerThreads;
+            if (g < groups) {
+                Vec16<T>::to_float(__ldg(reinterpret_cast<const uint4*>(z + a0 + g * N)), f[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) f[u][i] = -INFINITY;
+            }
+        }
+        float top = v.m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (!(f[u][i] < INFINITY)) v.bad = 1;
+                if (f[u][i] > top) top = f[u][i], v.at = a0 + (g0 + u * kVerThreads) * N + i;
+            }
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+        v.s *= __expf((v.m - ref) * inv_t);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v.s += __expf((f[u][i] - ref) * inv_t);
+        }
+        v.m = top;
+    }
+    if (a1 + (int)threadIdx.x < hi) one(a1 + threadIdx.x);
+    return v;
+}
+
+template <typename T, bool DRAFT, bool VEC>
+__global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant__ VerifyArgs p) {
     __shared__ Shared sh;
     uint32_t n_ctas;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ctas));
     const int ctas = (int)n_ctas, rank = (int)cluster_rank(), b = blockIdx.x / ctas, tid = threadIdx.x;
-    const int V = p.vocab, chunk = (V + ctas - 1) / ctas;
+    const int V = p.vocab, chunk = ((V + ctas - 1) / ctas + 7) / 8 * 8;
     const int lo = min(V, rank * chunk), hi = min(V, lo + chunk);
     int o0 = p.node_offsets[b], n = p.node_offsets[b + 1] - o0;
     if (o0 < 0 || n < 0 || n > p.max_nodes || o0 > p.T - n) n = 0;
@@ -165,23 +262,7 @@ __global__ void __launch_bounds__(kVerThreads) k_verify(const __grid_constant__ 
         ++keep;
         const T* z = static_cast<const T*>(p.logits) + (o0 + node) * p.logits_stride;
         const float* qrow = DRAFT ? p.draft + (o0 + node) * p.draft_stride : nullptr;
-        Sums v{-INFINITY, 0.f, V, 0};
-        for (int i0 = lo + tid; i0 < hi; i0 += kVerThreads * kVerUnroll) {
-            float f[kVerUnroll];
-            float top = v.m;
-#pragma unroll
-            for (int u = 0; u < kVerUnroll; ++u) {
-                const int i = i0 + u * kVerThreads;
-                f[u] = i < hi ? to_f32(z[i]) : -INFINITY;
-                if (!(f[u] < INFINITY)) v.bad = 1;
-                if (f[u] > top) top = f[u], v.at = i;
-            }
-            const float ref = top == -INFINITY ? 0.f : top;
-            v.s *= __expf((v.m - ref) * w.inv_t);
-#pragma unroll
-            for (int u = 0; u < kVerUnroll; ++u) v.s += __expf((f[u] - ref) * w.inv_t);
-            v.m = top;
-        }
+        Sums v = row_stats(z, lo, hi, V, w.inv_t);
         v = join_all<join_stats>(sh, v, w.inv_t, turn, ctas);
         if (v.bad || v.m == -INFINITY) break;               // token stays -1
         w.m = v.m;
@@ -199,17 +280,10 @@ __global__ void __launch_bounds__(kVerThreads) k_verify(const __grid_constant__ 
             if (pending) {
                 // the residual after the last rejection: its sum over the vocabulary
                 Sums t{0.f, 0.f, 0, 0};
-                for (int i0 = lo + tid; i0 < hi; i0 += kVerThreads * kVerUnroll) {
-#pragma unroll
-                    for (int u = 0; u < kVerUnroll; ++u) {
-                        const int i = i0 + u * kVerThreads;
-                        if (i < hi) {
-                            float q = DRAFT ? qrow[i] : 0.f;
-                            const float r = residual<DRAFT>(sh, w, w.k - 1, i, to_f32(z[i]), q);
-                            t.s += DRAFT ? fmaxf(r - q, 0.f) : (i == sh.x[w.k - 1] ? 0.f : r);
-                        }
-                    }
-                }
+                pass<T, VEC, DRAFT, false>(z, qrow, nullptr, lo, hi, [&](int i, float zi, float q, float) {
+                    const float r = residual<DRAFT>(sh, w, w.k - 1, i, zi, q);
+                    t.s += DRAFT ? fmaxf(r - q, 0.f) : (i == sh.x[w.k - 1] ? 0.f : r);
+                });
                 t = join_all<join_plain>(sh, t, 0.f, turn, ctas);
                 if (tid == 0) sh.rz[w.k - 1] = t.s > 0.f ? 1.f / t.s : 0.f;
                 __syncthreads();
@@ -246,18 +320,11 @@ __global__ void __launch_bounds__(kVerThreads) k_verify(const __grid_constant__ 
         // where that leaves nothing the residual before it counts.
         for (int k = w.k; ; --k) {
             Sums t{-1.f, 0.f, V, 0};
-            for (int i0 = lo + tid; i0 < hi; i0 += kVerThreads * kVerUnroll) {
-#pragma unroll
-                for (int u = 0; u < kVerUnroll; ++u) {
-                    const int i = i0 + u * kVerThreads;
-                    if (i < hi) {
-                        float q = DRAFT ? qrow[i] : 0.f;
-                        const float r = residual<DRAFT>(sh, w, k, i, to_f32(z[i]), q);
-                        const float g = r > 0.f ? r / noise[i] : -1.f;
-                        if (g > t.m) t.m = g, t.at = i;
-                    }
-                }
-            }
+            pass<T, VEC, DRAFT, true>(z, qrow, noise, lo, hi, [&](int i, float zi, float q, float e) {
+                const float r = residual<DRAFT>(sh, w, k, i, zi, q);
+                const float g = r > 0.f ? r / e : -1.f;
+                if (g > t.m || (g == t.m && i < t.at)) t.m = g, t.at = i;
+            });
             t = join_all<join_plain>(sh, t, 0.f, turn, ctas);
             if (t.m >= 0.f) token = t.at;
             if (t.m >= 0.f || !pending || k < w.k) break;
@@ -280,7 +347,7 @@ ace_status ver_fail(ace_status st, const std::string& m) {
     return st;
 }
 
-template <typename T, bool DRAFT>
+template <typename T, bool DRAFT, bool VEC>
 cudaError_t launch_verify(const VerifyArgs& p, int B, int ctas, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)B * ctas);
@@ -292,7 +359,13 @@ cudaError_t launch_verify(const VerifyArgs& p, int B, int ctas, cudaStream_t s) 
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_verify<T, DRAFT>, p);
+    return cudaLaunchKernelEx(&cfg, k_verify<T, DRAFT, VEC>, p);
+}
+
+template <typename T>
+cudaError_t verify_of(const VerifyArgs& p, int B, int ctas, bool vec, cudaStream_t s) {
+    if (p.draft) return vec ? launch_verify<T, true, true>(p, B, ctas, s) : launch_verify<T, true, false>(p, B, ctas, s);
+    return vec ? launch_verify<T, false, true>(p, B, ctas, s) : launch_verify<T, false, false>(p, B, ctas, s);
 }
 
 }  // namespace
@@ -316,17 +389,17 @@ extern "C" ace_status ace_verify_tree(const void* logits, int dtype, long long l
     int dev = 0, sms = 1;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    // as many CTAs a request as the SMs hold for the batch, and no more than a row fills
+    // as many CTAs a request as the SMs hold for the batch (two each), and no more than a row fills
     int ctas = 1;
-    while (ctas < kMaxCluster && 2LL * ctas * B <= sms && vocab / (2 * ctas) >= kVerThreads) ctas *= 2;
+    while (ctas < kMaxCluster && 2LL * ctas * B <= 2 * sms && vocab / (2 * ctas) >= 2 * kVerThreads) ctas *= 2;
     if (e == cudaSuccess) {
         const VerifyArgs p{logits, logits_stride, draft_stride, noise_stride, tokens, parents, node_offsets, draft_probs,
                            temperature, uniforms, noise, path, n_keep, next_token, vocab, T, max_nodes};
         cudaStream_t s = static_cast<cudaStream_t>(stream);
-        if (dtype == ACE_BF16)
-            e = draft_probs ? launch_verify<__nv_bfloat16, true>(p, B, ctas, s) : launch_verify<__nv_bfloat16, false>(p, B, ctas, s);
-        else
-            e = draft_probs ? launch_verify<float, true>(p, B, ctas, s) : launch_verify<float, false>(p, B, ctas, s);
+        const bool vec = ((uintptr_t)logits | (uintptr_t)draft_probs | (uintptr_t)noise) % 16 == 0 && logits_stride % (dtype == ACE_BF16 ? 8 : 4) == 0 &&
+                         (!draft_probs || draft_stride % 4 == 0) && noise_stride % 4 == 0;
+        if (dtype == ACE_BF16) e = verify_of<__nv_bfloat16>(p, B, ctas, vec, s);
+        else e = verify_of<float>(p, B, ctas, vec, s);
     }
     if (e != cudaSuccess)
         return ver_fail(ACE_ERR_CUDA, std::string("verify launch: ") + cudaGetErrorName(e) + " (" + cudaGetErrorString(e) + ")");
