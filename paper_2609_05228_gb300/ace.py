@@ -345,9 +345,24 @@ def ace_tree_attention(kv: int, layer: int, q, q_token_stride: int, q_head_strid
                                     _ptr(lse), _stream(stream)))
 
 
+_dtypes = None
+
+
+def _dtype(name: str):
+    """torch's dtype of that name (torch is imported at the first use)."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+
+        _dtypes = {n: getattr(torch, n) for n in ("bfloat16", "float32", "int32", "int64", "uint8", "float8_e4m3fn")}
+    return _dtypes[name]
+
+
 def _want(name: str, t, dtype: str, shape=None, contiguous: bool = True):
     """Checks a torch tensor argument: its type, shape (None: any size) and layout."""
-    if str(t.dtype) != "torch." + dtype:
+    if t.dtype is _dtype(dtype) and (shape is None or t.shape == shape) and (not contiguous or t.is_contiguous()) and t.is_cuda:
+        return
+    if t.dtype is not _dtype(dtype):
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if shape is not None and (t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape))):
         raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
@@ -363,10 +378,10 @@ def ace_verify_tree(logits, tokens, parents, node_offsets, max_nodes: int, unifo
     n_keep [B] and next_token [B] (int32). logits and draft_probs [T, vocab] and noise [B, vocab] may have padded rows."""
     T, V = logits.shape
     B = node_offsets.shape[0] - 1
-    dt = {"torch.bfloat16": ACE_BF16, "torch.float32": ACE_F32}.get(str(logits.dtype))
-    if dt is None:
+    dt = ACE_BF16 if logits.dtype is _dtype("bfloat16") else ACE_F32
+    if dt == ACE_F32 and logits.dtype is not _dtype("float32"):
         raise ValueError(f"logits must be bfloat16 or float32, not {logits.dtype}")
-    _want("logits", logits, str(logits.dtype)[6:], (T, V), False)
+    _want("logits", logits, "bfloat16" if dt == ACE_BF16 else "float32", (T, V), False)
     _want("noise", noise, "float32", (B, V), False)
     _want("uniforms", uniforms, "float32", (T,))
     if draft_probs is not None:
@@ -399,6 +414,7 @@ class AceKvCache:
             raise ValueError("dtype must be 'bf16' or 'f32' and fmt 'plain' or 'fp8'")
         self.handle = None
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self._dt = "bfloat16" if dtype == "bf16" else "float32"
         self.layers, self.n_pages, self.page_size = int(layers), int(n_pages), int(page_size)
         self.n_kv_heads, self.head_dim = int(n_kv_heads), int(head_dim)
         rows = (self.layers, self.n_pages, self.n_kv_heads, self.page_size)
@@ -425,7 +441,7 @@ class AceKvCache:
 
     def _rows(self, name, t, heads):
         """(token stride, head stride) of rows [T, heads, head_dim] of any strides but the last."""
-        _want(name, t, str(self.torch_dtype)[6:], (None, heads, self.head_dim), False)
+        _want(name, t, self._dt, (t.shape[0], heads, self.head_dim), False)
         if t.numel() and t.stride(2) != 1:
             raise ValueError(f"the last axis of {name} must be contiguous")
         return t.stride(0), t.stride(1)
@@ -448,7 +464,7 @@ class AceKvCache:
             layer, shape = -1, (self.layers,) + shape
         _want("slots", slots, "int64", (T,))
         for name, t in (("k_out", k_out), ("v_out", v_out)):
-            _want(name, t, str(self.torch_dtype)[6:], shape)
+            _want(name, t, self._dt, shape)
         ace_kv_read(self.handle, layer, slots, T, k_out, v_out, stream)
 
     def keep(self, page_table, lens, path, n_keep, new_lens=None, stream=None) -> None:
@@ -471,7 +487,7 @@ class AceKvCache:
         _want("page_table", page_table, "int32")
         _want("lens", lens, "int32", (B,))
         _want("node_offsets", node_offsets, "int32", (B + 1,))
-        _want("out", out, str(self.torch_dtype)[6:], tuple(q.shape))
+        _want("out", out, self._dt, q.shape)
         if mask is not None:
             _want("mask", mask, "int64", (T, (max_nodes + 63) // 64))
         if lse is not None:

@@ -19,7 +19,7 @@ namespace {
 using namespace ace;
 
 constexpr int kVerThreads = 512, kVerWarps = kVerThreads / 32, kMaxCluster = 8;
-constexpr int kPassUnroll = 2, kPass = 4 * kVerThreads * kPassUnroll;      // elements of a turn of a pass
+constexpr int kPassUnroll = 2;          // loads of four elements a thread, row and turn of a pass (twice as many without the noise)
 
 struct VerifyArgs {
     const void* logits;
@@ -74,6 +74,8 @@ struct Shared {
     Sums cta[2][kMaxCluster];           // by turns, so that a fast CTA's next values find the other buffer
     int parent[kMaxNodes];
     int token[kMaxNodes];
+    // the current node's children: logit and draft probability at their token, and u
+    float zx[kMaxNodes], qx[kMaxNodes], u[kMaxNodes];
     // rejected children of the current node: token, 1 / Z (0: the residual stayed), 1 / (1 - q)
     int x[kMaxNodes];
     float rz[kMaxNodes], rq[kMaxNodes];
@@ -143,10 +145,11 @@ __device__ __forceinline__ float residual(const Shared& sh, const Row& w, int k,
 // loads of a turn are under way together.
 template <typename T, bool VEC, bool Q, bool NOISE, typename F>
 __device__ __forceinline__ void pass(const T* z, const float* q, const float* noise, int lo, int hi, F f) {
-    for (int base = lo; base < hi; base += kPass) {
-        float zf[kPassUnroll][4], qf[kPassUnroll][4], nf[kPassUnroll][4];
+    constexpr int U = NOISE ? kPassUnroll : 2 * kPassUnroll;
+    for (int base = lo; base < hi; base += 4 * kVerThreads * U) {
+        float zf[U][4], qf[U][4], nf[NOISE ? U : 1][4];
 #pragma unroll
-        for (int u = 0; u < kPassUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int i = base + 4 * (threadIdx.x + kVerThreads * u);
             if (VEC && i + 4 <= hi) {
                 if constexpr (sizeof(T) == 2) {
@@ -157,7 +160,7 @@ __device__ __forceinline__ void pass(const T* z, const float* q, const float* no
                     *reinterpret_cast<float4*>(zf[u]) = __ldg(reinterpret_cast<const float4*>(z + i));
                 }
                 if (Q) *reinterpret_cast<float4*>(qf[u]) = __ldg(reinterpret_cast<const float4*>(q + i));
-                if (NOISE) *reinterpret_cast<float4*>(nf[u]) = __ldg(reinterpret_cast<const float4*>(noise + i));
+                if constexpr (NOISE) *reinterpret_cast<float4*>(nf[u]) = __ldg(reinterpret_cast<const float4*>(noise + i));
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -165,19 +168,27 @@ __device__ __forceinline__ void pass(const T* z, const float* q, const float* no
                     const bool in = e < hi;
                     zf[u][j] = in ? to_f32(z[e]) : -INFINITY;
                     qf[u][j] = Q && in ? __ldg(q + e) : 0.f;
-                    nf[u][j] = NOISE && in ? __ldg(noise + e) : 1.f;
+                    if constexpr (NOISE) nf[u][j] = in ? __ldg(noise + e) : 1.f;
                 }
             }
         }
 #pragma unroll
-        for (int u = 0; u < kPassUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int e = VEC ? base + 4 * ((int)threadIdx.x + kVerThreads * u) + j : base + (int)threadIdx.x + kVerThreads * (4 * u + j);
-                if (e < hi) f(e, zf[u][j], Q ? qf[u][j] : 0.f, NOISE ? nf[u][j] : 1.f);
+                if (e < hi) f(e, zf[u][j], Q ? qf[u][j] : 0.f, nf[NOISE ? u : 0][j]);
             }
         }
     }
+}
+
+// Asks for a row's elements lo .. hi in L2, a line a thread and turn.
+template <typename T>
+__device__ __forceinline__ void prefetch_row(const T* row, int lo, int hi) {
+    const char* end = reinterpret_cast<const char*>(row + hi);
+    for (const char* p = reinterpret_cast<const char*>(row + lo) + threadIdx.x * 128; p < end; p += kVerThreads * 128)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
 }
 
 // Softmax statistics of z[lo .. hi): 16-byte loads between the unaligned ends, 4 a thread under way together.
@@ -255,6 +266,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
     w.inv_t = greedy ? 1.f : 1.f / temp;
     const float* noise = p.noise + b * p.noise_stride;
     int turn = 0, node = 0, keep = 0, token = -1;
+    if (n > 0 && !greedy) prefetch_row(noise, lo, hi);
     // every CTA of the cluster has started before another writes into its shared memory
     cluster_sync();
     while (n > 0) {
@@ -262,6 +274,21 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
         ++keep;
         const T* z = static_cast<const T*>(p.logits) + (o0 + node) * p.logits_stride;
         const float* qrow = DRAFT ? p.draft + (o0 + node) * p.draft_stride : nullptr;
+        // what this node's walk may need next: its draft row where it has a child, and the first child's logits
+        int first = node + 1;
+        while (first < n && sh.parent[first] != node) ++first;
+        if (first < n) {
+            if (DRAFT && !greedy) prefetch_row(qrow, lo, hi);
+            prefetch_row(static_cast<const T*>(p.logits) + (o0 + first) * p.logits_stride, lo, hi);
+        }
+        // (a later node's children may lie in the same places: the walk has passed a barrier since it read them)
+        for (int c = node + 1 + tid; c < n; c += kVerThreads) {
+            const int x = sh.token[c];
+            if (sh.parent[c] != node || x < 0 || x >= V) continue;
+            sh.zx[c] = to_f32(z[x]);
+            sh.qx[c] = DRAFT ? qrow[x] : 1.f;
+            sh.u[c] = p.uniforms[o0 + c];
+        }
         Sums v = row_stats(z, lo, hi, V, w.inv_t);
         v = join_all<join_stats>(sh, v, w.inv_t, turn, ctas);
         if (v.bad || v.m == -INFINITY) break;               // token stays -1
@@ -290,9 +317,9 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
                 pending = false;
             }
             if (x < 0 || x >= V) continue;  // never accepted, takes nothing from the residual
-            float q = DRAFT ? qrow[x] : 1.f;
-            const float r = residual<DRAFT>(sh, w, w.k, x, to_f32(z[x]), q);
-            if (r > 0.f && p.uniforms[o0 + c] * q <= r) {
+            float q = sh.qx[c];
+            const float r = residual<DRAFT>(sh, w, w.k, x, sh.zx[c], q);
+            if (r > 0.f && sh.u[c] * q <= r) {
                 taken = c;
             } else {
                 __syncthreads();            // the lists are read above
