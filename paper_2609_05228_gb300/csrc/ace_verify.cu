@@ -5,9 +5,10 @@
 // cluster's CTAs, and the row's maximum, sum and argmax are joined through distributed shared memory, so all
 // CTAs take the same branch from the same bits. Only the rows that the walk visits are read: one pass for
 // the softmax's statistics; where a child is rejected and another follows, one for the residual's sum;
-// one for the argmax at the end. Later passes hit L2. No element is stored: after k rejections the residual
-// at v is k steps from its logit and draft probability,
-//   r <- max(r - q, 0) / Z_j,   q <- q / (1 - q(x_j)), 0 at x_j.
+// one for the argmax at the end. Later passes hit L2. No element is stored: with q's normalisations and the
+// residuals' gathered in scalars, the residual at v after k rejections is nu rho_k with
+//   rho_0 = 2^(z a + b),   rho_j = max(rho_(j-1) - c_j q, 0),   q <- 0 at x_j,
+// two operations a rejection and element (the passes of a request that rejects are bound by them).
 #include <math.h>
 
 #include <string>
@@ -47,26 +48,39 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 
-// What a pass adds up: a maximum, a sum relative to it (or plain), an index, a flag.
+// What a pass adds up: a maximum with its lowest index, a sum (relative to the maximum, for the softmax), a flag.
 struct Sums {
     float m, s;
     int at, bad;
 };
 
-// Softmax statistics (sums relative to their maxima, in temperature units) and the lowest index of the maximum.
-__device__ __forceinline__ Sums join_stats(const Sums& a, const Sums& b, float inv_t) {
-    Sums r;
-    r.m = fmaxf(a.m, b.m);
-    const float ref = r.m == -INFINITY ? 0.f : r.m;
-    r.s = a.s * __expf((a.m - ref) * inv_t) + b.s * __expf((b.m - ref) * inv_t);
-    r.at = a.m > b.m ? a.at : b.m > a.m ? b.at : min(a.at, b.at);
-    r.bad = a.bad | b.bad;
-    return r;
+enum Join { kStats, kSum, kArgmax };
+
+// Floats in the order of integers (NaN must not occur).
+__device__ __forceinline__ float warp_top(float x) {
+    int i = __float_as_int(x);
+    i ^= (i >> 31) & 0x7fffffff;
+    i = __reduce_max_sync(0xffffffffu, i);
+    return __int_as_float(i ^ ((i >> 31) & 0x7fffffff));
 }
 
-// Plain sum and maximum (with the lowest index).
-__device__ __forceinline__ Sums join_plain(const Sums& a, const Sums& b, float) {
-    return Sums{fmaxf(a.m, b.m), a.s + b.s, a.m > b.m ? a.at : b.m > a.m ? b.at : min(a.at, b.at), a.bad | b.bad};
+// Joins a warp's values; every lane gets the same bits.
+template <Join J>
+__device__ __forceinline__ Sums join_warp(Sums v, float inv_t) {
+    Sums r{0.f, 0.f, 0, 0};
+    if (J != kSum) {
+        r.m = warp_top(v.m);
+        r.at = (int)__reduce_min_sync(0xffffffffu, v.m == r.m ? (unsigned)v.at : 0x7fffffffu);
+    }
+    if (J != kArgmax) {
+        float x = v.s;
+        if (J == kStats) x *= r.m == -INFINITY ? 0.f : __expf((v.m - r.m) * inv_t);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        r.s = x;
+    }
+    if (J == kStats) r.bad = __any_sync(0xffffffffu, v.bad);
+    return r;
 }
 
 struct Shared {
@@ -76,110 +90,108 @@ struct Shared {
     int token[kMaxNodes];
     // the current node's children: logit and draft probability at their token, and u
     float zx[kMaxNodes], qx[kMaxNodes], u[kMaxNodes];
-    // rejected children of the current node: token, 1 / Z (0: the residual stayed), 1 / (1 - q)
+    // rejected children of the current node: factor c of the draft probability (0: the residual stayed), token
+    float c[kMaxNodes];
     int x[kMaxNodes];
-    float rz[kMaxNodes], rq[kMaxNodes];
 };
 
 // Joins every thread's value over the CTA, then over the cluster; all threads of all CTAs get the same bits.
-template <Sums (*JOIN)(const Sums&, const Sums&, float)>
+template <Join J>
 __device__ Sums join_all(Shared& sh, Sums v, float inv_t, int& turn, int ctas) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Sums u;
-        u.m = __shfl_xor_sync(0xffffffffu, v.m, o);
-        u.s = __shfl_xor_sync(0xffffffffu, v.s, o);
-        u.at = __shfl_xor_sync(0xffffffffu, v.at, o);
-        u.bad = __shfl_xor_sync(0xffffffffu, v.bad, o);
-        // the lower lane first, so that both lanes of a pair get the same bits
-        v = (threadIdx.x & o) ? JOIN(u, v, inv_t) : JOIN(v, u, inv_t);
-    }
-    if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = v;
+    const int lane = threadIdx.x & 31;
+    const Sums none{-INFINITY, 0.f, 0x7fffffff, 0};
+    v = join_warp<J>(v, inv_t);
+    if (lane == 0) sh.warp[threadIdx.x >> 5] = v;
     __syncthreads();
     if (threadIdx.x < 32) {
-        Sums t = sh.warp[threadIdx.x % kVerWarps];
-#pragma unroll
-        for (int o = kVerWarps / 2; o > 0; o >>= 1) {
-            Sums u;
-            u.m = __shfl_xor_sync(0xffffffffu, t.m, o);
-            u.s = __shfl_xor_sync(0xffffffffu, t.s, o);
-            u.at = __shfl_xor_sync(0xffffffffu, t.at, o);
-            u.bad = __shfl_xor_sync(0xffffffffu, t.bad, o);
-            t = (threadIdx.x & o) ? JOIN(u, t, inv_t) : JOIN(t, u, inv_t);
-        }
-        if ((int)threadIdx.x < ctas) {          // lane c hands it to CTA c
+        const Sums t = join_warp<J>(lane < kVerWarps ? sh.warp[lane % kVerWarps] : none, inv_t);
+        if (lane < ctas) {                      // lane c hands it to CTA c
             const uint32_t mine = smem_u32(&sh.cta[turn][cluster_rank()]);
             uint32_t there;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(threadIdx.x));
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(lane));
             asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(there), "r"(__float_as_uint(t.m)),
                          "r"(__float_as_uint(t.s)), "r"(t.at), "r"(t.bad)
                          : "memory");
         }
+        __syncwarp();
     }
     cluster_sync();
-    Sums r = sh.cta[turn][0];
-    for (int c = 1; c < ctas; ++c) r = JOIN(r, sh.cta[turn][c], inv_t);
+    const Sums r = join_warp<J>(lane < ctas ? sh.cta[turn][lane % kMaxCluster] : none, inv_t);
     turn ^= 1;
     return r;
 }
 
+// A node's softmax as rho_0 = 2^(z a + b), and what its rejections make of it.
 struct Row {
-    float m, inv_t, inv_s;
+    float a, b, nu, q_mul;              // residual = nu rho_k; draft probabilities of what is left: q_mul q
     int k;                              // rejections so far
 };
 
-// Residual at v after the row's first `k` rejections; the last one not yet applied is the caller's.
-template <bool DRAFT>
-__device__ __forceinline__ float residual(const Shared& sh, const Row& w, int k, int v, float z, float& q) {
-    float r = __expf((z - w.m) * w.inv_t) * w.inv_s;
-    for (int j = 0; j < k; ++j) {
-        const float less = DRAFT ? fmaxf(r - q, 0.f) : (v == sh.x[j] ? 0.f : r);
-        if (sh.rz[j] > 0.f) r = less * sh.rz[j];
-        if (DRAFT) q = v == sh.x[j] ? 0.f : q * sh.rq[j];
-    }
-    return r;
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
-// A turn of a pass over elements lo <= i < hi of up to three rows: calls f(i, z, q, noise) for each of the thread's. With VEC a
+// rho_k of N elements from their indices, logits and draft probabilities; q becomes 0 at rejected tokens.
+template <bool DRAFT, int N>
+__device__ __forceinline__ void residuals(const Shared& sh, const Row& w, const int (&v)[N], const float (&z)[N], float (&q)[N], float (&rho)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) rho[i] = exp2_of(fmaf(z[i], w.a, w.b));
+    for (int j = 0; j < w.k; ++j) {
+        const float c = sh.c[j];
+        const int x = sh.x[j];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (DRAFT) {
+                rho[i] = fmaxf(fmaf(-c, q[i], rho[i]), 0.f);
+                if (v[i] == x) q[i] = 0.f;
+            } else if (v[i] == x) {
+                rho[i] = c > 0.f ? 0.f : rho[i];
+            }
+        }
+    }
+}
+
+// A pass over elements lo <= i < hi of up to three rows: calls f(indices, z, q, noise) for batches of the thread's. With VEC a
 // thread's elements come four at a time in one load a row (all rows 16-byte aligned), else one by one. All
 // loads of a turn are under way together.
 template <typename T, bool VEC, bool Q, bool NOISE, typename F>
 __device__ __forceinline__ void pass(const T* z, const float* q, const float* noise, int lo, int hi, F f) {
-    constexpr int U = NOISE ? kPassUnroll : 2 * kPassUnroll;
-    for (int base = lo; base < hi; base += 4 * kVerThreads * U) {
-        float zf[U][4], qf[U][4], nf[NOISE ? U : 1][4];
+    constexpr int U = NOISE ? kPassUnroll : 2 * kPassUnroll, N = 4 * U;
+    for (int base = lo; base < hi; base += kVerThreads * N) {
+        float zf[N], qf[N], nf[NOISE ? N : 1];
+        int at[N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = base + 4 * (threadIdx.x + kVerThreads * u);
+            const int i = base + 4 * ((int)threadIdx.x + kVerThreads * u);
             if (VEC && i + 4 <= hi) {
                 if constexpr (sizeof(T) == 2) {
                     const uint2 w = __ldg(reinterpret_cast<const uint2*>(z + i));
-                    zf[u][0] = __uint_as_float(w.x << 16), zf[u][1] = __uint_as_float(w.x & 0xffff0000u);
-                    zf[u][2] = __uint_as_float(w.y << 16), zf[u][3] = __uint_as_float(w.y & 0xffff0000u);
+                    zf[4 * u] = __uint_as_float(w.x << 16), zf[4 * u + 1] = __uint_as_float(w.x & 0xffff0000u);
+                    zf[4 * u + 2] = __uint_as_float(w.y << 16), zf[4 * u + 3] = __uint_as_float(w.y & 0xffff0000u);
                 } else {
-                    *reinterpret_cast<float4*>(zf[u]) = __ldg(reinterpret_cast<const float4*>(z + i));
+                    *reinterpret_cast<float4*>(zf + 4 * u) = __ldg(reinterpret_cast<const float4*>(z + i));
                 }
-                if (Q) *reinterpret_cast<float4*>(qf[u]) = __ldg(reinterpret_cast<const float4*>(q + i));
-                if constexpr (NOISE) *reinterpret_cast<float4*>(nf[u]) = __ldg(reinterpret_cast<const float4*>(noise + i));
+                if (Q) *reinterpret_cast<float4*>(qf + 4 * u) = __ldg(reinterpret_cast<const float4*>(q + i));
+                if constexpr (NOISE) *reinterpret_cast<float4*>(nf + 4 * u) = __ldg(reinterpret_cast<const float4*>(noise + i));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) at[4 * u + j] = i + j;
             } else {
+                // (an element past the end: a logit of -inf, so a residual of zero)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int e = VEC ? i + j : base + (int)threadIdx.x + kVerThreads * (4 * u + j);
                     const bool in = e < hi;
-                    zf[u][j] = in ? to_f32(z[e]) : -INFINITY;
-                    qf[u][j] = Q && in ? __ldg(q + e) : 0.f;
-                    if constexpr (NOISE) nf[u][j] = in ? __ldg(noise + e) : 1.f;
+                    at[4 * u + j] = e;
+                    zf[4 * u + j] = in ? to_f32(z[e]) : -INFINITY;
+                    qf[4 * u + j] = Q && in ? __ldg(q + e) : 0.f;
+                    if constexpr (NOISE) nf[4 * u + j] = in ? __ldg(noise + e) : 1.f;
                 }
             }
+            if (!Q) qf[4 * u] = qf[4 * u + 1] = qf[4 * u + 2] = qf[4 * u + 3] = 0.f;
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int e = VEC ? base + 4 * ((int)threadIdx.x + kVerThreads * u) + j : base + (int)threadIdx.x + kVerThreads * (4 * u + j);
-                if (e < hi) f(e, zf[u][j], Q ? qf[u][j] : 0.f, nf[NOISE ? u : 0][j]);
-            }
-        }
+        f(at, zf, qf, nf);
     }
 }
 
@@ -193,7 +205,7 @@ __device__ __forceinline__ void prefetch_row(const T* row, int lo, int hi) {
 
 // Softmax statistics of z[lo .. hi): 16-byte loads between the unaligned ends, 4 a thread under way together.
 template <typename T>
-__device__ Sums row_stats(const T* z, int lo, int hi, int none, float inv_t) {
+__device__ Sums row_stats(const T* z, int lo, int hi, int none, float inv_t, bool find) {
     constexpr int N = Vec16<T>::N, U = 4;
     Sums v{-INFINITY, 0.f, none, 0};
     auto one = [&](int i) {
@@ -229,7 +241,15 @@ __device__ Sums row_stats(const T* z, int lo, int hi, int none, float inv_t) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 if (!(f[u][i] < INFINITY)) v.bad = 1;
-                if (f[u][i] > top) top = f[u][i], v.at = a0 + (g0 + u * kVerThreads) * N + i;
+                top = fmaxf(top, f[u][i]);
+            }
+        }
+        if (find && top > v.m) {            // greedy requests: where the maximum is first
+#pragma unroll
+            for (int u = U - 1; u >= 0; --u) {
+#pragma unroll
+                for (int i = N - 1; i >= 0; --i)
+                    if (f[u][i] == top) v.at = a0 + (g0 + u * kVerThreads) * N + i;
             }
         }
         const float ref = top == -INFINITY ? 0.f : top;
@@ -263,7 +283,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
     const float temp = p.temperature ? p.temperature[b] : 1.f;
     const bool greedy = !(temp > 0.f);
     Row w;
-    w.inv_t = greedy ? 1.f : 1.f / temp;
+    const float inv_t = greedy ? 1.f : 1.f / temp;
     const float* noise = p.noise + b * p.noise_stride;
     int turn = 0, node = 0, keep = 0, token = -1;
     if (n > 0 && !greedy) prefetch_row(noise, lo, hi);
@@ -289,11 +309,13 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
             sh.qx[c] = DRAFT ? qrow[x] : 1.f;
             sh.u[c] = p.uniforms[o0 + c];
         }
-        Sums v = row_stats(z, lo, hi, V, w.inv_t);
-        v = join_all<join_stats>(sh, v, w.inv_t, turn, ctas);
+        Sums v = row_stats(z, lo, hi, V, inv_t, greedy);
+        v = join_all<kStats>(sh, v, inv_t, turn, ctas);
         if (v.bad || v.m == -INFINITY) break;               // token stays -1
-        w.m = v.m;
-        w.inv_s = 1.f / v.s;
+        w.a = inv_t * 1.4426950408889634f;
+        w.b = -v.m * w.a;
+        w.nu = 1.f / v.s;
+        w.q_mul = 1.f;
         w.k = 0;
         int taken = -1;
         bool pending = false;               // the last rejection's residual has not been summed
@@ -307,29 +329,39 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
             if (pending) {
                 // the residual after the last rejection: its sum over the vocabulary
                 Sums t{0.f, 0.f, 0, 0};
-                pass<T, VEC, DRAFT, false>(z, qrow, nullptr, lo, hi, [&](int i, float zi, float q, float) {
-                    const float r = residual<DRAFT>(sh, w, w.k - 1, i, zi, q);
-                    t.s += DRAFT ? fmaxf(r - q, 0.f) : (i == sh.x[w.k - 1] ? 0.f : r);
+                pass<T, VEC, DRAFT, false>(z, qrow, nullptr, lo, hi, [&](const auto& at, const auto& zi, auto& q, const auto&) {
+                    float rho[sizeof(zi) / 4];
+                    residuals<DRAFT>(sh, w, at, zi, q, rho);
+#pragma unroll
+                    for (int i = 0; i < (int)(sizeof(zi) / 4); ++i) t.s += rho[i];
                 });
-                t = join_all<join_plain>(sh, t, 0.f, turn, ctas);
-                if (tid == 0) sh.rz[w.k - 1] = t.s > 0.f ? 1.f / t.s : 0.f;
-                __syncthreads();
+                t = join_all<kSum>(sh, t, 0.f, turn, ctas);
+                if (t.s > 0.f) {
+                    w.nu = 1.f / t.s;
+                } else {
+                    __syncthreads();
+                    if (tid == 0) sh.c[w.k - 1] = 0.f;
+                    __syncthreads();
+                }
                 pending = false;
             }
             if (x < 0 || x >= V) continue;  // never accepted, takes nothing from the residual
-            float q = sh.qx[c];
-            const float r = residual<DRAFT>(sh, w, w.k, x, sh.zx[c], q);
+            const int at[1] = {x};
+            const float zx[1] = {sh.zx[c]};
+            float q1[1] = {sh.qx[c]}, rho[1];
+            residuals<DRAFT>(sh, w, at, zx, q1, rho);
+            const float r = rho[0] * w.nu, q = DRAFT ? q1[0] * w.q_mul : 1.f;
             if (r > 0.f && sh.u[c] * q <= r) {
                 taken = c;
             } else {
                 __syncthreads();            // the lists are read above
                 if (tid == 0) {
-                    const float rest = 1.f - q;
                     sh.x[w.k] = x;
-                    sh.rz[w.k] = 1.f;
-                    sh.rq[w.k] = rest > 0.f ? 1.f / rest : 0.f;
+                    sh.c[w.k] = DRAFT ? w.q_mul / w.nu : 1.f;
                 }
                 __syncthreads();
+                const float rest = 1.f - q;
+                w.q_mul = rest > 0.f ? w.q_mul / rest : 0.f;
                 ++w.k;
                 pending = true;
             }
@@ -345,16 +377,23 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
         }
         // a sample of the residual: argmax of r / noise. It is not normalised after the last rejection, and
         // where that leaves nothing the residual before it counts.
-        for (int k = w.k; ; --k) {
+        for (bool again = pending; ; again = false) {
             Sums t{-1.f, 0.f, V, 0};
-            pass<T, VEC, DRAFT, true>(z, qrow, noise, lo, hi, [&](int i, float zi, float q, float e) {
-                const float r = residual<DRAFT>(sh, w, k, i, zi, q);
-                const float g = r > 0.f ? r / e : -1.f;
-                if (g > t.m || (g == t.m && i < t.at)) t.m = g, t.at = i;
+            pass<T, VEC, DRAFT, true>(z, qrow, noise, lo, hi, [&](const auto& at, const auto& zi, auto& q, const auto& e) {
+                float rho[sizeof(zi) / 4];
+                residuals<DRAFT>(sh, w, at, zi, q, rho);
+#pragma unroll
+                for (int i = 0; i < (int)(sizeof(zi) / 4); ++i) {
+                    const float g = rho[i] > 0.f ? rho[i] / e[i] : -1.f;
+                    if (g > t.m || (g == t.m && at[i] < t.at)) t.m = g, t.at = at[i];
+                }
             });
-            t = join_all<join_plain>(sh, t, 0.f, turn, ctas);
+            t = join_all<kArgmax>(sh, t, 0.f, turn, ctas);
             if (t.m >= 0.f) token = t.at;
-            if (t.m >= 0.f || !pending || k < w.k) break;
+            if (t.m >= 0.f || !again) break;
+            __syncthreads();
+            if (tid == 0) sh.c[w.k - 1] = 0.f;
+            __syncthreads();
         }
         break;
     }
