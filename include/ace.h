@@ -446,7 +446,7 @@ ace_status ace_kv_sync(ace_kv* kv);
  *           h * k_head_stride elements and is contiguous (any stride >= 0)
  *   slots   [T] int64 device: slot of each token, negative to leave it out; a slot
  *           that two tokens name holds either one's row
- * Errors: INVALID_ARG (NULL, layer, T < 0, negative stride).
+ * Errors: INVALID_ARG (NULL, layer, T < 0, negative stride); UNSUPPORTED for 2 T H > 2^30.
  */
 ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_stride, long long k_head_stride,
                         const void* v, long long v_token_stride, long long v_head_stride, const int64_t* slots, int T,
@@ -457,6 +457,7 @@ ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_
  *   layer         0 .. layers - 1, or -1 for all of them
  *   k_out, v_out  [T, H, D] (layer -1: [layers, T, H, D]), contiguous, 16-byte aligned;
  *                 a negative slot gives zeros
+ * Errors: as ace_kv_write (2 T H layers for layer -1).
  */
 ace_status ace_kv_read(ace_kv* kv, int layer, const int64_t* slots, int T, void* k_out, void* v_out, void* stream);
 

@@ -26,7 +26,7 @@ struct RowArgs {
     uint8_t* pool[2];
     uint8_t* scale[2];
     const int64_t* slots;
-    long long rows;                     // (layers *) T * 2 * H
+    uint32_t rows;                      // (layers *) T * 2 * H
     long long n_slots;                  // of a layer
     int T, H, D, page_size, page_shift;
     int* err;
@@ -37,17 +37,28 @@ __device__ __forceinline__ long long pool_row(const RowArgs& p, long long slot, 
     return (((slot >> p.page_shift) * p.H + h) << p.page_shift) + (slot & (p.page_size - 1));
 }
 
-template <typename T, bool ALIGNED>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
-    if constexpr (!ALIGNED) {
+// 8 elements of a row as they lie in memory.
+template <typename T>
+struct Raw8 {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void to_float(float (&f)[8]) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = to_f32(p[i]);
-    } else if constexpr (sizeof(T) == 2) {
-        Vec16<T>::to_float(ld_stream(p), f);
-    } else {
-        Vec16<T>::to_float(ld_stream(p), f);
-        Vec16<T>::to_float(ld_stream(p + 4), f + 4);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) Vec16<T>::to_float(w[i], f + i * Vec16<T>::N);
     }
+};
+
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ Raw8<T> load8(const T* p) {
+    Raw8<T> r;
+    if constexpr (ALIGNED) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ld_stream(p + i * Vec16<T>::N);
+    } else {
+        T* e = reinterpret_cast<T*>(r.w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = p[i];
+    }
+    return r;
 }
 
 template <typename T>
@@ -67,80 +78,128 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
 }
 
 // LANES lanes (a power of two, at least D / 8) hold one row, 8 elements each: its largest magnitude is
-// a shuffle reduction, nothing is read twice. Bound by memory.
+// a shuffle reduction, nothing is read twice. Bound by memory: each group of lanes has kRowTurns neighbouring rows under way
+// together, and the rows are not waited for by way of their slots.
+constexpr int kRowTurns = 4;
+
+// Row r of a call: (token, K or V, head), heads fastest.
+struct RowAt {
+    uint32_t th;                        // 2 * token + (V: 1)
+    int h;
+    __device__ __forceinline__ RowAt(uint32_t r, uint32_t H) : th(r / H), h((int)(r - r / H * H)) {}
+    __device__ __forceinline__ void next(int H) {
+        if (++h == H) h = 0, ++th;
+    }
+};
+
 template <typename T, bool FP8, bool ALIGNED, int LANES>
-__global__ void __launch_bounds__(256) k_kv_write(RowArgs p) {
+__global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ RowArgs p) {
     const int sub = threadIdx.x % LANES;
     const bool in = sub * 8 < p.D;
-    const long long step = (long long)gridDim.x * (256 / LANES);
-    for (long long r0 = (long long)blockIdx.x * (256 / LANES); r0 < p.rows; r0 += step) {
-        const long long r = r0 + threadIdx.x / LANES;
-        const bool live = r < p.rows;
-        const int h = (int)(r % p.H), kv = (int)(r / p.H & 1);
-        const long long t = r / p.H / 2;
-        float f[8] = {};
-        long long slot = -1;
-        if (live) {
-            slot = p.slots[t];
-            if (slot >= p.n_slots) {
-                if (sub == 0) atomicOr(p.err, kErrIndex);
-                slot = -1;
-            }
-            if (in && slot >= 0)
-                load8<T, ALIGNED>(static_cast<const T*>(p.src[kv]) + t * p.token_stride[kv] + h * p.head_stride[kv] + sub * 8, f);
+    const uint32_t r0 = (blockIdx.x * (256 / LANES) + threadIdx.x / LANES) * kRowTurns;
+    RowAt at(r0, p.H);
+    long long slot[kRowTurns];
+    Raw8<T> raw[kRowTurns];
+#pragma unroll
+    for (int j = 0; j < kRowTurns; ++j, at.next(p.H)) {
+        const bool live = r0 + j < p.rows;
+        const int kv = at.th & 1;
+        const long long t = at.th >> 1;
+        slot[j] = live ? p.slots[t] : -1;
+        if (live && in) raw[j] = load8<T, ALIGNED>(static_cast<const T*>(p.src[kv]) + t * p.token_stride[kv] + at.h * p.head_stride[kv] + sub * 8);
+        else raw[j] = Raw8<T>{};
+    }
+    at = RowAt(r0, p.H);
+#pragma unroll
+    for (int j = 0; j < kRowTurns; ++j, at.next(p.H)) {
+        const int kv = at.th & 1;
+        if (slot[j] >= p.n_slots) {
+            if (sub == 0) atomicOr(p.err, kErrIndex);
+            slot[j] = -1;
         }
-        const long long row = slot >= 0 ? pool_row(p, slot, h) : 0;
+        const long long row = slot[j] >= 0 ? pool_row(p, slot[j], at.h) : 0;
+        const bool put = in && slot[j] >= 0;
         if constexpr (FP8) {
-            float amax = 0.f;
+            float f[8], amax = 0.f;
+            raw[j].to_float(f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 f[i] = finite_or_nan(f[i]);
-                amax = fmaxf(amax, fabsf(f[i]));         // fmaxf drops NaN
+                amax = fmaxf(amax, fabsf(f[i]));             // fmaxf drops NaN
             }
 #pragma unroll
             for (int o = LANES / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
             const int byte = e4m3_scale_byte(amax);
             const float m = pow2_of_minus_byte(byte);
-            if (in && slot >= 0) {
+            if (put) {
                 uint2 w;
                 w.x = e4m3x2(f[0] * m, f[1] * m) | e4m3x2(f[2] * m, f[3] * m) << 16;
                 w.y = e4m3x2(f[4] * m, f[5] * m) | e4m3x2(f[6] * m, f[7] * m) << 16;
                 *reinterpret_cast<uint2*>(p.pool[kv] + row * p.D + sub * 8) = w;
                 if (sub == 0) p.scale[kv][row] = (uint8_t)byte;
             }
-        } else if (in && slot >= 0) {
-            store8(reinterpret_cast<T*>(p.pool[kv]) + row * p.D + sub * 8, f);
+        } else if (put) {
+            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.pool[kv]) + row * p.D + sub * 8);
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) dst[i] = raw[j].w[i];
         }
     }
 }
 
 template <typename T, bool FP8, int LANES>
-__global__ void __launch_bounds__(256) k_kv_read(RowArgs p) {
+__global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ RowArgs p) {
     const int sub = threadIdx.x % LANES;
     if (sub * 8 >= p.D) return;
-    const long long step = (long long)gridDim.x * (256 / LANES);
-    for (long long r = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; r < p.rows; r += step) {
-        const int h = (int)(r % p.H), kv = (int)(r / p.H & 1);
-        const long long lt = r / p.H / 2;               // layer * T + token
-        const long long layer = lt / p.T;
-        long long slot = p.slots[lt - layer * p.T];
+    const uint32_t r0 = (blockIdx.x * (256 / LANES) + threadIdx.x / LANES) * kRowTurns;
+    RowAt at(r0, p.H);
+    long long row[kRowTurns];           // -1: zeros
+#pragma unroll
+    for (int j = 0; j < kRowTurns; ++j, at.next(p.H)) {
+        row[j] = -1;
+        if (r0 + j >= p.rows) continue;
+        const uint32_t lt = at.th >> 1, layer = lt / (uint32_t)p.T;          // layer * T + token
+        const long long slot = p.slots[lt - layer * p.T];
         if (slot >= p.n_slots) {
             if (sub == 0) atomicOr(p.err, kErrIndex);
-            slot = -1;
+        } else if (slot >= 0) {
+            row[j] = layer * p.n_slots * p.H + pool_row(p, slot, at.h);
         }
-        float f[8] = {};
-        if (slot >= 0) {
-            const long long row = layer * p.n_slots * p.H + pool_row(p, slot, h);
-            if constexpr (FP8) {
-                e4m3x8_to_float(__ldg(reinterpret_cast<const uint2*>(p.pool[kv] + row * p.D + sub * 8)), f);
-                const float m = pow2_of_byte(p.scale[kv][row]);
+    }
+    Raw8<T> raw[FP8 ? 1 : kRowTurns];
+    uint2 code[kRowTurns];
+    uint8_t byte[kRowTurns];
+    at = RowAt(r0, p.H);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= m;
-            } else {
-                load8<T, true>(reinterpret_cast<const T*>(p.pool[kv]) + row * p.D + sub * 8, f);
+    for (int j = 0; j < kRowTurns; ++j, at.next(p.H)) {
+        const int kv = at.th & 1;
+        if constexpr (FP8) {
+            code[j] = make_uint2(0, 0);
+            byte[j] = 1;
+            if (row[j] >= 0) {
+                code[j] = __ldg(reinterpret_cast<const uint2*>(p.pool[kv] + row[j] * p.D + sub * 8));
+                byte[j] = __ldg(p.scale[kv] + row[j]);
             }
+        } else {
+            if (row[j] >= 0) raw[j] = load8<T, true>(reinterpret_cast<const T*>(p.pool[kv]) + row[j] * p.D + sub * 8);
+            else raw[j] = Raw8<T>{};
         }
-        store8(static_cast<T*>(p.dst[kv]) + (lt * p.H + h) * p.D + sub * 8, f);
+    }
+    at = RowAt(r0, p.H);
+#pragma unroll
+    for (int j = 0; j < kRowTurns; ++j, at.next(p.H)) {
+        if (r0 + j >= p.rows) break;
+        T* dst = static_cast<T*>(p.dst[at.th & 1]) + ((long long)(at.th >> 1) * p.H + at.h) * p.D + sub * 8;
+        if constexpr (FP8) {
+            float f[8];
+            e4m3x8_to_float(code[j], f);
+            const float m = pow2_of_byte(byte[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= m;
+            store8(dst, f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(dst)[i] = raw[j].w[i];
+        }
     }
 }
 
@@ -152,19 +211,20 @@ struct KeepArgs {
     const int32_t* path;
     const int32_t* n_keep;
     int32_t* new_lens;
-    int max_pages, max_nodes, H, row_words, page_size, page_shift, n_pages, layers;   // row_words: 8-byte words of a row
+    int max_pages, max_nodes, H, row_words, page_size, page_shift, n_pages, layers;   // row_words: 8- or 16-byte words of a row
     int* err;
 };
 
-constexpr int kKeepThreads = 128, kKeepWords = 4;
+constexpr int kKeepThreads = 256, kKeepWords = 4;
 
-// Block (request, layer * H + head). Rows move towards the front (path[i] >= i and increasing), so a pass that
-// has read its rows before it writes any never overwrites a row of a later pass.
-__global__ void __launch_bounds__(kKeepThreads) k_kv_keep(KeepArgs p) {
-    __shared__ int src_row[kMaxNodes], dst_row[kMaxNodes];
+// Block (request, share of the layers and heads); W is a word of 8 or 16 bytes. The path is looked up once; then all rows'
+// words, in the order (layer, head), node, move in passes. Rows move towards the front (path[i] >= i and
+// increasing), so a pass that has read its words before it writes any never overwrites a word of a later pass.
+template <typename W>
+__global__ void __launch_bounds__(kKeepThreads) k_kv_keep(const __grid_constant__ KeepArgs p) {
+    __shared__ int src_row[kMaxNodes], dst_row[kMaxNodes];          // of head 0
     __shared__ int bad;
     const int b = blockIdx.x, tid = threadIdx.x;
-    const int layer = blockIdx.y / p.H, h = blockIdx.y % p.H;
     const int n = p.n_keep[b], len = p.lens[b];
     if (tid == 0) bad = n < 0 || n > p.max_nodes || len < 0;
     __syncthreads();
@@ -179,8 +239,8 @@ __global__ void __launch_bounds__(kKeepThreads) k_kv_keep(KeepArgs p) {
                 const int32_t* table = p.page_table + (long long)b * p.max_pages;
                 const int ps = table[sp >> p.page_shift], pd = table[dp >> p.page_shift];
                 ok = ps >= 0 && ps < p.n_pages && pd >= 0 && pd < p.n_pages;
-                src_row[i] = (((ps * p.H + h) << p.page_shift) + (int)(sp & (p.page_size - 1)));
-                dst_row[i] = (((pd * p.H + h) << p.page_shift) + (int)(dp & (p.page_size - 1)));
+                src_row[i] = (ps * p.H << p.page_shift) + (int)(sp & (p.page_size - 1));
+                dst_row[i] = (pd * p.H << p.page_shift) + (int)(dp & (p.page_size - 1));
             }
             if (!ok) bad = 1;
         }
@@ -194,35 +254,45 @@ __global__ void __launch_bounds__(kKeepThreads) k_kv_keep(KeepArgs p) {
         return;
     }
     if (tid == 0 && p.new_lens && blockIdx.y == 0) p.new_lens[b] = len + n;
+    if (n == 0) return;
+    const int all = p.layers * p.H, lh0 = (int)((long long)all * blockIdx.y / gridDim.y), lh1 = (int)((long long)all * (blockIdx.y + 1) / gridDim.y);
     const long long layer_rows = (long long)p.n_pages * p.H << p.page_shift;
-    const int words = n * 2 * p.row_words;
-    for (int w0 = 0; w0 < words; w0 += kKeepThreads * kKeepWords) {
-        uint2 v[kKeepWords];
+    // word `w` of the share: (layer, head), node, K or V, word of the row
+    const uint32_t of_node = 2 * p.row_words, of_head = n * of_node;
+    const uint64_t words = (uint64_t)(lh1 - lh0) * of_head;
+    for (uint64_t w0 = 0; w0 < words; w0 += kKeepThreads * kKeepWords) {
+        W v[kKeepWords];
+        W* to[kKeepWords];
 #pragma unroll
         for (int j = 0; j < kKeepWords; ++j) {
-            const int w = w0 + j * kKeepThreads + tid;
+            const uint64_t w = w0 + j * kKeepThreads + tid;
+            to[j] = nullptr;
             if (w < words) {
-                const int i = w / (2 * p.row_words), u = w % (2 * p.row_words), kv = u >= p.row_words;
-                v[j] = *reinterpret_cast<const uint2*>(p.pool[kv] + ((layer * layer_rows + src_row[i]) * p.row_words + u - kv * p.row_words) * 8);
+                const uint32_t lh = (uint32_t)w / of_head, rest = (uint32_t)w - lh * of_head, i = rest / of_node, u = rest - i * of_node;
+                const int kv = u >= (uint32_t)p.row_words, layer = (lh0 + (int)lh) / p.H, h = lh0 + (int)lh - layer * p.H;
+                if (src_row[i] != dst_row[i]) {
+                    const long long head = layer * layer_rows + ((long long)h << p.page_shift);
+                    W* pool = reinterpret_cast<W*>(p.pool[kv]) + (u - kv * p.row_words);
+                    v[j] = pool[(head + src_row[i]) * p.row_words];
+                    to[j] = pool + (head + dst_row[i]) * p.row_words;
+                }
             }
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kKeepWords; ++j) {
-            const int w = w0 + j * kKeepThreads + tid;
-            if (w < words) {
-                const int i = w / (2 * p.row_words), u = w % (2 * p.row_words), kv = u >= p.row_words;
-                *reinterpret_cast<uint2*>(p.pool[kv] + ((layer * layer_rows + dst_row[i]) * p.row_words + u - kv * p.row_words) * 8) = v[j];
-            }
-        }
+        for (int j = 0; j < kKeepWords; ++j)
+            if (to[j]) *to[j] = v[j];
     }
     if (p.scale[0]) {
-        for (int i0 = 0; i0 < 2 * n; i0 += kKeepThreads) {
-            const int i = i0 + tid;
+        const uint32_t bytes = (uint32_t)(lh1 - lh0) * 2 * n;
+        for (uint32_t w0 = 0; w0 < bytes; w0 += kKeepThreads) {
+            const uint32_t w = w0 + tid, lh = w / (2 * n), rest = w - lh * 2 * n, i = rest >> 1;
+            const int layer = (lh0 + (int)lh) / p.H, h = lh0 + (int)lh - layer * p.H;
+            const long long head = layer * layer_rows + ((long long)h << p.page_shift);
             uint8_t v = 0;
-            if (i < 2 * n) v = p.scale[i & 1][layer * layer_rows + src_row[i >> 1]];
+            if (w < bytes) v = p.scale[rest & 1][head + src_row[i]];
             __syncthreads();
-            if (i < 2 * n) p.scale[i & 1][layer * layer_rows + dst_row[i >> 1]] = v;
+            if (w < bytes) p.scale[rest & 1][head + dst_row[i]] = v;
         }
     }
 }
@@ -281,24 +351,24 @@ RowArgs row_args(const ace_kv* kv, int layer, const int64_t* slots, int T) {
     return p;
 }
 
-int row_grid(const ace_kv* kv, long long rows, int per_block) {
-    const long long want = (rows + per_block - 1) / per_block, most = 8LL * kv->num_sms;
-    return (int)(want < most ? want : most);
-}
+// Blocks for all rows, `groups` groups of lanes a block.
+unsigned row_grid(uint32_t rows, int groups) { return (rows + groups * kRowTurns - 1) / (groups * kRowTurns); }
 
 template <typename T, bool FP8, bool ALIGNED>
-void write_rows(const ace_kv* kv, const RowArgs& p, cudaStream_t s) {
-    if (p.D <= 64) k_kv_write<T, FP8, ALIGNED, 8><<<row_grid(kv, p.rows, 32), 256, 0, s>>>(p);
-    else if (p.D <= 128) k_kv_write<T, FP8, ALIGNED, 16><<<row_grid(kv, p.rows, 16), 256, 0, s>>>(p);
-    else k_kv_write<T, FP8, ALIGNED, 32><<<row_grid(kv, p.rows, 8), 256, 0, s>>>(p);
+void write_rows(const RowArgs& p, cudaStream_t s) {
+    if (p.D <= 64) k_kv_write<T, FP8, ALIGNED, 8><<<row_grid(p.rows, 32), 256, 0, s>>>(p);
+    else if (p.D <= 128) k_kv_write<T, FP8, ALIGNED, 16><<<row_grid(p.rows, 16), 256, 0, s>>>(p);
+    else k_kv_write<T, FP8, ALIGNED, 32><<<row_grid(p.rows, 8), 256, 0, s>>>(p);
 }
 
 template <typename T, bool FP8>
-void read_rows(const ace_kv* kv, const RowArgs& p, cudaStream_t s) {
-    if (p.D <= 64) k_kv_read<T, FP8, 8><<<row_grid(kv, p.rows, 32), 256, 0, s>>>(p);
-    else if (p.D <= 128) k_kv_read<T, FP8, 16><<<row_grid(kv, p.rows, 16), 256, 0, s>>>(p);
-    else k_kv_read<T, FP8, 32><<<row_grid(kv, p.rows, 8), 256, 0, s>>>(p);
+void read_rows(const RowArgs& p, cudaStream_t s) {
+    if (p.D <= 64) k_kv_read<T, FP8, 8><<<row_grid(p.rows, 32), 256, 0, s>>>(p);
+    else if (p.D <= 128) k_kv_read<T, FP8, 16><<<row_grid(p.rows, 16), 256, 0, s>>>(p);
+    else k_kv_read<T, FP8, 32><<<row_grid(p.rows, 8), 256, 0, s>>>(p);
 }
+
+constexpr long long kMaxRows = 1LL << 30;       // of a write or read call: row numbers are 32-bit
 
 bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 
@@ -395,7 +465,8 @@ ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_
     kv->last_stream = s;
     if (T == 0) return ACE_OK;
     RowArgs p = row_args(kv, layer, slots, T);
-    p.rows = 2LL * T * p.H;
+    if (2LL * T * p.H > kMaxRows) return kv_fail(ACE_ERR_UNSUPPORTED, "a call writes at most 2^30 rows (2 T n_kv_heads)");
+    p.rows = 2u * T * p.H;
     p.src[0] = k;
     p.src[1] = v;
     p.token_stride[0] = k_token_stride;
@@ -408,11 +479,11 @@ ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_
                     v_token_stride % vec == 0 && v_head_stride % vec == 0;
     const bool fp8 = kv->desc.format == ACE_KV_FP8;
     if (kv->desc.dtype == ACE_BF16) {
-        if (fp8) al ? write_rows<__nv_bfloat16, true, true>(kv, p, s) : write_rows<__nv_bfloat16, true, false>(kv, p, s);
-        else al ? write_rows<__nv_bfloat16, false, true>(kv, p, s) : write_rows<__nv_bfloat16, false, false>(kv, p, s);
+        if (fp8) al ? write_rows<__nv_bfloat16, true, true>(p, s) : write_rows<__nv_bfloat16, true, false>(p, s);
+        else al ? write_rows<__nv_bfloat16, false, true>(p, s) : write_rows<__nv_bfloat16, false, false>(p, s);
     } else {
-        if (fp8) al ? write_rows<float, true, true>(kv, p, s) : write_rows<float, true, false>(kv, p, s);
-        else al ? write_rows<float, false, true>(kv, p, s) : write_rows<float, false, false>(kv, p, s);
+        if (fp8) al ? write_rows<float, true, true>(p, s) : write_rows<float, true, false>(p, s);
+        else al ? write_rows<float, false, true>(p, s) : write_rows<float, false, false>(p, s);
     }
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? ACE_OK : kv_cuda(e, "cache write launch");
@@ -428,12 +499,14 @@ ace_status ace_kv_read(ace_kv* kv, int layer, const int64_t* slots, int T, void*
     kv->last_stream = s;
     if (T == 0) return ACE_OK;
     RowArgs p = row_args(kv, layer < 0 ? 0 : layer, slots, T);
-    p.rows = 2LL * T * p.H * (layer < 0 ? kv->desc.layers : 1);
+    const long long rows = 2LL * T * p.H * (layer < 0 ? kv->desc.layers : 1);
+    if (rows > kMaxRows) return kv_fail(ACE_ERR_UNSUPPORTED, "a call reads at most 2^30 rows (2 T n_kv_heads layers)");
+    p.rows = (uint32_t)rows;
     p.dst[0] = k_out;
     p.dst[1] = v_out;
     const bool fp8 = kv->desc.format == ACE_KV_FP8;
-    if (kv->desc.dtype == ACE_BF16) fp8 ? read_rows<__nv_bfloat16, true>(kv, p, s) : read_rows<__nv_bfloat16, false>(kv, p, s);
-    else fp8 ? read_rows<float, true>(kv, p, s) : read_rows<float, false>(kv, p, s);
+    if (kv->desc.dtype == ACE_BF16) fp8 ? read_rows<__nv_bfloat16, true>(p, s) : read_rows<__nv_bfloat16, false>(p, s);
+    else fp8 ? read_rows<float, true>(p, s) : read_rows<float, false>(p, s);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? ACE_OK : kv_cuda(e, "cache read launch");
 }
@@ -462,14 +535,21 @@ ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, con
     p.max_pages = max_pages;
     p.max_nodes = max_nodes;
     p.H = D.n_kv_heads;
-    p.row_words = D.head_dim * (D.format == ACE_KV_FP8 ? 1 : kv->elem) / 8;
+    const int row_bytes = D.head_dim * (D.format == ACE_KV_FP8 ? 1 : kv->elem), word = row_bytes % 16 ? 8 : 16;
+    p.row_words = row_bytes / word;
     p.page_size = D.page_size;
     p.page_shift = r.page_shift;
     p.n_pages = D.n_pages;
     p.layers = D.layers;
     p.err = kv->err;
     p.new_lens = new_lens;
-    k_kv_keep<<<dim3(B, D.layers * D.n_kv_heads), kKeepThreads, 0, s>>>(p);
+    // about eight blocks an SM, or a block for every layer and head
+    const int all = D.layers * D.n_kv_heads;
+    long long shares = (8LL * kv->num_sms + B - 1) / B;
+    if (shares > all) shares = all;
+    const dim3 grid(B, (unsigned)shares);
+    if (word == 16) k_kv_keep<uint4><<<grid, kKeepThreads, 0, s>>>(p);
+    else k_kv_keep<uint2><<<grid, kKeepThreads, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? ACE_OK : kv_cuda(e, "cache keep launch");
 }
