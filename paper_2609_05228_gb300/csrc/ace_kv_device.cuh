@@ -202,67 +202,91 @@ __device__ __forceinline__ unsigned long long sees_word(const AttnArgs& a, int n
 }
 
 // Joins a unit's partial results: row r of the unit from the slots of CTAs first .. last, in that order, 4
-// dimensions a thread and turn. Every thread of a CTA calls it; all partial results must be visible. kJoin loads are
-// under way together: a unit of a long context is spread over many CTAs, and each load takes most of a microsecond.
-constexpr int kJoin = 4;
-
-template <typename T, int ROWS>
-__device__ void join_unit(const AttnArgs& a, const Segment& s, int tid, int threads) {
-    const int D = a.head_dim, quads = D / 4;
-    for (int idx = tid; idx < s.rows * quads; idx += threads) {
-        const int r = idx / quads, d = idx % quads * 4;
+// dimensions a thread and turn. Every thread of a CTA calls it; all partial results must be visible. ITEMS x PARTS
+// loads are under way together, each of which takes most of a microsecond: a unit with few rows has many parts (a
+// long context), one with many rows has work for all threads several times over.
+template <typename T, int ROWS, int ITEMS, int PARTS>
+__device__ __forceinline__ void join_items(const AttnArgs& a, const Segment& s, int tid, int threads) {
+    const int D = a.head_dim, quads = D / 4, items = s.rows * quads;
+    for (int i0 = tid; i0 < items; i0 += threads * ITEMS) {
         // partial results with the reference that they turn up with: they are rescaled as it grows
-        float M = -INFINITY, L = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c0 = s.first; c0 <= s.last; c0 += kJoin) {
-            float2 ml[kJoin];
-            float4 v[kJoin];
+        float M[ITEMS], L[ITEMS];
+        float4 o[ITEMS];
+        int r[ITEMS], d[ITEMS];
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) {
-                const int c = c0 + j;
-                ml[j] = make_float2(-INFINITY, 0.f);
-                v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (c <= s.last) {
-                    const long long slot = (long long)part_slot(c, s.first) * ROWS + r;
-                    ml[j] = __ldcg(&a.ws.part_ml[slot]);
-                    v[j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + slot * D + d));
+        for (int k = 0; k < ITEMS; ++k) {
+            M[k] = -INFINITY;
+            L[k] = 0.f;
+            o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            const int i = min(i0 + k * threads, items - 1);
+            r[k] = i / quads;
+            d[k] = (i - r[k] * quads) * 4;
+        }
+        for (int c0 = s.first; c0 <= s.last; c0 += PARTS) {
+            float2 ml[ITEMS][PARTS];
+            float4 v[ITEMS][PARTS];
+#pragma unroll
+            for (int j = 0; j < PARTS; ++j) {
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) {
+                    const int c = c0 + j;
+                    ml[k][j] = make_float2(-INFINITY, 0.f);
+                    v[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (c <= s.last) {
+                        const long long slot = (long long)part_slot(c, s.first) * ROWS + r[k];
+                        ml[k][j] = __ldcg(&a.ws.part_ml[slot]);
+                        v[k][j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + slot * D + d[k]));
+                    }
                 }
             }
-            float top = M;
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) top = fmaxf(top, ml[j].x);
-            const float ref = top == -INFINITY ? 0.f : top, back = exp2f(M - ref);
-            M = top;
-            L *= back;
-            o.x *= back;
-            o.y *= back;
-            o.z *= back;
-            o.w *= back;
+            for (int k = 0; k < ITEMS; ++k) {
+                float top = M[k];
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) {
-                const float f = exp2f(ml[j].x - ref);
-                L = fmaf(ml[j].y, f, L);
-                o.x = fmaf(v[j].x, f, o.x);
-                o.y = fmaf(v[j].y, f, o.y);
-                o.z = fmaf(v[j].z, f, o.z);
-                o.w = fmaf(v[j].w, f, o.w);
+                for (int j = 0; j < PARTS; ++j) top = fmaxf(top, ml[k][j].x);
+                const float ref = top == -INFINITY ? 0.f : top, back = exp2f(M[k] - ref);
+                M[k] = top;
+                L[k] *= back;
+                o[k].x *= back;
+                o[k].y *= back;
+                o[k].z *= back;
+                o[k].w *= back;
+#pragma unroll
+                for (int j = 0; j < PARTS; ++j) {
+                    const float f = exp2f(ml[k][j].x - ref);
+                    L[k] = fmaf(ml[k][j].y, f, L[k]);
+                    o[k].x = fmaf(v[k][j].x, f, o[k].x);
+                    o[k].y = fmaf(v[k][j].y, f, o[k].y);
+                    o[k].z = fmaf(v[k][j].z, f, o[k].z);
+                    o[k].w = fmaf(v[k][j].w, f, o[k].w);
+                }
             }
         }
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        const int row = s.row0 + r, node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
-        const long long at = (long long)node * a.n_heads + hq;
-        T* out = static_cast<T*>(a.out) + at * D + d;
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        } else {
-            __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
-            uint2 w;
-            w.x = *reinterpret_cast<uint32_t*>(&lo);
-            w.y = *reinterpret_cast<uint32_t*>(&hi);
-            *reinterpret_cast<uint2*>(out) = w;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            if (i0 + k * threads >= items) break;
+            const float inv = L[k] == 0.f ? 0.f : 1.f / L[k];
+            const int row = s.row0 + r[k], node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
+            const long long at = (long long)node * a.n_heads + hq;
+            T* out = static_cast<T*>(a.out) + at * D + d[k];
+            if constexpr (sizeof(T) == 4) {
+                *reinterpret_cast<float4*>(out) = make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv);
+            } else {
+                __nv_bfloat162 lo = __floats2bfloat162_rn(o[k].x * inv, o[k].y * inv), hi = __floats2bfloat162_rn(o[k].z * inv, o[k].w * inv);
+                uint2 w;
+                w.x = *reinterpret_cast<uint32_t*>(&lo);
+                w.y = *reinterpret_cast<uint32_t*>(&hi);
+                *reinterpret_cast<uint2*>(out) = w;
+            }
+            if (d[k] == 0 && a.lse) a.lse[at] = (M[k] + log2f(L[k])) * 0.69314718055994530942f;
         }
-        if (d == 0 && a.lse) a.lse[at] = (M + log2f(L)) * 0.69314718055994530942f;
     }
+}
+
+template <typename T, int ROWS>
+__device__ __forceinline__ void join_unit(const AttnArgs& a, const Segment& s, int tid, int threads) {
+    if (ROWS > 16 && s.rows * a.head_dim / 4 >= 2 * threads) join_items<T, ROWS, 4, 2>(a, s, tid, threads);
+    else join_items<T, ROWS, 1, 8>(a, s, tid, threads);
 }
 
 // One thread, after all of the CTA's partial results are visible on the device: true in the last CTA of the unit.
