@@ -1,5 +1,5 @@
 // ace_attn_few.cu — attention for trees of drafted tokens on the tensor cores where a unit has few query rows
-// (nodes times query heads a kv head at most 16 or 32: decode steps and small trees, bound by the cache's bytes).
+// (nodes times query heads a kv head at most 32: decode steps and small trees, bound by the cache's bytes).
 // The products are turned round, so that the 128 rows of a tcgen05.mma are positions of the cache and not mostly
 // empty query rows:
 //   S^T = K Q^T        128 positions x NR rows
@@ -20,19 +20,20 @@ namespace {
 
 constexpr float kNone = -1e30f;         // reference of a row that has seen nothing: any score passes it
 
-template <bool FP8, int D, int NR>
+template <bool FP8, int D, int NR, int RG>
 struct FewCfg {
     static constexpr int ROW = D * (FP8 ? 1 : 2);               // bytes of a cached row
     static constexpr int TILE = 128 * ROW;
-    static constexpr int Q = NR * D * 2;                        // bf16, or two e4m3 terms
+    static constexpr int ROWS = NR * RG;                        // of a unit
+    static constexpr int Q = NR * D * 2;                        // a group's rows: bf16, or two e4m3 terms
     static constexpr int TERMS = FP8 ? 4 : 1;
     static constexpr int PIECES = TERMS * NR * (FP8 ? 1 : 2) / 16;      // 16-byte pieces of a position's row of P^T
     static constexpr int P = PIECES * 128 * 16;                 // one group's P^T
-    static constexpr int NK = D == 64 ? 6 : FP8 ? 5 : 3, NV = NK;
+    static constexpr int NK = D == 64 ? 6 : FP8 ? 5 : 3, NV = !FP8 && D == 128 && RG == 2 ? 2 : NK;
     static constexpr int OFF_K = 0;
     static constexpr int OFF_V = OFF_K + NK * TILE;
     static constexpr int OFF_Q = OFF_V + NV * TILE;             // 1024-byte multiples up to here
-    static constexpr int OFF_P = OFF_Q + Q;
+    static constexpr int OFF_P = OFF_Q + RG * Q;
     static constexpr int OFF_MISC = OFF_P + 2 * P;
     // fp8: q's terms and the weights' terms lie side by side along N, so that a product reads K and V once; their results
     // are added when they are read
@@ -41,12 +42,12 @@ struct FewCfg {
     static_assert(2 * (SN + ON) <= (int)COLS && (COLS & (COLS - 1)) == 0, "a power of two");
 };
 
-template <bool FP8, int NR>
+template <bool FP8, int NR, int RG>
 struct FewShared : TcShared {
     uint64_t s_free[2];
     float4 kf[FP8 ? kAuxRing : 1][32], vf[FP8 ? kAuxRing : 1][32];
-    float f_row[2][NR];                 // q's scale times the softmax's, by turns of segments
-    int node[2][NR];                    // row's node of the request
+    float f_row[2][NR * RG];            // q's scale times the softmax's, by turns of segments
+    int node[2][NR * RG];               // row's node of the request
     float ref[2][2][NR];                // [group][turn]
     float top[2][4][NR];                // [group][warp]: maxima of a tile's scores
     float sum[2][4][NR];                // end: sums of weights
@@ -55,10 +56,11 @@ struct FewShared : TcShared {
     int eref_end[2];
 };
 
-template <bool FP8, int D, int NR>
-constexpr int few_smem() { return 1024 + FewCfg<FP8, D, NR>::OFF_MISC + (int)sizeof(FewShared<FP8, NR>); }
+template <bool FP8, int D, int NR, int RG>
+constexpr int few_smem() { return 1024 + FewCfg<FP8, D, NR, RG>::OFF_MISC + (int)sizeof(FewShared<FP8, NR, RG>); }
 
-static_assert(few_smem<false, 128, 32>() <= 232448 && few_smem<true, 128, 32>() <= 232448, "shared memory");
+static_assert(few_smem<false, 128, 16, 1>() <= 232448 && few_smem<true, 128, 16, 1>() <= 232448, "shared memory");
+static_assert(few_smem<false, 128, 16, 2>() <= 232448 && few_smem<true, 128, 16, 2>() <= 232448, "shared memory");
 
 // D = A B with A and B in shared memory, operands' descriptors apart.
 template <bool F8>
@@ -148,13 +150,14 @@ __device__ __forceinline__ bool meet_or(int id, int threads, bool x) {
     return r != 0;
 }
 
-template <bool FP8, int D, int NR>
+// RG = 1: the two groups take even and odd tiles of all NR rows; RG = 2: each takes half of 2 NR rows of every tile.
+template <bool FP8, int D, int NR, int RG>
 __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constant__ TcAttnArgs p) {
-    using C = FewCfg<FP8, D, NR>;
+    using C = FewCfg<FP8, D, NR, RG>;
     constexpr int NK = C::NK, NV = C::NV;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    using M = FewShared<FP8, NR>;
+    using M = FewShared<FP8, NR, RG>;
     M& m = *reinterpret_cast<M*>(smem + C::OFF_MISC);
     const AttnArgs& a = p.a;
     volatile int* abort_flag = &m.abort_flag;
@@ -177,7 +180,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
         }
         for (int i = 0; i < kAuxRing; ++i) {
             mbar_init(&m.aux_full[i], 1);
-            mbar_init(&m.aux_empty[i], 4);
+            mbar_init(&m.aux_empty[i], 4 * RG);
         }
         m.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -193,7 +196,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
     Walk walk{m, a, {}};
 
     if (warp == 3) {
-        role_schedule<NR>(m, a);
+        role_schedule<C::ROWS>(m, a);
     } else if (warp == 0) {
         role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V);
     } else if (warp == 2) {
@@ -211,39 +214,43 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             while (true) {
                 if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
                 if (!m.seg[walk.seg.i].go) break;
-                const int tiles = m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0;
+                const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * RG;
                 mbar_arrive(&m.seg_empty[walk.seg.i]);
                 walk.seg.next<kSegRing>();
                 if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
                 q_phase ^= 1u;
-                for (int i = 0; i < tiles + 2; ++i) {
-                    if (i < tiles) {
+                for (int i = 0; i < items + 2; ++i) {
+                    if (i < items) {
+                        const bool last = RG == 1 || (i & 1);
+                        const uint32_t ql = q0 + (RG == 2 ? (uint32_t)((i & 1) * (C::Q >> 4)) : 0u);
                         // S^T of group i & 1, once the group has read its scores of two tiles ago
                         if (!mbar_wait_or_abort(&m.s_free[i & 1], f_phase >> (i & 1) & 1u, a.err, abort_flag)) { ok = false; break; }
                         f_phase ^= 1u << (i & 1);
-                        if (!mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
+                        if ((RG == 1 || !(i & 1)) && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
                         const uint32_t d = tmem + C::S + (uint32_t)((i & 1) * C::SN), kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4));
                         if constexpr (FP8) {
 #pragma unroll
                             for (int kk = 0; kk < D / 32; ++kk)
-                                mma_few<true>(d, kl + 2 * kk, kHi, q0 + 2 * kk, kHi, few_idesc(0, 0, 128, C::SN, false, false), kk > 0);
+                                mma_few<true>(d, kl + 2 * kk, kHi, ql + 2 * kk, kHi, few_idesc(0, 0, 128, C::SN, false, false), kk > 0);
                         } else {
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk)
-                                mma_few<false>(d, kl + (kk >> 2) * (16384 >> 4) + (kk & 3) * 2, kHi, q0 + (kk >> 2) * (NR * 128 >> 4) + (kk & 3) * 2,
+                                mma_few<false>(d, kl + (kk >> 2) * (16384 >> 4) + (kk & 3) * 2, kHi, ql + (kk >> 2) * (NR * 128 >> 4) + (kk & 3) * 2,
                                                kHi, few_idesc(1, 1, 128, NR, false, false), kk > 0);
                         }
                         mma_commit(&m.s_full[i & 1]);
-                        mma_commit(&m.k_empty[rk.i]);
-                        rk.next<NK>();
-                        if (i == tiles - 1) mma_commit(&m.q_free);
+                        if (last) {
+                            mma_commit(&m.k_empty[rk.i]);
+                            rk.next<NK>();
+                        }
+                        if (i == items - 1) mma_commit(&m.q_free);
                     }
                     if (i > 1) {
                         const int j = i - 2, g = j & 1;
                         if (!mbar_wait_or_abort(&m.p_ready[g], p_phase >> g & 1u, a.err, abort_flag)) { ok = false; break; }
                         p_phase ^= 1u << g;
-                        if (!mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                        if ((RG == 1 || g == 0) && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
                         const uint32_t d = tmem + C::O + (uint32_t)(g * C::ON), vl = v0 + (uint32_t)(rv.i * (C::TILE >> 4));
                         const uint32_t pl = p0 + (uint32_t)(g * (C::P >> 4));
@@ -257,8 +264,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                                 mma_few<false>(d, vl + kk * 128, kRows128, pl + kk * 16, kPHi, few_idesc(1, 1, D, NR, true, true), j >= 2 || kk > 0);
                         }
                         mma_commit(&m.o_done[g]);
-                        mma_commit(&m.v_empty[rv.i]);
-                        rv.next<NV>();
+                        if (RG == 1 || g == 1) {
+                            mma_commit(&m.v_empty[rv.i]);
+                            rv.next<NV>();
+                        }
                     }
                 }
                 if (!ok) break;
@@ -281,7 +290,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             const Segment& s = walk.segment();
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             const float f_row0 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
-            constexpr int kChunks = D / 8, kStep = 128 / kChunks, kTurns = NR > kStep ? NR / kStep : 1;
+            constexpr int kChunks = D / 8, kStep = 128 / kChunks, kTurns = C::ROWS > kStep ? C::ROWS / kStep : 1;
             uint4 qv[kTurns];
 #pragma unroll
             for (int j = 0; j < kTurns; ++j) {
@@ -291,10 +300,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             // the rows are under way while the last products with the segment before read its q
             if (!mbar_wait_warp(&m.q_free, q_phase, a.err, abort_flag)) { ok = false; break; }
             q_phase ^= 1u;
-            unsigned char* tile = smem + C::OFF_Q;
 #pragma unroll 1
             for (int j = 0; j < kTurns; ++j) {
-                const int r = j * kStep + tid / kChunks, c = tid % kChunks;
+                const int r = j * kStep + tid / kChunks, c = tid % kChunks, rr = r % NR;
+                unsigned char* tile = smem + C::OFF_Q + r / NR * C::Q;
                 uint4 w0 = qv[0];
 #pragma unroll
                 for (int i = 1; i < kTurns; ++i)
@@ -307,7 +316,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     for (int i = 0; i < 8; ++i) f[i] = finite_or_nan(f[i] * q_mul), amax = fmaxf(amax, fabsf(f[i]));
 #pragma unroll
                     for (int o = kChunks / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                    if (kStep > NR && r >= NR) continue;
+                    if (kStep > C::ROWS && r >= C::ROWS) continue;
                     const int byte = e4m3_scale_byte(amax);
                     const float mul = pow2_of_minus_byte(byte);
                     uint32_t hi[4], lo[4];
@@ -319,7 +328,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
                         lo[i] = e4m3x2(x - back.x, y - back.y);
                     }
-                    const int off = raw_v_offset<D>(r, c >> 1) + (c & 1) * 8;
+                    const int off = raw_v_offset<D>(rr, c >> 1) + (c & 1) * 8;
                     *reinterpret_cast<uint2*>(tile + off) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
                     *reinterpret_cast<uint2*>(tile + C::Q / 2 + off) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
                     if (c == 0) m.f_row[walk.seg.i & 1][r] = fmaxf(f_row0 * pow2_of_byte(byte), 0x1p-126f);   // 0 times a masked -inf is no score
@@ -330,7 +339,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
                         w[i] = *reinterpret_cast<const uint32_t*>(&v);
                     }
-                    *reinterpret_cast<uint4*>(tile + (c >> 3) * (NR * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4*>(tile + (c >> 3) * (NR * 128) + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                     if (c == 0) m.f_row[walk.seg.i & 1][r] = f_row0;
                 }
                 if (c == 0) m.node[walk.seg.i & 1][r] = r < s.rows ? (s.row0 + r) / a.group : 0;
@@ -374,14 +383,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             if (meet_or(3, 256, none || dead)) break;
             const Segment& s = walk.segment();
             const int tiles = s.tile1 - s.tile0, total = s.len + s.n;
-            const float* f_row = m.f_row[walk.seg.i & 1];
+            constexpr int kPer = RG == 2 ? NR : 0;          // first row of group g: g * kPer
+            const float* f_row = m.f_row[walk.seg.i & 1] + g * kPer;
+            const int* nodes = m.node[walk.seg.i & 1] + g * kPer;
             float l[NR];
 #pragma unroll
             for (int r = 0; r < NR; ++r) l[r] = 0.f;
             int eref = 0, turn = 0;     // turn: which half of ref and flag holds
             int mine = 0;
             for (int t = 0; t < tiles; ++t) {
-                if ((t & 1) != g) {
+                if (RG == 1 && (t & 1) != g) {
                     if (FP8) ra.next<kAuxRing>();
                     continue;
                 }
@@ -423,7 +434,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     const int nd = pos - s.len;
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
-                        const bool sees = pos < total && (sees_word(a, s.node0, s.n, m.node[walk.seg.i & 1][r], nd >> 6) >> (nd & 63) & 1);
+                        const bool sees = pos < total && (sees_word(a, s.node0, s.n, nodes[r], nd >> 6) >> (nd & 63) & 1);
                         if (!sees) x[r] = -INFINITY;
                     }
                 }
@@ -566,68 +577,73 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 if (key < NR) m.ref_end[g][key] = mine ? m.ref[g][turn][key] : kNone;
                 if (key == 0) m.eref_end[g] = eref;
             }
-            meet(3, 256);
+            if (RG == 1) meet(3, 256);
+            else meet(1 + g, 128);
             const bool whole = s.part < 0;
             const unsigned long long* bad = m.seg[walk.seg.i].bad;
             const bool any_bad = bad[0] | bad[1] | bad[2] | bad[3];
+            // RG = 1: half of the rows from both accumulators; RG = 2: the group's own rows from its own, half at a time
             constexpr int HALF = NR / 2;
-            const int r0 = g * HALF;
-            if (lane < HALF) {
-                const int r = r0 + lane;
-                const float x = m.ref_end[0][r], y = m.ref_end[1][r], top = fmaxf(x, y);
-                float u0 = exp2_approx(x - top), u1 = exp2_approx(y - top);
-                const float sum = ((m.sum[0][0][r] + m.sum[0][1][r]) + (m.sum[0][2][r] + m.sum[0][3][r])) * u0 +
-                                  ((m.sum[1][0][r] + m.sum[1][1][r]) + (m.sum[1][2][r] + m.sum[1][3][r])) * u1;
-                if (FP8) {
-                    u0 *= exp2f((float)(m.eref_end[0] - kVUp));
-                    u1 *= exp2f((float)(m.eref_end[1] - kVUp));
+            for (int pass = 0; pass < RG; ++pass) {
+                const int c0 = (RG == 1 ? g : pass) * HALF, r0 = g * kPer + c0;        // first column, first row of the unit
+                if (lane < HALF) {
+                    const int c = c0 + lane, r = r0 + lane, ga = RG == 1 ? 0 : g;
+                    const float x = m.ref_end[ga][c], y = RG == 1 ? m.ref_end[1][c] : kNone, top = fmaxf(x, y);
+                    float u0 = exp2_approx(x - top), u1 = RG == 1 ? exp2_approx(y - top) : 0.f;
+                    float sum = ((m.sum[ga][0][c] + m.sum[ga][1][c]) + (m.sum[ga][2][c] + m.sum[ga][3][c])) * u0;
+                    if (RG == 1) sum += ((m.sum[1][0][c] + m.sum[1][1][c]) + (m.sum[1][2][c] + m.sum[1][3][c])) * u1;
+                    if (FP8) {
+                        u0 *= exp2f((float)(m.eref_end[ga] - kVUp));
+                        if (RG == 1) u1 *= exp2f((float)(m.eref_end[1] - kVUp));
+                    }
+                    if (whole) {
+                        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                        u0 *= inv;
+                        u1 *= inv;
+                    }
+                    m.fac[warp - 4][lane] = make_float2(u0, u1);
+                    if (quad == 0 && r < s.rows) {
+                        const float ref = top == kNone ? -INFINITY : top;
+                        const int ur = s.row0 + r, nd = ur / a.group;
+                        if (!whole) a.ws.part_ml[(long long)s.part * C::ROWS + r] = make_float2(ref, sum);
+                        else if (a.lse) a.lse[(long long)(s.node0 + nd) * a.n_heads + s.head * a.group + ur - nd * a.group] = (ref + log2f(sum)) * 0.69314718055994530942f;
+                    }
                 }
-                if (whole) {
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    u0 *= inv;
-                    u1 *= inv;
-                }
-                m.fac[warp - 4][lane] = make_float2(u0, u1);
-                if (quad == 0 && r < s.rows) {
-                    const float ref = top == kNone ? -INFINITY : top;
-                    const int ur = s.row0 + r, nd = ur / a.group;
-                    if (!whole) a.ws.part_ml[(long long)s.part * NR + r] = make_float2(ref, sum);
-                    else if (a.lse) a.lse[(long long)(s.node0 + nd) * a.n_heads + s.head * a.group + ur - nd * a.group] = (ref + log2f(sum)) * 0.69314718055994530942f;
-                }
-            }
-            __syncwarp();
-            {
+                __syncwarp();
                 // D = 64: an accumulator of 64 rows lies in the first 16 lanes of each warp's 32
                 const int d = D == 128 ? key : quad * 16 + lane;
                 const bool in = D == 128 || lane < 16;
+                const bool both = RG == 1 && tiles > 1;
                 float o0[HALF], o1[HALF];
-                sum_terms<C::TERMS, NR, HALF>(tmem + lanes + C::O + (uint32_t)r0, o0);
-                if (tiles > 1) sum_terms<C::TERMS, NR, HALF>(tmem + lanes + C::O + (uint32_t)(C::ON + r0), o1);
+                sum_terms<C::TERMS, NR, HALF>(tmem + lanes + C::O + (uint32_t)((RG == 1 ? 0 : g * C::ON) + c0), o0);
+                if (both) sum_terms<C::TERMS, NR, HALF>(tmem + lanes + C::O + (uint32_t)(C::ON + c0), o1);
+                tmem_ld_wait();
 #pragma unroll
                 for (int i = 0; i < HALF; ++i) {
                     const int r = r0 + i;
                     if (r >= s.rows) break;
                     const float2 f = m.fac[warp - 4][i];
                     float o = f.x == 0.f ? 0.f : o0[i] * f.x;
-                    if (tiles > 1 && f.y != 0.f) o += o1[i] * f.y;
+                    if (both && f.y != 0.f) o += o1[i] * f.y;
                     if (in) {
-                        const int hq = s.head * a.group + (s.row0 + r) - m.node[walk.seg.i & 1][r] * a.group;
-                        if (whole) static_cast<__nv_bfloat16*>(a.out)[((long long)(s.node0 + m.node[walk.seg.i & 1][r]) * a.n_heads + hq) * D + d] = from_f32<__nv_bfloat16>(o);
-                        else a.ws.part_o[((long long)s.part * NR + r) * D + d] = o;
+                        const int nd = nodes[r - g * kPer], hq = s.head * a.group + (s.row0 + r) - nd * a.group;
+                        if (whole) static_cast<__nv_bfloat16*>(a.out)[((long long)(s.node0 + nd) * a.n_heads + hq) * D + d] = from_f32<__nv_bfloat16>(o);
+                        else a.ws.part_o[((long long)s.part * C::ROWS + r) * D + d] = o;
                     }
                 }
                 if (any_bad && in)
-                    for (int r = r0; r < min(r0 + HALF, s.rows); ++r) add_not_finite<FP8, NR>(a, s, bad, r, d, 1);
+                    for (int r = r0; r < min(r0 + HALF, s.rows); ++r) add_not_finite<FP8, C::ROWS>(a, s, bad, r, d, 1);
+                __syncwarp();
             }
             tc_fence_before();
             if (!whole) __threadfence();
-            meet(3, 256);               // O may be overwritten, partial results are written
+            if (RG == 1 || !whole) meet(3, 256);        // O may be overwritten, partial results are written
             if (!whole) {
                 if (tid == 0) m.joins = last_of_unit(a, s);
                 meet(3, 256);
                 if (m.joins) {
                     __threadfence();
-                    join_unit<__nv_bfloat16, NR>(a, s, tid, 256);
+                    join_unit<__nv_bfloat16, C::ROWS>(a, s, tid, 256);
                 }
             }
             walk.done();
@@ -639,30 +655,35 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::COLS));
 }
 
+template <bool FP8, int D, int NR, int RG>
+cudaError_t few_attr() {
+    return raise_smem_limit(k_attn_few<FP8, D, NR, RG>, few_smem<FP8, D, NR, RG>());
+}
+
 template <bool FP8, int D>
 cudaError_t few_attrs() {
-    cudaError_t e = cudaSuccess;
-    if constexpr (FP8) e = raise_smem_limit(k_attn_few<FP8, D, 8>, few_smem<FP8, D, 8>());
-    if (e == cudaSuccess) e = raise_smem_limit(k_attn_few<FP8, D, 16>, few_smem<FP8, D, 16>());
-    return e == cudaSuccess ? raise_smem_limit(k_attn_few<FP8, D, 32>, few_smem<FP8, D, 32>()) : e;
+    cudaError_t e = few_attr<FP8, D, 16, 1>();
+    if constexpr (FP8)
+        if (e == cudaSuccess) e = few_attr<FP8, D, 8, 1>();
+    return e == cudaSuccess ? few_attr<FP8, D, 16, 2>() : e;
+}
+
+template <bool FP8, int D, int NR, int RG>
+cudaError_t few_run(const TcAttnArgs& p, int ctas, cudaStream_t s) {
+    k_attn_few<FP8, D, NR, RG><<<ctas, kTcThreads, few_smem<FP8, D, NR, RG>(), s>>>(p);
+    return cudaGetLastError();
 }
 
 template <bool FP8, int D>
 cudaError_t few_go(const TcAttnArgs& p, int ctas, cudaStream_t s) {
     // NR by the rows of the largest tree; 8 are too few for plain caches (M = 128 wants N a multiple of 16, which two terms of
-    // an fp8 q make of them), whose larger tiles leave the softmax time enough
+    // an fp8 q make of them), whose larger tiles leave the softmax time enough. 32 rows a thread (and 64 a unit) were
+    // slower than ace_attn_tc.cu: their code and registers spill over (a unit of 40 rows 266 us, there 181)
     const long long rows = (long long)p.a.max_nodes * p.a.group;
-    if constexpr (FP8) {
-        if (rows <= 8) {
-            k_attn_few<FP8, D, 8><<<ctas, kTcThreads, few_smem<FP8, D, 8>(), s>>>(p);
-            return cudaGetLastError();
-        }
-    }
-    if (rows <= 16)
-        k_attn_few<FP8, D, 16><<<ctas, kTcThreads, few_smem<FP8, D, 16>(), s>>>(p);
-    else
-        k_attn_few<FP8, D, 32><<<ctas, kTcThreads, few_smem<FP8, D, 32>(), s>>>(p);
-    return cudaGetLastError();
+    if constexpr (FP8)
+        if (rows <= 8) return few_run<FP8, D, 8, 1>(p, ctas, s);
+    if (rows <= 16) return few_run<FP8, D, 16, 1>(p, ctas, s);
+    return few_run<FP8, D, 16, 2>(p, ctas, s);
 }
 
 }  // namespace
