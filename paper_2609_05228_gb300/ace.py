@@ -436,7 +436,6 @@ class AceKvCache:
         self.desc = ace_kv_desc(self.layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
                                 ACE_BF16 if dtype == "bf16" else ACE_F32, ACE_KV_FP8 if fmt == "fp8" else ACE_KV_PLAIN)
         with torch.cuda.device(self.k_pool.device):
-            torch.cuda.synchronize()
             self.handle = ace_kv_create(self.desc, self.k_pool, self.v_pool, self.k_scale, self.v_scale)
 
     def _rows(self, name, t, heads):

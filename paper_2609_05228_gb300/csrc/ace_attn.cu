@@ -222,11 +222,16 @@ cudaError_t attn_init(ace_kv* kv) {
         rows = kRows;
     }
     if (e != cudaSuccess) return e;
-    if ((e = cudaMalloc(&kv->ws.part_o, 2 * ctas * rows * D.head_dim * sizeof(float))) != cudaSuccess) return e;
-    if ((e = cudaMalloc(&kv->ws.part_ml, 2 * ctas * rows * sizeof(float2))) != cudaSuccess) return e;
-    if ((e = cudaMalloc(&kv->ws.ticket, ctas * sizeof(int))) != cudaSuccess) return e;
+    // error word, tickets, maxima and sums, outputs
+    const size_t head = (256 + ctas * sizeof(int) + 255) / 256 * 256, ml = (2 * ctas * rows * sizeof(float2) + 255) / 256 * 256;
+    if ((e = cudaMalloc(&kv->block, head + ml + 2 * ctas * rows * D.head_dim * sizeof(float))) != cudaSuccess) return e;
+    char* at = static_cast<char*>(kv->block);
+    kv->err = reinterpret_cast<int*>(at);
+    kv->ws.ticket = reinterpret_cast<int*>(at + 256);
+    kv->ws.part_ml = reinterpret_cast<float2*>(at + head);
+    kv->ws.part_o = reinterpret_cast<float*>(at + head + ml);
     kv->tickets = (int)ctas;
-    return cudaMemsetAsync(kv->ws.ticket, 0, ctas * sizeof(int), kv->last_stream);
+    return cudaMemsetAsync(at, 0, head, kv->last_stream);
 }
 
 cudaError_t launch_tree_attention(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {

@@ -46,8 +46,9 @@ template <bool FP8, int NR, int RG>
 struct FewShared : TcShared {
     uint64_t s_free[2];
     float4 kf[FP8 ? kAuxRing : 1][32], vf[FP8 ? kAuxRing : 1][32];
-    float f_row[2][NR * RG];            // q's scale times the softmax's, by turns of segments
-    int node[2][NR * RG];               // row's node of the request
+    // by segments of the ring: the next q rows may come while a segment's end still reads these
+    float f_row[kSegRing][NR * RG];     // q's scale times the softmax's
+    int node[kSegRing][NR * RG];        // row's node of the request
     float ref[2][2][NR];                // [group][turn]
     float top[2][4][NR];                // [group][warp]: maxima of a tile's scores
     float sum[2][4][NR];                // end: sums of weights
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     const int off = raw_v_offset<D>(rr, c >> 1) + (c & 1) * 8;
                     *reinterpret_cast<uint2*>(tile + off) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
                     *reinterpret_cast<uint2*>(tile + C::Q / 2 + off) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-                    if (c == 0) m.f_row[walk.seg.i & 1][r] = fmaxf(f_row0 * pow2_of_byte(byte), 0x1p-126f);   // 0 times a masked -inf is no score
+                    if (c == 0) m.f_row[walk.seg.i][r] = fmaxf(f_row0 * pow2_of_byte(byte), 0x1p-126f);   // 0 times a masked -inf is no score
                 } else {
                     uint32_t w[4];
 #pragma unroll
@@ -340,9 +341,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         w[i] = *reinterpret_cast<const uint32_t*>(&v);
                     }
                     *reinterpret_cast<uint4*>(tile + (c >> 3) * (NR * 128) + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                    if (c == 0) m.f_row[walk.seg.i & 1][r] = f_row0;
+                    if (c == 0) m.f_row[walk.seg.i][r] = f_row0;
                 }
-                if (c == 0) m.node[walk.seg.i & 1][r] = r < s.rows ? (s.row0 + r) / a.group : 0;
+                if (c == 0) m.node[walk.seg.i][r] = r < s.rows ? (s.row0 + r) / a.group : 0;
             }
             fence_async_smem();
             __syncwarp();
@@ -384,8 +385,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             const Segment& s = walk.segment();
             const int tiles = s.tile1 - s.tile0, total = s.len + s.n;
             constexpr int kPer = RG == 2 ? NR : 0;          // first row of group g: g * kPer
-            const float* f_row = m.f_row[walk.seg.i & 1] + g * kPer;
-            const int* nodes = m.node[walk.seg.i & 1] + g * kPer;
+            const float* f_row = m.f_row[walk.seg.i] + g * kPer;
+            const int* nodes = m.node[walk.seg.i] + g * kPer;
             float l[NR];
 #pragma unroll
             for (int r = 0; r < NR; ++r) l[r] = 0.f;

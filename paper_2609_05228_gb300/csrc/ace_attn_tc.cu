@@ -14,6 +14,8 @@
 // hold 8 significant bits, all of a bf16 q (elements 2^-10 and more below the row's largest lose their last bits, a
 // 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory (exact), with
 // their scales on P: P V accumulates in units of 2^eref, a power of two above the scales seen so far.
+#include <cudaTypedefs.h>
+
 #include "ace_attn_tc.cuh"
 
 namespace ace {
@@ -40,7 +42,7 @@ struct Misc : TcShared {
     uint64_t c_empty[2];
     float2 ml[RT == 1 ? 256 : 1];               // RT = 1: both halves' running maximum and sum
     int eref1[RT == 1 ? 2 : 1];
-    float q_scale[2][FP8 ? 128 * RT : 1];       // by turns of segments: softmax may be one behind
+    float q_scale[kSegRing][FP8 ? 128 * RT : 1];        // by segments of the ring: softmax may be behind
     float4 kf[FP8 ? kAuxRing : 1][32];          // 128 factors a tile
     uint2 vf[FP8 ? kAuxRing : 1][32];           // the same as fp16
 };
@@ -366,7 +368,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                             *reinterpret_cast<uint2*>(tile + off + (c & 1) * 8) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
                             *reinterpret_cast<uint2*>(tile + C::Q / 2 + off + (c & 1) * 8) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
                         }
-                        if (c == 0) m.q_scale[walk.seg.i & 1][r] = pow2_of_byte(byte);
+                        if (c == 0) m.q_scale[walk.seg.i][r] = pow2_of_byte(byte);
                     } else {
                         if (r >= s.rows) continue;
                         uint32_t w[4];
@@ -503,7 +505,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 if (warp_live) {
                     const float4* kf = m.kf[FP8 ? ra.i : 0];
                     if (FP8) {
-                        if (!mine) f_row = fmaxf(f_row0 * m.q_scale[walk.seg.i & 1][row], 0x1p-126f);    // 0 times a masked -inf is no score
+                        if (!mine) f_row = fmaxf(f_row0 * m.q_scale[walk.seg.i][row], 0x1p-126f);    // 0 times a masked -inf is no score
                         const int e = m.eref[ra.i];
                         if (mine && e > eref) st.o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
                         eref = e;
@@ -714,6 +716,24 @@ cudaError_t tc_launch(const TcAttnArgs& p, int ctas, cudaStream_t s) {
 
 }  // namespace
 
+// 2-D map of a pool's rows of `row` bytes, boxes of box_rows x at most 128 bytes (plain rows: 64 bf16).
+static cudaError_t row_map(CUtensorMap* m, const void* base, uint64_t rows, bool fp8, uint32_t head_dim, uint32_t box_rows) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+    if (e != cudaSuccess) return e;
+    if (q != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {head_dim, rows};
+    const cuuint64_t strides[1] = {head_dim * (fp8 ? 1u : 2u)};
+    const cuuint32_t box[2] = {fp8 ? head_dim : 64u, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn)(
+        m, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, fp8 && head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 bool attn_tc_supported(const ace_kv* kv) {
     return kv->desc.dtype == ACE_BF16 && (kv->desc.head_dim == 64 || kv->desc.head_dim == 128);
 }
@@ -725,14 +745,9 @@ cudaError_t attn_tc_init(ace_kv* kv) {
     const uint32_t box = D.page_size < kTcKeys ? D.page_size : kTcKeys;
     cudaError_t e = attn_few_init(kv);
     if (e != cudaSuccess) return e;
-    if (fp8) {
-        const int swizzle = D.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
-        if ((e = make_byte_map(&kv->maps.k, kv->k_pool, rows, D.head_dim, box, swizzle)) != cudaSuccess) return e;
-        if ((e = make_byte_map(&kv->maps.v, kv->v_pool, rows, D.head_dim, box, swizzle)) != cudaSuccess) return e;
-        return D.head_dim == 128 ? tc_attrs<true, 128>() : tc_attrs<true, 64>();
-    }
-    if ((e = make_tensor_map(&kv->maps.k, kv->k_pool, rows, D.head_dim, box, true)) != cudaSuccess) return e;
-    if ((e = make_tensor_map(&kv->maps.v, kv->v_pool, rows, D.head_dim, box, true)) != cudaSuccess) return e;
+    if ((e = row_map(&kv->maps.k, kv->k_pool, rows, fp8, D.head_dim, box)) != cudaSuccess) return e;
+    if ((e = row_map(&kv->maps.v, kv->v_pool, rows, fp8, D.head_dim, box)) != cudaSuccess) return e;
+    if (fp8) return D.head_dim == 128 ? tc_attrs<true, 128>() : tc_attrs<true, 64>();
     return D.head_dim == 128 ? tc_attrs<false, 128>() : tc_attrs<false, 64>();
 }
 

@@ -410,8 +410,6 @@ ace_status ace_kv_create(const ace_kv_desc* desc, void* k_pool, void* v_pool, vo
     kv->last_stream = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaGetDevice(&kv->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, kv->device);
-    if (e == cudaSuccess) e = cudaMalloc(&kv->err, 16);
-    if (e == cudaSuccess) e = cudaMemsetAsync(kv->err, 0, 16, kv->last_stream);
     if (e == cudaSuccess) e = attn_init(kv);
     if (e == cudaSuccess) e = cudaStreamSynchronize(kv->last_stream);
     if (e != cudaSuccess) {
@@ -429,9 +427,7 @@ ace_status ace_kv_create(const ace_kv_desc* desc, void* k_pool, void* v_pool, vo
 void ace_kv_destroy(ace_kv* kv) {
     if (!kv) return;
     cudaDeviceSynchronize();
-    void* ptrs[] = {kv->err, kv->ws.part_o, kv->ws.part_ml, kv->ws.ticket};
-    for (void* p : ptrs)
-        if (p) cudaFree(p);
+    if (kv->block) cudaFree(kv->block);
     delete kv;
 }
 

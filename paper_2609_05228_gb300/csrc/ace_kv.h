@@ -36,6 +36,7 @@ struct ace_kv {
     uint8_t* k_scale = nullptr;
     uint8_t* v_scale = nullptr;
     long long slots = 0;                // n_pages * page_size, per layer
+    void* block = nullptr;              // one allocation for what follows
     int* err = nullptr;
     ace::AttnWorkspace ws;
     int tickets = 0;
@@ -79,7 +80,4 @@ cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaSt
 constexpr int kFewRows = 32;
 cudaError_t attn_few_init(const ace_kv* kv);
 cudaError_t launch_attn_few(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
-// 2-D map of bytes [rows, cols], boxes of box_rows whole rows (ace_expert_tc.cu)
-cudaError_t make_byte_map(CUtensorMap* m, const void* base, uint64_t rows, uint32_t cols, uint32_t box_rows, int swizzle);
-
 }  // namespace ace
