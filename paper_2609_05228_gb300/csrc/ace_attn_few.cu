@@ -13,12 +13,14 @@
 // The rows' references lie in shared memory and move only where a score passes them by 2^kLazy (one barrier with an
 // "or" a tile). Two groups of four warps take even and odd tiles into accumulators of their own; a group's next
 // scores are computed as soon as it has read the last ones.
+#include <cfloat>
+
 #include "ace_attn_tc.cuh"
 
 namespace ace {
 namespace {
 
-constexpr float kNone = -1e30f;         // reference of a row that has seen nothing: any score passes it
+constexpr float kNone = -FLT_MAX;       // reference of a row that has seen nothing: any score passes it
 
 template <bool FP8, int D, int NR, int RG>
 struct FewCfg {
@@ -84,13 +86,11 @@ constexpr uint32_t few_idesc(int type_a, int type_b, int M, int N, bool a_mn, bo
            ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-// N columns of TMEM (4, 8, 16 or 32), not waited for.
+// N columns of TMEM (4, 8 or 16), not waited for.
 template <int N>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&x)[N]) {
     uint32_t* r = reinterpret_cast<uint32_t*>(x);
-    if constexpr (N == 32) {
-        tmem_ld32(taddr, *reinterpret_cast<uint32_t(*)[32]>(r));
-    } else if constexpr (N == 16) {
+    if constexpr (N == 16) {
         tmem_ld16(taddr, *reinterpret_cast<uint32_t(*)[16]>(r));
     } else if constexpr (N == 8) {
         asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : ACE_R8(r, 0) : "r"(taddr));
@@ -487,16 +487,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     }
                     if (mine) {
 #pragma unroll 1
-                        for (int c = 0; c < C::ON; c += NR < 16 ? 16 : NR) {
+                        for (int c = 0; c < C::ON; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o_t + c, o);
+                            tmem_ld_wait();
 #pragma unroll
-                            for (int r = 0; r < NR; r += 16) {
-                                uint32_t o[16];
-                                tmem_ld16(o_t + c + r, o);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f[(r + i) % NR]);
-                                tmem_st16(o_t + c + r, o);
-                            }
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f[i % NR]);
+                            tmem_st16(o_t + c, o);
                         }
                         tmem_st_wait();
                     }
@@ -509,56 +506,44 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                     wait(&m.o_done[g], o_phase);    // the product has read the P^T before
                     o_phase ^= 1u;
                 }
-                // weights, 16 (or 8) rows at a time; a 16-byte piece holds 16 e5m2 or 8 bf16 values along N = term * NR + row
-                constexpr int RB = NR < 16 ? NR : 16;
+                // weights; a 16-byte piece of P^T holds 16 e5m2 or 8 bf16 values along N = term * NR + row
+                uint32_t h[NR / 2];
 #pragma unroll
-                for (int b = 0; b < NR / RB; ++b) {
-                    uint32_t h[RB / 2];
+                for (int r = 0; r < NR; r += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(ref + r);
+                    float e[4] = {x[r] - f.x, x[r + 1] - f.y, x[r + 2] - f.z, x[r + 3] - f.w};
 #pragma unroll
-                    for (int i = 0; i < RB; i += 4) {
-                        const int r = RB * b + i;
-                        const float4 f = *reinterpret_cast<const float4*>(ref + r);
-                        float e[4] = {x[r] - f.x, x[r + 1] - f.y, x[r + 2] - f.z, x[r + 3] - f.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]), l[r + j] += e[j];
-                        if constexpr (FP8) {
-                            const __half2 p0 = __floats2half2_rn(e[0] * vf, e[1] * vf), p1 = __floats2half2_rn(e[2] * vf, e[3] * vf);
-                            h[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
-                            h[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
-                        } else {
-                            const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
-                            h[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
-                            h[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
-                        }
-                    }
+                    for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]), l[r + j] += e[j];
                     if constexpr (FP8) {
-                        uint32_t w[4][RB / 4];
+                        const __half2 p0 = __floats2half2_rn(e[0] * vf, e[1] * vf), p1 = __floats2half2_rn(e[2] * vf, e[3] * vf);
+                        h[r / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                        h[r / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+                    } else {
+                        const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
+                        h[r / 2] = *reinterpret_cast<const uint32_t*>(&p0);
+                        h[r / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+                    }
+                }
+                if constexpr (FP8) {
+                    uint32_t w[NR];             // NR / 4 words a term
 #pragma unroll
-                        for (int term = 0; term < 4; ++term) {
+                    for (int term = 0; term < 4; ++term) {
 #pragma unroll
-                            for (int i = 0; i < RB / 4; ++i) w[term][i] = __byte_perm(h[2 * i], h[2 * i + 1], 0x7531);
-                            if (term < 3) {
+                        for (int i = 0; i < NR / 4; ++i) w[term * (NR / 4) + i] = __byte_perm(h[2 * i], h[2 * i + 1], 0x7531);
+                        if (term < 3) {
 #pragma unroll
-                                for (int i = 0; i < RB / 2; ++i) {
-                                    const uint32_t top = h[i] & 0xff00ff00u;
-                                    const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&top));
-                                    h[i] = *reinterpret_cast<const uint32_t*>(&rest);
-                                }
+                            for (int i = 0; i < NR / 2; ++i) {
+                                const uint32_t top = h[i] & 0xff00ff00u;
+                                const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&top));
+                                h[i] = *reinterpret_cast<const uint32_t*>(&rest);
                             }
                         }
-                        if constexpr (NR == 8) {
-                            *reinterpret_cast<uint4*>(p_out) = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
-                            *reinterpret_cast<uint4*>(p_out + 2048) = make_uint4(w[2][0], w[2][1], w[3][0], w[3][1]);
-                        } else {
-#pragma unroll
-                            for (int term = 0; term < 4; ++term)
-                                *reinterpret_cast<uint4*>(p_out + (term * (NR / 16) + b) * 2048) =
-                                    make_uint4(w[term][0], w[term][1], w[term][RB / 4 - 2], w[term][RB / 4 - 1]);
-                        }
-                    } else {
-                        *reinterpret_cast<uint4*>(p_out + (2 * b) * 2048) = make_uint4(h[0], h[1], h[2], h[3]);
-                        *reinterpret_cast<uint4*>(p_out + (2 * b + 1) * 2048) = make_uint4(h[RB / 2 - 4], h[RB / 2 - 3], h[RB / 2 - 2], h[RB / 2 - 1]);
                     }
+#pragma unroll
+                    for (int i = 0; i < NR; i += 4) *reinterpret_cast<uint4*>(p_out + i / 4 * 2048) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NR / 2; i += 4) *reinterpret_cast<uint4*>(p_out + i / 4 * 2048) = make_uint4(h[i], h[i + 1], h[i + 2], h[i + 3]);
                 }
                 fence_async_smem();
                 tc_fence_before();

@@ -39,7 +39,7 @@ struct Cfg {
 
 template <bool FP8, int RT>
 struct Misc : TcShared {
-    uint64_t c_empty[2];
+    uint64_t c_empty[2], soft, group[2];
     float2 ml[RT == 1 ? 256 : 1];               // RT = 1: both halves' running maximum and sum
     int eref1[RT == 1 ? 2 : 1];
     float q_scale[kSegRing][FP8 ? 128 * RT : 1];        // by segments of the ring: softmax may be behind
@@ -153,14 +153,18 @@ __device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s
         if (!first) st.o_mul *= f;
     }
     const float shift = st.ref == -INFINITY ? 0.f : -st.ref;
-    if constexpr (N == 32) {
-        st.l += store_weights<FP8>(s_t + col / 2, x, f_row, shift);
-    } else {
+    // x f + shift in one operation is off by what `ref` lost in its rounding, nothing below 2^20; past that x f is rounded
+    // too (by rows: what a row gets must not depend on its neighbours)
+    const bool large = fabsf(shift) > 0x1p20f, any_large = __any_sync(0xffffffffu, large);
+    const float before = large ? f_row : 1.f, f = large ? 1.f : f_row;
 #pragma unroll 1
-        for (int c = col; c < col + N; c += 32) {
-            load_scores<FP8>(s_t + c, x, kf + c / 4, drafted, drafted ? sees32(a, s, node, pos0 + c) : 0u);
-            st.l += store_weights<FP8>(s_t + c / 2, x, f_row, shift);
+    for (int c = col; c < col + N; c += 32) {
+        load_scores<FP8>(s_t + c, x, kf + c / 4, drafted, drafted ? sees32(a, s, node, pos0 + c) : 0u);
+        if (any_large) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] *= before;
         }
+        st.l += store_weights<FP8>(s_t + c / 2, x, f, shift);
     }
     if constexpr (N < 128) {
         const uint32_t zero[16] = {};
@@ -178,8 +182,8 @@ __device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
     return *reinterpret_cast<const uint32_t*>(&z);
 }
 
-// CP: with few rows (RT = 1) the block holds them CP = 2 or 4 times, 64 or 32 lanes apart, and each copy's warps take that
-// share of a tile's columns: the tile's softmax takes as much less time, and the copies' O are added at the end.
+// CP = 2 (at most 64 rows): the block holds them twice, 64 lanes apart, and each copy's warps take half of a tile's
+// columns: the tile's softmax takes half the time, and the copies' O are added at the end.
 template <bool FP8, int D, int RT, int CP>
 __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant__ TcAttnArgs p) {
     using C = Cfg<FP8, D, RT, CP>;

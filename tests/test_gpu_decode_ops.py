@@ -368,6 +368,29 @@ def test_attention_sharp_and_wide_scores(fmt, dtype, D):
     s.check(*s.run(scale=-1.0), scale=-1.0)
 
 
+@pytest.mark.parametrize("size", [1e5, 1e17])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("fmt", ["fp8", "plain"])
+@pytest.mark.parametrize("nodes", [1, 3, 6, 15, 30, 50])
+def test_attention_equal_scores_of_any_size(fmt, nodes, sign, size):
+    """Rows of one key score alike however large the score, so the output is the mean of V: values of an eighth from 1 to 2
+    have exact codes and sums, and a weight's rounding is at most 2^-8 of it, as the output's."""
+    rng = np.random.default_rng(nodes)
+    H, G, D, page, length = 1, 4, 128, 16, 333
+    total = length + nodes
+    v = torch.from_numpy(1 + rng.integers(0, 8, (total, H, D)) / 8.0).bfloat16()
+    kv = ace.AceKvCache(H, D, page, 24, 1, "bf16", fmt)
+    kv.write(0, torch.full((total, H, D), size, dtype=torch.bfloat16, device="cuda"), v.cuda(), torch.arange(total, device="cuda"))
+    q = torch.full((nodes, H * G, D), sign * size, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    kv.attend(0, q, torch.arange(24, dtype=torch.int32, device="cuda")[None], torch.tensor([length], dtype=torch.int32, device="cuda"),
+              torch.tensor([0, nodes], dtype=torch.int32, device="cuda"), out, None, nodes)
+    kv.sync()
+    sums = v.double().numpy().cumsum(0)
+    want = np.stack([sums[length + i] / (length + i + 1) for i in range(nodes)])
+    assert (np.abs(out.double().cpu().numpy() - want) <= 2.0 ** -7 * want).all()
+
+
 def test_attention_sink_beside_many_small_weights():
     """A first key with weight e^12 of the others': 30000 weights of 6e-6 still sum to their share of the output."""
     L, D = 30000, 128
