@@ -7,9 +7,10 @@
 //   S = Q K^T              tcgen05.mma, 128 x 128 fp32 in TMEM
 //   P = 2^(S - m), l += P  softmax warps, a thread per row; P goes back to TMEM as bf16 / fp16
 //   O += P V               tcgen05.mma, A = P from TMEM, B = V as stored (its rows are K indices)
-// Two accumulators and two S buffers: with RT = 2 they belong to two blocks of 128 rows that share each
-// loaded tile; with RT = 1 to even and odd tiles of one block, joined at the end, so that the softmax
-// of one tile runs beside the products of the next either way.
+// In items of 64 positions, two groups of four softmax warps and two accumulators: with RT = 2 a group has a block of 128
+// rows, and both halves of each tile; with RT = 1 both have the same rows, and a half of each tile, joined at the end. A
+// group has two buffers of S, so that the products of one item run beside the softmax of the next: with whole tiles and
+// one buffer a group waited for its products half of the time (256 rows and 128 positions took 4400 cycles).
 // fp8 caches: K's codes are the B operand as stored (kind::f8f6f4), against q split into two e4m3 terms, which
 // hold 8 significant bits, all of a bf16 q (elements 2^-10 and more below the row's largest lose their last bits, a
 // 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory (exact), with
@@ -20,6 +21,8 @@
 
 namespace ace {
 namespace {
+
+constexpr int kHalf = 64;               // positions of an item
 
 template <bool FP8, int D, int RT, int CP>
 struct Cfg {
@@ -58,20 +61,13 @@ static_assert(tc_smem<false, 64, 2, 1>() <= 232448 && tc_smem<true, 64, 1, 2>() 
 // conversion overflow the instruction cache, and warps that run different roles then stall on fetches (a fp8 tile of
 // 128 rows 9600 cycles unrolled; no_instruction stalls 2.7 an issue against 0.5).
 
-// 32 of a row's scores from TMEM, with fp8 rows' scales, and -inf where the row does not see the position.
+// 32 of a row's scores with fp8 rows' scales, and -inf where the row does not see the position.
 template <bool FP8>
-__device__ __forceinline__ void load_scores(uint32_t s_t, float (&x)[32], const float4* kf, bool masked, uint32_t see) {
-    tmem_ld32(s_t, *reinterpret_cast<uint32_t(*)[32]>(&x));
-    float4 k[8];
-    if (FP8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) k[i] = kf[i];
-    }
-    tmem_ld_wait();
+__device__ __forceinline__ void finish_scores(float* x, const float4* kf, bool masked, uint32_t see) {
     if (FP8) {
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-            const float4 f = k[i / 4];
+            const float4 f = kf[i / 4];
             unpair(mul2(pair(x[i], x[i + 1]), pair(f.x, f.y)), x[i], x[i + 1]);
             unpair(mul2(pair(x[i + 2], x[i + 3]), pair(f.z, f.w)), x[i + 2], x[i + 3]);
         }
@@ -82,7 +78,7 @@ __device__ __forceinline__ void load_scores(uint32_t s_t, float (&x)[32], const 
     }
 }
 
-__device__ __forceinline__ float max32(const float (&x)[32]) {
+__device__ __forceinline__ float max32(const float* x) {
     float top[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
     for (int i = 4; i < 28; i += 8) {
@@ -96,7 +92,7 @@ __device__ __forceinline__ float max32(const float (&x)[32]) {
 
 // 32 weights 2^(x f + shift) to TMEM; returns their sum.
 template <bool FP8>
-__device__ __forceinline__ float store_weights(uint32_t p_t, const float (&x)[32], float f, float shift) {
+__device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, float f, float shift) {
     const uint64_t f2 = pair(f, f), shift2 = pair(shift, shift);
     uint64_t sum[2] = {0ull, 0ull};
     uint32_t w[16];
@@ -131,17 +127,20 @@ struct RowState {
     float ref, l, o_mul;                // reference, sum, what O has to be multiplied with
 };
 
-// One tile of a row: N scores from column `col` on become weights, over the scores that are read already; the row's other
-// columns of P are zero.
+// One item of a row: N scores from column `col` on become weights, over the scores that are read already; the row's other
+// columns of P (of the item's kHalf) are zero.
 template <bool FP8, int N>
-__device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s, uint32_t s_t, int col, const float4* kf, bool drafted,
+__device__ __forceinline__ void softmax_item(const AttnArgs& a, const Segment& s, uint32_t s_t, int col, const float4* kf, bool drafted,
                                              int node, int pos0, float f_row, bool first, RowState& st) {
-    float x[32];
+    float x[N];
+#pragma unroll
+    for (int c = 0; c < N; c += 32) tmem_ld32(s_t + col + c, *reinterpret_cast<uint32_t(*)[32]>(x + c));
+    tmem_ld_wait();
     float top = -INFINITY;
-#pragma unroll 1
-    for (int c = col; c < col + N; c += 32) {
-        load_scores<FP8>(s_t + c, x, kf + c / 4, drafted, drafted ? sees32(a, s, node, pos0 + c) : 0u);
-        top = fmaxf(top, max32(x));
+#pragma unroll
+    for (int c = 0; c < N; c += 32) {
+        finish_scores<FP8>(x + c, kf + (col + c) / 4, drafted, drafted ? sees32(a, s, node, pos0 + col + c) : 0u);
+        top = fmaxf(top, max32(x + c));
     }
     top = top == -INFINITY ? top : top * f_row;
     constexpr float kUp = FP8 ? (float)kPUp : 0.f;
@@ -157,20 +156,15 @@ __device__ __forceinline__ void softmax_tile(const AttnArgs& a, const Segment& s
     // too (by rows: what a row gets must not depend on its neighbours)
     const bool large = fabsf(shift) > 0x1p20f, any_large = __any_sync(0xffffffffu, large);
     const float before = large ? f_row : 1.f, f = large ? 1.f : f_row;
-#pragma unroll 1
-    for (int c = col; c < col + N; c += 32) {
-        load_scores<FP8>(s_t + c, x, kf + c / 4, drafted, drafted ? sees32(a, s, node, pos0 + c) : 0u);
-        if (any_large) {
+    if (any_large) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] *= before;
-        }
-        st.l += store_weights<FP8>(s_t + c / 2, x, f, shift);
+        for (int i = 0; i < N; ++i) x[i] *= before;
     }
-    if constexpr (N < 128) {
-        const uint32_t zero[16] = {};
 #pragma unroll
-        for (int c = 0; c < 64; c += 16)
-            if (c < col / 2 || c >= col / 2 + N / 2) tmem_st16(s_t + c, zero);
+    for (int c = 0; c < N; c += 32) st.l += store_weights<FP8>(s_t + (col + c) / 2, x + c, f, shift);
+    if constexpr (N < kHalf) {
+        const uint32_t zero[16] = {};
+        tmem_st16(s_t + 16 - col / 2, zero);
     }
     tmem_st_wait();
 }
@@ -199,10 +193,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         for (int i = 0; i < NK; ++i) mbar_init(&m.k_full[i], 1), mbar_init(&m.k_empty[i], 1);
         for (int i = 0; i < NV; ++i) mbar_init(&m.v_full[i], 1), mbar_init(&m.v_empty[i], FP8 ? 4 : 1);
         for (int i = 0; i < (FP8 ? NC : NV); ++i) mbar_init(&m.v_ready[i], 4);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&m.c_empty[i], 1);
+        for (int i = 0; i < 4; ++i) {
             mbar_init(&m.s_full[i], 1);
             mbar_init(&m.p_ready[i], 4);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&m.c_empty[i], 1);
             mbar_init(&m.o_done[i], 1);
         }
         mbar_init(&m.q_full, 4);
@@ -216,7 +212,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         }
         for (int i = 0; i < kAuxRing; ++i) {
             mbar_init(&m.aux_full[i], 1);
-            mbar_init(&m.aux_empty[i], 4 * RT + 4);
+            mbar_init(&m.aux_empty[i], 12);          // 8 softmax and 4 converting warps
         }
         m.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -228,7 +224,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = m.tmem;                       // S0, S1, O0, O1
+    const uint32_t tmem = m.tmem;                       // four buffers of S, O0, O1
     constexpr uint32_t kO = 256;
     Walk walk{m, a, {}};
 
@@ -242,62 +238,63 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             Ring rk, rv;                        // rv: V's ring, as stored (plain) or as fp16 (fp8)
             constexpr int NP = FP8 ? NC : NV, kVTile = FP8 ? C::CONV : C::TILE;
             uint64_t* v_free = FP8 ? m.c_empty : m.v_empty;
-            uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit g of the two S buffers
+            uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit b of the four S buffers
+            constexpr int kItems = 2 * RT;      // of a tile
             const uint32_t q0 = desc_lo(smem_u32(smem), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
             const uint32_t v0 = desc_lo(smem_u32(smem + (FP8 ? C::OFF_C : C::OFF_V)), kVBlock);
             bool ok = true;
             while (true) {
                 if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
                 if (!m.seg[walk.seg.i].go) break;
-                const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * RT;
+                const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * kItems;
                 mbar_arrive(&m.seg_empty[walk.seg.i]);
                 walk.seg.next<kSegRing>();
                 if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
                 q_phase ^= 1u;
-                for (int i = 0; i <= items; ++i) {
-                    const int rt = RT == 2 ? i & 1 : 0;
+                for (int i = 0; i < items + 3; ++i) {
                     if (i < items) {
-                        // S[i & 1] = Q K^T; the product that read P from this buffer was issued before
-                        if (rt == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
+                        // S[i & 3] = Q K^T; the product that read P from this buffer was issued before
+                        if (i % kItems == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t d = tmem + (uint32_t)((i & 1) * 128);
-                        const uint32_t ql = q0 + (uint32_t)(rt * (C::Q >> 4)), kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4));
+                        const int rt = RT == 2 ? i & 1 : 0, half = RT == 2 ? i >> 1 & 1 : i & 1;
+                        const uint32_t d = tmem + (uint32_t)((i & 3) * kHalf);
+                        const uint32_t ql = q0 + (uint32_t)(rt * (C::Q >> 4));
+                        const uint32_t kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4) + half * (kHalf * (FP8 ? D : 128) >> 4));
                         if constexpr (FP8) {
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
                                 const uint32_t st = kk % (D / 32) * 2;
                                 mma_ss<true>(d, ql + (kk < D / 32 ? 0 : C::Q >> 5) + st, kl + st, D == 128 ? kRows128 : kRows64,
-                                             idesc_of(0, 128, 128, false), kk > 0);
+                                             idesc_of(0, 128, kHalf, false), kk > 0);
                             }
                         } else {
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk) {
                                 const uint32_t st = (kk >> 2) * (16384 >> 4) + (kk & 3) * 2;
-                                mma_ss<false>(d, ql + st, kl + st, kRows128, idesc_of(1, 128, 128, false), kk > 0);
+                                mma_ss<false>(d, ql + st, kl + st, kRows128, idesc_of(1, 128, kHalf, false), kk > 0);
                             }
                         }
-                        mma_commit(&m.s_full[i & 1]);
-                        if (rt == RT - 1) {
+                        mma_commit(&m.s_full[i & 3]);
+                        if (i % kItems == kItems - 1) {
                             mma_commit(&m.k_empty[rk.i]);
                             rk.next<NK>();
                         }
                         if (i == items - 1) mma_commit(&m.q_free);
                     }
-                    if (i > 0) {
-                        // O[j & 1] += P V, j = i - 1
-                        const int j = i - 1, g = j & 1;
-                        const bool last = RT == 1 || g == 1;
-                        if (!mbar_wait_or_abort(&m.p_ready[g], p_phase >> g & 1u, a.err, abort_flag)) { ok = false; break; }
-                        p_phase ^= 1u << g;
-                        if ((RT == 1 || g == 0) && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                    if (i > 2) {
+                        // O[j & 1] += P V, j = i - 3
+                        const int j = i - 3, g = j & 1, half = RT == 2 ? j >> 1 & 1 : g;
+                        if (!mbar_wait_or_abort(&m.p_ready[j & 3], p_phase >> (j & 3) & 1u, a.err, abort_flag)) { ok = false; break; }
+                        p_phase ^= 1u << (j & 3);
+                        if (j % kItems == 0 && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t vl = v0 + (uint32_t)(rv.i * (kVTile >> 4));
-                        const uint32_t d = tmem + kO + (uint32_t)(g * D), pa = tmem + (uint32_t)(g * 128);
+                        const uint32_t vl = v0 + (uint32_t)(rv.i * (kVTile >> 4) + half * (kHalf * 128 >> 4));
+                        const uint32_t d = tmem + kO + (uint32_t)(g * D), pa = tmem + (uint32_t)((j & 3) * kHalf);
 #pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)
+                        for (int kk = 0; kk < kHalf / 16; ++kk)
                             mma_ts(d, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j >= 2 || kk > 0);
                         mma_commit(&m.o_done[g]);
-                        if (last) {
+                        if (j % kItems == kItems - 1) {
                             mma_commit(&v_free[rv.i]);
                             rv.next<NP>();
                         }
@@ -459,7 +456,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         const int g = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const int tid = threadIdx.x - 128;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const uint32_t s_t = tmem + lanes + (uint32_t)(g * 128), o_t = tmem + lanes + kO + (uint32_t)(g * D);
+        const uint32_t s_t = tmem + lanes, o_t = tmem + lanes + kO + (uint32_t)(g * D);
         uint32_t s_phase = 0, o_phase = 0, soft_phase = 0;
         // the eight warps meet
         auto soft_sync = [&]() -> bool {
@@ -482,47 +479,42 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             const Segment& s = walk.segment();
             constexpr int apart = 128 / CP;
             const int row = RT == 2 ? g * 128 + r : r & (apart - 1);        // of the unit
-            const int col = RT == 2 ? 0 : r / apart * apart;                // first column of this copy
+            const int col = RT == 2 ? 0 : r / apart * (kHalf / CP);         // first column of this copy
             const bool live = row < s.rows;
             const bool warp_live = row - lane < s.rows;
             const int node = live ? (s.row0 + row) / a.group : 0;
             const int hq = s.head * a.group + (live ? (s.row0 + row) % a.group : 0);
-            const int tiles = s.tile1 - s.tile0;
             const float f_row0 = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
             float f_row = f_row0;
             RowState st{-INFINITY, 0.f, 1.f};
             int eref = 0;
-            int mine = 0;               // tiles of this group so far
-            for (int t = 0; t < tiles; ++t) {
-                const bool turn = RT == 2 || (t & 1) == g;
-                if (!turn) {
-                    if (FP8) ra.next<kAuxRing>();
-                    continue;
-                }
-                const int pos0 = (s.tile0 + t) * kTcKeys;
-                const bool drafted = pos0 + kTcKeys > s.len;
-                if (FP8 && !mbar_wait_warp(&m.aux_full[ra.i], ra.phase, a.err, abort_flag)) { ok = false; break; }
-                if (!mbar_wait_warp(&m.s_full[g], s_phase, a.err, abort_flag)) { ok = false; break; }
-                s_phase ^= 1u;
+            // this group's items: all of its rows (RT = 2), half of the tile's positions (RT = 1)
+            const int items = (s.tile1 - s.tile0) * RT;
+            for (int i = 0; i < items; ++i) {
+                const int buf = (i & 1) * 2 + g, half = RT == 2 ? i & 1 : g, pos0 = (s.tile0 + i / RT) * kTcKeys + half * kHalf;
+                const bool drafted = pos0 + kHalf > s.len, tile_first = i % RT == 0, tile_last = i % RT == RT - 1;
+                if (FP8 && tile_first && !mbar_wait_warp(&m.aux_full[ra.i], ra.phase, a.err, abort_flag)) { ok = false; break; }
+                if (!mbar_wait_warp(&m.s_full[buf], s_phase >> (i & 1) & 1u, a.err, abort_flag)) { ok = false; break; }
+                s_phase ^= 1u << (i & 1);
                 tc_fence_after();
                 st.o_mul = 1.f;
                 if (warp_live) {
-                    const float4* kf = m.kf[FP8 ? ra.i : 0];
-                    if (FP8) {
-                        if (!mine) f_row = fmaxf(f_row0 * m.q_scale[walk.seg.i][row], 0x1p-126f);    // 0 times a masked -inf is no score
+                    const float4* kf = m.kf[FP8 ? ra.i : 0] + half * (kHalf / 4);
+                    if (FP8 && tile_first) {
+                        if (i == 0) f_row = fmaxf(f_row0 * m.q_scale[walk.seg.i][row], 0x1p-126f);     // 0 times a masked -inf is no score
                         const int e = m.eref[ra.i];
-                        if (mine && e > eref) st.o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
+                        if (i > 0 && e > eref) st.o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
                         eref = e;
                     }
-                    softmax_tile<FP8, apart>(a, s, s_t, col, kf, drafted, node, pos0, f_row, !mine, st);
+                    softmax_item<FP8, kHalf / CP>(a, s, s_t + buf * kHalf, col, kf, drafted, node, pos0, f_row, i == 0, st);
                 }
-                if (FP8) {
+                if (FP8 && tile_last) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&m.aux_empty[ra.i]);
                     ra.next<kAuxRing>();
                 }
                 // the group's previous product has left O
-                if (mine) {
+                if (i > 0) {
                     if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
                     o_phase ^= 1u;
                     if (__any_sync(0xffffffffu, st.o_mul != 1.f)) {
@@ -541,14 +533,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&m.p_ready[g]);
-                ++mine;
+                if (lane == 0) mbar_arrive(&m.p_ready[buf]);
             }
             if (!ok) break;
-            if (mine) {
-                if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
-                o_phase ^= 1u;
-            }
+            if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
+            o_phase ^= 1u;
             tc_fence_after();
             // ---------------- the unit's result, or this CTA's part of it
             const bool whole = s.part < 0;
@@ -566,7 +555,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 l_all = 0.f;
                 for (int k = row; k < 256; k += apart) l_all += m.ml[k].y * exp2f(m.ml[k].x - z);
                 up0 = exp2f(m.ml[r].x - z);
-                up1 = tiles > 1 ? exp2f(m.ml[128 + r].x - z) : 0.f;
+                up1 = exp2f(m.ml[128 + r].x - z);
                 if (FP8) {
                     up0 *= exp2f((float)(m.eref1[0] - kVUp));
                     up1 *= exp2f((float)(m.eref1[1] - kVUp));
@@ -574,7 +563,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             } else {
                 up0 = st.ref == -INFINITY ? 0.f : FP8 ? exp2f((float)(eref - kVUp)) : 1.f;
             }
-            // (read behind the meeting above: a group without tiles has waited for nothing else)
             const unsigned long long* bad = m.seg[walk.seg.i].bad;
             const bool any_bad = bad[0] | bad[1] | bad[2] | bad[3];
             if (whole) {
@@ -607,7 +595,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         for (int d = 0; d < w; d += 16) {
                             uint32_t x[16], y[16];
                             tmem_ld16(ta + c + d, x);
-                            if (tiles > 1) tmem_ld16(tb + c + d, y);
+                            tmem_ld16(tb + c + d, y);
                             tmem_ld_wait();
                             if (!live) continue;
 #pragma unroll
@@ -616,7 +604,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) {
                                     o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[i + j]) * up0;
-                                    if (tiles > 1 && up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
+                                    if (up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
                                 }
                                 // 16-byte chunks turned by the row: rows' equal chunks lie in distinct banks
                                 *reinterpret_cast<float4*>(buf + mine_at + ((d + i) / 4 + row) % (wide / 4) * 4) = make_float4(o[0], o[1], o[2], o[3]);
@@ -646,7 +634,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 for (int c = c0; c < c1; c += 16) {
                     uint32_t x[16], y[16];
                     tmem_ld16(ta + c, x);
-                    if (RT == 1 && tiles > 1) tmem_ld16(tb + c, y);
+                    if (RT == 1) tmem_ld16(tb + c, y);
                     tmem_ld_wait();
                     if (!live) continue;
 #pragma unroll
@@ -655,7 +643,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[i + j]) * up0;
-                            if (RT == 1 && tiles > 1 && up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
+                            if (RT == 1 && up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
                         }
                         emit4(row, at, c + i, make_float4(o[0], o[1], o[2], o[3]));
                     }
