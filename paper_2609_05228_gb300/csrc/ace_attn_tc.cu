@@ -146,7 +146,8 @@ __device__ __forceinline__ void softmax_item(const AttnArgs& a, const Segment& s
     constexpr float kUp = FP8 ? (float)kPUp : 0.f;
     if (top > st.ref + (float)kLazy + kUp || st.ref == -INFINITY) {
         const float ref = top - kUp;
-        const float f = st.ref == -INFINITY ? 0.f : exp2_approx(st.ref - ref);
+        // (what it has summed before its first score is zero)
+        const float f = st.ref == -INFINITY ? 1.f : exp2_approx(st.ref - ref);
         st.ref = ref;
         st.l *= f;
         if (!first) st.o_mul *= f;
@@ -196,11 +197,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         for (int i = 0; i < 4; ++i) {
             mbar_init(&m.s_full[i], 1);
             mbar_init(&m.p_ready[i], 4);
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&m.c_empty[i], 1);
             mbar_init(&m.o_done[i], 1);
         }
+        mbar_init(&m.c_empty[0], 1), mbar_init(&m.c_empty[1], 1);
         mbar_init(&m.q_full, 4);
         mbar_init(&m.soft, 8);
         mbar_init(&m.group[0], 4), mbar_init(&m.group[1], 4);
@@ -293,7 +292,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
 #pragma unroll
                         for (int kk = 0; kk < kHalf / 16; ++kk)
                             mma_ts(d, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j >= 2 || kk > 0);
-                        mma_commit(&m.o_done[g]);
+                        mma_commit(&m.o_done[j & 3]);
                         if (j % kItems == kItems - 1) {
                             mma_commit(&v_free[rv.i]);
                             rv.next<NP>();
@@ -457,7 +456,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         const int tid = threadIdx.x - 128;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t s_t = tmem + lanes, o_t = tmem + lanes + kO + (uint32_t)(g * D);
-        uint32_t s_phase = 0, o_phase = 0, soft_phase = 0;
+        uint32_t s_phase = 0, soft_phase = 0;         // s_phase: bit i of the group's two buffers, of S and of its product
         // the eight warps meet
         auto soft_sync = [&]() -> bool {
             __syncwarp();
@@ -479,7 +478,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             const Segment& s = walk.segment();
             constexpr int apart = 128 / CP;
             const int row = RT == 2 ? g * 128 + r : r & (apart - 1);        // of the unit
-            const int col = RT == 2 ? 0 : r / apart * (kHalf / CP);         // first column of this copy
+            const int col = CP == 1 ? 0 : quad / 2 * (kHalf / CP);          // first column of this copy (as a warp's value)
             const bool live = row < s.rows;
             const bool warp_live = row - lane < s.rows;
             const int node = live ? (s.row0 + row) / a.group : 0;
@@ -513,31 +512,28 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     if (lane == 0) mbar_arrive(&m.aux_empty[ra.i]);
                     ra.next<kAuxRing>();
                 }
-                // the group's previous product has left O
-                if (i > 0) {
-                    if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
-                    o_phase ^= 1u;
-                    if (__any_sync(0xffffffffu, st.o_mul != 1.f)) {
-                        tc_fence_after();
+                if (i > 0 && __any_sync(0xffffffffu, live && st.o_mul != 1.f)) {
+                    // once the group's product before has left O (which runs beside this item's softmax, and is not waited
+                    // for otherwise); the scores of this item came after the one before that
+                    if (!mbar_wait_warp(&m.o_done[buf ^ 2], (s_phase >> (~i & 1) & 1u) ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
 #pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t x[32];
-                            tmem_ld32(o_t + 32 * c, x);
-                            tmem_ld_wait();
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t x[32];
+                        tmem_ld32(o_t + 32 * c, x);
+                        tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * st.o_mul);
-                            tmem_st32(o_t + 32 * c, x);
-                        }
-                        tmem_st_wait();
+                        for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * st.o_mul);
+                        tmem_st32(o_t + 32 * c, x);
                     }
+                    tmem_st_wait();
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&m.p_ready[buf]);
             }
             if (!ok) break;
-            if (!mbar_wait_warp(&m.o_done[g], o_phase, a.err, abort_flag)) { ok = false; break; }
-            o_phase ^= 1u;
+            if (!mbar_wait_warp(&m.o_done[(~items & 1) * 2 + g], (s_phase >> (~items & 1) & 1u) ^ 1u, a.err, abort_flag)) { ok = false; break; }
             tc_fence_after();
             // ---------------- the unit's result, or this CTA's part of it
             const bool whole = s.part < 0;

@@ -41,7 +41,7 @@ struct TcSegment {
 // Barriers and hand-overs of a CTA.
 struct TcShared {
     uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], v_ready[6];
-    uint64_t s_full[4], p_ready[4], o_done[2], q_full, q_free, drain;
+    uint64_t s_full[4], p_ready[4], o_done[4], q_full, q_free, drain;
     uint64_t seg_full[kSegRing], seg_empty[kSegRing], aux_full[kAuxRing], aux_empty[kAuxRing];
     uint32_t tmem;
     int abort_flag, joins, pad;
