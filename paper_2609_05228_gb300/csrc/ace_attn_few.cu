@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
         }
         mbar_init(&m.q_full, 4);
         mbar_init(&m.q_free, 1);
-        mbar_init(&m.drain, 1);
+        mbar_init(&m.drain[0], 1);
         for (int i = 0; i < kSegRing; ++i) {
             mbar_init(&m.seg_full[i], 1);
             mbar_init(&m.seg_empty[i], FP8 ? 15 : 14);  // load, MMA, (scales,) 8 softmax and 4 other warps
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
     if (warp == 3) {
         role_schedule<C::ROWS>(m, a);
     } else if (warp == 0) {
-        role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V);
+        role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [] { return true; });
     } else if (warp == 2) {
         if constexpr (FP8) role_scales(m, a, m.kf, m.vf);
     } else if (warp == 1) {
@@ -276,8 +276,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
             if (!ok) *abort_flag = 1;
             if (*abort_flag) {
                 // products in flight read shared memory and write TMEM
-                mma_commit(&m.drain);
-                mbar_wait(&m.drain, 0, a.err);
+                mma_commit(&m.drain[0]);
+                mbar_wait(&m.drain[0], 0, a.err);
             }
         }
         __syncwarp();

@@ -9,8 +9,8 @@
 //   O += P V               tcgen05.mma, A = P from TMEM, B = V as stored (its rows are K indices)
 // In items of 64 positions, two groups of four softmax warps and two accumulators: with RT = 2 a group has a block of 128
 // rows, and both halves of each tile; with RT = 1 both have the same rows, and a half of each tile, joined at the end. A
-// group has two buffers of S, so that the products of one item run beside the softmax of the next: with whole tiles and
-// one buffer a group waited for its products half of the time (256 rows and 128 positions took 4400 cycles).
+// group has two buffers of S, so that the products of one item run beside the softmax of the next, and a thread of its own
+// that issues them: an item's twelve products, waits and hand-overs take it 1050 cycles, as long as the softmax.
 // fp8 caches: K's codes are the B operand as stored (kind::f8f6f4), against q split into two e4m3 terms, which
 // hold 8 significant bits, all of a bf16 q (elements 2^-10 and more below the row's largest lose their last bits, a
 // 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory (exact), with
@@ -170,6 +170,11 @@ __device__ __forceinline__ void softmax_item(const AttnArgs& a, const Segment& s
     tmem_st_wait();
 }
 
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
 // Two codes as fp16 times `f`.
 __device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
     const uint32_t y = f16x2_of_e4m3x2(codes);
@@ -191,23 +196,23 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     volatile int* abort_flag = &m.abort_flag;
     const int warp = warp_index(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < NK; ++i) mbar_init(&m.k_full[i], 1), mbar_init(&m.k_empty[i], 1);
-        for (int i = 0; i < NV; ++i) mbar_init(&m.v_full[i], 1), mbar_init(&m.v_empty[i], FP8 ? 4 : 1);
+        for (int i = 0; i < NK; ++i) mbar_init(&m.k_full[i], 1), mbar_init(&m.k_empty[i], 2);
+        for (int i = 0; i < NV; ++i) mbar_init(&m.v_full[i], 1), mbar_init(&m.v_empty[i], FP8 ? 4 : 2);
         for (int i = 0; i < (FP8 ? NC : NV); ++i) mbar_init(&m.v_ready[i], 4);
         for (int i = 0; i < 4; ++i) {
             mbar_init(&m.s_full[i], 1);
             mbar_init(&m.p_ready[i], 4);
             mbar_init(&m.o_done[i], 1);
         }
-        mbar_init(&m.c_empty[0], 1), mbar_init(&m.c_empty[1], 1);
+        mbar_init(&m.c_empty[0], 2), mbar_init(&m.c_empty[1], 2);
         mbar_init(&m.q_full, 4);
         mbar_init(&m.soft, 8);
         mbar_init(&m.group[0], 4), mbar_init(&m.group[1], 4);
-        mbar_init(&m.q_free, 1);
-        mbar_init(&m.drain, 1);
+        mbar_init(&m.q_free, 2);
+        mbar_init(&m.drain[0], 1), mbar_init(&m.drain[1], 1);
         for (int i = 0; i < kSegRing; ++i) {
             mbar_init(&m.seg_full[i], 1);
-            mbar_init(&m.seg_empty[i], FP8 ? 15 : 14);  // producer, MMA, (scales,) 8 softmax and 4 converting warps
+            mbar_init(&m.seg_empty[i], FP8 ? 16 : 15);  // load, 2 MMA, (scales,) 8 softmax and 4 converting warps
         }
         for (int i = 0; i < kAuxRing; ++i) {
             mbar_init(&m.aux_full[i], 1);
@@ -227,73 +232,74 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     constexpr uint32_t kO = 256;
     Walk walk{m, a, {}};
 
-    if (warp == 3) {
-        role_schedule<ROWS>(m, a);
-    } else if (warp == 0) {
-        role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V);
-    } else if (warp == 1) {
-        // ------------------------------------------------ MMA issuer
+    if (warp == 0) {
+        Scheduler<ROWS> sched(m, a);                    // a segment ahead of the loads
+        if (sched.publish()) role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [&] { return sched.publish(); });
+    } else if (warp == 2) {
+        if constexpr (FP8) role_scales(m, a, m.kf, m.vf);
+    } else if (warp == 1 || warp == 3) {
+        // ------------------------------------------------ MMA issuers, one a softmax group
         if (elect_one()) {
+            const int g = warp >> 1;
             Ring rk, rv;                        // rv: V's ring, as stored (plain) or as fp16 (fp8)
             constexpr int NP = FP8 ? NC : NV, kVTile = FP8 ? C::CONV : C::TILE;
             uint64_t* v_free = FP8 ? m.c_empty : m.v_empty;
-            uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit b of the four S buffers
-            constexpr int kItems = 2 * RT;      // of a tile
-            const uint32_t q0 = desc_lo(smem_u32(smem), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
+            uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit n & 1 of the group's two S buffers
+            const uint32_t q0 = desc_lo(smem_u32(smem + (RT == 2 ? g * C::Q : 0)), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
             const uint32_t v0 = desc_lo(smem_u32(smem + (FP8 ? C::OFF_C : C::OFF_V)), kVBlock);
+            const uint32_t o = tmem + kO + (uint32_t)(g * D);
             bool ok = true;
             while (true) {
                 if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
                 if (!m.seg[walk.seg.i].go) break;
-                const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * kItems;
+                const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * RT;        // the group's
                 mbar_arrive(&m.seg_empty[walk.seg.i]);
                 walk.seg.next<kSegRing>();
                 if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
                 q_phase ^= 1u;
-                for (int i = 0; i < items + 3; ++i) {
-                    if (i < items) {
-                        // S[i & 3] = Q K^T; the product that read P from this buffer was issued before
-                        if (i % kItems == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
+                for (int n = 0; n <= items; ++n) {
+                    if (n < items) {
+                        // S of item n = Q K^T; the product that read P from this buffer (item n - 2) was issued before
+                        const int half = RT == 2 ? n & 1 : g, buf = (n & 1) * 2 + g;
+                        if (n % RT == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
-                        const int rt = RT == 2 ? i & 1 : 0, half = RT == 2 ? i >> 1 & 1 : i & 1;
-                        const uint32_t d = tmem + (uint32_t)((i & 3) * kHalf);
-                        const uint32_t ql = q0 + (uint32_t)(rt * (C::Q >> 4));
+                        const uint32_t d = tmem + (uint32_t)(buf * kHalf);
                         const uint32_t kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4) + half * (kHalf * (FP8 ? D : 128) >> 4));
                         if constexpr (FP8) {
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
                                 const uint32_t st = kk % (D / 32) * 2;
-                                mma_ss<true>(d, ql + (kk < D / 32 ? 0 : C::Q >> 5) + st, kl + st, D == 128 ? kRows128 : kRows64,
+                                mma_ss<true>(d, q0 + (kk < D / 32 ? 0 : C::Q >> 5) + st, kl + st, D == 128 ? kRows128 : kRows64,
                                              idesc_of(0, 128, kHalf, false), kk > 0);
                             }
                         } else {
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk) {
                                 const uint32_t st = (kk >> 2) * (16384 >> 4) + (kk & 3) * 2;
-                                mma_ss<false>(d, ql + st, kl + st, kRows128, idesc_of(1, 128, kHalf, false), kk > 0);
+                                mma_ss<false>(d, q0 + st, kl + st, kRows128, idesc_of(1, 128, kHalf, false), kk > 0);
                             }
                         }
-                        mma_commit(&m.s_full[i & 3]);
-                        if (i % kItems == kItems - 1) {
+                        mma_commit(&m.s_full[buf]);
+                        if (n % RT == RT - 1) {
                             mma_commit(&m.k_empty[rk.i]);
                             rk.next<NK>();
                         }
-                        if (i == items - 1) mma_commit(&m.q_free);
+                        if (n == items - 1) mma_commit(&m.q_free);
                     }
-                    if (i > 2) {
-                        // O[j & 1] += P V, j = i - 3
-                        const int j = i - 3, g = j & 1, half = RT == 2 ? j >> 1 & 1 : g;
-                        if (!mbar_wait_or_abort(&m.p_ready[j & 3], p_phase >> (j & 3) & 1u, a.err, abort_flag)) { ok = false; break; }
-                        p_phase ^= 1u << (j & 3);
-                        if (j % kItems == 0 && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                    if (n > 0) {
+                        // O += P V of item j = n - 1
+                        const int j = n - 1, half = RT == 2 ? j & 1 : g, buf = (j & 1) * 2 + g;
+                        if (!mbar_wait_or_abort(&m.p_ready[buf], p_phase >> (j & 1) & 1u, a.err, abort_flag)) { ok = false; break; }
+                        p_phase ^= 1u << (j & 1);
+                        if (j % RT == 0 && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
                         tc_fence_after();
                         const uint32_t vl = v0 + (uint32_t)(rv.i * (kVTile >> 4) + half * (kHalf * 128 >> 4));
-                        const uint32_t d = tmem + kO + (uint32_t)(g * D), pa = tmem + (uint32_t)((j & 3) * kHalf);
+                        const uint32_t pa = tmem + (uint32_t)(buf * kHalf);
 #pragma unroll
                         for (int kk = 0; kk < kHalf / 16; ++kk)
-                            mma_ts(d, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j >= 2 || kk > 0);
-                        mma_commit(&m.o_done[j & 3]);
-                        if (j % kItems == kItems - 1) {
+                            mma_ts(o, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j > 0 || kk > 0);
+                        mma_commit(&m.o_done[buf]);
+                        if (j % RT == RT - 1) {
                             mma_commit(&v_free[rv.i]);
                             rv.next<NP>();
                         }
@@ -304,13 +310,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             if (!ok) *abort_flag = 1;
             if (*abort_flag) {
                 // products in flight read shared memory and TMEM
-                mma_commit(&m.drain);
-                mbar_wait(&m.drain, 0, a.err);
+                mma_commit(&m.drain[g]);
+                mbar_wait(&m.drain[g], 0, a.err);
             }
         }
         __syncwarp();
-    } else if (warp == 2) {
-        if constexpr (FP8) role_scales(m, a, m.kf, m.vf);
     } else if (warp >= 12) {
         // ------------------------------------------------ q rows, and V tiles made ready
         const int tid = threadIdx.x - 384;
@@ -569,17 +573,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             // group g takes half of the dimensions of both accumulators (RT = 1), or its own accumulator
             const int c0 = RT == 1 ? g * (D / 2) : 0, c1 = RT == 1 ? c0 + D / 2 : D;
             const uint32_t ta = tmem + lanes + kO + (uint32_t)(RT == 1 ? 0 : g * D), tb = ta + D;
-            auto emit4 = [&](int urow, long long to, int d, float4 o) {      // 4 dimensions of a finished row
-                if (whole) {
-                    const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x, o.y), hi = __floats2bfloat162_rn(o.z, o.w);
-                    uint2 w;
-                    w.x = *reinterpret_cast<const uint32_t*>(&lo);
-                    w.y = *reinterpret_cast<const uint32_t*>(&hi);
-                    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to * D + d) = w;
-                } else {
-                    *reinterpret_cast<float4*>(a.ws.part_o + ((long long)s.part * ROWS + urow) * D + d) = o;
-                }
-            };
             if constexpr (CP > 1) {
                 // as many dimensions at a time as the buffer holds of the unit's rows and copies: 16 to D / 2
                 float* buf = reinterpret_cast<float*>(smem + C::OFF_MERGE) + g * 128 * 16;
@@ -619,7 +612,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                             o.w += v.w;
                         }
                         const int ur = s.row0 + urow, nd = ur / a.group;
-                        emit4(urow, (long long)(s.node0 + nd) * a.n_heads + s.head * a.group + ur - nd * a.group, c + q4 * 4, o);
+                        if (whole) {
+                            const long long to = (long long)(s.node0 + nd) * a.n_heads + s.head * a.group + ur - nd * a.group;
+                            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to * D + c + q4 * 4) = make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
+                        } else {
+                            *reinterpret_cast<float4*>(a.ws.part_o + ((long long)s.part * ROWS + urow) * D + c + q4 * 4) = o;
+                        }
                     }
                     if (any_bad)
                         for (int i = r; i < s.rows * (w / 4); i += 128) add_not_finite<FP8, ROWS>(a, s, bad, i / (w / 4), c + i % (w / 4) * 4, 4);
@@ -627,25 +625,35 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 }
                 if (!ok) break;
             } else if (warp_live) {
+#pragma unroll 1
                 for (int c = c0; c < c1; c += 16) {
                     uint32_t x[16], y[16];
                     tmem_ld16(ta + c, x);
                     if (RT == 1) tmem_ld16(tb + c, y);
                     tmem_ld_wait();
                     if (!live) continue;
+                    float o[16];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        float o[4];
+                    for (int i = 0; i < 16; ++i) {
+                        o[i] = up0 == 0.f ? 0.f : __uint_as_float(x[i]) * up0;
+                        if (RT == 1 && up1 != 0.f) o[i] += __uint_as_float(y[i]) * up1;
+                    }
+                    if (whole) {
+                        uint32_t w[8];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[i + j]) * up0;
-                            if (RT == 1 && up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
-                        }
-                        emit4(row, at, c + i, make_float4(o[0], o[1], o[2], o[3]));
+                        for (int i = 0; i < 8; ++i) w[i] = bf16x2(o[2 * i], o[2 * i + 1]);
+                        uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + at * D + c);
+                        to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                        to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                    } else {
+                        // parts of these units lie by dimensions, then rows: a store of a warp is 512 bytes on end
+                        float4* to = reinterpret_cast<float4*>(a.ws.part_o) + ((long long)s.part * (D / 4) + c / 4) * ROWS + row;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) to[i * ROWS] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     }
                 }
                 if (any_bad && live)
-                    for (int d = c0; d < c1; d += 4) add_not_finite<FP8, ROWS>(a, s, bad, row, d, 4);
+                    for (int d = c0; d < c1; d += 4) add_not_finite<FP8, ROWS, true>(a, s, bad, row, d, 4);
             }
             if (live && c0 == 0 && r < apart) {
                 if (!whole) a.ws.part_ml[(long long)s.part * ROWS + row] = make_float2(m_all, l_all);
@@ -660,7 +668,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     if (!soft_sync()) { ok = false; break; }
                     if (m.joins) {
                         __threadfence();
-                        join_unit<__nv_bfloat16, ROWS>(a, s, tid, 256);
+                        join_unit<__nv_bfloat16, ROWS, CP == 1>(a, s, tid, 256);
                     }
                 }
             }

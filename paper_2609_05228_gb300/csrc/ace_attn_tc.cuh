@@ -41,7 +41,7 @@ struct TcSegment {
 // Barriers and hand-overs of a CTA.
 struct TcShared {
     uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], v_ready[6];
-    uint64_t s_full[4], p_ready[4], o_done[4], q_full, q_free, drain;
+    uint64_t s_full[4], p_ready[4], o_done[4], q_full, q_free, drain[2];
     uint64_t seg_full[kSegRing], seg_empty[kSegRing], aux_full[kAuxRing], aux_empty[kAuxRing];
     uint32_t tmem;
     int abort_flag, joins, pad;
@@ -158,7 +158,7 @@ __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, 
 
 // Values of V that are not finite were left out of the products: row `urow` of the unit, written already, gets those of
 // the nodes that it sees in dimensions d .. d + count - 1.
-template <bool FP8, int ROWS>
+template <bool FP8, int ROWS, bool BY_DIMS = false>
 __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment& s, const unsigned long long* bad, int urow, int d,
                                                int count) {
     const int nd = (s.row0 + urow) / a.group, hq = s.head * a.group + (s.row0 + urow) % a.group;
@@ -178,7 +178,7 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment&
                 __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + ((long long)(s.node0 + nd) * a.n_heads + hq) * a.head_dim + i;
                 *out = from_f32<__nv_bfloat16>(to_f32(*out) + v);
             } else {
-                a.ws.part_o[((long long)s.part * ROWS + urow) * a.head_dim + i] += v;
+                a.ws.part_o[part_place<ROWS, BY_DIMS>(a.head_dim, s.part, urow, i)] += v;
             }
         }
     }
@@ -281,17 +281,23 @@ struct Walk {
     }
 };
 
-// One warp: the CTA's segments, a few ahead of the roles that work on them.
+// The CTA's segments, published by one warp ahead of the roles that work on them.
 template <int ROWS>
-__device__ __forceinline__ void role_schedule(TcShared& m, const AttnArgs& a) {
-    volatile int* abort_flag = &m.abort_flag;
+struct Scheduler {
+    TcShared& m;
+    const AttnArgs& a;
     Ring seg;
-    Cursor cur{};
-    bool more = cursor_init<ROWS, kTcKeys>(a, blockIdx.x, gridDim.x, cur);
-    while (true) {
-        if (!mbar_wait_warp(&m.seg_empty[seg.i], seg.phase ^ 1u, a.err, abort_flag)) {
-            *abort_flag = 1;
-            break;
+    Cursor cur;
+    bool more, done;
+    __device__ __forceinline__ Scheduler(TcShared& m_, const AttnArgs& a_) : m(m_), a(a_), seg{}, cur{}, done(false) {
+        more = cursor_init<ROWS, kTcKeys>(a, blockIdx.x, gridDim.x, cur);
+    }
+    // The next segment, or that there is none. False: given up.
+    __device__ __forceinline__ bool publish() {
+        if (done) return true;
+        if (!mbar_wait_warp(&m.seg_empty[seg.i], seg.phase ^ 1u, a.err, &m.abort_flag)) {
+            *static_cast<volatile int*>(&m.abort_flag) = 1;
+            return false;
         }
         Segment s{};
         more = more && cursor_next<ROWS, kTcKeys>(a, blockIdx.x, cur, s);
@@ -302,13 +308,21 @@ __device__ __forceinline__ void role_schedule(TcShared& m, const AttnArgs& a) {
             mbar_arrive(&m.seg_full[seg.i]);
         }
         seg.next<kSegRing>();
-        if (!more) break;
+        done = !more;
+        return true;
     }
+};
+
+template <int ROWS>
+__device__ __forceinline__ void role_schedule(TcShared& m, const AttnArgs& a) {
+    Scheduler<ROWS> sched(m, a);
+    while (!sched.done && sched.publish()) {}
 }
 
-// One warp: TMA loads of K and V tiles; lane x loads box x of a tile.
-template <bool FP8, int D, int NK, int NV>
-__device__ __forceinline__ void role_load(TcShared& m, const TcAttnArgs& p, unsigned char* k_smem, unsigned char* v_smem) {
+// One warp: TMA loads of K and V tiles; lane x loads box x of a tile. started(): called when a segment's first tile is under
+// way; false gives up.
+template <bool FP8, int D, int NK, int NV, typename Started>
+__device__ __forceinline__ void role_load(TcShared& m, const TcAttnArgs& p, unsigned char* k_smem, unsigned char* v_smem, Started started) {
     constexpr int kTile = 128 * D * (FP8 ? 1 : 2);
     const AttnArgs& a = p.a;
     volatile int* abort_flag = &m.abort_flag;
@@ -354,6 +368,7 @@ __device__ __forceinline__ void role_load(TcShared& m, const TcAttnArgs& p, unsi
                 }
                 if (kv) ++nv, rv.next<NV>(); else ++nk, rk.next<NK>();
             }
+            if (ok && t == s.tile0) ok = started();
             if (!ok) break;
         }
         walk.done();
@@ -368,7 +383,8 @@ __device__ __forceinline__ void role_load(TcShared& m, const TcAttnArgs& p, unsi
     }
 }
 
-// One warp, fp8 caches: a tile's scales, 4 positions a lane. K's as factors 2^e; V's as 2^(e - eref + kVUp) with the tile's eref.
+// One warp, fp8 caches: a tile's scales, 4 positions a lane. K's as factors 2^e; V's as 2^(e - eref + kVUp) with the tile's
+// eref.
 template <typename V4>
 __device__ __forceinline__ void role_scales(TcShared& m, const AttnArgs& a, float4 (*kf_out)[32], V4 (*vf_out)[32]) {
     volatile int* abort_flag = &m.abort_flag;

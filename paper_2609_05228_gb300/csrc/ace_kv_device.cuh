@@ -201,13 +201,20 @@ __device__ __forceinline__ unsigned long long sees_word(const AttnArgs& a, int n
     return left >= 64 ? m : m & ((1ull << left) - 1ull);
 }
 
+// Place of dimension d of row r in partial result `slot`: by rows, or (BY_DIMS) by 4 dimensions and then rows, for kernels
+// in which a thread holds a row.
+template <int ROWS, bool BY_DIMS>
+__device__ __forceinline__ long long part_place(int D, long long slot, int r, int d) {
+    return BY_DIMS ? ((slot * (D / 4) + d / 4) * ROWS + r) * 4 + d % 4 : (slot * ROWS + r) * D + d;
+}
+
 // Joins a unit's partial results: row r of the unit from the slots of CTAs first .. last, in that order, 4
 // dimensions a thread and turn. Every thread of a CTA calls it; all partial results must be visible. ITEMS x PARTS
 // loads are under way together, each of which takes most of a microsecond: a unit with few rows has many parts (a
 // long context), one with many rows has work for all threads several times over.
-template <typename T, int ROWS, int ITEMS, int PARTS>
+template <typename T, int ROWS, bool BY_DIMS, int ITEMS, int PARTS>
 __device__ __forceinline__ void join_items(const AttnArgs& a, const Segment& s, int tid, int threads) {
-    const int D = a.head_dim, quads = D / 4, items = s.rows * quads;
+    const int D = a.head_dim, quads = D / 4, items = (BY_DIMS ? (s.rows + 7) / 8 * 8 : s.rows) * quads;
     for (int i0 = tid; i0 < items; i0 += threads * ITEMS) {
         // partial results with the reference that they turn up with: they are rescaled as it grows
         float M[ITEMS], L[ITEMS];
@@ -219,8 +226,15 @@ __device__ __forceinline__ void join_items(const AttnArgs& a, const Segment& s, 
             L[k] = 0.f;
             o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
             const int i = min(i0 + k * threads, items - 1);
-            r[k] = i / quads;
-            d[k] = (i - r[k] * quads) * 4;
+            if (BY_DIMS) {
+                // 4 quads of 8 rows a warp and turn: whole lines of the parts, and whole sectors of the output
+                const int blocks = quads / 4, block = i / 32, rb = block / blocks;
+                r[k] = min(rb * 8 + i % 8, s.rows - 1);
+                d[k] = ((block - rb * blocks) * 4 + i / 8 % 4) * 4;
+            } else {
+                r[k] = i / quads;
+                d[k] = (i - r[k] * quads) * 4;
+            }
         }
         for (int c0 = s.first; c0 <= s.last; c0 += PARTS) {
             float2 ml[ITEMS][PARTS];
@@ -233,9 +247,9 @@ __device__ __forceinline__ void join_items(const AttnArgs& a, const Segment& s, 
                     ml[k][j] = make_float2(-INFINITY, 0.f);
                     v[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (c <= s.last) {
-                        const long long slot = (long long)part_slot(c, s.first) * ROWS + r[k];
-                        ml[k][j] = __ldcg(&a.ws.part_ml[slot]);
-                        v[k][j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + slot * D + d[k]));
+                        const long long slot = part_slot(c, s.first);
+                        ml[k][j] = __ldcg(&a.ws.part_ml[slot * ROWS + r[k]]);
+                        v[k][j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + part_place<ROWS, BY_DIMS>(D, slot, r[k], d[k])));
                     }
                 }
             }
@@ -283,10 +297,10 @@ __device__ __forceinline__ void join_items(const AttnArgs& a, const Segment& s, 
     }
 }
 
-template <typename T, int ROWS>
+template <typename T, int ROWS, bool BY_DIMS = false>
 __device__ __forceinline__ void join_unit(const AttnArgs& a, const Segment& s, int tid, int threads) {
-    if (ROWS > 16 && s.rows * a.head_dim / 4 >= 2 * threads) join_items<T, ROWS, 4, 2>(a, s, tid, threads);
-    else join_items<T, ROWS, 1, 8>(a, s, tid, threads);
+    if (ROWS > 16 && s.rows * a.head_dim / 4 >= 2 * threads) join_items<T, ROWS, BY_DIMS, 4, 2>(a, s, tid, threads);
+    else join_items<T, ROWS, BY_DIMS, 1, 8>(a, s, tid, threads);
 }
 
 // One thread, after all of the CTA's partial results are visible on the device: true in the last CTA of the unit.
