@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
         __syncthreads();
         if (joins) {
             __threadfence();
-            join_unit<T, kRows>(a, s, tid, kThreads);
+            join_unit<T, kRows, 0>(a, s, tid, kThreads);
         }
     }
 }

@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 meet(3, 256);
                 if (m.joins) {
                     __threadfence();
-                    join_unit<__nv_bfloat16, C::ROWS>(a, s, tid, 256);
+                    join_unit<__nv_bfloat16, C::ROWS, D>(a, s, tid, 256);
                 }
             }
             walk.done();

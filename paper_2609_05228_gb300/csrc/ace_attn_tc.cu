@@ -668,7 +668,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     if (!soft_sync()) { ok = false; break; }
                     if (m.joins) {
                         __threadfence();
-                        join_unit<__nv_bfloat16, ROWS, CP == 1>(a, s, tid, 256);
+                        join_unit<__nv_bfloat16, ROWS, D, CP == 1>(a, s, tid, 256);
                     }
                 }
             }

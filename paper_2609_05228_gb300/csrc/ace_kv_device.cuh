@@ -208,99 +208,108 @@ __device__ __forceinline__ long long part_place(int D, long long slot, int r, in
     return BY_DIMS ? ((slot * (D / 4) + d / 4) * ROWS + r) * 4 + d % 4 : (slot * ROWS + r) * D + d;
 }
 
-// Joins a unit's partial results: row r of the unit from the slots of CTAs first .. last, in that order, 4
-// dimensions a thread and turn. Every thread of a CTA calls it; all partial results must be visible. ITEMS x PARTS
-// loads are under way together, each of which takes most of a microsecond: a unit with few rows has many parts (a
-// long context), one with many rows has work for all threads several times over.
-template <typename T, int ROWS, bool BY_DIMS, int ITEMS, int PARTS>
-__device__ __forceinline__ void join_items(const AttnArgs& a, const Segment& s, int tid, int threads) {
-    const int D = a.head_dim, quads = D / 4, items = (BY_DIMS ? (s.rows + 7) / 8 * 8 : s.rows) * quads;
-    for (int i0 = tid; i0 < items; i0 += threads * ITEMS) {
-        // partial results with the reference that they turn up with: they are rescaled as it grows
-        float M[ITEMS], L[ITEMS];
-        float4 o[ITEMS];
-        int r[ITEMS], d[ITEMS];
+// 4 dimensions of an output row.
+template <typename T>
+__device__ __forceinline__ void store_joined(const AttnArgs& a, long long at, int d, float4 o, float inv) {
+    T* out = static_cast<T*>(a.out) + at * a.head_dim + d;
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    } else {
+        __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+        uint2 w;
+        w.x = *reinterpret_cast<uint32_t*>(&lo);
+        w.y = *reinterpret_cast<uint32_t*>(&hi);
+        *reinterpret_cast<uint2*>(out) = w;
+    }
+}
+
+// A row's partial results over parts c0 .. c0 + PARTS - 1 of a unit, 4 dimensions at each of ITEMS places, onto what came
+// before: with the reference that they turn up with, rescaled as it grows.
+template <int ROWS, bool BY_DIMS, int ITEMS, int PARTS>
+__device__ __forceinline__ void join_parts(const AttnArgs& a, const Segment& s, int c0, int r, int d, float& M, float& L, float4 (&o)[ITEMS]) {
+    float2 ml[PARTS];
+    float4 v[ITEMS][PARTS];
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            M[k] = -INFINITY;
-            L[k] = 0.f;
-            o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-            const int i = min(i0 + k * threads, items - 1);
-            if (BY_DIMS) {
-                // 4 quads of 8 rows a warp and turn: whole lines of the parts, and whole sectors of the output
-                const int blocks = quads / 4, block = i / 32, rb = block / blocks;
-                r[k] = min(rb * 8 + i % 8, s.rows - 1);
-                d[k] = ((block - rb * blocks) * 4 + i / 8 % 4) * 4;
-            } else {
-                r[k] = i / quads;
-                d[k] = (i - r[k] * quads) * 4;
-            }
+    for (int j = 0; j < PARTS; ++j) {
+        const int c = c0 + j;
+        ml[j] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) v[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c <= s.last) {
+            const long long slot = part_slot(c, s.first);
+            ml[j] = __ldcg(&a.ws.part_ml[slot * ROWS + r]);
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k)
+                v[k][j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + part_place<ROWS, BY_DIMS>(a.head_dim, slot, r, d + 16 * k)));
         }
-        for (int c0 = s.first; c0 <= s.last; c0 += PARTS) {
-            float2 ml[ITEMS][PARTS];
-            float4 v[ITEMS][PARTS];
+    }
+    float top = M;
 #pragma unroll
-            for (int j = 0; j < PARTS; ++j) {
+    for (int j = 0; j < PARTS; ++j) top = fmaxf(top, ml[j].x);
+    const float ref = top == -INFINITY ? 0.f : top, back = exp2f(M - ref);
+    M = top;
+    L *= back;
+    float f[PARTS];
 #pragma unroll
-                for (int k = 0; k < ITEMS; ++k) {
-                    const int c = c0 + j;
-                    ml[k][j] = make_float2(-INFINITY, 0.f);
-                    v[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (c <= s.last) {
-                        const long long slot = part_slot(c, s.first);
-                        ml[k][j] = __ldcg(&a.ws.part_ml[slot * ROWS + r[k]]);
-                        v[k][j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + part_place<ROWS, BY_DIMS>(D, slot, r[k], d[k])));
-                    }
-                }
-            }
+    for (int j = 0; j < PARTS; ++j) {
+        f[j] = exp2f(ml[j].x - ref);
+        L = fmaf(ml[j].y, f[j], L);
+    }
 #pragma unroll
-            for (int k = 0; k < ITEMS; ++k) {
-                float top = M[k];
+    for (int k = 0; k < ITEMS; ++k) {
+        o[k].x *= back;
+        o[k].y *= back;
+        o[k].z *= back;
+        o[k].w *= back;
 #pragma unroll
-                for (int j = 0; j < PARTS; ++j) top = fmaxf(top, ml[k][j].x);
-                const float ref = top == -INFINITY ? 0.f : top, back = exp2f(M[k] - ref);
-                M[k] = top;
-                L[k] *= back;
-                o[k].x *= back;
-                o[k].y *= back;
-                o[k].z *= back;
-                o[k].w *= back;
-#pragma unroll
-                for (int j = 0; j < PARTS; ++j) {
-                    const float f = exp2f(ml[k][j].x - ref);
-                    L[k] = fmaf(ml[k][j].y, f, L[k]);
-                    o[k].x = fmaf(v[k][j].x, f, o[k].x);
-                    o[k].y = fmaf(v[k][j].y, f, o[k].y);
-                    o[k].z = fmaf(v[k][j].z, f, o[k].z);
-                    o[k].w = fmaf(v[k][j].w, f, o[k].w);
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            if (i0 + k * threads >= items) break;
-            const float inv = L[k] == 0.f ? 0.f : 1.f / L[k];
-            const int row = s.row0 + r[k], node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
-            const long long at = (long long)node * a.n_heads + hq;
-            T* out = static_cast<T*>(a.out) + at * D + d[k];
-            if constexpr (sizeof(T) == 4) {
-                *reinterpret_cast<float4*>(out) = make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv);
-            } else {
-                __nv_bfloat162 lo = __floats2bfloat162_rn(o[k].x * inv, o[k].y * inv), hi = __floats2bfloat162_rn(o[k].z * inv, o[k].w * inv);
-                uint2 w;
-                w.x = *reinterpret_cast<uint32_t*>(&lo);
-                w.y = *reinterpret_cast<uint32_t*>(&hi);
-                *reinterpret_cast<uint2*>(out) = w;
-            }
-            if (d[k] == 0 && a.lse) a.lse[at] = (M[k] + log2f(L[k])) * 0.69314718055994530942f;
+        for (int j = 0; j < PARTS; ++j) {
+            o[k].x = fmaf(v[k][j].x, f[j], o[k].x);
+            o[k].y = fmaf(v[k][j].y, f[j], o[k].y);
+            o[k].z = fmaf(v[k][j].z, f[j], o[k].z);
+            o[k].w = fmaf(v[k][j].w, f[j], o[k].w);
         }
     }
 }
 
-template <typename T, int ROWS, bool BY_DIMS = false>
+// Joins a unit's partial results: row r of the unit from the slots of CTAs first .. last, in that order. Every thread of a
+// CTA calls it; all partial results must be visible. What it costs is rounds of loads, each of which takes more than a
+// microsecond. Few rows (which have many parts: a long context): 8 parts at a time, 4 dimensions a thread. Many rows (D
+// given): two parts at a time, a warp takes 8 rows whole, so that it reads lines and writes sectors.
+template <typename T, int ROWS, int D, bool BY_DIMS = false>
 __device__ __forceinline__ void join_unit(const AttnArgs& a, const Segment& s, int tid, int threads) {
-    if (ROWS > 16 && s.rows * a.head_dim / 4 >= 2 * threads) join_items<T, ROWS, BY_DIMS, 4, 2>(a, s, tid, threads);
-    else join_items<T, ROWS, BY_DIMS, 1, 8>(a, s, tid, threads);
+    const int quads = a.head_dim / 4;
+    if constexpr (ROWS > 16) {
+        if (s.rows * quads >= 2 * threads) {
+#pragma unroll 1
+            for (int r0 = tid / 32 * 8; r0 < s.rows; r0 += threads / 4) {
+                const int r = min(r0 + tid % 8, s.rows - 1), d = tid / 8 % 4 * 4;
+                float M = -INFINITY, L = 0.f;
+                float4 o[D / 16] = {};
+#pragma unroll 1
+                for (int c = s.first; c <= s.last; c += 2) join_parts<ROWS, BY_DIMS, D / 16, 2>(a, s, c, r, d, M, L, o);
+                const float inv = L == 0.f ? 0.f : 1.f / L;
+                const int row = s.row0 + r, node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
+                const long long at = (long long)node * a.n_heads + hq;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) store_joined<T>(a, at, d + 16 * k, o[k], inv);
+                if (d == 0 && a.lse) a.lse[at] = (M + log2f(L)) * 0.69314718055994530942f;
+            }
+            return;
+        }
+    }
+#pragma unroll 1
+    for (int i = tid; i < s.rows * quads; i += threads) {
+        const int r = i / quads, d = (i - r * quads) * 4;
+        float M = -INFINITY, L = 0.f;
+        float4 o[1] = {};
+#pragma unroll 1
+        for (int c = s.first; c <= s.last; c += 8) join_parts<ROWS, BY_DIMS, 1, 8>(a, s, c, r, d, M, L, o);
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const int row = s.row0 + r, node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
+        const long long at = (long long)node * a.n_heads + hq;
+        store_joined<T>(a, at, d, o[0], inv);
+        if (d == 0 && a.lse) a.lse[at] = (M + log2f(L)) * 0.69314718055994530942f;
+    }
 }
 
 // One thread, after all of the CTA's partial results are visible on the device: true in the last CTA of the unit.
