@@ -29,7 +29,6 @@ __device__ __forceinline__ void cached8(const void* pool, long long row, int D, 
 
 template <typename T, bool FP8>
 __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ AttnArgs a) {
-    using W = Work<kRows, kKeys>;
     extern __shared__ __align__(16) float sm[];
     const int D = a.head_dim, P = pitch(D);
     float* sk = sm;
@@ -41,11 +40,11 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
     const int tid = threadIdx.x, row = tid >> 4, sub = tid & 15;
     Cursor cur{};
     bool more = false;
-    if (tid < 32) more = cursor_init<kRows, kKeys>(a, blockIdx.x, gridDim.x, cur);
+    if (tid < 32) more = cursor_init<kRows, kKeys, 0>(a, blockIdx.x, gridDim.x, cur);
     while (true) {
         if (tid < 32) {
             Segment s;
-            const bool ok = more && cursor_next<kRows, kKeys>(a, blockIdx.x, cur, s);
+            const bool ok = more && cursor_next<kRows, kKeys, 0>(a, blockIdx.x, cur, s);
             if (tid == 0) {
                 go = ok;
                 if (ok) seg = s;

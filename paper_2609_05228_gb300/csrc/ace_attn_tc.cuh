@@ -282,7 +282,7 @@ struct Walk {
 };
 
 // The CTA's segments, published by one warp ahead of the roles that work on them.
-template <int ROWS>
+template <int ROWS, int START>
 struct Scheduler {
     TcShared& m;
     const AttnArgs& a;
@@ -290,7 +290,7 @@ struct Scheduler {
     Cursor cur;
     bool more, done;
     __device__ __forceinline__ Scheduler(TcShared& m_, const AttnArgs& a_) : m(m_), a(a_), seg{}, cur{}, done(false) {
-        more = cursor_init<ROWS, kTcKeys>(a, blockIdx.x, gridDim.x, cur);
+        more = cursor_init<ROWS, kTcKeys, START>(a, blockIdx.x, gridDim.x, cur);
     }
     // The next segment, or that there is none. False: given up.
     __device__ __forceinline__ bool publish() {
@@ -300,7 +300,7 @@ struct Scheduler {
             return false;
         }
         Segment s{};
-        more = more && cursor_next<ROWS, kTcKeys>(a, blockIdx.x, cur, s);
+        more = more && cursor_next<ROWS, kTcKeys, START>(a, blockIdx.x, cur, s);
         if ((threadIdx.x & 31) == 0) {
             m.seg[seg.i].s = s;
             m.seg[seg.i].go = more;
@@ -313,9 +313,9 @@ struct Scheduler {
     }
 };
 
-template <int ROWS>
+template <int ROWS, int START>
 __device__ __forceinline__ void role_schedule(TcShared& m, const AttnArgs& a) {
-    Scheduler<ROWS> sched(m, a);
+    Scheduler<ROWS, START> sched(m, a);
     while (!sched.done && sched.publish()) {}
 }
 

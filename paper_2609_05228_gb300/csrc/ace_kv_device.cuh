@@ -78,12 +78,13 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int b) {
 // The work is a line of key tiles: request by request, in it unit by unit (head, then row block), in it tile by
 // tile. CTA c of g takes the tiles [c W / g, (c + 1) W / g), whatever units they belong to, so ragged
 // lengths load every SM alike; a unit cut by a boundary leaves partial results, joined by the CTA that finishes last.
-template <int ROWS, int KEYS>
+// START places of the line come before each unit's tiles: the time of as many tiles that its start and end cost.
+template <int ROWS, int KEYS, int START>
 struct Work {
     __device__ static int tiles(const Request& r) { return r.n > 0 ? (r.len + r.n + KEYS - 1) / KEYS : 0; }
     __device__ static int blocks(const AttnArgs& a, const Request& r) { return (r.n * a.group + ROWS - 1) / ROWS; }
     __device__ static long long of(const AttnArgs& a, const Request& r) {
-        return (long long)tiles(r) * blocks(a, r) * a.kv_heads;
+        return r.n > 0 ? (long long)(START + tiles(r)) * blocks(a, r) * a.kv_heads : 0;
     }
 };
 
@@ -104,12 +105,12 @@ __device__ __forceinline__ long long share_start(long long W, int c, int g) { re
 __device__ __forceinline__ int share_of(long long W, long long w, int g) { return (int)(((w + 1) * g - 1) / W); }
 
 // By one converged warp: the CTA's share. False: nothing to do.
-template <int ROWS, int KEYS>
+template <int ROWS, int KEYS, int START>
 __device__ bool cursor_init(const AttnArgs& a, int cta, int max_ctas, Cursor& c) {
     const int lane = threadIdx.x & 31;
     long long total = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32)
-        if (b0 + lane < a.B) total += Work<ROWS, KEYS>::of(a, request_of(a, b0 + lane));
+        if (b0 + lane < a.B) total += Work<ROWS, KEYS, START>::of(a, request_of(a, b0 + lane));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
     c.W = total;
@@ -119,7 +120,7 @@ __device__ bool cursor_init(const AttnArgs& a, int cta, int max_ctas, Cursor& c)
     c.w_end = share_start(total, cta + 1, c.ctas);
     long long base = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
-        const long long mine = b0 + lane < a.B ? Work<ROWS, KEYS>::of(a, request_of(a, b0 + lane)) : 0;
+        const long long mine = b0 + lane < a.B ? Work<ROWS, KEYS, START>::of(a, request_of(a, b0 + lane)) : 0;
         long long sum = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -139,19 +140,21 @@ __device__ bool cursor_init(const AttnArgs& a, int cta, int max_ctas, Cursor& c)
 }
 
 // The next segment of the share. False: the share is done.
-template <int ROWS, int KEYS>
+template <int ROWS, int KEYS, int START>
 __device__ bool cursor_next(const AttnArgs& a, int cta, Cursor& c, Segment& s) {
     if (c.w >= c.w_end) return false;
     Request r = request_of(a, c.b);
-    long long work = Work<ROWS, KEYS>::of(a, r);
+    long long work = Work<ROWS, KEYS, START>::of(a, r);
     while (c.w >= c.base + work) {
         c.base += work;
         r = request_of(a, ++c.b);
-        work = Work<ROWS, KEYS>::of(a, r);
+        work = Work<ROWS, KEYS, START>::of(a, r);
     }
-    const int tiles = Work<ROWS, KEYS>::tiles(r), blocks = Work<ROWS, KEYS>::blocks(a, r);
-    const long long unit = (c.w - c.base) / tiles;
-    const long long u0 = c.base + unit * tiles;
+    const int tiles = Work<ROWS, KEYS, START>::tiles(r), blocks = Work<ROWS, KEYS, START>::blocks(a, r);
+    const long long unit = (c.w - c.base) / (START + tiles);
+    const long long u0 = c.base + unit * (START + tiles) + START;      // place of its first tile
+    if (c.w < u0) c.w = u0;
+    if (c.w >= c.w_end) return false;
     s.b = c.b;
     s.head = (int)(unit / blocks);
     s.row0 = (int)(unit % blocks) * ROWS;
