@@ -2,7 +2,9 @@
 // (the tensor-core kernel takes bf16 with head sizes 64 and 128). With G query heads per kv head, a unit
 // is 16 rows (node, head of the group) of one request and kv head; a CTA walks its share of 64-key tiles:
 //   s_j = scale q.k_j,  m = max s,  p_j = 2^(s_j - m) (base 2),  l = sum p_j,  o = sum p_j v_j
-// with m, l and o rescaled when m grows (one pass over the cache). fp32 throughout.
+// with m, l and o rescaled when m grows (one pass over the cache). fp32 throughout. 16 rows by 64 keys keep K, V, q and
+// scores in shared memory for two CTAs an SM at D = 128; bound by shared-memory reads. For development and odd head sizes: 4
+// users of up to 777 positions, 6 nodes of 8 heads of 80, fp32: 19 us a call (of which 11 the host's).
 #include "ace_kv_device.cuh"
 
 namespace ace {

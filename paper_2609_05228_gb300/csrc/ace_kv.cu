@@ -77,9 +77,11 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
     }
 }
 
-// LANES lanes (a power of two, at least D / 8) hold one row, 8 elements each: its largest magnitude is
+// Write: e the least with amax 2^-e <= 448, scale byte e + 127, codes = the row's elements times 2^-e in e4m3 (the only
+// rounding). LANES lanes (a power of two, at least D / 8) hold one row, 8 elements each: its largest magnitude is
 // a shuffle reduction, nothing is read twice. Bound by memory: each group of lanes has kRowTurns neighbouring rows under way
-// together, and the rows are not waited for by way of their slots.
+// together, and the rows are not waited for by way of their slots. Write and read back of 16384 tokens (8 heads of 128, bf16
+// to fp8): 51 us for 201 MB, 4.0 TB/s (46 with the rows in L2, 61 then with one row at a time).
 constexpr int kRowTurns = 4;
 
 // Row r of a call: (token, K or V, head), heads fastest.
@@ -146,6 +148,7 @@ __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ RowArg
     }
 }
 
+// Read: code times 2^e, rounded to the storage type; the same lanes and turns as the write.
 template <typename T, bool FP8, int LANES>
 __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ RowArgs p) {
     const int sub = threadIdx.x % LANES;
@@ -219,7 +222,9 @@ constexpr int kKeepThreads = 256, kKeepWords = 4;
 
 // Block (request, share of the layers and heads); W is a word of 8 or 16 bytes. The path is looked up once; then all rows'
 // words, in the order (layer, head), node, move in passes. Rows move towards the front (path[i] >= i and
-// increasing), so a pass that has read its words before it writes any never overwrites a word of a later pass.
+// increasing), so a pass that has read its words before it writes any never overwrites a word of a later pass. Bound by
+// memory: 128 requests of up to 64 nodes, 48 layers of 8 heads of 128, bf16: 77 us for 352 MB, 4.6 TB/s (110 with a block a
+// layer, which looked the path up again); 32 of 16, 16 layers of 4: 8.9 us on the device, most of it the path's chain of loads.
 template <typename W>
 __global__ void __launch_bounds__(kKeepThreads) k_kv_keep(const __grid_constant__ KeepArgs p) {
     __shared__ int src_row[kMaxNodes], dst_row[kMaxNodes];          // of head 0
@@ -297,7 +302,8 @@ __global__ void __launch_bounds__(kKeepThreads) k_kv_keep(const __grid_constant_
     }
 }
 
-// Block per request: node i's chain of parents, walked in shared memory (a parent is below its node, so it ends).
+// Block per request: node i's chain of parents, walked in shared memory (a parent is below its node, so it ends). Bound by
+// the launch and the deepest chain.
 __global__ void __launch_bounds__(kMaxNodes) k_tree_mask(const int32_t* parents, const int32_t* node_offsets, int max_nodes,
                                                          int words, unsigned long long* mask, int32_t* depth) {
     __shared__ int par[kMaxNodes];

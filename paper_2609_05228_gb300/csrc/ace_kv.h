@@ -15,7 +15,7 @@ constexpr int kMaxHeadDim = 256;
 // Workspace of the attention kernels: a CTA's share of the work begins and ends inside a unit (request, head,
 // row block), so two partial results a CTA are enough for any batch.
 struct AttnWorkspace {
-    float* part_o = nullptr;            // [2 * ctas][rows of a unit][D] unnormalised outputs
+    float* part_o = nullptr;            // [2 * ctas][rows of a unit, D] unnormalised outputs (part_place)
     float2* part_ml = nullptr;          // [2 * ctas][rows of a unit] running maximum (base 2) and sum
     int* ticket = nullptr;              // [ctas] partial results that have arrived (zero between calls)
 };

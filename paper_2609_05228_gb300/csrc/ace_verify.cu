@@ -8,7 +8,9 @@
 // one for the argmax at the end. Later passes hit L2. No element is stored: with q's normalisations and the
 // residuals' gathered in scalars, the residual at v after k rejections is nu rho_k with
 //   rho_0 = 2^(z a + b),   rho_j = max(rho_(j-1) - c_j q, 0),   q <- 0 at x_j,
-// two operations a rejection and element (the passes of a request that rejects are bound by them).
+// two operations a rejection and element (the passes of a request that rejects are bound by them). Sums are fp32.
+// Measured: 64 requests of 16 nodes over 128000 tokens: 82 us (floor 19: the rows that are visited, once; the longest walk,
+// of some ten passes that wait for one another, bounds it). One request's chain of 8 over 32000: 25 us.
 #include <math.h>
 
 #include <string>
