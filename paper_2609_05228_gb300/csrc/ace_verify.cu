@@ -9,8 +9,8 @@
 // residuals' gathered in scalars, the residual at v after k rejections is nu rho_k with
 //   rho_0 = 2^(z a + b),   rho_j = max(rho_(j-1) - c_j q, 0),   q <- 0 at x_j,
 // two operations a rejection and element (the passes of a request that rejects are bound by them). Sums are fp32.
-// Measured: 64 requests of 16 nodes over 128000 tokens: 82 us (floor 19: the rows that are visited, once; the longest walk,
-// of some ten passes that wait for one another, bounds it). One request's chain of 8 over 32000: 25 us.
+// Measured: 64 requests of 16 nodes over 128000 tokens: 80 us (floor 19: the rows that are visited, once; the longest walk,
+// of some ten passes that wait for one another, bounds it). One request's chain of 8 over 32000: 17 us.
 #include <math.h>
 
 #include <string>
@@ -22,6 +22,7 @@ namespace {
 using namespace ace;
 
 constexpr int kVerThreads = 512, kVerWarps = kVerThreads / 32, kMaxCluster = 8;
+constexpr int kAheadVocab = 65536;
 constexpr int kPassUnroll = 2;          // loads of four elements a thread, row and turn of a pass (twice as many without the noise)
 
 struct VerifyArgs {
@@ -88,6 +89,7 @@ __device__ __forceinline__ Sums join_warp(Sums v, float inv_t) {
 struct Shared {
     Sums warp[kVerWarps];
     Sums cta[2][kMaxCluster];           // by turns, so that a fast CTA's next values find the other buffer
+    Sums node[kMaxCluster];             // AHEAD: every node's statistics
     int parent[kMaxNodes];
     int token[kMaxNodes];
     // the current node's children: logit and draft probability at their token, and u
@@ -97,9 +99,9 @@ struct Shared {
     int x[kMaxNodes];
 };
 
-// Joins every thread's value over the CTA, then over the cluster; all threads of all CTAs get the same bits.
+// Joins every thread's value over the CTA and writes it to `place` in the shared memory of all CTAs of the cluster.
 template <Join J>
-__device__ Sums join_all(Shared& sh, Sums v, float inv_t, int& turn, int ctas) {
+__device__ void hand_out(Shared& sh, Sums v, Sums* place, float inv_t, int ctas) {
     const int lane = threadIdx.x & 31;
     const Sums none{-INFINITY, 0.f, 0x7fffffff, 0};
     v = join_warp<J>(v, inv_t);
@@ -108,7 +110,7 @@ __device__ Sums join_all(Shared& sh, Sums v, float inv_t, int& turn, int ctas) {
     if (threadIdx.x < 32) {
         const Sums t = join_warp<J>(lane < kVerWarps ? sh.warp[lane % kVerWarps] : none, inv_t);
         if (lane < ctas) {                      // lane c hands it to CTA c
-            const uint32_t mine = smem_u32(&sh.cta[turn][cluster_rank()]);
+            const uint32_t mine = smem_u32(place);
             uint32_t there;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(lane));
             asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(there), "r"(__float_as_uint(t.m)),
@@ -117,6 +119,14 @@ __device__ Sums join_all(Shared& sh, Sums v, float inv_t, int& turn, int ctas) {
         }
         __syncwarp();
     }
+}
+
+// Joins every thread's value over the cluster; all threads of all CTAs get the same bits.
+template <Join J>
+__device__ Sums join_all(Shared& sh, Sums v, float inv_t, int& turn, int ctas) {
+    const int lane = threadIdx.x & 31;
+    const Sums none{-INFINITY, 0.f, 0x7fffffff, 0};
+    hand_out<J>(sh, v, &sh.cta[turn][cluster_rank()], inv_t, ctas);
     cluster_sync();
     const Sums r = join_warp<J>(lane < ctas ? sh.cta[turn][lane % kMaxCluster] : none, inv_t);
     turn ^= 1;
@@ -267,7 +277,9 @@ __device__ Sums row_stats(const T* z, int lo, int hi, int none, float inv_t, boo
     return v;
 }
 
-template <typename T, bool DRAFT, bool VEC>
+// AHEAD: all nodes' statistics at once before the walk, a row a CTA (so no tree has more nodes than the cluster CTAs), and what
+// the walk asks of their children: then a step down costs no pass.
+template <typename T, bool DRAFT, bool VEC, bool AHEAD>
 __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant__ VerifyArgs p) {
     __shared__ Shared sh;
     uint32_t n_ctas;
@@ -291,6 +303,21 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
     if (n > 0 && !greedy) prefetch_row(noise, lo, hi);
     // every CTA of the cluster has started before another writes into its shared memory
     cluster_sync();
+    if constexpr (AHEAD) {
+        if (tid < n && sh.parent[tid] >= 0) {
+            const int of = sh.parent[tid], x = sh.token[tid];
+            if (x >= 0 && x < V) {
+                sh.zx[tid] = to_f32(static_cast<const T*>(p.logits)[(o0 + of) * p.logits_stride + x]);
+                sh.qx[tid] = DRAFT ? p.draft[(o0 + of) * p.draft_stride + x] : 1.f;
+                sh.u[tid] = p.uniforms[o0 + tid];
+            }
+        }
+        if (rank < n) {
+            const Sums v = row_stats(static_cast<const T*>(p.logits) + (o0 + rank) * p.logits_stride, 0, V, V, inv_t, greedy);
+            hand_out<kStats>(sh, v, &sh.node[rank], inv_t, ctas);
+        }
+        cluster_sync();
+    }
     while (n > 0) {
         if (rank == 0 && tid == 0) p.path[(long long)b * p.max_nodes + keep] = node;
         ++keep;
@@ -301,18 +328,23 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
         while (first < n && sh.parent[first] != node) ++first;
         if (first < n) {
             if (DRAFT && !greedy) prefetch_row(qrow, lo, hi);
-            prefetch_row(static_cast<const T*>(p.logits) + (o0 + first) * p.logits_stride, lo, hi);
+            if (!AHEAD) prefetch_row(static_cast<const T*>(p.logits) + (o0 + first) * p.logits_stride, lo, hi);
         }
-        // (a later node's children may lie in the same places: the walk has passed a barrier since it read them)
-        for (int c = node + 1 + tid; c < n; c += kVerThreads) {
-            const int x = sh.token[c];
-            if (sh.parent[c] != node || x < 0 || x >= V) continue;
-            sh.zx[c] = to_f32(z[x]);
-            sh.qx[c] = DRAFT ? qrow[x] : 1.f;
-            sh.u[c] = p.uniforms[o0 + c];
+        Sums v;
+        if constexpr (AHEAD) {
+            v = sh.node[node];
+        } else {
+            // (a later node's children may lie in the same places: the walk has passed a barrier since it read them)
+            for (int c = node + 1 + tid; c < n; c += kVerThreads) {
+                const int x = sh.token[c];
+                if (sh.parent[c] != node || x < 0 || x >= V) continue;
+                sh.zx[c] = to_f32(z[x]);
+                sh.qx[c] = DRAFT ? qrow[x] : 1.f;
+                sh.u[c] = p.uniforms[o0 + c];
+            }
+            v = row_stats(z, lo, hi, V, inv_t, greedy);
+            v = join_all<kStats>(sh, v, inv_t, turn, ctas);
         }
-        Sums v = row_stats(z, lo, hi, V, inv_t, greedy);
-        v = join_all<kStats>(sh, v, inv_t, turn, ctas);
         if (v.bad || v.m == -INFINITY) break;               // token stays -1
         w.a = inv_t * 1.4426950408889634f;
         w.b = -v.m * w.a;
@@ -417,6 +449,9 @@ ace_status ver_fail(ace_status st, const std::string& m) {
 
 template <typename T, bool DRAFT, bool VEC>
 cudaError_t launch_verify(const VerifyArgs& p, int B, int ctas, cudaStream_t s) {
+    // statistics ahead pay from the second node on that a walk visits, for what a whole row costs a CTA more than its share: a
+    // chain of 8 over 32000 tokens 17 us and not 25; over 128000 25 to 29 and, as the walk goes, 19 to 38 without
+    const bool ahead = p.max_nodes > 1 && p.max_nodes <= ctas && p.vocab <= kAheadVocab;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)B * ctas);
     cfg.blockDim = dim3(kVerThreads);
@@ -427,7 +462,7 @@ cudaError_t launch_verify(const VerifyArgs& p, int B, int ctas, cudaStream_t s) 
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_verify<T, DRAFT, VEC>, p);
+    return ahead ? cudaLaunchKernelEx(&cfg, k_verify<T, DRAFT, VEC, true>, p) : cudaLaunchKernelEx(&cfg, k_verify<T, DRAFT, VEC, false>, p);
 }
 
 template <typename T>

@@ -610,6 +610,22 @@ def test_verify_filtered_and_broken_rows():
     _check_verify(c, _run_verify(c, 4), 4)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("V", [20000, 20003])
+def test_verify_few_requests_with_small_trees(dtype, draft, V):
+    """Trees on both sides of a node a CTA; a NaN in a row that no walk visits is nothing to the others."""
+    rng = np.random.default_rng(V)
+    sizes = [2, 8, 1, 0, 5, 9, 7, 8]
+    c = _verify_case(rng, sizes, V, dtype, draft, temps=[1.0, 0.8, 1.0, 1.0, 0.0, 1.2, 0.0, 1.0])
+    c["parents"][7] = [-1, 0, 1, 2, 3, 4, 0, 0]
+    o = c["off"][7]
+    c["tokens"][o + 1] = -1                         # never accepted, so nodes 2 to 5 are not visited
+    c["logits"][o + 2, 11] = float("nan")
+    c["logits"][o + 4] = float("-inf")
+    _check_verify(c, _run_verify(c, 9), 9)
+
+
 def test_verify_is_lossless():
     """The first token after the root follows the target's distribution whatever the draft is: 20000 walks over
     12 tokens, each frequency within five standard deviations."""
