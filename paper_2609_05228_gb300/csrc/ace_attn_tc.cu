@@ -1,10 +1,10 @@
 // ace_attn_tc.cu — attention for trees of drafted tokens on the tensor cores (bf16 activations, head sizes 64 and
-// 128, plain and fp8 caches): flash attention with the keys of a request split over CTAs by the work line of
-// ace_kv_device.cuh.
+// 128, plain and fp8 caches): one pass over the cached rows with a softmax's running maximum and sum, the keys of a request
+// split over CTAs by the work line of ace_kv_device.cuh.
 //
 // A unit is one request, kv head and block of query rows r = node * G + g (G query heads share a kv head, so
 // they share its cached rows too). A CTA walks key tiles of 128 positions:
-//   S = Q K^T              tcgen05.mma, 128 x 128 fp32 in TMEM
+//   S = Q K^T              tcgen05.mma, 128 x 64 fp32 in TMEM an item
 //   P = 2^(S - m), l += P  softmax warps, a thread per row; P goes back to TMEM as bf16 / fp16
 //   O += P V               tcgen05.mma, A = P from TMEM, B = V as stored (its rows are K indices)
 // In items of 64 positions, two groups of four softmax warps and two accumulators: with RT = 2 a group has a block of 128
@@ -15,8 +15,9 @@
 // and not 123, bf16 168 and not 130.)
 // fp8 caches: K's codes are the B operand as stored (kind::f8f6f4), against q split into two e4m3 terms, which
 // hold 8 significant bits, all of a bf16 q (elements 2^-10 and more below the row's largest lose their last bits, a
-// 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory (exact), with
-// their scales on P: P V accumulates in units of 2^eref, a power of two above the scales seen so far.
+// 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory with their scales, in units
+// of 2^eref, a power of two above the scales seen so far: exact but for rows whose scale is 2^-20 of the largest and less, whose
+// codes' last bits fall under fp16's least.
 // P is rounded to bf16 (2^-9 of a weight; plain caches) or fp16 (2^-12), as the products need; sums, maxima and O are fp32.
 // Measured: 8 users of up to 16384 positions, 128 nodes of 64 heads (8 kv heads of 128), bf16: 297 us, 870 TFLOP/s. 64 users
 // of up to 8192, 4 kv heads of 128: 64 rows a unit 119 us fp8, 127 bf16; 128 rows 155 and 131; 192 rows 220 and 159. Bound by
@@ -30,8 +31,8 @@ namespace ace {
 namespace {
 
 constexpr int kHalf = 64;               // positions of an item
-// A unit's start and end in tiles of the work line: 7 us or so (64 users, at most 8192 positions, 64 rows a unit: 119 us
-// with 6, 121 with 4, 137 without).
+// A unit's start and end in tiles of the work line (64 users, at most 8192 positions, 64 fp8 rows a unit: 118 us with 9, 119
+// with 6, 121 with 4, 137 without; 192 rows: 222, 219, 220, 232).
 constexpr int kTcStart = 7;
 
 template <bool FP8, int D, int RT, int CP>
@@ -67,9 +68,9 @@ static_assert(tc_smem<false, 128, 2, 1>() <= 232448 && tc_smem<false, 128, 1, 2>
 static_assert(tc_smem<true, 128, 2, 1>() <= 232448 && tc_smem<true, 128, 1, 2>() <= 232448, "shared memory");
 static_assert(tc_smem<false, 64, 2, 1>() <= 232448 && tc_smem<true, 64, 1, 2>() <= 232448, "shared memory");
 
-// The tile's loops are rolled (32 scores a turn) on purpose: unrolled over a tile's 128 scores they and the fp16
-// conversion overflow the instruction cache, and warps that run different roles then stall on fetches (a fp8 tile of
-// 128 rows 9600 cycles unrolled; no_instruction stalls 2.7 an issue against 0.5).
+// An item's 64 scores stay in registers, and its code is as long as the instruction cache bears beside the other roles': with
+// 128 scores unrolled, and the conversion, warps of different roles stalled on fetches (no_instruction 2.7 an issue, now 0.6
+// to 0.9); read twice from TMEM, 32 at a time, they took twice the cycles of the second pass.
 
 // 32 of a row's scores with fp8 rows' scales, and -inf where the row does not see the position.
 template <bool FP8>
@@ -712,8 +713,8 @@ cudaError_t tc_go(const TcAttnArgs& p, int ctas, cudaStream_t s) {
 
 template <bool FP8, int D>
 cudaError_t tc_launch(const TcAttnArgs& p, int ctas, cudaStream_t s) {
-    // by the rows of the largest tree: one block of 128 rows a unit where that holds them (as often as it can), else two
-    // that share the loaded tiles
+    // by the rows of the largest tree: one block of 128 rows a unit where that holds them (twice, if it can), else two that
+    // share the loaded tiles
     const long long rows = (long long)p.a.max_nodes * p.a.group;
     if (rows <= 64) return tc_go<FP8, D, 1, 2>(p, ctas, s);
     if (rows <= 128) return tc_go<FP8, D, 1, 1>(p, ctas, s);
