@@ -10,7 +10,7 @@
 namespace ace {
 namespace {
 
-constexpr int kRows = 16, kKeys = 64, kThreads = 256;
+constexpr int kRows = 16, kKeys = 64, kThreads = 256, kJoinParts = 8;
 
 __host__ __device__ constexpr int pitch(int D) { return D + 4; }   // floats a row: 16-byte chunks of 8 rows in distinct banks
 int core_smem(int D) { return (2 * kKeys * pitch(D) + kRows * pitch(D) + kRows * kKeys) * 4; }
@@ -38,10 +38,11 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
     float* sq = sv + kKeys * P;
     float* sp = sq + kRows * P;
     __shared__ Segment seg;
-    __shared__ int go, joins;
+    __shared__ int go;
     const int tid = threadIdx.x, row = tid >> 4, sub = tid & 15;
     Cursor cur{};
     bool more = false;
+    if (tid == 0) note_none(a);
     if (tid < 32) more = cursor_init<kRows, kKeys, 0>(a, blockIdx.x, gridDim.x, cur);
     while (true) {
         if (tid < 32) {
@@ -49,7 +50,10 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
             const bool ok = more && cursor_next<kRows, kKeys, 0>(a, blockIdx.x, cur, s);
             if (tid == 0) {
                 go = ok;
-                if (ok) seg = s;
+                if (ok) {
+                    seg = s;
+                    note_unit(a, s);
+                }
             }
         }
         __syncthreads();
@@ -188,15 +192,84 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
             }
             if (sub == 0) a.ws.part_ml[slot] = make_float2(m, l);
         }
-        __threadfence();
         __syncthreads();
-        if (tid == 0) joins = last_of_unit(a, s);
-        __syncthreads();
-        if (joins) {
-            __threadfence();
-            join_unit<T, kRows, 0>(a, s, tid, kThreads);
-        }
     }
+}
+
+// Joins the units that were cut: block (CTA, 8 rows), where the CTA's note names the unit that begins in it; parts in the
+// line's order, 8 at a time (a round of loads takes more than a microsecond), 4 dimensions a thread, with the reference that they
+// turn up with: what came before is rescaled as it grows. A kernel of its own, so that all SMs join: when the last CTA of
+// a unit joined it, that took 10 us for 128 rows of two parts and 20 for 40 rows of 19. Bound by the launch and its loads.
+template <typename T, bool BY_DIMS>
+__global__ void __launch_bounds__(kThreads) k_attn_join(const __grid_constant__ AttnArgs a, int rows) {
+    pdl_wait();
+    const int r0 = blockIdx.y * 8;
+    if (r0 >= a.ws.unit[blockIdx.x].rows) return;
+    const Segment s = a.ws.unit[blockIdx.x];
+    const int D = a.head_dim, quads = D / 4;
+    for (int i = threadIdx.x; i < 8 * quads; i += kThreads) {
+        // by dimensions: 8 rows of 4 quads a warp, lines of the parts and sectors of the output
+        const int r = r0 + (BY_DIMS ? i % 8 : i / quads), d = (BY_DIMS ? i / 8 : i % quads) * 4;
+        if (r >= s.rows) continue;
+        float M = -INFINITY, L = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c0 = s.first; c0 <= s.last; c0 += kJoinParts) {
+            float2 ml[kJoinParts];
+            float4 v[kJoinParts];
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) {
+                ml[j] = make_float2(-INFINITY, 0.f);
+                v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (c0 + j <= s.last) {
+                    const long long slot = part_slot(c0 + j, s.first);
+                    ml[j] = __ldcg(&a.ws.part_ml[slot * rows + r]);
+                    v[j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + part_place<BY_DIMS>(rows, D, slot, r, d)));
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) top = fmaxf(top, ml[j].x);
+            const float ref = top == -INFINITY ? 0.f : top, back = exp2f(M - ref);
+            M = top;
+            L *= back;
+            o = make_float4(o.x * back, o.y * back, o.z * back, o.w * back);
+#pragma unroll
+            for (int j = 0; j < kJoinParts; ++j) {
+                const float f = exp2f(ml[j].x - ref);
+                L = fmaf(ml[j].y, f, L);
+                o.x = fmaf(v[j].x, f, o.x);
+                o.y = fmaf(v[j].y, f, o.y);
+                o.z = fmaf(v[j].z, f, o.z);
+                o.w = fmaf(v[j].w, f, o.w);
+            }
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const int row = s.row0 + r, node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
+        const long long at = (long long)node * a.n_heads + hq;
+        T* out = static_cast<T*>(a.out) + at * D + d;
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        } else {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+            *reinterpret_cast<uint2*>(out) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+        if (d == 0 && a.lse) a.lse[at] = (M + log2f(L)) * 0.69314718055994530942f;
+    }
+}
+
+template <typename T, bool BY_DIMS>
+cudaError_t join_of(const AttnArgs& a, int rows, int ctas, cudaStream_t s) {
+    const long long most = (long long)a.max_nodes * a.group;       // rows of the largest request
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas, (unsigned)(((most < rows ? most : rows) + 7) / 8));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_attn_join<T, BY_DIMS>, a, rows);
 }
 
 template <typename T, bool FP8>
@@ -223,15 +296,14 @@ cudaError_t attn_init(ace_kv* kv) {
         rows = kRows;
     }
     if (e != cudaSuccess) return e;
-    // error word, tickets, maxima and sums, outputs
-    const size_t head = (256 + ctas * sizeof(int) + 255) / 256 * 256, ml = (2 * ctas * rows * sizeof(float2) + 255) / 256 * 256;
+    // error word, notes of units, maxima and sums, outputs
+    const size_t head = (256 + ctas * sizeof(Segment) + 255) / 256 * 256, ml = (2 * ctas * rows * sizeof(float2) + 255) / 256 * 256;
     if ((e = cudaMalloc(&kv->block, head + ml + 2 * ctas * rows * D.head_dim * sizeof(float))) != cudaSuccess) return e;
     char* at = static_cast<char*>(kv->block);
     kv->err = reinterpret_cast<int*>(at);
-    kv->ws.ticket = reinterpret_cast<int*>(at + 256);
+    kv->ws.unit = reinterpret_cast<Segment*>(at + 256);
     kv->ws.part_ml = reinterpret_cast<float2*>(at + head);
     kv->ws.part_o = reinterpret_cast<float*>(at + head + ml);
-    kv->tickets = (int)ctas;
     return cudaMemsetAsync(at, 0, head, kv->last_stream);
 }
 
@@ -246,7 +318,13 @@ cudaError_t launch_tree_attention(const ace_kv* kv, const AttnArgs& a, cudaStrea
         if (fp8) k_attn_core<float, true><<<grid, kThreads, smem, s>>>(a);
         else k_attn_core<float, false><<<grid, kThreads, smem, s>>>(a);
     }
-    return cudaGetLastError();
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? launch_join(a, kv->desc.dtype, false, kRows, grid, s) : e;
+}
+
+cudaError_t launch_join(const AttnArgs& a, int dtype, bool by_dims, int rows, int ctas, cudaStream_t s) {
+    if (dtype != ACE_BF16) return join_of<float, false>(a, rows, ctas, s);
+    return by_dims ? join_of<__nv_bfloat16, true>(a, rows, ctas, s) : join_of<__nv_bfloat16, false>(a, rows, ctas, s);
 }
 
 }  // namespace ace

@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
         if (!ok) *abort_flag = 1;
     } else {
         // ------------------------------------------------ softmax: group g of 4 warps, a thread per position of a tile
-        const int g = (warp - 4) >> 2, quad = warp & 3, key = quad * 32 + lane, tid = threadIdx.x - 128;
+        const int g = (warp - 4) >> 2, quad = warp & 3, key = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t s_t = tmem + lanes + C::S + (uint32_t)(g * C::SN), o_t = tmem + lanes + C::O + (uint32_t)(g * C::ON);
         unsigned char* p_out = smem + C::OFF_P + g * C::P + key * 16;
@@ -629,16 +629,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 __syncwarp();
             }
             tc_fence_before();
-            if (!whole) __threadfence();
-            if (RG == 1 || !whole) meet(3, 256);        // O may be overwritten, partial results are written
-            if (!whole) {
-                if (tid == 0) m.joins = last_of_unit(a, s);
-                meet(3, 256);
-                if (m.joins) {
-                    __threadfence();
-                    join_unit<__nv_bfloat16, C::ROWS, D>(a, s, tid, 256);
-                }
-            }
+            if (RG == 1) meet(3, 256);          // O may be overwritten
             walk.done();
         }
     }
@@ -664,7 +655,8 @@ cudaError_t few_attrs() {
 template <bool FP8, int D, int NR, int RG>
 cudaError_t few_run(const TcAttnArgs& p, int ctas, cudaStream_t s) {
     k_attn_few<FP8, D, NR, RG><<<ctas, kTcThreads, few_smem<FP8, D, NR, RG>(), s>>>(p);
-    return cudaGetLastError();
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? launch_join(p.a, ACE_BF16, false, FewCfg<FP8, D, NR, RG>::ROWS, ctas, s) : e;
 }
 
 template <bool FP8, int D>

@@ -468,7 +468,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     } else {
         // ------------------------------------------------ softmax: group g of 4 warps, a thread per row
         const int g = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
-        const int tid = threadIdx.x - 128;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t s_t = tmem + lanes, o_t = tmem + lanes + kO + (uint32_t)(g * D);
         uint32_t s_phase = 0, soft_phase = 0;         // s_phase: bit i of the group's two buffers, of S and of its product
@@ -671,18 +670,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 else if (a.lse) a.lse[at] = (m_all + log2f(l_all)) * 0.69314718055994530942f;
             }
             tc_fence_before();
-            if (RT == 1 || !whole) {
-                if (!whole) __threadfence();
-                if (!soft_sync()) { ok = false; break; }        // O and ml may be overwritten, partial results are written
-                if (!whole) {
-                    if (tid == 0) m.joins = last_of_unit(a, s);
-                    if (!soft_sync()) { ok = false; break; }
-                    if (m.joins) {
-                        __threadfence();
-                        join_unit<__nv_bfloat16, ROWS, D, CP == 1>(a, s, tid, 256);
-                    }
-                }
-            }
+            if (RT == 1 && !soft_sync()) { ok = false; break; }         // O and ml may be overwritten
             walk.done();
         }
         if (!ok) *abort_flag = 1;
@@ -708,7 +696,8 @@ cudaError_t tc_attrs() {
 template <bool FP8, int D, int RT, int CP>
 cudaError_t tc_go(const TcAttnArgs& p, int ctas, cudaStream_t s) {
     k_attn_tc<FP8, D, RT, CP><<<ctas, kTcThreads, tc_smem<FP8, D, RT, CP>(), s>>>(p);
-    return cudaGetLastError();
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? launch_join(p.a, ACE_BF16, CP == 1, Cfg<FP8, D, RT, CP>::ROWS, ctas, s) : e;
 }
 
 template <bool FP8, int D>

@@ -44,7 +44,7 @@ struct TcShared {
     uint64_t s_full[4], p_ready[4], o_done[4], q_full, q_free, drain[2];
     uint64_t seg_full[kSegRing], seg_empty[kSegRing], aux_full[kAuxRing], aux_empty[kAuxRing];
     uint32_t tmem;
-    int abort_flag, joins, pad;
+    int abort_flag, pad[2];
     TcSegment seg[kSegRing];
     int eref[kAuxRing];
 };
@@ -178,7 +178,7 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment&
                 __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + ((long long)(s.node0 + nd) * a.n_heads + hq) * a.head_dim + i;
                 *out = from_f32<__nv_bfloat16>(to_f32(*out) + v);
             } else {
-                a.ws.part_o[part_place<ROWS, BY_DIMS>(a.head_dim, s.part, urow, i)] += v;
+                a.ws.part_o[part_place<BY_DIMS>(ROWS, a.head_dim, s.part, urow, i)] += v;
             }
         }
     }
@@ -290,6 +290,7 @@ struct Scheduler {
     Cursor cur;
     bool more, done;
     __device__ __forceinline__ Scheduler(TcShared& m_, const AttnArgs& a_) : m(m_), a(a_), seg{}, cur{}, done(false) {
+        if ((threadIdx.x & 31) == 0) note_none(a);
         more = cursor_init<ROWS, kTcKeys, START>(a, blockIdx.x, gridDim.x, cur);
     }
     // The next segment, or that there is none. False: given up.
@@ -304,6 +305,7 @@ struct Scheduler {
         if ((threadIdx.x & 31) == 0) {
             m.seg[seg.i].s = s;
             m.seg[seg.i].go = more;
+            if (more) note_unit(a, s);
             for (int w = 0; w < kMaxNodes / 64; ++w) m.seg[seg.i].bad[w] = 0;
             mbar_arrive(&m.seg_full[seg.i]);
         }

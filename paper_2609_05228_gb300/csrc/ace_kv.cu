@@ -446,8 +446,6 @@ ace_status ace_kv_sync(ace_kv* kv) {
     if (!err) return ACE_OK;
     if ((e = cudaMemset(kv->err, 0, sizeof(int))) != cudaSuccess) return kv_cuda(e, "clear device error word");
     if (err & kErrTimeout) {
-        // a kernel that gave up may have left tickets
-        if ((e = cudaMemset(kv->ws.ticket, 0, kv->tickets * sizeof(int))) != cudaSuccess) return kv_cuda(e, "clear tickets");
         return kv_fail(ACE_ERR_TIMEOUT, "a bounded device wait ran out");
     }
     return kv_fail(ACE_ERR_INVALID_ARG, "a slot, page, length, offset or path in device memory was out of range and left out");

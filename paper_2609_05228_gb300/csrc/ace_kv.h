@@ -12,12 +12,21 @@ constexpr int kErrIndex = 8;
 constexpr int kMaxNodes = 256;          // nodes of a request's tree
 constexpr int kMaxHeadDim = 256;
 
+// A CTA's part of a unit.
+struct Segment {
+    int b, head, row0, rows;        // request, kv head, first row of the unit (node * G + g) and its rows
+    int node0, len, n;              // the request
+    int tile0, tile1;               // key tiles of this CTA
+    int part;                       // partial result slot, -1: the whole unit is here
+    int first, last;                // CTAs that share the unit
+};
+
 // Workspace of the attention kernels: a CTA's share of the work begins and ends inside a unit (request, head,
 // row block), so two partial results a CTA are enough for any batch.
 struct AttnWorkspace {
     float* part_o = nullptr;            // [2 * ctas][rows of a unit, D] unnormalised outputs (part_place)
     float2* part_ml = nullptr;          // [2 * ctas][rows of a unit] running maximum (base 2) and sum
-    int* ticket = nullptr;              // [ctas] partial results that have arrived (zero between calls)
+    Segment* unit = nullptr;            // [ctas] the cut unit that begins in a CTA (rows = 0: none)
 };
 
 struct KvMaps {                         // tensor-core attention (head sizes 64 and 128, bf16)
@@ -39,7 +48,6 @@ struct ace_kv {
     void* block = nullptr;              // one allocation for what follows
     int* err = nullptr;
     ace::AttnWorkspace ws;
-    int tickets = 0;
     int core_ctas_per_sm = 1;           // CUDA-core attention
     bool tc = false;                    // tensor-core attention in use
     ace::KvMaps maps;
@@ -71,6 +79,8 @@ struct AttnArgs {
 
 cudaError_t attn_init(ace_kv* kv);      // kernel attributes, workspace, tensor maps
 cudaError_t launch_tree_attention(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
+// Joins the partial results of the kernel before: units of `rows` rows, `ctas` CTAs.
+cudaError_t launch_join(const AttnArgs& a, int dtype, bool by_dims, int rows, int ctas, cudaStream_t s);
 // tensor-core kernel (ace_attn_tc.cu): bf16, head sizes 64 and 128
 constexpr int kTcMaxRows = 256;         // rows of a unit
 bool attn_tc_supported(const ace_kv* kv);

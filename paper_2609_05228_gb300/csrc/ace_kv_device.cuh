@@ -77,7 +77,7 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int b) {
 
 // The work is a line of key tiles: request by request, in it unit by unit (head, then row block), in it tile by
 // tile. CTA c of g takes the tiles [c W / g, (c + 1) W / g), whatever units they belong to, so ragged
-// lengths load every SM alike; a unit cut by a boundary leaves partial results, joined by the CTA that finishes last.
+// lengths load every SM alike; a unit cut by a boundary leaves partial results, which a kernel after this one joins.
 // START places of the line come before each unit's tiles: the time of as many tiles that its start and end cost.
 template <int ROWS, int KEYS, int START>
 struct Work {
@@ -86,14 +86,6 @@ struct Work {
     __device__ static long long of(const AttnArgs& a, const Request& r) {
         return r.n > 0 ? (long long)(START + tiles(r)) * blocks(a, r) * a.kv_heads : 0;
     }
-};
-
-struct Segment {
-    int b, head, row0, rows;        // request, kv head, first row of the unit (node * G + g) and its rows
-    int node0, len, n;              // the request
-    int tile0, tile1;               // key tiles of this CTA
-    int part;                       // partial result slot, -1: the whole unit is here
-    int first, last;                // CTAs that share the unit
 };
 
 struct Cursor {
@@ -204,123 +196,17 @@ __device__ __forceinline__ unsigned long long sees_word(const AttnArgs& a, int n
     return left >= 64 ? m : m & ((1ull << left) - 1ull);
 }
 
-// Place of dimension d of row r in partial result `slot`: by rows, or (BY_DIMS) by 4 dimensions and then rows, for kernels
-// in which a thread holds a row.
-template <int ROWS, bool BY_DIMS>
-__device__ __forceinline__ long long part_place(int D, long long slot, int r, int d) {
-    return BY_DIMS ? ((slot * (D / 4) + d / 4) * ROWS + r) * 4 + d % 4 : (slot * ROWS + r) * D + d;
+// Place of dimension d of row r in partial result `slot` (ROWS rows each): by rows, or (BY_DIMS) by 4 dimensions and then
+// rows, for kernels in which a thread holds a row.
+template <bool BY_DIMS>
+__device__ __forceinline__ long long part_place(int rows, int D, long long slot, int r, int d) {
+    return BY_DIMS ? ((slot * (D / 4) + d / 4) * rows + r) * 4 + d % 4 : (slot * rows + r) * D + d;
 }
 
-// 4 dimensions of an output row.
-template <typename T>
-__device__ __forceinline__ void store_joined(const AttnArgs& a, long long at, int d, float4 o, float inv) {
-    T* out = static_cast<T*>(a.out) + at * a.head_dim + d;
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    } else {
-        __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
-        uint2 w;
-        w.x = *reinterpret_cast<uint32_t*>(&lo);
-        w.y = *reinterpret_cast<uint32_t*>(&hi);
-        *reinterpret_cast<uint2*>(out) = w;
-    }
-}
-
-// A row's partial results over parts c0 .. c0 + PARTS - 1 of a unit, 4 dimensions at each of ITEMS places, onto what came
-// before: with the reference that they turn up with, rescaled as it grows.
-template <int ROWS, bool BY_DIMS, int ITEMS, int PARTS>
-__device__ __forceinline__ void join_parts(const AttnArgs& a, const Segment& s, int c0, int r, int d, float& M, float& L, float4 (&o)[ITEMS]) {
-    float2 ml[PARTS];
-    float4 v[ITEMS][PARTS];
-#pragma unroll
-    for (int j = 0; j < PARTS; ++j) {
-        const int c = c0 + j;
-        ml[j] = make_float2(-INFINITY, 0.f);
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) v[k][j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c <= s.last) {
-            const long long slot = part_slot(c, s.first);
-            ml[j] = __ldcg(&a.ws.part_ml[slot * ROWS + r]);
-#pragma unroll
-            for (int k = 0; k < ITEMS; ++k)
-                v[k][j] = __ldcg(reinterpret_cast<const float4*>(a.ws.part_o + part_place<ROWS, BY_DIMS>(a.head_dim, slot, r, d + 16 * k)));
-        }
-    }
-    float top = M;
-#pragma unroll
-    for (int j = 0; j < PARTS; ++j) top = fmaxf(top, ml[j].x);
-    const float ref = top == -INFINITY ? 0.f : top, back = exp2f(M - ref);
-    M = top;
-    L *= back;
-    float f[PARTS];
-#pragma unroll
-    for (int j = 0; j < PARTS; ++j) {
-        f[j] = exp2f(ml[j].x - ref);
-        L = fmaf(ml[j].y, f[j], L);
-    }
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        o[k].x *= back;
-        o[k].y *= back;
-        o[k].z *= back;
-        o[k].w *= back;
-#pragma unroll
-        for (int j = 0; j < PARTS; ++j) {
-            o[k].x = fmaf(v[k][j].x, f[j], o[k].x);
-            o[k].y = fmaf(v[k][j].y, f[j], o[k].y);
-            o[k].z = fmaf(v[k][j].z, f[j], o[k].z);
-            o[k].w = fmaf(v[k][j].w, f[j], o[k].w);
-        }
-    }
-}
-
-// Joins a unit's partial results: row r of the unit from the slots of CTAs first .. last, in that order. Every thread of a
-// CTA calls it; all partial results must be visible. What it costs is rounds of loads, each of which takes more than a
-// microsecond. Few rows (which have many parts: a long context): 8 parts at a time, 4 dimensions a thread. Many rows (D
-// given): two parts at a time, a warp takes 8 rows whole, so that it reads lines and writes sectors.
-template <typename T, int ROWS, int D, bool BY_DIMS = false>
-__device__ __forceinline__ void join_unit(const AttnArgs& a, const Segment& s, int tid, int threads) {
-    const int quads = a.head_dim / 4;
-    if constexpr (ROWS > 16) {
-        if (s.rows * quads >= 2 * threads) {
-#pragma unroll 1
-            for (int r0 = tid / 32 * 8; r0 < s.rows; r0 += threads / 4) {
-                const int r = min(r0 + tid % 8, s.rows - 1), d = tid / 8 % 4 * 4;
-                float M = -INFINITY, L = 0.f;
-                float4 o[D / 16] = {};
-#pragma unroll 1
-                for (int c = s.first; c <= s.last; c += 2) join_parts<ROWS, BY_DIMS, D / 16, 2>(a, s, c, r, d, M, L, o);
-                const float inv = L == 0.f ? 0.f : 1.f / L;
-                const int row = s.row0 + r, node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
-                const long long at = (long long)node * a.n_heads + hq;
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) store_joined<T>(a, at, d + 16 * k, o[k], inv);
-                if (d == 0 && a.lse) a.lse[at] = (M + log2f(L)) * 0.69314718055994530942f;
-            }
-            return;
-        }
-    }
-#pragma unroll 1
-    for (int i = tid; i < s.rows * quads; i += threads) {
-        const int r = i / quads, d = (i - r * quads) * 4;
-        float M = -INFINITY, L = 0.f;
-        float4 o[1] = {};
-#pragma unroll 1
-        for (int c = s.first; c <= s.last; c += 8) join_parts<ROWS, BY_DIMS, 1, 8>(a, s, c, r, d, M, L, o);
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        const int row = s.row0 + r, node = s.node0 + row / a.group, hq = s.head * a.group + row % a.group;
-        const long long at = (long long)node * a.n_heads + hq;
-        store_joined<T>(a, at, d, o[0], inv);
-        if (d == 0 && a.lse) a.lse[at] = (M + log2f(L)) * 0.69314718055994530942f;
-    }
-}
-
-// One thread, after all of the CTA's partial results are visible on the device: true in the last CTA of the unit.
-__device__ __forceinline__ bool last_of_unit(const AttnArgs& a, const Segment& s) {
-    const int want = s.last - s.first;
-    if (atomicAdd(a.ws.ticket + s.first, 1) != want) return false;
-    a.ws.ticket[s.first] = 0;           // for the next call
-    return true;
+// By one thread: the CTA's note of the cut unit that begins in it, for the joining kernel (none, until there is one).
+__device__ __forceinline__ void note_none(const AttnArgs& a) { a.ws.unit[blockIdx.x].rows = 0; }
+__device__ __forceinline__ void note_unit(const AttnArgs& a, const Segment& s) {
+    if (s.part >= 0 && s.first == (int)blockIdx.x) a.ws.unit[blockIdx.x] = s;
 }
 
 }  // namespace ace
