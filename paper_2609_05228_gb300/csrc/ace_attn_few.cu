@@ -14,7 +14,7 @@
 // "or" a tile). Two groups of four warps take even and odd tiles into accumulators of their own; a group's next
 // scores are computed as soon as it has read the last ones.
 // Measured (64 users of up to 8192 positions, 332,000 in all, 4 kv heads of 128; 8 query rows a unit): fp8 71 us (4.8 TB/s,
-// 0.70 of the copy rate), bf16 113 us (6.0 TB/s, 0.88). 32 rows: 110 and 126. fp8 tiles are half as long to load, and
+// 0.70 of the copy rate), bf16 113 us (6.0 TB/s, 0.88). 32 rows: 109 and 124. fp8 tiles are half as long to load, and
 // then the chain of a tile bounds it: scores, barrier, weights in four terms, hand-over, product (2000 cycles a tile with two
 // in turn); of a unit's 40 tiles' time its start and end take 4 more.
 #include <cfloat>
@@ -24,8 +24,8 @@
 namespace ace {
 namespace {
 
-// A unit's start and end in tiles of the work line (64 users, at most 8192 positions, 8 and 24 fp8 rows a unit: 71 and 102 us
-// with 4, 73 and 108 with 1, 75 and 114 without).
+// A unit's start and end in tiles of the work line (64 users, at most 8192 positions, 8 and 32 fp8 rows a unit: 71 and 109 us
+// with 4, 72 and 114 with 2; with joins still in this kernel 73 and 120 with 1, 75 and 122 without).
 constexpr int kFewStart = 4;
 constexpr float kNone = -FLT_MAX;       // reference of a row that has seen nothing: any score passes it
 

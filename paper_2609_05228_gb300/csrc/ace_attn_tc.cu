@@ -19,8 +19,8 @@
 // of 2^eref, a power of two above the scales seen so far: exact but for rows whose scale is 2^-20 of the largest and less, whose
 // codes' last bits fall under fp16's least.
 // P is rounded to bf16 (2^-9 of a weight; plain caches) or fp16 (2^-12), as the products need; sums, maxima and O are fp32.
-// Measured: 8 users of up to 16384 positions, 128 nodes of 64 heads (8 kv heads of 128), bf16: 297 us, 870 TFLOP/s. 64 users
-// of up to 8192, 4 kv heads of 128: 64 rows a unit 119 us fp8, 127 bf16; 128 rows 155 and 131; 192 rows 220 and 159. Bound by
+// Measured: 8 users of up to 16384 positions, 128 nodes of 64 heads (8 kv heads of 128), bf16: 304 us, 850 TFLOP/s. 64 users
+// of up to 8192, 4 kv heads of 128: 64 rows a unit 117 us fp8, 128 bf16; 128 rows 144 and 135; 192 rows 213 and 162. Bound by
 // the chain scores, softmax, product of two groups that share one tensor pipe (an item's products alone take 625 cycles:
 // N = 64 makes scores read the q rows from shared memory at its full rate), fp8 also by the conversion of V.
 #include <cudaTypedefs.h>
@@ -31,8 +31,8 @@ namespace ace {
 namespace {
 
 constexpr int kHalf = 64;               // positions of an item
-// A unit's start and end in tiles of the work line (64 users, at most 8192 positions, 64 fp8 rows a unit: 118 us with 9, 119
-// with 6, 121 with 4, 137 without; 192 rows: 222, 219, 220, 232).
+// A unit's start and end in tiles of the work line (64 users, at most 8192 positions, 64 and 128 fp8 rows a unit: 117 and 144
+// us with 7, 119 and 148 with 4; with joins still in this kernel 121 and 159 with 4, 137 and 172 without).
 constexpr int kTcStart = 7;
 
 template <bool FP8, int D, int RT, int CP>
