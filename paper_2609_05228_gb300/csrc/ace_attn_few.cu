@@ -9,7 +9,10 @@
 // to become fp16.
 // fp8 caches: both products take the cached codes as they are (kind::f8f6f4). q is split into two e4m3 terms as in
 // ace_attn_tc.cu; a weight (at most 2^kLazy) times its V row's factor (at most 2^kVUp), rounded to fp16, into four e5m2
-// terms: the upper byte of an fp16 is one, and so on with what is left; each takes at least three of the eleven bits.
+// terms: the upper byte of an fp16 is one, and so on with what is left, times 2^kTermUp a term. A byte takes an fp16's three
+// leading bits, or what of them is not below e5m2's least, 2^-16; so what is left fits in fp16 times 2^3 and four terms hold
+// all bits down to fp16's least, 2^-24. (Not scaled, all terms end at 2^-16, which weights of 2^-20 of the largest are: beside
+// a key that takes nearly all of the weight without a value, thousands of others lose 1 to 100% of theirs.)
 // The rows' references lie in shared memory and move only where a score passes them by 2^kLazy (one barrier with an
 // "or" a tile). Two groups of four warps take even and odd tiles into accumulators of their own; a group's next
 // scores are computed as soon as it has read the last ones.
@@ -27,6 +30,7 @@ namespace {
 // A unit's start and end in tiles of the work line (64 users, at most 8192 positions, 8 and 32 fp8 rows a unit: 71 and 109 us
 // with 4, 72 and 114 with 2; with joins still in this kernel 73 and 120 with 1, 75 and 122 without).
 constexpr int kFewStart = 4;
+constexpr int kTermUp = 3;
 constexpr float kNone = -FLT_MAX;       // reference of a row that has seen nothing: any score passes it
 
 template <bool FP8, int D, int NR, int RG>
@@ -106,18 +110,18 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&x)[N]) {
     }
 }
 
-// N columns of an accumulator whose TERMS parts lie STEP columns apart.
+// N columns of an accumulator whose TERMS parts lie STEP columns apart, each 2^kTermUp times the one before.
 template <int TERMS, int STEP, int N>
 __device__ __forceinline__ void sum_terms(uint32_t taddr, float (&x)[N]) {
-    tmem_ld<N>(taddr, x);
+    tmem_ld<N>(taddr + (TERMS - 1) * STEP, x);
     tmem_ld_wait();
 #pragma unroll 1
-    for (int t = 1; t < TERMS; ++t) {
+    for (int t = TERMS - 2; t >= 0; --t) {
         float y[N];
         tmem_ld<N>(taddr + t * STEP, y);
         tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] += y[i];
+        for (int i = 0; i < N; ++i) x[i] = fmaf(x[i], 1.f / (1 << kTermUp), y[i]);
     }
 }
 
@@ -541,7 +545,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
 #pragma unroll
                             for (int i = 0; i < NR / 2; ++i) {
                                 const uint32_t top = h[i] & 0xff00ff00u;
-                                const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&top));
+                                const __half2 rest = __hmul2(__hsub2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&top)),
+                                                             __float2half2_rn((float)(1 << kTermUp)));
                                 h[i] = *reinterpret_cast<const uint32_t*>(&rest);
                             }
                         }

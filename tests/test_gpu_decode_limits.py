@@ -1,0 +1,47 @@
+"""The speculative decode step's operators where their number formats end: small weights, values of very different size,
+temperatures near zero, pages that do not exist."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode_oracle as R
+from paper_2609_05228_gb300 import ace
+
+pytestmark = pytest.mark.gpu
+
+
+# ----------------------------------------------------------------------- attention
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "plain"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", [5, 8, 16, 24, 32, 40, 128])
+@pytest.mark.parametrize("e", [14, 16, 18, 20, 22])
+def test_attention_sink_of_no_value_beside_small_weights(fmt, D, rows, e):
+    """A first key takes nearly all of the weight and has V = 0; 8191 keys of 2^-e of it (up to 2^(7/8) more) make the output.
+    As many requests as two an SM, so that a CTA meets the sink and all that follows; they share their pages.
+
+    Relative bounds: the weight's rounding (fp8: 2^-12, in fp16's subnormals 2^-25 of a weight times 2^3 or more; plain: 2^-9),
+    the sums of L positive terms, the weight's own (exp2 and a score's rounding of up to 22 units), the output's."""
+    L, B, page = 8192, 304, 64
+    rng = np.random.default_rng(e)
+    x = rng.integers(0, 8, L) / 8.0
+    x[0] = e
+    k = torch.zeros(L, 1, D)
+    k[:, 0, 0] = torch.from_numpy(x)
+    vd = 1 + rng.integers(0, 8, (L, D)) / 8.0
+    vd[0] = 0
+    kv = ace.AceKvCache(1, D, page, L // page, 1, "bf16", fmt)
+    kv.write(0, k.bfloat16().cuda(), torch.from_numpy(vd)[:, None].bfloat16().cuda(), torch.arange(L, device="cuda"))
+    q = torch.zeros(B, rows, D, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    out = torch.empty_like(q)
+    table = torch.arange(L // page, dtype=torch.int32, device="cuda").repeat(B, 1)
+    lens = torch.full((B,), L - 1, dtype=torch.int32, device="cuda")
+    kv.attend(0, q, table, lens, torch.arange(B + 1, dtype=torch.int32, device="cuda"), out, scale=float(np.log(2.0)))
+    kv.sync()
+    p = 2.0 ** (x - e)
+    want = (p @ vd) / p.sum()
+    rel = (2.0 ** -12 + 2.0 ** (e - 28) if fmt == "fp8" else 2.0 ** -9) + (L + 16) * 2.0 ** -24 + 2 * 22 * 2.0 ** -22 + 2.0 ** -8
+    err = np.abs(out.double().cpu().numpy() - want) / want
+    assert err.max() <= rel, (err.max(), rel)
