@@ -7,10 +7,13 @@
 // the softmax's statistics; where a child is rejected and another follows, one for the residual's sum;
 // one for the argmax at the end. Later passes hit L2. No element is stored: with q's normalisations and the
 // residuals' gathered in scalars, the residual at v after k rejections is nu rho_k with
-//   rho_0 = 2^(z a + b),   rho_j = max(rho_(j-1) - c_j q, 0),   q <- 0 at x_j,
-// two operations a rejection and element (the passes of a request that rejects are bound by them). Sums are fp32.
-// Measured: 64 requests of 16 nodes over 128000 tokens: 80 us (floor 19: the rows that are visited, once; the longest walk,
-// of some ten passes that wait for one another, bounds it). One request's chain of 8 over 32000: 17 us.
+//   rho_0 = 2^((z - m) a),   rho_j = max(rho_(j-1) - c_j q, 0),   q <- 0 at x_j,
+// two operations a rejection and element (the passes of a request that rejects are bound by them). m is the row's maximum,
+// taken off before the product with a = log2(e) / temperature as the softmax's sum has it: z a - m a in one operation would be
+// off by the rounding of m a, a factor that all of the row shares and its sum does not. Sums are fp32.
+// Measured: 64 requests of 16 nodes over 128000 tokens: 81 us (floor 19: the rows that are visited, once; the longest walk,
+// of some ten passes that wait for one another, bounds it). One request's chain of 8 over 32000: 16 us.
+#include <float.h>
 #include <math.h>
 
 #include <string>
@@ -133,9 +136,9 @@ __device__ Sums join_all(Shared& sh, Sums v, float inv_t, int& turn, int ctas) {
     return r;
 }
 
-// A node's softmax as rho_0 = 2^(z a + b), and what its rejections make of it.
+// A node's softmax as rho_0 = 2^((z - m) a), and what its rejections make of it.
 struct Row {
-    float a, b, nu, q_mul;              // residual = nu rho_k; draft probabilities of what is left: q_mul q
+    float a, m, nu, q_mul;              // residual = nu rho_k; draft probabilities of what is left: q_mul q
     int k;                              // rejections so far
 };
 
@@ -149,7 +152,7 @@ __device__ __forceinline__ float exp2_of(float x) {
 template <bool DRAFT, int N>
 __device__ __forceinline__ void residuals(const Shared& sh, const Row& w, const int (&v)[N], const float (&z)[N], float (&q)[N], float (&rho)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) rho[i] = exp2_of(fmaf(z[i], w.a, w.b));
+    for (int i = 0; i < N; ++i) rho[i] = exp2_of((z[i] - w.m) * w.a);
     for (int j = 0; j < w.k; ++j) {
         const float c = sh.c[j];
         const int x = sh.x[j];
@@ -297,7 +300,7 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
     const float temp = p.temperature ? p.temperature[b] : 1.f;
     const bool greedy = !(temp > 0.f);
     Row w;
-    const float inv_t = greedy ? 1.f : 1.f / temp;
+    const float inv_t = greedy ? 1.f : fminf(1.f / temp, FLT_MAX);       // (finite: 0 times it is the maximum's exponent)
     const float* noise = p.noise + b * p.noise_stride;
     int turn = 0, node = 0, keep = 0, token = -1;
     if (n > 0 && !greedy) prefetch_row(noise, lo, hi);
@@ -346,8 +349,8 @@ __global__ void __launch_bounds__(kVerThreads, 2) k_verify(const __grid_constant
             v = join_all<kStats>(sh, v, inv_t, turn, ctas);
         }
         if (v.bad || v.m == -INFINITY) break;               // token stays -1
-        w.a = inv_t * 1.4426950408889634f;
-        w.b = -v.m * w.a;
+        w.a = fminf(inv_t * 1.4426950408889634f, FLT_MAX);
+        w.m = v.m;
         w.nu = 1.f / v.s;
         w.q_mul = 1.f;
         w.k = 0;

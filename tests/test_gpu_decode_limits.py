@@ -7,6 +7,8 @@ import torch
 from oracle import decode_oracle as R
 from paper_2609_05228_gb300 import ace
 
+from test_gpu_decode_ops import _check_verify, _run_verify, _verify_case
+
 pytestmark = pytest.mark.gpu
 
 
@@ -45,3 +47,34 @@ def test_attention_sink_of_no_value_beside_small_weights(fmt, D, rows, e):
     rel = (2.0 ** -12 + 2.0 ** (e - 28) if fmt == "fp8" else 2.0 ** -9) + (L + 16) * 2.0 ** -24 + 2 * 22 * 2.0 ** -22 + 2.0 ** -8
     err = np.abs(out.double().cpu().numpy() - want) / want
     assert err.max() <= rel, (err.max(), rel)
+
+
+# ----------------------------------------------------------------------- verification
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("sizes,V", [([6, 1, 4, 8, 5], 9000), ([12, 9, 3], 1500), ([7] * 40, 700)])
+@pytest.mark.parametrize("temp", [1e-3, 1e-4, 1e-5, 1e-6, 1e-7, 1e-8, 1e-20, 1e-30, 1e-37, 1e-40, 1e-45])
+def test_verify_temperatures_near_zero(dtype, draft, sizes, V, temp):
+    """The softmax of any positive temperature, down to fp32's least, for trees with and without a node a CTA."""
+    rng = np.random.default_rng(V + int(-np.log10(temp)))
+    c = _verify_case(rng, sizes, V, dtype, draft, temps=np.full(len(sizes), temp), sharp=6.0)
+    # half of the nodes draft the likely token, or the second
+    z = c["logits"].double().cpu().numpy()
+    for b, ps in enumerate(c["parents"]):
+        for i in range(1, len(ps)):
+            if rng.random() < 0.5:
+                c["tokens"][c["off"][b] + i] = np.argsort(-z[c["off"][b] + ps[i]], kind="stable")[rng.integers(0, 2)]
+    n_max = max(sizes)
+    _check_verify(c, _run_verify(c, n_max), n_max)
+
+
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("shift", [1e6, -3e6, 1e7, 1e8, -1e9, 1e30])
+def test_verify_logits_far_from_zero(draft, shift):
+    """Logits that share a large offset: their differences alone count."""
+    rng = np.random.default_rng(int(abs(shift) % 1000003))
+    c = _verify_case(rng, [6, 4, 8, 5] * 8, 3000, "f32", draft, temps=np.ones(32))
+    c["logits"] += shift
+    _check_verify(c, _run_verify(c, 8), 8)
