@@ -422,7 +422,7 @@ typedef struct ace_kv ace_kv;   /* opaque */
 /*
  * ace_kv_create - a handle over caller-owned cache memory on the current device.
  *   k_pool, v_pool    device, 16-byte aligned; they must outlive the handle
- *   k_scale, v_scale  device; ACE_KV_FP8 only (ignored otherwise)
+ *   k_scale, v_scale  device, 16-byte aligned; ACE_KV_FP8 only (ignored otherwise)
  * The pools' contents are not touched: rows that no call wrote may hold
  * anything, NaN included. Allocates the attention's workspace (tens of MB);
  * the calls below allocate nothing, are asynchronous on `stream` and can be

@@ -399,6 +399,8 @@ ace_status ace_kv_create(const ace_kv_desc* desc, void* k_pool, void* v_pool, vo
     if (!aligned16(k_pool) || !aligned16(v_pool)) return kv_fail(ACE_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
     if (D.format == ACE_KV_FP8 && (!k_scale || !v_scale))
         return kv_fail(ACE_ERR_INVALID_ARG, "an fp8 cache needs k_scale and v_scale");
+    if (D.format == ACE_KV_FP8 && (!aligned16(k_scale) || !aligned16(v_scale)))     // the attention reads four at a time
+        return kv_fail(ACE_ERR_INVALID_ARG, "the scales must be 16-byte aligned");
     // products one at a time, each below 2^31 before the next
     long long rows = (long long)D.n_pages * D.page_size;
     if (rows <= INT32_MAX) rows *= D.n_kv_heads;
