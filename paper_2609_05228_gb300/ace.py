@@ -372,6 +372,16 @@ def _want(name: str, t, dtype: str, shape=None, contiguous: bool = True):
         raise ValueError(f"{name} must be on a GPU")
 
 
+def _row_stride(name: str, t, V: int) -> int:
+    """Elements from one row of t [rows, V] to the next. A single row's stride says nothing and counts as V."""
+    rows, stride = t.shape[0], t.stride(0)
+    if rows and V > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if rows > 1 and stride < V:
+        raise ValueError(f"the rows of {name} must not overlap (a broadcast tensor has to be laid out)")
+    return max(V, stride)
+
+
 def ace_verify_tree(logits, tokens, parents, node_offsets, max_nodes: int, uniforms, noise, path, n_keep, next_token,
                     draft_probs=None, temperature=None, stream=None) -> None:
     """Verification of drafted tokens (torch tensors; layouts in include/ace.h): fills path [B, max_nodes],
@@ -391,13 +401,11 @@ def ace_verify_tree(logits, tokens, parents, node_offsets, max_nodes: int, unifo
     for name, t, shape in (("tokens", tokens, (T,)), ("parents", parents, (T,)), ("node_offsets", node_offsets, (B + 1,)),
                            ("path", path, (B, max_nodes)), ("n_keep", n_keep, (B,)), ("next_token", next_token, (B,))):
         _want(name, t, "int32", shape)
-    for name, t in (("logits", logits), ("noise", noise), ("draft_probs", draft_probs)):
-        if t is not None and t.shape[0] and t.stride(1) != 1 and V > 1:
-            raise ValueError(f"the rows of {name} must be contiguous")
-    _check(lib().ace_verify_tree(logits.data_ptr(), dt, max(V, logits.stride(0)), V, tokens.data_ptr(), parents.data_ptr(),
-                                 node_offsets.data_ptr(), B, T, max_nodes, _ptr(draft_probs),
-                                 max(V, draft_probs.stride(0)) if draft_probs is not None else V, _ptr(temperature),
-                                 uniforms.data_ptr(), noise.data_ptr(), max(V, noise.stride(0)), path.data_ptr(),
+    logits_stride, noise_stride = _row_stride("logits", logits, V), _row_stride("noise", noise, V)
+    draft_stride = _row_stride("draft_probs", draft_probs, V) if draft_probs is not None else V
+    _check(lib().ace_verify_tree(logits.data_ptr(), dt, logits_stride, V, tokens.data_ptr(), parents.data_ptr(),
+                                 node_offsets.data_ptr(), B, T, max_nodes, _ptr(draft_probs), draft_stride,
+                                 _ptr(temperature), uniforms.data_ptr(), noise.data_ptr(), noise_stride, path.data_ptr(),
                                  n_keep.data_ptr(), next_token.data_ptr(), _stream(stream)))
 
 

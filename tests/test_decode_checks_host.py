@@ -3,6 +3,7 @@ import ctypes
 import os
 
 import pytest
+import torch
 
 from paper_2609_05228_gb300 import ace, build
 
@@ -24,3 +25,64 @@ def test_create_refuses_scales_that_are_not_aligned(L, head_dim, dtype, ks, vs):
     d = ace.ace_kv_desc(1, 4, 16, 2, head_dim, dtype, ace.ACE_KV_FP8)
     assert L.ace_kv_create(ctypes.byref(d), 16, 16, ks, vs, None, ctypes.byref(out)) == INVALID
     assert out.value is None and b"scales" in L.ace_last_error_message()
+
+
+class Calls:
+    """A library that notes its calls and launches nothing."""
+
+    def __init__(self):
+        self.made = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.made.append((name, args))
+            return 0
+        return call
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The binding over a library that does nothing; CPU tensors count as the GPU's."""
+    fake = Calls()
+    monkeypatch.setattr(ace, "lib", lambda: fake)
+    want = ace._want
+
+    def on_cpu(name, t, *args):
+        try:
+            want(name, t, *args)
+        except ValueError as e:
+            if "on a GPU" not in str(e):
+                raise
+    monkeypatch.setattr(ace, "_want", on_cpu)
+    return fake.made
+
+
+def _verify_args(T=4, B=2, V=16):
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)       # noqa: E731
+    return dict(logits=torch.zeros(T, V), tokens=i(T), parents=i(T), node_offsets=i(B + 1), max_nodes=4, uniforms=torch.zeros(T),
+                noise=torch.ones(B, V), path=i(B, 4), n_keep=i(B), next_token=i(B), draft_probs=torch.zeros(T, V))
+
+
+@pytest.mark.parametrize("name", ["logits", "noise", "draft_probs"])
+def test_verify_refuses_rows_that_overlap(calls, name):
+    """Broadcast rows have a stride of 0, windows into one buffer a small one: neither is a row every `vocab` elements."""
+    a = _verify_args()
+    rows, V = a[name].shape
+    for t in (torch.zeros(1, V).expand(rows, V), torch.zeros(2 * V).as_strided((rows, V), (3, 1))):
+        with pytest.raises(ValueError, match=name):
+            ace.ace_verify_tree(**dict(a, **{name: t}))
+    assert calls == []
+
+
+def test_verify_passes_on_the_strides_of_rows(calls):
+    """Padded rows, and single rows, whose stride says nothing."""
+    a = _verify_args()
+    a["logits"] = torch.zeros(4, 24)[:, :16]
+    a["noise"] = torch.zeros(2, 40)[:, :16]
+    ace.ace_verify_tree(**a)
+    one = _verify_args(1, 1)
+    one["logits"], one["noise"] = torch.zeros(16).expand(1, 16), torch.zeros(32).as_strided((1, 16), (0, 1))
+    ace.ace_verify_tree(**one)
+    (n0, c0), (n1, c1) = calls
+    assert n0 == n1 == "ace_verify_tree"
+    assert (c0[2], c0[11], c0[15]) == (24, 16, 40) and (c1[2], c1[11], c1[15]) == (16, 16, 16)
