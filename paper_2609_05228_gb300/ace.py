@@ -333,7 +333,13 @@ def ace_kv_keep(kv: int, page_table, max_pages: int, lens, path, max_nodes: int,
 
 
 def ace_tree_mask(parents, node_offsets, B: int, max_nodes: int, mask, depth=None, stream=None) -> None:
-    """Ancestor masks [T, ceil(max_nodes / 64)] (64-bit words) and depths of trees given by parents."""
+    """Ancestor masks [T, ceil(max_nodes / 64)] (int64 words) and depths [T] of trees given by parents [T] (torch tensors)."""
+    T = parents.shape[0]
+    for name, t in (("parents", parents), ("depth", depth)):
+        if t is not None:
+            _want(name, t, "int32", (T,))
+    _want("node_offsets", node_offsets, "int32", (B + 1,))
+    _want("mask", mask, "int64", (T, (max_nodes + 63) // 64))
     _check(lib().ace_tree_mask(_ptr(parents), _ptr(node_offsets), B, max_nodes, _ptr(mask), _ptr(depth), _stream(stream)))
 
 

@@ -86,3 +86,33 @@ def test_verify_passes_on_the_strides_of_rows(calls):
     (n0, c0), (n1, c1) = calls
     assert n0 == n1 == "ace_verify_tree"
     assert (c0[2], c0[11], c0[15]) == (24, 16, 40) and (c1[2], c1[11], c1[15]) == (16, 16, 16)
+
+
+def _mask_args(T=5, B=2, n=70, depth=True):
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)       # noqa: E731
+    return dict(parents=i(T), node_offsets=i(B + 1), B=B, max_nodes=n, mask=torch.zeros(T, -(-n // 64), dtype=torch.int64),
+                depth=i(T) if depth else None)
+
+
+@pytest.mark.parametrize("name,t", [
+    ("mask", torch.zeros(5, 2, dtype=torch.int32)), ("mask", torch.zeros(5, 1, dtype=torch.int64)),
+    ("mask", torch.zeros(4, 2, dtype=torch.int64)), ("mask", torch.zeros(2, 5, dtype=torch.int64).T),
+    ("parents", torch.zeros(5, dtype=torch.int64)), ("parents", torch.zeros(10, dtype=torch.int32)[::2]),
+    ("node_offsets", torch.zeros(2, dtype=torch.int32)), ("node_offsets", torch.zeros(3)),
+    ("depth", torch.zeros(4, dtype=torch.int32)), ("depth", torch.zeros(5))])
+def test_tree_mask_refuses_tensors_that_it_would_overrun(calls, name, t):
+    with pytest.raises(ValueError, match=name):
+        ace.ace_tree_mask(**dict(_mask_args(), **{name: t}))
+    assert calls == []
+
+
+def test_tree_mask_takes_its_own_layouts(calls):
+    ace.ace_tree_mask(**_mask_args())
+    ace.ace_tree_mask(**_mask_args(depth=False))
+    ace.ace_tree_mask(**_mask_args(0, 0, 1))
+    assert len(calls) == 3
+
+
+def test_tree_mask_refuses_memory_of_the_host():
+    with pytest.raises(ValueError, match="on a GPU"):
+        ace.ace_tree_mask(**_mask_args())
