@@ -483,9 +483,14 @@ ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, con
  *   depth        [T] int32 out: number of ancestors (so position lens[b] + depth); may be NULL
  * Errors: INVALID_ARG (NULL, B < 0, max_nodes outside 1..256). Requests with more than
  * max_nodes nodes are left out.
+ * ace_tree_mask takes node_offsets at its word. ace_tree_mask_rows is told T, the rows of parents,
+ * mask and depth, and leaves out requests whose offsets decrease or are not within 0 .. T (T < 0:
+ * INVALID_ARG). Neither call has a handle to report them on.
  */
 ace_status ace_tree_mask(const int32_t* parents, const int32_t* node_offsets, int B, int max_nodes, uint64_t* mask,
                          int32_t* depth, void* stream);
+ace_status ace_tree_mask_rows(const int32_t* parents, const int32_t* node_offsets, int B, int T, int max_nodes,
+                              uint64_t* mask, int32_t* depth, void* stream);
 
 /*
  * ace_tree_attention - with G = n_heads / H, for row t (node i of request b) and head q,
@@ -527,8 +532,9 @@ ace_status ace_tree_attention(ace_kv* kv, int layer, const void* q, long long q_
  *   noise        [B, vocab] float32 > 0, rows noise_stride apart
  *   path         [B, max_nodes] int32 out: node 0 and the accepted nodes, then -1
  *   n_keep       [B] int32 out: length of the path (0 for a request without nodes)
- *   next_token   [B] int32 out; -1 for a request without nodes, and where a visited row has a
- *                NaN, a +inf or no finite logit (the walk ends there). -inf is a filtered token.
+ *   next_token   [B] int32 out; -1 for a request without nodes (one whose offsets decrease or are not
+ *                within 0 .. T, or with more than max_nodes, counts as one), and where a visited row has
+ *                a NaN, a +inf or no finite logit (the walk ends there). -inf is a filtered token.
  * A drafted token outside the vocabulary is never accepted.
  * Errors: INVALID_ARG (NULL, dtype, vocab < 1, strides < vocab, max_nodes outside 1..256), CUDA.
  */

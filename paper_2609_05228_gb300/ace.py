@@ -101,6 +101,7 @@ def lib() -> ctypes.CDLL:
             "ace_kv_read": (_S, [_P, _I, _P, _I, _P, _P, _P]),
             "ace_kv_keep": (_S, [_P, _P, _I, _P, _P, _I, _P, _I, _P, _P]),
             "ace_tree_mask": (_S, [_P, _P, _I, _I, _P, _P, _P]),
+            "ace_tree_mask_rows": (_S, [_P, _P, _I, _I, _I, _P, _P, _P]),
             "ace_tree_attention": (_S, [_P, _I, _P, _LL, _LL, _I, _P, _I, _P, _P, _P, _I, _I, _I, _F, _P, _P, _P]),
             "ace_verify_tree": (_S, [_P, _I, _LL, _I, _P, _P, _P, _I, _I, _I, _P, _LL, _P, _P, _P, _LL, _P, _P, _P, _P]),
             "ace_status_string": (ctypes.c_char_p, [_S]),
@@ -333,14 +334,15 @@ def ace_kv_keep(kv: int, page_table, max_pages: int, lens, path, max_nodes: int,
 
 
 def ace_tree_mask(parents, node_offsets, B: int, max_nodes: int, mask, depth=None, stream=None) -> None:
-    """Ancestor masks [T, ceil(max_nodes / 64)] (int64 words) and depths [T] of trees given by parents [T] (torch tensors)."""
+    """Ancestor masks [T, ceil(max_nodes / 64)] (int64 words) and depths [T] of trees given by parents [T] (torch tensors).
+    Requests whose offsets are not within 0 .. T are left out."""
     T = parents.shape[0]
     for name, t in (("parents", parents), ("depth", depth)):
         if t is not None:
             _want(name, t, "int32", (T,))
     _want("node_offsets", node_offsets, "int32", (B + 1,))
     _want("mask", mask, "int64", (T, (max_nodes + 63) // 64))
-    _check(lib().ace_tree_mask(_ptr(parents), _ptr(node_offsets), B, max_nodes, _ptr(mask), _ptr(depth), _stream(stream)))
+    _check(lib().ace_tree_mask_rows(_ptr(parents), _ptr(node_offsets), B, T, max_nodes, _ptr(mask), _ptr(depth), _stream(stream)))
 
 
 def ace_tree_attention(kv: int, layer: int, q, q_token_stride: int, q_head_stride: int, n_heads: int, page_table,

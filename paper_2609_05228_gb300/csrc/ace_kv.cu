@@ -304,11 +304,12 @@ __global__ void __launch_bounds__(kKeepThreads) k_kv_keep(const __grid_constant_
 
 // Block per request: node i's chain of parents, walked in shared memory (a parent is below its node, so it ends). Bound by
 // the launch and the deepest chain.
-__global__ void __launch_bounds__(kMaxNodes) k_tree_mask(const int32_t* parents, const int32_t* node_offsets, int max_nodes,
-                                                         int words, unsigned long long* mask, int32_t* depth) {
+__global__ void __launch_bounds__(kMaxNodes) k_tree_mask(const int32_t* parents, const int32_t* node_offsets, int T,
+                                                         int max_nodes, int words, unsigned long long* mask, int32_t* depth) {
     __shared__ int par[kMaxNodes];
-    const int o0 = node_offsets[blockIdx.x], n = node_offsets[blockIdx.x + 1] - o0, i = threadIdx.x;
-    if (n <= 0 || n > max_nodes) return;
+    const int o0 = node_offsets[blockIdx.x], o1 = node_offsets[blockIdx.x + 1], i = threadIdx.x;
+    if (o0 < 0 || o1 <= o0 || o1 > T || o1 - o0 > max_nodes) return;
+    const int n = o1 - o0;
     if (i < n) {
         const int q = parents[o0 + i];
         par[i] = q >= 0 && q < i ? q : -1;
@@ -558,12 +559,17 @@ ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, con
 
 ace_status ace_tree_mask(const int32_t* parents, const int32_t* node_offsets, int B, int max_nodes, uint64_t* mask,
                          int32_t* depth, void* stream) {
-    if (B < 0) return kv_fail(ACE_ERR_INVALID_ARG, "B must be >= 0");
+    return ace_tree_mask_rows(parents, node_offsets, B, INT32_MAX, max_nodes, mask, depth, stream);
+}
+
+ace_status ace_tree_mask_rows(const int32_t* parents, const int32_t* node_offsets, int B, int T, int max_nodes,
+                              uint64_t* mask, int32_t* depth, void* stream) {
+    if (B < 0 || T < 0) return kv_fail(ACE_ERR_INVALID_ARG, "B and T must be >= 0");
     if (max_nodes < 1 || max_nodes > kMaxNodes) return kv_fail(ACE_ERR_INVALID_ARG, "max_nodes must be in [1, 256]");
-    if (B == 0) return ACE_OK;
+    if (B == 0 || T == 0) return ACE_OK;
     if (!parents || !node_offsets || !mask) return kv_fail(ACE_ERR_INVALID_ARG, "parents, node_offsets and mask must be non-NULL");
     k_tree_mask<<<B, (max_nodes + 31) / 32 * 32, 0, static_cast<cudaStream_t>(stream)>>>(
-        parents, node_offsets, max_nodes, (max_nodes + 63) / 64, reinterpret_cast<unsigned long long*>(mask), depth);
+        parents, node_offsets, T, max_nodes, (max_nodes + 63) / 64, reinterpret_cast<unsigned long long*>(mask), depth);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? ACE_OK : kv_cuda(e, "tree mask launch");
 }

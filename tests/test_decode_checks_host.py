@@ -116,3 +116,18 @@ def test_tree_mask_takes_its_own_layouts(calls):
 def test_tree_mask_refuses_memory_of_the_host():
     with pytest.raises(ValueError, match="on a GPU"):
         ace.ace_tree_mask(**_mask_args())
+
+
+def test_tree_mask_tells_its_rows(calls):
+    ace.ace_tree_mask(**_mask_args())
+    (name, args), = calls
+    assert name == "ace_tree_mask_rows" and args[2:5] == (2, 5, 70)
+
+
+def test_tree_mask_rows_refuses(L):
+    assert L.ace_tree_mask_rows(16, 16, 1, -1, 4, 16, None, None) == INVALID
+    assert L.ace_tree_mask_rows(16, 16, -1, 4, 4, 16, None, None) == INVALID
+    for n in (0, 257):
+        assert L.ace_tree_mask_rows(16, 16, 1, 4, n, 16, None, None) == INVALID
+    assert L.ace_tree_mask_rows(None, 16, 1, 4, 4, 16, None, None) == INVALID
+    assert L.ace_tree_mask_rows(None, None, 2, 0, 4, None, None, None) == 0

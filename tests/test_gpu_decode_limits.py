@@ -78,3 +78,26 @@ def test_verify_logits_far_from_zero(draft, shift):
     c = _verify_case(rng, [6, 4, 8, 5] * 8, 3000, "f32", draft, temps=np.ones(32))
     c["logits"] += shift
     _check_verify(c, _run_verify(c, 8), 8)
+
+
+# ----------------------------------------------------------------------- masks
+
+
+def test_tree_mask_leaves_out_offsets_outside_its_rows():
+    """Offsets below zero, past the rows, decreasing, or of too many nodes: no row is written for them."""
+    for off in ([0, 3, 9], [-2, 3, 5], [0, 3, 1 << 30], [-(1 << 31), 3, 5], [0, 3, -(1 << 31)], [0, 3, 2], [6, 3, 5]):
+        mask = torch.full((64, 1), -1, dtype=torch.int64, device="cuda")
+        depth = torch.full((64,), -1, dtype=torch.int32, device="cuda")
+        parents = torch.full((64,), -1, dtype=torch.int32, device="cuda")
+        parents[1:] = torch.arange(63, device="cuda")
+        rows = slice(16, 22)                        # six rows of the 64
+        ace.ace_tree_mask(parents[:6], torch.tensor(off, dtype=torch.int32, device="cuda"), 2, 4, mask[rows], depth[rows])
+        torch.cuda.synchronize()
+        want_mask, want_depth = np.full(64, -1), np.full(64, -1)
+        for o0, o1 in zip(off, off[1:]):
+            if 0 <= o0 < o1 <= 6 and o1 - o0 <= 4:
+                ps = [int(p) for p in parents[o0:o1].tolist()]
+                sees = R.ancestors(ps)
+                want_mask[16 + o0: 16 + o1] = R.mask_words(sees, 1).view(np.int64)[:, 0]
+                want_depth[16 + o0: 16 + o1] = sees.sum(1) - 1
+        assert (mask[:, 0].cpu().numpy() == want_mask).all() and (depth.cpu().numpy() == want_depth).all(), off
