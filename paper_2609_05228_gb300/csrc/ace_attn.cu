@@ -112,11 +112,12 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
                 }
             }
             const bool drafted = pos0 + kKeys > s.len;      // holds rows that not every node sees
+            uint32_t masked = 0;
             if (drafted) {
 #pragma unroll
                 for (int i = 0; i < kKeys / 16; ++i) {
                     const int pos = pos0 + sub + 16 * i, mth = pos - s.len;
-                    if (mth >= 0 && !(sees_word(a, s.node0, s.n, node, mth >> 6) >> (mth & 63) & 1)) sc[i] = -INFINITY;
+                    if (mth >= 0 && !(sees_word(a, s.node0, s.n, node, mth >> 6) >> (mth & 63) & 1)) sc[i] = -INFINITY, masked |= 1u << i;
                 }
             }
             float top = sc[0];
@@ -131,7 +132,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
             for (int i = 0; i < kKeys / 16; ++i) {
                 const float p = exp2f(sc[i] - ref);
                 sum += p;
-                sp[row * kKeys + sub + 16 * i] = p;
+                sp[row * kKeys + sub + 16 * i] = masked >> i & 1 ? -0.f : p;
             }
 #pragma unroll
             for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
@@ -145,10 +146,11 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
                 o[i].w *= back;
             }
             __syncwarp();
-            // thread (row, sub): dimensions 4 sub + 64 i; a weight of zero leaves out whatever a masked row holds
+            // thread (row, sub): dimensions 4 sub + 64 i; a weight of minus zero, which no exp2f is, leaves out whatever a masked
+            // row holds
             for (int j = 0; j < kKeys; ++j) {
                 const float p = sp[row * kKeys + j];
-                if (drafted && p == 0.f) continue;
+                if (drafted && __float_as_uint(p) == 0x80000000u) continue;
 #pragma unroll
                 for (int i = 0; i < kMaxHeadDim / 64; ++i) {
                     const int d = 4 * sub + 64 * i;

@@ -7,7 +7,7 @@ import torch
 from oracle import decode_oracle as R
 from paper_2609_05228_gb300 import ace
 
-from test_gpu_decode_ops import _check_verify, _run_verify, _verify_case
+from test_gpu_decode_ops import DT, _check_verify, _run_verify, _verify_case
 
 pytestmark = pytest.mark.gpu
 
@@ -47,6 +47,31 @@ def test_attention_sink_of_no_value_beside_small_weights(fmt, D, rows, e):
     rel = (2.0 ** -12 + 2.0 ** (e - 28) if fmt == "fp8" else 2.0 ** -9) + (L + 16) * 2.0 ** -24 + 2 * 22 * 2.0 ** -22 + 2.0 ** -8
     err = np.abs(out.double().cpu().numpy() - want) / want
     assert err.max() <= rel, (err.max(), rel)
+
+
+@pytest.mark.parametrize("fmt,dtype,D", [("plain", "f32", 64), ("fp8", "f32", 40), ("plain", "bf16", 80), ("fp8", "bf16", 80), ("plain", "bf16", 128),
+                                         ("fp8", "bf16", 128)])
+@pytest.mark.parametrize("nodes", [3, 40])
+def test_attention_nan_of_no_weight_reaches_rows_that_see_it(fmt, dtype, D, nodes):
+    """A drafted V of NaN whose weight is below fp32's least is NaN in the rows that see it, as in the prefix, and in no other."""
+    length, H, G, page = 40, 2, 2, 16
+    dt = DT[dtype]
+    total = length + nodes
+    kv = ace.AceKvCache(H, D, page, 8, 1, dtype, fmt)
+    k, v = torch.zeros(total, H, D, dtype=dt, device="cuda"), torch.ones(total, H, D, dtype=dt, device="cuda")
+    k[length + 1, :, 0] = -448.0                    # scores of -13440
+    v[length + 1, :, 2] = float("nan")
+    kv.write(0, k, v, torch.arange(total, device="cuda"))
+    q = torch.zeros(nodes, H * G, D, dtype=dt, device="cuda")
+    q[..., 0] = 30.0
+    out = torch.empty_like(q)
+    kv.attend(0, q, torch.arange(8, dtype=torch.int32, device="cuda")[None], torch.tensor([length], dtype=torch.int32, device="cuda"),
+              torch.tensor([0, nodes], dtype=torch.int32, device="cuda"), out, None, nodes, 1.0)
+    kv.sync()
+    want = torch.ones_like(out)
+    want[1:, :, 2] = float("nan")
+    assert torch.equal(torch.isnan(out), torch.isnan(want))
+    assert (torch.nan_to_num(out, 1.0).float() - 1).abs().max() <= 2.0 ** -8
 
 
 # ----------------------------------------------------------------------- verification
