@@ -428,7 +428,8 @@ typedef struct ace_kv ace_kv;   /* opaque */
  * the calls below allocate nothing, are asynchronous on `stream` and can be
  * captured in a CUDA graph. One call may be in flight per handle at a time.
  * Indices in device memory (slots, pages, lengths, offsets, paths) are checked
- * by the kernels: what points outside is left out, and the next ace_kv_sync
+ * by the kernels: what points outside is left out (to the attention, a position
+ * whose page does not exist has a K and V of zeros), and the next ace_kv_sync
  * returns ACE_ERR_INVALID_ARG.
  * Errors: INVALID_ARG (NULL, sizes, alignment), UNSUPPORTED (page_size, head_dim,
  * more than 2^31 - 1 rows layers * n_pages * H * P), OOM, CUDA.

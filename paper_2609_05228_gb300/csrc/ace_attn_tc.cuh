@@ -337,18 +337,19 @@ __device__ __forceinline__ void role_load(TcShared& m, const TcAttnArgs& p, unsi
     while (ok && walk.next()) {
         const Segment& s = walk.segment();
         const int total = s.len + s.n;
-        // a tile's pages are looked up while the tile before it is loaded
+        // a tile's pages are looked up while the tile before it is loaded; -1: a page that does not exist, whose rows are read
+        // from before the pool, where TMA fills in zeros (what the buffer held before may be another request's)
         auto look_up = [&](int t) {
             const int at = t * kTcKeys + lane * p.box_rows;
-            return t < s.tile1 && lane < boxes && at < total ? page_of(a, s.b, at) : -1;
+            return t < s.tile1 && lane < boxes && at < total ? page_of(a, s.b, at) : -2;
         };
         int next_page = look_up(s.tile0);
         for (int t = s.tile0; t < s.tile1; ++t) {
             const int pos = t * kTcKeys + lane * p.box_rows;
             const int page = next_page;
             next_page = look_up(t + 1);
-            const int row = a.row0 + (page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-            const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= 0)) * (uint32_t)(p.box_rows * (kTile / 128));
+            const int row = page < 0 ? -kTcKeys : a.row0 + (page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
+            const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= -1)) * (uint32_t)(p.box_rows * (kTile / 128));
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 Ring& r = kv ? rv : rk;
@@ -357,7 +358,7 @@ __device__ __forceinline__ void role_load(TcShared& m, const TcAttnArgs& p, unsi
                 if (!mbar_wait_warp(&empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
                 if (lane == 0) mbar_expect_tx(&full[r.i], bytes);
                 __syncwarp();
-                if (page >= 0) {
+                if (page >= -1) {
                     unsigned char* dst = (kv ? v_smem : k_smem) + r.i * kTile;
                     const CUtensorMap* map = kv ? &p.v : &p.k;
                     if constexpr (FP8) {

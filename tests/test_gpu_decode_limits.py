@@ -7,7 +7,7 @@ import torch
 from oracle import decode_oracle as R
 from paper_2609_05228_gb300 import ace
 
-from test_gpu_decode_ops import DT, _check_verify, _run_verify, _verify_case
+from test_gpu_decode_ops import DT, Step, _check_verify, _run_verify, _verify_case
 
 pytestmark = pytest.mark.gpu
 
@@ -72,6 +72,64 @@ def test_attention_nan_of_no_weight_reaches_rows_that_see_it(fmt, dtype, D, node
     want[1:, :, 2] = float("nan")
     assert torch.equal(torch.isnan(out), torch.isnan(want))
     assert (torch.nan_to_num(out, 1.0).float() - 1).abs().max() <= 2.0 ** -8
+
+
+def _check_by_row(s, out, ls):
+    """The bounds of Step.check with each row's own positions: a value that a row does not see has no part in its bound. (L
+    2^-25: weights down to fp16's least, 2^-24 of a factor of one or more for the largest.)"""
+    out, scale = out.double().cpu().numpy(), s.D ** -0.5
+    w = 0.0 if s.dtype == "f32" else 2.0 ** -9 if s.fmt == "plain" else 2.0 ** -12
+    for b, n in enumerate(s.sizes):
+        if not n:
+            continue
+        G = s.qd.shape[1] // s.k[b].shape[1]
+        L = s.lens[b] + n
+        for i in range(n):
+            at = np.concatenate([np.arange(s.lens[b]), s.lens[b] + np.nonzero(s.sees[b][i])[0]])
+            row = s.off[b] + i
+            if not len(at):
+                assert (out[row] == 0).all() and torch.isneginf(ls[row]).all()
+                continue
+            q = s.qd[row]
+            k, v = np.repeat(s.k[b][at], G, 1), np.repeat(s.v[b][at], G, 1)
+            x = np.einsum("hd,lhd->hl", q, k) * scale
+            top = x.max(1)
+            p = np.exp(x - top[:, None])
+            want = np.einsum("hl,lhd->hd", p, v) / p.sum(1)[:, None]
+            lse = top + np.log(p.sum(1))
+            ds = (s.D + 8) * 2.0 ** -24 * np.einsum("hd,lhd->hl", np.abs(q), np.abs(k)).max(1) * scale + 2.0 ** -20
+            tol = (2 * ds + (L + 16) * 2.0 ** -24 + L * 2.0 ** -25 + w) * np.abs(v).max((0, 2))
+            o_tol = tol[:, None] + (0 if s.dtype == "f32" else 2.0 ** -8) * np.abs(want)
+            err = np.abs(out[row] - want)
+            assert (err <= o_tol).all(), (b, i, (err / o_tol).max())
+            g = ls[row].double().cpu().numpy()
+            assert (np.abs(g - lse) <= ds + (L + 16) * 2.0 ** -24 + 2.0 ** -22 * np.abs(lse)).all(), (b, i)
+
+
+@pytest.mark.parametrize("fmt,dtype,D", [("fp8", "bf16", 128), ("plain", "bf16", 128), ("fp8", "bf16", 64), ("plain", "bf16", 64),
+                                         ("plain", "f32", 40), ("fp8", "bf16", 80)])
+@pytest.mark.parametrize("Hq,H,n", [(4, 2, 1), (8, 2, 8), (4, 2, 30), (6, 2, 40), (4, 2, 100)])
+@pytest.mark.parametrize("page,length,gone", [(16, 700, (0, 11, 12)), (16, 700, (42, 43)), (64, 5000, (3, 40)), (128, 900, (2,)), (256, 900, (0, 3)), (16, 20, (0, 1))])
+def test_attention_has_zeros_for_pages_that_do_not_exist(fmt, dtype, D, Hq, H, n, page, length, gone):
+    """Positions whose table entry names no page of the pool have K and V of zeros, in the prefix, among the nodes, a whole tile's;
+    the other requests' results keep their bits, and the error is reported."""
+    s = Step([length, 333], [n, n], Hq, H, D, page, fmt, dtype, seed=page + n)
+    s.random_masks(0.6)
+    good, good_ls = s.run()
+    for i, g in enumerate(gone):
+        s.table[0, g] = (-1, 1 << 20, -(1 << 31))[i % 3]
+    out = torch.full_like(good, 7.0)
+    ls = torch.full_like(good_ls, 7.0)
+    args = [torch.from_numpy(np.asarray(a, np.int32)).cuda() for a in (s.table, s.lens, s.off)]
+    s.kv.attend(0, s.q, *args, out, s.mask(), s.n_max, None, ls)
+    with pytest.raises(ace.AceError) as err:
+        s.kv.sync()
+    assert err.value.status == 1
+    assert torch.equal(out[n:], good[n:]) and torch.equal(ls[n:], good_ls[n:])
+    pos = np.arange(length + n)
+    s.k[0][np.isin(pos // page, gone)] = 0
+    s.v[0][np.isin(pos // page, gone)] = 0
+    _check_by_row(s, out, ls)
 
 
 # ----------------------------------------------------------------------- verification
