@@ -17,7 +17,7 @@
 // "or" a tile). Two groups of four warps take even and odd tiles into accumulators of their own; a group's next
 // scores are computed as soon as it has read the last ones.
 // Measured (64 users of up to 8192 positions, 332,000 in all, 4 kv heads of 128; 8 query rows a unit): fp8 71 us (4.8 TB/s,
-// 0.70 of the copy rate), bf16 113 us (6.0 TB/s, 0.88). 32 rows: 109 and 124. fp8 tiles are half as long to load, and
+// 0.70 of the copy rate), bf16 113 us (6.0 TB/s, 0.88). 32 rows: 110 and 124. fp8 tiles are half as long to load, and
 // then the chain of a tile bounds it: scores, barrier, weights in four terms, hand-over, product (2000 cycles a tile with two
 // in turn); of a unit's 40 tiles' time its start and end take 4 more.
 #include <cfloat>
@@ -31,6 +31,7 @@ namespace {
 // with 4, 72 and 114 with 2; with joins still in this kernel 73 and 120 with 1, 75 and 122 without).
 constexpr int kFewStart = 4;
 constexpr int kTermUp = 3;
+constexpr int kFewRoom = 4;             // a weight of one is then 2^0 or more in fp16, whose least is 2^-24
 constexpr float kNone = -FLT_MAX;       // reference of a row that has seen nothing: any score passes it
 
 template <bool FP8, int D, int NR, int RG>
@@ -67,6 +68,7 @@ struct FewShared : TcShared {
     float sum[2][4][NR];                // end: sums of weights
     float ref_end[2][NR];
     float2 fac[8][NR];                  // [warp]: factors of both accumulators
+    float2 end[FP8 ? NR * RG : 1];      // a row's reference and sum
     int eref_end[2];
 };
 
@@ -212,7 +214,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
     } else if (warp == 0) {
         role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [] { return true; });
     } else if (warp == 2) {
-        if constexpr (FP8) role_scales(m, a, m.kf, m.vf);
+        if constexpr (FP8) role_scales<kFewRoom>(m, a, m.kf, m.vf);
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issuer
         if (elect_one()) {
@@ -600,6 +602,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                         u1 *= inv;
                     }
                     m.fac[warp - 4][lane] = make_float2(u0, u1);
+                    if (FP8 && quad == 0) m.end[r] = make_float2(top, sum);
                     if (quad == 0 && r < s.rows) {
                         const float ref = top == kNone ? -INFINITY : top;
                         const int ur = s.row0 + r, nd = ur / a.group;
@@ -632,6 +635,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_few(const __grid_constan
                 if (any_bad && in)
                     for (int r = r0; r < min(r0 + HALF, s.rows); ++r) add_not_finite<FP8, C::ROWS>(a, s, bad, r, d, 1);
                 __syncwarp();
+            }
+            if constexpr (FP8) {
+                const unsigned long long* far = m.seg[walk.seg.i].far;
+                if (far[0] | far[1] | far[2] | far[3]) {
+                    if (RG == 1) meet(3, 256);
+                    else meet(1 + g, 128);
+                    add_far_rows<C::ROWS, false>(a, s, far, m.end, RG == 1 ? warp - 4 : g * NR + quad, g * kPer + NR, RG == 1 ? 8 : 4);
+                }
             }
             tc_fence_before();
             if (RG == 1) meet(3, 256);          // O may be overwritten

@@ -16,11 +16,11 @@
 // fp8 caches: K's codes are the B operand as stored (kind::f8f6f4), against q split into two e4m3 terms, which
 // hold 8 significant bits, all of a bf16 q (elements 2^-10 and more below the row's largest lose their last bits, a
 // 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory with their scales, in units
-// of 2^eref, a power of two above the scales seen so far: exact but for rows whose scale is 2^-20 of the largest and less, whose
-// codes' last bits fall under fp16's least.
+// of 2^eref, a power of two above the scales so far (ace_attn_tc.cuh: Reference): exact but for rows whose scale is 2^-20 of the
+// largest and less, whose codes' last bits fall under fp16's least.
 // P is rounded to bf16 (2^-9 of a weight; plain caches) or fp16 (2^-12), as the products need; sums, maxima and O are fp32.
 // Measured: 8 users of up to 16384 positions, 128 nodes of 64 heads (8 kv heads of 128), bf16: 304 us, 850 TFLOP/s. 64 users
-// of up to 8192, 4 kv heads of 128: 64 rows a unit 117 us fp8, 128 bf16; 128 rows 144 and 135; 192 rows 213 and 162. Bound by
+// of up to 8192, 4 kv heads of 128: 64 rows a unit 114 us fp8, 128 bf16; 128 rows 139 and 135; 192 rows 213 and 162. Bound by
 // the chain scores, softmax, product of two groups that share one tensor pipe (an item's products alone take 625 cycles:
 // N = 64 makes scores read the q rows from shared memory at its full rate), fp8 also by the conversion of V.
 #include <cudaTypedefs.h>
@@ -32,8 +32,9 @@ namespace {
 
 constexpr int kHalf = 64;               // positions of an item
 // A unit's start and end in tiles of the work line (64 users, at most 8192 positions, 64 and 128 fp8 rows a unit: 117 and 144
-// us with 7, 119 and 148 with 4; with joins still in this kernel 121 and 159 with 4, 137 and 172 without).
+// us with 7, 119 and 148 with 4, before they took 114 and 139; with joins still in this kernel 121 and 159 with 4, 137 and 172 without).
 constexpr int kTcStart = 7;
+constexpr int kTcRoom = 16;             // V in fp16 is then off by 2^-20 of the largest that all rows see, or exact
 
 template <bool FP8, int D, int RT, int CP>
 struct Cfg {
@@ -54,7 +55,7 @@ struct Cfg {
 template <bool FP8, int RT>
 struct Misc : TcShared {
     uint64_t c_empty[2], soft, group[2];
-    float2 ml[RT == 1 ? 256 : 1];               // RT = 1: both halves' running maximum and sum
+    float2 ml[RT == 1 || FP8 ? 256 : 1];        // RT = 1: both halves' running maximum and sum; else a row's
     int eref1[RT == 1 ? 2 : 1];
     float q_scale[kSegRing][FP8 ? 128 * RT : 1];        // by segments of the ring: softmax may be behind
     float4 kf[FP8 ? kAuxRing : 1][32];          // 128 factors a tile
@@ -247,7 +248,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         Scheduler<ROWS, kTcStart> sched(m, a);                    // a segment ahead of the loads
         if (sched.publish()) role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [&] { return sched.publish(); });
     } else if (warp == 2) {
-        if constexpr (FP8) role_scales(m, a, m.kf, m.vf);
+        if constexpr (FP8) role_scales<kTcRoom>(m, a, m.kf, m.vf);
     } else if (warp == 1 || warp == 3) {
         // ------------------------------------------------ MMA issuers, one a softmax group
         if (elect_one()) {
@@ -668,6 +669,26 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             if (live && c0 == 0 && r < apart) {
                 if (!whole) a.ws.part_ml[(long long)s.part * ROWS + row] = make_float2(m_all, l_all);
                 else if (a.lse) a.lse[at] = (m_all + log2f(l_all)) * 0.69314718055994530942f;
+            }
+            if constexpr (FP8) {
+                const unsigned long long* far = m.seg[walk.seg.i].far;
+                if (far[0] | far[1] | far[2] | far[3]) {
+                    // (the calls as they are: one call of add_far_rows with RT = 1 moved the compiler to code that took 160 us
+                    // for 128 fp8 rows and not 139, calls by rows with RT = 2 to spills and 220 us for 192 rows, not 213)
+                    if constexpr (RT == 1) {
+                        if (!soft_sync()) { ok = false; break; }
+                        for (int k = warp - 4; k < min(s.rows, 128); k += 8) {
+                            float2 e = make_float2(-INFINITY, 0.f);
+                            for (int c = k; c < 256; c += apart) e.x = fmaxf(e.x, m.ml[c].x);
+                            for (int c = k; c < 256; c += apart) e.y += e.x == -INFINITY ? 0.f : m.ml[c].y * exp2f(m.ml[c].x - e.x);
+                            add_far<ROWS, CP == 1>(a, s, far, k, e.x, !whole ? 1.f : e.y == 0.f ? 0.f : 1.f / e.y);
+                        }
+                    } else {
+                        m.ml[row] = make_float2(m_all, l_all);
+                        if (!group_sync()) { ok = false; break; }
+                        add_far_rows<ROWS, true>(a, s, far, m.ml, g * 128 + quad, g * 128 + 128, 4);
+                    }
+                }
             }
             tc_fence_before();
             if (RT == 1 && !soft_sync()) { ok = false; break; }         // O and ml may be overwritten

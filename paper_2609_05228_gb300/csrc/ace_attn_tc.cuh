@@ -36,6 +36,7 @@ struct TcSegment {
     Segment s;
     int go, pad;
     unsigned long long bad[kMaxNodes / 64];     // nodes whose V row holds what is not finite
+    unsigned long long far[kMaxNodes / 64];     // fp8: nodes whose V is left out of the products for its scale (Reference)
 };
 
 // Barriers and hand-overs of a CTA.
@@ -184,6 +185,63 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment&
     }
 }
 
+// By one warp, over an fp8 cache: row `urow` of the unit, written already, gets its share of the V rows that were left out for
+// their scale: weights 2^(score - ref) times `mult`, which the row's sum has in it.
+template <int ROWS, bool BY_DIMS>
+__device__ __noinline__ void add_far(const AttnArgs& a, const Segment& s, const unsigned long long* far, int urow, float ref, float mult) {
+    constexpr int kMost = 4;            // dimensions a lane (head sizes 64 and 128)
+    const int lane = threadIdx.x & 31, per = a.head_dim / 32, d0 = lane * per;
+    const int nd = (s.row0 + urow) / a.group, hq = s.head * a.group + (s.row0 + urow) % a.group;
+    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + (s.node0 + nd) * a.q_token_stride + hq * a.q_head_stride + d0;
+    float sum[kMost] = {};
+    bool any = false;
+#pragma unroll 1
+    for (int w = 0; w < kMaxNodes / 64; ++w) {
+#pragma unroll 1
+        for (unsigned long long bits = far[w] & sees_word(a, s.node0, s.n, nd, w); bits; bits &= bits - 1) {
+            const int pos = s.len + w * 64 + __ffsll(bits) - 1, page = page_of(a, s.b, pos);
+            if (page < 0) continue;
+            const long long row = ((long long)page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
+            float x = 0.f, v[kMost];
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                v[i] = 0.f;
+                if (i >= per) continue;
+                const uint32_t codes = static_cast<const uint8_t*>(a.k_pool)[row * a.head_dim + d0 + i] |
+                                       static_cast<const uint8_t*>(a.v_pool)[row * a.head_dim + d0 + i] << 8;
+                const uint32_t h = f16x2_of_e4m3x2(codes);
+                const float2 kv = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                x = fmaf(to_f32(q[i]), kv.x, x);
+                v[i] = kv.y == kv.y ? kv.y : 0.f;       // (NaN: add_not_finite)
+            }
+            x = warp_sum(x) * pow2_of_byte(a.k_scale[row]) * a.scale_log2;
+            const float p = exp2f(x - ref) * mult, up = pow2_of_byte(a.v_scale[row]);
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) sum[i] = fmaf(p * v[i], up, sum[i]);
+            any = true;
+        }
+    }
+    if (!any) return;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        if (i >= per) break;
+        if (s.part < 0) {
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + ((long long)(s.node0 + nd) * a.n_heads + hq) * a.head_dim + d0 + i;
+            *out = from_f32<__nv_bfloat16>(to_f32(*out) + sum[i]);
+        } else {
+            a.ws.part_o[part_place<BY_DIMS>(ROWS, a.head_dim, s.part, urow, d0 + i)] += sum[i];
+        }
+    }
+}
+
+// The same for rows first, first + step, .. below `end`. ml: a row's maximum (base 2) and sum.
+template <int ROWS, bool BY_DIMS>
+__device__ __noinline__ void add_far_rows(const AttnArgs& a, const Segment& s, const unsigned long long* far, const float2* ml, int first, int end,
+                                          int step) {
+    if (end > s.rows) end = s.rows;
+    for (int r = first; r < end; r += step) add_far<ROWS, BY_DIMS>(a, s, far, r, ml[r].x, s.part >= 0 ? 1.f : ml[r].y == 0.f ? 0.f : 1.f / ml[r].y);
+}
+
 // 8 elements of a unit's q row (bf16), from dimension d on.
 __device__ __forceinline__ uint4 load_q(const AttnArgs& a, const Segment& s, int row, int d) {
     const int nd = row / a.group;
@@ -306,7 +364,7 @@ struct Scheduler {
             m.seg[seg.i].s = s;
             m.seg[seg.i].go = more;
             if (more) note_unit(a, s);
-            for (int w = 0; w < kMaxNodes / 64; ++w) m.seg[seg.i].bad[w] = 0;
+            for (int w = 0; w < kMaxNodes / 64; ++w) m.seg[seg.i].bad[w] = m.seg[seg.i].far[w] = 0;
             mbar_arrive(&m.seg_full[seg.i]);
         }
         seg.next<kSegRing>();
@@ -386,9 +444,70 @@ __device__ __forceinline__ void role_load(TcShared& m, const TcAttnArgs& p, unsi
     }
 }
 
+// fp8 caches: `eref`, the power of two that V's factors are relative to, is above the scales e of all positions that count in the
+// products. It is the rows' common unit, so what some of them do not see may not raise it as it likes: `common` is two octaves
+// above the scales so far that every row of the unit sees (where there are none, above the least of the request's nodes), and
+// nodes that some rows do not see raise eref by at most ROOM from there. A node still higher is far: it counts in the softmax, but
+// its V is left out of the products, and added to the rows that see it once they are done.
+constexpr int kNoRef = -1000, kLeastRef = -125;
+struct Reference {
+    int eref, common;
+};
+
+// By one warp: the reference with nodes of the tile above it. vb: scale bytes of V at the lane's four positions from `pos` on
+// (0: none).
+template <int ROOM>
+__device__ __noinline__ Reference raise_reference(const AttnArgs& a, const Segment& s, unsigned long long* far, uint32_t vb, int pos, Reference r) {
+    const int lane = threadIdx.x & 31;
+    // nodes that every row's node sees
+    const int first = s.row0 / a.group, last = (s.row0 + s.rows - 1) / a.group;
+    unsigned long long all[kMaxNodes / 64];
+#pragma unroll
+    for (int w = 0; w < kMaxNodes / 64; ++w) {
+        unsigned long long x = ~0ull;
+        for (int i = first + lane; i <= last; i += 32) x &= sees_word(a, s.node0, s.n, i, w);
+        all[w] = (unsigned long long)__reduce_and_sync(0xffffffffu, (unsigned)(x >> 32)) << 32 | __reduce_and_sync(0xffffffffu, (unsigned)x);
+    }
+    auto seen = [&](int m) {
+        unsigned long long x = 0;
+#pragma unroll
+        for (int w = 0; w < kMaxNodes / 64; ++w)
+            if (w == m >> 6) x = all[w];
+        return (x >> (m & 63) & 1) != 0;
+    };
+    int top = 0, low = 256;             // scale bytes: the largest that all see, the least of any
+    if (r.common == kNoRef) {
+        for (int m = lane; m < s.n; m += 32) {
+            const int page = page_of(a, s.b, s.len + m);
+            if (page < 0) continue;
+            const int byte = a.v_scale[((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + m) & (a.page_size - 1))];
+            if (seen(m)) top = max(top, byte);
+            low = min(low, byte);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (pos + i >= s.len && seen(pos + i - s.len)) top = max(top, (int)(vb >> (8 * i) & 0xff));
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    low = __reduce_min_sync(0xffffffffu, low);
+    if (r.common == kNoRef && top == 0) top = low;
+    if (top - 127 > r.common) r.common = top - 127 + 2;
+    int e_top = r.common;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int byte = (int)(vb >> (8 * i) & 0xff), m = pos + i - s.len;
+        if (m < 0 || byte == 0) continue;
+        if (byte - 127 <= r.common + ROOM) e_top = max(e_top, byte - 127);
+        else atomicOr(&far[m >> 6], 1ull << (m & 63));
+    }
+    r.eref = max(r.eref, __reduce_max_sync(0xffffffffu, e_top));
+    return r;
+}
+
 // One warp, fp8 caches: a tile's scales, 4 positions a lane. K's as factors 2^e; V's as 2^(e - eref + kVUp) with the tile's
 // eref.
-template <typename V4>
+template <int ROOM, typename V4>
 __device__ __forceinline__ void role_scales(TcShared& m, const AttnArgs& a, float4 (*kf_out)[32], V4 (*vf_out)[32]) {
     volatile int* abort_flag = &m.abort_flag;
     const int lane = threadIdx.x & 31;
@@ -398,7 +517,7 @@ __device__ __forceinline__ void role_scales(TcShared& m, const AttnArgs& a, floa
     while (ok && walk.next()) {
         const Segment& s = walk.segment();
         const int total = s.len + s.n;
-        int eref = -1000;
+        Reference ref{kLeastRef, kNoRef};
         // in batches of 4 tiles, pages two and scales one batch ahead: a load takes longer than a tile
         auto look_up = [&](int t, int (&page)[4]) {
 #pragma unroll
@@ -440,20 +559,25 @@ __device__ __forceinline__ void role_scales(TcShared& m, const AttnArgs& a, floa
                 kb &= have;
                 vb &= have;
             }
-            int top = 0;
+            int top = 0, nodes_top = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top = max(top, (int)(vb >> (8 * i) & 0xff));
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            for (int i = 0; i < 4; ++i) {
+                const int byte = (int)(vb >> (8 * i) & 0xff);
+                if (pos + i < s.len) top = max(top, byte);
+                else nodes_top = max(nodes_top, byte);
+            }
+            top = __reduce_max_sync(0xffffffffu, top);
             // two octaves of room, so that small differences between tiles do not move it
-            if (top - 127 > eref) eref = top - 127 + 2;
+            if (top - 127 > ref.common && top != 0) ref.common = top - 127 + 2, ref.eref = max(ref.eref, ref.common);
+            if (__any_sync(0xffffffffu, nodes_top - 127 > ref.eref)) ref = raise_reference<ROOM>(a, s, m.seg[walk.seg.i].far, vb, pos, ref);
+            const int eref = ref.eref;
             float kf[4], vf[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int vbyte = (int)(vb >> (8 * i) & 0xff);
                 kf[i] = pow2_of_byte((int)(kb >> (8 * i) & 0xff));
                 const int e = vbyte - eref + kVUp;      // biased exponent
-                vf[i] = vbyte == 0 || e <= 0 ? 0.f : pow2_of_byte(e);
+                vf[i] = vbyte == 0 || e <= 0 || vbyte - 127 > eref ? 0.f : pow2_of_byte(e);
             }
             if (!mbar_wait_warp(&m.aux_empty[r.i], r.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
             kf_out[r.i][lane] = make_float4(kf[0], kf[1], kf[2], kf[3]);

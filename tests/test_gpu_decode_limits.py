@@ -7,7 +7,7 @@ import torch
 from oracle import decode_oracle as R
 from paper_2609_05228_gb300 import ace
 
-from test_gpu_decode_ops import DT, Step, _check_verify, _run_verify, _verify_case
+from test_gpu_decode_ops import DT, Step, _check_verify, _rows, _run_verify, _verify_case
 
 pytestmark = pytest.mark.gpu
 
@@ -104,6 +104,50 @@ def _check_by_row(s, out, ls):
             assert (err <= o_tol).all(), (b, i, (err / o_tol).max())
             g = ls[row].double().cpu().numpy()
             assert (np.abs(g - lse) <= ds + (L + 16) * 2.0 ** -24 + 2.0 ** -22 * np.abs(lse)).all(), (b, i)
+
+
+def _scale_value(s, b, node, factor):
+    """The V row of a node is `factor` times a new random one."""
+    v, _ = _rows(s.rng, (1,) + s.v[b].shape[1:], s.dtype, factor)
+    k = torch.from_numpy(s.k[b][s.lens[b] + node][None]).to(v.dtype).cuda()       # (exact: bf16 and fp32 hold a code's value)
+    pos = s.lens[b] + node
+    slot = int(s.table[b, pos // s.page]) * s.page + pos % s.page
+    s.kv.write(s.layer, k, v, torch.tensor([slot], device="cuda"))
+    vd = v.double().cpu().numpy()
+    s.v[b][pos] = (R.quantise_rows(vd)[2] if s.fmt == "fp8" else vd)[0]
+
+
+@pytest.mark.parametrize("fmt,dtype,D", [("fp8", "bf16", 128), ("fp8", "bf16", 64), ("plain", "bf16", 128), ("fp8", "f32", 40)])
+@pytest.mark.parametrize("Hq,H,n", [(2, 1, 3), (4, 2, 4), (8, 2, 4), (4, 2, 16), (8, 2, 16), (4, 2, 60), (8, 2, 60), (3, 3, 200)])
+@pytest.mark.parametrize("power", [3, 7, 12, 20, 60, 110])
+@pytest.mark.parametrize("length", [0, 5, 300])
+def test_attention_values_of_any_size_that_others_see(fmt, dtype, D, Hq, H, n, power, length):
+    """A drafted node whose finite V is 2^power times the others' is nothing to the nodes that do not see it, and what it is to
+    those that do: the last node of a chain, a node that none sees, one that two of three see, one before an empty prefix."""
+    s = Step([length, 140, 30], [n, n, max(1, n // 2)], Hq, H, D, 16, fmt, dtype, seed=n + power)
+    _scale_value(s, 0, n - 1, 2.0 ** power)                     # seen by itself alone
+    _scale_value(s, 1, n // 2, 2.0 ** power)
+    s.sees[1][:, n // 2] = False                                # by none
+    _scale_value(s, 2, 0, 2.0 ** power)
+    s.sees[2][::3, 0] = False                                   # node 0 is not seen by every third, not by itself
+    out, ls = s.run()
+    _check_by_row(s, out, ls)
+
+
+@pytest.mark.parametrize("fmt,D", [("fp8", 128), ("fp8", 64)])
+@pytest.mark.parametrize("Hq,H,n", [(4, 2, 4), (8, 2, 8), (8, 2, 16), (8, 2, 60), (2, 2, 250)])
+def test_attention_values_of_many_sizes_in_trees(fmt, D, Hq, H, n):
+    """Every node's V of another size, any masks, rows that see nothing, lengths that are cut over many CTAs."""
+    s = Step([0, 9000, 127, 128], [n, n, n, max(1, n // 3)], Hq, H, D, 32, fmt, "bf16", seed=n)
+    s.random_masks(0.3, empty=(1,))
+    for b, size in enumerate(s.sizes):
+        for i in range(0, size, 1 + size // 40):
+            _scale_value(s, b, i, 2.0 ** float(s.rng.integers(-60, 61)))
+    first = s.run()
+    _check_by_row(s, *first)
+    for q in (s.q, s.q.transpose(0, 1).contiguous().transpose(0, 1)):
+        again = s.run(q=q)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
 @pytest.mark.parametrize("fmt,dtype,D", [("fp8", "bf16", 128), ("plain", "bf16", 128), ("fp8", "bf16", 64), ("plain", "bf16", 64),
