@@ -459,6 +459,34 @@ struct Reference {
 template <int ROOM>
 __device__ __noinline__ Reference raise_reference(const AttnArgs& a, const Segment& s, unsigned long long* far, uint32_t vb, int pos, Reference r) {
     const int lane = threadIdx.x & 31;
+    int top = 0, low = 256;             // scale bytes of nodes: the largest (that all rows see), the least of any
+    if (r.common == kNoRef) {
+        const int tile = pos - 4 * lane;
+        if (s.len >= tile && s.len + s.n <= tile + kTcKeys) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int byte = (int)(vb >> (8 * i) & 0xff);
+                top = max(top, byte);
+                if (byte) low = min(low, byte);
+            }
+        } else {
+            for (int m = lane; m < s.n; m += 32) {
+                const int page = page_of(a, s.b, s.len + m);
+                if (page < 0) continue;
+                const int byte = a.v_scale[((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + m) & (a.page_size - 1))];
+                top = max(top, byte);
+                if (byte) low = min(low, byte);
+            }
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        low = __reduce_min_sync(0xffffffffu, low);
+        // who sees what makes no difference while all are within ROOM
+        if (top - low <= ROOM) {
+            if (top) r.common = low - 127 + 2, r.eref = max(r.eref, max(r.common, top - 127));
+            return r;
+        }
+        top = 0;
+    }
     // nodes that every row's node sees
     const int first = s.row0 / a.group, last = (s.row0 + s.rows - 1) / a.group;
     unsigned long long all[kMaxNodes / 64];
@@ -475,14 +503,11 @@ __device__ __noinline__ Reference raise_reference(const AttnArgs& a, const Segme
             if (w == m >> 6) x = all[w];
         return (x >> (m & 63) & 1) != 0;
     };
-    int top = 0, low = 256;             // scale bytes: the largest that all see, the least of any
     if (r.common == kNoRef) {
         for (int m = lane; m < s.n; m += 32) {
-            const int page = page_of(a, s.b, s.len + m);
+            const int page = seen(m) ? page_of(a, s.b, s.len + m) : -1;
             if (page < 0) continue;
-            const int byte = a.v_scale[((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + m) & (a.page_size - 1))];
-            if (seen(m)) top = max(top, byte);
-            low = min(low, byte);
+            top = max(top, (int)a.v_scale[((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + m) & (a.page_size - 1))]);
         }
     } else {
 #pragma unroll
@@ -490,7 +515,6 @@ __device__ __noinline__ Reference raise_reference(const AttnArgs& a, const Segme
             if (pos + i >= s.len && seen(pos + i - s.len)) top = max(top, (int)(vb >> (8 * i) & 0xff));
     }
     top = __reduce_max_sync(0xffffffffu, top);
-    low = __reduce_min_sync(0xffffffffu, low);
     if (r.common == kNoRef && top == 0) top = low;
     if (top - 127 > r.common) r.common = top - 127 + 2;
     int e_top = r.common;
