@@ -335,14 +335,15 @@ def ace_kv_keep(kv: int, page_table, max_pages: int, lens, path, max_nodes: int,
 
 def ace_tree_mask(parents, node_offsets, B: int, max_nodes: int, mask, depth=None, stream=None) -> None:
     """Ancestor masks [T, ceil(max_nodes / 64)] (int64 words) and depths [T] of trees given by parents [T] (torch tensors).
-    Requests whose offsets are not within 0 .. T are left out."""
+    Requests whose offsets are not within 0 .. T are left out. Runs on torch's current stream unless one is given."""
     T = parents.shape[0]
     for name, t in (("parents", parents), ("depth", depth)):
         if t is not None:
             _want(name, t, "int32", (T,))
     _want("node_offsets", node_offsets, "int32", (B + 1,))
     _want("mask", mask, "int64", (T, (max_nodes + 63) // 64))
-    _check(lib().ace_tree_mask_rows(_ptr(parents), _ptr(node_offsets), B, T, max_nodes, _ptr(mask), _ptr(depth), _stream(stream)))
+    _check(lib().ace_tree_mask_rows(_ptr(parents), _ptr(node_offsets), B, T, max_nodes, _ptr(mask), _ptr(depth),
+                                    _stream_for(parents, stream)))
 
 
 def ace_tree_attention(kv: int, layer: int, q, q_token_stride: int, q_head_stride: int, n_heads: int, page_table,
@@ -364,6 +365,24 @@ def _dtype(name: str):
 
         _dtypes = {n: getattr(torch, n) for n in ("bfloat16", "float32", "int32", "int64", "uint8", "float8_e4m3fn")}
     return _dtypes[name]
+
+
+_current_stream = None
+
+
+def _raw_stream(device: int) -> int:
+    """torch's current stream on a device, as a pointer (torch is imported at the first use)."""
+    global _current_stream
+    if _current_stream is None:
+        import torch
+
+        _current_stream = torch._C._cuda_getCurrentRawStream
+    return _current_stream(device)
+
+
+def _stream_for(t, stream) -> int:
+    """The stream of a call on torch tensors such as t: the one given, or torch's current one, which made them."""
+    return _raw_stream(t.get_device()) if stream is None else _stream(stream)
 
 
 def _want(name: str, t, dtype: str, shape=None, contiguous: bool = True):
@@ -393,7 +412,8 @@ def _row_stride(name: str, t, V: int) -> int:
 def ace_verify_tree(logits, tokens, parents, node_offsets, max_nodes: int, uniforms, noise, path, n_keep, next_token,
                     draft_probs=None, temperature=None, stream=None) -> None:
     """Verification of drafted tokens (torch tensors; layouts in include/ace.h): fills path [B, max_nodes],
-    n_keep [B] and next_token [B] (int32). logits and draft_probs [T, vocab] and noise [B, vocab] may have padded rows."""
+    n_keep [B] and next_token [B] (int32). logits and draft_probs [T, vocab] and noise [B, vocab] may have padded rows. Runs on
+    torch's current stream unless one is given."""
     T, V = logits.shape
     B = node_offsets.shape[0] - 1
     dt = ACE_BF16 if logits.dtype is _dtype("bfloat16") else ACE_F32
@@ -414,13 +434,13 @@ def ace_verify_tree(logits, tokens, parents, node_offsets, max_nodes: int, unifo
     _check(lib().ace_verify_tree(logits.data_ptr(), dt, logits_stride, V, tokens.data_ptr(), parents.data_ptr(),
                                  node_offsets.data_ptr(), B, T, max_nodes, _ptr(draft_probs), draft_stride,
                                  _ptr(temperature), uniforms.data_ptr(), noise.data_ptr(), noise_stride, path.data_ptr(),
-                                 n_keep.data_ptr(), next_token.data_ptr(), _stream(stream)))
+                                 n_keep.data_ptr(), next_token.data_ptr(), _stream_for(logits, stream)))
 
 
 class AceKvCache:
     """A paged key/value cache of a model's layers and its ace_kv handle. The pools are torch tensors:
     those given, or new ones (zeros). fmt "plain" keeps rows in dtype, "fp8" e4m3 codes and a scale
-    byte per (token, head). Slots are page * page_size + row."""
+    byte per (token, head). Slots are page * page_size + row. Calls run on torch's current stream unless one is given."""
 
     def __init__(self, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, layers: int = 1, dtype: str = "bf16",
                  fmt: str = "fp8", k_pool=None, v_pool=None, k_scale=None, v_scale=None, device: int = 0):
@@ -452,7 +472,8 @@ class AceKvCache:
         self.desc = ace_kv_desc(self.layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
                                 ACE_BF16 if dtype == "bf16" else ACE_F32, ACE_KV_FP8 if fmt == "fp8" else ACE_KV_PLAIN)
         with torch.cuda.device(self.k_pool.device):
-            self.handle = ace_kv_create(self.desc, self.k_pool, self.v_pool, self.k_scale, self.v_scale)
+            self.handle = ace_kv_create(self.desc, self.k_pool, self.v_pool, self.k_scale, self.v_scale,
+                                        _stream_for(self.k_pool, None))
 
     def _rows(self, name, t, heads):
         """(token stride, head stride) of rows [T, heads, head_dim] of any strides but the last."""
@@ -468,7 +489,7 @@ class AceKvCache:
         if v.shape[0] != T:
             raise ValueError("k and v must have the same tokens")
         _want("slots", slots, "int64", (T,))
-        ace_kv_write(self.handle, layer, k, *ks, v, *vs, slots, T, stream)
+        ace_kv_write(self.handle, layer, k, *ks, v, *vs, slots, T, _stream_for(k, stream))
 
     def read(self, layer, slots, k_out, v_out, stream=None) -> None:
         """The rows at `slots` [T] to k_out, v_out [T, n_kv_heads, head_dim]; layer None: of all layers,
@@ -480,7 +501,7 @@ class AceKvCache:
         _want("slots", slots, "int64", (T,))
         for name, t in (("k_out", k_out), ("v_out", v_out)):
             _want(name, t, self._dt, shape)
-        ace_kv_read(self.handle, layer, slots, T, k_out, v_out, stream)
+        ace_kv_read(self.handle, layer, slots, T, k_out, v_out, _stream_for(slots, stream))
 
     def keep(self, page_table, lens, path, n_keep, new_lens=None, stream=None) -> None:
         """The rows of nodes path[b, :n_keep[b]] move to positions lens[b] + 0, 1, .. in every layer."""
@@ -490,7 +511,7 @@ class AceKvCache:
         _want("path", path, "int32", (B, max_nodes))
         for name, t in (("lens", lens), ("n_keep", n_keep)) + ((("new_lens", new_lens),) if new_lens is not None else ()):
             _want(name, t, "int32", (B,))
-        ace_kv_keep(self.handle, page_table, max_pages, lens, path, max_nodes, n_keep, B, new_lens, stream)
+        ace_kv_keep(self.handle, page_table, max_pages, lens, path, max_nodes, n_keep, B, new_lens, _stream_for(lens, stream))
 
     def attend(self, layer: int, q, page_table, lens, node_offsets, out, mask=None, max_nodes: int = 1, scale=None,
                lse=None, stream=None) -> None:
@@ -508,7 +529,7 @@ class AceKvCache:
         if lse is not None:
             _want("lse", lse, "float32", (T, heads))
         ace_tree_attention(self.handle, layer, q, *qs, heads, page_table, max_pages, lens, node_offsets, mask, B, T,
-                           max_nodes, self.head_dim ** -0.5 if scale is None else scale, out, lse, stream)
+                           max_nodes, self.head_dim ** -0.5 if scale is None else scale, out, lse, _stream_for(q, stream))
 
     def sync(self) -> None:
         """Waits for the last call and raises AceError for what its kernels found."""

@@ -54,6 +54,7 @@ def calls(monkeypatch):
             if "on a GPU" not in str(e):
                 raise
     monkeypatch.setattr(ace, "_want", on_cpu)
+    monkeypatch.setattr(ace, "_raw_stream", lambda device: 0, raising=False)
     return fake.made
 
 
@@ -131,3 +132,34 @@ def test_tree_mask_rows_refuses(L):
         assert L.ace_tree_mask_rows(16, 16, 1, 4, n, 16, None, None) == INVALID
     assert L.ace_tree_mask_rows(None, 16, 1, 4, 4, 16, None, None) == INVALID
     assert L.ace_tree_mask_rows(None, None, 2, 0, 4, None, None, None) == 0
+
+
+def _cache(calls, layers=2):
+    """A cache object over CPU tensors, without a handle's memory."""
+    kv = ace.AceKvCache.__new__(ace.AceKvCache)
+    kv.handle, kv.layers, kv.n_pages, kv.page_size, kv.n_kv_heads, kv.head_dim = 7, layers, 4, 16, 2, 64
+    kv.torch_dtype, kv._dt = torch.bfloat16, "bfloat16"
+    return kv
+
+
+def test_calls_run_on_the_current_stream(calls, monkeypatch):
+    """Without a stream, calls on torch tensors are ordered with what made the tensors: torch's current stream."""
+    seen = []
+    monkeypatch.setattr(ace, "_raw_stream", lambda device: seen.append(device) or 77, raising=False)
+    kv = _cache(calls)
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)       # noqa: E731
+    b = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)    # noqa: E731
+    slots = torch.zeros(3, dtype=torch.int64)
+    runs = [lambda **s: kv.write(0, b(3, 2, 64), b(3, 2, 64), slots, **s), lambda **s: kv.read(0, slots, b(3, 2, 64), b(3, 2, 64), **s),
+            lambda **s: kv.keep(i(2, 4), i(2), i(2, 8), i(2), i(2), **s),
+            lambda **s: kv.attend(0, b(3, 4, 64), i(2, 4), i(2), i(3), b(3, 4, 64), **s),
+            lambda **s: ace.ace_tree_mask(**_mask_args(), **s), lambda **s: ace.ace_verify_tree(**_verify_args(), **s)]
+    for run in runs:
+        run()
+        assert calls[-1][1][-1] == 77, calls[-1]
+        run(stream=5)
+        assert calls[-1][1][-1] == 5, calls[-1]
+        run(stream=0)                               # the legacy default stream, if that is what is wanted
+        assert calls[-1][1][-1] == 0
+    assert len(seen) == len(runs) and all(d == -1 for d in seen)
+    kv.handle = None

@@ -228,3 +228,31 @@ def test_tree_mask_leaves_out_offsets_outside_its_rows():
                 want_mask[16 + o0: 16 + o1] = R.mask_words(sees, 1).view(np.int64)[:, 0]
                 want_depth[16 + o0: 16 + o1] = sees.sum(1) - 1
         assert (mask[:, 0].cpu().numpy() == want_mask).all() and (depth.cpu().numpy() == want_depth).all(), off
+
+
+# ----------------------------------------------------------------------- streams
+
+
+def test_calls_follow_the_current_stream():
+    """A step inside `with torch.cuda.stream(...)`, behind a long kernel there that makes its inputs, and captured in a graph."""
+    side = torch.cuda.Stream()
+    s = Step([700, 20], [6, 3], 8, 2, 128, 64, "fp8", "bf16", seed=12)
+    want, _ = s.run(chain=True)
+    args = [torch.from_numpy(np.asarray(a, np.int32)).cuda() for a in (s.table, s.lens, s.off)]
+    q, out = torch.zeros_like(s.q), torch.empty_like(want)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        q.copy_(s.q)
+        s.kv.attend(0, q, *args, out, None, s.n_max)
+        got = out.clone()
+    s.kv.sync()
+    side.synchronize()
+    assert torch.equal(got, want)
+    g = torch.cuda.CUDAGraph()
+    out.zero_()
+    with torch.cuda.graph(g):
+        s.kv.attend(0, q, *args, out, None, s.n_max)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
