@@ -426,7 +426,8 @@ typedef struct ace_kv ace_kv;   /* opaque */
  * The pools' contents are not touched: rows that no call wrote may hold
  * anything, NaN included. Allocates the attention's workspace (tens of MB);
  * the calls below allocate nothing, are asynchronous on `stream` and can be
- * captured in a CUDA graph. One call may be in flight per handle at a time.
+ * captured in a CUDA graph. One call may be in flight per handle at a time, and
+ * the current device must be the one that was current at creation (INVALID_ARG).
  * Indices in device memory (slots, pages, lengths, offsets, paths) are checked
  * by the kernels: what points outside is left out (to the attention, a position
  * whose page does not exist has a K and V of zeros), and the next ace_kv_sync

@@ -19,6 +19,14 @@ ace_status kv_cuda(cudaError_t e, const char* where) {
     return kv_fail(ACE_ERR_CUDA, std::string(where) + ": " + cudaGetErrorName(e) + " (" + cudaGetErrorString(e) + ")");
 }
 
+// A launch goes to the current device: the cache's, or nothing is launched.
+ace_status kv_here(const ace_kv* kv) {
+    int dev = -1;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return kv_cuda(e, "cudaGetDevice");
+    return dev == kv->device ? ACE_OK : kv_fail(ACE_ERR_INVALID_ARG, "the cache belongs to another device than the current one");
+}
+
 struct RowArgs {
     const void* src[2];                 // write: K and V
     long long token_stride[2], head_stride[2];
@@ -464,6 +472,7 @@ ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_
     if (k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0)
         return kv_fail(ACE_ERR_INVALID_ARG, "strides must be >= 0");
     if ((uintptr_t)k % kv->elem || (uintptr_t)v % kv->elem) return kv_fail(ACE_ERR_INVALID_ARG, "k and v must be aligned to their type");
+    if (const ace_status st = kv_here(kv)) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     kv->last_stream = s;
     if (T == 0) return ACE_OK;
@@ -498,6 +507,7 @@ ace_status ace_kv_read(ace_kv* kv, int layer, const int64_t* slots, int T, void*
     if (T < 0) return kv_fail(ACE_ERR_INVALID_ARG, "T must be >= 0");
     if (T > 0 && (!k_out || !v_out || !slots)) return kv_fail(ACE_ERR_INVALID_ARG, "k_out, v_out and slots must be non-NULL");
     if (!aligned16(k_out) || !aligned16(v_out)) return kv_fail(ACE_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+    if (const ace_status st = kv_here(kv)) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     kv->last_stream = s;
     if (T == 0) return ACE_OK;
@@ -524,6 +534,7 @@ ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, con
     if (new_lens && new_lens == lens) return kv_fail(ACE_ERR_INVALID_ARG, "new_lens must not alias lens");
     if ((long long)kv->desc.layers * kv->desc.n_kv_heads > 65535)
         return kv_fail(ACE_ERR_UNSUPPORTED, "layers * n_kv_heads must be at most 65535");
+    if (const ace_status st = kv_here(kv)) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     kv->last_stream = s;
     if (B == 0) return ACE_OK;
@@ -591,6 +602,7 @@ ace_status ace_tree_attention(ace_kv* kv, int layer, const void* q, long long q_
         return kv_fail(ACE_ERR_INVALID_ARG, "q, out, page_table, lens and node_offsets must be non-NULL");
     if (!aligned16(out)) return kv_fail(ACE_ERR_INVALID_ARG, "out must be 16-byte aligned");
     if ((uintptr_t)q % kv->elem) return kv_fail(ACE_ERR_INVALID_ARG, "q must be aligned to its type");
+    if (const ace_status st = kv_here(kv)) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     kv->last_stream = s;
     if (B == 0 || T == 0) return ACE_OK;

@@ -1,5 +1,7 @@
 """The speculative decode step's operators where their number formats end: small weights, values of very different size,
 temperatures near zero, pages that do not exist."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -256,3 +258,27 @@ def test_calls_follow_the_current_stream():
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_calls_refuse_another_current_device():
+    """A cache belongs to the device that was current at its creation: there is one here, so the handle's note of it is changed."""
+    s = Step([30], [2], 4, 2, 64, 16, "fp8", "bf16")
+    good, _ = s.run(chain=True)
+    device = ctypes.c_int.from_address(s.kv.handle + ctypes.sizeof(ace.ace_kv_desc))
+    assert device.value == torch.cuda.current_device()
+    i = lambda *a: torch.zeros(*a, dtype=torch.int32, device="cuda")    # noqa: E731
+    rows, slots = torch.zeros(1, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.full((1,), -1, dtype=torch.int64, device="cuda")
+    calls = [lambda: s.kv.write(0, rows, rows, slots), lambda: s.kv.read(0, slots, rows, rows),
+             lambda: s.kv.keep(i(1, 3), i(1), i(1, 2), i(1)), lambda: s.run(chain=True)]
+    device.value += 1
+    try:
+        for call in calls:
+            with pytest.raises(ace.AceError, match="another device") as err:
+                call()
+            assert err.value.status == 1
+    finally:
+        device.value -= 1
+    for call in calls:
+        call()
+    again, _ = s.run(chain=True)
+    assert torch.equal(again, good)
