@@ -22,6 +22,7 @@ from paper_2609_05228_gb300 import ace, offline, synth  # noqa: E402
 
 VOCAB, LAYERS, HEADS, KV_HEADS, DIM, PAGE = 512, 2, 8, 2, 64, 16
 MAX_NODES = 8
+TREE = [-1, 0, 0, 1, 1, 3]          # a drafted tree's parents
 
 
 class Decoder:
@@ -96,7 +97,7 @@ def draft_trees(last, decoder, drafted: bool):
     """A tree after each request's last token: two children by a bigram drafter, two below the first, one below that.
     Returns tokens, parents, offsets and the drafter's probabilities. `drafted` False: the last token alone."""
     B = last.shape[0]
-    shape = [-1, 0, 0, 1, 1, 3] if drafted else [-1]
+    shape = TREE if drafted else [-1]
     n = len(shape)
     tokens = torch.empty(B, n, dtype=torch.int32, device="cuda")
     probs = torch.empty(B, n, VOCAB, device="cuda")
@@ -113,9 +114,21 @@ def draft_trees(last, decoder, drafted: bool):
     return tokens.view(-1), parents, offsets, probs.view(-1, VOCAB), n
 
 
+def positions(count: int, drafted: bool = True) -> int:
+    """Cache rows that `count` tokens of the slowest request may take of the fastest: a token a step and a whole path a step,
+    and the tree of the last step."""
+    depth = [1] * len(TREE)
+    for i, p in enumerate(TREE[1:], 1):
+        depth[i] = depth[p] + 1
+    return max((count - 1) * max(depth) + len(TREE), count * max(depth)) if drafted else count
+
+
 def generate(decoder: Decoder, first, count: int, temperature: float, drafted: bool = True):
     """`count` tokens (or a few more) of every request after its `first` one: [B] lists, and the steps taken."""
     B = first.shape[0]
+    have = decoder.pages.shape[1] * PAGE - int(decoder.lens.max())
+    if positions(count, drafted) > have:
+        raise ValueError(f"{count} tokens may take {positions(count, drafted)} positions of a request, which has {have} left")
     out = [[] for _ in range(B)]
     temps = torch.full((B,), temperature, device="cuda")
     last, steps = first.int(), 0
@@ -144,7 +157,7 @@ def main():
     ap.add_argument("--temperature", type=float, default=0.8)
     a = ap.parse_args()
     torch.manual_seed(0)
-    decoder = Decoder(a.dtype, a.format, max_len=2 * a.tokens + 64)
+    decoder = Decoder(a.dtype, a.format, max_len=positions(a.tokens))
     out, steps = generate(decoder, torch.arange(4, device="cuda"), a.tokens, a.temperature)
     made = np.mean([len(o) for o in out])
     print(f"{made:.1f} tokens a request in {steps} steps ({made / steps:.2f} a step)")

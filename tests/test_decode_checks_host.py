@@ -1,5 +1,6 @@
 """What the speculative decode step's calls refuse before any device call: memory that its kernels could not read."""
 import ctypes
+import importlib.util
 import os
 
 import pytest
@@ -163,3 +164,39 @@ def test_calls_run_on_the_current_stream(calls, monkeypatch):
         assert calls[-1][1][-1] == 0
     assert len(seen) == len(runs) and all(d == -1 for d in seen)
     kv.handle = None
+
+
+@pytest.fixture(scope="module")
+def example():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "speculative_decode.py")
+    spec = importlib.util.spec_from_file_location("speculative_decode", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+@pytest.mark.parametrize("count,drafted,used", [(64, True, 0), (17, True, 0), (59, False, 6)])
+def test_example_refuses_more_tokens_than_its_pages_hold(example, count, drafted, used):
+    """The request that accepts most runs ahead of the one that ends the loop; its rows have to have pages."""
+    class Full:
+        pages, lens = torch.zeros(4, 4, dtype=torch.int32), torch.tensor([0, used, 0, 0], dtype=torch.int32)
+    assert Full.pages.shape[1] * example.PAGE == 64
+    with pytest.raises(ValueError, match="positions"):
+        example.generate(Full(), torch.zeros(4, dtype=torch.int32), count, 0.8, drafted)
+
+
+def test_example_counts_the_positions_of_the_luckiest_request(example):
+    """Every step one token for the slowest request and all that a path can give for the fastest; a tree's rows in each step."""
+    tree = example.TREE
+    depth = max(len(_path(tree, i)) for i in range(len(tree)))
+    for count in (1, 2, 15, 64):
+        rows = slow = fast = 0
+        while slow < count:
+            rows = max(rows, fast + len(tree))
+            slow, fast = slow + 1, fast + depth
+        assert example.positions(count) == max(rows, fast)
+        assert example.positions(count, False) == count
+
+
+def _path(parents, i):
+    return [] if i < 0 else _path(parents, parents[i]) + [i]
