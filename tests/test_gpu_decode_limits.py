@@ -209,6 +209,25 @@ def test_verify_logits_far_from_zero(draft, shift):
     _check_verify(c, _run_verify(c, 8), 8)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("V", [20000, 20003])
+@pytest.mark.parametrize("n_max", [8, 9])
+def test_verify_trees_of_a_node_a_cta_and_one_more(dtype, draft, V, n_max):
+    """A few requests whose largest tree has as many nodes as a cluster CTAs (all rows' statistics at once), or one more: absent
+    requests, mixed sizes and temperatures; a NaN or a row of -inf where no walk comes is nothing to the others."""
+    rng = np.random.default_rng(V + n_max)
+    sizes = [2, n_max, 1, 0, 5, n_max, 7, 8]
+    c = _verify_case(rng, sizes, V, dtype, draft, temps=[1.0, 0.8, 1.0, 1.0, 0.0, 1.2, 0.0, 1.0])
+    c["parents"][7] = [-1, 0, 1, 2, 3, 4, 0, 0]
+    o = c["off"][7]
+    c["tokens"][o + 1] = -1                         # never accepted, so nodes 2 to 5 are not visited
+    c["logits"][o + 2, 11] = float("nan")
+    c["logits"][o + 4] = float("-inf")
+    c["logits"][c["off"][0], 17] = float("nan")     # a root: the walk ends there
+    _check_verify(c, _run_verify(c, n_max), n_max)
+
+
 # ----------------------------------------------------------------------- masks
 
 
