@@ -447,7 +447,7 @@ ace_status ace_kv_sync(ace_kv* kv);
  *   k, v    device, dtype: head h of token t starts at k + t * k_token_stride +
  *           h * k_head_stride elements and is contiguous (any stride >= 0)
  *   slots   [T] int64 device: slot of each token, negative to leave it out; a slot
- *           that two tokens name holds either one's row
+ *           that two tokens name may hold parts of both rows
  * Errors: INVALID_ARG (NULL, layer, T < 0, negative stride); UNSUPPORTED for 2 T H > 2^30.
  */
 ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_stride, long long k_head_stride,
@@ -504,9 +504,14 @@ ace_status ace_tree_mask_rows(const int32_t* parents, const int32_t* node_offset
  *   q     device, dtype: head q of row t at q + t * q_token_stride + q * q_head_stride
  *   mask  [T, ceil(max_nodes / 64)] uint64; NULL: node i sees nodes 0 .. i (a chain)
  *   out   [T, n_heads, D] dtype, contiguous, 16-byte aligned; lse [T, n_heads] float32 or NULL
- *   T     rows of q and out, node_offsets[B]; max_nodes bounds every n_b
- * Scores, softmax and sums are fp32. bf16 caches round the softmax weights to bf16 for the
- * tensor cores, fp8 caches to fp16. The work is split over the long axis by the lengths, in an
+ *   T     rows of q and out, node_offsets[B]; max_nodes bounds every n_b. The host does not know the
+ *         trees, so max_nodes also chooses the kernel: a bound far above them is right, and slower
+ * Softmax and sums are fp32. What is rounded on the way: plain bf16 caches, the softmax weights to
+ * bf16 (2^-9 of a weight); bf16 q and out over fp8 caches with head sizes 64 and 128, the weights
+ * to fp16 (2^-12 of a weight, 2^-25 of the row's largest), q to two e4m3 terms (elements
+ * 2^-10 and more below its row's largest lose bits that are 2^-18 of that one) and V rows whose
+ * scale is far below that of others that the row sees (2^-20 of the largest V that all rows of a
+ * block of rows see). Nothing else. The work is split over the long axis by the lengths, in an
  * order that depends on them alone: the same call gives the same bits.
  * Errors: INVALID_ARG (NULL, layer, n_heads no multiple of H, max_nodes outside 1..256, scale not
  * finite, misaligned out).

@@ -1,5 +1,5 @@
 // ace_kv_device.cuh — device helpers of the speculative decode step: e4m3 rows, the division of
-// the attention's work over CTAs, and the joining of partial results.
+// the attention's work over CTAs, and where partial results lie.
 #pragma once
 
 #include <cuda_fp16.h>
