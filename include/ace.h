@@ -511,7 +511,7 @@ ace_status ace_tree_mask_rows(const int32_t* parents, const int32_t* node_offset
  * to fp16 (2^-12 of a weight, 2^-25 of the row's largest), q to two e4m3 terms (elements
  * 2^-10 and more below its row's largest lose bits that are 2^-18 of that one) and V rows whose
  * scale is far below that of others that the row sees (2^-20 of the largest V that all rows of a
- * block of rows see). Nothing else. The work is split over the long axis by the lengths, in an
+ * block of rows see); and out to its type. The work is split over the long axis by the lengths, in an
  * order that depends on them alone: the same call gives the same bits.
  * Errors: INVALID_ARG (NULL, layer, n_heads no multiple of H, max_nodes outside 1..256, scale not
  * finite, misaligned out).
