@@ -506,13 +506,13 @@ ace_status ace_tree_mask_rows(const int32_t* parents, const int32_t* node_offset
  *   out   [T, n_heads, D] dtype, contiguous, 16-byte aligned; lse [T, n_heads] float32 or NULL
  *   T     rows of q and out, node_offsets[B]; max_nodes bounds every n_b. The host does not know the
  *         trees, so max_nodes also chooses the kernel: a bound far above them is right, and slower
- * Softmax and sums are fp32. What is rounded on the way: plain bf16 caches, the softmax weights to
- * bf16 (2^-9 of a weight); bf16 q and out over fp8 caches with head sizes 64 and 128, the weights
- * to fp16 (2^-12 of a weight, 2^-25 of the row's largest), q to two e4m3 terms (elements
- * 2^-10 and more below its row's largest lose bits that are 2^-18 of that one) and V rows whose
- * scale is far below that of others that the row sees (2^-20 of the largest V that all rows of a
- * block of rows see); and out to its type. The work is split over the long axis by the lengths, in an
- * order that depends on them alone: the same call gives the same bits.
+ * Softmax and sums are fp32, and out is rounded to dtype. On the tensor cores (bf16, head sizes 64
+ * and 128) more is rounded on the way. Over plain caches: the softmax weights to bf16 (2^-9 of a
+ * weight). Over fp8 caches: the weights to fp16 (2^-12 of a weight, 2^-25 of the row's largest), q
+ * to two e4m3 terms (elements 2^-10 and more below its row's largest lose bits that are 2^-18 of
+ * that one), and V rows whose scale is 2^-20 or less of the largest that every row of a block sees.
+ * The work is split over the long axis by the lengths, in an order that depends on them alone: the
+ * same call gives the same bits.
  * Errors: INVALID_ARG (NULL, layer, n_heads no multiple of H, max_nodes outside 1..256, scale not
  * finite, misaligned out).
  */

@@ -186,7 +186,8 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment&
 }
 
 // By one warp, over an fp8 cache: row `urow` of the unit, written already, gets its share of the V rows that were left out for
-// their scale: weights 2^(score - ref) times `mult`, which the row's sum has in it.
+// their scale: weights 2^(score - ref) times `mult`, which the row's sum has in it. (A whole unit's output is rounded once more by it:
+// 2^-9 of what the products gave, where a far V is 2^6 of the others' or more.)
 template <int ROWS, bool BY_DIMS>
 __device__ __noinline__ void add_far(const AttnArgs& a, const Segment& s, const unsigned long long* far, int urow, float ref, float mult) {
     constexpr int kMost = 4;            // dimensions a lane (head sizes 64 and 128)
