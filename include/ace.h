@@ -397,15 +397,24 @@ ace_status ace_layer_get_desc(const ace_layer* layer, ace_layer_desc* desc);
  * Cache memory belongs to the caller. With H = n_kv_heads, P = page_size, D = head_dim:
  *   pool   [layers, n_pages, H, P, D]   K and V each; position p of request b is row
  *          p % P of page page_table[b, p / P]; slot = page * P + row
- *   scale  [layers, n_pages, H, P] uint8, format ACE_KV_FP8 only
+ *   scale  [layers, n_pages, H, P] uint8, format ACE_KV_FP8
+ * In format ACE_KV_INT4 the pools are [layers, n_pages, H, P, D / 2] bytes and the scales
+ * [layers, n_pages, H, P, ceil(D / 32)] bf16.
  * ACE_KV_PLAIN keeps rows in dtype. ACE_KV_FP8 keeps e4m3 codes: with e the
  * smallest integer >= -126 such that the row's largest finite |x| <= 448 * 2^e,
  * scale = e + 127 and code = x * 2^-e rounded to nearest even (NaN and
  * infinities to e4m3's NaN); a code stands for code * 2^e. A power of two
  * loses nothing against 448 / max |x|: a float's rounding is relative, and
  * scaling is exact in both directions.
+ * ACE_KV_INT4 takes a row in groups of 32 elements (the last one may be shorter),
+ * each with a scale s: the smallest number of 4 significant bits with
+ * max |x| <= 7 s, at least 2^-126 and at most 1.125 * 2^125. The code is x / s
+ * rounded to nearest even, -7 .. 7, and stands for code * s, which bf16 holds
+ * exactly. It is kept as code + 8 in 4 bits, two a byte, the even element in the
+ * lower half. A group with a NaN or an infinity has the scale NaN: all of it
+ * stands for NaN. A row of 128 takes 72 bytes (fp8: 129, bf16: 256).
  */
-typedef enum ace_kv_format { ACE_KV_PLAIN = 0, ACE_KV_FP8 = 1 } ace_kv_format;
+typedef enum ace_kv_format { ACE_KV_PLAIN = 0, ACE_KV_FP8 = 1, ACE_KV_INT4 = 2 } ace_kv_format;
 
 typedef struct ace_kv_desc {
     int layers;          /* >= 1 */
@@ -422,7 +431,7 @@ typedef struct ace_kv ace_kv;   /* opaque */
 /*
  * ace_kv_create - a handle over caller-owned cache memory on the current device.
  *   k_pool, v_pool    device, 16-byte aligned; they must outlive the handle
- *   k_scale, v_scale  device, 16-byte aligned; ACE_KV_FP8 only (ignored otherwise)
+ *   k_scale, v_scale  device, 16-byte aligned; ACE_KV_FP8 and ACE_KV_INT4 (ignored otherwise)
  * The pools' contents are not touched: rows that no call wrote may hold
  * anything, NaN included. Allocates the attention's workspace (tens of MB);
  * the calls below allocate nothing, are asynchronous on `stream` and can be
@@ -455,7 +464,7 @@ ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_
                         void* stream);
 
 /*
- * ace_kv_read - the rows at `slots` [T] as dtype values (code * 2^e rounded to dtype).
+ * ace_kv_read - the rows at `slots` [T] as dtype values (code * 2^e rounded to dtype; code * s).
  *   layer         0 .. layers - 1, or -1 for all of them
  *   k_out, v_out  [T, H, D] (layer -1: [layers, T, H, D]), contiguous, 16-byte aligned;
  *                 a negative slot gives zeros
@@ -474,6 +483,80 @@ ace_status ace_kv_read(ace_kv* kv, int layer, const int64_t* slots, int T, void*
  */
 ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, const int32_t* lens, const int32_t* path,
                        int max_nodes, const int32_t* n_keep, int B, int32_t* new_lens, void* stream);
+
+/*
+ * Rotary positions: dimensions 0 .. rot_dim - 1 of a row are turned in pairs by its token's position p,
+ *   (x, y) -> magnitude (x cos(p f_i) - y sin(p f_i), x sin(p f_i) + y cos(p f_i)),  i = 0 .. rot_dim / 2 - 1,
+ * with pairs (i, i + rot_dim / 2) in layout HALF and (2 i, 2 i + 1) in layout INTERLEAVED; the other dimensions
+ * stay. With t_i = base^(-2 i / rot_dim):
+ *   NONE      f_i = t_i
+ *   LINEAR    f_i = t_i / factor
+ *   BY_TURNS  g = clamp((original_len t_i / 2 pi - low) / (high - low), 0, 1), f_i = t_i (g + (1 - g) / factor):
+ *             pairs that turn more than `high` times over the trained context keep their frequency, those that
+ *             turn less than `low` times have it divided, between them it goes over with the number of turns
+ *   BY_INDEX  the same, going over with the pair's index: c(b) = rot_dim ln(original_len / (2 pi b)) / (2 ln base),
+ *             a = max(floor(c(high)), 0), z = min(ceil(c(low)), rot_dim - 1) (a + 0.001 where that is a),
+ *             g = 1 - clamp((i - a) / (z - a), 0, 1)
+ */
+typedef enum ace_rope_layout { ACE_ROPE_HALF = 0, ACE_ROPE_INTERLEAVED = 1 } ace_rope_layout;
+typedef enum ace_rope_scaling {
+    ACE_ROPE_NONE = 0, ACE_ROPE_LINEAR = 1, ACE_ROPE_BY_TURNS = 2, ACE_ROPE_BY_INDEX = 3
+} ace_rope_scaling;
+
+typedef struct ace_rope_desc {
+    int head_dim;        /* multiple of 8, <= 256 */
+    int rot_dim;         /* even, 2 .. head_dim */
+    int layout;          /* ace_rope_layout */
+    int dtype;           /* ace_dtype of the rows */
+    int scaling;         /* ace_rope_scaling */
+    double base;         /* > 1 */
+    double factor;       /* > 0; read unless NONE */
+    double original_len; /* > 0; BY_TURNS and BY_INDEX */
+    double low, high;    /* turns, 0 < low < high; BY_TURNS and BY_INDEX */
+    double magnitude;    /* > 0 */
+} ace_rope_desc;
+
+typedef struct ace_rope ace_rope;   /* opaque; never changes after its creation, so calls may share it */
+
+/*
+ * ace_rope_create - the frequencies on the current device. divisors [rot_dim / 2] host, or NULL: f_i is divided by
+ * divisors[i] besides. Synchronises `stream`. Frequencies are kept as 2^-64ths of a turn: the angle at position p is off by
+ * about 2^-53 p f_i at most, at any position an int32 holds.
+ * Errors: INVALID_ARG (NULL, a field out of its range, a divisor that is not positive and finite), UNSUPPORTED (head_dim),
+ * OOM, CUDA.
+ */
+ace_status ace_rope_create(const ace_rope_desc* desc, const double* divisors, void* stream, ace_rope** out_rope);
+/* Frees it. NULL is a no-op. Synchronises the device. */
+void ace_rope_destroy(ace_rope* rope);
+
+/*
+ * ace_rope_apply - turns the rows of q and k [T, heads, head_dim] by their tokens' positions; with `inverse`, by the same
+ * angles backwards, and the same magnitude: the gradients of q and k from those of q_out and k_out.
+ *   positions   [T] int32 device, any value
+ *   q, k        head h of token t starts at q + t * q_token_stride + h * q_head_stride elements and is contiguous (any
+ *               strides >= 0); n_kv_heads 0: no k
+ *   q_out, k_out  the same with their own strides, rows apart from one another; an output may be its input (the same
+ *               address and strides), and must not overlap q, k or the other output otherwise
+ * fp32, rounded once. Asynchronous on `stream`, allocates nothing, can be captured. The current device must be the rope's.
+ * Errors: INVALID_ARG (NULL, negative sizes or strides, alignment, outputs whose rows overlap, device); UNSUPPORTED for more
+ * than 2^30 rows.
+ */
+ace_status ace_rope_apply(const ace_rope* rope, int inverse, const int32_t* positions, int T, const void* q, long long q_token_stride,
+                          long long q_head_stride, int n_heads, void* q_out, long long q_out_token_stride, long long q_out_head_stride,
+                          const void* k, long long k_token_stride, long long k_head_stride, int n_kv_heads, void* k_out,
+                          long long k_out_token_stride, long long k_out_head_stride, void* stream);
+
+/*
+ * ace_kv_write_rotated - ace_rope_apply to q and ace_kv_write of the rotated k and of v, in one pass: the same bits as the two
+ * calls (k is rounded to dtype after its rotation). q and q_out as ace_rope_apply takes them (n_heads 0: no q); k, v and slots
+ * as ace_kv_write takes them. A token with a negative slot has its q turned and its k and v left out.
+ * Errors: those of both; INVALID_ARG where rope and cache differ in head_dim or dtype; UNSUPPORTED for
+ * T (n_heads + 2 H) > 2^30.
+ */
+ace_status ace_kv_write_rotated(ace_kv* kv, int layer, const ace_rope* rope, const int32_t* positions, const void* q,
+                                long long q_token_stride, long long q_head_stride, int n_heads, void* q_out, long long q_out_token_stride,
+                                long long q_out_head_stride, const void* k, long long k_token_stride, long long k_head_stride, const void* v,
+                                long long v_token_stride, long long v_head_stride, const int64_t* slots, int T, void* stream);
 
 /*
  * ace_tree_mask - ancestor masks and depths of trees given by their parents.

@@ -20,7 +20,10 @@ LIBPATH = os.path.join(_LIBDIR, LIBNAME)
 
 ACE_BF16, ACE_F32 = 0, 1
 ACE_SKIP_THRESHOLD, ACE_SKIP_RATIO = 0, 1
-ACE_KV_PLAIN, ACE_KV_FP8 = 0, 1
+ACE_KV_PLAIN, ACE_KV_FP8, ACE_KV_INT4 = 0, 1, 2
+ACE_ROPE_HALF, ACE_ROPE_INTERLEAVED = 0, 1
+# Scaling of rotary frequencies (ace_rope_scaling): index = enum value.
+ROPE_SCALINGS = ("none", "linear", "by_turns", "by_index")
 # Skip rules (ace_fusion): index = enum value. "max" is ACE.
 FUSIONS = ("max", "min", "mean", "gsp", "rcr", "score")
 ACE_FUSION_MAX, ACE_FUSION_MIN, ACE_FUSION_MEAN, ACE_FUSION_GSP, ACE_FUSION_RCR, ACE_FUSION_SCORE = range(6)
@@ -49,6 +52,13 @@ class ace_kv_desc(ctypes.Structure):
     _fields_ = [("layers", ctypes.c_int), ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int),
                 ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("dtype", ctypes.c_int),
                 ("format", ctypes.c_int)]
+
+
+class ace_rope_desc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int), ("rot_dim", ctypes.c_int), ("layout", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("scaling", ctypes.c_int), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("magnitude", ctypes.c_double)]
 
 
 _lib = None
@@ -94,6 +104,10 @@ def lib() -> ctypes.CDLL:
             "ace_stack_forward_host": (_S, [_P, _P, _P, _I, ace_skip_ctl, _P]),
             "ace_offline_tables_device": (_S, [_I, _I, _I, _P, _P, _P, _P, _P, ctypes.c_double, _I, ctypes.c_size_t,
                                                _P, _P, _P]),
+            "ace_rope_create": (_S, [ctypes.POINTER(ace_rope_desc), ctypes.POINTER(ctypes.c_double), _P, ctypes.POINTER(_P)]),
+            "ace_rope_destroy": (None, [_P]),
+            "ace_rope_apply": (_S, [_P, _I, _P, _I, _P, _LL, _LL, _I, _P, _LL, _LL, _P, _LL, _LL, _I, _P, _LL, _LL, _P]),
+            "ace_kv_write_rotated": (_S, [_P, _I, _P, _P, _P, _LL, _LL, _I, _P, _LL, _LL, _P, _LL, _LL, _P, _LL, _LL, _P, _I, _P]),
             "ace_kv_create": (_S, [ctypes.POINTER(ace_kv_desc), _P, _P, _P, _P, _P, ctypes.POINTER(_P)]),
             "ace_kv_destroy": (None, [_P]),
             "ace_kv_sync": (_S, [_P]),
@@ -333,6 +347,39 @@ def ace_kv_keep(kv: int, page_table, max_pages: int, lens, path, max_nodes: int,
                              _ptr(new_lens), _stream(stream)))
 
 
+def ace_rope_create(desc: ace_rope_desc, divisors=None, stream=None) -> int:
+    """divisors: rot_dim / 2 numbers that the frequencies are divided by besides, or None."""
+    d = None
+    if divisors is not None:
+        if len(divisors) != desc.rot_dim // 2:
+            raise ValueError(f"divisors must have rot_dim / 2 = {desc.rot_dim // 2} entries, not {len(divisors)}")
+        d = (ctypes.c_double * len(divisors))(*[float(x) for x in divisors])
+    out = _P()
+    _check(lib().ace_rope_create(ctypes.byref(desc), d, _stream(stream), ctypes.byref(out)))
+    return out.value
+
+
+def ace_rope_destroy(rope: int) -> None:
+    if rope:
+        lib().ace_rope_destroy(rope)
+
+
+def ace_rope_apply(rope: int, inverse: bool, positions, T: int, q, q_token_stride: int, q_head_stride: int, n_heads: int, q_out,
+                   q_out_token_stride: int, q_out_head_stride: int, k=None, k_token_stride: int = 0, k_head_stride: int = 0,
+                   n_kv_heads: int = 0, k_out=None, k_out_token_stride: int = 0, k_out_head_stride: int = 0, stream=None) -> None:
+    _check(lib().ace_rope_apply(rope, int(inverse), _ptr(positions), T, _ptr(q), q_token_stride, q_head_stride, n_heads, _ptr(q_out),
+                                q_out_token_stride, q_out_head_stride, _ptr(k), k_token_stride, k_head_stride, n_kv_heads, _ptr(k_out),
+                                k_out_token_stride, k_out_head_stride, _stream(stream)))
+
+
+def ace_kv_write_rotated(kv: int, layer: int, rope: int, positions, q, q_token_stride: int, q_head_stride: int, n_heads: int, q_out,
+                         q_out_token_stride: int, q_out_head_stride: int, k, k_token_stride: int, k_head_stride: int, v,
+                         v_token_stride: int, v_head_stride: int, slots, T: int, stream=None) -> None:
+    _check(lib().ace_kv_write_rotated(kv, layer, rope, _ptr(positions), _ptr(q), q_token_stride, q_head_stride, n_heads, _ptr(q_out),
+                                      q_out_token_stride, q_out_head_stride, _ptr(k), k_token_stride, k_head_stride, _ptr(v),
+                                      v_token_stride, v_head_stride, _ptr(slots), T, _stream(stream)))
+
+
 def ace_tree_mask(parents, node_offsets, B: int, max_nodes: int, mask, depth=None, stream=None) -> None:
     """Ancestor masks [T, ceil(max_nodes / 64)] (int64 words) and depths [T] of trees given by parents [T] (torch tensors).
     Requests whose offsets are not within 0 .. T are left out. Runs on torch's current stream unless one is given."""
@@ -437,17 +484,74 @@ def ace_verify_tree(logits, tokens, parents, node_offsets, max_nodes: int, unifo
                                  n_keep.data_ptr(), next_token.data_ptr(), _stream_for(logits, stream)))
 
 
+def _head_rows(name: str, t, dtype: str, T, heads, dim: int):
+    """(token stride, head stride) of rows [T, heads, dim] of any strides but the last."""
+    _want(name, t, dtype, (T, heads, dim), False)
+    if t.numel() and t.stride(2) != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+    return t.stride(0), t.stride(1)
+
+
+class AceRope:
+    """Rotary positions of one kind (formulas in include/ace.h): rot_dim dimensions (None: all) of each head in layout "half" or
+    "interleaved"; scaling "none", "linear" (factor), "by_turns" or "by_index" (factor, original_len, low, high); divisors
+    [rot_dim / 2] divide the frequencies besides. Calls run on torch's current stream unless one is given."""
+
+    def __init__(self, head_dim: int, rot_dim=None, layout: str = "half", base: float = 10000.0, scaling: str = "none",
+                 factor: float = 1.0, original_len: float = 0.0, low: float = 1.0, high: float = 32.0, magnitude: float = 1.0,
+                 divisors=None, dtype: str = "bf16", device: int = 0):
+        import torch
+
+        if dtype not in ("bf16", "f32") or layout not in ("half", "interleaved") or scaling not in ROPE_SCALINGS:
+            raise ValueError(f"dtype must be 'bf16' or 'f32', layout 'half' or 'interleaved' and scaling one of {ROPE_SCALINGS}")
+        self.handle = None
+        self.head_dim = int(head_dim)
+        self._dt = "bfloat16" if dtype == "bf16" else "float32"
+        self.desc = ace_rope_desc(self.head_dim, self.head_dim if rot_dim is None else int(rot_dim),
+                                  ACE_ROPE_HALF if layout == "half" else ACE_ROPE_INTERLEAVED, ACE_BF16 if dtype == "bf16" else ACE_F32,
+                                  ROPE_SCALINGS.index(scaling), base, factor, original_len, low, high, magnitude)
+        with torch.cuda.device(device):
+            self.handle = ace_rope_create(self.desc, divisors, _raw_stream(device))
+
+    def apply(self, positions, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
+        """q [T, n_heads, head_dim] (and k) turned by `positions` [T] int32 into q_out (and k_out), which may be q (and k)
+        themselves; `inverse`: the gradients of q and k from those of their results."""
+        T, heads = q.shape[0], q.shape[1]
+        _want("positions", positions, "int32", (T,))
+        qs = _head_rows("q", q, self._dt, T, heads, self.head_dim)
+        qo = _head_rows("q_out", q_out, self._dt, T, heads, self.head_dim)
+        ks, ko, kv_heads = (0, 0), (0, 0), 0
+        if (k is None) != (k_out is None):
+            raise ValueError("k and k_out are given together")
+        if k is not None:
+            kv_heads = k.shape[1]
+            ks = _head_rows("k", k, self._dt, T, kv_heads, self.head_dim)
+            ko = _head_rows("k_out", k_out, self._dt, T, kv_heads, self.head_dim)
+        ace_rope_apply(self.handle, inverse, positions, T, q, *qs, heads, q_out, *qo, k, *ks, kv_heads, k_out, *ko, _stream_for(q, stream))
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            ace_rope_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class AceKvCache:
     """A paged key/value cache of a model's layers and its ace_kv handle. The pools are torch tensors:
     those given, or new ones (zeros). fmt "plain" keeps rows in dtype, "fp8" e4m3 codes and a scale
-    byte per (token, head). Slots are page * page_size + row. Calls run on torch's current stream unless one is given."""
+    byte per (token, head), "int4" 4-bit codes (two a byte, uint8) and a bf16 scale for every 32 of them. Slots are page * page_size + row. Calls run on torch's current stream unless one is given."""
 
     def __init__(self, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, layers: int = 1, dtype: str = "bf16",
                  fmt: str = "fp8", k_pool=None, v_pool=None, k_scale=None, v_scale=None, device: int = 0):
         import torch
 
-        if dtype not in ("bf16", "f32") or fmt not in ("plain", "fp8"):
-            raise ValueError("dtype must be 'bf16' or 'f32' and fmt 'plain' or 'fp8'")
+        if dtype not in ("bf16", "f32") or fmt not in ("plain", "fp8", "int4"):
+            raise ValueError("dtype must be 'bf16' or 'f32' and fmt 'plain', 'fp8' or 'int4'")
         self.handle = None
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self._dt = "bfloat16" if dtype == "bf16" else "float32"
@@ -455,7 +559,8 @@ class AceKvCache:
         self.n_kv_heads, self.head_dim = int(n_kv_heads), int(head_dim)
         rows = (self.layers, self.n_pages, self.n_kv_heads, self.page_size)
         dev = torch.device("cuda", device)
-        pool_dt = torch.float8_e4m3fn if fmt == "fp8" else self.torch_dtype
+        pool_dt = {"plain": self.torch_dtype, "fp8": torch.float8_e4m3fn, "int4": torch.uint8}[fmt]
+        width = self.head_dim // 2 if fmt == "int4" else self.head_dim
 
         def own(t, shape, dt, name):
             if t is None:
@@ -463,24 +568,22 @@ class AceKvCache:
             _want(name, t, str(dt)[6:], shape)
             return t
 
-        self.k_pool = own(k_pool, rows + (self.head_dim,), pool_dt, "k_pool")
-        self.v_pool = own(v_pool, rows + (self.head_dim,), pool_dt, "v_pool")
+        self.k_pool = own(k_pool, rows + (width,), pool_dt, "k_pool")
+        self.v_pool = own(v_pool, rows + (width,), pool_dt, "v_pool")
         self.k_scale = self.v_scale = None
-        if fmt == "fp8":
-            self.k_scale = own(k_scale, rows, torch.uint8, "k_scale")
-            self.v_scale = own(v_scale, rows, torch.uint8, "v_scale")
+        if fmt != "plain":
+            shape, scale_dt = (rows, torch.uint8) if fmt == "fp8" else (rows + (-(-self.head_dim // 32),), torch.bfloat16)
+            self.k_scale = own(k_scale, shape, scale_dt, "k_scale")
+            self.v_scale = own(v_scale, shape, scale_dt, "v_scale")
         self.desc = ace_kv_desc(self.layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
-                                ACE_BF16 if dtype == "bf16" else ACE_F32, ACE_KV_FP8 if fmt == "fp8" else ACE_KV_PLAIN)
+                                ACE_BF16 if dtype == "bf16" else ACE_F32,
+                                {"plain": ACE_KV_PLAIN, "fp8": ACE_KV_FP8, "int4": ACE_KV_INT4}[fmt])
         with torch.cuda.device(self.k_pool.device):
             self.handle = ace_kv_create(self.desc, self.k_pool, self.v_pool, self.k_scale, self.v_scale,
                                         _stream_for(self.k_pool, None))
 
     def _rows(self, name, t, heads):
-        """(token stride, head stride) of rows [T, heads, head_dim] of any strides but the last."""
-        _want(name, t, self._dt, (t.shape[0], heads, self.head_dim), False)
-        if t.numel() and t.stride(2) != 1:
-            raise ValueError(f"the last axis of {name} must be contiguous")
-        return t.stride(0), t.stride(1)
+        return _head_rows(name, t, self._dt, t.shape[0], heads, self.head_dim)
 
     def write(self, layer: int, k, v, slots, stream=None) -> None:
         """k, v [T, n_kv_heads, head_dim] (any strides but the last) to `slots` [T] int64 of a layer."""
@@ -490,6 +593,19 @@ class AceKvCache:
             raise ValueError("k and v must have the same tokens")
         _want("slots", slots, "int64", (T,))
         ace_kv_write(self.handle, layer, k, *ks, v, *vs, slots, T, _stream_for(k, stream))
+
+    def write_rotated(self, layer: int, rope: AceRope, positions, q, q_out, k, v, slots, stream=None) -> None:
+        """q [T, n_heads, head_dim] turned by `positions` [T] int32 into q_out (or in place), k turned and written to `slots` with v:
+        rope.apply and write in one pass."""
+        T, heads = q.shape[0], q.shape[1]
+        qs, qo = self._rows("q", q, heads), _head_rows("q_out", q_out, self._dt, T, heads, self.head_dim)
+        ks, vs = self._rows("k", k, self.n_kv_heads), self._rows("v", v, self.n_kv_heads)
+        if k.shape[0] != T or v.shape[0] != T:
+            raise ValueError("q, k and v must have the same tokens")
+        _want("positions", positions, "int32", (T,))
+        _want("slots", slots, "int64", (T,))
+        ace_kv_write_rotated(self.handle, layer, rope.handle, positions, q, *qs, heads, q_out, *qo, k, *ks, v, *vs, slots, T,
+                             _stream_for(q, stream))
 
     def read(self, layer, slots, k_out, v_out, stream=None) -> None:
         """The rows at `slots` [T] to k_out, v_out [T, n_kv_heads, head_dim]; layer None: of all layers,

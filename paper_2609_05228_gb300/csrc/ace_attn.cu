@@ -15,11 +15,17 @@ constexpr int kRows = 16, kKeys = 64, kThreads = 256, kJoinParts = 8;
 __host__ __device__ constexpr int pitch(int D) { return D + 4; }   // floats a row: 16-byte chunks of 8 rows in distinct banks
 int core_smem(int D) { return (2 * kKeys * pitch(D) + kRows * pitch(D) + kRows * kKeys) * 4; }
 
-// 8 elements of a cached row as floats.
-template <typename T, bool FP8>
-__device__ __forceinline__ void cached8(const void* pool, long long row, int D, int d, float (&f)[8]) {
-    if constexpr (FP8) {
+// 8 elements of a cached row as floats; `scale` is the layer's.
+template <typename T, int FMT>
+__device__ __forceinline__ void cached8(const void* pool, const uint8_t* scale, long long row, int D, int d, float (&f)[8]) {
+    if constexpr (FMT == ACE_KV_INT4) {
+        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(pool) + row * (D / 2) + d / 2));
+        int4x8_to_float(w, float_of_bf16(__ldg(reinterpret_cast<const uint16_t*>(scale) + row * groups4(D) + d / kGroup4)), f);
+    } else if constexpr (FMT == ACE_KV_FP8) {
         e4m3x8_to_float(__ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + row * D + d)), f);
+        const float m = pow2_of_byte(scale[row]);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) f[x] *= m;
     } else if constexpr (sizeof(T) == 2) {
         Vec16<T>::to_float(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(pool) + row * D + d)), f);
     } else {
@@ -29,7 +35,7 @@ __device__ __forceinline__ void cached8(const void* pool, long long row, int D, 
     }
 }
 
-template <typename T, bool FP8>
+template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ AttnArgs a) {
     extern __shared__ __align__(16) float sm[];
     const int D = a.head_dim, P = pitch(D);
@@ -88,13 +94,8 @@ __global__ void __launch_bounds__(kThreads) k_attn_core(const __grid_constant__ 
                     const int page = page_of(a, s.b, pos);
                     if (page >= 0) {
                         const long long r = ((long long)page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-                        cached8<T, FP8>(a.k_pool, r, D, d, fk);
-                        cached8<T, FP8>(a.v_pool, r, D, d, fv);
-                        if constexpr (FP8) {
-                            const float mk = pow2_of_byte(a.k_scale[r]), mv = pow2_of_byte(a.v_scale[r]);
-#pragma unroll
-                            for (int x = 0; x < 8; ++x) fk[x] *= mk, fv[x] *= mv;
-                        }
+                        cached8<T, FMT>(a.k_pool, a.k_scale, r, D, d, fk);
+                        cached8<T, FMT>(a.v_pool, a.v_scale, r, D, d, fv);
                     }
                 }
                 store8f(sk + j * P + d, fk);
@@ -274,24 +275,26 @@ cudaError_t join_of(const AttnArgs& a, int rows, int ctas, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, k_attn_join<T, BY_DIMS>, a, rows);
 }
 
-template <typename T, bool FP8>
-cudaError_t core_attr(int D) {
-    return raise_smem_limit(k_attn_core<T, FP8>, core_smem(D));
+using CoreKernel = void (*)(const AttnArgs);
+
+template <typename T>
+CoreKernel core_of(int format) {
+    return format == ACE_KV_INT4 ? k_attn_core<T, ACE_KV_INT4> : format == ACE_KV_FP8 ? k_attn_core<T, ACE_KV_FP8> : k_attn_core<T, ACE_KV_PLAIN>;
 }
+
+CoreKernel core_kernel(const ace_kv_desc& D) { return D.dtype == ACE_BF16 ? core_of<__nv_bfloat16>(D.format) : core_of<float>(D.format); }
 
 }  // namespace
 
 cudaError_t attn_init(ace_kv* kv) {
     const ace_kv_desc& D = kv->desc;
-    const bool fp8 = D.format == ACE_KV_FP8, bf = D.dtype == ACE_BF16;
     kv->tc = attn_tc_supported(kv);
     size_t ctas = kv->num_sms, rows = kTcMaxRows;
     cudaError_t e;
     if (kv->tc) {
         e = attn_tc_init(kv);
     } else {
-        e = bf ? (fp8 ? core_attr<__nv_bfloat16, true>(D.head_dim) : core_attr<__nv_bfloat16, false>(D.head_dim))
-               : (fp8 ? core_attr<float, true>(D.head_dim) : core_attr<float, false>(D.head_dim));
+        e = raise_smem_limit(core_kernel(D), core_smem(D.head_dim));
         const int fit = 220 * 1024 / (core_smem(D.head_dim) + 2048);
         kv->core_ctas_per_sm = fit < 1 ? 1 : fit > 4 ? 4 : fit;
         ctas *= kv->core_ctas_per_sm;
@@ -311,15 +314,8 @@ cudaError_t attn_init(ace_kv* kv) {
 
 cudaError_t launch_tree_attention(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
     if (kv->tc) return launch_tree_attention_tc(kv, a, s);
-    const bool fp8 = kv->desc.format == ACE_KV_FP8;
-    const int grid = kv->num_sms * kv->core_ctas_per_sm, smem = core_smem(a.head_dim);
-    if (kv->desc.dtype == ACE_BF16) {
-        if (fp8) k_attn_core<__nv_bfloat16, true><<<grid, kThreads, smem, s>>>(a);
-        else k_attn_core<__nv_bfloat16, false><<<grid, kThreads, smem, s>>>(a);
-    } else {
-        if (fp8) k_attn_core<float, true><<<grid, kThreads, smem, s>>>(a);
-        else k_attn_core<float, false><<<grid, kThreads, smem, s>>>(a);
-    }
+    const int grid = kv->num_sms * kv->core_ctas_per_sm;
+    core_kernel(kv->desc)<<<grid, kThreads, core_smem(a.head_dim), s>>>(a);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? launch_join(a, kv->desc.dtype, false, kRows, grid, s) : e;
 }

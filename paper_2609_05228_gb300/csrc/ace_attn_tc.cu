@@ -752,7 +752,7 @@ static cudaError_t row_map(CUtensorMap* m, const void* base, uint64_t rows, bool
 }
 
 bool attn_tc_supported(const ace_kv* kv) {
-    return kv->desc.dtype == ACE_BF16 && (kv->desc.head_dim == 64 || kv->desc.head_dim == 128);
+    return kv->desc.dtype == ACE_BF16 && kv->desc.format != ACE_KV_INT4 && (kv->desc.head_dim == 64 || kv->desc.head_dim == 128);
 }
 
 cudaError_t attn_tc_init(ace_kv* kv) {

@@ -4,11 +4,9 @@
 
 #include <string>
 
-#include "ace_kv_device.cuh"
+#include "ace_kv_rows.cuh"
 
-namespace {
-
-using namespace ace;
+namespace ace {
 
 ace_status kv_fail(ace_status st, const std::string& m) {
     set_last_error(m.c_str());
@@ -19,78 +17,26 @@ ace_status kv_cuda(cudaError_t e, const char* where) {
     return kv_fail(ACE_ERR_CUDA, std::string(where) + ": " + cudaGetErrorName(e) + " (" + cudaGetErrorString(e) + ")");
 }
 
-// A launch goes to the current device: the cache's, or nothing is launched.
-ace_status kv_here(const ace_kv* kv) {
+ace_status on_device(int device, const char* what) {
     int dev = -1;
     const cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return kv_cuda(e, "cudaGetDevice");
-    return dev == kv->device ? ACE_OK : kv_fail(ACE_ERR_INVALID_ARG, "the cache belongs to another device than the current one");
+    return dev == device ? ACE_OK : kv_fail(ACE_ERR_INVALID_ARG, std::string("the ") + what + " belongs to another device than the current one");
 }
 
-struct RowArgs {
-    const void* src[2];                 // write: K and V
-    long long token_stride[2], head_stride[2];
-    void* dst[2];                       // read: K and V
-    uint8_t* pool[2];
-    uint8_t* scale[2];
-    const int64_t* slots;
-    uint32_t rows;                      // (layers *) T * 2 * H
-    long long n_slots;                  // of a layer
-    int T, H, D, page_size, page_shift;
-    int* err;
-};
+}  // namespace ace
 
-// Row (within the layer's pool) of head h at `slot`: [page][h][row].
-__device__ __forceinline__ long long pool_row(const RowArgs& p, long long slot, int h) {
-    return (((slot >> p.page_shift) * p.H + h) << p.page_shift) + (slot & (p.page_size - 1));
-}
+namespace {
 
-// 8 elements of a row as they lie in memory.
-template <typename T>
-struct Raw8 {
-    uint4 w[sizeof(T) / 2];
-    __device__ __forceinline__ void to_float(float (&f)[8]) const {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) Vec16<T>::to_float(w[i], f + i * Vec16<T>::N);
-    }
-};
+using namespace ace;
 
-template <typename T, bool ALIGNED>
-__device__ __forceinline__ Raw8<T> load8(const T* p) {
-    Raw8<T> r;
-    if constexpr (ALIGNED) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ld_stream(p + i * Vec16<T>::N);
-    } else {
-        T* e = reinterpret_cast<T*>(r.w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = p[i];
-    }
-    return r;
-}
+ace_status kv_here(const ace_kv* kv) { return on_device(kv->device, "cache"); }
 
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&v);
-        }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
-
-// Write: e the least with amax 2^-e <= 448, scale byte e + 127, codes = the row's elements times 2^-e in e4m3 (the only
-// rounding). LANES lanes (a power of two, at least D / 8) hold one row, 8 elements each: its largest magnitude is
+// Write. fp8: e the least with amax 2^-e <= 448, scale byte e + 127, codes = the row's elements times 2^-e in e4m3 (the only
+// rounding); int4: groups of 32 with a scale of 4 significant bits each. LANES lanes (a power of two, at least D / 8) hold one row, 8 elements each: its largest magnitude is
 // a shuffle reduction, nothing is read twice. Bound by memory: each group of lanes has kRowTurns neighbouring rows under way
 // together, and the rows are not waited for by way of their slots. Write and read back of 16384 tokens (8 heads of 128, bf16
 // to fp8): 51 us for 201 MB, 4.0 TB/s (46 with the rows in L2, 61 then with one row at a time).
-constexpr int kRowTurns = 4;
 
 // Row r of a call: (token, K or V, head), heads fastest.
 struct RowAt {
@@ -102,7 +48,7 @@ struct RowAt {
     }
 };
 
-template <typename T, bool FP8, bool ALIGNED, int LANES>
+template <typename T, int FMT, bool ALIGNED, int LANES>
 __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ RowArgs p) {
     const int sub = threadIdx.x % LANES;
     const bool in = sub * 8 < p.D;
@@ -127,37 +73,12 @@ __global__ void __launch_bounds__(256) k_kv_write(const __grid_constant__ RowArg
             if (sub == 0) atomicOr(p.err, kErrIndex);
             slot[j] = -1;
         }
-        const long long row = slot[j] >= 0 ? pool_row(p, slot[j], at.h) : 0;
-        const bool put = in && slot[j] >= 0;
-        if constexpr (FP8) {
-            float f[8], amax = 0.f;
-            raw[j].to_float(f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                f[i] = finite_or_nan(f[i]);
-                amax = fmaxf(amax, fabsf(f[i]));             // fmaxf drops NaN
-            }
-#pragma unroll
-            for (int o = LANES / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            const int byte = e4m3_scale_byte(amax);
-            const float m = pow2_of_minus_byte(byte);
-            if (put) {
-                uint2 w;
-                w.x = e4m3x2(f[0] * m, f[1] * m) | e4m3x2(f[2] * m, f[3] * m) << 16;
-                w.y = e4m3x2(f[4] * m, f[5] * m) | e4m3x2(f[6] * m, f[7] * m) << 16;
-                *reinterpret_cast<uint2*>(p.pool[kv] + row * p.D + sub * 8) = w;
-                if (sub == 0) p.scale[kv][row] = (uint8_t)byte;
-            }
-        } else if (put) {
-            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.pool[kv]) + row * p.D + sub * 8);
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) dst[i] = raw[j].w[i];
-        }
+        put_row<T, FMT, LANES>(p, kv, slot[j] >= 0 ? pool_row(p, slot[j], at.h) : 0, sub, in && slot[j] >= 0, raw[j]);
     }
 }
 
-// Read: code times 2^e, rounded to the storage type; the same lanes and turns as the write.
-template <typename T, bool FP8, int LANES>
+// Read: code times its scale, rounded to the storage type; the same lanes and turns as the write.
+template <typename T, int FMT, int LANES>
 __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ RowArgs p) {
     const int sub = threadIdx.x % LANES;
     if (sub * 8 >= p.D) return;
@@ -176,19 +97,27 @@ __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ RowArgs
             row[j] = layer * p.n_slots * p.H + pool_row(p, slot, at.h);
         }
     }
-    Raw8<T> raw[FP8 ? 1 : kRowTurns];
+    constexpr bool CODES = FMT != ACE_KV_PLAIN;
+    Raw8<T> raw[CODES ? 1 : kRowTurns];
     uint2 code[kRowTurns];
-    uint8_t byte[kRowTurns];
+    uint16_t scale[kRowTurns];
     at = RowAt(r0, p.H);
 #pragma unroll
     for (int j = 0; j < kRowTurns; ++j, at.next(p.H)) {
         const int kv = at.th & 1;
-        if constexpr (FP8) {
+        if constexpr (FMT == ACE_KV_INT4) {
+            code[j] = make_uint2(0x88888888u, 0);
+            scale[j] = 0;
+            if (row[j] >= 0) {
+                code[j].x = __ldg(reinterpret_cast<const uint32_t*>(p.pool[kv] + row[j] * (p.D / 2) + sub * 4));
+                scale[j] = __ldg(reinterpret_cast<const uint16_t*>(p.scale[kv]) + row[j] * groups4(p.D) + sub / 4);
+            }
+        } else if constexpr (FMT == ACE_KV_FP8) {
             code[j] = make_uint2(0, 0);
-            byte[j] = 1;
+            scale[j] = 1;
             if (row[j] >= 0) {
                 code[j] = __ldg(reinterpret_cast<const uint2*>(p.pool[kv] + row[j] * p.D + sub * 8));
-                byte[j] = __ldg(p.scale[kv] + row[j]);
+                scale[j] = __ldg(p.scale[kv] + row[j]);
             }
         } else {
             if (row[j] >= 0) raw[j] = load8<T, true>(reinterpret_cast<const T*>(p.pool[kv]) + row[j] * p.D + sub * 8);
@@ -200,12 +129,16 @@ __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ RowArgs
     for (int j = 0; j < kRowTurns; ++j, at.next(p.H)) {
         if (r0 + j >= p.rows) break;
         T* dst = static_cast<T*>(p.dst[at.th & 1]) + ((long long)(at.th >> 1) * p.H + at.h) * p.D + sub * 8;
-        if constexpr (FP8) {
+        if constexpr (CODES) {
             float f[8];
-            e4m3x8_to_float(code[j], f);
-            const float m = pow2_of_byte(byte[j]);
+            if constexpr (FMT == ACE_KV_INT4) {
+                int4x8_to_float(code[j].x, float_of_bf16(scale[j]), f);
+            } else {
+                e4m3x8_to_float(code[j], f);
+                const float m = pow2_of_byte(scale[j]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] *= m;
+                for (int i = 0; i < 8; ++i) f[i] *= m;
+            }
             store8(dst, f);
         } else {
 #pragma unroll
@@ -222,13 +155,31 @@ struct KeepArgs {
     const int32_t* path;
     const int32_t* n_keep;
     int32_t* new_lens;
-    int max_pages, max_nodes, H, row_words, page_size, page_shift, n_pages, layers;   // row_words: 8- or 16-byte words of a row
+    int max_pages, max_nodes, H, row_words, page_size, page_shift, n_pages, layers;   // row_words: words of a row
+    int scale_units;                    // int4: bf16 scales of a row; fp8: 0, a byte
     int* err;
 };
 
 constexpr int kKeepThreads = 256, kKeepWords = 4;
 
-// Block (request, share of the layers and heads); W is a word of 8 or 16 bytes. The path is looked up once; then all rows'
+// A share's scales of a request's kept rows, `units` of type U a row, in passes as the words below.
+template <typename U>
+__device__ __forceinline__ void keep_scales(const KeepArgs& p, int units, int lh0, int lh1, int n, const int* src_row, const int* dst_row,
+                                            long long layer_rows) {
+    const uint32_t of_head = 2u * n * units, all = (uint32_t)(lh1 - lh0) * of_head;
+    for (uint32_t w0 = 0; w0 < all; w0 += kKeepThreads) {
+        const uint32_t w = w0 + threadIdx.x, lh = w / of_head, rest = w - lh * of_head, i = rest / (2 * units), u = rest - i * 2 * units;
+        const int kv = u >= (uint32_t)units, layer = (lh0 + (int)lh) / p.H, h = lh0 + (int)lh - layer * p.H;
+        const long long head = layer * layer_rows + ((long long)h << p.page_shift);
+        U* scale = reinterpret_cast<U*>(p.scale[kv]) + (u - kv * units);
+        U v = 0;
+        if (w < all) v = scale[(head + src_row[i]) * units];
+        __syncthreads();
+        if (w < all) scale[(head + dst_row[i]) * units] = v;
+    }
+}
+
+// Block (request, share of the layers and heads); W is a word of 4, 8 or 16 bytes. The path is looked up once; then all rows'
 // words, in the order (layer, head), node, move in passes. Rows move towards the front (path[i] >= i and
 // increasing), so a pass that has read its words before it writes any never overwrites a word of a later pass. Bound by
 // memory: 128 requests of up to 64 nodes, 48 layers of 8 heads of 128, bf16: 77 us for 352 MB, 4.6 TB/s (110 with a block a
@@ -297,16 +248,8 @@ __global__ void __launch_bounds__(kKeepThreads) k_kv_keep(const __grid_constant_
             if (to[j]) *to[j] = v[j];
     }
     if (p.scale[0]) {
-        const uint32_t bytes = (uint32_t)(lh1 - lh0) * 2 * n;
-        for (uint32_t w0 = 0; w0 < bytes; w0 += kKeepThreads) {
-            const uint32_t w = w0 + tid, lh = w / (2 * n), rest = w - lh * 2 * n, i = rest >> 1;
-            const int layer = (lh0 + (int)lh) / p.H, h = lh0 + (int)lh - layer * p.H;
-            const long long head = layer * layer_rows + ((long long)h << p.page_shift);
-            uint8_t v = 0;
-            if (w < bytes) v = p.scale[rest & 1][head + src_row[i]];
-            __syncthreads();
-            if (w < bytes) p.scale[rest & 1][head + dst_row[i]] = v;
-        }
+        if (p.scale_units > 0) keep_scales<uint16_t>(p, p.scale_units, lh0, lh1, n, src_row, dst_row, layer_rows);
+        else keep_scales<uint8_t>(p, 1, lh0, lh1, n, src_row, dst_row, layer_rows);
     }
 }
 
@@ -344,16 +287,18 @@ int log2_of(int x) {
     return s;
 }
 
-RowArgs row_args(const ace_kv* kv, int layer, const int64_t* slots, int T) {
+}  // namespace
+
+RowArgs ace::row_args(const ace_kv* kv, int layer, const int64_t* slots, int T) {
     RowArgs p{};
     const ace_kv_desc& D = kv->desc;
     const long long rows = (long long)D.n_pages * D.n_kv_heads * D.page_size;
-    const int row_bytes = D.head_dim * (D.format == ACE_KV_FP8 ? 1 : kv->elem);
-    p.pool[0] = static_cast<uint8_t*>(kv->k_pool) + rows * row_bytes * layer;
-    p.pool[1] = static_cast<uint8_t*>(kv->v_pool) + rows * row_bytes * layer;
-    if (D.format == ACE_KV_FP8) {
-        p.scale[0] = kv->k_scale + rows * layer;
-        p.scale[1] = kv->v_scale + rows * layer;
+    const int bytes = row_bytes(D.format, D.head_dim, kv->elem), scales = scale_bytes(D.format, D.head_dim);
+    p.pool[0] = static_cast<uint8_t*>(kv->k_pool) + rows * bytes * layer;
+    p.pool[1] = static_cast<uint8_t*>(kv->v_pool) + rows * bytes * layer;
+    if (scales) {
+        p.scale[0] = kv->k_scale + rows * scales * layer;
+        p.scale[1] = kv->v_scale + rows * scales * layer;
     }
     p.slots = slots;
     p.n_slots = kv->slots;
@@ -366,26 +311,38 @@ RowArgs row_args(const ace_kv* kv, int layer, const int64_t* slots, int T) {
     return p;
 }
 
+namespace {
+
 // Blocks for all rows, `groups` groups of lanes a block.
 unsigned row_grid(uint32_t rows, int groups) { return (rows + groups * kRowTurns - 1) / (groups * kRowTurns); }
 
-template <typename T, bool FP8, bool ALIGNED>
-void write_rows(const RowArgs& p, cudaStream_t s) {
-    if (p.D <= 64) k_kv_write<T, FP8, ALIGNED, 8><<<row_grid(p.rows, 32), 256, 0, s>>>(p);
-    else if (p.D <= 128) k_kv_write<T, FP8, ALIGNED, 16><<<row_grid(p.rows, 16), 256, 0, s>>>(p);
-    else k_kv_write<T, FP8, ALIGNED, 32><<<row_grid(p.rows, 8), 256, 0, s>>>(p);
+template <typename T, int FMT, bool ALIGNED>
+void write_rows_of(const RowArgs& p, cudaStream_t s) {
+    if (p.D <= 64) k_kv_write<T, FMT, ALIGNED, 8><<<row_grid(p.rows, 32), 256, 0, s>>>(p);
+    else if (p.D <= 128) k_kv_write<T, FMT, ALIGNED, 16><<<row_grid(p.rows, 16), 256, 0, s>>>(p);
+    else k_kv_write<T, FMT, ALIGNED, 32><<<row_grid(p.rows, 8), 256, 0, s>>>(p);
 }
 
-template <typename T, bool FP8>
-void read_rows(const RowArgs& p, cudaStream_t s) {
-    if (p.D <= 64) k_kv_read<T, FP8, 8><<<row_grid(p.rows, 32), 256, 0, s>>>(p);
-    else if (p.D <= 128) k_kv_read<T, FP8, 16><<<row_grid(p.rows, 16), 256, 0, s>>>(p);
-    else k_kv_read<T, FP8, 32><<<row_grid(p.rows, 8), 256, 0, s>>>(p);
+template <typename T, bool ALIGNED>
+void write_rows(int format, const RowArgs& p, cudaStream_t s) {
+    if (format == ACE_KV_INT4) write_rows_of<T, ACE_KV_INT4, ALIGNED>(p, s);
+    else if (format == ACE_KV_FP8) write_rows_of<T, ACE_KV_FP8, ALIGNED>(p, s);
+    else write_rows_of<T, ACE_KV_PLAIN, ALIGNED>(p, s);
 }
 
-constexpr long long kMaxRows = 1LL << 30;       // of a write or read call: row numbers are 32-bit
+template <typename T, int FMT>
+void read_rows_of(const RowArgs& p, cudaStream_t s) {
+    if (p.D <= 64) k_kv_read<T, FMT, 8><<<row_grid(p.rows, 32), 256, 0, s>>>(p);
+    else if (p.D <= 128) k_kv_read<T, FMT, 16><<<row_grid(p.rows, 16), 256, 0, s>>>(p);
+    else k_kv_read<T, FMT, 32><<<row_grid(p.rows, 8), 256, 0, s>>>(p);
+}
 
-bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
+template <typename T>
+void read_rows(int format, const RowArgs& p, cudaStream_t s) {
+    if (format == ACE_KV_INT4) read_rows_of<T, ACE_KV_INT4>(p, s);
+    else if (format == ACE_KV_FP8) read_rows_of<T, ACE_KV_FP8>(p, s);
+    else read_rows_of<T, ACE_KV_PLAIN>(p, s);
+}
 
 }  // namespace
 
@@ -399,16 +356,16 @@ ace_status ace_kv_create(const ace_kv_desc* desc, void* k_pool, void* v_pool, vo
     if (D.layers <= 0 || D.n_pages <= 0 || D.page_size <= 0 || D.n_kv_heads <= 0 || D.head_dim <= 0)
         return kv_fail(ACE_ERR_INVALID_ARG, "layers, n_pages, page_size, n_kv_heads and head_dim must be positive");
     if (D.dtype != ACE_BF16 && D.dtype != ACE_F32) return kv_fail(ACE_ERR_INVALID_ARG, "unknown dtype");
-    if (D.format != ACE_KV_PLAIN && D.format != ACE_KV_FP8) return kv_fail(ACE_ERR_INVALID_ARG, "unknown cache format");
+    if (D.format != ACE_KV_PLAIN && D.format != ACE_KV_FP8 && D.format != ACE_KV_INT4) return kv_fail(ACE_ERR_INVALID_ARG, "unknown cache format");
     if (D.page_size < 16 || D.page_size > 256 || (D.page_size & (D.page_size - 1)))
         return kv_fail(ACE_ERR_UNSUPPORTED, "page_size must be 16, 32, 64, 128 or 256");
     if (D.head_dim % 8 || D.head_dim > kMaxHeadDim)
         return kv_fail(ACE_ERR_UNSUPPORTED, "head_dim must be a multiple of 8, at most 256");
     if (!k_pool || !v_pool) return kv_fail(ACE_ERR_INVALID_ARG, "k_pool and v_pool must be non-NULL");
     if (!aligned16(k_pool) || !aligned16(v_pool)) return kv_fail(ACE_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
-    if (D.format == ACE_KV_FP8 && (!k_scale || !v_scale))
-        return kv_fail(ACE_ERR_INVALID_ARG, "an fp8 cache needs k_scale and v_scale");
-    if (D.format == ACE_KV_FP8 && (!aligned16(k_scale) || !aligned16(v_scale)))     // the attention reads four at a time
+    if (D.format != ACE_KV_PLAIN && (!k_scale || !v_scale))
+        return kv_fail(ACE_ERR_INVALID_ARG, "an fp8 or int4 cache needs k_scale and v_scale");
+    if (D.format != ACE_KV_PLAIN && (!aligned16(k_scale) || !aligned16(v_scale)))     // the attention reads four at a time
         return kv_fail(ACE_ERR_INVALID_ARG, "the scales must be 16-byte aligned");
     // products one at a time, each below 2^31 before the next
     long long rows = (long long)D.n_pages * D.page_size;
@@ -421,8 +378,8 @@ ace_status ace_kv_create(const ace_kv_desc* desc, void* k_pool, void* v_pool, vo
     kv->elem = D.dtype == ACE_BF16 ? 2 : 4;
     kv->k_pool = k_pool;
     kv->v_pool = v_pool;
-    kv->k_scale = static_cast<uint8_t*>(D.format == ACE_KV_FP8 ? k_scale : nullptr);
-    kv->v_scale = static_cast<uint8_t*>(D.format == ACE_KV_FP8 ? v_scale : nullptr);
+    kv->k_scale = static_cast<uint8_t*>(D.format != ACE_KV_PLAIN ? k_scale : nullptr);
+    kv->v_scale = static_cast<uint8_t*>(D.format != ACE_KV_PLAIN ? v_scale : nullptr);
     kv->slots = (long long)D.n_pages * D.page_size;
     kv->last_stream = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaGetDevice(&kv->device);
@@ -489,14 +446,9 @@ ace_status ace_kv_write(ace_kv* kv, int layer, const void* k, long long k_token_
     const long long vec = 16 / kv->elem;
     const bool al = aligned16(k) && aligned16(v) && k_token_stride % vec == 0 && k_head_stride % vec == 0 &&
                     v_token_stride % vec == 0 && v_head_stride % vec == 0;
-    const bool fp8 = kv->desc.format == ACE_KV_FP8;
-    if (kv->desc.dtype == ACE_BF16) {
-        if (fp8) al ? write_rows<__nv_bfloat16, true, true>(p, s) : write_rows<__nv_bfloat16, true, false>(p, s);
-        else al ? write_rows<__nv_bfloat16, false, true>(p, s) : write_rows<__nv_bfloat16, false, false>(p, s);
-    } else {
-        if (fp8) al ? write_rows<float, true, true>(p, s) : write_rows<float, true, false>(p, s);
-        else al ? write_rows<float, false, true>(p, s) : write_rows<float, false, false>(p, s);
-    }
+    const int format = kv->desc.format;
+    if (kv->desc.dtype == ACE_BF16) al ? write_rows<__nv_bfloat16, true>(format, p, s) : write_rows<__nv_bfloat16, false>(format, p, s);
+    else al ? write_rows<float, true>(format, p, s) : write_rows<float, false>(format, p, s);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? ACE_OK : kv_cuda(e, "cache write launch");
 }
@@ -517,9 +469,8 @@ ace_status ace_kv_read(ace_kv* kv, int layer, const int64_t* slots, int T, void*
     p.rows = (uint32_t)rows;
     p.dst[0] = k_out;
     p.dst[1] = v_out;
-    const bool fp8 = kv->desc.format == ACE_KV_FP8;
-    if (kv->desc.dtype == ACE_BF16) fp8 ? read_rows<__nv_bfloat16, true>(p, s) : read_rows<__nv_bfloat16, false>(p, s);
-    else fp8 ? read_rows<float, true>(p, s) : read_rows<float, false>(p, s);
+    if (kv->desc.dtype == ACE_BF16) read_rows<__nv_bfloat16>(kv->desc.format, p, s);
+    else read_rows<float>(kv->desc.format, p, s);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? ACE_OK : kv_cuda(e, "cache read launch");
 }
@@ -549,8 +500,9 @@ ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, con
     p.max_pages = max_pages;
     p.max_nodes = max_nodes;
     p.H = D.n_kv_heads;
-    const int row_bytes = D.head_dim * (D.format == ACE_KV_FP8 ? 1 : kv->elem), word = row_bytes % 16 ? 8 : 16;
-    p.row_words = row_bytes / word;
+    const int bytes = row_bytes(D.format, D.head_dim, kv->elem), word = bytes % 8 ? 4 : bytes % 16 ? 8 : 16;
+    p.row_words = bytes / word;
+    p.scale_units = D.format == ACE_KV_INT4 ? groups4(D.head_dim) : 0;
     p.page_size = D.page_size;
     p.page_shift = r.page_shift;
     p.n_pages = D.n_pages;
@@ -563,7 +515,8 @@ ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, con
     if (shares > all) shares = all;
     const dim3 grid(B, (unsigned)shares);
     if (word == 16) k_kv_keep<uint4><<<grid, kKeepThreads, 0, s>>>(p);
-    else k_kv_keep<uint2><<<grid, kKeepThreads, 0, s>>>(p);
+    else if (word == 8) k_kv_keep<uint2><<<grid, kKeepThreads, 0, s>>>(p);
+    else k_kv_keep<uint32_t><<<grid, kKeepThreads, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? ACE_OK : kv_cuda(e, "cache keep launch");
 }

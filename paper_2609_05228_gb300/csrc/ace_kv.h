@@ -1,6 +1,8 @@
 // ace_kv.h — the cache handle and what the speculative decode step's kernels share.
 #pragma once
 
+#include <string>
+
 #include "ace_internal.h"
 
 namespace ace {
@@ -11,6 +13,12 @@ constexpr int kErrIndex = 8;
 
 constexpr int kMaxNodes = 256;          // nodes of a request's tree
 constexpr int kMaxHeadDim = 256;
+constexpr int kGroup4 = 32;             // elements that share a scale in ACE_KV_INT4
+
+__host__ __device__ constexpr int groups4(int D) { return (D + kGroup4 - 1) / kGroup4; }
+// Bytes of a cached row, and of its scale or scales.
+__host__ __device__ constexpr int row_bytes(int format, int D, int elem) { return format == ACE_KV_INT4 ? D / 2 : format == ACE_KV_FP8 ? D : D * elem; }
+__host__ __device__ constexpr int scale_bytes(int format, int D) { return format == ACE_KV_INT4 ? 2 * groups4(D) : format == ACE_KV_FP8 ? 1 : 0; }
 
 // A CTA's part of a unit.
 struct Segment {
@@ -55,6 +63,30 @@ struct ace_kv {
 };
 
 namespace ace {
+
+ace_status kv_fail(ace_status st, const std::string& message);
+ace_status kv_cuda(cudaError_t e, const char* where);
+// A launch goes to the current device: that of the `what`, or nothing is launched.
+ace_status on_device(int device, const char* what);
+inline bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
+
+constexpr long long kMaxRows = 1LL << 30;       // of a write or read call: row numbers are 32-bit
+
+struct RowArgs {
+    const void* src[2];                 // write: K and V
+    long long token_stride[2], head_stride[2];
+    void* dst[2];                       // read: K and V
+    uint8_t* pool[2];
+    uint8_t* scale[2];
+    const int64_t* slots;
+    uint32_t rows;                      // (layers *) T * 2 * H
+    long long n_slots;                  // of a layer
+    int T, H, D, page_size, page_shift;
+    int* err;
+};
+
+// What a call says of the layer and the tokens' slots; src, strides, dst and rows are left to it.
+RowArgs row_args(const ace_kv* kv, int layer, const int64_t* slots, int T);
 
 struct AttnArgs {
     const void* q;

@@ -56,6 +56,36 @@ __device__ __forceinline__ float finite_or_nan(float x) {
     return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __uint_as_float(0x7fffffffu) : x;
 }
 
+// ---------------------------------------------------------------- rows in 4 bits
+
+// Scale of a group whose largest |x| is amax (finite): the smallest number of 4 significant bits that amax <= 7 times it.
+// amax / 7 rounded towards zero to 4 bits is at most a step from it, whatever its own rounding; 7 s is exact.
+__device__ __forceinline__ float int4_scale(float amax) {
+    if (!(amax > 7.f * 0x1p-126f)) return 0x1p-126f;
+    const uint32_t b = __float_as_uint(amax * (1.f / 7.f)) & 0xfff00000u;
+    float s = __uint_as_float(b);
+    if (7.f * s < amax) s = __uint_as_float(b + 0x100000u);
+    else if (7.f * __uint_as_float(b - 0x100000u) >= amax) s = __uint_as_float(b - 0x100000u);
+    return fminf(fmaxf(s, 0x1p-126f), 1.125f * 0x1p125f);
+}
+
+// x / s rounded to nearest even, -7 .. 7, plus 8; inv = 1 / s. The product with inv may lie on the wrong side of a half, so the
+// remainder decides (exact: x is a whole number of its last place, at most 2 s away).
+__device__ __forceinline__ uint32_t int4_code(float x, float s, float inv) {
+    float q = rintf(x * inv);
+    const float r = fmaf(-q, s, x), half = 0.5f * s;
+    if (fabsf(r) > half || (fabsf(r) == half && (static_cast<int>(q) & 1))) q += copysignf(1.f, r);
+    return (uint32_t)(static_cast<int>(fminf(fmaxf(q, -7.f), 7.f)) + 8);
+}
+
+// 8 codes times their scale (exact: 3 significant bits times 4).
+__device__ __forceinline__ void int4x8_to_float(uint32_t w, float s, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (float)(static_cast<int>(w >> (4 * i) & 15u) - 8) * s;
+}
+
+__device__ __forceinline__ float float_of_bf16(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+
 // ---------------------------------------------------------------- requests and their share of the work
 
 struct Request {
