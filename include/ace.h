@@ -394,6 +394,9 @@ ace_status ace_layer_get_desc(const ace_layer* layer, ace_layer_desc* desc);
  *   ace_verify_tree     which nodes are accepted, and the next token
  *   ace_kv_keep         the accepted nodes' rows move to positions lens[b] + 0, 1, ..
  *
+ * Around them: ace_rope_apply and ace_kv_write_rotated (rotary positions), ace_kv_fork, ace_kv_reserve, ace_kv_release,
+ * ace_kv_compact and ace_kv_copy_pages (the life of the cache's pages).
+ *
  * Cache memory belongs to the caller. With H = n_kv_heads, P = page_size, D = head_dim:
  *   pool   [layers, n_pages, H, P, D]   K and V each; position p of request b is row
  *          p % P of page page_table[b, p / P]; slot = page * P + row
@@ -414,7 +417,7 @@ ace_status ace_layer_get_desc(const ace_layer* layer, ace_layer_desc* desc);
  * lower half. A group with a NaN or an infinity has the scale NaN: all of it
  * stands for NaN. A row of 128 takes 72 bytes (fp8: 129, bf16: 256).
  */
-typedef enum ace_kv_format { ACE_KV_PLAIN = 0, ACE_KV_FP8 = 1, ACE_KV_INT4 = 2 } ace_kv_format;
+typedef enum ace_kv_format { ACE_KV_PLAIN = 0, ACE_KV_FP8 = 1, ACE_KV_INT4 = 4 } ace_kv_format;
 
 typedef struct ace_kv_desc {
     int layers;          /* >= 1 */
@@ -483,6 +486,53 @@ ace_status ace_kv_read(ace_kv* kv, int layer, const int64_t* slots, int T, void*
  */
 ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, const int32_t* lens, const int32_t* path,
                        int max_nodes, const int32_t* n_keep, int B, int32_t* new_lens, void* stream);
+
+/*
+ * Pages of requests that come, fork and go. The caller keeps, in device memory,
+ *   refs        [n_pages] int32: how many entries of its page tables name the page; 0: the page is free
+ *   page_table  [B, max_pages] int32: entries that name no page are negative
+ * and a request holds every page that its row names. The calls below are asynchronous, allocate nothing and can be captured;
+ * what they decide they decide on the device. Errors of all: INVALID_ARG (NULL, sizes, overlapping arrays, device), CUDA.
+ *
+ * ace_kv_fork - requests after a step that keeps some of them, more than once or not at all: request b of the new batch has the
+ * pages of its parent's lens tokens, and -1 behind them, lens as its parent's; without a parent it is empty. The counts lose what
+ * the old rows named and gain what the new ones name, so pages that nobody holds any more are free. No rows are copied: forked
+ * requests share their pages, the last, partly filled one too, until ace_kv_reserve.
+ *   parents     [B_out] int32: a row of the old tables, negative for none
+ *   new_table   [B_out, max_pages] int32 out, new_lens [B_out] int32 out; apart from the old ones
+ * A parent past the old rows, a length past its row, a page that does not exist are left out (no parent, an empty request, -1) and
+ * reported by ace_kv_sync.
+ *
+ * ace_kv_reserve - room for grow[b] more tokens of each request: its partly filled page, where other requests hold it too, is
+ * replaced by a fresh one with a copy of its rows, in all layers; entries up to position lens[b] + grow[b] that name no page get
+ * fresh ones. (Of requests that hold a partly filled page and grow, the last keeps it if nobody else does.) Fresh pages are
+ * those with a count of 0 before the call, the lowest first, for request by request, each the copy before the rest.
+ *   grow        [B] int32 >= 0
+ *   missing     [1] int32 out: 0, or how many pages the pool is short of; then nothing was changed
+ * B is at most 8192, and B * max_pages 2^29 (UNSUPPORTED above). A request whose lens or grow is negative, whose tokens leave its row or whose partly
+ * filled page does not exist is left out and reported by ace_kv_sync.
+ *
+ * ace_kv_release - requests b with ended[b] != 0 give their pages back: counts fall, their entries become -1, their lens 0.
+ *
+ * ace_kv_compact - with n pages in use, those at n and above move into the free ones below n (the i-th into the i-th, in all
+ * layers); the tables' entries and the counts follow, so that pages n .. n_pages - 1 are free.
+ *   used        [1] int32 out: n
+ *   new_page    [n_pages] int32 out, or NULL: where each page is now, -1 for those that were free
+ * An entry that names a page with a count of 0, or none of the pool's, becomes -1 and is reported.
+ *
+ * ace_kv_copy_pages - page src[i] to page dst[i] in all layers, rows and scales as they are, i < n. Entries that name a page
+ * outside the pool, a dst that another entry names too, or one that is another's src, are left out and reported; src[i] = dst[i]
+ * is nothing to do. Counts and tables are the caller's.
+ */
+ace_status ace_kv_fork(ace_kv* kv, const int32_t* page_table, const int32_t* lens, int B, const int32_t* parents, int B_out,
+                       int max_pages, int32_t* refs, int32_t* new_table, int32_t* new_lens, void* stream);
+ace_status ace_kv_reserve(ace_kv* kv, int32_t* page_table, int max_pages, const int32_t* lens, const int32_t* grow, int B,
+                          int32_t* refs, int32_t* missing, void* stream);
+ace_status ace_kv_release(ace_kv* kv, int32_t* page_table, int max_pages, int32_t* lens, const int32_t* ended, int B, int32_t* refs,
+                          void* stream);
+ace_status ace_kv_compact(ace_kv* kv, int32_t* page_table, int max_pages, int B, int32_t* refs, int32_t* used, int32_t* new_page,
+                          void* stream);
+ace_status ace_kv_copy_pages(ace_kv* kv, const int32_t* src, const int32_t* dst, int n, void* stream);
 
 /*
  * Rotary positions: dimensions 0 .. rot_dim - 1 of a row are turned in pairs by its token's position p,

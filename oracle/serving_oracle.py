@@ -86,3 +86,63 @@ def rotate(x, positions, freq, layout="half", magnitude=1.0, inverse=False):
     u, w = x[..., a].copy(), x[..., b].copy()
     x[..., a], x[..., b] = u * c - w * s, u * s + w * c
     return x
+
+
+def fork(table, lens, parents, refs, page):
+    """(new table, new lens, new refs), row by row."""
+    refs = refs.copy()
+    new, new_lens = np.full((len(parents), table.shape[1]), -1, np.int32), np.zeros(len(parents), np.int32)
+    for row in table:
+        for x in row[row >= 0]:
+            refs[x] -= 1
+    for b, p in enumerate(parents):
+        if p >= 0:
+            n = -(-int(lens[p]) // page)
+            new[b, :n], new_lens[b] = table[p, :n], lens[p]
+            for x in new[b, :n]:
+                refs[x] += 1
+    return new, new_lens, refs
+
+
+def reserve(table, lens, grow, refs, page):
+    """(table, refs, missing, moves): request after request, as the free pages are at the beginning; moves are (from, to, rows)."""
+    new, now, moves = table.copy(), refs.copy(), []
+    free = [int(x) for x in np.nonzero(refs == 0)[0]]
+    asked = 0
+
+    def take():
+        nonlocal asked
+        asked += 1
+        return free[asked - 1] if asked <= len(free) else None
+    for b in range(len(lens)):
+        if grow[b] == 0:
+            continue
+        first, end = -(-int(lens[b]) // page), -(-int(lens[b] + grow[b]) // page)
+        if lens[b] % page:
+            x = new[b, first - 1]
+            if now[x] > 1:
+                y = take()
+                now[x] -= 1
+                if y is not None:
+                    moves.append((int(x), y, int(lens[b] % page)))
+                    new[b, first - 1], now[y] = y, 1
+        for i in range(first, end):
+            if new[b, i] < 0:
+                y = take()
+                if y is not None:
+                    new[b, i], now[y] = y, 1
+    if asked > len(free):
+        return table.copy(), refs.copy(), asked - len(free), []
+    return new, now, 0, moves
+
+
+def compact(table, refs):
+    """(table, refs, pages in use, their places, moves)."""
+    n = int((refs > 0).sum())
+    high = [x for x in range(n, len(refs)) if refs[x] > 0]
+    low = [x for x in range(n) if refs[x] == 0]
+    at = np.where(refs > 0, np.arange(len(refs)), -1).astype(np.int32)
+    refs = refs.copy()
+    for a, b in zip(high, low):
+        at[a], refs[b], refs[a] = b, refs[a], 0
+    return np.where(table >= 0, at[table], -1).astype(np.int32), refs, n, at, list(zip(high, low))

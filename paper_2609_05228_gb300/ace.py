@@ -20,7 +20,7 @@ LIBPATH = os.path.join(_LIBDIR, LIBNAME)
 
 ACE_BF16, ACE_F32 = 0, 1
 ACE_SKIP_THRESHOLD, ACE_SKIP_RATIO = 0, 1
-ACE_KV_PLAIN, ACE_KV_FP8, ACE_KV_INT4 = 0, 1, 2
+ACE_KV_PLAIN, ACE_KV_FP8, ACE_KV_INT4 = 0, 1, 4
 ACE_ROPE_HALF, ACE_ROPE_INTERLEAVED = 0, 1
 # Scaling of rotary frequencies (ace_rope_scaling): index = enum value.
 ROPE_SCALINGS = ("none", "linear", "by_turns", "by_index")
@@ -104,6 +104,11 @@ def lib() -> ctypes.CDLL:
             "ace_stack_forward_host": (_S, [_P, _P, _P, _I, ace_skip_ctl, _P]),
             "ace_offline_tables_device": (_S, [_I, _I, _I, _P, _P, _P, _P, _P, ctypes.c_double, _I, ctypes.c_size_t,
                                                _P, _P, _P]),
+            "ace_kv_fork": (_S, [_P, _P, _P, _I, _P, _I, _I, _P, _P, _P, _P]),
+            "ace_kv_reserve": (_S, [_P, _P, _I, _P, _P, _I, _P, _P, _P]),
+            "ace_kv_release": (_S, [_P, _P, _I, _P, _P, _I, _P, _P]),
+            "ace_kv_compact": (_S, [_P, _P, _I, _I, _P, _P, _P, _P]),
+            "ace_kv_copy_pages": (_S, [_P, _P, _P, _I, _P]),
             "ace_rope_create": (_S, [ctypes.POINTER(ace_rope_desc), ctypes.POINTER(ctypes.c_double), _P, ctypes.POINTER(_P)]),
             "ace_rope_destroy": (None, [_P]),
             "ace_rope_apply": (_S, [_P, _I, _P, _I, _P, _LL, _LL, _I, _P, _LL, _LL, _P, _LL, _LL, _I, _P, _LL, _LL, _P]),
@@ -345,6 +350,27 @@ def ace_kv_keep(kv: int, page_table, max_pages: int, lens, path, max_nodes: int,
                 stream=None) -> None:
     _check(lib().ace_kv_keep(kv, _ptr(page_table), max_pages, _ptr(lens), _ptr(path), max_nodes, _ptr(n_keep), B,
                              _ptr(new_lens), _stream(stream)))
+
+
+def ace_kv_fork(kv: int, page_table, lens, B: int, parents, B_out: int, max_pages: int, refs, new_table, new_lens, stream=None) -> None:
+    _check(lib().ace_kv_fork(kv, _ptr(page_table), _ptr(lens), B, _ptr(parents), B_out, max_pages, _ptr(refs), _ptr(new_table),
+                             _ptr(new_lens), _stream(stream)))
+
+
+def ace_kv_reserve(kv: int, page_table, max_pages: int, lens, grow, B: int, refs, missing, stream=None) -> None:
+    _check(lib().ace_kv_reserve(kv, _ptr(page_table), max_pages, _ptr(lens), _ptr(grow), B, _ptr(refs), _ptr(missing), _stream(stream)))
+
+
+def ace_kv_release(kv: int, page_table, max_pages: int, lens, ended, B: int, refs, stream=None) -> None:
+    _check(lib().ace_kv_release(kv, _ptr(page_table), max_pages, _ptr(lens), _ptr(ended), B, _ptr(refs), _stream(stream)))
+
+
+def ace_kv_compact(kv: int, page_table, max_pages: int, B: int, refs, used, new_page=None, stream=None) -> None:
+    _check(lib().ace_kv_compact(kv, _ptr(page_table), max_pages, B, _ptr(refs), _ptr(used), _ptr(new_page), _stream(stream)))
+
+
+def ace_kv_copy_pages(kv: int, src, dst, n: int, stream=None) -> None:
+    _check(lib().ace_kv_copy_pages(kv, _ptr(src), _ptr(dst), n, _stream(stream)))
 
 
 def ace_rope_create(desc: ace_rope_desc, divisors=None, stream=None) -> int:
@@ -646,6 +672,55 @@ class AceKvCache:
             _want("lse", lse, "float32", (T, heads))
         ace_tree_attention(self.handle, layer, q, *qs, heads, page_table, max_pages, lens, node_offsets, mask, B, T,
                            max_nodes, self.head_dim ** -0.5 if scale is None else scale, out, lse, _stream_for(q, stream))
+
+    def _table(self, page_table, refs):
+        """(B, max_pages) of a page table, with the pages' counts."""
+        _want("page_table", page_table, "int32", (None, None))
+        _want("refs", refs, "int32", (self.n_pages,))
+        return page_table.shape
+
+    def fork(self, page_table, lens, parents, refs, new_table, new_lens, stream=None) -> None:
+        """Row b of new_table and new_lens becomes row parents[b] (int32, negative: empty) of page_table and lens; refs [n_pages]
+        int32 follow. Rows are shared until `reserve`."""
+        B, max_pages = self._table(page_table, refs)
+        B_out = parents.shape[0]
+        _want("lens", lens, "int32", (B,))
+        _want("new_table", new_table, "int32", (B_out, max_pages))
+        for name, t in (("parents", parents), ("new_lens", new_lens)):
+            _want(name, t, "int32", (B_out,))
+        ace_kv_fork(self.handle, page_table, lens, B, parents, B_out, max_pages, refs, new_table, new_lens, _stream_for(page_table, stream))
+
+    def reserve(self, page_table, lens, grow, refs, missing, stream=None) -> None:
+        """Pages for grow[b] (int32) more tokens of every request; partly filled pages that others hold too are copied. missing [1]
+        int32: pages that the pool is short of (then nothing was changed), or 0."""
+        B, max_pages = self._table(page_table, refs)
+        for name, t in (("lens", lens), ("grow", grow)):
+            _want(name, t, "int32", (B,))
+        _want("missing", missing, "int32", (1,))
+        ace_kv_reserve(self.handle, page_table, max_pages, lens, grow, B, refs, missing, _stream_for(page_table, stream))
+
+    def release(self, page_table, lens, ended, refs, stream=None) -> None:
+        """Requests with ended[b] (int32) other than 0 give their pages back and are empty."""
+        B, max_pages = self._table(page_table, refs)
+        for name, t in (("lens", lens), ("ended", ended)):
+            _want(name, t, "int32", (B,))
+        ace_kv_release(self.handle, page_table, max_pages, lens, ended, B, refs, _stream_for(page_table, stream))
+
+    def compact(self, page_table, refs, used, new_page=None, stream=None) -> None:
+        """The pages in use move to the front of the pool, page_table and refs follow; used [1] int32: how many they are;
+        new_page [n_pages] int32: where each page is now."""
+        B, max_pages = self._table(page_table, refs)
+        _want("used", used, "int32", (1,))
+        if new_page is not None:
+            _want("new_page", new_page, "int32", (self.n_pages,))
+        ace_kv_compact(self.handle, page_table, max_pages, B, refs, used, new_page, _stream_for(page_table, stream))
+
+    def copy_pages(self, src, dst, stream=None) -> None:
+        """Pages src [n] int32 to pages dst [n], in every layer."""
+        n = src.shape[0]
+        for name, t in (("src", src), ("dst", dst)):
+            _want(name, t, "int32", (n,))
+        ace_kv_copy_pages(self.handle, src, dst, n, _stream_for(src, stream))
 
     def sync(self) -> None:
         """Waits for the last call and raises AceError for what its kernels found."""

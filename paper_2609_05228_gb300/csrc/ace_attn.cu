@@ -301,12 +301,17 @@ cudaError_t attn_init(ace_kv* kv) {
         rows = kRows;
     }
     if (e != cudaSuccess) return e;
-    // error word, notes of units, maxima and sums, outputs
-    const size_t head = (256 + ctas * sizeof(Segment) + 255) / 256 * 256, ml = (2 * ctas * rows * sizeof(float2) + 255) / 256 * 256;
+    // error word and count of moves, notes of units, pages' marks, list and moves; maxima and sums, outputs
+    const size_t pages = 256 + (ctas * sizeof(Segment) + 255) / 256 * 256, n_pages = D.n_pages;
+    const size_t head = pages + (n_pages * (3 * sizeof(int) + sizeof(int3)) + 255) / 256 * 256, ml = (2 * ctas * rows * sizeof(float2) + 255) / 256 * 256;
     if ((e = cudaMalloc(&kv->block, head + ml + 2 * ctas * rows * D.head_dim * sizeof(float))) != cudaSuccess) return e;
     char* at = static_cast<char*>(kv->block);
     kv->err = reinterpret_cast<int*>(at);
     kv->ws.unit = reinterpret_cast<Segment*>(at + 256);
+    kv->pages.count = reinterpret_cast<int*>(at + 128);
+    kv->pages.mark = reinterpret_cast<int*>(at + pages);
+    kv->pages.list = kv->pages.mark + 2 * n_pages;
+    kv->pages.move = reinterpret_cast<int3*>(kv->pages.list + n_pages);
     kv->ws.part_ml = reinterpret_cast<float2*>(at + head);
     kv->ws.part_o = reinterpret_cast<float*>(at + head + ml);
     return cudaMemsetAsync(at, 0, head, kv->last_stream);

@@ -37,6 +37,14 @@ struct AttnWorkspace {
     Segment* unit = nullptr;            // [ctas] the cut unit that begins in a CTA (rows = 0: none)
 };
 
+// Workspace of the calls that plan on the device which pages move.
+struct PageWorkspace {
+    int* count = nullptr;               // moves of the last plan
+    int3* move = nullptr;               // [n_pages] source, destination, rows of each head
+    int* mark = nullptr;                // [2 * n_pages] zeros between calls
+    int* list = nullptr;                // [n_pages]
+};
+
 struct KvMaps {                         // tensor-core attention (head sizes 64 and 128, bf16)
     CUtensorMap k, v;
 };
@@ -56,6 +64,7 @@ struct ace_kv {
     void* block = nullptr;              // one allocation for what follows
     int* err = nullptr;
     ace::AttnWorkspace ws;
+    ace::PageWorkspace pages;
     int core_ctas_per_sm = 1;           // CUDA-core attention
     bool tc = false;                    // tensor-core attention in use
     ace::KvMaps maps;

@@ -239,7 +239,7 @@ class Step:
                 none, nan = np.isneginf(wl), np.isnan(wl)
                 assert (np.isneginf(g) == none).all() and (np.isnan(g) == nan).all()
                 some = ~none & ~nan
-                assert (np.abs(g - wl)[some] <= (ds + (L + 16) * 2.0 ** -24)[some] + 2.0 ** -22 * np.abs(wl[some])).all()
+                assert (np.abs(g[some] - wl[some]) <= (ds + (L + 16) * 2.0 ** -24)[some] + 2.0 ** -22 * np.abs(wl[some])).all()
 
 
 TYPES = [("bf16", 128), ("bf16", 64), ("bf16", 80), ("bf16", 256), ("f32", 64), ("f32", 24)]
