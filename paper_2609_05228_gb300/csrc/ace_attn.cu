@@ -302,7 +302,8 @@ cudaError_t attn_init(ace_kv* kv) {
     }
     if (e != cudaSuccess) return e;
     // error word and count of moves, notes of units, pages' marks, list and moves; maxima and sums, outputs
-    const size_t pages = 256 + (ctas * sizeof(Segment) + 255) / 256 * 256, n_pages = D.n_pages;
+    const size_t units = D.format == ACE_KV_INT4 && kv->tc ? 2 * ctas : ctas;       // CTAs of a launch
+    const size_t pages = 256 + (units * sizeof(Segment) + 255) / 256 * 256, n_pages = D.n_pages;
     const size_t head = pages + (n_pages * (3 * sizeof(int) + sizeof(int3)) + 255) / 256 * 256, ml = (2 * ctas * rows * sizeof(float2) + 255) / 256 * 256;
     if ((e = cudaMalloc(&kv->block, head + ml + 2 * ctas * rows * D.head_dim * sizeof(float))) != cudaSuccess) return e;
     char* at = static_cast<char*>(kv->block);

@@ -752,7 +752,7 @@ static cudaError_t row_map(CUtensorMap* m, const void* base, uint64_t rows, bool
 }
 
 bool attn_tc_supported(const ace_kv* kv) {
-    return kv->desc.dtype == ACE_BF16 && kv->desc.format != ACE_KV_INT4 && (kv->desc.head_dim == 64 || kv->desc.head_dim == 128);
+    return kv->desc.dtype == ACE_BF16 && (kv->desc.head_dim == 64 || kv->desc.head_dim == 128);
 }
 
 cudaError_t attn_tc_init(ace_kv* kv) {
@@ -760,6 +760,7 @@ cudaError_t attn_tc_init(ace_kv* kv) {
     const bool fp8 = D.format == ACE_KV_FP8;
     const uint64_t rows = (uint64_t)D.layers * D.n_pages * D.n_kv_heads * D.page_size;
     const uint32_t box = D.page_size < kTcKeys ? D.page_size : kTcKeys;
+    if (D.format == ACE_KV_INT4) return attn_q4_init(kv);
     cudaError_t e = attn_few_init(kv);
     if (e != cudaSuccess) return e;
     if ((e = row_map(&kv->maps.k, kv->k_pool, rows, fp8, D.head_dim, box)) != cudaSuccess) return e;
@@ -769,6 +770,7 @@ cudaError_t attn_tc_init(ace_kv* kv) {
 }
 
 cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
+    if (kv->desc.format == ACE_KV_INT4) return launch_attn_q4(kv, a, s);
     if ((long long)a.max_nodes * a.group <= kFewRows) return launch_attn_few(kv, a, s);
     TcAttnArgs p;
     p.a = a;

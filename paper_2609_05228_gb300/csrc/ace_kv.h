@@ -131,4 +131,7 @@ cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaSt
 constexpr int kFewRows = 32;
 cudaError_t attn_few_init(const ace_kv* kv);
 cudaError_t launch_attn_few(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
+// caches in 4 bits (ace_attn_q4.cu): two CTAs an SM
+cudaError_t attn_q4_init(const ace_kv* kv);
+cudaError_t launch_attn_q4(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
 }  // namespace ace
