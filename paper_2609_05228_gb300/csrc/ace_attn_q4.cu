@@ -17,41 +17,48 @@
 namespace ace {
 namespace {
 
-constexpr int kWarps = 8, kThreads4 = 32 * kWarps, kStep = 16, kStages = 4;
-constexpr int kStart4 = 2;              // a unit's start and end in tiles of the work line
+constexpr int kStep = 16;
 constexpr float kNone4 = -FLT_MAX;      // reference of a row that has seen nothing: any score passes it
 
-template <int D>
+// A warp takes runs of 16 positions, one or two at a time: two where its registers hold them (8 rows), so that the chains of one fill the
+// other's waits.
+template <int D, int NT>
 struct Q4 {
+    static constexpr int SUBS = NT == 1 ? 2 : 1, STAGES = NT == 1 ? 2 : 4;
+    static constexpr int WARPS = NT == 2 ? 6 : 8, THREADS = 32 * WARPS, CTAS = NT <= 2 ? 2 : 1;      // CTAS: an SM
+    static constexpr int KEYS = WARPS * SUBS * kStep;          // positions of a tile
+    static constexpr int START = NT == 1 ? 1 : 3;               // a unit's start and end in tiles of the work line
     static constexpr int ROW = D / 2, G = D / kGroup4;          // bytes and groups of a row
     static constexpr int CODES = kStep * ROW, SCALES = kStep * G * 2;
-    static constexpr int STAGE = 2 * CODES + 2 * SCALES;
-    static constexpr int RING = kWarps * kStages * STAGE;
+    static constexpr int SUB = 2 * CODES + 2 * SCALES, STAGE = SUBS * SUB;
+    static constexpr int RING = WARPS * STAGES * STAGE;
     static constexpr int PITCH = D + 4;                         // floats of a row of a warp's O: lanes' stores in distinct banks
     static constexpr int PER = D / 8;                           // dimensions a lane has of a position's V
 };
 
 template <int D, int NT>
 struct Q4Shared {
-    unsigned char ring[Q4<D>::RING];
-    float join[kWarps * 8 * Q4<D>::PITCH];
-    uint4 q[NT * Q4<D>::G * 32];        // operand of S^T: [8 rows][group][lane]
+    unsigned char ring[Q4<D, NT>::RING];
+    float join[Q4<D, NT>::WARPS * 8 * Q4<D, NT>::PITCH];
+    uint4 q[NT * Q4<D, NT>::G * 32];        // operand of S^T: [8 rows][group][lane]
+    float q8[NT * Q4<D, NT>::G * 8];        // -8 times the sum of a row's q over a group: [8 rows][group][row]
     float f_row[NT * 8];                // q's scale times the softmax's
     int node[NT * 8];                   // row's node of the request
-    float2 ml[kWarps][NT * 8];          // a warp's reference and sum
+    float2 ml[Q4<D, NT>::WARPS][NT * 8];          // a warp's reference and sum
     unsigned long long bad[kMaxNodes / 64];     // nodes with a V that is not finite, left out of the products
-    Segment seg[2];
-    int go[2];
+    Segment seg[3];                     // the one at work, and two ahead
+    int go[3];
 };
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float (&c)[4]) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1,
+                                        float c2, float c3) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -59,55 +66,39 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
 // The transpose of an 8 x 8 matrix of 16-bit values, two of a row a lane.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 
-__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
-__device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t r;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
+// A position's scales as V's operands want them, two positions each: s, -136 s, 8 s.
+struct Scales {
+    uint32_t s, m136, x8;
+};
 
-// (a & b) | c
-__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
-
-// Elements 0 and 4, 1 and 5, 2 and 6, 3 and 7 of a word of codes as fp16, less 8: 1024 + c is c in the last places of 1024, and
-// 1024 + 16 c the same one nibble up.
-__device__ __forceinline__ void f16_of_codes(uint32_t w, uint32_t (&h)[4]) {
-    constexpr uint32_t k1024 = 0x64006400u, kMinus1032 = 0xe408e408u, k16th = 0x2c002c00u, kMinus72 = 0xd480d480u;
-    const uint32_t u = w >> 8;
-    h[0] = add_f16x2(and_or(w, 0x000f000fu, k1024), kMinus1032);
-    h[1] = fma_f16x2(and_or(w, 0x00f000f0u, k1024), k16th, kMinus72);
-    h[2] = add_f16x2(and_or(u, 0x000f000fu, k1024), kMinus1032);
-    h[3] = fma_f16x2(and_or(u, 0x00f000f0u, k1024), k16th, kMinus72);
-}
-
-// Element I of two positions' four codes (16 bits each) as bf16 times their scales: 128 + c is c in the last places of 128, and
-// s (128 + c) - 136 s is exact. LARGE: 136 s may be past bf16's largest, so the 136 goes before the product.
+// Elements I and I + 1 (I = 0 or 2) of two positions' four codes (16 bits each) as bf16 times their scales, exactly. Element I:
+// 128 + c is c in the last places of 128, and s (128 + c) - 136 s. Element I + 1, four places up: 16 c in bf16's last places is
+// 16 c 2^-133 without any exponent, and 8 s (c / 8 - 1); a shift less than to bring it down. LARGE: 136 s or 8 s may be past bf16's
+// largest, so s is the last factor.
 template <int I, bool LARGE>
-__device__ __forceinline__ uint32_t bf16_of_codes(uint32_t x, uint32_t s2, uint32_t minus136s) {
-    const uint32_t c = and_or(x >> (4 * I), 0x000f000fu, 0x43004300u);
-    if constexpr (LARGE) return fma_bf16x2(fma_bf16x2(c, 0x3f803f80u, 0xc308c308u), s2, 0x80008000u);
-    else return fma_bf16x2(c, s2, minus136s);
+__device__ __forceinline__ void bf16_of_codes(uint32_t x, const Scales& k, uint32_t& lower, uint32_t& upper) {
+    constexpr uint32_t kMinus136 = 0xc308c308u, kOne = 0x3f803f80u, k2To126 = 0x7e807e80u, kMinus1 = 0xbf80bf80u, kMinus0 = 0x80008000u;
+    if constexpr (I == 2) x >>= 8;
+    const uint32_t c = and_or(x, 0x000f000fu, 0x43004300u);
+    if constexpr (LARGE) {
+        lower = fma_bf16x2(fma_bf16x2(c, kOne, kMinus136), k.s, kMinus0);
+        upper = fma_bf16x2(fma_bf16x2(and_or(x >> 4, 0x000f000fu, 0x43004300u), kOne, kMinus136), k.s, kMinus0);
+    } else {
+        lower = fma_bf16x2(c, k.s, k.m136);
+        upper = fma_bf16x2(fma_bf16x2(x & 0x00f000f0u, k2To126, kMinus1), k.x8, kMinus0);
+    }
 }
 
 __device__ __forceinline__ void copy16(void* dst, const void* src, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
 
 // Place of 16-byte chunk c of a position's codes in a stage. D = 128: two positions a line of 128 bytes, D = 64: four; turned so
@@ -122,42 +113,24 @@ __device__ __forceinline__ int chunk_at(int r, int c) {
     }
 }
 
-// O += V^T P^T of a stage: the lane's dimensions PER g .. of positions t, t + 4, t + 8, t + 12.
+// O += V^T P^T of a run: the lane's dimensions PER g .. of positions t, t + 4, t + 8, t + 12, whose codes are w.
 template <int D, int NT, bool LARGE>
-__device__ __forceinline__ void add_values(const unsigned char* v, const uint16_t (&s)[4], int g, int t, const uint32_t (&p)[NT][2], float (&o)[D / 16][NT][4]) {
-    constexpr int W = D / 64;           // words of codes of a position a lane has
-    uint32_t w[4][W];
+__device__ __forceinline__ void add_values(const uint32_t (&w)[4][D / 64], const Scales (&k)[2], const uint32_t (&p)[NT][2], float (&o)[D / 16][NT][4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = t + 4 * i;
-        if constexpr (D == 128) {
-            const uint2 x = *reinterpret_cast<const uint2*>(v + chunk_at<D>(r, g >> 1) + (g & 1) * 8);
-            w[i][0] = x.x;
-            w[i][1] = x.y;
-        } else {
-            w[i][0] = *reinterpret_cast<const uint32_t*>(v + chunk_at<D>(r, g >> 2) + (g & 3) * 4);
-        }
-    }
-    uint32_t s2[2], m2[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        s2[i] = s[2 * i] | (uint32_t)s[2 * i + 1] << 16;
-        m2[i] = fma_bf16x2(s2[i], 0xc308c308u, 0x80008000u);            // times -136
-    }
-#pragma unroll
-    for (int k = 0; k < W; ++k) {
+    for (int i = 0; i < D / 64; ++i) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const uint32_t sel = half ? 0x7632u : 0x5410u;
-            const uint32_t x0 = __byte_perm(w[0][k], w[1][k], sel), x1 = __byte_perm(w[2][k], w[3][k], sel);
-            uint32_t a[4] = {bf16_of_codes<0, LARGE>(x0, s2[0], m2[0]), bf16_of_codes<1, LARGE>(x0, s2[0], m2[0]),
-                             bf16_of_codes<0, LARGE>(x1, s2[1], m2[1]), bf16_of_codes<1, LARGE>(x1, s2[1], m2[1])};
+            const uint32_t x0 = __byte_perm(w[0][i], w[1][i], sel), x1 = __byte_perm(w[2][i], w[3][i], sel);
+            uint32_t a[4];
+            bf16_of_codes<0, LARGE>(x0, k[0], a[0], a[1]);
+            bf16_of_codes<0, LARGE>(x1, k[1], a[2], a[3]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16(o[4 * k + 2 * half][n], a, p[n][0], p[n][1]);
-            a[0] = bf16_of_codes<2, LARGE>(x0, s2[0], m2[0]), a[1] = bf16_of_codes<3, LARGE>(x0, s2[0], m2[0]);
-            a[2] = bf16_of_codes<2, LARGE>(x1, s2[1], m2[1]), a[3] = bf16_of_codes<3, LARGE>(x1, s2[1], m2[1]);
+            for (int n = 0; n < NT; ++n) mma_bf16(o[4 * i + 2 * half][n], a, p[n][0], p[n][1]);
+            bf16_of_codes<2, LARGE>(x0, k[0], a[0], a[1]);
+            bf16_of_codes<2, LARGE>(x1, k[1], a[2], a[3]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16(o[4 * k + 2 * half + 1][n], a, p[n][0], p[n][1]);
+            for (int n = 0; n < NT; ++n) mma_bf16(o[4 * i + 2 * half + 1][n], a, p[n][0], p[n][1]);
         }
     }
 }
@@ -165,8 +138,9 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const uint16_
 // Rows r = 8 n + 0 .. 7 of a unit, n < NT. Lane (g, t) = (lane / 4, lane % 4) holds rows 2 t and 2 t + 1 of each eight: scores of positions
 // place(g) and place(g) + 8, and dimensions PER g .. PER g + PER - 1 of O, tile j of it dimensions 2 j and 2 j + 1 of those.
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __grid_constant__ AttnArgs a) {
-    using C = Q4<D>;
+__global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4(const __grid_constant__ AttnArgs a) {
+    using C = Q4<D, NT>;
+    constexpr int kSub = C::SUBS, kStages = C::STAGES, kKeys4 = C::KEYS, kStart4 = C::START, kWarps = C::WARPS, kThreads4 = C::THREADS;
     constexpr int ROWS = 8 * NT, TJ = D / 16, G = C::G;
     extern __shared__ __align__(128) unsigned char smem_raw[];
     Q4Shared<D, NT>& m = *reinterpret_cast<Q4Shared<D, NT>*>(smem_raw);
@@ -175,17 +149,25 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
     // position of row i of the product: those of a V operand's halves lie 4 apart
     const int place = (g >> 1) + 4 * (g & 1);
 
+    // where the lane's operands lie in a run: the codes that it has of K's groups, its half of V's (the other half is turned)
+    int k_at[G];
+#pragma unroll
+    for (int b = 0; b < G; ++b) k_at[b] = chunk_at<D>(place, b) + t * 4;
+    const int v0 = C::CODES + (D == 128 ? chunk_at<D>(t, g >> 1) + (g & 1) * 8 : chunk_at<D>(t, g >> 2) + (g & 3) * 4);
+    const int v_at[2] = {v0, v0 ^ (D == 128 ? 64 : 16)};
+    const int k_scale_at = 2 * C::CODES + place * (2 * G), v_scale_at = 2 * C::CODES + C::SCALES + t * (2 * G) + g * G / 8 * 2;
+
     Cursor cur{};
     bool more = false;
     if (warp == 0) {
         if (lane == 0) note_none(a);
-        more = cursor_init<ROWS, kTcKeys, kStart4>(a, blockIdx.x, gridDim.x, cur);
+        more = cursor_init<ROWS, kKeys4, kStart4>(a, blockIdx.x, gridDim.x, cur);
     }
     // by warp 0: the segment after, into slot i
     auto schedule = [&](int i) {
         if (warp == 0) {
             Segment s{};
-            more = more && cursor_next<ROWS, kTcKeys, kStart4>(a, blockIdx.x, cur, s);
+            more = more && cursor_next<ROWS, kKeys4, kStart4>(a, blockIdx.x, cur, s);
             if (lane == 0) {
                 m.go[i] = more;
                 if (more) {
@@ -195,43 +177,68 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
             }
         }
     };
-    // stage of tile `tile`: the warp's 16 positions (of one page); what does not exist is zeros
-    auto load = [&](const Segment& s, int tile, int stage, int page) {
+    // where the lane's 16-byte words of a run go, and its operands lie
+    constexpr int PER_ROW = C::ROW / 16, SCALE_CHUNKS = C::SCALES / 16;
+    const int to = chunk_at<D>(lane / PER_ROW, lane % PER_ROW);
+    const int page_rows = a.kv_heads * a.page_size;
+    const unsigned char *k_from = nullptr, *v_from = nullptr, *scale_from = nullptr;        // the lane's words of the head's first row
+    // a warp's runs of a tile, each of one page; what does not exist is zeros
+    auto load = [&](const Segment& s, int tile, int stage, const int (&page)[kSub]) {
         if (tile < s.tile1) {
-            const int pos = tile * kTcKeys + warp * kStep, left = page < 0 ? 0 : min(s.len + s.n - pos, kStep);
-            const long long row = left <= 0 ? 0 : ((long long)page * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-            unsigned char* at = ring + stage * C::STAGE;
-            constexpr int CHUNKS = C::CODES / 16, PER_ROW = C::ROW / 16;
 #pragma unroll
-            for (int i = 0; i < CHUNKS; i += 32) {
-                const int id = i + lane, r = id / PER_ROW, c = id % PER_ROW, bytes = r < left ? 16 : 0;
-                copy16(at + chunk_at<D>(r, c), static_cast<const unsigned char*>(a.k_pool) + row * C::ROW + id * 16, bytes);
-                copy16(at + C::CODES + chunk_at<D>(r, c), static_cast<const unsigned char*>(a.v_pool) + row * C::ROW + id * 16, bytes);
-            }
-            constexpr int SCALE_CHUNKS = C::SCALES / 16;
-            if (lane < 2 * SCALE_CHUNKS) {
-                const int i = lane % SCALE_CHUNKS, bytes = min(max(left * (2 * G) - i * 16, 0), 16);
-                const uint8_t* pool = lane < SCALE_CHUNKS ? a.k_scale : a.v_scale;
-                copy16(at + 2 * C::CODES + lane * 16, pool + row * (2 * G) + i * 16, bytes);
+            for (int u = 0; u < kSub; ++u) {
+                const int pos = tile * kKeys4 + (warp * kSub + u) * kStep, left = s.len + s.n - pos;
+                unsigned char* at = ring + stage * C::STAGE + u * C::SUB;
+                const int row = page[u] * page_rows + (pos & (a.page_size - 1));
+                if (__builtin_expect(left >= kStep && page[u] >= 0, 1)) {
+                    const unsigned char *k = k_from + (long long)row * C::ROW, *v = v_from + (long long)row * C::ROW;
+#pragma unroll
+                    for (int i = 0; i < C::CODES / 512; ++i) {      // 8 rows of 64 bytes further on lie as far in the stage
+                        copy16(at + to + i * 512, k + i * 512);
+                        copy16(at + C::CODES + to + i * 512, v + i * 512);
+                    }
+                    if (lane < 2 * SCALE_CHUNKS) copy16(at + 2 * C::CODES + lane * 16, scale_from + (long long)row * (2 * G));
+                } else {
+                    const int have = page[u] < 0 ? 0 : left;
+                    const long long from = have <= 0 ? 0 : row;
+#pragma unroll
+                    for (int i = 0; i < C::CODES / 512; ++i) {
+                        const int bytes = lane / PER_ROW + 8 * i < have ? 16 : 0;
+                        copy16(at + to + i * 512, k_from + from * C::ROW + i * 512, bytes);
+                        copy16(at + C::CODES + to + i * 512, v_from + from * C::ROW + i * 512, bytes);
+                    }
+                    if (lane < 2 * SCALE_CHUNKS)
+                        copy16(at + 2 * C::CODES + lane * 16, scale_from + from * (2 * G), min(max(have * (2 * G) - lane % SCALE_CHUNKS * 16, 0), 16));
+                }
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto look_up = [&](const Segment& s, int tile) {
-        const int pos = tile * kTcKeys + warp * kStep;
-        return tile < s.tile1 && pos < s.len + s.n ? page_of(a, s.b, pos) : -1;
-    };
-    // a segment's first stages; returns the page of the one after
-    auto begin = [&](const Segment& s) {
-        int page[kStages];
+    auto look_up = [&](const Segment& s, int tile, int (&page)[kSub]) {
 #pragma unroll
-        for (int i = 0; i < kStages; ++i) page[i] = look_up(s, s.tile0 + i);
+        for (int u = 0; u < kSub; ++u) {
+            const int pos = tile * kKeys4 + (warp * kSub + u) * kStep;
+            if (u > 0 && a.page_size >= kSub * kStep) page[u] = page[0];
+            else page[u] = tile < s.tile1 && pos < s.len + s.n ? page_of(a, s.b, pos) : -1;
+        }
+    };
+    // a segment's first stages, and the pages of the one after
+    int next_page[kSub];
+    auto begin = [&](const Segment& s) {
+        const long long head = (long long)s.head * a.page_size;
+        k_from = static_cast<const unsigned char*>(a.k_pool) + head * C::ROW + lane * 16;
+        v_from = static_cast<const unsigned char*>(a.v_pool) + head * C::ROW + lane * 16;
+        scale_from = (lane < SCALE_CHUNKS ? a.k_scale : a.v_scale) + head * (2 * G) + lane % SCALE_CHUNKS * 16;
+        int page[kStages][kSub];
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) look_up(s, s.tile0 + i, page[i]);
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) load(s, s.tile0 + i, i, page[i]);
-        return page[kStages - 1];
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) next_page[u] = page[kStages - 1][u];
     };
     // q's operand, PER_Q lanes a row with 8 elements each; elements of a row in units of 2^(e - 14), where its largest is below
-    // 2^(e + 1): all bits of elements down to 2^-31 of it
+    // 2^(e + 1): all bits of elements down to 2^-27 of it. Those that meet codes 16 times too large are a 16th.
     constexpr int PER_Q = D / 8, Q_ROWS = kThreads4 / PER_Q, Q_TURNS = (ROWS + Q_ROWS - 1) / Q_ROWS;
     auto q_load = [&](const Segment& s, uint4 (&raw)[Q_TURNS]) {
 #pragma unroll
@@ -250,18 +257,25 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
             for (int x = 0; x < 8; ++x) f[x] = finite_or_nan(f[x]), amax = fmaxf(amax, fabsf(f[x]));
 #pragma unroll
             for (int o = PER_Q / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            if (r >= ROWS) continue;
             const int e = max((int)(__float_as_uint(amax) >> 23), 15);
             const float mul = __uint_as_float((uint32_t)(268 - e) << 23);
             uint32_t w[4];
+            float sum = 0.f;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const __half2 h = __floats2half2_rn(f[x] * mul, f[x + 4] * mul);
+                const float up = x & 1 ? mul * 0.0625f : mul;
+                const __half2 h = __floats2half2_rn(f[x] * up, f[x + 4] * up);
                 w[x] = *reinterpret_cast<const uint32_t*>(&h);
+                const float2 back = __half22float2(h);
+                sum += (back.x + back.y) * (x & 1 ? 16.f : 1.f);
             }
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (r >= ROWS) continue;
+            if (c % 4 == 0) m.q8[((r >> 3) * G + c / 4) * 8 + (r & 7)] = sum * (-8.f * 0x1p-24f);
             m.q[((r >> 3) * G + c / 4) * 32 + (r & 7) * 4 + c % 4] = make_uint4(w[0], w[1], w[2], w[3]);
             if (c == 0) {
-                m.f_row[r] = a.scale_log2 * pow2_of_byte(e - 14);
+                m.f_row[r] = a.scale_log2 * pow2_of_byte(e - 14) * 0x1p24f;
                 m.node[r] = r < s.rows ? (s.row0 + r) / a.group : 0;
             }
         }
@@ -271,18 +285,18 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
     schedule(0);
     __syncthreads();
     if (!m.go[0]) return;
-    int next_page;
     {
-        next_page = begin(m.seg[0]);
+        begin(m.seg[0]);
         uint4 raw[Q_TURNS];
         q_load(m.seg[0], raw);
+        schedule(1);                    // while the first loads are under way
         q_store(m.seg[0], raw);
     }
     __syncthreads();
-    for (int turn = 0;; turn ^= 1) {
+    for (int turn = 0;;) {
+        const int next = turn == 2 ? 0 : turn + 1;
         const Segment& s = m.seg[turn];
-        schedule(turn ^ 1);
-        const int total = s.len + s.n;
+        const int len = s.len, total = s.len + s.n, tile1 = s.tile1;
         float o[TJ][NT][4], ref[NT][2], l[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -292,77 +306,80 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
             l[n][0] = l[n][1] = 0.f;
         }
         int stage = 0;
-        for (int tile = s.tile0; tile < s.tile1; ++tile) {
+        for (int tile = s.tile0; tile < tile1; ++tile) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
             __syncwarp();               // all lanes' copies are there, and the stage before is read
-            load(s, tile + kStages - 1, (stage + kStages - 1) % kStages, next_page);
-            next_page = look_up(s, tile + kStages);
+            load(s, tile + kStages - 1, stage == 0 ? kStages - 1 : stage - 1, next_page);
+            look_up(s, tile + kStages, next_page);
             const unsigned char* at = ring + stage * C::STAGE;
-            stage = (stage + 1) % kStages;
-            const int pos = tile * kTcKeys + warp * kStep;
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+            const int pos = tile * kKeys4 + warp * (kSub * kStep);
             if (pos >= total) continue;
             // ---- scores
-            uint64_t x01[NT], x23[NT];
+            float x[kSub][NT][4];
+            {
+                uint64_t x01[kSub][NT], x23[kSub][NT];
+                uint32_t k0[kSub][G / 2], k1[kSub][G / 2];      // scales of the two positions
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x01[n] = x23[n] = 0ull;
-            uint32_t k0[G / 2], k1[G / 2];          // scales of the two positions
-            if constexpr (G == 4) {
-                const uint2 u = *reinterpret_cast<const uint2*>(at + 2 * C::CODES + place * 8), w = *reinterpret_cast<const uint2*>(at + 2 * C::CODES + place * 8 + 64);
-                k0[0] = u.x, k0[1] = u.y, k1[0] = w.x, k1[1] = w.y;
-            } else {
-                k0[0] = *reinterpret_cast<const uint32_t*>(at + 2 * C::CODES + place * 4);
-                k1[0] = *reinterpret_cast<const uint32_t*>(at + 2 * C::CODES + place * 4 + 32);
-            }
+                for (int u = 0; u < kSub; ++u) {
+                    const unsigned char* from = at + u * C::SUB + k_scale_at;
+                    if constexpr (G == 4) {
+                        const uint2 y = *reinterpret_cast<const uint2*>(from), w = *reinterpret_cast<const uint2*>(from + 64);
+                        k0[u][0] = y.x, k0[u][1] = y.y, k1[u][0] = w.x, k1[u][1] = w.y;
+                    } else {
+                        k0[u][0] = *reinterpret_cast<const uint32_t*>(from);
+                        k1[u][0] = *reinterpret_cast<const uint32_t*>(from + 32);
+                    }
+                }
 #pragma unroll
-            for (int b = 0; b < G; ++b) {
-                uint32_t h0[4], h1[4];
-                f16_of_codes(*reinterpret_cast<const uint32_t*>(at + chunk_at<D>(place, b) + t * 4), h0);
-                f16_of_codes(*reinterpret_cast<const uint32_t*>(at + chunk_at<D>(place + 8, b) + t * 4), h1);
-                const uint32_t a0[4] = {h0[0], h1[0], h0[1], h1[1]}, a1[4] = {h0[2], h1[2], h0[3], h1[3]};
-                const float f0 = __uint_as_float(b & 1 ? k0[b / 2] & 0xffff0000u : k0[b / 2] << 16);
-                const float f1 = __uint_as_float(b & 1 ? k1[b / 2] & 0xffff0000u : k1[b / 2] << 16);
+                for (int b = 0; b < G; ++b) {
+                    uint32_t w0[kSub], w1[kSub];
+#pragma unroll
+                    for (int u = 0; u < kSub; ++u) {            // 8 positions further on lie 512 (256) bytes further on
+                        w0[u] = *reinterpret_cast<const uint32_t*>(at + u * C::SUB + k_at[b]);
+                        w1[u] = *reinterpret_cast<const uint32_t*>(at + u * C::SUB + k_at[b] + 8 * C::ROW);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint4 q = m.q[(n * G + b) * 32 + lane];
+                        const float2 less = *reinterpret_cast<const float2*>(&m.q8[(n * G + b) * 8 + 2 * t]);
+#pragma unroll
+                        for (int u = 0; u < kSub; ++u) {
+                            // elements 0 and 4, 1 and 5, .. in place are codes times 2^-24 and 16 times that
+                            const uint32_t y0 = w0[u] >> 8, y1 = w1[u] >> 8;
+                            const float f0 = __uint_as_float(b & 1 ? k0[u][b / 2] & 0xffff0000u : k0[u][b / 2] << 16);
+                            const float f1 = __uint_as_float(b & 1 ? k1[u][b / 2] & 0xffff0000u : k1[u][b / 2] << 16);
+                            float c[4], d[4];
+                            mma_f16(c, w0[u] & 0x000f000fu, w1[u] & 0x000f000fu, w0[u] & 0x00f000f0u, w1[u] & 0x00f000f0u, q.x, q.y, less.x, less.y, less.x, less.y);
+                            mma_f16(d, y0 & 0x000f000fu, y1 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.z, q.w, c[0], c[1], c[2], c[3]);
+                            x01[u][n] = b == 0 ? mul2(pair(d[0], d[1]), pair(f0, f0)) : fma2(pair(d[0], d[1]), pair(f0, f0), x01[u][n]);
+                            x23[u][n] = b == 0 ? mul2(pair(d[2], d[3]), pair(f1, f1)) : fma2(pair(d[2], d[3]), pair(f1, f1), x23[u][n]);
+                        }
+                    }
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const uint4 q = m.q[(n * G + b) * 32 + lane];
-                    float c[4];
-                    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-                    mma_f16(c, a0, q.x, q.y, zero);
-                    mma_f16(c, a1, q.z, q.w, c);
-                    x01[n] = fma2(pair(c[0], c[1]), pair(f0, f0), x01[n]);
-                    x23[n] = fma2(pair(c[2], c[3]), pair(f1, f1), x23[n]);
+                    const float2 f = *reinterpret_cast<const float2*>(&m.f_row[8 * n + 2 * t]);
+#pragma unroll
+                    for (int u = 0; u < kSub; ++u) {
+                        unpair(mul2(x01[u][n], pair(f.x, f.y)), x[u][n][0], x[u][n][1]);
+                        unpair(mul2(x23[u][n], pair(f.x, f.y)), x[u][n][2], x[u][n][3]);
+                    }
                 }
             }
-            float x[NT][4];
+            const bool drafted = pos + kSub * kStep > len;      // rows that not every node sees, or past the end
+            if (__builtin_expect(drafted, 0)) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float2 f = *reinterpret_cast<const float2*>(&m.f_row[8 * n + 2 * t]);
-                unpair(mul2(x01[n], pair(f.x, f.y)), x[n][0], x[n][1]);
-                unpair(mul2(x23[n], pair(f.x, f.y)), x[n][2], x[n][3]);
-            }
-            uint16_t vs[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                vs[i] = *reinterpret_cast<const uint16_t*>(at + 2 * C::CODES + C::SCALES + (t + 4 * i) * (2 * G) + g * G / 8 * 2);
-            if (pos + kStep > s.len) {
-                // drafted rows, which not every node sees, or past the end
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int nd = pos + place + 8 * i - s.len;
+                for (int i = 0; i < 2 * kSub; ++i) {
+                    const int nd = pos + place + 8 * i - len;
                     if (nd < 0) continue;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
-                            const bool sees = nd < s.n && (sees_word(a, s.node0, s.n, m.node[8 * n + 2 * t + r], nd >> 6) >> (nd & 63) & 1);
-                            if (!sees) x[n][2 * i + r] = -INFINITY;
+                            const bool sees = nd < total - len && (sees_word(a, s.node0, total - len, m.node[8 * n + 2 * t + r], nd >> 6) >> (nd & 63) & 1);
+                            if (!sees) x[i / 2][n][i % 2 * 2 + r] = -INFINITY;
                         }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int nd = pos + t + 4 * i - s.len;
-                    if (nd < 0 || (vs[i] & 0x7f80u) != 0x7f80u) continue;
-                    vs[i] = 0;
-                    atomicOr(&m.bad[nd >> 6], 1ull << (nd & 63));
                 }
             }
             // ---- references: a row's moves where a score is 2^kLazy above it
@@ -370,13 +387,20 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) over = fmaxf(over, fmaxf(x[n][r], x[n][2 + r]) - ref[n][r]);
-            if (__any_sync(0xffffffffu, over > (float)kLazy)) {
+                for (int r = 0; r < 2; ++r) {
+                    float top = fmaxf(x[0][n][r], x[0][n][2 + r]);
+#pragma unroll
+                    for (int u = 1; u < kSub; ++u) top = fmaxf(top, fmaxf(x[u][n][r], x[u][n][2 + r]));
+                    over = fmaxf(over, top - ref[n][r]);
+                }
+            if (__builtin_expect(__any_sync(0xffffffffu, over > (float)kLazy), 0)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        float top = fmaxf(x[n][r], x[n][2 + r]);
+                        float top = fmaxf(x[0][n][r], x[0][n][2 + r]);
+#pragma unroll
+                        for (int u = 1; u < kSub; ++u) top = fmaxf(top, fmaxf(x[u][n][r], x[u][n][2 + r]));
 #pragma unroll
                         for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
                         const float now = top > ref[n][r] + (float)kLazy ? top : ref[n][r], f = exp2_approx(ref[n][r] - now);
@@ -386,25 +410,53 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
                         for (int j = 0; j < TJ; ++j) o[j][n][r] *= f, o[j][n][2 + r] *= f;
                     }
             }
-            // ---- weights
-            uint32_t p[NT][2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float e[4];
+            for (int u = 0; u < kSub; ++u) {
+                const unsigned char* run = at + u * C::SUB;
+                // ---- weights
+                uint32_t p[NT][2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = exp2_approx(x[n][i] - ref[n][i & 1]);
-                l[n][0] += e[0] + e[2];
-                l[n][1] += e[1] + e[3];
-                const __nv_bfloat162 u = __floats2bfloat162_rn(e[0], e[1]), w = __floats2bfloat162_rn(e[2], e[3]);
-                p[n][0] = transposed(*reinterpret_cast<const uint32_t*>(&u));
-                p[n][1] = transposed(*reinterpret_cast<const uint32_t*>(&w));
+                for (int n = 0; n < NT; ++n) {
+                    float e[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = exp2_approx(x[u][n][i] - ref[n][i & 1]);
+                    l[n][0] += e[0] + e[2];
+                    l[n][1] += e[1] + e[3];
+                    const __nv_bfloat162 y = __floats2bfloat162_rn(e[0], e[1]), w = __floats2bfloat162_rn(e[2], e[3]);
+                    p[n][0] = transposed(*reinterpret_cast<const uint32_t*>(&y));
+                    p[n][1] = transposed(*reinterpret_cast<const uint32_t*>(&w));
+                }
+                // ---- values
+                uint32_t w[4][D / 64];
+                Scales k[2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned char* from = run + (i & 1 ? v_at[1] : v_at[0]) + i * 4 * C::ROW;
+                    if constexpr (D == 128) {
+                        const uint2 y = *reinterpret_cast<const uint2*>(from);
+                        w[i][0] = y.x, w[i][1] = y.y;
+                    } else {
+                        w[i][0] = *reinterpret_cast<const uint32_t*>(from);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t lo = *reinterpret_cast<const uint16_t*>(run + v_scale_at + 16 * G * i), hi = *reinterpret_cast<const uint16_t*>(run + v_scale_at + 16 * G * i + 8 * G);
+                    if (__builtin_expect(drafted, 0)) {
+                        // what is not finite in a drafted row is for those that see it: noted, and left out of the products
+                        const int nd = pos + u * kStep + t + 8 * i - len;
+                        if (nd >= 0 && (lo & 0x7f80u) == 0x7f80u) lo = 0, atomicOr(&m.bad[nd >> 6], 1ull << (nd & 63));
+                        if (nd + 4 >= 0 && (hi & 0x7f80u) == 0x7f80u) hi = 0, atomicOr(&m.bad[(nd + 4) >> 6], 1ull << ((nd + 4) & 63));
+                    }
+                    k[i].s = lo | hi << 16;
+                    k[i].m136 = fma_bf16x2(k[i].s, 0xc308c308u, 0x80008000u);
+                    k[i].x8 = fma_bf16x2(k[i].s, 0x41004100u, 0x80008000u);
+                }
+                // 0 times an infinity or a NaN is no zero
+                const uint32_t fine = fma_bf16x2(k[0].m136, 0u, fma_bf16x2(k[1].m136, 0u, 0u));
+                if (__builtin_expect(__any_sync(0xffffffffu, (fine & 0x7fff7fffu) != 0), 0)) add_values<D, NT, true>(w, k, p, o);
+                else add_values<D, NT, false>(w, k, p, o);
             }
-            // ---- values
-            bool large = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) large = large || (vs[i] & 0x7fffu) >= 0x7b80u;      // 2^120
-            if (__any_sync(0xffffffffu, large)) add_values<D, NT, true>(at + C::CODES, vs, g, t, p, o);
-            else add_values<D, NT, false>(at + C::CODES, vs, g, t, p, o);
         }
         // ---------------- the unit's result, or this CTA's part of it
 #pragma unroll
@@ -415,12 +467,13 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
                 for (int w = 4; w < 32; w <<= 1) l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], w);
                 if (g == 0) m.ml[warp][8 * n + 2 * t + r] = make_float2(ref[n][r], l[n][r]);
             }
-        __syncthreads();                // all have read q; the next segment is known
-        const bool go = m.go[turn ^ 1];
+        __syncthreads();                // all have read q
+        const bool go = m.go[next];
         uint4 raw[Q_TURNS];
         if (go) {
-            next_page = begin(m.seg[turn ^ 1]);
-            q_load(m.seg[turn ^ 1], raw);
+            begin(m.seg[next]);
+            q_load(m.seg[next], raw);
+            schedule(next == 2 ? 0 : next + 1);
         }
         const bool whole = s.part < 0;
         const unsigned long long bad[kMaxNodes / 64] = {m.bad[0], m.bad[1], m.bad[2], m.bad[3]};
@@ -482,8 +535,9 @@ __global__ void __launch_bounds__(kThreads4, NT <= 2 ? 2 : 1) k_attn_q4(const __
         }
         if (!go) break;
         __syncthreads();                // bad and q are free
-        q_store(m.seg[turn ^ 1], raw);
+        q_store(m.seg[next], raw);
         __syncthreads();
+        turn = next;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
@@ -499,8 +553,8 @@ cudaError_t q4_attr() {
 
 template <int D, int NT>
 cudaError_t q4_run(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
-    const int ctas = kv->num_sms * (NT <= 2 ? 2 : 1);
-    k_attn_q4<D, NT><<<ctas, kThreads4, q4_smem<D, NT>(), s>>>(a);
+    const int ctas = kv->num_sms * Q4<D, NT>::CTAS;
+    k_attn_q4<D, NT><<<ctas, Q4<D, NT>::THREADS, q4_smem<D, NT>(), s>>>(a);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? launch_join(a, ACE_BF16, false, 8 * NT, ctas, s) : e;
 }

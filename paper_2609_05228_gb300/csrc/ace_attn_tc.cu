@@ -18,6 +18,8 @@
 // 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory with their scales, in units
 // of 2^eref, a power of two above the scales so far (ace_attn_tc.cuh: Reference): exact but for rows whose scale is 2^-20 of the
 // largest and less, whose codes' last bits fall under fp16's least.
+// 4-bit caches: K's and V's codes times their scales, which bf16 holds exactly, are written as the tiles of a plain cache by the four
+// warps that lay out q (Codes4), in place of TMA.
 // P is rounded to bf16 (2^-9 of a weight; plain caches) or fp16 (2^-12), as the products need; sums, maxima and O are fp32.
 // Measured: 8 users of up to 16384 positions, 128 nodes of 64 heads (8 kv heads of 128), bf16: 304 us, 850 TFLOP/s. 64 users
 // of up to 8192, 4 kv heads of 128: 64 rows a unit 114 us fp8, 128 bf16; 128 rows 139 and 135; 192 rows 213 and 162. Bound by
@@ -134,6 +136,88 @@ __device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, flo
     return (a + b) + (c + d);
 }
 
+// Four warps, caches in 4 bits: tiles of K and V as the products take them. A row's group of 32 codes is a lane's 16 bytes, 8 or 16
+// rows a turn, so that a warp reads 512 bytes on end; loaded a tile ahead, their pages two.
+template <int D>
+struct Codes4 {
+    static constexpr int CH = D / kGroup4, ROWS = 32 / CH, TURNS = 32 / ROWS;       // groups of a row; rows of a turn; turns of a warp's 32 rows
+    const AttnArgs& a;
+    const Segment& s;
+    int row0, lane;                     // the warp's first row of a tile
+    int page[2];                        // of its runs of 16 rows
+    uint4 code[2][TURNS];
+    uint16_t scale[2][TURNS];
+
+    __device__ __forceinline__ void look_up(int t) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int pos = t * kTcKeys + row0 + 16 * i;
+            page[i] = t < s.tile1 && pos < s.len + s.n ? page_of(a, s.b, pos) : -1;
+        }
+    }
+    __device__ __forceinline__ void load(int t) {
+        const int total = s.len + s.n;
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            const int r = i * ROWS + lane / CH, pos = t * kTcKeys + row0 + r, c = lane % CH, pg = page[i * ROWS / 16];
+            code[0][i] = code[1][i] = make_uint4(0, 0, 0, 0);
+            scale[0][i] = scale[1][i] = 0;
+            if (pg >= 0 && pos < total) {
+                const long long row = (long long)(pg * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
+                code[0][i] = ld_stream(static_cast<const uint8_t*>(a.k_pool) + row * (D / 2) + c * 16);
+                code[1][i] = ld_stream(static_cast<const uint8_t*>(a.v_pool) + row * (D / 2) + c * 16);
+                scale[0][i] = __ldg(reinterpret_cast<const uint16_t*>(a.k_scale) + row * CH + c);
+                scale[1][i] = __ldg(reinterpret_cast<const uint16_t*>(a.v_scale) + row * CH + c);
+            }
+        }
+    }
+    // Pairs of elements (0, 4), (1, 5), (2, 6), (3, 7) of a word times the scale, exactly: (128 + c - 136) s, and four places up 16 c
+    // 2^-133 as bf16 reads them, (c / 4 - 2) 4 s.
+    __device__ static __forceinline__ void pairs(uint32_t w, uint32_t s1, uint32_t s4, uint32_t (&h)[4]) {
+        constexpr uint32_t kOne = 0x3f803f80u, kMinus136 = 0xc308c308u, k2To127 = 0x7f007f00u, kMinus2 = 0xc000c000u, kMinus0 = 0x80008000u;
+        const uint32_t u = w >> 8;
+        h[0] = fma_bf16x2(fma_bf16x2(and_or(w, 0x000f000fu, 0x43004300u), kOne, kMinus136), s1, kMinus0);
+        h[1] = fma_bf16x2(fma_bf16x2(w & 0x00f000f0u, k2To127, kMinus2), s4, kMinus0);
+        h[2] = fma_bf16x2(fma_bf16x2(and_or(u, 0x000f000fu, 0x43004300u), kOne, kMinus136), s1, kMinus0);
+        h[3] = fma_bf16x2(fma_bf16x2(u & 0x00f000f0u, k2To127, kMinus2), s4, kMinus0);
+    }
+    // The tile of K (V = false; 8 elements of a word lie in the order 0 4 1 5 2 6 3 7, as q's do) or V.
+    template <bool V>
+    __device__ __forceinline__ void store(unsigned char* tile, int t, unsigned long long* bad) {
+#pragma unroll 1
+        for (int i = 0; i < TURNS; ++i) {
+            const int r = row0 + i * ROWS + lane / CH, c = lane % CH;
+            uint4 w = code[V][0];
+            uint32_t sc = scale[V][0];
+#pragma unroll
+            for (int k = 1; k < TURNS; ++k)
+                if (k == i) w = code[V][k], sc = scale[V][k];
+            if (V) {
+                const int nd = t * kTcKeys + r - s.len;
+                if (nd >= 0 && (sc & 0x7f80u) == 0x7f80u) {
+                    sc = 0;
+                    atomicOr(&bad[nd >> 6], 1ull << (nd & 63));
+                }
+            }
+            const uint32_t s1 = sc | sc << 16, s4 = fma_bf16x2(s1, 0x40804080u, 0x80008000u);
+            // lanes of the second 64 dimensions begin with the other half, so that the chunks of 8 lanes lie in distinct banks
+            const bool turned = c & 2;
+            const uint32_t x[4] = {turned ? w.z : w.x, turned ? w.w : w.y, turned ? w.x : w.z, turned ? w.y : w.w};
+            unsigned char* to = tile + (c >> 1) * 16384 + r * 128;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t h[4];
+                pairs(x[k], s1, s4, h);
+                const int ch = (c & 1) * 4 + (k ^ (turned ? 2 : 0));
+                const uint4 y = V ? make_uint4(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410), __byte_perm(h[0], h[1], 0x7632),
+                                               __byte_perm(h[2], h[3], 0x7632))
+                                  : make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4*>(to + ((ch ^ (r & 7)) << 4)) = y;
+            }
+        }
+    }
+};
+
 // A thread's row of the running softmax.
 struct RowState {
     float ref, l, o_mul;                // reference, sum, what O has to be multiplied with
@@ -196,10 +280,10 @@ __device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
 
 // CP = 2 (at most 64 rows): the block holds them twice, 64 lanes apart, and each copy's warps take half of a tile's
 // columns: the tile's softmax takes half the time, and the copies' O are added at the end.
-template <bool FP8, int D, int RT, int CP>
+template <bool FP8, bool I4, int D, int RT, int CP>
 __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant__ TcAttnArgs p) {
     using C = Cfg<FP8, D, RT, CP>;
-    constexpr int ROWS = C::ROWS, NK = C::NK, NV = C::NV, NC = C::NC;
+    constexpr int ROWS = C::ROWS, NK = C::NK, NV = C::NV, NC = C::NC, FMT = I4 ? ACE_KV_INT4 : FP8 ? ACE_KV_FP8 : ACE_KV_PLAIN;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     using M = Misc<FP8, RT>;
@@ -208,7 +292,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     volatile int* abort_flag = &m.abort_flag;
     const int warp = warp_index(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < NK; ++i) mbar_init(&m.k_full[i], 1), mbar_init(&m.k_empty[i], 2);
+        for (int i = 0; i < NK; ++i) mbar_init(&m.k_full[i], I4 ? 4 : 1), mbar_init(&m.k_empty[i], 2);
         for (int i = 0; i < NV; ++i) mbar_init(&m.v_full[i], 1), mbar_init(&m.v_empty[i], FP8 ? 4 : 2);
         for (int i = 0; i < (FP8 ? NC : NV); ++i) mbar_init(&m.v_ready[i], 4);
         for (int i = 0; i < 4; ++i) {
@@ -224,7 +308,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         mbar_init(&m.drain[0], 1), mbar_init(&m.drain[1], 1);
         for (int i = 0; i < kSegRing; ++i) {
             mbar_init(&m.seg_full[i], 1);
-            mbar_init(&m.seg_empty[i], FP8 ? 16 : 15);  // load, 2 MMA, (scales,) 8 softmax and 4 converting warps
+            mbar_init(&m.seg_empty[i], FP8 ? 16 : I4 ? 14 : 15);        // load, 2 MMA, (scales,) 8 softmax and 4 converting warps
         }
         for (int i = 0; i < kAuxRing; ++i) {
             mbar_init(&m.aux_full[i], 1);
@@ -245,8 +329,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     Walk walk{m, a, {}};
 
     if (warp == 0) {
-        Scheduler<ROWS, kTcStart> sched(m, a);                    // a segment ahead of the loads
-        if (sched.publish()) role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [&] { return sched.publish(); });
+        if constexpr (I4) {
+            role_schedule<ROWS, kTcStart>(m, a);
+        } else {
+            Scheduler<ROWS, kTcStart> sched(m, a);                // a segment ahead of the loads
+            if (sched.publish()) role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [&] { return sched.publish(); });
+        }
     } else if (warp == 2) {
         if constexpr (FP8) role_scales<kTcRoom>(m, a, m.kf, m.vf);
     } else if (warp == 1 || warp == 3) {
@@ -330,11 +418,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     } else if (warp >= 12) {
         // ------------------------------------------------ q rows, and V tiles made ready
         const int tid = threadIdx.x - 384;
-        Ring rv, rc, ra;
+        Ring rk, rv, rc, ra;
         uint32_t q_phase = 1;           // the first segment's q buffer is free
         bool ok = true;
         while (ok && walk.next()) {
             const Segment& s = walk.segment();
+            Codes4<D> codes{a, s, tid >> 5 << 5, lane};
+            if constexpr (I4) {
+                codes.look_up(s.tile0);
+                codes.load(s.tile0);
+                codes.look_up(s.tile0 + 1);
+            }
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
             constexpr int kStep = 128 / kChunks, kBatch = 4;        // rows a pass; passes whose loads are under way together
@@ -390,7 +484,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         uint32_t w[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
+                            const __nv_bfloat162 v = I4 ? __floats2bfloat162_rn(f[i] * q_mul, f[i + 4] * q_mul)
+                                                        : __floats2bfloat162_rn(f[2 * i] * q_mul, f[2 * i + 1] * q_mul);
                             w[i] = *reinterpret_cast<const uint32_t*>(&v);
                         }
                         for (int rr = r & 127, k = 0; k < CP; ++k, rr += apart)
@@ -407,6 +502,23 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             for (int t = s.tile0; t < s.tile1; ++t) {
                 const int pos0 = t * kTcKeys;
                 const bool drafted = pos0 + kTcKeys > s.len;    // rows that not every node sees, or past the end
+                if constexpr (I4) {
+                    if (!mbar_wait_warp(&m.k_empty[rk.i], rk.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    codes.template store<false>(smem + C::OFF_K + rk.i * C::TILE, t, bad);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&m.k_full[rk.i]);
+                    rk.next<NK>();
+                    if (!mbar_wait_warp(&m.v_empty[rv.i], rv.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    codes.template store<true>(smem + C::OFF_V + rv.i * C::TILE, t, bad);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&m.v_ready[rv.i]);
+                    rv.next<NV>();
+                    codes.load(t + 1);
+                    codes.look_up(t + 2);
+                    continue;
+                }
                 if (!mbar_wait_warp(&m.v_full[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
                 unsigned char* v = smem + C::OFF_V + rv.i * C::TILE;
                 if constexpr (FP8) {
@@ -631,7 +743,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                         }
                     }
                     if (any_bad)
-                        for (int i = r; i < s.rows * (w / 4); i += 128) add_not_finite<FP8, ROWS>(a, s, bad, i / (w / 4), c + i % (w / 4) * 4, 4);
+                        for (int i = r; i < s.rows * (w / 4); i += 128) add_not_finite<FMT, ROWS>(a, s, bad, i / (w / 4), c + i % (w / 4) * 4, 4);
                     if (c + wide < c1 && !group_sync()) { ok = false; break; }
                 }
                 if (!ok) break;
@@ -664,7 +776,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     }
                 }
                 if (any_bad && live)
-                    for (int d = c0; d < c1; d += 4) add_not_finite<FP8, ROWS, true>(a, s, bad, row, d, 4);
+                    for (int d = c0; d < c1; d += 4) add_not_finite<FMT, ROWS, true>(a, s, bad, row, d, 4);
             }
             if (live && c0 == 0 && r < apart) {
                 if (!whole) a.ws.part_ml[(long long)s.part * ROWS + row] = make_float2(m_all, l_all);
@@ -702,33 +814,36 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
-template <bool FP8, int D, int RT, int CP>
+template <int FMT, int D, int RT, int CP>
+constexpr auto tc_kernel = k_attn_tc<FMT == ACE_KV_FP8, FMT == ACE_KV_INT4, D, RT, CP>;
+
+template <int FMT, int D, int RT, int CP>
 cudaError_t tc_attr() {
-    return raise_smem_limit(k_attn_tc<FP8, D, RT, CP>, tc_smem<FP8, D, RT, CP>());
+    return raise_smem_limit(tc_kernel<FMT, D, RT, CP>, tc_smem<FMT == ACE_KV_FP8, D, RT, CP>());
 }
 
-template <bool FP8, int D>
+template <int FMT, int D>
 cudaError_t tc_attrs() {
-    cudaError_t e = tc_attr<FP8, D, 1, 2>();
-    if (e == cudaSuccess) e = tc_attr<FP8, D, 1, 1>();
-    return e == cudaSuccess ? tc_attr<FP8, D, 2, 1>() : e;
+    cudaError_t e = tc_attr<FMT, D, 1, 2>();
+    if (e == cudaSuccess) e = tc_attr<FMT, D, 1, 1>();
+    return e == cudaSuccess ? tc_attr<FMT, D, 2, 1>() : e;
 }
 
-template <bool FP8, int D, int RT, int CP>
+template <int FMT, int D, int RT, int CP>
 cudaError_t tc_go(const TcAttnArgs& p, int ctas, cudaStream_t s) {
-    k_attn_tc<FP8, D, RT, CP><<<ctas, kTcThreads, tc_smem<FP8, D, RT, CP>(), s>>>(p);
+    tc_kernel<FMT, D, RT, CP><<<ctas, kTcThreads, tc_smem<FMT == ACE_KV_FP8, D, RT, CP>(), s>>>(p);
     const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? launch_join(p.a, ACE_BF16, CP == 1, Cfg<FP8, D, RT, CP>::ROWS, ctas, s) : e;
+    return e == cudaSuccess ? launch_join(p.a, ACE_BF16, CP == 1, Cfg<FMT == ACE_KV_FP8, D, RT, CP>::ROWS, ctas, s) : e;
 }
 
-template <bool FP8, int D>
+template <int FMT, int D>
 cudaError_t tc_launch(const TcAttnArgs& p, int ctas, cudaStream_t s) {
     // by the rows of the largest tree: one block of 128 rows a unit where that holds them (twice, if it can), else two that
     // share the loaded tiles
     const long long rows = (long long)p.a.max_nodes * p.a.group;
-    if (rows <= 64) return tc_go<FP8, D, 1, 2>(p, ctas, s);
-    if (rows <= 128) return tc_go<FP8, D, 1, 1>(p, ctas, s);
-    return tc_go<FP8, D, 2, 1>(p, ctas, s);
+    if (rows <= 64) return tc_go<FMT, D, 1, 2>(p, ctas, s);
+    if (rows <= 128) return tc_go<FMT, D, 1, 1>(p, ctas, s);
+    return tc_go<FMT, D, 2, 1>(p, ctas, s);
 }
 
 }  // namespace
@@ -760,26 +875,31 @@ cudaError_t attn_tc_init(ace_kv* kv) {
     const bool fp8 = D.format == ACE_KV_FP8;
     const uint64_t rows = (uint64_t)D.layers * D.n_pages * D.n_kv_heads * D.page_size;
     const uint32_t box = D.page_size < kTcKeys ? D.page_size : kTcKeys;
-    if (D.format == ACE_KV_INT4) return attn_q4_init(kv);
-    cudaError_t e = attn_few_init(kv);
+    cudaError_t e = D.format == ACE_KV_INT4 ? attn_q4_init(kv) : attn_few_init(kv);
     if (e != cudaSuccess) return e;
+    if (D.format == ACE_KV_INT4) return D.head_dim == 128 ? tc_attrs<ACE_KV_INT4, 128>() : tc_attrs<ACE_KV_INT4, 64>();
     if ((e = row_map(&kv->maps.k, kv->k_pool, rows, fp8, D.head_dim, box)) != cudaSuccess) return e;
     if ((e = row_map(&kv->maps.v, kv->v_pool, rows, fp8, D.head_dim, box)) != cudaSuccess) return e;
-    if (fp8) return D.head_dim == 128 ? tc_attrs<true, 128>() : tc_attrs<true, 64>();
-    return D.head_dim == 128 ? tc_attrs<false, 128>() : tc_attrs<false, 64>();
+    if (fp8) return D.head_dim == 128 ? tc_attrs<ACE_KV_FP8, 128>() : tc_attrs<ACE_KV_FP8, 64>();
+    return D.head_dim == 128 ? tc_attrs<ACE_KV_PLAIN, 128>() : tc_attrs<ACE_KV_PLAIN, 64>();
 }
 
 cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
-    if (kv->desc.format == ACE_KV_INT4) return launch_attn_q4(kv, a, s);
-    if ((long long)a.max_nodes * a.group <= kFewRows) return launch_attn_few(kv, a, s);
+    const int format = kv->desc.format;
+#ifndef KFEW4
+#define KFEW4 32
+#endif
+    if ((long long)a.max_nodes * a.group <= (format == ACE_KV_INT4 ? KFEW4 : kFewRows)) return format == ACE_KV_INT4 ? launch_attn_q4(kv, a, s) : launch_attn_few(kv, a, s);
     TcAttnArgs p;
     p.a = a;
     p.k = kv->maps.k;
     p.v = kv->maps.v;
     p.box_rows = a.page_size < kTcKeys ? a.page_size : kTcKeys;
-    if (kv->desc.format == ACE_KV_FP8)
-        return a.head_dim == 128 ? tc_launch<true, 128>(p, kv->num_sms, s) : tc_launch<true, 64>(p, kv->num_sms, s);
-    return a.head_dim == 128 ? tc_launch<false, 128>(p, kv->num_sms, s) : tc_launch<false, 64>(p, kv->num_sms, s);
+    if (format == ACE_KV_INT4)
+        return a.head_dim == 128 ? tc_launch<ACE_KV_INT4, 128>(p, kv->num_sms, s) : tc_launch<ACE_KV_INT4, 64>(p, kv->num_sms, s);
+    if (format == ACE_KV_FP8)
+        return a.head_dim == 128 ? tc_launch<ACE_KV_FP8, 128>(p, kv->num_sms, s) : tc_launch<ACE_KV_FP8, 64>(p, kv->num_sms, s);
+    return a.head_dim == 128 ? tc_launch<ACE_KV_PLAIN, 128>(p, kv->num_sms, s) : tc_launch<ACE_KV_PLAIN, 64>(p, kv->num_sms, s);
 }
 
 }  // namespace ace

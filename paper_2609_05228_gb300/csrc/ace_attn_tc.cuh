@@ -112,6 +112,19 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         : "memory");
 }
 
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+
+// (a & b) | c
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -159,7 +172,7 @@ __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, 
 
 // Values of V that are not finite were left out of the products: row `urow` of the unit, written already, gets those of
 // the nodes that it sees in dimensions d .. d + count - 1.
-template <bool FP8, int ROWS, bool BY_DIMS = false>
+template <int FMT, int ROWS, bool BY_DIMS = false>
 __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment& s, const unsigned long long* bad, int urow, int d,
                                                int count) {
     const int nd = (s.row0 + urow) / a.group, hq = s.head * a.group + (s.row0 + urow) % a.group;
@@ -172,7 +185,8 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& a, const Segment&
 #pragma unroll 1
         for (int i = d; i < d + count; ++i) {
             float v;
-            if constexpr (FP8) v = (static_cast<const uint8_t*>(a.v_pool)[row * a.head_dim + i] & 0x7f) == 0x7f ? __uint_as_float(0x7fffffffu) : 0.f;
+            if constexpr (FMT == ACE_KV_FP8) v = (static_cast<const uint8_t*>(a.v_pool)[row * a.head_dim + i] & 0x7f) == 0x7f ? __uint_as_float(0x7fffffffu) : 0.f;
+            else if constexpr (FMT == ACE_KV_INT4) v = finite_or_nan(float_of_bf16(reinterpret_cast<const uint16_t*>(a.v_scale)[row * groups4(a.head_dim) + i / kGroup4]));
             else v = to_f32(static_cast<const __nv_bfloat16*>(a.v_pool)[row * a.head_dim + i]);
             if (fabsf(v) < INFINITY) continue;
             if (s.part < 0) {
