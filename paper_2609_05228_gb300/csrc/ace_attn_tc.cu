@@ -137,7 +137,7 @@ __device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, flo
 }
 
 // Four warps, caches in 4 bits: tiles of K and V as the products take them. A row's group of 32 codes is a lane's 16 bytes, 8 or 16
-// rows a turn, so that a warp reads 512 bytes on end; loaded a tile ahead, their pages two.
+// rows a turn, so that a warp reads 512 bytes on end; loaded a tile ahead, their pages two. (s: the tile's segment.)
 template <int D>
 struct Codes4 {
     static constexpr int CH = D / kGroup4, ROWS = 32 / CH, TURNS = 32 / ROWS;       // groups of a row; rows of a turn; turns of a warp's 32 rows
@@ -155,68 +155,86 @@ struct Codes4 {
             page[i] = t < s.tile1 && pos < s.len + s.n ? page_of(a, s.b, pos) : -1;
         }
     }
+    // The lines of tile t, whose pages have been looked up, on their way to L2: 128 bytes of K's or V's codes a lane, and some lanes'
+    // scales.
+    __device__ __forceinline__ void ask(int t) {
+        constexpr int LINE = 256 / D;   // rows of a line
+        const int r = (lane & 15) * LINE, pg = r < 16 ? page[0] : page[1];
+        if (r < 32 && pg >= 0) {
+            const long long row = (long long)(pg * a.kv_heads + s.head) * a.page_size + ((t * kTcKeys + row0 + r) & (a.page_size - 1));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t*>(lane < 16 ? a.k_pool : a.v_pool) + row * (D / 2)));
+            if (r % 16 == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"((lane < 16 ? a.k_scale : a.v_scale) + row * (2 * CH)));
+        }
+    }
+    // K's (V = false) or V's codes of tile t, whose pages have been looked up.
+    template <bool V>
     __device__ __forceinline__ void load(int t) {
         const int total = s.len + s.n;
+        const uint8_t* pool = static_cast<const uint8_t*>(V ? a.v_pool : a.k_pool);
+        const uint16_t* scales = reinterpret_cast<const uint16_t*>(V ? a.v_scale : a.k_scale);
 #pragma unroll
         for (int i = 0; i < TURNS; ++i) {
-            const int r = i * ROWS + lane / CH, pos = t * kTcKeys + row0 + r, c = lane % CH, pg = page[i * ROWS / 16];
-            code[0][i] = code[1][i] = make_uint4(0, 0, 0, 0);
-            scale[0][i] = scale[1][i] = 0;
+            const int pos = t * kTcKeys + row0 + i * ROWS + lane % ROWS, c = lane / ROWS, pg = page[i * ROWS / 16];
+            code[V][i] = make_uint4(0, 0, 0, 0);
+            scale[V][i] = 0;
             if (pg >= 0 && pos < total) {
                 const long long row = (long long)(pg * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-                code[0][i] = ld_stream(static_cast<const uint8_t*>(a.k_pool) + row * (D / 2) + c * 16);
-                code[1][i] = ld_stream(static_cast<const uint8_t*>(a.v_pool) + row * (D / 2) + c * 16);
-                scale[0][i] = __ldg(reinterpret_cast<const uint16_t*>(a.k_scale) + row * CH + c);
-                scale[1][i] = __ldg(reinterpret_cast<const uint16_t*>(a.v_scale) + row * CH + c);
+                code[V][i] = ld_stream(pool + row * (D / 2) + c * 16);
+                scale[V][i] = __ldg(scales + row * CH + c);
             }
         }
     }
-    // Pairs of elements (0, 4), (1, 5), (2, 6), (3, 7) of a word times the scale, exactly: (128 + c - 136) s, and four places up 16 c
-    // 2^-133 as bf16 reads them, (c / 4 - 2) 4 s.
-    __device__ static __forceinline__ void pairs(uint32_t w, uint32_t s1, uint32_t s4, uint32_t (&h)[4]) {
+    // Pairs of elements (0, 4), (1, 5), (2, 6), (3, 7) of a word times the scale s, exactly: 128 + c is c in the last places of 128, and
+    // s (128 + c) - 136 s; four places up, bf16 reads 16 c 2^-133, and 4 s (c / 4 - 2). LARGE: 136 s may be past bf16's largest.
+    template <bool LARGE>
+    __device__ static __forceinline__ uint4 pairs(uint32_t w, uint32_t s1, uint32_t m136, uint32_t s4) {
         constexpr uint32_t kOne = 0x3f803f80u, kMinus136 = 0xc308c308u, k2To127 = 0x7f007f00u, kMinus2 = 0xc000c000u, kMinus0 = 0x80008000u;
-        const uint32_t u = w >> 8;
-        h[0] = fma_bf16x2(fma_bf16x2(and_or(w, 0x000f000fu, 0x43004300u), kOne, kMinus136), s1, kMinus0);
-        h[1] = fma_bf16x2(fma_bf16x2(w & 0x00f000f0u, k2To127, kMinus2), s4, kMinus0);
-        h[2] = fma_bf16x2(fma_bf16x2(and_or(u, 0x000f000fu, 0x43004300u), kOne, kMinus136), s1, kMinus0);
-        h[3] = fma_bf16x2(fma_bf16x2(u & 0x00f000f0u, k2To127, kMinus2), s4, kMinus0);
+        const uint32_t u = w >> 8, c0 = and_or(w, 0x000f000fu, 0x43004300u), c2 = and_or(u, 0x000f000fu, 0x43004300u);
+        return make_uint4(LARGE ? fma_bf16x2(fma_bf16x2(c0, kOne, kMinus136), s1, kMinus0) : fma_bf16x2(c0, s1, m136),
+                          fma_bf16x2(fma_bf16x2(w & 0x00f000f0u, k2To127, kMinus2), s4, kMinus0),
+                          LARGE ? fma_bf16x2(fma_bf16x2(c2, kOne, kMinus136), s1, kMinus0) : fma_bf16x2(c2, s1, m136),
+                          fma_bf16x2(fma_bf16x2(u & 0x00f000f0u, k2To127, kMinus2), s4, kMinus0));
     }
-    // The tile of K (V = false; 8 elements of a word lie in the order 0 4 1 5 2 6 3 7, as q's do) or V.
+    // The tile of K (V = false) or V. 8 elements lie in the order 0 4 1 5 2 6 3 7, as q's do, and O's columns after V. 8 lanes store rows
+    // on end, whose chunks lie in distinct banks.
     template <bool V>
     __device__ __forceinline__ void store(unsigned char* tile, int t, unsigned long long* bad) {
-#pragma unroll 1
-        for (int i = 0; i < TURNS; ++i) {
-            const int r = row0 + i * ROWS + lane / CH, c = lane % CH;
-            uint4 w = code[V][0];
-            uint32_t sc = scale[V][0];
+        bool large = false;
 #pragma unroll
-            for (int k = 1; k < TURNS; ++k)
-                if (k == i) w = code[V][k], sc = scale[V][k];
-            if (V) {
-                const int nd = t * kTcKeys + r - s.len;
-                if (nd >= 0 && (sc & 0x7f80u) == 0x7f80u) {
-                    sc = 0;
+        for (int i = 0; i < TURNS; ++i) {
+            if (V && t * kTcKeys + kTcKeys > s.len) {
+                const int nd = t * kTcKeys + row0 + lane % ROWS + i * ROWS - s.len;
+                if (nd >= 0 && (scale[V][i] & 0x7f80u) == 0x7f80u) {
+                    scale[V][i] = 0;
                     atomicOr(&bad[nd >> 6], 1ull << (nd & 63));
                 }
             }
-            const uint32_t s1 = sc | sc << 16, s4 = fma_bf16x2(s1, 0x40804080u, 0x80008000u);
-            // lanes of the second 64 dimensions begin with the other half, so that the chunks of 8 lanes lie in distinct banks
-            const bool turned = c & 2;
-            const uint32_t x[4] = {turned ? w.z : w.x, turned ? w.w : w.y, turned ? w.x : w.z, turned ? w.y : w.w};
-            unsigned char* to = tile + (c >> 1) * 16384 + r * 128;
+            large = large || (scale[V][i] & 0x7fffu) >= 0x7b80u;        // 2^120
+        }
+        if (__builtin_expect(__any_sync(0xffffffffu, large), 0)) store_rows<V, true>(tile);
+        else store_rows<V, false>(tile);
+    }
+    template <bool V, bool LARGE>
+    __device__ __forceinline__ void store_rows(unsigned char* tile) {
+        const int c = lane / ROWS, r = row0 + lane % ROWS;
+        unsigned char* to = tile + (c >> 1) * 16384 + r * 128;
+        int off[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t h[4];
-                pairs(x[k], s1, s4, h);
-                const int ch = (c & 1) * 4 + (k ^ (turned ? 2 : 0));
-                const uint4 y = V ? make_uint4(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410), __byte_perm(h[0], h[1], 0x7632),
-                                               __byte_perm(h[2], h[3], 0x7632))
-                                  : make_uint4(h[0], h[1], h[2], h[3]);
-                *reinterpret_cast<uint4*>(to + ((ch ^ (r & 7)) << 4)) = y;
-            }
+        for (int k = 0; k < 4; ++k) off[k] = (((c & 1) * 4 + k) ^ (r & 7)) << 4;
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            const uint32_t sc = scale[V][i], s1 = sc | sc << 16, s4 = fma_bf16x2(s1, 0x40804080u, 0x80008000u);
+            const uint32_t m136 = fma_bf16x2(s1, 0xc308c308u, 0x80008000u);
+            const uint32_t x[4] = {code[V][i].x, code[V][i].y, code[V][i].z, code[V][i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(to + i * ROWS * 128 + off[k]) = pairs<LARGE>(x[k], s1, m136, s4);
         }
     }
 };
+
+// Column of O, of 16 that begin with a multiple of 16, that has dimension i.
+template <bool I4>
+__device__ __forceinline__ constexpr int column_of(int i) { return I4 ? (i & 8) + (i & 3) * 2 + (i >> 2 & 1) : i; }
 
 // A thread's row of the running softmax.
 struct RowState {
@@ -426,7 +444,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
             Codes4<D> codes{a, s, tid >> 5 << 5, lane};
             if constexpr (I4) {
                 codes.look_up(s.tile0);
-                codes.load(s.tile0);
+                codes.template load<false>(s.tile0);
+                codes.template load<true>(s.tile0);
                 codes.look_up(s.tile0 + 1);
             }
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
@@ -503,8 +522,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 const int pos0 = t * kTcKeys;
                 const bool drafted = pos0 + kTcKeys > s.len;    // rows that not every node sees, or past the end
                 if constexpr (I4) {
+                    codes.ask(t + 1);
                     if (!mbar_wait_warp(&m.k_empty[rk.i], rk.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
                     codes.template store<false>(smem + C::OFF_K + rk.i * C::TILE, t, bad);
+                    codes.template load<false>(t + 1);          // under way while V's are stored, and the other way round
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&m.k_full[rk.i]);
@@ -515,7 +536,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&m.v_ready[rv.i]);
                     rv.next<NV>();
-                    codes.load(t + 1);
+                    codes.template load<true>(t + 1);
                     codes.look_up(t + 2);
                     continue;
                 }
@@ -715,8 +736,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                                 float o[4];
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) {
-                                    o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[i + j]) * up0;
-                                    if (up1 != 0.f) o[j] += __uint_as_float(y[i + j]) * up1;
+                                    const int k = column_of<I4>(i + j);
+                                    o[j] = up0 == 0.f ? 0.f : __uint_as_float(x[k]) * up0;
+                                    if (up1 != 0.f) o[j] += __uint_as_float(y[k]) * up1;
                                 }
                                 // 16-byte chunks turned by the row: rows' equal chunks lie in distinct banks
                                 *reinterpret_cast<float4*>(buf + mine_at + ((d + i) / 4 + row) % (wide / 4) * 4) = make_float4(o[0], o[1], o[2], o[3]);
@@ -758,8 +780,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                     float o[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        o[i] = up0 == 0.f ? 0.f : __uint_as_float(x[i]) * up0;
-                        if (RT == 1 && up1 != 0.f) o[i] += __uint_as_float(y[i]) * up1;
+                        const int k = column_of<I4>(i);
+                        o[i] = up0 == 0.f ? 0.f : __uint_as_float(x[k]) * up0;
+                        if (RT == 1 && up1 != 0.f) o[i] += __uint_as_float(y[k]) * up1;
                     }
                     if (whole) {
                         uint32_t w[8];
