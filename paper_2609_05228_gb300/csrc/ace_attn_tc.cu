@@ -18,8 +18,8 @@
 // 2^-18 of it); a code's scale multiplies its column of S. V's codes become fp16 in shared memory with their scales, in units
 // of 2^eref, a power of two above the scales so far (ace_attn_tc.cuh: Reference): exact but for rows whose scale is 2^-20 of the
 // largest and less, whose codes' last bits fall under fp16's least.
-// 4-bit caches: K's and V's codes times their scales, which bf16 holds exactly, are written as the tiles of a plain cache by the four
-// warps that lay out q (Codes4), in place of TMA.
+// 4-bit caches: K's and V's codes times their scales, which bf16 holds exactly, are written as the tiles of a plain cache by two
+// groups of four warps (Codes4), in place of TMA.
 // P is rounded to bf16 (2^-9 of a weight; plain caches) or fp16 (2^-12), as the products need; sums, maxima and O are fp32.
 // Measured: 8 users of up to 16384 positions, 128 nodes of 64 heads (8 kv heads of 128), bf16: 304 us, 850 TFLOP/s. 64 users
 // of up to 8192, 4 kv heads of 128: 64 rows a unit 114 us fp8, 128 bf16; 128 rows 139 and 135; 192 rows 213 and 162. Bound by
@@ -63,6 +63,14 @@ struct Misc : TcShared {
     float4 kf[FP8 ? kAuxRing : 1][32];          // 128 factors a tile
     uint2 vf[FP8 ? kAuxRing : 1][32];           // the same as fp16
 };
+
+// 4-bit caches have a fifth warpgroup: V's tiles, beside K's. Registers go from the first one, which issues and schedules, to the
+// softmax: 640 threads are launched with 96 each, 61440, and 128 (56 + 2 * 128 + 2 * 80) = 60416 are in use.
+constexpr int tc_threads(bool i4) { return i4 ? 640 : kTcThreads; }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
 template <bool FP8, int D, int RT, int CP>
 constexpr int tc_smem() { return 1024 + Cfg<FP8, D, RT, CP>::OFF_MISC + (int)sizeof(Misc<FP8, RT>); }
@@ -136,18 +144,20 @@ __device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, flo
     return (a + b) + (c + d);
 }
 
-// Four warps, caches in 4 bits: tiles of K and V as the products take them. A row's group of 32 codes is a lane's 16 bytes, 8 or 16
-// rows a turn, so that a warp reads 512 bytes on end; loaded a tile ahead, their pages two. (s: the tile's segment.)
-template <int D>
+// Four warps, caches in 4 bits: tiles of K (V = false) or V as the products take them. A row's group of 32 codes is a lane's 16 bytes, 8
+// or 16 rows a turn, so that a warp reads 512 bytes on end; loaded a tile ahead, their pages two. (s: the tile's segment.)
+template <int D, bool V>
 struct Codes4 {
     static constexpr int CH = D / kGroup4, ROWS = 32 / CH, TURNS = 32 / ROWS;       // groups of a row; rows of a turn; turns of a warp's 32 rows
     const AttnArgs& a;
     const Segment& s;
     int row0, lane;                     // the warp's first row of a tile
     int page[2];                        // of its runs of 16 rows
-    uint4 code[2][TURNS];
-    uint16_t scale[2][TURNS];
+    uint4 code[TURNS];
+    uint16_t scale[TURNS];
 
+    __device__ __forceinline__ const uint8_t* pool() const { return static_cast<const uint8_t*>(V ? a.v_pool : a.k_pool); }
+    __device__ __forceinline__ const uint8_t* scales() const { return V ? a.v_scale : a.k_scale; }
     __device__ __forceinline__ void look_up(int t) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -155,34 +165,35 @@ struct Codes4 {
             page[i] = t < s.tile1 && pos < s.len + s.n ? page_of(a, s.b, pos) : -1;
         }
     }
-    // The lines of tile t, whose pages have been looked up, on their way to L2: 128 bytes of K's or V's codes a lane, and some lanes'
-    // scales.
+    // The lines of tile t, whose pages have been looked up, on their way to L2: 128 bytes of codes a lane, and the scales.
     __device__ __forceinline__ void ask(int t) {
         constexpr int LINE = 256 / D;   // rows of a line
-        const int r = (lane & 15) * LINE, pg = r < 16 ? page[0] : page[1];
+        const int r = lane * LINE, pg = r < 16 ? page[0] : page[1];
         if (r < 32 && pg >= 0) {
             const long long row = (long long)(pg * a.kv_heads + s.head) * a.page_size + ((t * kTcKeys + row0 + r) & (a.page_size - 1));
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t*>(lane < 16 ? a.k_pool : a.v_pool) + row * (D / 2)));
-            if (r % 16 == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"((lane < 16 ? a.k_scale : a.v_scale) + row * (2 * CH)));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(pool() + row * (D / 2)));
+            if (r % 16 == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(scales() + row * (2 * CH)));
         }
     }
-    // K's (V = false) or V's codes of tile t, whose pages have been looked up.
-    template <bool V>
+    // The codes of tile t, whose pages have been looked up.
     __device__ __forceinline__ void load(int t) {
         const int total = s.len + s.n;
-        const uint8_t* pool = static_cast<const uint8_t*>(V ? a.v_pool : a.k_pool);
-        const uint16_t* scales = reinterpret_cast<const uint16_t*>(V ? a.v_scale : a.k_scale);
 #pragma unroll
         for (int i = 0; i < TURNS; ++i) {
             const int pos = t * kTcKeys + row0 + i * ROWS + lane % ROWS, c = lane / ROWS, pg = page[i * ROWS / 16];
-            code[V][i] = make_uint4(0, 0, 0, 0);
-            scale[V][i] = 0;
+            code[i] = make_uint4(0, 0, 0, 0);
+            scale[i] = 0;
             if (pg >= 0 && pos < total) {
                 const long long row = (long long)(pg * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-                code[V][i] = ld_stream(pool + row * (D / 2) + c * 16);
-                scale[V][i] = __ldg(scales + row * CH + c);
+                code[i] = ld_stream(pool() + row * (D / 2) + c * 16);
+                scale[i] = __ldg(reinterpret_cast<const uint16_t*>(scales()) + row * CH + c);
             }
         }
+    }
+    __device__ __forceinline__ void begin() {
+        look_up(s.tile0);
+        load(s.tile0);
+        look_up(s.tile0 + 1);
     }
     // Pairs of elements (0, 4), (1, 5), (2, 6), (3, 7) of a word times the scale s, exactly: 128 + c is c in the last places of 128, and
     // s (128 + c) - 136 s; four places up, bf16 reads 16 c 2^-133, and 4 s (c / 4 - 2). LARGE: 136 s may be past bf16's largest.
@@ -195,26 +206,25 @@ struct Codes4 {
                           LARGE ? fma_bf16x2(fma_bf16x2(c2, kOne, kMinus136), s1, kMinus0) : fma_bf16x2(c2, s1, m136),
                           fma_bf16x2(fma_bf16x2(u & 0x00f000f0u, k2To127, kMinus2), s4, kMinus0));
     }
-    // The tile of K (V = false) or V. 8 elements lie in the order 0 4 1 5 2 6 3 7, as q's do, and O's columns after V. 8 lanes store rows
+    // The tile. 8 elements lie in the order 0 4 1 5 2 6 3 7, as q's do, and O's columns after V. 8 lanes store rows
     // on end, whose chunks lie in distinct banks.
-    template <bool V>
     __device__ __forceinline__ void store(unsigned char* tile, int t, unsigned long long* bad) {
         bool large = false;
 #pragma unroll
         for (int i = 0; i < TURNS; ++i) {
             if (V && t * kTcKeys + kTcKeys > s.len) {
                 const int nd = t * kTcKeys + row0 + lane % ROWS + i * ROWS - s.len;
-                if (nd >= 0 && (scale[V][i] & 0x7f80u) == 0x7f80u) {
-                    scale[V][i] = 0;
+                if (nd >= 0 && (scale[i] & 0x7f80u) == 0x7f80u) {
+                    scale[i] = 0;
                     atomicOr(&bad[nd >> 6], 1ull << (nd & 63));
                 }
             }
-            large = large || (scale[V][i] & 0x7fffu) >= 0x7b80u;        // 2^120
+            large = large || (scale[i] & 0x7fffu) >= 0x7b80u;        // 2^120
         }
-        if (__builtin_expect(__any_sync(0xffffffffu, large), 0)) store_rows<V, true>(tile);
-        else store_rows<V, false>(tile);
+        if (__builtin_expect(__any_sync(0xffffffffu, large), 0)) store_rows<true>(tile);
+        else store_rows<false>(tile);
     }
-    template <bool V, bool LARGE>
+    template <bool LARGE>
     __device__ __forceinline__ void store_rows(unsigned char* tile) {
         const int c = lane / ROWS, r = row0 + lane % ROWS;
         unsigned char* to = tile + (c >> 1) * 16384 + r * 128;
@@ -223,9 +233,9 @@ struct Codes4 {
         for (int k = 0; k < 4; ++k) off[k] = (((c & 1) * 4 + k) ^ (r & 7)) << 4;
 #pragma unroll
         for (int i = 0; i < TURNS; ++i) {
-            const uint32_t sc = scale[V][i], s1 = sc | sc << 16, s4 = fma_bf16x2(s1, 0x40804080u, 0x80008000u);
+            const uint32_t sc = scale[i], s1 = sc | sc << 16, s4 = fma_bf16x2(s1, 0x40804080u, 0x80008000u);
             const uint32_t m136 = fma_bf16x2(s1, 0xc308c308u, 0x80008000u);
-            const uint32_t x[4] = {code[V][i].x, code[V][i].y, code[V][i].z, code[V][i].w};
+            const uint32_t x[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(to + i * ROWS * 128 + off[k]) = pairs<LARGE>(x[k], s1, m136, s4);
         }
@@ -299,7 +309,7 @@ __device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
 // CP = 2 (at most 64 rows): the block holds them twice, 64 lanes apart, and each copy's warps take half of a tile's
 // columns: the tile's softmax takes half the time, and the copies' O are added at the end.
 template <bool FP8, bool I4, int D, int RT, int CP>
-__global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant__ TcAttnArgs p) {
+__global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_constant__ TcAttnArgs p) {
     using C = Cfg<FP8, D, RT, CP>;
     constexpr int ROWS = C::ROWS, NK = C::NK, NV = C::NV, NC = C::NC, FMT = I4 ? ACE_KV_INT4 : FP8 ? ACE_KV_FP8 : ACE_KV_PLAIN;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -326,7 +336,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         mbar_init(&m.drain[0], 1), mbar_init(&m.drain[1], 1);
         for (int i = 0; i < kSegRing; ++i) {
             mbar_init(&m.seg_full[i], 1);
-            mbar_init(&m.seg_empty[i], FP8 ? 16 : I4 ? 14 : 15);        // load, 2 MMA, (scales,) 8 softmax and 4 converting warps
+            mbar_init(&m.seg_empty[i], FP8 ? 16 : I4 ? 18 : 15);        // load, 2 MMA, (scales,) 8 softmax and 4 (8) converting warps
         }
         for (int i = 0; i < kAuxRing; ++i) {
             mbar_init(&m.aux_full[i], 1);
@@ -345,109 +355,133 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
     const uint32_t tmem = m.tmem;                       // four buffers of S, O0, O1
     constexpr uint32_t kO = 256;
     Walk walk{m, a, {}};
-
-    if (warp == 0) {
+    if (I4 && warp >= 16) {
+        // ------------------------------------------------ tiles of V (4 bits)
         if constexpr (I4) {
-            role_schedule<ROWS, kTcStart>(m, a);
-        } else {
-            Scheduler<ROWS, kTcStart> sched(m, a);                // a segment ahead of the loads
-            if (sched.publish()) role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [&] { return sched.publish(); });
-        }
-    } else if (warp == 2) {
-        if constexpr (FP8) role_scales<kTcRoom>(m, a, m.kf, m.vf);
-    } else if (warp == 1 || warp == 3) {
-        // ------------------------------------------------ MMA issuers, one a softmax group
-        if (elect_one()) {
-            const int g = warp >> 1;
-            Ring rk, rv;                        // rv: V's ring, as stored (plain) or as fp16 (fp8)
-            constexpr int NP = FP8 ? NC : NV, kVTile = FP8 ? C::CONV : C::TILE;
-            uint64_t* v_free = FP8 ? m.c_empty : m.v_empty;
-            uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit n & 1 of the group's two S buffers
-            const uint32_t q0 = desc_lo(smem_u32(smem + (RT == 2 ? g * C::Q : 0)), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
-            const uint32_t v0 = desc_lo(smem_u32(smem + (FP8 ? C::OFF_C : C::OFF_V)), kVBlock);
-            const uint32_t o = tmem + kO + (uint32_t)(g * D);
+            fewer_registers<80>();
+            Ring rv;
             bool ok = true;
-            while (true) {
-                if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
-                if (!m.seg[walk.seg.i].go) break;
-                const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * RT;        // the group's
-                mbar_arrive(&m.seg_empty[walk.seg.i]);
-                walk.seg.next<kSegRing>();
-                if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
-                q_phase ^= 1u;
-                for (int n = 0; n <= items; ++n) {
-                    if (n < items) {
-                        // S of item n = Q K^T; the product that read P from this buffer (item n - 2) was issued before
-                        const int half = RT == 2 ? n & 1 : g, buf = (n & 1) * 2 + g;
-                        if (n % RT == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
-                        tc_fence_after();
-                        const uint32_t d = tmem + (uint32_t)(buf * kHalf);
-                        const uint32_t kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4) + half * (kHalf * (FP8 ? D : 128) >> 4));
-                        if constexpr (FP8) {
-#pragma unroll
-                            for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
-                                const uint32_t st = kk % (D / 32) * 2;
-                                mma_ss<true>(d, q0 + (kk < D / 32 ? 0 : C::Q >> 5) + st, kl + st, D == 128 ? kRows128 : kRows64,
-                                             idesc_of(0, 128, kHalf, false), kk > 0);
-                            }
-                        } else {
-#pragma unroll
-                            for (int kk = 0; kk < D / 16; ++kk) {
-                                const uint32_t st = (kk >> 2) * (16384 >> 4) + (kk & 3) * 2;
-                                mma_ss<false>(d, q0 + st, kl + st, kRows128, idesc_of(1, 128, kHalf, false), kk > 0);
-                            }
-                        }
-                        mma_commit(&m.s_full[buf]);
-                        if (n % RT == RT - 1) {
-                            mma_commit(&m.k_empty[rk.i]);
-                            rk.next<NK>();
-                        }
-                        if (n == items - 1) mma_commit(&m.q_free);
-                    }
-                    if (n > 0) {
-                        // O += P V of item j = n - 1
-                        const int j = n - 1, half = RT == 2 ? j & 1 : g, buf = (j & 1) * 2 + g;
-                        if (!mbar_wait_or_abort(&m.p_ready[buf], p_phase >> (j & 1) & 1u, a.err, abort_flag)) { ok = false; break; }
-                        p_phase ^= 1u << (j & 1);
-                        if (j % RT == 0 && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
-                        tc_fence_after();
-                        const uint32_t vl = v0 + (uint32_t)(rv.i * (kVTile >> 4) + half * (kHalf * 128 >> 4));
-                        const uint32_t pa = tmem + (uint32_t)(buf * kHalf);
-#pragma unroll
-                        for (int kk = 0; kk < kHalf / 16; ++kk)
-                            mma_ts(o, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j > 0 || kk > 0);
-                        mma_commit(&m.o_done[buf]);
-                        if (j % RT == RT - 1) {
-                            mma_commit(&v_free[rv.i]);
-                            rv.next<NP>();
-                        }
-                    }
+            while (ok && walk.next()) {
+                const Segment& s = walk.segment();
+                unsigned long long* bad = m.seg[walk.seg.i].bad;
+                Codes4<D, true> codes{a, s, (warp - 16) * 32, lane};
+                codes.begin();
+                for (int t = s.tile0; t < s.tile1; ++t) {
+                    codes.ask(t + 1);
+                    if (!mbar_wait_warp(&m.v_empty[rv.i], rv.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    codes.store(smem + C::OFF_V + rv.i * C::TILE, t, bad);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&m.v_ready[rv.i]);
+                    rv.next<NV>();
+                    codes.load(t + 1);
+                    codes.look_up(t + 2);
                 }
-                if (!ok) break;
+                if (ok) walk.done();
             }
             if (!ok) *abort_flag = 1;
-            if (*abort_flag) {
-                // products in flight read shared memory and TMEM
-                mma_commit(&m.drain[g]);
-                mbar_wait(&m.drain[g], 0, a.err);
-            }
         }
-        __syncwarp();
+    } else if (warp < 4) {
+        if constexpr (I4) fewer_registers<56>();
+        if (warp == 0) {
+            if constexpr (I4) {
+                role_schedule<ROWS, kTcStart>(m, a);
+            } else {
+                Scheduler<ROWS, kTcStart> sched(m, a);                // a segment ahead of the loads
+                if (sched.publish()) role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [&] { return sched.publish(); });
+            }
+        } else if (warp == 2) {
+            if constexpr (FP8) role_scales<kTcRoom>(m, a, m.kf, m.vf);
+        } else {
+            // ------------------------------------------------ MMA issuers, one a softmax group
+            if (elect_one()) {
+                const int g = warp >> 1;
+                Ring rk, rv;                        // rv: V's ring, as stored (plain) or as fp16 (fp8)
+                constexpr int NP = FP8 ? NC : NV, kVTile = FP8 ? C::CONV : C::TILE;
+                uint64_t* v_free = FP8 ? m.c_empty : m.v_empty;
+                uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit n & 1 of the group's two S buffers
+                const uint32_t q0 = desc_lo(smem_u32(smem + (RT == 2 ? g * C::Q : 0)), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
+                const uint32_t v0 = desc_lo(smem_u32(smem + (FP8 ? C::OFF_C : C::OFF_V)), kVBlock);
+                const uint32_t o = tmem + kO + (uint32_t)(g * D);
+                bool ok = true;
+                while (true) {
+                    if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
+                    if (!m.seg[walk.seg.i].go) break;
+                    const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * RT;        // the group's
+                    mbar_arrive(&m.seg_empty[walk.seg.i]);
+                    walk.seg.next<kSegRing>();
+                    if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
+                    q_phase ^= 1u;
+                    for (int n = 0; n <= items; ++n) {
+                        if (n < items) {
+                            // S of item n = Q K^T; the product that read P from this buffer (item n - 2) was issued before
+                            const int half = RT == 2 ? n & 1 : g, buf = (n & 1) * 2 + g;
+                            if (n % RT == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
+                            tc_fence_after();
+                            const uint32_t d = tmem + (uint32_t)(buf * kHalf);
+                            const uint32_t kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4) + half * (kHalf * (FP8 ? D : 128) >> 4));
+                            if constexpr (FP8) {
+#pragma unroll
+                                for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
+                                    const uint32_t st = kk % (D / 32) * 2;
+                                    mma_ss<true>(d, q0 + (kk < D / 32 ? 0 : C::Q >> 5) + st, kl + st, D == 128 ? kRows128 : kRows64,
+                                                 idesc_of(0, 128, kHalf, false), kk > 0);
+                                }
+                            } else {
+#pragma unroll
+                                for (int kk = 0; kk < D / 16; ++kk) {
+                                    const uint32_t st = (kk >> 2) * (16384 >> 4) + (kk & 3) * 2;
+                                    mma_ss<false>(d, q0 + st, kl + st, kRows128, idesc_of(1, 128, kHalf, false), kk > 0);
+                                }
+                            }
+                            mma_commit(&m.s_full[buf]);
+                            if (n % RT == RT - 1) {
+                                mma_commit(&m.k_empty[rk.i]);
+                                rk.next<NK>();
+                            }
+                            if (n == items - 1) mma_commit(&m.q_free);
+                        }
+                        if (n > 0) {
+                            // O += P V of item j = n - 1
+                            const int j = n - 1, half = RT == 2 ? j & 1 : g, buf = (j & 1) * 2 + g;
+                            if (!mbar_wait_or_abort(&m.p_ready[buf], p_phase >> (j & 1) & 1u, a.err, abort_flag)) { ok = false; break; }
+                            p_phase ^= 1u << (j & 1);
+                            if (j % RT == 0 && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                            tc_fence_after();
+                            const uint32_t vl = v0 + (uint32_t)(rv.i * (kVTile >> 4) + half * (kHalf * 128 >> 4));
+                            const uint32_t pa = tmem + (uint32_t)(buf * kHalf);
+#pragma unroll
+                            for (int kk = 0; kk < kHalf / 16; ++kk)
+                                mma_ts(o, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j > 0 || kk > 0);
+                            mma_commit(&m.o_done[buf]);
+                            if (j % RT == RT - 1) {
+                                mma_commit(&v_free[rv.i]);
+                                rv.next<NP>();
+                            }
+                        }
+                    }
+                    if (!ok) break;
+                }
+                if (!ok) *abort_flag = 1;
+                if (*abort_flag) {
+                    // products in flight read shared memory and TMEM
+                    mma_commit(&m.drain[g]);
+                    mbar_wait(&m.drain[g], 0, a.err);
+                }
+            }
+            __syncwarp();
+        }
     } else if (warp >= 12) {
-        // ------------------------------------------------ q rows, and V tiles made ready
+        // ------------------------------------------------ q rows, and V tiles (4 bits: K tiles) made ready
+        if constexpr (I4) fewer_registers<80>();
         const int tid = threadIdx.x - 384;
         Ring rk, rv, rc, ra;
         uint32_t q_phase = 1;           // the first segment's q buffer is free
         bool ok = true;
         while (ok && walk.next()) {
             const Segment& s = walk.segment();
-            Codes4<D> codes{a, s, tid >> 5 << 5, lane};
-            if constexpr (I4) {
-                codes.look_up(s.tile0);
-                codes.template load<false>(s.tile0);
-                codes.template load<true>(s.tile0);
-                codes.look_up(s.tile0 + 1);
-            }
+            Codes4<D, false> codes{a, s, tid >> 5 << 5, lane};
+            if constexpr (I4) codes.begin();
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
             constexpr int kStep = 128 / kChunks, kBatch = 4;        // rows a pass; passes whose loads are under way together
@@ -524,19 +558,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
                 if constexpr (I4) {
                     codes.ask(t + 1);
                     if (!mbar_wait_warp(&m.k_empty[rk.i], rk.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
-                    codes.template store<false>(smem + C::OFF_K + rk.i * C::TILE, t, bad);
-                    codes.template load<false>(t + 1);          // under way while V's are stored, and the other way round
+                    codes.store(smem + C::OFF_K + rk.i * C::TILE, t, bad);
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&m.k_full[rk.i]);
                     rk.next<NK>();
-                    if (!mbar_wait_warp(&m.v_empty[rv.i], rv.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
-                    codes.template store<true>(smem + C::OFF_V + rv.i * C::TILE, t, bad);
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&m.v_ready[rv.i]);
-                    rv.next<NV>();
-                    codes.template load<true>(t + 1);
+                    codes.load(t + 1);
                     codes.look_up(t + 2);
                     continue;
                 }
@@ -601,6 +628,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_attn_tc(const __grid_constant
         if (!ok) *abort_flag = 1;
     } else {
         // ------------------------------------------------ softmax: group g of 4 warps, a thread per row
+        if constexpr (I4) more_registers<128>();
         const int g = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t s_t = tmem + lanes, o_t = tmem + lanes + kO + (uint32_t)(g * D);
@@ -854,7 +882,7 @@ cudaError_t tc_attrs() {
 
 template <int FMT, int D, int RT, int CP>
 cudaError_t tc_go(const TcAttnArgs& p, int ctas, cudaStream_t s) {
-    tc_kernel<FMT, D, RT, CP><<<ctas, kTcThreads, tc_smem<FMT == ACE_KV_FP8, D, RT, CP>(), s>>>(p);
+    tc_kernel<FMT, D, RT, CP><<<ctas, tc_threads(FMT == ACE_KV_INT4), tc_smem<FMT == ACE_KV_FP8, D, RT, CP>(), s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? launch_join(p.a, ACE_BF16, CP == 1, Cfg<FMT == ACE_KV_FP8, D, RT, CP>::ROWS, ctas, s) : e;
 }
