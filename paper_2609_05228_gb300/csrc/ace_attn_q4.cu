@@ -1,5 +1,5 @@
 // ace_attn_q4.cu — attention for trees of drafted tokens over a cache in 4 bits where a unit has few query rows (nodes times query
-// heads a kv head at most 32; bf16 activations, head sizes 64 and 128): bound by the cache's bytes, 72 a row of 128.
+// heads a kv head at most 16; bf16 activations, head sizes 64 and 128): bound by the cache's bytes, 72 a row of 128.
 //   S^T = K Q^T       16 positions x 8 rows a product (m16n8k16); codes are exact in fp16, q too once its row is scaled by a power
 //                     of two, so a group's product is exact but for fp32's sums, and its scale is one factor of 16 x 8 sums
 //   P^T = 2^(S^T - ref)   bf16
@@ -11,6 +11,7 @@
 // CTA walk their 16 positions of each tile on their own, with their own running maxima, from rings of cp.async stages; they meet at
 // a unit's end only.
 #include <cfloat>
+#include <type_traits>
 
 #include "ace_attn_tc.cuh"
 
@@ -25,7 +26,7 @@ constexpr float kNone4 = -FLT_MAX;      // reference of a row that has seen noth
 template <int D, int NT>
 struct Q4 {
     static constexpr int SUBS = NT == 1 ? 2 : 1, STAGES = NT == 1 ? 2 : 4;
-    static constexpr int WARPS = NT == 2 ? 6 : 8, THREADS = 32 * WARPS, CTAS = NT <= 2 ? 2 : 1;      // CTAS: an SM
+    static constexpr int WARPS = NT == 1 ? 8 : 6, THREADS = 32 * WARPS, CTAS = 2;        // CTAS: an SM
     static constexpr int KEYS = WARPS * SUBS * kStep;          // positions of a tile
     static constexpr int START = NT == 1 ? 1 : 3;               // a unit's start and end in tiles of the work line
     static constexpr int ROW = D / 2, G = D / kGroup4;          // bytes and groups of a row
@@ -382,6 +383,27 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
                         }
                 }
             }
+            // ---- V's scales; 0 times an infinity or a NaN is no zero
+            Scales k[kSub][2];
+            uint32_t fine = 0;
+#pragma unroll
+            for (int u = 0; u < kSub; ++u)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const unsigned char* from = at + u * C::SUB + v_scale_at + 16 * G * i;
+                    uint32_t lo = *reinterpret_cast<const uint16_t*>(from), hi = *reinterpret_cast<const uint16_t*>(from + 8 * G);
+                    if (__builtin_expect(drafted, 0)) {
+                        // what is not finite in a drafted row is for those that see it: noted, and left out of the products
+                        const int nd = pos + u * kStep + t + 8 * i - len;
+                        if (nd >= 0 && (lo & 0x7f80u) == 0x7f80u) lo = 0, atomicOr(&m.bad[nd >> 6], 1ull << (nd & 63));
+                        if (nd + 4 >= 0 && (hi & 0x7f80u) == 0x7f80u) hi = 0, atomicOr(&m.bad[(nd + 4) >> 6], 1ull << ((nd + 4) & 63));
+                    }
+                    k[u][i].s = lo | hi << 16;
+                    k[u][i].m136 = fma_bf16x2(k[u][i].s, 0xc308c308u, 0x80008000u);
+                    k[u][i].x8 = fma_bf16x2(k[u][i].s, 0x41004100u, 0x80008000u);
+                    fine = fma_bf16x2(k[u][i].m136, 0u, fine);
+                }
+            const bool large = (fine & 0x7fff7fffu) != 0;
             // ---- references: a row's moves where a score is 2^kLazy above it
             float over = -INFINITY;
 #pragma unroll
@@ -393,7 +415,9 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
                     for (int u = 1; u < kSub; ++u) top = fmaxf(top, fmaxf(x[u][n][r], x[u][n][2 + r]));
                     over = fmaxf(over, top - ref[n][r]);
                 }
-            if (__builtin_expect(__any_sync(0xffffffffu, over > (float)kLazy), 0)) {
+            bool any_large = false;
+            if (__builtin_expect(__any_sync(0xffffffffu, over > (float)kLazy || large), 0)) {
+                any_large = __any_sync(0xffffffffu, large);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -410,53 +434,37 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
                         for (int j = 0; j < TJ; ++j) o[j][n][r] *= f, o[j][n][2 + r] *= f;
                     }
             }
+            // ---- weights and values
+            auto finish = [&](auto is_large) {
 #pragma unroll
-            for (int u = 0; u < kSub; ++u) {
-                const unsigned char* run = at + u * C::SUB;
-                // ---- weights
-                uint32_t p[NT][2];
+                for (int u = 0; u < kSub; ++u) {
+                    uint32_t p[NT][2], w[4][D / 64];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float e[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = exp2_approx(x[u][n][i] - ref[n][i & 1]);
-                    l[n][0] += e[0] + e[2];
-                    l[n][1] += e[1] + e[3];
-                    const __nv_bfloat162 y = __floats2bfloat162_rn(e[0], e[1]), w = __floats2bfloat162_rn(e[2], e[3]);
-                    p[n][0] = transposed(*reinterpret_cast<const uint32_t*>(&y));
-                    p[n][1] = transposed(*reinterpret_cast<const uint32_t*>(&w));
-                }
-                // ---- values
-                uint32_t w[4][D / 64];
-                Scales k[2];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const unsigned char* from = run + (i & 1 ? v_at[1] : v_at[0]) + i * 4 * C::ROW;
-                    if constexpr (D == 128) {
-                        const uint2 y = *reinterpret_cast<const uint2*>(from);
-                        w[i][0] = y.x, w[i][1] = y.y;
-                    } else {
-                        w[i][0] = *reinterpret_cast<const uint32_t*>(from);
+                    for (int i = 0; i < 4; ++i) {
+                        const unsigned char* from = at + u * C::SUB + (i & 1 ? v_at[1] : v_at[0]) + i * 4 * C::ROW;
+                        if constexpr (D == 128) {
+                            const uint2 y = *reinterpret_cast<const uint2*>(from);
+                            w[i][0] = y.x, w[i][1] = y.y;
+                        } else {
+                            w[i][0] = *reinterpret_cast<const uint32_t*>(from);
+                        }
                     }
-                }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t lo = *reinterpret_cast<const uint16_t*>(run + v_scale_at + 16 * G * i), hi = *reinterpret_cast<const uint16_t*>(run + v_scale_at + 16 * G * i + 8 * G);
-                    if (__builtin_expect(drafted, 0)) {
-                        // what is not finite in a drafted row is for those that see it: noted, and left out of the products
-                        const int nd = pos + u * kStep + t + 8 * i - len;
-                        if (nd >= 0 && (lo & 0x7f80u) == 0x7f80u) lo = 0, atomicOr(&m.bad[nd >> 6], 1ull << (nd & 63));
-                        if (nd + 4 >= 0 && (hi & 0x7f80u) == 0x7f80u) hi = 0, atomicOr(&m.bad[(nd + 4) >> 6], 1ull << ((nd + 4) & 63));
+                    for (int n = 0; n < NT; ++n) {
+                        float e[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) e[i] = exp2_approx(x[u][n][i] - ref[n][i & 1]);
+                        l[n][0] += e[0] + e[2];
+                        l[n][1] += e[1] + e[3];
+                        const __nv_bfloat162 y = __floats2bfloat162_rn(e[0], e[1]), z = __floats2bfloat162_rn(e[2], e[3]);
+                        p[n][0] = transposed(*reinterpret_cast<const uint32_t*>(&y));
+                        p[n][1] = transposed(*reinterpret_cast<const uint32_t*>(&z));
                     }
-                    k[i].s = lo | hi << 16;
-                    k[i].m136 = fma_bf16x2(k[i].s, 0xc308c308u, 0x80008000u);
-                    k[i].x8 = fma_bf16x2(k[i].s, 0x41004100u, 0x80008000u);
+                    add_values<D, NT, decltype(is_large)::value>(w, k[u], p, o);
                 }
-                // 0 times an infinity or a NaN is no zero
-                const uint32_t fine = fma_bf16x2(k[0].m136, 0u, fma_bf16x2(k[1].m136, 0u, 0u));
-                if (__builtin_expect(__any_sync(0xffffffffu, (fine & 0x7fff7fffu) != 0), 0)) add_values<D, NT, true>(w, k, p, o);
-                else add_values<D, NT, false>(w, k, p, o);
-            }
+            };
+            if (__builtin_expect(any_large, 0)) finish(std::true_type{});
+            else finish(std::false_type{});
         }
         // ---------------- the unit's result, or this CTA's part of it
 #pragma unroll
@@ -563,15 +571,13 @@ template <int D>
 cudaError_t q4_go(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
     const long long rows = (long long)a.max_nodes * a.group;
     if (rows <= 8) return q4_run<D, 1>(kv, a, s);
-    if (rows <= 16) return q4_run<D, 2>(kv, a, s);
-    return q4_run<D, 4>(kv, a, s);
+    return q4_run<D, 2>(kv, a, s);
 }
 
 template <int D>
 cudaError_t q4_attrs() {
-    cudaError_t e = q4_attr<D, 1>();
-    if (e == cudaSuccess) e = q4_attr<D, 2>();
-    return e == cudaSuccess ? q4_attr<D, 4>() : e;
+    const cudaError_t e = q4_attr<D, 1>();
+    return e == cudaSuccess ? q4_attr<D, 2>() : e;
 }
 
 }  // namespace

@@ -937,10 +937,9 @@ cudaError_t attn_tc_init(ace_kv* kv) {
 
 cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaStream_t s) {
     const int format = kv->desc.format;
-#ifndef KFEW4
-#define KFEW4 32
-#endif
-    if ((long long)a.max_nodes * a.group <= (format == ACE_KV_INT4 ? KFEW4 : kFewRows)) return format == ACE_KV_INT4 ? launch_attn_q4(kv, a, s) : launch_attn_few(kv, a, s);
+    const long long rows = (long long)a.max_nodes * a.group;
+    if (format == ACE_KV_INT4 && rows <= kFewRows4) return launch_attn_q4(kv, a, s);
+    if (format != ACE_KV_INT4 && rows <= kFewRows) return launch_attn_few(kv, a, s);
     TcAttnArgs p;
     p.a = a;
     p.k = kv->maps.k;
