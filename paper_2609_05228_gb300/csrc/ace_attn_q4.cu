@@ -28,7 +28,7 @@ struct Q4 {
     static constexpr int SUBS = NT == 1 ? 2 : 1, STAGES = NT == 1 ? 2 : 4;
     static constexpr int WARPS = NT == 1 ? 8 : 6, THREADS = 32 * WARPS, CTAS = 2;        // CTAS: an SM
     static constexpr int KEYS = WARPS * SUBS * kStep;          // positions of a tile
-    static constexpr int START = NT == 1 ? 1 : 3;               // a unit's start and end in tiles of the work line
+    static constexpr int START = NT == 1 ? 2 : 3;               // a unit's start and end in tiles of the work line
     static constexpr int ROW = D / 2, G = D / kGroup4;          // bytes and groups of a row
     static constexpr int CODES = kStep * ROW, SCALES = kStep * G * 2;
     static constexpr int SUB = 2 * CODES + 2 * SCALES, STAGE = SUBS * SUB;
@@ -49,6 +49,7 @@ struct Q4Shared {
     unsigned long long bad[kMaxNodes / 64];     // nodes with a V that is not finite, left out of the products
     Segment seg[3];                     // the one at work, and two ahead
     int go[3];
+    RequestTable requests;
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1,
@@ -159,16 +160,15 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
     const int k_scale_at = 2 * C::CODES + place * (2 * G), v_scale_at = 2 * C::CODES + C::SCALES + t * (2 * G) + g * G / 8 * 2;
 
     Cursor cur{};
-    bool more = false;
-    if (warp == 0) {
-        if (lane == 0) note_none(a);
-        more = cursor_init<ROWS, kKeys4, kStart4>(a, blockIdx.x, gridDim.x, cur);
-    }
+    if (tid == 0) note_none(a);
+    bool more = cursor_init_block<ROWS, kKeys4, kStart4, kThreads4>(a, blockIdx.x, gridDim.x, cur, m.requests);
+    if (!more) return;
     // by warp 0: the segment after, into slot i
     auto schedule = [&](int i) {
         if (warp == 0) {
             Segment s{};
-            more = more && cursor_next<ROWS, kKeys4, kStart4>(a, blockIdx.x, cur, s);
+            more = more && cursor_next<ROWS, kKeys4, kStart4>(a, blockIdx.x, cur, s,
+                                                              [&](int b) { return b < kTabled ? m.requests.request[b] : request_of(a, b); });
             if (lane == 0) {
                 m.go[i] = more;
                 if (more) {
@@ -285,20 +285,99 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
 
     schedule(0);
     __syncthreads();
-    if (!m.go[0]) return;
-    {
-        begin(m.seg[0]);
+    float o[TJ][NT][4], ref[NT][2], l[NT][2];
+    // Round by round: the segment before (`turn`) is finished while the loads of the one at hand (`next`) are under way. One copy of the
+    // code for the first segment and the later ones: code that runs for the first time waits for its instructions.
+    int turn = 2, next = 0;
+    for (bool first = true;; first = false) {
+        if (!first) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], w);
+                    if (g == 0) m.ml[warp][8 * n + 2 * t + r] = make_float2(ref[n][r], l[n][r]);
+                }
+            __syncthreads();            // all have read q
+        }
+        const bool go = m.go[next];
         uint4 raw[Q_TURNS];
-        q_load(m.seg[0], raw);
-        schedule(1);                    // while the first loads are under way
-        q_store(m.seg[0], raw);
-    }
-    __syncthreads();
-    for (int turn = 0;;) {
-        const int next = turn == 2 ? 0 : turn + 1;
+        if (go) {
+            begin(m.seg[next]);
+            q_load(m.seg[next], raw);
+        }
+        if (!first) {
+            // ---------------- the unit's result, or this CTA's part of it
+            const Segment& s = m.seg[turn];
+            const bool whole = s.part < 0;
+            const unsigned long long bad[kMaxNodes / 64] = {m.bad[0], m.bad[1], m.bad[2], m.bad[3]};
+            const bool any_bad = (bad[0] | bad[1] | bad[2] | bad[3]) != 0;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (n > 0) __syncthreads();
+                if (8 * n >= s.rows) break;
+                // this warp's share of its rows, relative to the rows' largest reference
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    float top = kNone4;
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, m.ml[w][8 * n + 2 * t + r].x);
+                    const float f = exp2_approx(ref[n][r] - top);
+                    float* to = m.join + (warp * 8 + 2 * t + r) * C::PITCH + g * 2;
+#pragma unroll
+                    for (int j = 0; j < TJ; ++j) *reinterpret_cast<float2*>(to + j * 16) = make_float2(o[j][n][r] * f, o[j][n][2 + r] * f);
+                }
+                __syncthreads();
+                // dimensions 2 u and 2 u + 1 of a row: lane group g = 2 u / PER, tile j = u % (PER / 2)
+                for (int i = tid; i < 8 * (D / 2); i += kThreads4) {
+                    const int r8 = i / (D / 2), u = i % (D / 2), r = 8 * n + r8, at = u % (C::PER / 2) * 16 + u / (C::PER / 2) * 2;
+                    if (r >= s.rows) break;
+                    float top = kNone4, sum = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, m.ml[w][r].x);
+                    float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        const float2 e = m.ml[w][r], y = *reinterpret_cast<const float2*>(m.join + (w * 8 + r8) * C::PITCH + at);
+                        sum = fmaf(e.y, exp2_approx(e.x - top), sum);
+                        v.x += y.x;
+                        v.y += y.y;
+                    }
+                    const int ur = s.row0 + r, nd = ur / a.group, hq = s.head * a.group + ur - nd * a.group;
+                    if (any_bad) {
+                        // what is not finite in a V that the row sees
+                        for (int k = 0; k < s.n; ++k) {
+                            if (!(m.bad[k >> 6] & sees_word(a, s.node0, s.n, nd, k >> 6) & 1ull << (k & 63))) continue;
+                            const int page = page_of(a, s.b, s.len + k);
+                            if (page < 0) continue;
+                            const long long row = ((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + k) & (a.page_size - 1));
+                            const uint16_t scale = reinterpret_cast<const uint16_t*>(a.v_scale)[row * G + 2 * u / kGroup4];
+                            if ((scale & 0x7f80u) == 0x7f80u) v.x = v.y = __uint_as_float(0x7fffffffu);
+                        }
+                    }
+                    const long long out = (long long)(s.node0 + nd) * a.n_heads + hq;
+                    if (whole) {
+                        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(v.x * inv, v.y * inv);
+                        reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(a.out) + out * D)[u] = b;
+                        if (u == 0 && a.lse) a.lse[out] = ((top == kNone4 ? -INFINITY : top) + log2f(sum)) * 0.69314718055994530942f;
+                    } else {
+                        *reinterpret_cast<float2*>(a.ws.part_o + ((long long)s.part * ROWS + r) * D + 2 * u) = v;
+                        if (u == 0) a.ws.part_ml[(long long)s.part * ROWS + r] = make_float2(top == kNone4 ? -INFINITY : top, sum);
+                    }
+                }
+            }
+        }
+        if (!go) break;
+        schedule(next == 2 ? 0 : next + 1);
+        if (!first) __syncthreads();    // bad and q are free
+        q_store(m.seg[next], raw);
+        __syncthreads();
+        turn = next;
+        next = next == 2 ? 0 : next + 1;
         const Segment& s = m.seg[turn];
         const int len = s.len, total = s.len + s.n, tile1 = s.tile1;
-        float o[TJ][NT][4], ref[NT][2], l[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -466,86 +545,6 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
             if (__builtin_expect(any_large, 0)) finish(std::true_type{});
             else finish(std::false_type{});
         }
-        // ---------------- the unit's result, or this CTA's part of it
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-#pragma unroll
-                for (int w = 4; w < 32; w <<= 1) l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], w);
-                if (g == 0) m.ml[warp][8 * n + 2 * t + r] = make_float2(ref[n][r], l[n][r]);
-            }
-        __syncthreads();                // all have read q
-        const bool go = m.go[next];
-        uint4 raw[Q_TURNS];
-        if (go) {
-            begin(m.seg[next]);
-            q_load(m.seg[next], raw);
-            schedule(next == 2 ? 0 : next + 1);
-        }
-        const bool whole = s.part < 0;
-        const unsigned long long bad[kMaxNodes / 64] = {m.bad[0], m.bad[1], m.bad[2], m.bad[3]};
-        const bool any_bad = (bad[0] | bad[1] | bad[2] | bad[3]) != 0;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (n > 0) __syncthreads();
-            if (8 * n >= s.rows) break;
-            // this warp's share of its rows, relative to the rows' largest reference
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float top = kNone4;
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) top = fmaxf(top, m.ml[w][8 * n + 2 * t + r].x);
-                const float f = exp2_approx(ref[n][r] - top);
-                float* to = m.join + (warp * 8 + 2 * t + r) * C::PITCH + g * 2;
-#pragma unroll
-                for (int j = 0; j < TJ; ++j) *reinterpret_cast<float2*>(to + j * 16) = make_float2(o[j][n][r] * f, o[j][n][2 + r] * f);
-            }
-            __syncthreads();
-            // dimensions 2 u and 2 u + 1 of a row: lane group g = 2 u / PER, tile j = u % (PER / 2)
-            for (int i = tid; i < 8 * (D / 2); i += kThreads4) {
-                const int r8 = i / (D / 2), u = i % (D / 2), r = 8 * n + r8, at = u % (C::PER / 2) * 16 + u / (C::PER / 2) * 2;
-                if (r >= s.rows) break;
-                float top = kNone4, sum = 0.f;
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) top = fmaxf(top, m.ml[w][r].x);
-                float2 v = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const float2 e = m.ml[w][r], y = *reinterpret_cast<const float2*>(m.join + (w * 8 + r8) * C::PITCH + at);
-                    sum = fmaf(e.y, exp2_approx(e.x - top), sum);
-                    v.x += y.x;
-                    v.y += y.y;
-                }
-                const int ur = s.row0 + r, nd = ur / a.group, hq = s.head * a.group + ur - nd * a.group;
-                if (any_bad) {
-                    // what is not finite in a V that the row sees
-                    for (int k = 0; k < s.n; ++k) {
-                        if (!(m.bad[k >> 6] & sees_word(a, s.node0, s.n, nd, k >> 6) & 1ull << (k & 63))) continue;
-                        const int page = page_of(a, s.b, s.len + k);
-                        if (page < 0) continue;
-                        const long long row = ((long long)page * a.kv_heads + s.head) * a.page_size + ((s.len + k) & (a.page_size - 1));
-                        const uint16_t scale = reinterpret_cast<const uint16_t*>(a.v_scale)[row * G + 2 * u / kGroup4];
-                        if ((scale & 0x7f80u) == 0x7f80u) v.x = v.y = __uint_as_float(0x7fffffffu);
-                    }
-                }
-                const long long out = (long long)(s.node0 + nd) * a.n_heads + hq;
-                if (whole) {
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    const __nv_bfloat162 b = __floats2bfloat162_rn(v.x * inv, v.y * inv);
-                    reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(a.out) + out * D)[u] = b;
-                    if (u == 0 && a.lse) a.lse[out] = ((top == kNone4 ? -INFINITY : top) + log2f(sum)) * 0.69314718055994530942f;
-                } else {
-                    *reinterpret_cast<float2*>(a.ws.part_o + ((long long)s.part * ROWS + r) * D + 2 * u) = v;
-                    if (u == 0) a.ws.part_ml[(long long)s.part * ROWS + r] = make_float2(top == kNone4 ? -INFINITY : top, sum);
-                }
-            }
-        }
-        if (!go) break;
-        __syncthreads();                // bad and q are free
-        q_store(m.seg[next], raw);
-        __syncthreads();
-        turn = next;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
 }

@@ -120,11 +120,16 @@ struct Work {
 
 struct Cursor {
     long long W, w, w_end, base;    // all work, this CTA's rest [w, w_end), work before request b
+    long long start;                // where the CTA's share begins
     int b, ctas;
 };
 
-__device__ __forceinline__ long long share_start(long long W, int c, int g) { return (long long)c * W / g; }
-__device__ __forceinline__ int share_of(long long W, long long w, int g) { return (int)(((w + 1) * g - 1) / W); }
+// a / b for a >= 0, b > 0: in 32 bits where both fit, as they mostly do (a 64-bit division takes ten times as long).
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
+__device__ __forceinline__ long long share_start(long long W, int c, int g) { return quotient((long long)c * W, g); }
+__device__ __forceinline__ int share_of(long long W, long long w, int g) { return (int)quotient((w + 1) * g - 1, W); }
 
 // By one converged warp: the CTA's share. False: nothing to do.
 template <int ROWS, int KEYS, int START>
@@ -138,7 +143,7 @@ __device__ bool cursor_init(const AttnArgs& a, int cta, int max_ctas, Cursor& c)
     c.W = total;
     c.ctas = (int)(total < max_ctas ? total : max_ctas);
     if (cta >= c.ctas) return false;
-    c.w = share_start(total, cta, c.ctas);
+    c.w = c.start = share_start(total, cta, c.ctas);
     c.w_end = share_start(total, cta + 1, c.ctas);
     long long base = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
@@ -161,25 +166,25 @@ __device__ bool cursor_init(const AttnArgs& a, int cta, int max_ctas, Cursor& c)
     return false;
 }
 
-// The next segment of the share. False: the share is done.
-template <int ROWS, int KEYS, int START>
-__device__ bool cursor_next(const AttnArgs& a, int cta, Cursor& c, Segment& s) {
+// The next segment of the share. False: the share is done. request(b): shape of request b.
+template <int ROWS, int KEYS, int START, typename Requests>
+__device__ bool cursor_next(const AttnArgs& a, int cta, Cursor& c, Segment& s, Requests request) {
     if (c.w >= c.w_end) return false;
-    Request r = request_of(a, c.b);
+    Request r = request(c.b);
     long long work = Work<ROWS, KEYS, START>::of(a, r);
     while (c.w >= c.base + work) {
         c.base += work;
-        r = request_of(a, ++c.b);
+        r = request(++c.b);
         work = Work<ROWS, KEYS, START>::of(a, r);
     }
     const int tiles = Work<ROWS, KEYS, START>::tiles(r), blocks = Work<ROWS, KEYS, START>::blocks(a, r);
-    const long long unit = (c.w - c.base) / (START + tiles);
+    const long long unit = quotient(c.w - c.base, START + tiles);
     const long long u0 = c.base + unit * (START + tiles) + START;      // place of its first tile
     if (c.w < u0) c.w = u0;
     if (c.w >= c.w_end) return false;
     s.b = c.b;
-    s.head = (int)(unit / blocks);
-    s.row0 = (int)(unit % blocks) * ROWS;
+    s.head = blocks == 1 ? (int)unit : (int)quotient(unit, blocks);
+    s.row0 = (int)(unit - (long long)s.head * blocks) * ROWS;
     s.rows = min(ROWS, r.n * a.group - s.row0);
     s.node0 = r.node0;
     s.len = r.len;
@@ -191,11 +196,75 @@ __device__ bool cursor_next(const AttnArgs& a, int cta, Cursor& c, Segment& s) {
         s.part = -1;
         s.first = s.last = cta;
     } else {
-        s.part = 2 * cta + (u0 < share_start(c.W, cta, c.ctas) ? 0 : 1);
-        s.first = share_of(c.W, u0, c.ctas);
-        s.last = share_of(c.W, u0 + tiles - 1, c.ctas);
+        s.part = 2 * cta + (u0 < c.start ? 0 : 1);
+        s.first = u0 < c.start ? share_of(c.W, u0, c.ctas) : cta;
+        s.last = u0 + tiles > c.w_end ? share_of(c.W, u0 + tiles - 1, c.ctas) : cta;
     }
     c.w += s.tile1 - s.tile0;
+    return true;
+}
+
+template <int ROWS, int KEYS, int START>
+__device__ bool cursor_next(const AttnArgs& a, int cta, Cursor& c, Segment& s) {
+    return cursor_next<ROWS, KEYS, START>(a, cta, c, s, [&](int b) { return request_of(a, b); });
+}
+
+// The same as cursor_init by a whole block, whose threads look at a request each: what the block needs of the first kTabled requests
+// stays in `table`, so that its segments are cut without another look at memory.
+constexpr int kTabled = 256;
+struct RequestTable {
+    Request request[kTabled];
+    long long sums[32];
+    long long base;
+    int b;
+};
+
+template <int ROWS, int KEYS, int START, int THREADS>
+__device__ __forceinline__ bool cursor_init_block(const AttnArgs& a, int cta, int max_ctas, Cursor& c, RequestTable& t) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto request = [&](int b) { return b < kTabled ? t.request[b] : request_of(a, b); };
+    long long total = 0;
+    for (int b = tid; b < a.B; b += THREADS) {
+        const Request r = request_of(a, b);
+        if (b < kTabled) t.request[b] = r;
+        total += Work<ROWS, KEYS, START>::of(a, r);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (lane == 0) t.sums[warp] = total;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) total += t.sums[w];
+    c.W = total;
+    c.ctas = (int)(total < max_ctas ? total : max_ctas);
+    if (cta >= c.ctas) return false;
+    c.w = c.start = share_start(total, cta, c.ctas);
+    c.w_end = share_start(total, cta + 1, c.ctas);
+    // the request in which the share begins
+    long long base = 0;
+    for (int b0 = 0; b0 < a.B && base <= c.w; b0 += THREADS) {
+        const int b = b0 + tid;
+        const long long mine = b < a.B ? Work<ROWS, KEYS, START>::of(a, request(b)) : 0;
+        long long sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
+        }
+        __syncthreads();                // the sums before are read
+        if (lane == 31) t.sums[warp] = sum;
+        __syncthreads();
+        long long before = base + sum - mine;
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < warp) before += t.sums[w];
+            base += t.sums[w];
+        }
+        if (before <= c.w && c.w < before + mine) t.base = before, t.b = b;
+    }
+    __syncthreads();
+    c.base = t.base;
+    c.b = t.b;
     return true;
 }
 
