@@ -69,19 +69,28 @@ __device__ __forceinline__ float int4_scale(float amax) {
     return fminf(fmaxf(s, 0x1p-126f), 1.125f * 0x1p125f);
 }
 
-// x / s rounded to nearest even, -7 .. 7, plus 8; inv = 1 / s. The product with inv may lie on the wrong side of a half, so the
-// remainder decides (exact: x is a whole number of its last place, at most 2 s away).
+// x / s rounded to nearest even, plus 8; inv is 1 / s or nearly so, and |x| at most 7 s (7.2 s where s is the largest). The product
+// with inv may lie on the wrong side of a half, so the remainder decides (exact: x is a whole number of its last place, at most s
+// away from q s): more than half of s, or half of it and q odd. Adding 1.5 * 2^23 + 8 rounds to a whole number, whose bits come last.
 __device__ __forceinline__ uint32_t int4_code(float x, float s, float inv) {
-    float q = rintf(x * inv);
-    const float r = fmaf(-q, s, x), half = 0.5f * s;
-    if (fabsf(r) > half || (fabsf(r) == half && (static_cast<int>(q) & 1))) q += copysignf(1.f, r);
-    return (uint32_t)(static_cast<int>(fminf(fmaxf(q, -7.f), 7.f)) + 8);
+    constexpr float kWhole = 12582912.f + 8.f;
+    float y = fmaf(x, inv, kWhole);
+    const float r = fmaf(kWhole - y, s, x);
+    const float most = __uint_as_float(__float_as_uint(0.5f * s) - (__float_as_uint(y) & 1u));
+    if (fabsf(r) > most) y += copysignf(1.f, r);
+    return __float_as_uint(y) & 15u;
 }
 
-// 8 codes times their scale (exact: 3 significant bits times 4).
+__device__ __forceinline__ float reciprocal_approx(float s) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return r;
+}
+
+// 8 codes times their scale (exact: 3 significant bits times 4). 2^23 + c is c in the last places of 2^23.
 __device__ __forceinline__ void int4x8_to_float(uint32_t w, float s, float (&f)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)(static_cast<int>(w >> (4 * i) & 15u) - 8) * s;
+    for (int i = 0; i < 8; ++i) f[i] = (__uint_as_float((w >> (4 * i) & 15u) | 0x4b000000u) - 8388616.f) * s;
 }
 
 __device__ __forceinline__ float float_of_bf16(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }

@@ -66,7 +66,7 @@ __device__ __forceinline__ void put_row(const RowArgs& p, int kv, long long row,
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const bool fine = top < 0x7f800000u;
-        const float s = int4_scale(fine ? __uint_as_float(top) : 0.f), inv = 1.f / s;
+        const float s = int4_scale(fine ? __uint_as_float(top) : 0.f), inv = reciprocal_approx(s);
         if (put) {
             uint32_t w = 0;
 #pragma unroll

@@ -5,9 +5,9 @@
 // 2^64 (one integer product) is the angle without its whole turns, as exact for far positions as for near ones: off by
 // 2^-54 f_i position of a turn for F_i's rounding, where an fp32 angle at position 10^6 is off by a thirtieth of a radian.
 // Its nearest quarter turn picks sign and place, and sine and cosine are taken of what is left, at most an eighth of a turn.
-// A block has the rows of 256 / LANES * kRowTurns neighbouring heads; sine and cosine of its tokens' pairs go into a table in
-// shared memory once, while the rows are under way. In layout "half" a pair's partner comes by shuffles where a row is a
-// whole number of lanes' shares, from memory elsewhere. Bound by memory.
+// LANES lanes take kRowTurns neighbouring heads of a token, 8 elements of a row each, so that a lane needs its pairs' sines and
+// cosines once. They come from a table of the block's tokens in shared memory, made while the rows are under way. In layout
+// "half" a pair's partner comes by shuffles where a row is a whole number of lanes' shares, from memory elsewhere. Bound by memory.
 #include <math.h>
 
 #include <new>
@@ -35,21 +35,12 @@ struct RopeArgs {
     void* dst[2];                       // q, k (kNoCache)
     long long dst_token[2], dst_head[2];
     int heads[3];
-    int per_token;                      // rows of a token
-    uint32_t rows;
+    int quads[3];                       // units of a token in each tensor: kRowTurns heads
+    uint32_t blocks[3], T;              // blocks of k, v and q, in this order
     const int32_t* positions;
     const uint64_t* turns;
     int rot, interleaved;
     float magnitude, sin_mul;           // sin_mul: the magnitude, its sign turned for gradients
-};
-
-struct RopeRow {
-    uint32_t token;
-    int j;                              // of the token's rows: q heads, then k, then v
-    __device__ __forceinline__ RopeRow(uint32_t r, uint32_t per) : token(r / per), j((int)(r - r / per * per)) {}
-    __device__ __forceinline__ void next(int per) {
-        if (++j == per) j = 0, ++token;
-    }
 };
 
 __device__ __forceinline__ float2 turned(uint64_t turn) {
@@ -73,21 +64,25 @@ __device__ __forceinline__ Raw8<T> round8(const float (&f)[8]) {
 template <typename T, int FMT, bool VEC, int LANES>
 __global__ void __launch_bounds__(kBlock) k_rope(const __grid_constant__ RopeArgs p) {
     extern __shared__ float2 table[];
-    const int D = p.cache.D, R = p.rot, sub = threadIdx.x % LANES, d0 = sub * 8;
+    constexpr uint32_t kUnits = kBlock / LANES;
+    const int D = p.cache.D, R = p.rot, pairs = R / 2, sub = threadIdx.x % LANES, d0 = sub * 8;
     const bool in = d0 < D;
-    constexpr uint32_t kRows = kBlock / LANES * kRowTurns;
-    const uint32_t r_block = blockIdx.x * kRows, r0 = r_block + threadIdx.x / LANES * kRowTurns;
+    // a block has units of one tensor: what is quantised first, as it takes longest
+    const int which = blockIdx.x < p.blocks[0] ? 1 : blockIdx.x < p.blocks[0] + p.blocks[1] ? 2 : 0;
+    const uint32_t block = blockIdx.x - (which == 1 ? 0 : which == 2 ? p.blocks[0] : p.blocks[0] + p.blocks[1]);
+    const uint32_t per = p.quads[which], units = p.T * per;
+    const uint32_t u_block = block * kUnits, u = u_block + threadIdx.x / LANES, token = u / per, token0 = u_block / per;
+    const int h0 = (int)(u - token * per) * kRowTurns, live = u < units ? min(p.heads[which] - h0, kRowTurns) : 0;      // heads of the unit
+    const long long head_stride = p.src_head[which];
+    const T* src = static_cast<const T*>(p.src[which]) + token * p.src_token[which] + h0 * head_stride;
     Raw8<T> raw[kRowTurns];
     Raw8<T> other[VEC ? 1 : kRowTurns];
-    RopeRow at(r0, p.per_token);
 #pragma unroll
-    for (int i = 0; i < kRowTurns; ++i, at.next(p.per_token)) {
+    for (int i = 0; i < kRowTurns; ++i) {
         raw[i] = Raw8<T>{};
         if constexpr (!VEC) other[i] = Raw8<T>{};
-        if (r0 + i >= p.rows || !in) continue;
-        const int which = at.j < p.heads[0] ? 0 : at.j < p.heads[0] + p.heads[1] ? 1 : 2;
-        const int h = at.j - (which > 0 ? p.heads[0] : 0) - (which > 1 ? p.heads[1] : 0);
-        const T* row = static_cast<const T*>(p.src[which]) + at.token * p.src_token[which] + h * p.src_head[which];
+        if (i >= live || !in) continue;
+        const T* row = src + i * head_stride;
         if constexpr (VEC) {
 #pragma unroll
             for (int w = 0; w < (int)sizeof(T) / 2; ++w) raw[i].w[w] = reinterpret_cast<const uint4*>(row + d0)[w];
@@ -98,25 +93,44 @@ __global__ void __launch_bounds__(kBlock) k_rope(const __grid_constant__ RopeArg
             for (int x = 0; x < 8; ++x) {
                 const int d = d0 + x;
                 e[x] = row[d];
-                if (!p.interleaved && d < R) o[x] = row[d < R / 2 ? d + R / 2 : d - R / 2];
+                if (!p.interleaved && d < R) o[x] = row[d < pairs ? d + pairs : d - pairs];
             }
         }
     }
-    // the table of the block's tokens
-    const uint32_t token0 = r_block / p.per_token, last = min(r_block + kRows, p.rows) - 1;
-    const int pairs = R / 2, entries = (int)(last / p.per_token - token0 + 1) * pairs;
+    // the table of the block's tokens; a lane's pairs, 4 or 8 on end, lie apart, so that lanes read neighbouring entries
+    const int shift = p.interleaved ? 2 : 3, low = (1 << shift) - 1, apart = pairs & low ? 0 : pairs >> shift;
+    const int entries = which == 2 ? 0 : (int)((min(u_block + kUnits, units) - 1) / per - token0 + 1) * pairs;
     for (int e = threadIdx.x; e < entries; e += kBlock) {
         const int t = e / pairs, i = e - t * pairs;
         const float2 c = turned((uint64_t)(int64_t)p.positions[token0 + t] * p.turns[i]);
-        table[e] = make_float2(c.x * p.magnitude, c.y * p.sin_mul);
+        table[t * pairs + (apart ? (i & low) * apart + (i >> shift) : i)] = make_float2(c.x * p.magnitude, c.y * p.sin_mul);
     }
     __syncthreads();
-    at = RopeRow(r0, p.per_token);
+    const bool turns = live > 0 && which < 2 && d0 < R;
+    const bool second = !p.interleaved && d0 >= pairs;      // VEC: the lane has its pairs' second elements
+    float2 cs[8];
 #pragma unroll
-    for (int i = 0; i < kRowTurns; ++i, at.next(p.per_token)) {
-        const bool live = r0 + i < p.rows;
-        const int which = at.j < p.heads[0] ? 0 : at.j < p.heads[0] + p.heads[1] ? 1 : 2;
-        const int h = at.j - (which > 0 ? p.heads[0] : 0) - (which > 1 ? p.heads[1] : 0);
+    for (int x = 0; x < 8; ++x) {
+        cs[x] = make_float2(1.f, 0.f);
+        if (!turns || (p.interleaved && x >= 4)) continue;
+        int i = p.interleaved ? d0 / 2 + x : d0 + x;
+        if (!p.interleaved && i >= pairs) i -= pairs;
+        if (i < pairs && (p.interleaved || d0 + x < R)) cs[x] = table[(token - token0) * pairs + (apart ? (i & low) * apart + (i >> shift) : i)];
+    }
+    long long slot = -1;
+    if constexpr (FMT != kNoCache) {
+        if (live > 0 && which > 0) slot = p.cache.slots[token];
+        if (slot >= p.cache.n_slots) {
+            if (sub == 0) atomicOr(p.cache.err, kErrIndex);
+            slot = -1;
+        }
+    }
+    const bool keeps = FMT != kNoCache && which > 0;
+    const int out = which == 1;
+    T* dst = static_cast<T*>(p.dst[out]) + token * p.dst_token[out] + h0 * p.dst_head[out];
+#pragma unroll
+    for (int i = 0; i < kRowTurns; ++i) {
+        if (!__any_sync(0xffffffffu, i < live)) break;
         float f[8], y[8];
         raw[i].to_float(f);
         if constexpr (VEC) {
@@ -135,25 +149,19 @@ __global__ void __launch_bounds__(kBlock) k_rope(const __grid_constant__ RopeArg
             other[i].to_float(y);
         }
         Raw8<T> result = raw[i];
-        if (live && which < 2 && d0 < R) {
-            const float2* c = table + (at.token - token0) * pairs;
+        if (turns) {
             if (p.interleaved) {
 #pragma unroll
                 for (int x = 0; x < 8; x += 2) {
-                    if (d0 + x >= R) break;
-                    const float2 k = c[(d0 + x) >> 1];
-                    const float u = f[x], w = f[x + 1];
-                    f[x] = fmaf(u, k.x, -__fmul_rn(w, k.y));
-                    f[x + 1] = fmaf(u, k.y, __fmul_rn(w, k.x));
+                    const float a = f[x], b = f[x + 1];
+                    f[x] = fmaf(a, cs[x / 2].x, -__fmul_rn(b, cs[x / 2].y));
+                    f[x + 1] = fmaf(a, cs[x / 2].y, __fmul_rn(b, cs[x / 2].x));
                 }
             } else {
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
-                    const int d = d0 + x;
-                    if (d >= R) break;
-                    const bool first = d < pairs;
-                    const float2 k = c[first ? d : d - pairs];
-                    f[x] = first ? fmaf(f[x], k.x, -__fmul_rn(y[x], k.y)) : fmaf(y[x], k.y, __fmul_rn(f[x], k.x));
+                    const bool upper = VEC ? second : d0 + x >= pairs;
+                    f[x] = upper ? fmaf(y[x], cs[x].y, __fmul_rn(f[x], cs[x].x)) : fmaf(f[x], cs[x].x, -__fmul_rn(y[x], cs[x].y));
                 }
             }
             const Raw8<T> z = round8<T>(f);
@@ -167,8 +175,8 @@ __global__ void __launch_bounds__(kBlock) k_rope(const __grid_constant__ RopeArg
                     if (d0 + x < R) o[x] = e[x];
             }
         }
-        if (live && in && (FMT == kNoCache || which == 0)) {
-            T* row = static_cast<T*>(p.dst[which == 1]) + at.token * p.dst_token[which == 1] + h * p.dst_head[which == 1];
+        if (i < live && in && (FMT == kNoCache || which == 0)) {
+            T* row = dst + i * p.dst_head[out];
             if constexpr (VEC) {
 #pragma unroll
                 for (int w = 0; w < (int)sizeof(T) / 2; ++w) reinterpret_cast<uint4*>(row + d0)[w] = result.w[w];
@@ -178,24 +186,24 @@ __global__ void __launch_bounds__(kBlock) k_rope(const __grid_constant__ RopeArg
                 for (int x = 0; x < 8; ++x) row[d0 + x] = e[x];
             }
         }
-        if constexpr (FMT != kNoCache) {
-            const bool kept = live && which > 0;
-            if (!__any_sync(0xffffffffu, kept)) continue;
-            long long slot = kept ? p.cache.slots[at.token] : -1;
-            if (slot >= p.cache.n_slots) {
-                if (sub == 0) atomicOr(p.cache.err, kErrIndex);
-                slot = -1;
-            }
-            put_row<T, FMT, LANES>(p.cache, which == 2, slot >= 0 ? pool_row(p.cache, slot, h) : 0, sub, in && slot >= 0, result);
-        }
+        if constexpr (FMT != kNoCache)
+            if (keeps)
+                put_row<T, FMT, LANES>(p.cache, which == 2, slot >= 0 && i < live ? pool_row(p.cache, slot, h0 + i) : 0, sub, in && slot >= 0 && i < live, result);
     }
 }
 
 template <typename T, int FMT, bool VEC, int LANES>
-cudaError_t run(const RopeArgs& p, cudaStream_t s) {
-    const uint32_t rows = kBlock / LANES * kRowTurns;
-    const uint32_t tokens = (rows - 1) / p.per_token + 2;        // that a block's rows may belong to
-    k_rope<T, FMT, VEC, LANES><<<(p.rows + rows - 1) / rows, kBlock, tokens * (p.rot / 2) * sizeof(float2), s>>>(p);
+cudaError_t run(RopeArgs p, cudaStream_t s) {
+    constexpr int kUnits = kBlock / LANES, kOrder[3] = {1, 2, 0};
+    uint32_t blocks = 0;
+    int least = INT32_MAX;
+    for (int i = 0; i < 3; ++i) {
+        p.quads[i] = (p.heads[i] + kRowTurns - 1) / kRowTurns;
+        if (p.quads[i] && i < 2 && p.quads[i] < least) least = p.quads[i];
+    }
+    for (int i = 0; i < 3; ++i) blocks += p.blocks[i] = (uint32_t)(((long long)p.T * p.quads[kOrder[i]] + kUnits - 1) / kUnits);
+    const size_t tokens = (kUnits - 1) / least + 2;              // that a block's units may belong to
+    k_rope<T, FMT, VEC, LANES><<<blocks, kBlock, tokens * (p.rot / 2) * sizeof(float2), s>>>(p);
     return cudaGetLastError();
 }
 
@@ -356,8 +364,7 @@ ace_status ace_rope_apply(const ace_rope* rope, int inverse, const int32_t* posi
     p.dst[0] = q_out, p.dst_token[0] = q_out_token_stride, p.dst_head[0] = q_out_head_stride;
     p.dst[1] = k_out, p.dst_token[1] = k_out_token_stride, p.dst_head[1] = k_out_head_stride;
     p.heads[0] = n_heads, p.heads[1] = n_kv_heads;
-    p.per_token = n_heads + n_kv_heads;
-    p.rows = (uint32_t)rows;
+    p.T = (uint32_t)T;
     of_rope(rope, inverse, positions, p);
     const cudaError_t e = run_type<kNoCache>(rope->desc.dtype, words(p, elem, true), p, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? ACE_OK : kv_cuda(e, "rope launch");
@@ -398,8 +405,7 @@ ace_status ace_kv_write_rotated(ace_kv* kv, int layer, const ace_rope* rope, con
     p.src[2] = v, p.src_token[2] = v_token_stride, p.src_head[2] = v_head_stride;
     p.dst[0] = q_out, p.dst_token[0] = q_out_token_stride, p.dst_head[0] = q_out_head_stride;
     p.heads[0] = n_heads, p.heads[1] = p.heads[2] = D.n_kv_heads;
-    p.per_token = n_heads + 2 * D.n_kv_heads;
-    p.rows = (uint32_t)rows;
+    p.T = (uint32_t)T;
     of_rope(rope, 0, positions, p);
     const bool vec = words(p, elem, false);
     const cudaError_t e = D.format == ACE_KV_INT4  ? run_type<ACE_KV_INT4>(D.dtype, vec, p, s)
