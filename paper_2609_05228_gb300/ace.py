@@ -512,10 +512,12 @@ def ace_verify_tree(logits, tokens, parents, node_offsets, max_nodes: int, unifo
 
 def _head_rows(name: str, t, dtype: str, T, heads, dim: int):
     """(token stride, head stride) of rows [T, heads, dim] of any strides but the last."""
-    _want(name, t, dtype, (T, heads, dim), False)
-    if t.numel() and t.stride(2) != 1:
-        raise ValueError(f"the last axis of {name} must be contiguous")
-    return t.stride(0), t.stride(1)
+    strides = t.stride()
+    if not (t.dtype is _dtype(dtype) and t.shape == (T, heads, dim) and strides[2] == 1 and t.is_cuda):
+        _want(name, t, dtype, (T, heads, dim), False)
+        if t.numel() and strides[2] != 1:
+            raise ValueError(f"the last axis of {name} must be contiguous")
+    return strides[0], strides[1]
 
 
 class AceRope:
@@ -542,18 +544,20 @@ class AceRope:
     def apply(self, positions, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
         """q [T, n_heads, head_dim] (and k) turned by `positions` [T] int32 into q_out (and k_out), which may be q (and k)
         themselves; `inverse`: the gradients of q and k from those of their results."""
-        T, heads = q.shape[0], q.shape[1]
+        T, heads, _ = q.shape
+        dt, dim = self._dt, self.head_dim
         _want("positions", positions, "int32", (T,))
-        qs = _head_rows("q", q, self._dt, T, heads, self.head_dim)
-        qo = _head_rows("q_out", q_out, self._dt, T, heads, self.head_dim)
-        ks, ko, kv_heads = (0, 0), (0, 0), 0
+        qs, qo = _head_rows("q", q, dt, T, heads, dim), _head_rows("q_out", q_out, dt, T, heads, dim)
         if (k is None) != (k_out is None):
             raise ValueError("k and k_out are given together")
-        if k is not None:
+        if k is None:
+            rest = (None, 0, 0, 0, None, 0, 0)
+        else:
             kv_heads = k.shape[1]
-            ks = _head_rows("k", k, self._dt, T, kv_heads, self.head_dim)
-            ko = _head_rows("k_out", k_out, self._dt, T, kv_heads, self.head_dim)
-        ace_rope_apply(self.handle, inverse, positions, T, q, *qs, heads, q_out, *qo, k, *ks, kv_heads, k_out, *ko, _stream_for(q, stream))
+            rest = (k.data_ptr(), *_head_rows("k", k, dt, T, kv_heads, dim), kv_heads, k_out.data_ptr(),
+                    *_head_rows("k_out", k_out, dt, T, kv_heads, dim))
+        _check(lib().ace_rope_apply(self.handle, int(inverse), positions.data_ptr(), T, q.data_ptr(), *qs, heads, q_out.data_ptr(), *qo, *rest,
+                                    _stream_for(q, stream)))
 
     def close(self) -> None:
         if getattr(self, "handle", None):
@@ -623,15 +627,14 @@ class AceKvCache:
     def write_rotated(self, layer: int, rope: AceRope, positions, q, q_out, k, v, slots, stream=None) -> None:
         """q [T, n_heads, head_dim] turned by `positions` [T] int32 into q_out (or in place), k turned and written to `slots` with v:
         rope.apply and write in one pass."""
-        T, heads = q.shape[0], q.shape[1]
-        qs, qo = self._rows("q", q, heads), _head_rows("q_out", q_out, self._dt, T, heads, self.head_dim)
-        ks, vs = self._rows("k", k, self.n_kv_heads), self._rows("v", v, self.n_kv_heads)
-        if k.shape[0] != T or v.shape[0] != T:
-            raise ValueError("q, k and v must have the same tokens")
+        T, heads, _ = q.shape
+        dt, dim, kv_heads = self._dt, self.head_dim, self.n_kv_heads
+        qs, qo = _head_rows("q", q, dt, T, heads, dim), _head_rows("q_out", q_out, dt, T, heads, dim)
+        ks, vs = _head_rows("k", k, dt, T, kv_heads, dim), _head_rows("v", v, dt, T, kv_heads, dim)
         _want("positions", positions, "int32", (T,))
         _want("slots", slots, "int64", (T,))
-        ace_kv_write_rotated(self.handle, layer, rope.handle, positions, q, *qs, heads, q_out, *qo, k, *ks, v, *vs, slots, T,
-                             _stream_for(q, stream))
+        _check(lib().ace_kv_write_rotated(self.handle, layer, rope.handle, positions.data_ptr(), q.data_ptr(), *qs, heads, q_out.data_ptr(), *qo,
+                                          k.data_ptr(), *ks, v.data_ptr(), *vs, slots.data_ptr(), T, _stream_for(q, stream)))
 
     def read(self, layer, slots, k_out, v_out, stream=None) -> None:
         """The rows at `slots` [T] to k_out, v_out [T, n_kv_heads, head_dim]; layer None: of all layers,

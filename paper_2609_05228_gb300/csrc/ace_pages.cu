@@ -167,16 +167,19 @@ struct Want {
     }
 };
 
-// One block; warps take requests in turn. Of a request that asks for n pages, need holds 2 n, and one more where the first of
-// them is a copy; then the sum of n over the requests before it.
+constexpr int kShort = 16;              // entries of a row that one thread looks through
+
+// One block: a thread a request where few entries are asked for, a warp where they are many (a prompt's). Of a request that asks for n
+// pages, need holds 2 n, and one more where the first of them is a copy; then, in place of n, its sum over the requests before it.
 __global__ void __launch_bounds__(kPlan) k_reserve(const __grid_constant__ ReserveArgs p) {
     __shared__ int need[kPlanRows];
-    __shared__ int sums[33], moves;
+    __shared__ int sums[33], moves, any_long;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int* holders = p.ws.mark;           // requests that grow in a page
     int* last = p.ws.mark + p.n_pages;  // the last of them, + 1
     bool bad = false;
-    if (tid == 0) moves = 0;
+    if (tid == 0) moves = any_long = 0;
+    __syncthreads();
     Want w;
     for (int b = tid; b < p.B; b += kPlan) {
         if (!w.of(p, b)) bad = true;
@@ -184,24 +187,44 @@ __global__ void __launch_bounds__(kPlan) k_reserve(const __grid_constant__ Reser
             atomicAdd(&holders[w.part], 1);
             atomicMax(&last[w.part], b + 1);
         }
+        int n = -1;
+        if (w.end - w.first <= kShort) {
+            n = 0;
+            for (int i = w.first; i < w.end; ++i) {
+                const int page = p.table[(long long)b * p.max_pages + i];
+                n += page < 0;
+                bad = bad || page >= p.n_pages;
+            }
+        } else {
+            any_long = 1;
+        }
+        need[b] = n;
     }
+    __syncthreads();
+    if (any_long)
+        for (int b = warp; b < p.B; b += kPlan / 32) {
+            if (need[b] >= 0) continue;
+            w.of(p, b);
+            int n = 0;
+            for (int i = w.first + lane; i < w.end; i += 32) {
+                const int page = p.table[(long long)b * p.max_pages + i];
+                n += page < 0;
+                bad = bad || page >= p.n_pages;
+            }
+            n = warp_sum_int(n);
+            __syncwarp();
+            if (lane == 0) need[b] = n;
+        }
     if (bad) atomicOr(p.err, kErrIndex);
     __syncthreads();
-    for (int b = warp; b < p.B; b += kPlan / 32) {
+    for (int b = tid; b < p.B; b += kPlan) {
         w.of(p, b);
-        int n = 0;
-        for (int i = w.first + lane; i < w.end; i += 32) {
-            const int page = p.table[(long long)b * p.max_pages + i];
-            n += page < 0;
-            if (page >= p.n_pages) atomicOr(p.err, kErrIndex);
-        }
-        n = warp_sum_int(n);
         int copy = 0;
         if (w.part >= 0) {
             const int refs = p.refs[w.part];
             copy = refs > 1 && !(__ldcg(&holders[w.part]) == refs && __ldcg(&last[w.part]) == b + 1);
         }
-        if (lane == 0) need[b] = 2 * (n + copy) + copy;
+        need[b] = 2 * (need[b] + copy) + copy;
     }
     __syncthreads();
     int total = 0;
@@ -222,31 +245,50 @@ __global__ void __launch_bounds__(kPlan) k_reserve(const __grid_constant__ Reser
     __syncthreads();
     const bool enough = found >= total;
     if (tid == 0) *p.missing = enough ? 0 : total - found;
-    for (int b = warp; b < p.B; b += kPlan / 32) {
-        w.of(p, b);
-        if (w.part >= 0 && lane == 0) holders[w.part] = last[w.part] = 0;
-        if (!enough) continue;
+    // a request's fresh pages into its row; by one thread, or by a warp
+    auto give = [&](int b, bool by_warp) {
         int32_t* row = p.table + (long long)b * p.max_pages;
         int at = need[b] >> 1;
         const bool copy = need[b] & 1;
         const int fresh = copy ? __ldcg(&p.ws.list[at++]) : -1;
-        for (int i0 = w.first; i0 < w.end; i0 += 32) {
-            const int i = i0 + lane;
-            const bool none = i < w.end && row[i] < 0;
-            const unsigned word = __ballot_sync(0xffffffffu, none);
-            if (none) {
-                const int page = __ldcg(&p.ws.list[at + __popc(word & lanemask_lt())]);
-                row[i] = page;
-                p.refs[page] = 1;
+        if (by_warp) {
+            for (int i0 = w.first; i0 < w.end; i0 += 32) {
+                const int i = i0 + lane;
+                const bool none = i < w.end && row[i] < 0;
+                const unsigned word = __ballot_sync(0xffffffffu, none);
+                if (none) {
+                    const int page = __ldcg(&p.ws.list[at + __popc(word & lanemask_lt())]);
+                    row[i] = page;
+                    p.refs[page] = 1;
+                }
+                at += __popc(word);
             }
-            at += __popc(word);
+            __syncwarp();               // all lanes have read the row's partly filled page
+        } else {
+            for (int i = w.first; i < w.end; ++i)
+                if (row[i] < 0) {
+                    const int page = __ldcg(&p.ws.list[at++]);
+                    row[i] = page;
+                    p.refs[page] = 1;
+                }
         }
-        __syncwarp();                   // all lanes have read the row's partly filled page
-        if (copy && lane == 0) {
+        if (copy && (!by_warp || lane == 0)) {
             row[w.first - 1] = fresh;
             p.refs[fresh] = 1;
             atomicSub(&p.refs[w.part], 1);
             p.ws.move[atomicAdd(&moves, 1)] = make_int3(w.part, fresh, p.lens[b] & ((1 << p.page_shift) - 1));
+        }
+    };
+    for (int b = tid; b < p.B; b += kPlan) {
+        w.of(p, b);
+        if (w.part >= 0) holders[w.part] = last[w.part] = 0;
+        if (enough && w.end - w.first <= kShort) give(b, false);
+    }
+    if (any_long && enough) {
+        __syncthreads();                // marks are cleared by rows as they were
+        for (int b = warp; b < p.B; b += kPlan / 32) {
+            w.of(p, b);
+            if (w.end - w.first > kShort) give(b, true);
         }
     }
     __syncthreads();
@@ -330,9 +372,9 @@ __global__ void __launch_bounds__(kPlan) k_copy_plan(const __grid_constant__ Cop
 }
 
 struct MoveArgs {
-    uint8_t* pool[4];                   // K, V, their scales
-    int row[4];                         // bytes of a row in each
-    int pools, layers, H, page_size, n_pages;
+    uint8_t *pool[2], *scale[2];        // K and V
+    int row, scale_row;                 // bytes of a row and its scales
+    int layers, H, page_size, n_pages;
     PageWorkspace ws;
     // compaction: the tables follow
     int32_t* table;
@@ -341,11 +383,19 @@ struct MoveArgs {
     int* err;
 };
 
-constexpr int kMoveWords = 8;           // 16-byte words a lane has under way
+constexpr int kMoveWords = 8;           // 16-byte words of a lane's rows that are under way together
 
-// By one warp: `bytes` from src to dst, both 16-byte aligned.
-__device__ __forceinline__ void copy_bytes(uint8_t* dst, const uint8_t* src, int bytes) {
+// By one warp: what is left of `bytes` behind whole words of 16.
+__device__ __forceinline__ void copy_tail(uint8_t* dst, const uint8_t* src, int bytes) {
     const int lane = threadIdx.x & 31, words = bytes >> 4;
+    if (lane < (bytes & 15)) dst[words * 16 + lane] = src[words * 16 + lane];
+}
+
+// By one warp: `bytes` from src to dst, and `bytes2` from src2 to dst2 (all 16-byte aligned), the first words of both together.
+__device__ __forceinline__ void copy_rows(uint8_t* dst, const uint8_t* src, int bytes, uint8_t* dst2, const uint8_t* src2, int bytes2) {
+    const int lane = threadIdx.x & 31, words = bytes >> 4, words2 = bytes2 >> 4;
+    uint4 u;
+    if (lane < words2) u = __ldcs(reinterpret_cast<const uint4*>(src2) + lane);
     for (int w0 = 0; w0 < words; w0 += 32 * kMoveWords) {
         uint4 v[kMoveWords];
 #pragma unroll
@@ -359,7 +409,10 @@ __device__ __forceinline__ void copy_bytes(uint8_t* dst, const uint8_t* src, int
             if (w < words) __stcs(reinterpret_cast<uint4*>(dst) + w, v[i]);
         }
     }
-    if (lane < (bytes & 15)) dst[words * 16 + lane] = src[words * 16 + lane];
+    if (lane < words2) __stcs(reinterpret_cast<uint4*>(dst2) + lane, u);
+    for (int w = 32 + lane; w < words2; w += 32) __stcs(reinterpret_cast<uint4*>(dst2) + w, __ldcs(reinterpret_cast<const uint4*>(src2) + w));
+    copy_tail(dst, src, bytes);
+    copy_tail(dst2, src2, bytes2);
 }
 
 __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveArgs p) {
@@ -378,19 +431,18 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveArgs p
         if (p.new_page)
             for (long long i = tid; i < p.n_pages; i += threads) p.new_page[i] = p.ws.list[i];
     }
-    // a warp a (move, layer, pool, head)
-    const int per_move = p.layers * p.pools * p.H;
+    // a warp a (move, layer, K or V, head): its rows and their scales
+    const int per_move = p.layers * 2 * p.H;
     const long long all = (long long)*p.ws.count * per_move;
     for (long long i = tid >> 5; i < all; i += threads >> 5) {
-        const int3 m = p.ws.move[i / per_move];
-        const int rest = (int)(i % per_move), h = rest % p.H, which = rest / p.H % p.pools, layer = rest / p.H / p.pools;
-        int row = p.row[0];
-        uint8_t* pool = p.pool[0];
-#pragma unroll
-        for (int k = 1; k < 4; ++k)
-            if (which == k) row = p.row[k], pool = p.pool[k];
-        const long long head = (long long)p.page_size * row, page = head * p.H, at = (long long)layer * p.n_pages * page + h * head;
-        copy_bytes(pool + at + m.y * page, pool + at + m.x * page, m.z * row);
+        const long long n = (i | per_move) >> 32 ? i / per_move : (uint32_t)i / (uint32_t)per_move;
+        const int3 m = p.ws.move[n];
+        const int rest = (int)(i - n * per_move), lk = rest / p.H, h = rest - lk * p.H;
+        // first rows of the head in the two pages
+        const long long to = (((lk >> 1) * (long long)p.n_pages + m.y) * p.H + h) * p.page_size, from = (((lk >> 1) * (long long)p.n_pages + m.x) * p.H + h) * p.page_size;
+        uint8_t* pool = lk & 1 ? p.pool[1] : p.pool[0];
+        uint8_t* scale = lk & 1 ? p.scale[1] : p.scale[0];
+        copy_rows(pool + to * p.row, pool + from * p.row, m.z * p.row, scale + to * p.scale_row, scale + from * p.scale_row, m.z * p.scale_row);
     }
 }
 
@@ -399,11 +451,10 @@ ace_status pages_fail(const char* m) { return kv_fail(ACE_ERR_INVALID_ARG, m); }
 // Moves what the plan before on the stream lists.
 ace_status launch_moves(const ace_kv* kv, MoveArgs p, cudaStream_t s) {
     const ace_kv_desc& D = kv->desc;
-    const int row = row_bytes(D.format, D.head_dim, kv->elem), scale = scale_bytes(D.format, D.head_dim);
+    p.row = row_bytes(D.format, D.head_dim, kv->elem);
+    p.scale_row = scale_bytes(D.format, D.head_dim);
     p.pool[0] = static_cast<uint8_t*>(kv->k_pool), p.pool[1] = static_cast<uint8_t*>(kv->v_pool);
-    p.pool[2] = kv->k_scale, p.pool[3] = kv->v_scale;
-    p.row[0] = p.row[1] = row, p.row[2] = p.row[3] = scale;
-    p.pools = scale ? 4 : 2;
+    p.scale[0] = kv->k_scale, p.scale[1] = kv->v_scale;
     p.layers = D.layers, p.H = D.n_kv_heads, p.page_size = D.page_size, p.n_pages = D.n_pages;
     p.ws = kv->pages;
     p.err = kv->err;
