@@ -64,7 +64,7 @@ struct Misc : TcShared {
     uint2 vf[FP8 ? kAuxRing : 1][32];           // the same as fp16
 };
 
-// 4-bit caches have a fifth warpgroup: V's tiles, beside K's. Registers go from the first one, which issues and schedules, to the
+// 4-bit caches have a fifth group of four warps: V's tiles, beside K's. Registers go from the first one, which issues and schedules, to the
 // softmax: 640 threads are launched with 96 each, 61440, and 128 (56 + 2 * 128 + 2 * 80) = 60416 are in use.
 constexpr int tc_threads(bool i4) { return i4 ? 640 : kTcThreads; }
 template <int N>
@@ -144,20 +144,27 @@ __device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, flo
     return (a + b) + (c + d);
 }
 
-// Four warps, caches in 4 bits: tiles of K (V = false) or V as the products take them. A row's group of 32 codes is a lane's 16 bytes, 8
+// Four warps, caches in 4 bits: tiles of K or of V as the products take them (both by one copy of the code, which is as long as the
+// instruction cache bears). A row's group of 32 codes is a lane's 16 bytes, 8
 // or 16 rows a turn, so that a warp reads 512 bytes on end; loaded a tile ahead, their pages two. (s: the tile's segment.)
-template <int D, bool V>
+template <int D>
 struct Codes4 {
     static constexpr int CH = D / kGroup4, ROWS = 32 / CH, TURNS = 32 / ROWS;       // groups of a row; rows of a turn; turns of a warp's 32 rows
     const AttnArgs& a;
     const Segment& s;
+    bool of_v;
+    const uint8_t* pool;                // the lane's group of the head's first row, and its scale
+    const uint16_t* scales;
     int row0, lane;                     // the warp's first row of a tile
     int page[2];                        // of its runs of 16 rows
     uint4 code[TURNS];
     uint16_t scale[TURNS];
 
-    __device__ __forceinline__ const uint8_t* pool() const { return static_cast<const uint8_t*>(V ? a.v_pool : a.k_pool); }
-    __device__ __forceinline__ const uint8_t* scales() const { return V ? a.v_scale : a.k_scale; }
+    __device__ __forceinline__ Codes4(const AttnArgs& a_, const Segment& s_, bool v, int row, int lane_) : a(a_), s(s_), of_v(v), row0(row), lane(lane_) {
+        const long long head = (long long)s.head * a.page_size * CH + lane / ROWS;
+        pool = static_cast<const uint8_t*>(of_v ? a.v_pool : a.k_pool) + head * 16;
+        scales = reinterpret_cast<const uint16_t*>(of_v ? a.v_scale : a.k_scale) + head;
+    }
     __device__ __forceinline__ void look_up(int t) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -170,23 +177,24 @@ struct Codes4 {
         constexpr int LINE = 256 / D;   // rows of a line
         const int r = lane * LINE, pg = r < 16 ? page[0] : page[1];
         if (r < 32 && pg >= 0) {
-            const long long row = (long long)(pg * a.kv_heads + s.head) * a.page_size + ((t * kTcKeys + row0 + r) & (a.page_size - 1));
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(pool() + row * (D / 2)));
-            if (r % 16 == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(scales() + row * (2 * CH)));
+            // (the lane's group of these rows: the line that it lies in)
+            const long long at = (long long)(pg * (a.kv_heads * a.page_size) + ((t * kTcKeys + row0 + r) & (a.page_size - 1))) * CH;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(pool + at * 16));
+            if (r % 16 == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(scales + at));
         }
     }
     // The codes of tile t, whose pages have been looked up.
     __device__ __forceinline__ void load(int t) {
-        const int total = s.len + s.n;
+        const int left = s.len + s.n - t * kTcKeys - row0;      // of the warp's rows
 #pragma unroll
         for (int i = 0; i < TURNS; ++i) {
-            const int pos = t * kTcKeys + row0 + i * ROWS + lane % ROWS, c = lane / ROWS, pg = page[i * ROWS / 16];
+            const int r = i * ROWS + lane % ROWS, pg = page[i * ROWS / 16];
             code[i] = make_uint4(0, 0, 0, 0);
             scale[i] = 0;
-            if (pg >= 0 && pos < total) {
-                const long long row = (long long)(pg * a.kv_heads + s.head) * a.page_size + (pos & (a.page_size - 1));
-                code[i] = ld_stream(pool() + row * (D / 2) + c * 16);
-                scale[i] = __ldg(reinterpret_cast<const uint16_t*>(scales()) + row * CH + c);
+            if (pg >= 0 && r < left) {
+                const long long at = (long long)(pg * (a.kv_heads * a.page_size) + ((t * kTcKeys + row0 + r) & (a.page_size - 1))) * CH;
+                code[i] = ld_stream(pool + at * 16);
+                scale[i] = __ldg(scales + at);
             }
         }
     }
@@ -212,7 +220,7 @@ struct Codes4 {
         bool large = false;
 #pragma unroll
         for (int i = 0; i < TURNS; ++i) {
-            if (V && t * kTcKeys + kTcKeys > s.len) {
+            if (of_v && t * kTcKeys + kTcKeys > s.len) {
                 const int nd = t * kTcKeys + row0 + lane % ROWS + i * ROWS - s.len;
                 if (nd >= 0 && (scale[i] & 0x7f80u) == 0x7f80u) {
                     scale[i] = 0;
@@ -355,33 +363,7 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
     const uint32_t tmem = m.tmem;                       // four buffers of S, O0, O1
     constexpr uint32_t kO = 256;
     Walk walk{m, a, {}};
-    if (I4 && warp >= 16) {
-        // ------------------------------------------------ tiles of V (4 bits)
-        if constexpr (I4) {
-            fewer_registers<80>();
-            Ring rv;
-            bool ok = true;
-            while (ok && walk.next()) {
-                const Segment& s = walk.segment();
-                unsigned long long* bad = m.seg[walk.seg.i].bad;
-                Codes4<D, true> codes{a, s, (warp - 16) * 32, lane};
-                codes.begin();
-                for (int t = s.tile0; t < s.tile1; ++t) {
-                    codes.ask(t + 1);
-                    if (!mbar_wait_warp(&m.v_empty[rv.i], rv.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
-                    codes.store(smem + C::OFF_V + rv.i * C::TILE, t, bad);
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&m.v_ready[rv.i]);
-                    rv.next<NV>();
-                    codes.load(t + 1);
-                    codes.look_up(t + 2);
-                }
-                if (ok) walk.done();
-            }
-            if (!ok) *abort_flag = 1;
-        }
-    } else if (warp < 4) {
+    if (warp < 4) {
         if constexpr (I4) fewer_registers<56>();
         if (warp == 0) {
             if constexpr (I4) {
@@ -472,22 +454,24 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
             __syncwarp();
         }
     } else if (warp >= 12) {
-        // ------------------------------------------------ q rows, and V tiles (4 bits: K tiles) made ready
+        // ------------------------------------------------ q rows, and V tiles made ready; 4 bits: tiles of K, and of V by warps 16 to 19
         if constexpr (I4) fewer_registers<80>();
-        const int tid = threadIdx.x - 384;
-        Ring rk, rv, rc, ra;
+        const bool of_v = I4 && warp >= 16;
+        const int tid = threadIdx.x - (of_v ? 512 : 384);
+        Ring rv, rc, ra;
         uint32_t q_phase = 1;           // the first segment's q buffer is free
         bool ok = true;
         while (ok && walk.next()) {
             const Segment& s = walk.segment();
-            Codes4<D, false> codes{a, s, tid >> 5 << 5, lane};
+            Codes4<D> codes(a, s, of_v, tid >> 5 << 5, lane);
             if constexpr (I4) codes.begin();
+            const int q_rows = of_v ? 0 : s.rows;
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
             constexpr int kChunks = D / 8;              // 8 elements a thread, a row's threads side by side
             constexpr int kStep = 128 / kChunks, kBatch = 4;        // rows a pass; passes whose loads are under way together
             constexpr int apart = 128 / CP;
             // (rows of the block past the unit's keep what they hold: rows of S, P and O do not mix)
-            for (int b0 = 0; b0 < s.rows; b0 += kStep * kBatch) {
+            for (int b0 = 0; b0 < q_rows; b0 += kStep * kBatch) {
                 uint4 qv[kBatch];
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
@@ -548,21 +532,23 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
                 }
             }
             if (!ok) break;
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&m.q_full);
+            if (!of_v) {
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&m.q_full);
+            }
             unsigned long long* bad = m.seg[walk.seg.i].bad;
             for (int t = s.tile0; t < s.tile1; ++t) {
                 const int pos0 = t * kTcKeys;
                 const bool drafted = pos0 + kTcKeys > s.len;    // rows that not every node sees, or past the end
                 if constexpr (I4) {
                     codes.ask(t + 1);
-                    if (!mbar_wait_warp(&m.k_empty[rk.i], rk.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
-                    codes.store(smem + C::OFF_K + rk.i * C::TILE, t, bad);
+                    if (!mbar_wait_warp(of_v ? &m.v_empty[rv.i] : &m.k_empty[rv.i], rv.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
+                    codes.store(smem + (of_v ? C::OFF_V : C::OFF_K) + rv.i * C::TILE, t, bad);
                     fence_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&m.k_full[rk.i]);
-                    rk.next<NK>();
+                    if (lane == 0) mbar_arrive(of_v ? &m.v_ready[rv.i] : &m.k_full[rv.i]);
+                    if (++rv.i == (of_v ? NV : NK)) rv.i = 0, rv.phase ^= 1u;
                     codes.load(t + 1);
                     codes.look_up(t + 2);
                     continue;
