@@ -27,6 +27,8 @@
 // N = 64 makes scores read the q rows from shared memory at its full rate), fp8 also by the conversion of V.
 #include <cudaTypedefs.h>
 
+#include <type_traits>
+
 #include "ace_attn_tc.cuh"
 
 namespace ace {
@@ -65,7 +67,7 @@ struct Misc : TcShared {
 };
 
 // 4-bit caches have a fifth group of four warps: V's tiles, beside K's. Registers go from the first one, which issues and schedules, to the
-// softmax: 640 threads are launched with 96 each, 61440, and 128 (56 + 2 * 128 + 2 * 80) = 60416 are in use.
+// softmax: 640 threads are launched with 96 each, 61440, and 128 (64 + 2 * 120 + 2 * 80) = 59392 are in use.
 constexpr int tc_threads(bool i4) { return i4 ? 640 : kTcThreads; }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -250,6 +252,10 @@ struct Codes4 {
     }
 };
 
+struct NoCodes {
+    __device__ __forceinline__ NoCodes(const AttnArgs&, const Segment&, bool, int, int) {}
+};
+
 // Column of O, of 16 that begin with a multiple of 16, that has dimension i.
 template <bool I4>
 __device__ __forceinline__ constexpr int column_of(int i) { return I4 ? (i & 8) + (i & 3) * 2 + (i >> 2 & 1) : i; }
@@ -314,6 +320,91 @@ __device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
     return *reinterpret_cast<const uint32_t*>(&z);
 }
 
+// MMA issuers, a warp a softmax group g.
+template <bool FP8, int D, int RT, int CP>
+__device__ __forceinline__ void role_issue(Misc<FP8, RT>& m, const AttnArgs& a, unsigned char* smem, uint32_t tmem, int g) {
+    using C = Cfg<FP8, D, RT, CP>;
+    constexpr int NK = C::NK, NV = C::NV, NC = C::NC;
+    constexpr uint32_t kO = 256;
+    volatile int* abort_flag = &m.abort_flag;
+    Walk walk{m, a, {}};
+    if (elect_one()) {
+        Ring rk, rv;                        // rv: V's ring, as stored (plain) or as fp16 (fp8)
+        constexpr int NP = FP8 ? NC : NV, kVTile = FP8 ? C::CONV : C::TILE;
+        uint64_t* v_free = FP8 ? m.c_empty : m.v_empty;
+        uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit n & 1 of the group's two S buffers
+        const uint32_t q0 = desc_lo(smem_u32(smem + (RT == 2 ? g * C::Q : 0)), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
+        const uint32_t v0 = desc_lo(smem_u32(smem + (FP8 ? C::OFF_C : C::OFF_V)), kVBlock);
+        const uint32_t o = tmem + kO + (uint32_t)(g * D);
+        bool ok = true;
+        while (true) {
+            if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
+            if (!m.seg[walk.seg.i].go) break;
+            const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * RT;        // the group's
+            mbar_arrive(&m.seg_empty[walk.seg.i]);
+            walk.seg.next<kSegRing>();
+            if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
+            q_phase ^= 1u;
+            for (int n = 0; n <= items; ++n) {
+                if (n < items) {
+                    // S of item n = Q K^T; the product that read P from this buffer (item n - 2) was issued before
+                    const int half = RT == 2 ? n & 1 : g, buf = (n & 1) * 2 + g;
+                    if (n % RT == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t d = tmem + (uint32_t)(buf * kHalf);
+                    const uint32_t kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4) + half * (kHalf * (FP8 ? D : 128) >> 4));
+                    if constexpr (FP8) {
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
+                            const uint32_t st = kk % (D / 32) * 2;
+                            mma_ss<true>(d, q0 + (kk < D / 32 ? 0 : C::Q >> 5) + st, kl + st, D == 128 ? kRows128 : kRows64,
+                                         idesc_of(0, 128, kHalf, false), kk > 0);
+                        }
+                    } else {
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const uint32_t st = (kk >> 2) * (16384 >> 4) + (kk & 3) * 2;
+                            mma_ss<false>(d, q0 + st, kl + st, kRows128, idesc_of(1, 128, kHalf, false), kk > 0);
+                        }
+                    }
+                    mma_commit(&m.s_full[buf]);
+                    if (n % RT == RT - 1) {
+                        mma_commit(&m.k_empty[rk.i]);
+                        rk.next<NK>();
+                    }
+                    if (n == items - 1) mma_commit(&m.q_free);
+                }
+                if (n > 0) {
+                    // O += P V of item j = n - 1
+                    const int j = n - 1, half = RT == 2 ? j & 1 : g, buf = (j & 1) * 2 + g;
+                    if (!mbar_wait_or_abort(&m.p_ready[buf], p_phase >> (j & 1) & 1u, a.err, abort_flag)) { ok = false; break; }
+                    p_phase ^= 1u << (j & 1);
+                    if (j % RT == 0 && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t vl = v0 + (uint32_t)(rv.i * (kVTile >> 4) + half * (kHalf * 128 >> 4));
+                    const uint32_t pa = tmem + (uint32_t)(buf * kHalf);
+#pragma unroll
+                    for (int kk = 0; kk < kHalf / 16; ++kk)
+                        mma_ts(o, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j > 0 || kk > 0);
+                    mma_commit(&m.o_done[buf]);
+                    if (j % RT == RT - 1) {
+                        mma_commit(&v_free[rv.i]);
+                        rv.next<NP>();
+                    }
+                }
+            }
+            if (!ok) break;
+        }
+        if (!ok) *abort_flag = 1;
+        if (*abort_flag) {
+            // products in flight read shared memory and TMEM
+            mma_commit(&m.drain[g]);
+            mbar_wait(&m.drain[g], 0, a.err);
+        }
+    }
+    __syncwarp();
+}
+
 // CP = 2 (at most 64 rows): the block holds them twice, 64 lanes apart, and each copy's warps take half of a tile's
 // columns: the tile's softmax takes half the time, and the copies' O are added at the end.
 template <bool FP8, bool I4, int D, int RT, int CP>
@@ -363,96 +454,19 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
     const uint32_t tmem = m.tmem;                       // four buffers of S, O0, O1
     constexpr uint32_t kO = 256;
     Walk walk{m, a, {}};
-    if (warp < 4) {
-        if constexpr (I4) fewer_registers<56>();
-        if (warp == 0) {
-            if constexpr (I4) {
-                role_schedule<ROWS, kTcStart>(m, a);
-            } else {
-                Scheduler<ROWS, kTcStart> sched(m, a);                // a segment ahead of the loads
-                if (sched.publish()) role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [&] { return sched.publish(); });
-            }
-        } else if (warp == 2) {
-            if constexpr (FP8) role_scales<kTcRoom>(m, a, m.kf, m.vf);
-        } else {
-            // ------------------------------------------------ MMA issuers, one a softmax group
-            if (elect_one()) {
-                const int g = warp >> 1;
-                Ring rk, rv;                        // rv: V's ring, as stored (plain) or as fp16 (fp8)
-                constexpr int NP = FP8 ? NC : NV, kVTile = FP8 ? C::CONV : C::TILE;
-                uint64_t* v_free = FP8 ? m.c_empty : m.v_empty;
-                uint32_t q_phase = 0, p_phase = 0;  // p_phase: bit n & 1 of the group's two S buffers
-                const uint32_t q0 = desc_lo(smem_u32(smem + (RT == 2 ? g * C::Q : 0)), 0), k0 = desc_lo(smem_u32(smem + C::OFF_K), 0);
-                const uint32_t v0 = desc_lo(smem_u32(smem + (FP8 ? C::OFF_C : C::OFF_V)), kVBlock);
-                const uint32_t o = tmem + kO + (uint32_t)(g * D);
-                bool ok = true;
-                while (true) {
-                    if (!mbar_wait_or_abort(&m.seg_full[walk.seg.i], walk.seg.phase, a.err, abort_flag)) { ok = false; break; }
-                    if (!m.seg[walk.seg.i].go) break;
-                    const int items = (m.seg[walk.seg.i].s.tile1 - m.seg[walk.seg.i].s.tile0) * RT;        // the group's
-                    mbar_arrive(&m.seg_empty[walk.seg.i]);
-                    walk.seg.next<kSegRing>();
-                    if (!mbar_wait_or_abort(&m.q_full, q_phase, a.err, abort_flag)) { ok = false; break; }
-                    q_phase ^= 1u;
-                    for (int n = 0; n <= items; ++n) {
-                        if (n < items) {
-                            // S of item n = Q K^T; the product that read P from this buffer (item n - 2) was issued before
-                            const int half = RT == 2 ? n & 1 : g, buf = (n & 1) * 2 + g;
-                            if (n % RT == 0 && !mbar_wait_or_abort(&m.k_full[rk.i], rk.phase, a.err, abort_flag)) { ok = false; break; }
-                            tc_fence_after();
-                            const uint32_t d = tmem + (uint32_t)(buf * kHalf);
-                            const uint32_t kl = k0 + (uint32_t)(rk.i * (C::TILE >> 4) + half * (kHalf * (FP8 ? D : 128) >> 4));
-                            if constexpr (FP8) {
-#pragma unroll
-                                for (int kk = 0; kk < D / 16; ++kk) {       // q's upper terms, then its lower ones
-                                    const uint32_t st = kk % (D / 32) * 2;
-                                    mma_ss<true>(d, q0 + (kk < D / 32 ? 0 : C::Q >> 5) + st, kl + st, D == 128 ? kRows128 : kRows64,
-                                                 idesc_of(0, 128, kHalf, false), kk > 0);
-                                }
-                            } else {
-#pragma unroll
-                                for (int kk = 0; kk < D / 16; ++kk) {
-                                    const uint32_t st = (kk >> 2) * (16384 >> 4) + (kk & 3) * 2;
-                                    mma_ss<false>(d, q0 + st, kl + st, kRows128, idesc_of(1, 128, kHalf, false), kk > 0);
-                                }
-                            }
-                            mma_commit(&m.s_full[buf]);
-                            if (n % RT == RT - 1) {
-                                mma_commit(&m.k_empty[rk.i]);
-                                rk.next<NK>();
-                            }
-                            if (n == items - 1) mma_commit(&m.q_free);
-                        }
-                        if (n > 0) {
-                            // O += P V of item j = n - 1
-                            const int j = n - 1, half = RT == 2 ? j & 1 : g, buf = (j & 1) * 2 + g;
-                            if (!mbar_wait_or_abort(&m.p_ready[buf], p_phase >> (j & 1) & 1u, a.err, abort_flag)) { ok = false; break; }
-                            p_phase ^= 1u << (j & 1);
-                            if (j % RT == 0 && !mbar_wait_or_abort(&m.v_ready[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }
-                            tc_fence_after();
-                            const uint32_t vl = v0 + (uint32_t)(rv.i * (kVTile >> 4) + half * (kHalf * 128 >> 4));
-                            const uint32_t pa = tmem + (uint32_t)(buf * kHalf);
-#pragma unroll
-                            for (int kk = 0; kk < kHalf / 16; ++kk)
-                                mma_ts(o, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j > 0 || kk > 0);
-                            mma_commit(&m.o_done[buf]);
-                            if (j % RT == RT - 1) {
-                                mma_commit(&v_free[rv.i]);
-                                rv.next<NP>();
-                            }
-                        }
-                    }
-                    if (!ok) break;
-                }
-                if (!ok) *abort_flag = 1;
-                if (*abort_flag) {
-                    // products in flight read shared memory and TMEM
-                    mma_commit(&m.drain[g]);
-                    mbar_wait(&m.drain[g], 0, a.err);
-                }
-            }
-            __syncwarp();
+    if (I4 && warp < 4) {
+        if constexpr (I4) {             // (one register hand-over for the group's roles)
+            fewer_registers<64>();
+            if (warp == 0) role_schedule<ROWS, kTcStart>(m, a);
+            else if (warp != 2) role_issue<FP8, D, RT, CP>(m, a, smem, tmem, warp >> 1);
         }
+    } else if (!I4 && warp == 0) {
+        Scheduler<ROWS, kTcStart> sched(m, a);                    // a segment ahead of the loads
+        if (sched.publish()) role_load<FP8, D, NK, NV>(m, p, smem + C::OFF_K, smem + C::OFF_V, [&] { return sched.publish(); });
+    } else if (!I4 && warp == 2) {
+        if constexpr (FP8) role_scales<kTcRoom>(m, a, m.kf, m.vf);
+    } else if (!I4 && (warp == 1 || warp == 3)) {
+        if constexpr (!I4) role_issue<FP8, D, RT, CP>(m, a, smem, tmem, warp >> 1);
     } else if (warp >= 12) {
         // ------------------------------------------------ q rows, and V tiles made ready; 4 bits: tiles of K, and of V by warps 16 to 19
         if constexpr (I4) fewer_registers<80>();
@@ -463,7 +477,7 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
         bool ok = true;
         while (ok && walk.next()) {
             const Segment& s = walk.segment();
-            Codes4<D> codes(a, s, of_v, tid >> 5 << 5, lane);
+            std::conditional_t<I4, Codes4<D>, NoCodes> codes(a, s, of_v, tid >> 5 << 5, lane);
             if constexpr (I4) codes.begin();
             const int q_rows = of_v ? 0 : s.rows;
             const float q_mul = a.scale_log2 > 0.f ? 1.f : a.scale_log2 < 0.f ? -1.f : 0.f;
@@ -614,7 +628,7 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
         if (!ok) *abort_flag = 1;
     } else {
         // ------------------------------------------------ softmax: group g of 4 warps, a thread per row
-        if constexpr (I4) more_registers<128>();
+        if constexpr (I4) more_registers<120>();
         const int g = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t s_t = tmem + lanes, o_t = tmem + lanes + kO + (uint32_t)(g * D);
