@@ -1,12 +1,12 @@
-"""Speculative decoding with a small random decoder: attention over a paged cache, MoE layers with expert
-skipping, verification of drafted trees. Run on a GPU:
+"""Speculative decoding with a small random decoder: rotary positions, attention over a paged cache, MoE layers with
+expert skipping, verification of drafted trees. Run on a GPU:
 
-    python examples/speculative_decode.py [--dtype bf16|f32] [--format fp8|plain] [--tokens 64] [--temperature 0.8]
+    python examples/speculative_decode.py [--dtype bf16|f32] [--format fp8|plain|int4] [--tokens 64] [--temperature 0.8]
 
 One step, for all requests together: a drafter proposes a small tree of tokens after each request's last one; the
-decoder runs all trees' nodes as one batch (their K and V go into the cache at once, each node attends to
-the request's prefix and its own ancestors); the verification accepts a path of each tree and picks the next token; the
-cache keeps the path's rows.
+decoder runs all trees' nodes as one batch (requests get pages for them, their rotated K and their V go into the cache at
+once, each node attends to the request's prefix and its own ancestors); the verification accepts a path of each tree and
+picks the next token; the cache keeps the path's rows.
 """
 from __future__ import annotations
 
@@ -46,23 +46,19 @@ class Decoder:
             weights = synth.make_layer(spec, seed=seed + 10 + i)
             self.moe.append(ace.AceLayer(weights, *offline.tables(weights), max_tokens=requests * MAX_NODES, residual=True))
         self.skip = skip
-        # the cache: each request owns a row of pages (a server would hand them out as requests grow)
+        # the cache: requests get pages as they grow
         per = -(-max_len // PAGE)
         self.kv = ace.AceKvCache(KV_HEADS, DIM, PAGE, requests * per, LAYERS, dtype, fmt)
-        self.pages = torch.randperm(requests * per, generator=torch.Generator().manual_seed(seed)).int().view(requests, per).cuda()
+        self.pages = torch.full((requests, per), -1, dtype=torch.int32, device="cuda")
+        self.refs = torch.zeros(requests * per, dtype=torch.int32, device="cuda")
+        self.missing = torch.zeros(1, dtype=torch.int32, device="cuda")
         self.lens = torch.zeros(requests, dtype=torch.int32, device="cuda")
-        self.freq = 10000.0 ** (-torch.arange(0, DIM, 2, device="cuda") / DIM)
+        self.rope = ace.AceRope(DIM, layout="interleaved", dtype=dtype)
 
     @staticmethod
     def _norm(x):
         f = x.float()
         return (f * torch.rsqrt(f.square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
-
-    def _rotate(self, x, pos):
-        a = pos[:, None].float() * self.freq
-        c, s = a.cos()[:, None], a.sin()[:, None]
-        u, v = x.float()[..., 0::2], x.float()[..., 1::2]
-        return torch.stack([u * c - v * s, u * s + v * c], -1).flatten(-2).to(x.dtype)
 
     def forward(self, tokens, parents, offsets, max_nodes: int):
         """Logits [T, VOCAB] of all requests' nodes, whose K and V are in the cache afterwards."""
@@ -70,15 +66,16 @@ class Decoder:
         mask = torch.empty(T, (max_nodes + 63) // 64, dtype=torch.int64, device="cuda")
         depth = torch.empty(T, dtype=torch.int32, device="cuda")
         ace.ace_tree_mask(parents, offsets, B, max_nodes, mask, depth)
+        self.kv.reserve(self.pages, self.lens, offsets[1:] - offsets[:-1], self.refs, self.missing)
         request = torch.repeat_interleave(torch.arange(B, device="cuda"), (offsets[1:] - offsets[:-1]).long(), output_size=T)
         at = self.lens[request].long() + torch.arange(T, device="cuda") - offsets[request].long()
         slots = self.pages[request, at // PAGE].long() * PAGE + at % PAGE
+        pos = self.lens[request] + depth
         x = self.embed[tokens.long()]
         for i in range(LAYERS):
             rows = (self._norm(x) @ self.qkv[i].T).view(T, HEADS + 2 * KV_HEADS, DIM)
-            pos = self.lens[request] + depth
-            q, k = self._rotate(rows[:, :HEADS], pos), self._rotate(rows[:, HEADS: HEADS + KV_HEADS], pos)
-            self.kv.write(i, k, rows[:, HEADS + KV_HEADS:], slots)
+            q = torch.empty(T, HEADS, DIM, dtype=self.dt, device="cuda")
+            self.kv.write_rotated(i, self.rope, pos, rows[:, :HEADS], q, rows[:, HEADS: HEADS + KV_HEADS], rows[:, HEADS + KV_HEADS:], slots)
             o = torch.empty_like(q)
             self.kv.attend(i, q, self.pages, self.lens, offsets, o, mask, max_nodes)
             x = x + o.flatten(1) @ self.out[i].T
@@ -86,6 +83,12 @@ class Decoder:
             self.moe[i].forward(x, y, T, "ratio", self.skip)
             x = y
         return (self._norm(x) @ self.head.T).contiguous()
+
+    def reorder(self, parents):
+        """Request b goes on from request parents[b] (int32, negative: it ends and gives its pages back)."""
+        pages, lens = torch.empty_like(self.pages), torch.empty_like(self.lens)
+        self.kv.fork(self.pages, self.lens, parents, self.refs, pages, lens)
+        self.pages, self.lens = pages, lens
 
     def keep(self, path, n_keep):
         new = torch.empty_like(self.lens)
@@ -152,7 +155,7 @@ def generate(decoder: Decoder, first, count: int, temperature: float, drafted: b
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--dtype", default="bf16", choices=("bf16", "f32"))
-    ap.add_argument("--format", default="fp8", choices=("fp8", "plain"))
+    ap.add_argument("--format", default="fp8", choices=("fp8", "plain", "int4"))
     ap.add_argument("--tokens", type=int, default=64)
     ap.add_argument("--temperature", type=float, default=0.8)
     a = ap.parse_args()

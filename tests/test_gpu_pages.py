@@ -325,3 +325,69 @@ def test_a_beam_search_keeps_its_books():
         # bf16 holds whole numbers up to 256 exactly
         want = torch.tensor(said[b], dtype=torch.float32).bfloat16()
         assert torch.equal(k[:, 1, 5].cpu(), want) and torch.equal(v[:, 0, 0].cpu(), want)
+
+
+# ----------------------------------------------------------------------- all of it together, as the example's decoder runs it
+
+
+@pytest.fixture(scope="module")
+def example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "speculative_decode.py")
+    spec = importlib.util.spec_from_file_location("speculative_decode", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def _alone(decoder):
+    """Skipping by ratio looks at the whole batch, so that a token's experts would depend on its company."""
+    for layer in decoder.moe:
+        layer.forward = lambda x, y, T, mode, value, plain=layer.forward: plain(x, y, T, "threshold", 0.15)
+    return decoder
+
+
+def test_speculation_over_a_4_bit_cache_is_plain_decoding(example):
+    first = torch.arange(4, device="cuda") * 7
+    torch.manual_seed(1)
+    plain, steps = example.generate(_alone(example.Decoder("f32", "int4")), first, 40, 0.0, drafted=False)
+    torch.manual_seed(2)
+    d = _alone(example.Decoder("f32", "int4"))
+    fast, fewer = example.generate(d, first, 40, 0.0)
+    assert steps == 40 and fewer <= steps
+    assert [o[:40] for o in fast] == [o[:40] for o in plain]
+    # the pages in use are those that the requests' rows name
+    named = d.pages[d.pages >= 0]
+    assert torch.equal(torch.bincount(named, minlength=d.refs.shape[0]).int(), d.refs) and d.refs.max() == 1
+    assert int(named.numel()) >= int(((d.lens + example.PAGE - 1) // example.PAGE).sum())
+
+
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "int4"), ("f32", "plain")])
+def test_forked_requests_go_on_as_the_one_that_they_come_from(example, dtype, fmt):
+    """One request's tokens are run; it is forked into all places, and its copies, which share its pages until they write, have the
+    logits that requests with pages of their own have."""
+    d, own = (_alone(example.Decoder(dtype, fmt, seed=5)) for _ in range(2))
+    g = torch.Generator(device="cuda").manual_seed(9)
+    chain = torch.tensor([-1], dtype=torch.int32, device="cuda")
+
+    def step(decoder, tokens):
+        B = decoder.lens.shape[0]
+        logits = decoder.forward(tokens, chain.repeat(B), torch.arange(B + 1, dtype=torch.int32, device="cuda"), 1)
+        path = torch.zeros(B, 1, dtype=torch.int32, device="cuda")
+        decoder.keep(path, torch.ones(B, dtype=torch.int32, device="cuda"))
+        return logits
+
+    for i in range(37):                             # two pages and a part of the third
+        tokens = torch.randint(0, example.VOCAB, (4,), generator=g, device="cuda").int()
+        step(d, tokens)
+        step(own, tokens[2].repeat(4))
+    d.reorder(_int([2, 2, 2, 2]))
+    assert d.refs.max() == 4 and int((d.refs > 0).sum()) == 3
+    for i in range(20):
+        tokens = torch.randint(0, example.VOCAB, (4,), generator=g, device="cuda").int()
+        assert torch.equal(step(d, tokens), step(own, tokens))
+    assert torch.equal(torch.bincount(d.pages[d.pages >= 0], minlength=d.refs.shape[0]).int(), d.refs) and int((d.refs == 4).sum()) == 2
+    d.reorder(_int([-1, -1, -1, -1]))
+    assert d.refs.count_nonzero() == 0 and d.lens.count_nonzero() == 0
+    d.kv.sync()
