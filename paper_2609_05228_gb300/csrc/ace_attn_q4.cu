@@ -184,14 +184,14 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
     const int page_rows = a.kv_heads * a.page_size;
     const unsigned char *k_from = nullptr, *v_from = nullptr, *scale_from = nullptr;        // the lane's words of the head's first row
     // a warp's runs of a tile, each of one page; what does not exist is zeros
-    auto load = [&](const Segment& s, int tile, int stage, const int (&page)[kSub]) {
+    auto load = [&](const Segment& s, int tile, int stage, const Entries<kSub>& entries) {
         if (tile < s.tile1) {
 #pragma unroll
             for (int u = 0; u < kSub; ++u) {
                 const int pos = tile * kKeys4 + (warp * kSub + u) * kStep, left = s.len + s.n - pos;
                 unsigned char* at = ring + stage * C::STAGE + u * C::SUB;
-                const int row = page[u] * page_rows + (pos & (a.page_size - 1));
-                if (__builtin_expect(left >= kStep && page[u] >= 0, 1)) {
+                const int page = entries.page(s, tile, u), row = page * page_rows + (pos & (a.page_size - 1));
+                if (__builtin_expect(left >= kStep && page >= 0, 1)) {
                     const unsigned char *k = k_from + (long long)row * C::ROW, *v = v_from + (long long)row * C::ROW;
 #pragma unroll
                     for (int i = 0; i < C::CODES / 512; ++i) {      // 8 rows of 64 bytes further on lie as far in the stage
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
                     }
                     if (lane < 2 * SCALE_CHUNKS) copy16(at + 2 * C::CODES + lane * 16, scale_from + (long long)row * (2 * G));
                 } else {
-                    const int have = page[u] < 0 ? 0 : left;
+                    const int have = page < 0 ? 0 : left;
                     const long long from = have <= 0 ? 0 : row;
 #pragma unroll
                     for (int i = 0; i < C::CODES / 512; ++i) {
@@ -215,28 +215,17 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto look_up = [&](const Segment& s, int tile, int (&page)[kSub]) {
-#pragma unroll
-        for (int u = 0; u < kSub; ++u) {
-            const int pos = tile * kKeys4 + (warp * kSub + u) * kStep;
-            if (u > 0 && a.page_size >= kSub * kStep) page[u] = page[0];
-            else page[u] = tile < s.tile1 && pos < s.len + s.n ? page_of(a, s.b, pos) : -1;
-        }
-    };
-    // a segment's first stages, and the pages of the one after
-    int next_page[kSub];
+    // a segment's first stages
+    Entries<kSub> entries;
+    auto first_of = [&](int tile) { return tile * kKeys4 + warp * (kSub * kStep); };
     auto begin = [&](const Segment& s) {
         const long long head = (long long)s.head * a.page_size;
         k_from = static_cast<const unsigned char*>(a.k_pool) + head * C::ROW + lane * 16;
         v_from = static_cast<const unsigned char*>(a.v_pool) + head * C::ROW + lane * 16;
         scale_from = (lane < SCALE_CHUNKS ? a.k_scale : a.v_scale) + head * (2 * G) + lane % SCALE_CHUNKS * 16;
-        int page[kStages][kSub];
+        entries.begin(a, s, first_of);
 #pragma unroll
-        for (int i = 0; i < kStages; ++i) look_up(s, s.tile0 + i, page[i]);
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) load(s, s.tile0 + i, i, page[i]);
-#pragma unroll
-        for (int u = 0; u < kSub; ++u) next_page[u] = page[kStages - 1][u];
+        for (int i = 0; i < kStages - 1; ++i) load(s, s.tile0 + i, i, entries);
     };
     // q's operand, PER_Q lanes a row with 8 elements each; elements of a row in units of 2^(e - 14), where its largest is below
     // 2^(e + 1): all bits of elements down to 2^-27 of it. Those that meet codes 16 times too large are a 16th.
@@ -389,8 +378,8 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
         for (int tile = s.tile0; tile < tile1; ++tile) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
             __syncwarp();               // all lanes' copies are there, and the stage before is read
-            load(s, tile + kStages - 1, stage == 0 ? kStages - 1 : stage - 1, next_page);
-            look_up(s, tile + kStages, next_page);
+            entries.move_to(a, s, tile + kStages - 1, first_of);
+            load(s, tile + kStages - 1, stage == 0 ? kStages - 1 : stage - 1, entries);
             const unsigned char* at = ring + stage * C::STAGE;
             stage = stage == kStages - 1 ? 0 : stage + 1;
             const int pos = tile * kKeys4 + warp * (kSub * kStep);

@@ -148,7 +148,7 @@ __device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, flo
 
 // Four warps, caches in 4 bits: tiles of K or of V as the products take them (both by one copy of the code, which is as long as the
 // instruction cache bears). A row's group of 32 codes is a lane's 16 bytes, 8
-// or 16 rows a turn, so that a warp reads 512 bytes on end; loaded a tile ahead, their pages two. (s: the tile's segment.)
+// or 16 rows a turn, so that a warp reads 512 bytes on end; loaded a tile ahead, and asked for two. (s: the tile's segment.)
 template <int D>
 struct Codes4 {
     static constexpr int CH = D / kGroup4, ROWS = 32 / CH, TURNS = 32 / ROWS;       // groups of a row; rows of a turn; turns of a warp's 32 rows
@@ -158,7 +158,7 @@ struct Codes4 {
     const uint8_t* pool;                // the lane's group of the head's first row, and its scale
     const uint16_t* scales;
     int row0, lane;                     // the warp's first row of a tile
-    int page[2];                        // of its runs of 16 rows
+    Entries<2> entries;                 // of the warp's runs
     uint4 code[TURNS];
     uint16_t scale[TURNS];
 
@@ -167,17 +167,10 @@ struct Codes4 {
         pool = static_cast<const uint8_t*>(of_v ? a.v_pool : a.k_pool) + head * 16;
         scales = reinterpret_cast<const uint16_t*>(of_v ? a.v_scale : a.k_scale) + head;
     }
-    __device__ __forceinline__ void look_up(int t) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int pos = t * kTcKeys + row0 + 16 * i;
-            page[i] = t < s.tile1 && pos < s.len + s.n ? page_of(a, s.b, pos) : -1;
-        }
-    }
-    // The lines of tile t, whose pages have been looked up, on their way to L2: 128 bytes of codes a lane, and the scales.
+    // The lines of tile t on their way to L2: 128 bytes of codes a lane, and the scales.
     __device__ __forceinline__ void ask(int t) {
         constexpr int LINE = 256 / D;   // rows of a line
-        const int r = lane * LINE, pg = r < 16 ? page[0] : page[1];
+        const int r = lane * LINE, p0 = entries.page(s, t, 0), p1 = entries.page(s, t, 1), pg = r < 16 ? p0 : p1;
         if (r < 32 && pg >= 0) {
             // (the lane's group of these rows: the line that it lies in)
             const long long at = (long long)(pg * (a.kv_heads * a.page_size) + ((t * kTcKeys + row0 + r) & (a.page_size - 1))) * CH;
@@ -185,9 +178,9 @@ struct Codes4 {
             if (r % 16 == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(scales + at));
         }
     }
-    // The codes of tile t, whose pages have been looked up.
     __device__ __forceinline__ void load(int t) {
         const int left = s.len + s.n - t * kTcKeys - row0;      // of the warp's rows
+        const int page[2] = {entries.page(s, t, 0), entries.page(s, t, 1)};
 #pragma unroll
         for (int i = 0; i < TURNS; ++i) {
             const int r = i * ROWS + lane % ROWS, pg = page[i * ROWS / 16];
@@ -201,9 +194,14 @@ struct Codes4 {
         }
     }
     __device__ __forceinline__ void begin() {
-        look_up(s.tile0);
+        entries.begin(a, s, [&](int t) { return t * kTcKeys + row0; });
         load(s.tile0);
-        look_up(s.tile0 + 1);
+    }
+    // The next tile's codes, and the lines of the one after.
+    __device__ __forceinline__ void next(int t) {
+        load(t + 1);
+        entries.move_to(a, s, t + 2, [&](int t) { return t * kTcKeys + row0; });
+        ask(t + 2);
     }
     // Pairs of elements (0, 4), (1, 5), (2, 6), (3, 7) of a word times the scale s, exactly: 128 + c is c in the last places of 128, and
     // s (128 + c) - 136 s; four places up, bf16 reads 16 c 2^-133, and 4 s (c / 4 - 2). LARGE: 136 s may be past bf16's largest.
@@ -556,15 +554,13 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
                 const int pos0 = t * kTcKeys;
                 const bool drafted = pos0 + kTcKeys > s.len;    // rows that not every node sees, or past the end
                 if constexpr (I4) {
-                    codes.ask(t + 1);
                     if (!mbar_wait_warp(of_v ? &m.v_empty[rv.i] : &m.k_empty[rv.i], rv.phase ^ 1u, a.err, abort_flag)) { ok = false; break; }
                     codes.store(smem + (of_v ? C::OFF_V : C::OFF_K) + rv.i * C::TILE, t, bad);
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(of_v ? &m.v_ready[rv.i] : &m.k_full[rv.i]);
                     if (++rv.i == (of_v ? NV : NK)) rv.i = 0, rv.phase ^= 1u;
-                    codes.load(t + 1);
-                    codes.look_up(t + 2);
+                    codes.next(t);
                     continue;
                 }
                 if (!mbar_wait_warp(&m.v_full[rv.i], rv.phase, a.err, abort_flag)) { ok = false; break; }

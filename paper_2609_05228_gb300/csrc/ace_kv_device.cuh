@@ -290,6 +290,43 @@ __device__ __forceinline__ int page_of(const AttnArgs& a, int b, int pos) {
     return page;
 }
 
+// By whole warps that walk a segment's tiles and read RUNS runs of 16 positions of each: the table's entries of the next 32 / RUNS tiles,
+// one a lane, and of as many after them. A load a tile would be waited for with the codes' own loads, which share its scoreboard.
+template <int RUNS>
+struct Entries {
+    static constexpr int kTiles = 32 / RUNS;
+    int now = 0, then = 0;              // even and odd batches of kTiles
+    // Run i of tile t is at position first(t) + 16 i.
+    template <typename First>
+    __device__ __forceinline__ int fetch(const AttnArgs& a, const Segment& s, int t0, First first) const {
+        const int lane = threadIdx.x & 31, t = t0 + lane / RUNS;
+        const int pos = t < s.tile1 ? first(t) + 16 * (lane % RUNS) : s.len + s.n;
+        if (pos >= s.len + s.n) return -1;
+        const int page = a.page_table[(long long)s.b * a.max_pages + (pos >> a.page_shift)];
+        if (page >= 0 && page < a.n_pages) return page;
+        atomicOr(a.err, kErrIndex);
+        return -1;
+    }
+    template <typename First>
+    __device__ __forceinline__ void begin(const AttnArgs& a, const Segment& s, First first) {
+        now = fetch(a, s, s.tile0, first);
+        then = fetch(a, s, s.tile0 + kTiles, first);
+    }
+    // Before tiles from t on are asked for, t going up one by one: the batch behind t's takes the place of the one before.
+    template <typename First>
+    __device__ __forceinline__ void move_to(const AttnArgs& a, const Segment& s, int t, First first) {
+        const int k = t - s.tile0;
+        if (k == 0 || k % kTiles) return;
+        if (k / kTiles & 1) now = fetch(a, s, t + kTiles, first);
+        else then = fetch(a, s, t + kTiles, first);
+    }
+    // Page of run i of tile t, -1 where it has none.
+    __device__ __forceinline__ int page(const Segment& s, int t, int i) const {
+        const int k = t - s.tile0;
+        return __shfl_sync(0xffffffffu, k / kTiles & 1 ? then : now, k % kTiles * RUNS + i);
+    }
+};
+
 // Word `w` (64 nodes) of the nodes that node i of the request sees, cut to its n nodes.
 __device__ __forceinline__ unsigned long long sees_word(const AttnArgs& a, int node0, int n, int i, int w) {
     if (w * 64 >= n || w < 0) return 0ull;
