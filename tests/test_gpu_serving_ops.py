@@ -282,6 +282,20 @@ def test_int4_attention_long_and_ragged(dtype, D, nodes):
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("most", [1, 2, 5])
+def test_int4_attention_many_requests(D, most):
+    """More requests than a block keeps shapes of, many without nodes or without a prefix, a few long ones far apart."""
+    rng = np.random.default_rng(D + most)
+    lens = rng.integers(0, 40, 700)
+    lens[[0, 255, 256, 257, 511, 699]] = [900, 1700, 640, 0, 2500, 300]
+    sizes = rng.integers(0, most + 1, 700)
+    sizes[[0, 255, 256, 511, 699]] = most
+    s = Step(lens.tolist(), sizes.tolist(), 8, 2, D, 16, seed=5)
+    s.random_masks(0.6)
+    s.check(*s.run())
+
+
 @pytest.mark.parametrize("dtype,D", TYPES)
 @pytest.mark.parametrize("nodes,length", [(2, 0), (3, 63), (12, 0), (12, 90), (12, 126), (30, 126), (70, 5)])
 def test_int4_attention_masked_rows_never_matter(dtype, D, nodes, length):
