@@ -85,11 +85,13 @@ __global__ void __launch_bounds__(256) k_kv_read(const __grid_constant__ RowArgs
     const uint32_t r0 = (blockIdx.x * (256 / LANES) + threadIdx.x / LANES) * kRowTurns;
     RowAt at(r0, p.H);
     long long row[kRowTurns];           // -1: zeros
+    uint32_t layer = (at.th >> 1) / (uint32_t)p.T;
 #pragma unroll
     for (int j = 0; j < kRowTurns; ++j, at.next(p.H)) {
         row[j] = -1;
         if (r0 + j >= p.rows) continue;
-        const uint32_t lt = at.th >> 1, layer = lt / (uint32_t)p.T;          // layer * T + token
+        const uint32_t lt = at.th >> 1;         // layer * T + token, at most one more than the row's before
+        if (lt - layer * p.T >= (uint32_t)p.T) ++layer;
         const long long slot = p.slots[lt - layer * p.T];
         if (slot >= p.n_slots) {
             if (sub == 0) atomicOr(p.err, kErrIndex);

@@ -58,14 +58,11 @@ __device__ __forceinline__ float finite_or_nan(float x) {
 
 // ---------------------------------------------------------------- rows in 4 bits
 
-// Scale of a group whose largest |x| is amax (finite): the smallest number of 4 significant bits that amax <= 7 times it.
-// amax / 7 rounded towards zero to 4 bits is at most a step from it, whatever its own rounding; 7 s is exact.
+// Scale of a group whose largest |x| is amax (finite): the smallest number of 4 significant bits that amax <= 7 times it. amax / 7
+// cut to 4 bits is that, or the one below: where its rounding took it over a number of 4 bits, it was within 2^-22 of it. 7 s is exact.
 __device__ __forceinline__ float int4_scale(float amax) {
-    if (!(amax > 7.f * 0x1p-126f)) return 0x1p-126f;
     const uint32_t b = __float_as_uint(amax * (1.f / 7.f)) & 0xfff00000u;
-    float s = __uint_as_float(b);
-    if (7.f * s < amax) s = __uint_as_float(b + 0x100000u);
-    else if (7.f * __uint_as_float(b - 0x100000u) >= amax) s = __uint_as_float(b - 0x100000u);
+    const float s = __uint_as_float(7.f * __uint_as_float(b) < amax ? b + 0x100000u : b);
     return fminf(fmaxf(s, 0x1p-126f), 1.125f * 0x1p125f);
 }
 

@@ -61,8 +61,13 @@ __device__ __forceinline__ void put_row(const RowArgs& p, int kv, long long row,
         float f[8];
         raw.to_float(f);
         uint32_t top = 0;
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t x = __vmaxu2(__vmaxu2(raw.w[0].x & 0x7fff7fffu, raw.w[0].y & 0x7fff7fffu), __vmaxu2(raw.w[0].z & 0x7fff7fffu, raw.w[0].w & 0x7fff7fffu));
+            top = max(x & 0xffff0000u, x << 16);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+        }
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const bool fine = top < 0x7f800000u;
@@ -70,7 +75,8 @@ __device__ __forceinline__ void put_row(const RowArgs& p, int kv, long long row,
         if (put) {
             uint32_t w = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w |= (fine ? int4_code(f[i], s, inv) : 8u) << (4 * i);
+            for (int i = 0; i < 8; ++i) w |= int4_code(f[i], s, inv) << (4 * i);
+            if (!fine) w = 0x88888888u;
             *reinterpret_cast<uint32_t*>(p.pool[kv] + row * (p.D / 2) + sub * 4) = w;
             if (sub % 4 == 0)
                 reinterpret_cast<uint16_t*>(p.scale[kv])[row * groups4(p.D) + sub / 4] = fine ? (uint16_t)(__float_as_uint(s) >> 16) : (uint16_t)0x7fffu;

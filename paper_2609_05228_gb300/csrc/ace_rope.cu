@@ -131,20 +131,22 @@ __global__ void __launch_bounds__(kBlock) k_rope(const __grid_constant__ RopeArg
 #pragma unroll
     for (int i = 0; i < kRowTurns; ++i) {
         if (!__any_sync(0xffffffffu, i < live)) break;
-        float f[8], y[8];
+        float f[8], y[8] = {};
         raw[i].to_float(f);
         if constexpr (VEC) {
-            // lanes of pairs' first elements are R / 16 below their partners'
-            const int q = R / 16, from = p.interleaved || sub >= 2 * q ? sub : sub < q ? sub + q : sub - q;
-            Raw8<T> o;
+            if (!p.interleaved) {
+                // lanes of pairs' first elements are R / 16 below their partners'
+                const int q = R / 16, from = sub >= 2 * q ? sub : sub < q ? sub + q : sub - q;
+                Raw8<T> o;
 #pragma unroll
-            for (int w = 0; w < (int)sizeof(T) / 2; ++w) {
-                o.w[w].x = __shfl_sync(0xffffffffu, raw[i].w[w].x, from, LANES);
-                o.w[w].y = __shfl_sync(0xffffffffu, raw[i].w[w].y, from, LANES);
-                o.w[w].z = __shfl_sync(0xffffffffu, raw[i].w[w].z, from, LANES);
-                o.w[w].w = __shfl_sync(0xffffffffu, raw[i].w[w].w, from, LANES);
+                for (int w = 0; w < (int)sizeof(T) / 2; ++w) {
+                    o.w[w].x = __shfl_sync(0xffffffffu, raw[i].w[w].x, from, LANES);
+                    o.w[w].y = __shfl_sync(0xffffffffu, raw[i].w[w].y, from, LANES);
+                    o.w[w].z = __shfl_sync(0xffffffffu, raw[i].w[w].z, from, LANES);
+                    o.w[w].w = __shfl_sync(0xffffffffu, raw[i].w[w].w, from, LANES);
+                }
+                o.to_float(y);
             }
-            o.to_float(y);
         } else {
             other[i].to_float(y);
         }
