@@ -499,6 +499,8 @@ ace_status ace_kv_fork(ace_kv* kv, const int32_t* page_table, const int32_t* len
         if (meet(new_table, out, old[i], olds[i]) || meet(new_lens, B_out, old[i], olds[i]))
             return pages_fail("new_table and new_lens must not overlap the other arrays");
     if (meet(new_table, out, new_lens, B_out)) return pages_fail("new_table and new_lens must not overlap the other arrays");
+    for (int i = 0; i < 3; ++i)
+        if (meet(refs, kv->desc.n_pages, old[i], olds[i])) return pages_fail("refs must not overlap the other arrays");
     if (const ace_status st = on_device(kv->device, "cache")) return st;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     kv->last_stream = s;

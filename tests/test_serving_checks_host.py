@@ -216,6 +216,8 @@ A = [(i + 1) << 20 for i in range(8)]
     ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[3], A[4], None), b"non-NULL"), ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[3], A[0], A[5]), b"overlap"),
     ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[3], A[0] + 44, A[5]), b"overlap"), ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[3], A[4], A[1]), b"overlap"),
     ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[3], A[4], A[4] + 44), b"overlap"), ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[3], A[3] + 396, A[5]), b"overlap"),
+    ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[0] + 44, A[4], A[5]), b"overlap"), ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[1] + 12, A[4], A[5]), b"overlap"),
+    ("ace_kv_fork", (A[0], A[1], 4, A[2], 4, 3, A[2] - 396, A[4], A[5]), b"overlap"),
     ("ace_kv_reserve", (A[0], 3, A[1], A[2], -1, A[3], A[4]), b"B"), ("ace_kv_reserve", (A[0], 0, A[1], A[2], 4, A[3], A[4]), b"max_pages"),
     ("ace_kv_reserve", (None, 3, A[1], A[2], 4, A[3], A[4]), b"non-NULL"), ("ace_kv_reserve", (A[0], 3, None, A[2], 4, A[3], A[4]), b"non-NULL"),
     ("ace_kv_reserve", (A[0], 3, A[1], None, 4, A[3], A[4]), b"non-NULL"), ("ace_kv_reserve", (A[0], 3, A[1], A[2], 4, None, A[4]), b"non-NULL"),
