@@ -276,6 +276,64 @@ def test_pages_past_2_32_bytes():
     assert table.tolist() == [[0], [0]] and used.item() == 1 and refs[0] == 2 and (kv.k_pool[0, 0] == 37).all()
 
 
+def test_empty_calls_and_requests_that_do_not_grow():
+    """No requests, no pages, and requests with a grow of 0 whose lengths and rows are not looked at."""
+    kv, pools = _cache("int4", "bf16", 64, 16, 10)
+    before = [p.cpu().numpy() for p in pools]
+    refs = np.zeros(10, np.int32)
+    refs[[2, 3]] = 1
+    r, none, m, empty = _int(refs), _int(np.zeros((0, 3))), _int([77]), _int([])
+    kv.reserve(none, empty, empty, r, m)
+    assert m.item() == 0
+    kv.release(none, empty, empty, r)
+    kv.fork(none, empty, empty, r, none.clone(), empty.clone())
+    kv.copy_pages(empty, empty)
+    kv.sync()
+    assert (r.cpu().numpy() == refs).all()
+    table = _int([[99, -7, 5], [2, -1, -1], [3, 3, 3]])
+    kv.reserve(table, _int([-3, 4, 1000]), _int([0, 20, 0]), r, m)
+    kv.sync()
+    assert table.tolist() == [[99, -7, 5], [2, 0, -1], [3, 3, 3]] and m.item() == 0
+    refs[0] = 1
+    assert (r.cpu().numpy() == refs).all()
+    _same(pools, before)
+    kv.compact(none, r, m, new := _int(np.zeros(10)))
+    kv.sync()
+    assert m.item() == 3 and new.tolist() == [0, -1, 2, 1] + [-1] * 6
+    assert r.tolist() == [1, 1, 1] + [0] * 7
+    _same(pools, _moved(before, [(3, 1, 16)]))
+
+
+def test_graphs_of_one_cache_replayed_in_turn():
+    """Two captured graphs share a cache's workspace: each leaves what the other's plan needs as it found it."""
+    page, n_pages = 16, 12
+    kv, pools = _cache("int4", "bf16", 64, page, n_pages)
+    table, refs = np.array([[0, -1, -1, -1], [0, -1, -1, -1]], np.int32), np.zeros(n_pages, np.int32)
+    refs[0] = 2
+    lens, grow = np.array([5, 9], np.int32), np.array([20, 1], np.int32)
+    t, l, g, r, m = _int(table), _int(lens), _int(grow), _int(refs), _int([77])
+    src, dst = _int([0, 0]), _int([11, 10])
+    grows, copies = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(grows):
+        kv.reserve(t, l, g, r, m)
+    with torch.cuda.graph(copies):
+        kv.copy_pages(src, dst)
+    before = [p.cpu().numpy() for p in pools]
+    for _ in range(3):
+        t.copy_(_int(table)), r.copy_(_int(refs))
+        for p, b in zip(pools, before):
+            p.copy_(torch.from_numpy(b))
+        copies.replay()
+        grows.replay()
+        copies.replay()
+        kv.sync()
+        want = S.reserve(table, lens, grow, refs, page)
+        assert (t.cpu().numpy() == want[0]).all() and (r.cpu().numpy() == want[1]).all() and m.item() == 0
+        fresh = int(t[0, 0])
+        assert fresh != 0 and int(t[1, 0]) == 0
+        _same(pools, _moved(before, [(0, 11, page), (0, 10, page), (0, fresh, 5)]))
+
+
 def test_a_beam_search_keeps_its_books():
     """Steps of forks and reserves in one captured graph, against the account; the rows that a beam wrote are the rows that it reads."""
     rng = np.random.default_rng(12)
