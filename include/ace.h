@@ -436,7 +436,7 @@ typedef struct ace_kv ace_kv;   /* opaque */
  *   k_pool, v_pool    device, 16-byte aligned; they must outlive the handle
  *   k_scale, v_scale  device, 16-byte aligned; ACE_KV_FP8 and ACE_KV_INT4 (ignored otherwise)
  * The pools' contents are not touched: rows that no call wrote may hold
- * anything, NaN included. Allocates the attention's workspace (tens of MB);
+ * anything, NaN included. Allocates a workspace (tens of MB for the attention, 24 bytes a page for their moves);
  * the calls below allocate nothing, are asynchronous on `stream` and can be
  * captured in a CUDA graph. One call may be in flight per handle at a time, and
  * the current device must be the one that was current at creation (INVALID_ARG).
@@ -510,7 +510,7 @@ ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, con
  *   grow        [B] int32 >= 0
  *   missing     [1] int32 out: 0, or how many pages the pool is short of; then nothing was changed
  * B is at most 8192, and B * max_pages 2^29 (UNSUPPORTED above). A request whose lens or grow is negative, whose tokens leave its row or whose partly
- * filled page does not exist is left out and reported by ace_kv_sync.
+ * filled page does not exist is left out and reported by ace_kv_sync; one with a grow of 0 is not looked at.
  *
  * ace_kv_release - requests b with ended[b] != 0 give their pages back: counts fall, their entries become -1, their lens 0.
  *
@@ -640,8 +640,9 @@ ace_status ace_tree_mask_rows(const int32_t* parents, const int32_t* node_offset
  *   T     rows of q and out, node_offsets[B]; max_nodes bounds every n_b. The host does not know the
  *         trees, so max_nodes also chooses the kernel: a bound far above them is right, and slower
  * Softmax and sums are fp32, and out is rounded to dtype. On the tensor cores (bf16, head sizes 64
- * and 128) more is rounded on the way. Over plain caches: the softmax weights to bf16 (2^-9 of a
- * weight). Over fp8 caches: the weights to fp16 (2^-12 of a weight, 2^-25 of the row's largest), q
+ * and 128) more is rounded on the way. Over plain and int4 caches: the softmax weights to bf16 (2^-9
+ * of a weight; an int4 cache's code * s is exact in bf16, and elements of q 2^-27 and more below their
+ * row's largest may lose bits that are 2^-34 of that one). Over fp8 caches: the weights to fp16 (2^-12 of a weight, 2^-25 of the row's largest), q
  * to two e4m3 terms (elements 2^-10 and more below its row's largest lose bits that are 2^-18 of
  * that one), and V rows whose scale is 2^-20 or less of the largest that every row of a block sees.
  * The work is split over the long axis by the lengths, in an order that depends on them alone: the

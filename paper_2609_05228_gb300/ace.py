@@ -574,7 +574,8 @@ class AceRope:
 class AceKvCache:
     """A paged key/value cache of a model's layers and its ace_kv handle. The pools are torch tensors:
     those given, or new ones (zeros). fmt "plain" keeps rows in dtype, "fp8" e4m3 codes and a scale
-    byte per (token, head), "int4" 4-bit codes (two a byte, uint8) and a bf16 scale for every 32 of them. Slots are page * page_size + row. Calls run on torch's current stream unless one is given."""
+    byte per (token, head), "int4" 4-bit codes (two a byte, uint8) and a bf16 scale for every 32 of them.
+    Slots are page * page_size + row. Calls run on torch's current stream unless one is given."""
 
     def __init__(self, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, layers: int = 1, dtype: str = "bf16",
                  fmt: str = "fp8", k_pool=None, v_pool=None, k_scale=None, v_scale=None, device: int = 0):

@@ -4,17 +4,16 @@
 //                     of two, so a group's product is exact but for fp32's sums, and its scale is one factor of 16 x 8 sums
 //   P^T = 2^(S^T - ref)   bf16
 //   O^T += V^T P^T    V's code * scale is exact in bf16 (3 significant bits times 4)
-// At 4 bits a tile of 128 positions is 18 KB and takes HBM 750 cycles of an SM, in which its 32768 codes have to become operands: too
+// At 4 bits a tile of 128 positions is 18 KB and takes HBM 850 cycles of an SM (copy rate), in which its 32768 codes have to become operands: too
 // little time for the hand-overs of tcgen05 (scores, softmax, weights and conversion through shared and tensor memory take 2000
 // cycles a tile in ace_attn_few.cu, fp8 codes without any conversion). So the codes become operands in the registers of the warp
 // that multiplies them (mma.sync; about one operation a code), S^T turns into the second product's operand by movmatrix, and the
 // warps of a CTA walk their positions of each tile on their own, with their own running maxima, from rings of cp.async stages; they
 // meet at a unit's end only.
 // Measured (64 users of up to 8192 positions, 322,000 in all, 4 kv heads of 128): 8 rows a unit 57 us (3.3 TB/s, 0.49 of the copy rate;
-// ace_attn_few.cu over an fp8 cache 73), 16 rows 81. With 8 times the positions 5.1 TB/s: the rest is starts and ends of units (a
-// block's first look at the requests, page and codes takes 4 us) and the joining kernel. A step of 32 positions of 8 rows is 630
-// operations; 16 warps an SM issue 0.57 a cycle and scheduler, with no pipe above 45%: bound by the warps' dependent chains (20 or 24
-// warps of fewer registers spill, 12 of more are as fast).
+// ace_attn_few.cu over an fp8 cache 73), 16 rows 81. With 8 times the positions 5.1 TB/s: the rest is starts and ends of units and the
+// joining kernel. 16 warps an SM issue 0.55 to 0.60 a cycle and scheduler, with no pipe above 45%: bound by the warps' dependent
+// chains (12 warps of 168 registers had the same rate a position).
 #include <cfloat>
 #include <type_traits>
 

@@ -20,7 +20,7 @@
 // largest and less, whose codes' last bits fall under fp16's least.
 // 4-bit caches: K's and V's codes times their scales, which bf16 holds exactly, are written as the tiles of a plain cache by two
 // groups of four warps (Codes4), in place of TMA. 64 users as below: 33 to 64 rows a unit 126 to 128 us, 128 rows 139, 192 rows 191
-// (plain 126 to 128, 134, 162): with few rows V's conversion bounds it (2500 cycles a tile), with many the softmax; 8 users'
+// (plain 126 to 128, 134, 162): with few rows V's conversion bounds it (2400 of 3250 cycles a tile), with many the softmax; 8 users'
 // 128 nodes of 64 heads 342 us.
 // P is rounded to bf16 (2^-9 of a weight; plain caches) or fp16 (2^-12), as the products need; sums, maxima and O are fp32.
 // Measured: 8 users of up to 16384 positions, 128 nodes of 64 heads (8 kv heads of 128), bf16: 304 us, 850 TFLOP/s. 64 users

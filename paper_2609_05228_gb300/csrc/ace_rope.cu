@@ -8,9 +8,9 @@
 // LANES lanes take kRowTurns neighbouring heads of a token, 8 elements of a row each, so that a lane needs its pairs' sines and
 // cosines once. They come from a table of the block's tokens in shared memory, made while the rows are under way. In layout
 // "half" a pair's partner comes by shuffles where a row is a whole number of lanes' shares, from memory elsewhere. Bound by memory:
-// 16384 tokens of 72 heads of 128, half of each turned, 100 us for 604 MB, 6.0 TB/s (115 with a look at the table a row). Rows of 8192
-// tokens (32 heads, 8 kv heads) into a 4-bit cache 51 us for 177 MB, by issue slots (quantising takes 20 operations an element);
-// fp8 43, plain 41. A block has rows of one tensor: with q's, k's and v's mixed, 4 bits took 71.
+// 16384 tokens of 72 heads of 128, half of each turned, 100 us for 604 MB, 6.0 TB/s. With a look at the table a row,
+// and blocks that mixed rows of q, k and v, it took 115. Rows of 8192 tokens (32 heads, 8 kv heads) into a 4-bit cache 54 us, by issue
+// slots, fp8 46, plain 44 (layout "half" 62, 52, 50).
 #include <math.h>
 
 #include <new>
