@@ -47,7 +47,7 @@ struct Q4Shared {
     float join[Q4<D, NT>::WARPS * 8 * Q4<D, NT>::PITCH];
     uint4 q[NT * Q4<D, NT>::G * 32];        // operand of S^T: [8 rows][group][lane]
     float q8[NT * Q4<D, NT>::G * 8];        // -8 times the sum of a row's q over a group: [8 rows][group][row]
-    float f_row[NT * 8];                // q's scale times the softmax's
+    float f_row[2][NT * 8];             // q's scale times the softmax's, in two factors
     int node[NT * 8];                   // row's node of the request
     float2 ml[Q4<D, NT>::WARPS][NT * 8];          // a warp's reference and sum
     unsigned long long bad[kMaxNodes / 64];     // nodes with a V that is not finite, left out of the products
@@ -269,7 +269,11 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
             if (c % 4 == 0) m.q8[((r >> 3) * G + c / 4) * 8 + (r & 7)] = sum * (-8.f * 0x1p-24f);
             m.q[((r >> 3) * G + c / 4) * 32 + (r & 7) * 4 + c % 4] = make_uint4(w[0], w[1], w[2], w[3]);
             if (c == 0) {
-                m.f_row[r] = a.scale_log2 * pow2_of_byte(e - 14) * 0x1p24f;
+                // scale_log2 2^(e - 117) is infinite from q's of 2^121 on, where scores need not be: it is halved by exponents, so
+                // that what one factor gives lies between the sum and the score. (Past 2^250 no score but 0 is finite.)
+                const int k = min(max((int)(__float_as_uint(a.scale_log2) >> 23 & 255u), 1), 253) - 127, both = min(k + e - 117, 250), half = both >> 1;
+                m.f_row[0][r] = a.scale_log2 * pow2_of_byte(127 - k) * pow2_of_byte(127 + half);
+                m.f_row[1][r] = pow2_of_byte(127 + both - half);
                 m.node[r] = r < s.rows ? (s.row0 + r) / a.group : 0;
             }
         }
@@ -432,11 +436,11 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const float2 f = *reinterpret_cast<const float2*>(&m.f_row[8 * n + 2 * t]);
+                    const float2 f = *reinterpret_cast<const float2*>(&m.f_row[0][8 * n + 2 * t]), z = *reinterpret_cast<const float2*>(&m.f_row[1][8 * n + 2 * t]);
 #pragma unroll
                     for (int u = 0; u < kSub; ++u) {
-                        unpair(mul2(x01[u][n], pair(f.x, f.y)), x[u][n][0], x[u][n][1]);
-                        unpair(mul2(x23[u][n], pair(f.x, f.y)), x[u][n][2], x[u][n][3]);
+                        unpair(mul2(mul2(x01[u][n], pair(f.x, f.y)), pair(z.x, z.y)), x[u][n][0], x[u][n][1]);
+                        unpair(mul2(mul2(x23[u][n], pair(f.x, f.y)), pair(z.x, z.y)), x[u][n][2], x[u][n][3]);
                     }
                 }
             }
