@@ -586,10 +586,11 @@ void ace_rope_destroy(ace_rope* rope);
  *   q, k        head h of token t starts at q + t * q_token_stride + h * q_head_stride elements and is contiguous (any
  *               strides >= 0); n_kv_heads 0: no k
  *   q_out, k_out  the same with their own strides, rows apart from one another; an output may be its input (the same
- *               address and strides), and must not overlap q, k or the other output otherwise
+ *               address and strides), and must not overlap q, k, positions or the other output otherwise (rows between
+ *               another tensor's rows are apart)
  * fp32, rounded once. Asynchronous on `stream`, allocates nothing, can be captured. The current device must be the rope's.
- * Errors: INVALID_ARG (NULL, negative sizes or strides, alignment, outputs whose rows overlap, device); UNSUPPORTED for more
- * than 2^30 rows.
+ * Errors: INVALID_ARG (NULL, negative sizes or strides, alignment, outputs whose rows overlap one another or another tensor,
+ * device); UNSUPPORTED for more than 2^30 rows.
  */
 ace_status ace_rope_apply(const ace_rope* rope, int inverse, const int32_t* positions, int T, const void* q, long long q_token_stride,
                           long long q_head_stride, int n_heads, void* q_out, long long q_out_token_stride, long long q_out_head_stride,
@@ -598,8 +599,8 @@ ace_status ace_rope_apply(const ace_rope* rope, int inverse, const int32_t* posi
 
 /*
  * ace_kv_write_rotated - ace_rope_apply to q and ace_kv_write of the rotated k and of v, in one pass: the same bits as the two
- * calls (k is rounded to dtype after its rotation). q and q_out as ace_rope_apply takes them (n_heads 0: no q); k, v and slots
- * as ace_kv_write takes them. A token with a negative slot has its q turned and its k and v left out.
+ * calls (k is rounded to dtype after its rotation). q and q_out as ace_rope_apply takes them (n_heads 0: no q), q_out apart from
+ * k, v, slots and the cache too; k, v and slots as ace_kv_write takes them. A token with a negative slot has its q turned and its k and v left out.
  * Errors: those of both; INVALID_ARG where rope and cache differ in head_dim or dtype; UNSUPPORTED for
  * T (n_heads + 2 H) > 2^30.
  */

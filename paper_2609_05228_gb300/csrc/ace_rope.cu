@@ -13,10 +13,12 @@
 // slots, fp8 46, plain 44 (layout "half" 62, 52, 50).
 #include <math.h>
 
+#include <initializer_list>
 #include <new>
 #include <string>
 
 #include "ace_kv_rows.cuh"
+#include "ace_overlap.h"
 
 struct ace_rope {
     ace_rope_desc desc;
@@ -242,6 +244,22 @@ const char* bad_out(const void* x, long long token, long long head, const void* 
     return nullptr;
 }
 
+// Rows of a tensor of the call; the bytes of an array. (Other threads read and write them while an output is written.)
+RowSet rows_of(const void* x, long long token, long long head, int T, int heads, int D, int elem) {
+    return RowSet{(uintptr_t)x, (Wide)token * elem, (Wide)head * elem, T, heads, D * elem};
+}
+RowSet bytes_of(const void* x, long long bytes) { return RowSet{(uintptr_t)x, 0, 0, 1, 1, bytes}; }
+
+// Whether an output meets any of the others but the `own` input, when it lies in that one's place.
+bool meets(const RowSet& out, const RowSet& own, std::initializer_list<RowSet> others) {
+    if (out.at != own.at && rows_meet(out, own)) return true;
+    for (const RowSet& x : others)
+        if (rows_meet(out, x)) return true;
+    return false;
+}
+
+constexpr char kOverlap[] = "an output must not overlap the other tensors";
+
 ace_status rope_fail(const char* m) { return kv_fail(ACE_ERR_INVALID_ARG, m); }
 
 // Rows of a call whose rows all begin on 16 bytes, with whole words of pairs.
@@ -358,6 +376,10 @@ ace_status ace_rope_apply(const ace_rope* rope, int inverse, const int32_t* posi
         const char* bad = bad_out(q, q_token_stride, q_head_stride, q_out, q_out_token_stride, q_out_head_stride, T, n_heads, D);
         if (!bad) bad = bad_out(k, k_token_stride, k_head_stride, k_out, k_out_token_stride, k_out_head_stride, T, n_kv_heads, D);
         if (bad) return rope_fail(bad);
+        const RowSet rq = rows_of(q, q_token_stride, q_head_stride, T, n_heads, D, elem), rk = rows_of(k, k_token_stride, k_head_stride, T, n_kv_heads, D, elem);
+        const RowSet oq = rows_of(q_out, q_out_token_stride, q_out_head_stride, T, n_heads, D, elem);
+        const RowSet ok = rows_of(k_out, k_out_token_stride, k_out_head_stride, T, n_kv_heads, D, elem), at = bytes_of(positions, 4LL * T);
+        if (meets(oq, rq, {rk, ok, at}) || meets(ok, rk, {rq, at})) return rope_fail(kOverlap);
     }
     if (const ace_status st = on_device(rope->device, "rope")) return st;
     if (rows == 0) return ACE_OK;
@@ -393,9 +415,17 @@ ace_status ace_kv_write_rotated(ace_kv* kv, int layer, const ace_rope* rope, con
     const int elem = kv->elem;
     if ((uintptr_t)q % elem || (uintptr_t)q_out % elem || (uintptr_t)k % elem || (uintptr_t)v % elem)
         return rope_fail("q, q_out, k and v must be aligned to their type");
-    if (T > 0 && n_heads > 0)
+    if (T > 0 && n_heads > 0) {
         if (const char* bad = bad_out(q, q_token_stride, q_head_stride, q_out, q_out_token_stride, q_out_head_stride, T, n_heads, D.head_dim))
             return rope_fail(bad);
+        const long long rows = (long long)D.layers * D.n_pages * D.n_kv_heads * D.page_size, pool = rows * row_bytes(D.format, D.head_dim, elem);
+        const long long scales = rows * scale_bytes(D.format, D.head_dim);
+        auto heads_of = [&](const void* x, long long token, long long head, int heads) { return rows_of(x, token, head, T, heads, D.head_dim, elem); };
+        if (meets(heads_of(q_out, q_out_token_stride, q_out_head_stride, n_heads), heads_of(q, q_token_stride, q_head_stride, n_heads),
+                  {heads_of(k, k_token_stride, k_head_stride, D.n_kv_heads), heads_of(v, v_token_stride, v_head_stride, D.n_kv_heads), bytes_of(positions, 4LL * T),
+                   bytes_of(slots, 8LL * T), bytes_of(kv->k_pool, pool), bytes_of(kv->v_pool, pool), bytes_of(kv->k_scale, scales), bytes_of(kv->v_scale, scales)}))
+            return rope_fail(kOverlap);
+    }
     if (const ace_status st = on_device(kv->device, "cache")) return st;
     if (const ace_status st = on_device(rope->device, "rope")) return st;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
