@@ -570,8 +570,9 @@ typedef struct ace_rope ace_rope;   /* opaque; never changes after its creation,
 
 /*
  * ace_rope_create - the frequencies on the current device. divisors [rot_dim / 2] host, or NULL: f_i is divided by
- * divisors[i] besides. Synchronises `stream`. Frequencies are kept as 2^-64ths of a turn: the angle at position p is off by
- * about 2^-53 p f_i at most, at any position an int32 holds.
+ * divisors[i] besides. Synchronises `stream`. Frequencies are kept as 2^-64ths of a turn, to nearest: the angle at position p is
+ * off by 2 pi 2^-65 |p| + (4 + ln base) 2^-53 |p| f_i radians at most (BY_TURNS, between its ends: the second part factor * high /
+ * (high - low) times), at any position an int32 holds, and by 2^-25 where its sine and cosine are taken in fp32.
  * Errors: INVALID_ARG (NULL, a field out of its range, a divisor that is not positive and finite), UNSUPPORTED (head_dim),
  * OOM, CUDA.
  */

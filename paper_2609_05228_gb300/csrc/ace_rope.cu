@@ -2,9 +2,10 @@
 // turned and written into the paged cache in one pass.
 //   (x, y) -> magnitude (x cos a - y sin a, x sin a + y cos a),  a = position * f_i for pair i
 // The angle is kept as a fraction of a turn: F_i = f_i / 2 pi in units of 2^-64 of a turn, so that position * F_i modulo
-// 2^64 (one integer product) is the angle without its whole turns, as exact for far positions as for near ones: off by
-// 2^-54 f_i position of a turn for F_i's rounding, where an fp32 angle at position 10^6 is off by a thirtieth of a radian.
-// Its nearest quarter turn picks sign and place, and sine and cosine are taken of what is left, at most an eighth of a turn.
+// 2^64 (one integer product) is the angle without its whole turns, exact for F_i: off by 2^-65 |position| of a turn for F_i's
+// rounding and by what f_i is (ace_angles.h), where an fp32 angle at position 10^6 is off by a thirtieth of a radian.
+// Its nearest quarter turn picks sign and place, and sine and cosine are taken in fp32 of what is left, at most an eighth of a turn
+// (to 2^-28 of a turn).
 // LANES lanes take kRowTurns neighbouring heads of a token, 8 elements of a row each, so that a lane needs its pairs' sines and
 // cosines once. They come from a table of the block's tokens in shared memory, made while the rows are under way. In layout
 // "half" a pair's partner comes by shuffles where a row is a whole number of lanes' shares, from memory elsewhere. Bound by memory:
@@ -17,6 +18,7 @@
 #include <new>
 #include <string>
 
+#include "ace_angles.h"
 #include "ace_kv_rows.cuh"
 #include "ace_overlap.h"
 
@@ -282,24 +284,6 @@ void of_rope(const ace_rope* rope, int inverse, const int32_t* positions, RopeAr
     p.sin_mul = inverse ? -p.magnitude : p.magnitude;
 }
 
-// f_i in turns a position.
-double frequency(const ace_rope_desc& D, int i) {
-    constexpr double kTwoPi = 6.283185307179586476925;
-    const double t = pow(D.base, -2.0 * i / D.rot_dim) / kTwoPi;
-    double keep = 1.0;
-    if (D.scaling == ACE_ROPE_LINEAR) {
-        keep = 0.0;
-    } else if (D.scaling == ACE_ROPE_BY_TURNS) {
-        keep = (D.original_len * t - D.low) / (D.high - D.low);
-    } else if (D.scaling == ACE_ROPE_BY_INDEX) {
-        auto index_of = [&](double turns) { return D.rot_dim * log(D.original_len / (turns * kTwoPi)) / (2.0 * log(D.base)); };
-        const double lo = fmax(floor(index_of(D.high)), 0.0), hi = fmin(ceil(index_of(D.low)), D.rot_dim - 1.0);
-        keep = 1.0 - (i - lo) / ((hi == lo ? lo + 0.001 : hi) - lo);
-    }
-    keep = fmin(fmax(keep, 0.0), 1.0);
-    return D.scaling == ACE_ROPE_NONE ? t : t * (keep + (1.0 - keep) / D.factor);
-}
-
 }  // namespace
 
 extern "C" {
@@ -321,13 +305,13 @@ ace_status ace_rope_create(const ace_rope_desc* desc, const double* divisors, vo
         return rope_fail("scaling by turns or index needs original_len > 0 and 0 < low < high, all finite");
     uint64_t turns[kMaxHeadDim / 2];
     for (int i = 0; i < D.rot_dim / 2; ++i) {
-        double f = frequency(D, i);
+        double f = rope_frequency(D, i);
         if (divisors) {
             if (!(divisors[i] > 0.0) || !isfinite(divisors[i])) return rope_fail("divisors must be positive and finite");
             f /= divisors[i];
         }
         if (!isfinite(f)) return rope_fail("a frequency is not finite");
-        turns[i] = (uint64_t)ldexp(f - floor(f), 64);
+        turns[i] = rope_turn(f);
     }
     ace_rope* rope = new (std::nothrow) ace_rope();
     if (!rope) return kv_fail(ACE_ERR_OOM, "out of host memory");
