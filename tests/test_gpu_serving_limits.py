@@ -51,3 +51,64 @@ def test_int4_attention_large_q_and_small_keys(dtype, D, p, nodes):
     s.qd = s.q.double().cpu().numpy()
     assert np.isfinite(s.qd).all() and (p < 124 or dtype == "f32" or np.abs(s.qd).max() > 2.0 ** 125)
     s.check(*s.run())
+
+
+def _longest_share(lens, nodes, kv_heads, ctas, keys, start):
+    """Tiles of the longest part of a unit that one block walks: units of start + tiles places on a line that the blocks share alike."""
+    tiles = [-(-(n + nodes) // keys) for n in lens]
+    line = sum(start + t for t in tiles) * kv_heads
+    longest, at = 0, 0
+    for t in tiles:
+        for _ in range(kv_heads):
+            first = at + start
+            for c in range(first * ctas // line, min((first + t) * ctas // line + 1, ctas)):
+                longest = max(longest, min((c + 1) * line // ctas, first + t) - max(c * line // ctas, first))
+            at = first + t
+    return longest
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nodes,G,requests,length,keys,start,batch,per_sm", [
+    (1, 8, 20, 16600, 256, 2, 16, 2), (2, 4, 20, 16600, 256, 2, 16, 2), (4, 4, 20, 12500, 96, 3, 32, 2), (5, 4, 10, 8300, 128, 7, 16, 1),
+    (10, 8, 10, 8300, 128, 7, 16, 1), (32, 4, 10, 8300, 128, 7, 16, 1), (40, 4, 10, 8300, 128, 7, 16, 1)])
+def test_int4_attention_walks_of_many_batches_of_pages(nodes, G, requests, length, keys, start, batch, per_sm, D):
+    """Blocks that walk more tiles of a unit than three batches of page-table entries hold: every batch is taken over and filled again.
+    Every query row has a key of its own, somewhere in a request's scattered pages, that takes nearly all of its weight, so a tile
+    read from another page shows. Bounds as in test_gpu_serving_ops.py (weights and outputs rounded to bf16, 2^-8 each)."""
+    H, page, n_pages = 16, 16, 700
+    rng = np.random.default_rng(D + nodes)
+    lens = [length - int(x) for x in rng.integers(0, 100, requests)]
+    ctas = torch.cuda.get_device_properties(0).multi_processor_count * per_sm
+    assert _longest_share(lens, nodes, H, ctas, keys, start) > 3 * batch
+    kv = ace.AceKvCache(H, D, page, n_pages, 1, "bf16", "int4")
+    g = torch.Generator(device="cuda").manual_seed(D + nodes)
+    k, v = (torch.randn(n_pages * page, H, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    slots = torch.arange(n_pages * page, device="cuda")
+    kv.write(0, k, v, slots)
+    kv.read(0, slots, k, v)
+    table = torch.randint(0, n_pages, (requests, -(-(length + nodes) // page)), generator=g, device="cuda", dtype=torch.int32)
+    q = torch.empty(requests * nodes, H * G, D, dtype=torch.bfloat16, device="cuda")
+    at = []
+    for b, n in enumerate(lens):
+        pos = torch.arange(n + nodes, device="cuda")
+        at.append(table[b, pos // page].long() * page + pos % page)
+        needle = torch.randint(0, n, (nodes, H * G), generator=g, device="cuda")
+        head = torch.arange(H * G, device="cuda") // G
+        q[b * nodes: (b + 1) * nodes] = 4 * k[at[b][needle], head]
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    kv.attend(0, q, table, _int(lens), _int(range(0, requests * nodes + 1, nodes)), out, None, nodes, lse=lse)
+    kv.sync()
+    for b, n in enumerate(lens):
+        kd, vd = (x[at[b]].double().movedim(0, 1) for x in (k, v))
+        qd = q[b * nodes: (b + 1) * nodes].double().view(nodes, H, G, D).movedim(1, 0).reshape(H, nodes * G, D)
+        s = qd @ kd.mT * D ** -0.5
+        s_abs = qd.abs().amax((1, 2)) * kd.abs().sum(-1).amax(-1) * D ** -0.5
+        hidden = torch.arange(n + nodes, device="cuda")[None, :] > n + torch.arange(nodes, device="cuda").repeat_interleave(G)[:, None]
+        s.masked_fill_(hidden, float("-inf"))
+        want, wl = torch.softmax(s, -1) @ vd, torch.logsumexp(s, -1)
+        got = out[b * nodes: (b + 1) * nodes].double().view(nodes, H, G, D).movedim(1, 0).reshape(H, nodes * G, D)
+        ds = ((D + 8) * 2.0 ** -24 * s_abs + 2.0 ** -20)[:, None]
+        tol = (2 * ds + (n + nodes + 16) * 2.0 ** -24 + 2.0 ** -8) * vd.abs().amax((1, 2))[:, None]
+        assert ((got - want).abs() <= tol[..., None] + 2.0 ** -8 * want.abs()).all(), b
+        gl = lse[b * nodes: (b + 1) * nodes].double().view(nodes, H, G).movedim(1, 0).reshape(H, nodes * G)
+        assert ((gl - wl).abs() <= ds + (n + nodes + 16) * 2.0 ** -24 + 2.0 ** -22 * wl.abs()).all(), b
