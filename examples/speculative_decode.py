@@ -143,6 +143,8 @@ def generate(decoder: Decoder, first, count: int, temperature: float, drafted: b
         noise = torch.empty(B, VOCAB, device="cuda").exponential_().clamp_(min=1e-30)
         ace.ace_verify_tree(logits, tokens, parents, offsets, MAX_NODES, torch.rand(B * n, device="cuda"), noise, path, n_keep, nxt,
                             probs, temps)
+        if short := int(decoder.missing):               # the step's rows had no place (a wait, as for its tokens below)
+            raise RuntimeError(f"the cache's pool is {short} pages short of what the requests need")
         decoder.keep(path, n_keep)
         for b, (p, k, t) in enumerate(zip(path.tolist(), n_keep.tolist(), nxt.tolist())):
             out[b] += [int(tokens[b * n + i]) for i in p[1:k]] + [t]

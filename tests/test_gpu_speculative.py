@@ -46,3 +46,14 @@ def test_sampled_steps_run_and_keep_their_books(example, dtype, fmt):
     assert all(0 <= t < example.VOCAB for o in out for t in o)
     # every produced token but each request's last has its rows in the cache, after the first one's
     assert d.lens.tolist() == [len(o) for o in out]
+
+
+def test_a_pool_that_is_short_of_pages_ends_the_generation(example):
+    """The step that finds too few free pages says how many, before any of its tokens are taken."""
+    torch.manual_seed(4)
+    d = example.Decoder("bf16", "int4")
+    d.refs[5:] = 1                      # 5 pages are free: a tree takes a page of each of the four requests, then the next four are wanted
+    with pytest.raises(RuntimeError, match="3 pages short"):
+        example.generate(d, torch.arange(4, device="cuda"), 40, 0.0, drafted=False)
+    assert d.lens.tolist() == [example.PAGE] * 4
+    assert (d.pages >= 0).sum().item() == 4 and int(d.refs[:5].sum()) == 4
