@@ -642,9 +642,9 @@ ace_status ace_tree_mask_rows(const int32_t* parents, const int32_t* node_offset
  *   T     rows of q and out, node_offsets[B]; max_nodes bounds every n_b. The host does not know the
  *         trees, so max_nodes also chooses the kernel: a bound far above them is right, and slower
  * Softmax and sums are fp32, and out is rounded to dtype. On the tensor cores (bf16, head sizes 64
- * and 128) more is rounded on the way. Over plain and int4 caches: the softmax weights to bf16 (2^-9
- * of a weight; an int4 cache's code * s is exact in bf16, and elements of q 2^-27 and more below their
- * row's largest may lose bits that are 2^-34 of that one). Over fp8 caches: the weights to fp16 (2^-12 of a weight, 2^-25 of the row's largest), q
+ * and 128) more is rounded on the way. Over plain caches: the softmax weights to bf16 (2^-8 of a
+ * weight). Over int4 caches: the weights to two bf16 terms (2^-16 of a weight; code * s is exact in bf16), and elements of q 2^-27 and more
+ * below their row's largest may lose bits that are 2^-34 of that one. Over fp8 caches: the weights to fp16 (2^-11 of a weight, 2^-25 of the row's largest), q
  * to two e4m3 terms (elements 2^-10 and more below its row's largest lose bits that are 2^-18 of
  * that one), and V rows whose scale is 2^-20 or less of the largest that every row of a block sees.
  * The work is split over the long axis by the lengths, in an order that depends on them alone: the

@@ -2,17 +2,20 @@
 // heads a kv head at most 16; bf16 activations, head sizes 64 and 128): bound by the cache's bytes, 72 a row of 128.
 //   S^T = K Q^T       16 positions x 8 rows a product (m16n8k16); codes are exact in fp16, q too once its row is scaled by a power
 //                     of two, so a group's product is exact but for fp32's sums, and its scale is one factor of 16 x 8 sums
-//   P^T = 2^(S^T - ref)   bf16
-//   O^T += V^T P^T    V's code * scale is exact in bf16 (3 significant bits times 4)
+//   P^T = 2^(S^T - ref)   two bf16 terms (2^-16 of a weight)
+//   O^T += V^T P^T    V's code * scale is exact in bf16 (3 significant bits times 4), whose range spares it a unit; so weights have to be
+//                     bf16 as well, and one term (2^-8 of a weight) would be what the output loses most by: 0.0023 of its size against
+//                     64 bits, of which the output's own rounding is 0.0017. The second term's products take 3 us of 60 at 8 rows, 8 of 90
+//                     at 16.
 // At 4 bits a tile of 128 positions is 18 KB and takes HBM 850 cycles of an SM (copy rate), in which its 32768 codes have to become operands: too
 // little time for the hand-overs of tcgen05 (scores, softmax, weights and conversion through shared and tensor memory take 2000
 // cycles a tile in ace_attn_few.cu, fp8 codes without any conversion). So the codes become operands in the registers of the warp
 // that multiplies them (mma.sync; about one operation a code), S^T turns into the second product's operand by movmatrix, and the
 // warps of a CTA walk their positions of each tile on their own, with their own running maxima, from rings of cp.async stages; they
 // meet at a unit's end only.
-// Measured (64 users of up to 8192 positions, 322,000 in all, 4 kv heads of 128): 8 rows a unit 57 us (3.3 TB/s, 0.49 of the copy rate;
-// ace_attn_few.cu over an fp8 cache 73), 16 rows 81. With 8 times the positions 5.1 TB/s: the rest is starts and ends of units and the
-// joining kernel. 16 warps an SM issue 0.55 to 0.60 a cycle and scheduler, with no pipe above 45%: bound by the warps' dependent
+// Measured (64 users of up to 8192 positions, 322,000 in all, 4 kv heads of 128): 8 rows a unit 60 us (3.1 TB/s, 0.45 of the copy rate;
+// ace_attn_few.cu over an fp8 cache 73), 16 rows 90. With 8 times the positions 4.6 TB/s: the rest is starts and ends of units and the
+// joining kernel. They issue 0.54 and 0.47 a cycle and scheduler, with no pipe above 41%: bound by the warps' dependent
 // chains (12 warps of 168 registers had the same rate a position).
 #include <cfloat>
 #include <type_traits>
@@ -119,24 +122,30 @@ __device__ __forceinline__ int chunk_at(int r, int c) {
     }
 }
 
-// O += V^T P^T of a run: the lane's dimensions PER g .. of positions t, t + 4, t + 8, t + 12, whose codes are w.
+// O += V^T P^T of a run: the lane's dimensions PER g .. of positions t, t + 4, t + 8, t + 12, whose codes are w; p and z are the weights'
+// upper and lower terms.
 template <int D, int NT, bool LARGE>
-__device__ __forceinline__ void add_values(const uint32_t (&w)[4][D / 64], const Scales (&k)[2], const uint32_t (&p)[NT][2], float (&o)[D / 16][NT][4]) {
+__device__ __forceinline__ void add_values(const uint32_t (&w)[4][D / 64], const Scales (&k)[2], const uint32_t (&p)[NT][2], const uint32_t (&z)[NT][2], float (&o)[D / 16][NT][4]) {
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const uint32_t sel = half ? 0x7632u : 0x5410u;
             const uint32_t x0 = __byte_perm(w[0][i], w[1][i], sel), x1 = __byte_perm(w[2][i], w[3][i], sel);
-            uint32_t a[4];
-            bf16_of_codes<0, LARGE>(x0, k[0], a[0], a[1]);
-            bf16_of_codes<0, LARGE>(x1, k[1], a[2], a[3]);
+            uint32_t a[2][4];
+            bf16_of_codes<0, LARGE>(x0, k[0], a[0][0], a[0][1]);
+            bf16_of_codes<0, LARGE>(x1, k[1], a[0][2], a[0][3]);
+            bf16_of_codes<2, LARGE>(x0, k[0], a[1][0], a[1][1]);
+            bf16_of_codes<2, LARGE>(x1, k[1], a[1][2], a[1][3]);
+            // two tiles' products in turn, as those of one add to the same sums (one tile after the other: 59.4 for 57.4 us in a row of calls)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16(o[4 * i + 2 * half][n], a, p[n][0], p[n][1]);
-            bf16_of_codes<2, LARGE>(x0, k[0], a[0], a[1]);
-            bf16_of_codes<2, LARGE>(x1, k[1], a[2], a[3]);
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16(o[4 * i + 2 * half + 1][n], a, p[n][0], p[n][1]);
+                for (int n = 0; n < NT; ++n) mma_bf16(o[4 * i + 2 * half + j][n], a[j], p[n][0], p[n][1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma_bf16(o[4 * i + 2 * half + j][n], a[j], z[n][0], z[n][1]);
         }
     }
 }
@@ -514,7 +523,7 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
             auto finish = [&](auto is_large) {
 #pragma unroll
                 for (int u = 0; u < kSub; ++u) {
-                    uint32_t p[NT][2], w[4][D / 64];
+                    uint32_t p[NT][2], lower[NT][2], w[4][D / 64];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const unsigned char* from = at + u * C::SUB + (i & 1 ? v_at[1] : v_at[0]) + i * 4 * C::ROW;
@@ -532,11 +541,13 @@ __global__ void __launch_bounds__(Q4<D, NT>::THREADS, Q4<D, NT>::CTAS) k_attn_q4
                         for (int i = 0; i < 4; ++i) e[i] = exp2_approx(x[u][n][i] - ref[n][i & 1]);
                         l[n][0] += e[0] + e[2];
                         l[n][1] += e[1] + e[3];
-                        const __nv_bfloat162 y = __floats2bfloat162_rn(e[0], e[1]), z = __floats2bfloat162_rn(e[2], e[3]);
-                        p[n][0] = transposed(*reinterpret_cast<const uint32_t*>(&y));
-                        p[n][1] = transposed(*reinterpret_cast<const uint32_t*>(&z));
+                        uint32_t up[2], low[2];
+                        two_terms(e[0], e[1], up[0], low[0]);
+                        two_terms(e[2], e[3], up[1], low[1]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) p[n][i] = transposed(up[i]), lower[n][i] = transposed(low[i]);
                     }
-                    add_values<D, NT, decltype(is_large)::value>(w, k[u], p, o);
+                    add_values<D, NT, decltype(is_large)::value>(w, k[u], p, lower, o);
                 }
             };
             if (__builtin_expect(any_large, 0)) finish(std::true_type{});

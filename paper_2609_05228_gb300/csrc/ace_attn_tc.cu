@@ -19,10 +19,12 @@
 // of 2^eref, a power of two above the scales so far (ace_attn_tc.cuh: Reference): exact but for rows whose scale is 2^-20 of the
 // largest and less, whose codes' last bits fall under fp16's least.
 // 4-bit caches: K's and V's codes times their scales, which bf16 holds exactly, are written as the tiles of a plain cache by two
-// groups of four warps (Codes4), in place of TMA. 64 users as below: 33 to 64 rows a unit 126 to 128 us, 128 rows 139, 192 rows 191
-// (plain 126 to 128, 134, 162): with few rows V's conversion bounds it (2400 of 3250 cycles a tile), with many the softmax; 8 users'
-// 128 nodes of 64 heads 342 us.
-// P is rounded to bf16 (2^-9 of a weight; plain caches) or fp16 (2^-12), as the products need; sums, maxima and O are fp32.
+// groups of four warps (Codes4), in place of TMA. 64 users as below: 33 to 64 rows a unit 130 to 133 us, 128 rows 152, 192 rows 218
+// (plain 126 to 128, 134, 162): with few rows V's conversion bounds it (2400 of a tile's cycles, which were 3250 with one term of the
+// weights), with many the softmax.
+// P is rounded to what V's type asks for: bf16 (2^-8 of a weight; plain caches), fp16 (2^-11; fp8 caches) or two bf16 terms (2^-16; 4-bit
+// caches: as in ace_attn_q4.cu, the upper and lower ones beside each other in the scores' place, a product more; one term took 125 to 128,
+// 138 and 191 us, and 8 users' 128 nodes of 64 heads 349 for 392). Sums, maxima and O are fp32.
 // Measured: 8 users of up to 16384 positions, 128 nodes of 64 heads (8 kv heads of 128), bf16: 304 us, 850 TFLOP/s. 64 users
 // of up to 8192, 4 kv heads of 128: 64 rows a unit 114 us fp8, 128 bf16; 128 rows 139 and 135; 192 rows 213 and 162. Bound by
 // the chain scores, softmax, product of two groups that share one tensor pipe (an item's products alone take 625 cycles:
@@ -116,12 +118,12 @@ __device__ __forceinline__ float max32(const float* x) {
     return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
 
-// 32 weights 2^(x f + shift) to TMEM; returns their sum.
-template <bool FP8>
+// 32 weights 2^(x f + shift) to TMEM (I4: lower terms 32 columns behind the upper ones); returns their sum.
+template <bool FP8, bool I4>
 __device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, float f, float shift) {
     const uint64_t f2 = pair(f, f), shift2 = pair(shift, shift);
     uint64_t sum[2] = {0ull, 0ull};
-    uint32_t w[16];
+    uint32_t w[16], z[I4 ? 16 : 1];
 #pragma unroll
     for (int i = 0; i < 32; i += 4) {
         float e[4];
@@ -135,6 +137,9 @@ __device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, flo
             const __half2 p0 = __floats2half2_rn(e[0], e[1]), p1 = __floats2half2_rn(e[2], e[3]);
             w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
             w[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&p1);
+        } else if constexpr (I4) {
+            two_terms(e[0], e[1], w[i / 2], z[i / 2]);
+            two_terms(e[2], e[3], w[i / 2 + 1], z[i / 2 + 1]);
         } else {
             const __nv_bfloat162 p0 = __floats2bfloat162_rn(e[0], e[1]), p1 = __floats2bfloat162_rn(e[2], e[3]);
             w[i / 2] = *reinterpret_cast<const uint32_t*>(&p0);
@@ -142,6 +147,7 @@ __device__ __forceinline__ float store_weights(uint32_t p_t, const float* x, flo
         }
     }
     tmem_st16(p_t, w);
+    if constexpr (I4) tmem_st16(p_t + 32, z);
     float a, b, c, d;
     unpair(sum[0], a, b);
     unpair(sum[1], c, d);
@@ -267,7 +273,7 @@ struct RowState {
 
 // One item of a row: N scores from column `col` on become weights, over the scores that are read already; the row's other
 // columns of P (of the item's kHalf) are zero.
-template <bool FP8, int N>
+template <bool FP8, bool I4, int N>
 __device__ __forceinline__ void softmax_item(const AttnArgs& a, const Segment& s, uint32_t s_t, int col, const float4* kf, bool drafted,
                                              int node, int pos0, float f_row, bool first, RowState& st) {
     float x[N];
@@ -300,10 +306,11 @@ __device__ __forceinline__ void softmax_item(const AttnArgs& a, const Segment& s
         for (int i = 0; i < N; ++i) x[i] *= before;
     }
 #pragma unroll
-    for (int c = 0; c < N; c += 32) st.l += store_weights<FP8>(s_t + (col + c) / 2, x + c, f, shift);
+    for (int c = 0; c < N; c += 32) st.l += store_weights<FP8, I4>(s_t + (col + c) / 2, x + c, f, shift);
     if constexpr (N < kHalf) {
         const uint32_t zero[16] = {};
         tmem_st16(s_t + 16 - col / 2, zero);
+        if constexpr (I4) tmem_st16(s_t + 48 - col / 2, zero);
     }
     tmem_st_wait();
 }
@@ -321,7 +328,7 @@ __device__ __forceinline__ uint32_t f16x2_scaled(uint32_t codes, __half2 f) {
 }
 
 // MMA issuers, a warp a softmax group g.
-template <bool FP8, int D, int RT, int CP>
+template <bool FP8, bool I4, int D, int RT, int CP>
 __device__ __forceinline__ void role_issue(Misc<FP8, RT>& m, const AttnArgs& a, unsigned char* smem, uint32_t tmem, int g) {
     using C = Cfg<FP8, D, RT, CP>;
     constexpr int NK = C::NK, NV = C::NV, NC = C::NC;
@@ -386,6 +393,11 @@ __device__ __forceinline__ void role_issue(Misc<FP8, RT>& m, const AttnArgs& a, 
 #pragma unroll
                     for (int kk = 0; kk < kHalf / 16; ++kk)
                         mma_ts(o, pa + 8 * kk, vl + 128 * kk, kRows128, idesc_of(FP8 ? 0 : 1, 128, D, true), j > 0 || kk > 0);
+                    if constexpr (I4) {                     // the weights' lower terms
+#pragma unroll
+                        for (int kk = 0; kk < kHalf / 16; ++kk)
+                            mma_ts(o, pa + 32 + 8 * kk, vl + 128 * kk, kRows128, idesc_of(1, 128, D, true), true);
+                    }
                     mma_commit(&m.o_done[buf]);
                     if (j % RT == RT - 1) {
                         mma_commit(&v_free[rv.i]);
@@ -458,7 +470,7 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
         if constexpr (I4) {             // (one register hand-over for the group's roles)
             fewer_registers<64>();
             if (warp == 0) role_schedule<ROWS, kTcStart>(m, a);
-            else if (warp != 2) role_issue<FP8, D, RT, CP>(m, a, smem, tmem, warp >> 1);
+            else if (warp != 2) role_issue<FP8, I4, D, RT, CP>(m, a, smem, tmem, warp >> 1);
         }
     } else if (!I4 && warp == 0) {
         Scheduler<ROWS, kTcStart> sched(m, a);                    // a segment ahead of the loads
@@ -466,7 +478,7 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
     } else if (!I4 && warp == 2) {
         if constexpr (FP8) role_scales<kTcRoom>(m, a, m.kf, m.vf);
     } else if (!I4 && (warp == 1 || warp == 3)) {
-        if constexpr (!I4) role_issue<FP8, D, RT, CP>(m, a, smem, tmem, warp >> 1);
+        if constexpr (!I4) role_issue<FP8, I4, D, RT, CP>(m, a, smem, tmem, warp >> 1);
     } else if (warp >= 12) {
         // ------------------------------------------------ q rows, and V tiles made ready; 4 bits: tiles of K, and of V by warps 16 to 19
         if constexpr (I4) fewer_registers<80>();
@@ -679,7 +691,7 @@ __global__ void __launch_bounds__(tc_threads(I4), 1) k_attn_tc(const __grid_cons
                         if (i > 0 && e > eref) st.o_mul = e - eref > 126 ? 0.f : pow2_of_byte(127 - (e - eref));
                         eref = e;
                     }
-                    softmax_item<FP8, kHalf / CP>(a, s, s_t + buf * kHalf, col, kf, drafted, node, pos0, f_row, i == 0, st);
+                    softmax_item<FP8, I4, kHalf / CP>(a, s, s_t + buf * kHalf, col, kf, drafted, node, pos0, f_row, i == 0, st);
                 }
                 if (FP8 && tile_last) {
                     __syncwarp();

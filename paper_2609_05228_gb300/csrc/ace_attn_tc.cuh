@@ -157,6 +157,16 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     return r;
 }
 
+// Two weights (>= 0, or NaN) as two bf16 terms each: their upper 16 bits, and what is left of them, rounded: 2^-17 of a weight at most.
+__device__ __forceinline__ void two_terms(float a, float b, uint32_t& upper, uint32_t& lower) {
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    upper = __byte_perm(x, y, 0x7632);
+    float c, d;
+    unpair(add2(pair(a, b), pair(__uint_as_float(x & 0xffff0000u | 0x80000000u), __uint_as_float(y & 0xffff0000u | 0x80000000u))), c, d);
+    const __nv_bfloat162 z = __floats2bfloat162_rn(c, d);
+    lower = *reinterpret_cast<const uint32_t*>(&z);
+}
+
 // Which of the 32 keys from position `pos` on row `node` sees: the prefix, and the nodes of its mask.
 __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, const Segment& s, int node, int pos) {
     const int m0 = pos - s.len;         // first node

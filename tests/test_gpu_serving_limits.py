@@ -112,3 +112,39 @@ def test_int4_attention_walks_of_many_batches_of_pages(nodes, G, requests, lengt
         assert ((got - want).abs() <= tol[..., None] + 2.0 ** -8 * want.abs()).all(), b
         gl = lse[b * nodes: (b + 1) * nodes].double().view(nodes, H, G).movedim(1, 0).reshape(H, nodes * G)
         assert ((gl - wl).abs() <= ds + (n + nodes + 16) * 2.0 ** -24 + 2.0 ** -22 * wl.abs()).all(), b
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nodes,G", [(1, 8), (2, 8), (3, 8), (5, 8), (8, 8), (16, 8), (24, 8), (256, 2)])
+def test_int4_attention_weights_keep_their_bits(nodes, G, D):
+    """V of 7 and -7 in turn: outputs are differences of weights, so what a weight loses shows as it is. A score has one product that is
+    not zero. Bounds: that product and the softmax's scale and shift, exp2 (4 * 2^-24 of a score, 2^-21); sums of weights; weights to two
+    bf16 terms (2^-16); the output, 2^-8 of it."""
+    rng = np.random.default_rng(nodes + D)
+    H, page, lens = 2, 16, [1, 2, 3, 10, 60, 300, 0, 1]
+    B, need = len(lens), -(-(max(lens) + nodes) // page)
+    kv = ace.AceKvCache(H, D, page, B * need, 1, "bf16", "int4")
+    table = rng.permutation(B * need).reshape(B, need).astype(np.int32)
+    q = np.zeros((B, nodes, H * G, D))
+    q[..., 5] = rng.choice([-1, 1], (B, nodes, H * G)) * rng.integers(32, 256, (B, nodes, H * G)) / 128
+    k, v = np.zeros((B, max(lens) + nodes, H, D)), np.zeros((B, max(lens) + nodes, H, D))
+    k[..., 5], k[..., 7] = rng.integers(-7, 8, k.shape[:-1]) / 8, 7 / 8
+    v[:] = 7 * (1 - 2 * (np.arange(v.shape[1]) % 2))[None, :, None, None]
+    for b, n in enumerate(lens):
+        pos = np.arange(n + nodes)
+        slots = torch.from_numpy(table[b, pos // page].astype(np.int64) * page + pos % page).cuda()
+        kv.write(0, *(torch.from_numpy(x[b, : n + nodes]).bfloat16().cuda() for x in (k, v)), slots)
+    qt = torch.from_numpy(q).bfloat16().cuda().view(B * nodes, H * G, D)
+    out, scale = torch.empty_like(qt), 0.7
+    kv.attend(0, qt, _int(table), _int(lens), _int(range(0, B * nodes + 1, nodes)), out, None, nodes, scale)
+    kv.sync()
+    got = out.double().cpu().numpy().reshape(B, nodes, H * G, D)
+    for b, n in enumerate(lens):
+        kk = np.repeat(k[b, : n + nodes, :, 5], G, 1)
+        s = q[b, :, :, 5][:, None, :] * kk[None] * scale                   # [node, position, head]
+        s[np.arange(n + nodes)[None, :] > n + np.arange(nodes)[:, None]] = -np.inf
+        p = np.exp(s - s.max(1, keepdims=True))
+        want = np.einsum("nlh,l->nh", p, v[b, : n + nodes, 0, 0]) / p.sum(1)
+        ds = 4 * 2.0 ** -24 * np.abs(np.where(np.isfinite(s), s, 0)).max() + 2.0 ** -21
+        tol = 7 * (2 * ds + (n + nodes + 16) * 2.0 ** -24 + 2.0 ** -16) + 2.0 ** -8 * np.abs(want)
+        assert (np.abs(got[b] - want[..., None]) <= tol[..., None]).all(), (b, (np.abs(got[b] - want[..., None]) / tol[..., None]).max())
