@@ -522,7 +522,7 @@ ace_status ace_kv_keep(ace_kv* kv, const int32_t* page_table, int max_pages, con
  *
  * ace_kv_copy_pages - page src[i] to page dst[i] in all layers, rows and scales as they are, i < n. Entries that name a page
  * outside the pool, a dst that another entry names too, or one that is another's src, are left out and reported; src[i] = dst[i]
- * is nothing to do. Counts and tables are the caller's.
+ * is nothing to do (such entries, and those outside the pool, are no others to these rules). Counts and tables are the caller's.
  */
 ace_status ace_kv_fork(ace_kv* kv, const int32_t* page_table, const int32_t* lens, int B, const int32_t* parents, int B_out,
                        int max_pages, int32_t* refs, int32_t* new_table, int32_t* new_lens, void* stream);

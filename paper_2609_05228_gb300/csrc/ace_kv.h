@@ -131,9 +131,8 @@ cudaError_t launch_tree_attention_tc(const ace_kv* kv, const AttnArgs& a, cudaSt
 constexpr int kFewRows = 32;
 cudaError_t attn_few_init(const ace_kv* kv);
 cudaError_t launch_attn_few(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);
-// caches in 4 bits (ace_attn_q4.cu): two CTAs an SM. With 32 rows a warp it has no registers left for the chains to overlap: 24 and 32
-// rows of 64 users 143 and 150 us, in the kernel above 140 and 141 (at most 512 positions 41 and 45, there 37 and 39), which has since
-// come to 115 for both
+// caches in 4 bits (ace_attn_q4.cu): two CTAs an SM, up to 16 rows a unit 60 to 90 us for 64 users where the tcgen05 kernel (ace_attn_tc.cu)
+// takes 119 for any up to 32. With 32 rows a warp it would have no registers left for the chains to overlap.
 constexpr int kFewRows4 = 16;
 cudaError_t attn_q4_init(const ace_kv* kv);
 cudaError_t launch_attn_q4(const ace_kv* kv, const AttnArgs& a, cudaStream_t s);

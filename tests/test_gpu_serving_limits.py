@@ -148,3 +148,23 @@ def test_int4_attention_weights_keep_their_bits(nodes, G, D):
         ds = 4 * 2.0 ** -24 * np.abs(np.where(np.isfinite(s), s, 0)).max() + 2.0 ** -21
         tol = 7 * (2 * ds + (n + nodes + 16) * 2.0 ** -24 + 2.0 ** -16) + 2.0 ** -8 * np.abs(want)
         assert (np.abs(got[b] - want[..., None]) <= tol[..., None]).all(), (b, (np.abs(got[b] - want[..., None]) / tol[..., None]).max())
+
+
+def test_copies_beside_entries_that_do_nothing():
+    """Entries with their page as their own source, or outside the pool, are no others to a copy; two that differ for one page are."""
+    kv = ace.AceKvCache(2, 64, 16, 8, 2, "bf16", "int4")
+    pools = [p.view(torch.uint8) for p in (kv.k_pool, kv.v_pool, kv.k_scale, kv.v_scale)]
+    for i, p in enumerate(pools):
+        p.copy_(torch.randint(0, 256, tuple(p.shape), generator=torch.Generator().manual_seed(i), dtype=torch.uint8))
+    before = [p.clone() for p in pools]
+    kv.copy_pages(_int([1, 2, 0, 0]), _int([1, 1, 3, 4]))           # 2 -> 1 beside 1 -> 1; one source twice
+    kv.sync()
+    kv.copy_pages(_int([9, 7, 6, 5]), _int([5, 5, 7, -1]))          # outside; 7 -> 5 and 6 -> 7: page 7 is a source
+    with pytest.raises(ace.AceError) as err:
+        kv.sync()
+    assert err.value.status == 1
+    for p, old in zip(pools, before):
+        want = old.clone()
+        for s, d in ((2, 1), (0, 3), (0, 4), (7, 5)):
+            want[:, d] = old[:, s]
+        assert torch.equal(p, want)
