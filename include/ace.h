@@ -415,7 +415,9 @@ ace_status ace_layer_get_desc(const ace_layer* layer, ace_layer_desc* desc);
  * rounded to nearest even, -7 .. 7, and stands for code * s, which bf16 holds
  * exactly. It is kept as code + 8 in 4 bits, two a byte, the even element in the
  * lower half. A group with a NaN or an infinity has the scale NaN: all of it
- * stands for NaN. A row of 128 takes 72 bytes (fp8: 129, bf16: 256).
+ * stands for NaN. A row of 128 takes 72 bytes (fp8: 129, bf16: 256). That is its gain: attention over it takes 0.7 of fp8's time with up
+ * to 8 query rows a unit (nodes times query heads a kv head), about as long with 9 to 32 and from 65 on, 1.1 to 1.2 times as long with 33 to
+ * 64, and than over plain rows 0.5 to 1.0 times as long up to 128 rows, 1.2 to 1.3 beyond (bf16, heads of 128, many long requests).
  */
 typedef enum ace_kv_format { ACE_KV_PLAIN = 0, ACE_KV_FP8 = 1, ACE_KV_INT4 = 4 } ace_kv_format;
 

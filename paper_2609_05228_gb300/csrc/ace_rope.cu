@@ -10,8 +10,8 @@
 // cosines once. They come from a table of the block's tokens in shared memory, made while the rows are under way. In layout
 // "half" a pair's partner comes by shuffles where a row is a whole number of lanes' shares, from memory elsewhere. Bound by memory:
 // 16384 tokens of 72 heads of 128, half of each turned, 100 us for 604 MB, 6.0 TB/s. With a look at the table a row,
-// and blocks that mixed rows of q, k and v, it took 115. Rows of 8192 tokens (32 heads, 8 kv heads) into a 4-bit cache 54 us, by issue
-// slots, fp8 46, plain 44 (layout "half" 62, 52, 50).
+// and blocks that mixed rows of q, k and v, it took 115. Rows of 8192 tokens (32 heads, 8 kv heads) into a 4-bit cache 52 us, by issue
+// slots, fp8 46, plain 44 (all of each head in layout "half" 60, 52, 50).
 #include <math.h>
 
 #include <initializer_list>
